@@ -171,6 +171,7 @@ RESIDUAL_SCALE, BRANCH_SCALE = 1.0, 0.7
 def _own(s):
     from paper_2608_14385_b200 import binding
     c, op = s["case"], s["case"]["op"]
+    kind = {"channel": binding.GATE_CHANNEL, "token": binding.GATE_TOKEN, "full": binding.GATE_FULL}.get(c.get("gate"))
     if op == "tokens":
         off, pair_row, row_pair = binding.sort_pairs(s["idx"], c["experts"])
         rows = binding.dispatch(s["x"], pair_row, rows=s["rows"])
@@ -181,12 +182,12 @@ def _own(s):
     if op == "norms":
         h = binding.norm(s["x"], s["w_pre"], EPS)
         out, u = binding.norm_residual(s["x"], s["y"], s["w_post"], EPS, gate=s["gate"], residual_scale=RESIDUAL_SCALE,
-                                       branch_scale=BRANCH_SCALE, next_weight=s["w_next"])
+                                       branch_scale=BRANCH_SCALE, next_weight=s["w_next"], gate_kind=kind)
         return h, out, u
     if op == "norms_backward":
         dx, dy, dgate, dw, dnext = binding.norm_residual_backward(
             s["x"], s["y"], s["w_post"], EPS, s["dout"], gate=s["gate"], residual_scale=RESIDUAL_SCALE,
-            branch_scale=BRANCH_SCALE, next_weight=s["w_next"], du=s["du"])
+            branch_scale=BRANCH_SCALE, next_weight=s["w_next"], du=s["du"], gate_kind=kind)
         dx_pre, dpre = binding.norm_backward(s["x"], s["w_pre"], EPS, s["dh"], dadd=s["dout"])
         return [dx, dy, dw, dnext, dx_pre, dpre] + ([] if dgate is None else [dgate])
     return binding.quant_product(s["codes"], s["scales"], s["x"], c["group"], zeros=s["zeros"],
