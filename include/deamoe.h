@@ -304,6 +304,143 @@ deamoe_status_t deamoe_route_static(void *cuda_stream, const float *router, cons
                                     int32_t norm_topk, float route_scale, int32_t B, int32_t *topk_idx,
                                     float *topk_w);
 
+/* ------------------------------------------------------------------------------------------------
+ * Operators around a layer.  (The paper has no counterpart: they are what a model puts next to an MoE
+ * layer -- its token order, its norms, experts of another kind.)
+ *
+ * They need no layer object and keep nothing between calls.  All of them only ENQUEUE on the stream; none
+ * allocates or synchronises, and a call may be captured into a CUDA graph.  Scratch is the caller's: a
+ * workspace of the size the matching *_workspace function gives (0: may be NULL), which must not be used by
+ * two calls that can overlap on the GPU; its contents need no preparation and mean nothing afterwards.
+ * Pointers are DEVICE pointers of the current device, 4-byte aligned for int32 and fp32 arrays and aligned
+ * to their value for the others (rows that start on 16-byte boundaries are read 16 bytes at a time, any
+ * others value by value).  Matrices are row-major with a row stride in VALUES (>= the row's length), so a
+ * column range of a wider matrix is a valid operand.  Outputs must not overlap inputs except where it is
+ * said.  Sums, statistics and products are fp32; every output is rounded once.  Equal calls give equal
+ * bits: no kernel here adds in an order that depends on timing.  n_token == 0 is valid everywhere.
+ * Sizes: hidden <= DEAMOE_MAX_WIDTH, top_k <= DEAMOE_MAX_TOPK, n_expert <= DEAMOE_MAX_EXPERTS (else
+ * UNSUPPORTED); n_token * top_k < 2^31 (else BATCH).
+ */
+#define DEAMOE_MAX_WIDTH (1 << 20)
+
+/*
+ * Tokens sorted by expert and back.
+ *
+ * Pair p = t * top_k + q is slot q of token t.  deamoe_sort_pairs puts the pairs into expert order, pairs of
+ * one expert in the order of p:
+ *   topk_idx   [n_token, top_k]  experts, as deamoe_route gives them; an entry outside [0, n_expert) drops its
+ *              pair (an expert of another GPU, padding).  A token may name an expert twice.
+ *   expert_off [n_expert + 1]  out: expert e owns rows expert_off[e] .. expert_off[e + 1] - 1
+ *   pair_row   [n_token, top_k]  out: the pair's row, or -1 if it was dropped
+ *   row_pair   [n_token * top_k]  out: the row's pair; -1 for rows behind expert_off[n_expert]
+ * The other calls take pair_row and move rows of `hidden` values (dtype: deamoe_dtype_t) between [n_token,
+ * hidden] and the n_rows rows in expert order:
+ *   deamoe_dispatch           rows[pair_row[t, q]] = x[t]
+ *   deamoe_dispatch_backward  dx[t] = sum_q drows[pair_row[t, q]]
+ *   deamoe_combine            out[t] = sum_q topk_w[t, q] rows[pair_row[t, q]]           (Eq. (3))
+ *   deamoe_combine_backward   drows[pair_row[t, q]] = topk_w[t, q] dout[t],  dw[t, q] = <dout[t], rows[pair_row[t, q]]>
+ *                             (drows or dw may be NULL, not both; with dw NULL rows may be NULL)
+ * Sums run over q in order.  Dropped pairs contribute nothing, their weights are not looked at and their dw is 0; a
+ * token whose pairs are all dropped gets zeros.  A row index outside [0, n_rows) is treated as dropped.  Rows
+ * that no pair points to are left as they were.  pair_row must not name a row twice.
+ */
+uint64_t deamoe_sort_workspace(int32_t n_token, int32_t top_k, int32_t n_expert);
+deamoe_status_t deamoe_sort_pairs(void *cuda_stream, const int32_t *topk_idx, int32_t n_token, int32_t top_k,
+                                  int32_t n_expert, int32_t *expert_off, int32_t *pair_row, int32_t *row_pair,
+                                  void *workspace, uint64_t workspace_bytes);
+deamoe_status_t deamoe_dispatch(void *cuda_stream, int32_t dtype, const void *x, int64_t x_stride,
+                                const int32_t *pair_row, int32_t n_token, int32_t top_k, int32_t hidden, void *rows,
+                                int64_t rows_stride, int64_t n_rows);
+deamoe_status_t deamoe_dispatch_backward(void *cuda_stream, int32_t dtype, const void *drows, int64_t drows_stride,
+                                         int64_t n_rows, const int32_t *pair_row, int32_t n_token, int32_t top_k,
+                                         int32_t hidden, void *dx, int64_t dx_stride);
+deamoe_status_t deamoe_combine(void *cuda_stream, int32_t dtype, const void *rows, int64_t rows_stride, int64_t n_rows,
+                               const int32_t *pair_row, const float *topk_w, int32_t n_token, int32_t top_k,
+                               int32_t hidden, void *out, int64_t out_stride);
+deamoe_status_t deamoe_combine_backward(void *cuda_stream, int32_t dtype, const void *dout, int64_t dout_stride,
+                                        const void *rows, int64_t rows_stride, int64_t n_rows, const int32_t *pair_row,
+                                        const float *topk_w, int32_t n_token, int32_t top_k, int32_t hidden,
+                                        void *drows, int64_t drows_stride, float *dw);
+
+/*
+ * The norms of a block.  With rms(v) = sqrt(mean(v^2) + eps) over a row of `hidden` values:
+ *
+ *   deamoe_norm            out = x / rms(x) * weight                    (the layer's input; out may be x itself)
+ *   deamoe_norm_residual   s = residual_scale * x + branch_scale * gate * (y / rms(y) * weight)
+ *                          out = s rounded to dtype;   next = s / rms'(s) * next_weight, from the unrounded s
+ *
+ * y is what the block made of the normed x.  normalise = 0 leaves y as it is (weight must be NULL); next = NULL
+ * leaves the second output away (next_eps is the epsilon of rms').  weight / next_weight: [hidden] in
+ * weight_dtype, NULL = ones.  gate (dtype values): none, one per channel [hidden], one per token [n_token], or
+ * [n_token, hidden] with a row stride.  out may be x itself (same stride: the residual stream in place).
+ *
+ * The backward calls take the forward call's inputs and the gradients of its outputs:
+ *   deamoe_norm_backward            du -> dx (+ dadd, the gradient that reaches x by the residual path, or NULL; dx may
+ *                                   be dadd itself), dweight [hidden] fp32
+ *   deamoe_norm_residual_backward   dout, dnext (NULL if next was) -> dx, dy, and: dweight, dnext_weight [hidden] fp32,
+ *                                   given exactly if the weight is; dgate, given exactly if there is a gate: fp32
+ *                                   [hidden] or [n_token], or dtype [n_token, hidden]
+ * dweight of deamoe_norm_backward is always wanted, also for weight = NULL (the gradient of a gain of ones).
+ */
+typedef enum {
+  DEAMOE_GATE_NONE = 0,
+  DEAMOE_GATE_CHANNEL = 1,
+  DEAMOE_GATE_TOKEN = 2,
+  DEAMOE_GATE_FULL = 3
+} deamoe_gate_t;
+
+uint64_t deamoe_norm_workspace(int32_t n_token, int32_t hidden); /* of the two backward calls */
+deamoe_status_t deamoe_norm(void *cuda_stream, int32_t dtype, const void *x, int64_t x_stride, int32_t n_token,
+                            int32_t hidden, int32_t weight_dtype, const void *weight, float eps, void *out,
+                            int64_t out_stride);
+deamoe_status_t deamoe_norm_backward(void *cuda_stream, int32_t dtype, const void *x, int64_t x_stride, int32_t n_token,
+                                     int32_t hidden, int32_t weight_dtype, const void *weight, float eps, const void *du,
+                                     int64_t du_stride, const void *dadd, int64_t dadd_stride, void *dx,
+                                     int64_t dx_stride, float *dweight, void *workspace, uint64_t workspace_bytes);
+deamoe_status_t deamoe_norm_residual(void *cuda_stream, int32_t dtype, const void *x, int64_t x_stride, const void *y,
+                                     int64_t y_stride, int32_t n_token, int32_t hidden, int32_t normalise,
+                                     int32_t weight_dtype, const void *weight, float eps, int32_t gate_kind,
+                                     const void *gate, int64_t gate_stride, float residual_scale, float branch_scale,
+                                     void *out, int64_t out_stride, const void *next_weight, float next_eps, void *next,
+                                     int64_t next_stride);
+deamoe_status_t deamoe_norm_residual_backward(
+    void *cuda_stream, int32_t dtype, const void *x, int64_t x_stride, const void *y, int64_t y_stride, int32_t n_token,
+    int32_t hidden, int32_t normalise, int32_t weight_dtype, const void *weight, float eps, int32_t gate_kind,
+    const void *gate, int64_t gate_stride, float residual_scale, float branch_scale, const void *dout,
+    int64_t dout_stride, const void *next_weight, float next_eps, const void *dnext, int64_t dnext_stride, void *dx,
+    int64_t dx_stride, void *dy, int64_t dy_stride, void *dgate, int64_t dgate_stride, float *dweight,
+    float *dnext_weight, void *workspace, uint64_t workspace_bytes);
+
+/*
+ * Products with 4-bit matrices, for decode steps: out[r] = W[e(r)] x[src(r)].
+ *
+ *   W[e, i, c] = scales[e, i, c / group] * (code[e, i, c] - zeros[e, i, c / group])
+ *
+ *   codes      [n_expert, n_out, n_in / 2] bytes: columns 2b (low four bits) and 2b + 1 (high) of a row
+ *   scales     [n_expert, n_out, ceil(n_in / group)] in scale_dtype (DEAMOE_F32 or DEAMOE_BF16)
+ *   zeros      the same shape, one byte each, 0..15 (the low four bits count); NULL = 8 everywhere
+ *   x          [n_token, n_in] in dtype
+ *   expert_off [n_expert + 1], row_pair [n_rows]: as deamoe_sort_pairs gives them.  Row r belongs to the expert
+ *              whose range holds it and reads x row row_pair[r] / pairs_per_token.  expert_off may be NULL for
+ *              one matrix (n_expert 1: every row is its); row_pair may be NULL: src(r) = r (rows already in expert
+ *              order, as a second product's input is).  A row whose source lies outside x gets the product with 0.
+ *   swiglu     1: rows [0, n_out / 2) of a matrix are the gate, the others the up projection, and
+ *              out[r, i] = SiLU(W x)[i] * (W x)[n_out / 2 + i]  (Eq. (1); out has n_out / 2 columns)
+ *   out        [n_rows, n_out or n_out / 2] in dtype; rows behind expert_off[n_expert] are left as they were
+ *
+ * group: 32, 64 or 128; n_in a multiple of 32 (the last group may be short); n_out even with swiglu; codes 16-byte
+ * aligned; n_in <= DEAMOE_MAX_WIDTH (else UNSUPPORTED / INVALID_ARG).  Any number of rows is computed; the
+ * matrices of experts without rows are not read.  Products with bf16 x and with fp32 x are both accumulated in fp32
+ * without rounding x or the weights.
+ */
+uint64_t deamoe_quant_workspace(int32_t dtype, int32_t n_token, int32_t n_in);
+deamoe_status_t deamoe_quant_product(void *cuda_stream, int32_t dtype, const uint8_t *codes, int32_t scale_dtype,
+                                     const void *scales, const uint8_t *zeros, int32_t n_expert, int32_t n_out,
+                                     int32_t n_in, int32_t group, const void *x, int64_t x_stride, int32_t n_token,
+                                     const int32_t *expert_off, const int32_t *row_pair, int32_t pairs_per_token,
+                                     int32_t n_rows, int32_t swiglu, void *out, int64_t out_stride, void *workspace,
+                                     uint64_t workspace_bytes);
+
 /*
  * Measurement aid.  (The paper has no counterpart.)  Enqueues one kernel that reads `bytes` bytes
  * of `buf` (DEVICE, 16-byte aligned; a trailing remainder of fewer than 16 bytes is ignored) exactly

@@ -33,7 +33,13 @@ SYMBOLS = ("deamoe_layer_create", "deamoe_vanilla_create", "deamoe_layer_destroy
            "deamoe_forward", "deamoe_vanilla_forward", "deamoe_forward_host", "deamoe_forward_partial",
            "deamoe_finish_partial", "deamoe_get_routing",
            "deamoe_get_stats", "deamoe_profile_enable", "deamoe_profile_last_ms", "deamoe_route_static", "deamoe_failure_test", "deamoe_probe_read",
-           "deamoe_last_launches", "deamoe_device_bytes", "deamoe_status_string")
+           "deamoe_last_launches", "deamoe_device_bytes", "deamoe_status_string",
+           "deamoe_sort_workspace", "deamoe_sort_pairs", "deamoe_dispatch", "deamoe_dispatch_backward", "deamoe_combine",
+           "deamoe_combine_backward", "deamoe_norm_workspace", "deamoe_norm", "deamoe_norm_backward",
+           "deamoe_norm_residual", "deamoe_norm_residual_backward", "deamoe_quant_workspace", "deamoe_quant_product")
+
+GATE_NONE, GATE_CHANNEL, GATE_TOKEN, GATE_FULL = 0, 1, 2, 3
+MAX_WIDTH = 1 << 20
 
 
 class Config(C.Structure):
@@ -92,6 +98,24 @@ def lib():
         L.deamoe_probe_read.argtypes = [C.c_void_p, C.c_void_p, C.c_uint64, C.c_void_p]
         L.deamoe_profile_enable.argtypes = [C.c_void_p, C.c_int32]
         L.deamoe_profile_last_ms.argtypes = [C.c_void_p, C.POINTER(C.c_float)]
+        i, l, u, f, p = C.c_int32, C.c_int64, C.c_uint64, C.c_float, C.c_void_p
+        for name, res, args in (
+                ("deamoe_sort_workspace", u, (i, i, i)),
+                ("deamoe_sort_pairs", i, (p, p, i, i, i, p, p, p, p, u)),
+                ("deamoe_dispatch", i, (p, i, p, l, p, i, i, i, p, l, l)),
+                ("deamoe_dispatch_backward", i, (p, i, p, l, l, p, i, i, i, p, l)),
+                ("deamoe_combine", i, (p, i, p, l, l, p, p, i, i, i, p, l)),
+                ("deamoe_combine_backward", i, (p, i, p, l, p, l, l, p, p, i, i, i, p, l, p)),
+                ("deamoe_norm_workspace", u, (i, i)),
+                ("deamoe_norm", i, (p, i, p, l, i, i, i, p, f, p, l)),
+                ("deamoe_norm_backward", i, (p, i, p, l, i, i, i, p, f, p, l, p, l, p, l, p, p, u)),
+                ("deamoe_norm_residual", i, (p, i, p, l, p, l, i, i, i, i, p, f, i, p, l, f, f, p, l, p, f, p, l)),
+                ("deamoe_norm_residual_backward", i, (p, i, p, l, p, l, i, i, i, i, p, f, i, p, l, f, f, p, l, p, f, p, l,
+                                                      p, l, p, l, p, l, p, p, p, u)),
+                ("deamoe_quant_workspace", u, (i, i, i)),
+                ("deamoe_quant_product", i, (p, i, p, i, p, p, i, i, i, i, p, l, i, p, p, i, i, i, p, l, p, u))):
+            getattr(L, name).restype = res
+            getattr(L, name).argtypes = args
         _lib = L
     return _lib
 
@@ -150,6 +174,312 @@ def route_static(router, tokens, n_dept, experts_per_dept, top_k, norm_topk=1, r
     if st != OK:
         raise DeaMoEError(st, "deamoe_route_static")
     return idx, w
+
+
+# ---------------------------------------------------------------- operators around a layer
+# Thin wrappers like the rest of this file: they check what the C call cannot see (types, shapes, the device a tensor
+# lives on), make outputs and workspaces that were not handed in, and call.  Matrices may have any row stride.
+
+_TYPES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _refuse(where, why):
+    e = DeaMoEError(ERR_INVALID_ARG, where)
+    e.args = (f"{e.args[0]}: {why}",)
+    raise e
+
+
+def _mat(t, where, name, dtype, rows, cols):
+    """Address and row stride of a [rows, cols] matrix of the current device."""
+    if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        _refuse(where, f"{name} must be {dtype} [{rows}, {cols}], got {t.dtype} {list(t.shape)}")
+    if t.get_device() != torch.cuda.current_device():
+        _refuse(where, f"{name} is not on the current CUDA device")
+    if cols > 1 and t.stride(1) != 1:
+        _refuse(where, f"{name} must have consecutive values in a row")
+    return t.data_ptr(), t.stride(0) if rows > 1 else cols
+
+
+def _vec(t, where, name, dtype, *shape):
+    """Address of a contiguous array of the current device."""
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+        _refuse(where, f"{name} must be contiguous {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
+    if t.get_device() != torch.cuda.current_device():
+        _refuse(where, f"{name} is not on the current CUDA device")
+    return t.data_ptr()
+
+
+def _type(t, where, name):
+    code = _TYPES.get(t.dtype)
+    if code is None or t.dim() != 2:
+        _refuse(where, f"{name} must be a float32 or bfloat16 matrix, got {t.dtype} {list(t.shape)}")
+    return code
+
+
+def _workspace(nbytes, device):
+    """Scratch of one call: from torch's allocator on the current stream (a captured graph's own pool while capturing),
+    so no two calls share it unless the stream orders them."""
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def _done(status, where):
+    if status != OK:
+        raise DeaMoEError(status, where)
+
+
+def sort_pairs(topk_idx, n_expert):
+    """(token, slot) pairs in expert order (deamoe_sort_pairs).  topk_idx: int32 [T, k], as Layer.route gives it; entries
+    outside [0, n_expert) drop their pair.  Returns expert_off [n_expert + 1], pair_row [T, k] (-1 = dropped) and
+    row_pair [T * k] (-1 behind the last row), all int32."""
+    where = "deamoe_sort_pairs"
+    if topk_idx.dim() != 2:
+        _refuse(where, "topk_idx must be [T, k]")
+    T, k = topk_idx.shape
+    src = _vec(topk_idx, where, "topk_idx", torch.int32, T, k)
+    dev = topk_idx.device
+    n = int(n_expert)
+    off = torch.empty(max(n, 0) + 1, dtype=torch.int32, device=dev)
+    pair_row = torch.empty((T, k), dtype=torch.int32, device=dev)
+    row_pair = torch.empty(T * k, dtype=torch.int32, device=dev)
+    L = lib()
+    need = L.deamoe_sort_workspace(T, k, n)
+    ws = _workspace(need, dev)
+    _done(L.deamoe_sort_pairs(_stream(), src, T, k, n, off.data_ptr(), pair_row.data_ptr(), row_pair.data_ptr(),
+                              _dptr(ws), need), where)
+    return off, pair_row, row_pair
+
+
+def dispatch(x, pair_row, rows=None):
+    """rows[pair_row[t, q]] = x[t] (deamoe_dispatch).  rows: [n_rows, h] to fill; made with T * k rows if omitted (rows
+    that no pair points to are then uninitialised)."""
+    where = "deamoe_dispatch"
+    dt = _type(x, where, "x")
+    T, h = x.shape
+    k = pair_row.shape[-1]
+    if rows is None:
+        rows = torch.empty((T * k, h), dtype=x.dtype, device=x.device)
+    n = rows.shape[0]
+    px, sx = _mat(x, where, "x", x.dtype, T, h)
+    pr, sr = _mat(rows, where, "rows", x.dtype, n, h)
+    _done(lib().deamoe_dispatch(_stream(), dt, px, sx, _vec(pair_row, where, "pair_row", torch.int32, T, k), T, k, h, pr, sr,
+                                n), where)
+    return rows
+
+
+def dispatch_backward(drows, pair_row, dx=None):
+    """dx[t] = sum_q drows[pair_row[t, q]] (deamoe_dispatch_backward)."""
+    where = "deamoe_dispatch_backward"
+    dt = _type(drows, where, "drows")
+    n, h = drows.shape
+    T, k = pair_row.shape
+    if dx is None:
+        dx = torch.empty((T, h), dtype=drows.dtype, device=drows.device)
+    pd, sd = _mat(drows, where, "drows", drows.dtype, n, h)
+    px, sx = _mat(dx, where, "dx", drows.dtype, T, h)
+    _done(lib().deamoe_dispatch_backward(_stream(), dt, pd, sd, n, _vec(pair_row, where, "pair_row", torch.int32, T, k), T, k,
+                                         h, px, sx), where)
+    return dx
+
+
+def combine(rows, pair_row, topk_w, out=None):
+    """out[t] = sum_q topk_w[t, q] rows[pair_row[t, q]] (deamoe_combine)."""
+    where = "deamoe_combine"
+    dt = _type(rows, where, "rows")
+    n, h = rows.shape
+    T, k = pair_row.shape
+    if out is None:
+        out = torch.empty((T, h), dtype=rows.dtype, device=rows.device)
+    pr, sr = _mat(rows, where, "rows", rows.dtype, n, h)
+    po, so = _mat(out, where, "out", rows.dtype, T, h)
+    _done(lib().deamoe_combine(_stream(), dt, pr, sr, n, _vec(pair_row, where, "pair_row", torch.int32, T, k),
+                               _vec(topk_w, where, "topk_w", torch.float32, T, k), T, k, h, po, so), where)
+    return out
+
+
+def combine_backward(dout, rows, pair_row, topk_w, drows=None, dw=None):
+    """drows[pair_row[t, q]] = topk_w[t, q] dout[t] and dw[t, q] = <dout[t], rows[pair_row[t, q]]>
+    (deamoe_combine_backward).  Returns (drows, dw); rows of drows that no pair points to are left as they were
+    (uninitialised if drows was made here)."""
+    where = "deamoe_combine_backward"
+    dt = _type(dout, where, "dout")
+    T, h = dout.shape
+    k = pair_row.shape[-1]
+    n = rows.shape[0]
+    if drows is None:
+        drows = torch.empty((n, h), dtype=dout.dtype, device=dout.device)
+    if dw is None:
+        dw = torch.empty((T, k), dtype=torch.float32, device=dout.device)
+    pd, sd = _mat(dout, where, "dout", dout.dtype, T, h)
+    pr, sr = _mat(rows, where, "rows", dout.dtype, n, h)
+    pg, sg = _mat(drows, where, "drows", dout.dtype, n, h)
+    _done(lib().deamoe_combine_backward(_stream(), dt, pd, sd, pr, sr, n, _vec(pair_row, where, "pair_row", torch.int32, T, k),
+                                        _vec(topk_w, where, "topk_w", torch.float32, T, k), T, k, h, pg, sg,
+                                        _vec(dw, where, "dw", torch.float32, T, k)), where)
+    return drows, dw
+
+
+def _gain(w, where, name, h, other=None):
+    """Address and type code of a gain (None = ones).  Two gains of one call have one type."""
+    if w is None:
+        return None, (F32 if other is None else _TYPES.get(other.dtype, -1))
+    code = _TYPES.get(w.dtype)
+    if code is None or (other is not None and other.dtype != w.dtype):
+        _refuse(where, f"{name} must be float32 or bfloat16, and of one type with the call's other gain")
+    return _vec(w, where, name, w.dtype, h), code
+
+
+def norm(x, weight, eps, out=None):
+    """out = x / sqrt(mean(x^2) + eps) * weight, row by row (deamoe_norm).  weight [h] (float32 or bfloat16) or None; out may
+    be x."""
+    where = "deamoe_norm"
+    dt = _type(x, where, "x")
+    T, h = x.shape
+    if out is None:
+        out = torch.empty((T, h), dtype=x.dtype, device=x.device)
+    px, sx = _mat(x, where, "x", x.dtype, T, h)
+    po, so = _mat(out, where, "out", x.dtype, T, h)
+    pw, wdt = _gain(weight, where, "weight", h)
+    _done(lib().deamoe_norm(_stream(), dt, px, sx, T, h, wdt, pw, eps, po, so), where)
+    return out
+
+
+def norm_backward(x, weight, eps, du, dadd=None, dx=None):
+    """Gradients of `norm`: dx (plus dadd, the gradient that reaches x past the norm; dx may be dadd) and dweight
+    (float32 [h]) (deamoe_norm_backward)."""
+    where = "deamoe_norm_backward"
+    dt = _type(x, where, "x")
+    T, h = x.shape
+    dev = x.device
+    if dx is None:
+        dx = torch.empty((T, h), dtype=x.dtype, device=dev)
+    dw = torch.empty(h, dtype=torch.float32, device=dev)
+    px, sx = _mat(x, where, "x", x.dtype, T, h)
+    pu, su = _mat(du, where, "du", x.dtype, T, h)
+    pa, sa = _mat(dadd, where, "dadd", x.dtype, T, h) if dadd is not None else (None, 0)
+    pd, sd = _mat(dx, where, "dx", x.dtype, T, h)
+    pw, wdt = _gain(weight, where, "weight", h)
+    L = lib()
+    need = L.deamoe_norm_workspace(T, h)
+    ws = _workspace(need, dev)
+    _done(L.deamoe_norm_backward(_stream(), dt, px, sx, T, h, wdt, pw, eps, pu, su, pa, sa, pd, sd, dw.data_ptr(), _dptr(ws),
+                                 need), where)
+    return dx, dw
+
+
+def _gate(gate, where, dtype, T, h, kind):
+    """Kind, address and row stride of a gate.  [h] is one per channel, [T, 1] or [T] one per token, [T, h] full; a gate of
+    one dimension with T == h needs `gate_kind`."""
+    if gate is None:
+        return GATE_NONE, None, 0
+    shape = tuple(gate.shape)
+    if kind is None:
+        if len(shape) == 1 and T == h and shape == (h,):
+            _refuse(where, "gate [h] with as many tokens as channels: say gate_kind")
+        kind = {(h,): GATE_CHANNEL, (T,): GATE_TOKEN, (T, h): GATE_FULL}.get(shape)
+    if kind == GATE_FULL:
+        return (kind,) + _mat(gate, where, "gate", dtype, T, h)
+    if kind not in (GATE_CHANNEL, GATE_TOKEN):
+        _refuse(where, f"gate must be [{h}] (channels), [{T}] (tokens) or [{T}, {h}], got {list(shape)}")
+    return kind, _vec(gate, where, "gate", dtype, h if kind == GATE_CHANNEL else T), 0
+
+
+def norm_residual(x, y, weight, eps, gate=None, residual_scale=1.0, branch_scale=1.0, normalise=True, next_norm=True,
+                  next_weight=None, next_eps=None, gate_kind=None, out=None, next_out=None):
+    """s = residual_scale x + branch_scale gate (y / rms(y) weight); returns s and s / rms(s) next_weight (None with
+    next_norm=False) in one pass (deamoe_norm_residual).  gate: None, [h], [T] or [T, h]; normalise=False takes y as it
+    is.  out may be x."""
+    where = "deamoe_norm_residual"
+    dt = _type(x, where, "x")
+    T, h = x.shape
+    if out is None:
+        out = torch.empty((T, h), dtype=x.dtype, device=x.device)
+    if next_out is None and next_norm:
+        next_out = torch.empty((T, h), dtype=x.dtype, device=x.device)
+    px, sx = _mat(x, where, "x", x.dtype, T, h)
+    py, sy = _mat(y, where, "y", x.dtype, T, h)
+    po, so = _mat(out, where, "out", x.dtype, T, h)
+    pn, sn = _mat(next_out, where, "next_out", x.dtype, T, h) if next_norm else (None, 0)
+    pw, wdt = _gain(weight, where, "weight", h, next_weight)
+    pm, _ = _gain(next_weight, where, "next_weight", h, weight)
+    kind, pg, sg = _gate(gate, where, x.dtype, T, h, gate_kind)
+    _done(lib().deamoe_norm_residual(_stream(), dt, px, sx, py, sy, T, h, 1 if normalise else 0, wdt, pw, eps, kind, pg, sg,
+                                     residual_scale, branch_scale, po, so, pm, eps if next_eps is None else next_eps,
+                                     pn, sn), where)
+    return out, next_out if next_norm else None
+
+
+def norm_residual_backward(x, y, weight, eps, dout, gate=None, residual_scale=1.0, branch_scale=1.0, normalise=True,
+                           next_weight=None, next_eps=None, du=None, gate_kind=None, dx=None, dy=None):
+    """Gradients of `norm_residual` from those of its outputs (dout, and du of the next norm or None): dx, dy, dgate,
+    dweight, dnext_weight; the last three are None where the call has no such input.  dweight, dnext_weight and the
+    gradient of a per-channel or per-token gate are float32, that of a full gate has the gate's type
+    (deamoe_norm_residual_backward)."""
+    where = "deamoe_norm_residual_backward"
+    dt = _type(x, where, "x")
+    T, h = x.shape
+    dev = x.device
+    if dx is None:
+        dx = torch.empty((T, h), dtype=x.dtype, device=dev)
+    if dy is None:
+        dy = torch.empty((T, h), dtype=x.dtype, device=dev)
+    px, sx = _mat(x, where, "x", x.dtype, T, h)
+    py, sy = _mat(y, where, "y", x.dtype, T, h)
+    po, so = _mat(dout, where, "dout", x.dtype, T, h)
+    pu, su = _mat(du, where, "du", x.dtype, T, h) if du is not None else (None, 0)
+    pdx, sdx = _mat(dx, where, "dx", x.dtype, T, h)
+    pdy, sdy = _mat(dy, where, "dy", x.dtype, T, h)
+    pw, wdt = _gain(weight, where, "weight", h, next_weight)
+    pm, _ = _gain(next_weight, where, "next_weight", h, weight)
+    kind, pg, sg = _gate(gate, where, x.dtype, T, h, gate_kind)
+    dgate, sdg = None, 0
+    if kind == GATE_FULL:
+        dgate, sdg = torch.empty((T, h), dtype=x.dtype, device=dev), h
+    elif kind != GATE_NONE:
+        dgate = torch.empty(h if kind == GATE_CHANNEL else T, dtype=torch.float32, device=dev)
+    dw = torch.empty(h, dtype=torch.float32, device=dev) if weight is not None else None
+    dn = torch.empty(h, dtype=torch.float32, device=dev) if next_weight is not None else None
+    L = lib()
+    need = L.deamoe_norm_workspace(T, h)
+    ws = _workspace(need, dev)
+    _done(L.deamoe_norm_residual_backward(_stream(), dt, px, sx, py, sy, T, h, 1 if normalise else 0, wdt, pw, eps, kind, pg,
+                                          sg, residual_scale, branch_scale, po, so, pm,
+                                          eps if next_eps is None else next_eps, pu, su, pdx, sdx, pdy, sdy, _dptr(dgate),
+                                          sdg, _dptr(dw), _dptr(dn), _dptr(ws), need), where)
+    return dx, dy, dgate, dw, dn
+
+
+def quant_product(codes, scales, x, group, zeros=None, expert_off=None, row_pair=None, pairs_per_token=1, swiglu=False,
+                  out=None):
+    """Products with 4-bit matrices (deamoe_quant_product): codes uint8 [E, n_out, n_in / 2] (low four bits first),
+    scales (float32 or bfloat16) and zeros (uint8, None = 8) [E, n_out, ceil(n_in / group)], x [T, n_in].
+    expert_off / row_pair: as sort_pairs gives them; row r is a product with x[row_pair[r] // pairs_per_token].  Without
+    row_pair, row r takes x[r].  Rows behind the last expert's are left as they were (uninitialised if out was made here)."""
+    where = "deamoe_quant_product"
+    dt = _type(x, where, "x")
+    T, n_in = x.shape
+    if codes.dim() != 3 or n_in != 2 * codes.shape[2]:
+        _refuse(where, f"codes must be [E, n_out, {n_in} / 2], got {list(codes.shape)}")
+    E, n_out, _ = codes.shape
+    groups = -(-n_in // group) if group > 0 else 0
+    R = T if row_pair is None else row_pair.shape[0]
+    width = n_out // 2 if swiglu else n_out
+    if out is None:
+        out = torch.empty((R, width), dtype=x.dtype, device=x.device)
+    sdt = _TYPES.get(scales.dtype)
+    if sdt is None:
+        _refuse(where, "scales must be float32 or bfloat16")
+    px, sx = _mat(x, where, "x", x.dtype, T, n_in)
+    po, so = _mat(out, where, "out", x.dtype, R, width)
+    pz = _vec(zeros, where, "zeros", torch.uint8, E, n_out, groups) if zeros is not None else None
+    pe = _vec(expert_off, where, "expert_off", torch.int32, E + 1) if expert_off is not None else None
+    pp = _vec(row_pair, where, "row_pair", torch.int32, R) if row_pair is not None else None
+    L = lib()
+    need = L.deamoe_quant_workspace(dt, T, n_in)
+    ws = _workspace(need, x.device)
+    _done(L.deamoe_quant_product(_stream(), dt, _vec(codes, where, "codes", torch.uint8, E, n_out, n_in // 2), sdt,
+                                 _vec(scales, where, "scales", scales.dtype, E, n_out, groups), pz, E, n_out, n_in, group, px,
+                                 sx, T, pe, pp, pairs_per_token, R, 1 if swiglu else 0, po, so, _dptr(ws), need), where)
+    return out
 
 
 class Layer:

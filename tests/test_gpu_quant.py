@@ -1,0 +1,225 @@
+"""Products with 4-bit matrices against the definition in 64 bits."""
+import pytest
+import torch
+
+from paper_2608_14385_b200 import binding
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, BF16 = torch.float32, torch.bfloat16
+
+
+def _matrices(E, N, K, group, zeros, sdtype, seed):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    G = -(-K // group)
+    codes = torch.randint(0, 256, (E, N, K // 2), generator=g, device=DEV, dtype=torch.uint8)
+    scales = ((torch.rand((E, N, G), generator=g, device=DEV) - 0.3) * 0.02).to(sdtype)
+    z = torch.randint(0, 16, (E, N, G), generator=g, device=DEV, dtype=torch.uint8) if zeros else None
+    return codes, scales, z
+
+
+def _widened(codes, scales, z, group, K):
+    low, high = (codes & 15).double(), (codes >> 4).double()
+    q = torch.stack([low, high], dim=-1).flatten(-2)
+    col = torch.arange(K, device=DEV) // group
+    return (q - (8.0 if z is None else z.double()[..., col])) * scales.double()[..., col]
+
+
+def _want(codes, scales, z, group, x, experts, sources, swiglu):
+    """The products of every row in 64 bits, and what fp32 may be off by before the output's rounding: a sum of K + 2 G
+    terms, each addition good to one unit (2^-23: the tensor cores cut rather than round), fp32 x carried to 2^-23."""
+    K = x.shape[1]
+    N = codes.shape[1]
+    got = torch.zeros((len(experts), N), dtype=torch.float64, device=DEV)
+    err = torch.zeros_like(got)
+    for e in sorted(set(experts)):
+        rows = [r for r in range(len(experts)) if experts[r] == e]
+        w = _widened(codes[e], scales[e], None if z is None else z[e], group, K)
+        src = [sources[r] for r in rows]
+        xs = torch.stack([x[s].double() if 0 <= s < x.shape[0] else torch.zeros(K, dtype=torch.float64, device=DEV) for s in src])
+        got[rows] = xs @ w.T
+        err[rows] = (K + 2 * scales.shape[2] + 8) * 2.0 ** -23 * (xs.abs() @ w.abs().T)
+    if swiglu:
+        F = N // 2
+        v, u, ev, eu = got[:, :F], got[:, F:], err[:, :F], err[:, F:]
+        silu = v * torch.sigmoid(v)
+        es = 1.1 * ev + 8 * 2.0 ** -24 * (silu.abs() + 1.1 * ev)
+        got, err = silu * u, (silu.abs() + es) * eu + es * u.abs() + 2.0 ** -24 * (silu * u).abs()
+    return got, err
+
+
+def _check(got, want, err):
+    half = torch.finfo(got.dtype).eps / 2
+    bound = err + half * (want.abs() + err) + torch.finfo(got.dtype).tiny
+    diff = (got.double() - want).abs()
+    assert (diff <= bound).all(), (diff / bound).max().item()
+
+
+def _routed(T, k, E, seed, skew=False):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    score = torch.rand((T, E), generator=g, device=DEV)
+    if skew:
+        score[:, :2] += 0.8
+    idx = score.topk(k, dim=1).indices.to(torch.int32)
+    off, _, row_pair = binding.sort_pairs(idx, E)
+    o = off.tolist()
+    experts = [e for e in range(E) for _ in range(o[e], o[e + 1])]
+    return off, row_pair, experts, [p // k for p in row_pair.tolist()]
+
+
+# one and several rows, around 8-row passes; widths around 16-row tiles; columns around 128-column steps and short groups
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("group,zeros,sdtype", [(32, True, BF16), (64, False, F32), (128, True, F32), (128, False, BF16)])
+@pytest.mark.parametrize("T,N,K", [(1, 1, 32), (1, 16, 128), (1, 4096, 7168), (2, 17, 96), (3, 100, 1056), (7, 33, 160),
+                                   (8, 48, 224), (9, 1003, 2048), (20, 66, 608), (33, 130, 1408), (70, 24, 384)])
+def test_one_matrix(T, N, K, group, zeros, sdtype, dtype):
+    codes, scales, z = _matrices(1, N, K, group, zeros, sdtype, T + N)
+    x = torch.randn((T, K), generator=torch.Generator(device=DEV).manual_seed(K), device=DEV).to(dtype)
+    got = binding.quant_product(codes, scales, x, group, zeros=z)
+    _check(got, *_want(codes, scales, z, group, x, [0] * T, list(range(T)), False))
+    if N % 2 == 0:
+        got = binding.quant_product(codes, scales, x, group, zeros=z, swiglu=True)
+        _check(got, *_want(codes, scales, z, group, x, [0] * T, list(range(T)), True))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,k,E,N,K,group,zeros,skew", [
+    (1, 8, 32, 128, 512, 128, False, False), (4, 2, 16, 96, 1408, 64, True, False), (37, 2, 16, 1003, 1056, 32, True, False),
+    (16, 8, 64, 64, 768, 128, False, False), (50, 3, 5, 40, 320, 64, True, True), (128, 2, 4, 34, 256, 128, False, True),
+    (3, 1, 300, 32, 128, 32, False, False), (2, 2, 2, 18, 64, 64, True, False), (60, 4, 2048, 16, 96, 32, True, False)])
+def test_experts_over_sorted_rows(T, k, E, N, K, group, zeros, skew, dtype):
+    codes, scales, z = _matrices(E, N, K, group, zeros, dtype, T + E)
+    x = torch.randn((T, K), generator=torch.Generator(device=DEV).manual_seed(K), device=DEV).to(dtype)
+    off, row_pair, experts, sources = _routed(T, k, E, T, skew)
+    for swiglu in (False, True) if N % 2 == 0 else (False,):
+        got = binding.quant_product(codes, scales, x, group, zeros=z, expert_off=off, row_pair=row_pair, pairs_per_token=k,
+                                    swiglu=swiglu)
+        _check(got, *_want(codes, scales, z, group, x, experts, sources, swiglu))
+    rows = x[torch.tensor(sources, device=DEV)]                # rows already in expert order: no row_pair
+    again = binding.quant_product(codes, scales, rows, group, zeros=z, expert_off=off)
+    _check(again, *_want(codes, scales, z, group, rows, experts, list(range(len(experts))), False))
+
+
+def test_dropped_pairs_leave_their_rows_alone_and_strides_are_followed():
+    T, k, E, N, K, group = 9, 4, 8, 48, 288, 32
+    codes, scales, z = _matrices(E, N, K, group, True, BF16, 1)
+    g = torch.Generator(device=DEV).manual_seed(2)
+    idx = torch.rand((T, E), generator=g, device=DEV).topk(k, dim=1).indices.to(torch.int32)
+    idx[::2, 1] = -1
+    idx[5] = E
+    off, _, row_pair = binding.sort_pairs(idx, E)
+    o = off.tolist()
+    f = o[-1]
+    experts = [e for e in range(E) for _ in range(o[e], o[e + 1])]
+    sources = [p // k for p in row_pair.tolist()[:f]]
+    for pad, at in ((16, 8), (5, 3)):
+        x = torch.randn((T, K + pad), generator=g, device=DEV).to(BF16)[:, at:at + K]
+        out = torch.randn((T * k, N + pad), generator=g, device=DEV).to(BF16)
+        kept = out.clone()
+        binding.quant_product(codes, scales, x, group, zeros=z, expert_off=off, row_pair=row_pair, pairs_per_token=k,
+                              out=out[:, at:at + N])
+        _check(out[:f, at:at + N], *_want(codes, scales, z, group, x, experts, sources, False))
+        kept[:f, at:at + N] = out[:f, at:at + N]
+        assert torch.equal(out, kept)
+    empty = torch.zeros(E + 1, dtype=torch.int32, device=DEV)   # no expert has a row
+    out = torch.ones((T * k, N), dtype=BF16, device=DEV)
+    binding.quant_product(codes, scales, torch.zeros((T, K), dtype=BF16, device=DEV), group, zeros=z, expert_off=empty,
+                          row_pair=row_pair, pairs_per_token=k, out=out)
+    assert (out == 1).all()
+
+
+def test_values_of_every_size():
+    """Tokens whose values span the type's range, infinities and NaN: each stays in its own row."""
+    N, K, group = 32, 256, 64
+    codes, scales, z = _matrices(1, N, K, group, True, F32, 5)
+    x = torch.randn((6, K), generator=torch.Generator(device=DEV).manual_seed(6), device=DEV)
+    x[1] *= 1e30
+    x[2] *= 1e-30
+    x[3, :128] *= 1e-12
+    x[4] = 0
+    for dtype in (BF16, F32):
+        t = x.to(dtype)
+        want, err = _want(codes, scales, z, group, t, [0] * 6, list(range(6)), False)
+        got = binding.quant_product(codes, scales, t, group, zeros=z)
+        _check(got, want, err)
+        t2 = t.clone()
+        t2[0, 3], t2[5, 9] = float("inf"), float("nan")
+        got2 = binding.quant_product(codes, scales, t2, group, zeros=z)
+        assert torch.equal(got2[1:5], got[1:5])
+        assert not torch.isfinite(got2[0]).any() and torch.isnan(got2[5]).all()
+
+
+def test_sources_outside_x_count_as_zero():
+    N, K, group = 16, 64, 32
+    codes, scales, _ = _matrices(2, N, K, group, False, BF16, 7)
+    x = torch.randn((3, K), device=DEV).to(BF16)
+    off = torch.tensor([0, 3, 5], dtype=torch.int32, device=DEV)
+    row_pair = torch.tensor([0, 99, -5, 2, 2 ** 31 - 1], dtype=torch.int32, device=DEV)
+    got = binding.quant_product(codes, scales, x, group, expert_off=off, row_pair=row_pair)
+    _check(got, *_want(codes, scales, None, group, x, [0, 0, 0, 1, 1], [0, -1, -1, 2, -1], False))
+    assert (got[[1, 2, 4]] == 0).all()
+
+
+def test_offsets_beyond_the_rows_are_cut():
+    """expert_off entries past n_rows or out of order reach no row outside [0, n_rows)."""
+    N, K, group = 16, 64, 32
+    codes, scales, _ = _matrices(3, N, K, group, False, BF16, 8)
+    x = torch.randn((4, K), device=DEV).to(BF16)
+    off = torch.tensor([-3, 2, 1, 900], dtype=torch.int32, device=DEV)
+    out = torch.zeros((8, N), dtype=BF16, device=DEV)
+    binding.quant_product(codes, scales, x, group, expert_off=off, out=out[:4])
+    torch.cuda.synchronize()
+    assert (out[4:] == 0).all()
+
+
+def test_captured_product_follows_new_routing_and_two_graphs_share_nothing():
+    T, k, E, N, K, group = 12, 4, 32, 64, 640, 128
+    codes, scales, z = _matrices(E, N, K, group, True, BF16, 9)
+
+    def fill(seed):
+        off, row_pair, _, _ = _routed(T, k, E, seed)
+        return {"x": torch.randn((T, K), generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV).to(BF16),
+                "off": off, "row_pair": row_pair}
+
+    def step(s):
+        return binding.quant_product(codes, scales, s["x"], group, zeros=z, expert_off=s["off"], row_pair=s["row_pair"],
+                                     pairs_per_token=k)
+
+    states, graphs, outs = [fill(1), fill(2)], [], []
+    for s in states:
+        step(s)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(step(s))
+        graphs.append(g)
+    for i, s in enumerate(states):
+        for n, t in fill(5 + i).items():
+            s[n].copy_(t)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(3):
+        for g, st in zip(graphs, streams):
+            with torch.cuda.stream(st):
+                g.replay()
+    torch.cuda.synchronize()
+    for s, got in zip(states, outs):
+        assert torch.equal(got, step(s))
+
+
+def test_wrapper_refuses_what_does_not_fit():
+    codes, scales, z = _matrices(2, 16, 64, 32, True, BF16, 1)
+    x = torch.zeros((4, 64), dtype=BF16, device=DEV)
+    off, pairs = torch.tensor([0, 2, 4], dtype=torch.int32, device=DEV), torch.arange(4, dtype=torch.int32, device=DEV)
+    q = binding.quant_product
+    bad = [lambda: q(codes, scales, x, 16, expert_off=off), lambda: q(codes, scales, x, 0, expert_off=off), lambda: q(codes, scales, x, 32),
+           lambda: q(codes, scales, x.half(), 32, expert_off=off), lambda: q(codes, scales.half(), x, 32, expert_off=off),
+           lambda: q(codes, scales, x, 64, expert_off=off), lambda: q(codes, scales, x[:, :32], 32, expert_off=off),
+           lambda: q(codes, scales, x, 32, zeros=z[:1], expert_off=off), lambda: q(codes, scales, x, 32, expert_off=off[:2]),
+           lambda: q(codes[:, :15].contiguous(), scales[:, :15].contiguous(), x, 32, expert_off=off, swiglu=True),
+           lambda: q(codes, scales, x, 32, expert_off=off, row_pair=pairs, pairs_per_token=0),
+           lambda: q(codes, scales, x, 32, expert_off=off.long()), lambda: q(codes, scales, x.cpu(), 32, expert_off=off),
+           lambda: q(codes[:1, :, :8].contiguous(), scales[:1, :, :1].contiguous(), x[:, :16].contiguous(), 32)]
+    for call in bad:
+        with pytest.raises(binding.DeaMoEError):
+            call()
