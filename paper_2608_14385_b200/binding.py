@@ -189,22 +189,35 @@ def _refuse(where, why):
     raise e
 
 
+_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+
+
+def _raw_stream(device):
+    """The current stream's handle (a decode step's calls are short: torch.cuda.current_stream builds an object first)."""
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+if hasattr(torch._C, "_cuda_getCurrentRawStream"):
+    _raw_stream = torch._C._cuda_getCurrentRawStream
+
+
 def _mat(t, where, name, dtype, rows, cols):
     """Address and row stride of a [rows, cols] matrix of the current device."""
-    if t.dtype != dtype or t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+    if t.dtype is not dtype or t.shape != (rows, cols):
         _refuse(where, f"{name} must be {dtype} [{rows}, {cols}], got {t.dtype} {list(t.shape)}")
-    if t.get_device() != torch.cuda.current_device():
+    if t.get_device() != _device():
         _refuse(where, f"{name} is not on the current CUDA device")
-    if cols > 1 and t.stride(1) != 1:
+    stride, step = t.stride()
+    if step != 1 and cols > 1:
         _refuse(where, f"{name} must have consecutive values in a row")
-    return t.data_ptr(), t.stride(0) if rows > 1 else cols
+    return t.data_ptr(), stride if rows > 1 else cols
 
 
 def _vec(t, where, name, dtype, *shape):
     """Address of a contiguous array of the current device."""
-    if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+    if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         _refuse(where, f"{name} must be contiguous {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
-    if t.get_device() != torch.cuda.current_device():
+    if t.get_device() != _device():
         _refuse(where, f"{name} is not on the current CUDA device")
     return t.data_ptr()
 
@@ -238,13 +251,13 @@ def sort_pairs(topk_idx, n_expert):
     src = _vec(topk_idx, where, "topk_idx", torch.int32, T, k)
     dev = topk_idx.device
     n = int(n_expert)
-    off = torch.empty(max(n, 0) + 1, dtype=torch.int32, device=dev)
-    pair_row = torch.empty((T, k), dtype=torch.int32, device=dev)
-    row_pair = torch.empty(T * k, dtype=torch.int32, device=dev)
+    off = topk_idx.new_empty(max(n, 0) + 1)
+    pair_row = topk_idx.new_empty((T, k))
+    row_pair = topk_idx.new_empty(T * k)
     L = lib()
     need = L.deamoe_sort_workspace(T, k, n)
     ws = _workspace(need, dev)
-    _done(L.deamoe_sort_pairs(_stream(), src, T, k, n, off.data_ptr(), pair_row.data_ptr(), row_pair.data_ptr(),
+    _done(L.deamoe_sort_pairs(_raw_stream(_device()), src, T, k, n, off.data_ptr(), pair_row.data_ptr(), row_pair.data_ptr(),
                               _dptr(ws), need), where)
     return off, pair_row, row_pair
 
@@ -257,11 +270,11 @@ def dispatch(x, pair_row, rows=None):
     T, h = x.shape
     k = pair_row.shape[-1]
     if rows is None:
-        rows = torch.empty((T * k, h), dtype=x.dtype, device=x.device)
+        rows = x.new_empty((T * k, h))
     n = rows.shape[0]
     px, sx = _mat(x, where, "x", x.dtype, T, h)
     pr, sr = _mat(rows, where, "rows", x.dtype, n, h)
-    _done(lib().deamoe_dispatch(_stream(), dt, px, sx, _vec(pair_row, where, "pair_row", torch.int32, T, k), T, k, h, pr, sr,
+    _done(lib().deamoe_dispatch(_raw_stream(_device()), dt, px, sx, _vec(pair_row, where, "pair_row", torch.int32, T, k), T, k, h, pr, sr,
                                 n), where)
     return rows
 
@@ -273,10 +286,10 @@ def dispatch_backward(drows, pair_row, dx=None):
     n, h = drows.shape
     T, k = pair_row.shape
     if dx is None:
-        dx = torch.empty((T, h), dtype=drows.dtype, device=drows.device)
+        dx = drows.new_empty((T, h))
     pd, sd = _mat(drows, where, "drows", drows.dtype, n, h)
     px, sx = _mat(dx, where, "dx", drows.dtype, T, h)
-    _done(lib().deamoe_dispatch_backward(_stream(), dt, pd, sd, n, _vec(pair_row, where, "pair_row", torch.int32, T, k), T, k,
+    _done(lib().deamoe_dispatch_backward(_raw_stream(_device()), dt, pd, sd, n, _vec(pair_row, where, "pair_row", torch.int32, T, k), T, k,
                                          h, px, sx), where)
     return dx
 
@@ -288,10 +301,10 @@ def combine(rows, pair_row, topk_w, out=None):
     n, h = rows.shape
     T, k = pair_row.shape
     if out is None:
-        out = torch.empty((T, h), dtype=rows.dtype, device=rows.device)
+        out = rows.new_empty((T, h))
     pr, sr = _mat(rows, where, "rows", rows.dtype, n, h)
     po, so = _mat(out, where, "out", rows.dtype, T, h)
-    _done(lib().deamoe_combine(_stream(), dt, pr, sr, n, _vec(pair_row, where, "pair_row", torch.int32, T, k),
+    _done(lib().deamoe_combine(_raw_stream(_device()), dt, pr, sr, n, _vec(pair_row, where, "pair_row", torch.int32, T, k),
                                _vec(topk_w, where, "topk_w", torch.float32, T, k), T, k, h, po, so), where)
     return out
 
@@ -306,13 +319,13 @@ def combine_backward(dout, rows, pair_row, topk_w, drows=None, dw=None):
     k = pair_row.shape[-1]
     n = rows.shape[0]
     if drows is None:
-        drows = torch.empty((n, h), dtype=dout.dtype, device=dout.device)
+        drows = dout.new_empty((n, h))
     if dw is None:
         dw = torch.empty((T, k), dtype=torch.float32, device=dout.device)
     pd, sd = _mat(dout, where, "dout", dout.dtype, T, h)
     pr, sr = _mat(rows, where, "rows", dout.dtype, n, h)
     pg, sg = _mat(drows, where, "drows", dout.dtype, n, h)
-    _done(lib().deamoe_combine_backward(_stream(), dt, pd, sd, pr, sr, n, _vec(pair_row, where, "pair_row", torch.int32, T, k),
+    _done(lib().deamoe_combine_backward(_raw_stream(_device()), dt, pd, sd, pr, sr, n, _vec(pair_row, where, "pair_row", torch.int32, T, k),
                                         _vec(topk_w, where, "topk_w", torch.float32, T, k), T, k, h, pg, sg,
                                         _vec(dw, where, "dw", torch.float32, T, k)), where)
     return drows, dw
@@ -335,11 +348,11 @@ def norm(x, weight, eps, out=None):
     dt = _type(x, where, "x")
     T, h = x.shape
     if out is None:
-        out = torch.empty((T, h), dtype=x.dtype, device=x.device)
+        out = x.new_empty((T, h))
     px, sx = _mat(x, where, "x", x.dtype, T, h)
     po, so = _mat(out, where, "out", x.dtype, T, h)
     pw, wdt = _gain(weight, where, "weight", h)
-    _done(lib().deamoe_norm(_stream(), dt, px, sx, T, h, wdt, pw, eps, po, so), where)
+    _done(lib().deamoe_norm(_raw_stream(_device()), dt, px, sx, T, h, wdt, pw, eps, po, so), where)
     return out
 
 
@@ -351,7 +364,7 @@ def norm_backward(x, weight, eps, du, dadd=None, dx=None):
     T, h = x.shape
     dev = x.device
     if dx is None:
-        dx = torch.empty((T, h), dtype=x.dtype, device=dev)
+        dx = x.new_empty((T, h))
     dw = torch.empty(h, dtype=torch.float32, device=dev)
     px, sx = _mat(x, where, "x", x.dtype, T, h)
     pu, su = _mat(du, where, "du", x.dtype, T, h)
@@ -361,7 +374,7 @@ def norm_backward(x, weight, eps, du, dadd=None, dx=None):
     L = lib()
     need = L.deamoe_norm_workspace(T, h)
     ws = _workspace(need, dev)
-    _done(L.deamoe_norm_backward(_stream(), dt, px, sx, T, h, wdt, pw, eps, pu, su, pa, sa, pd, sd, dw.data_ptr(), _dptr(ws),
+    _done(L.deamoe_norm_backward(_raw_stream(_device()), dt, px, sx, T, h, wdt, pw, eps, pu, su, pa, sa, pd, sd, dw.data_ptr(), _dptr(ws),
                                  need), where)
     return dx, dw
 
@@ -392,9 +405,9 @@ def norm_residual(x, y, weight, eps, gate=None, residual_scale=1.0, branch_scale
     dt = _type(x, where, "x")
     T, h = x.shape
     if out is None:
-        out = torch.empty((T, h), dtype=x.dtype, device=x.device)
+        out = x.new_empty((T, h))
     if next_out is None and next_norm:
-        next_out = torch.empty((T, h), dtype=x.dtype, device=x.device)
+        next_out = x.new_empty((T, h))
     px, sx = _mat(x, where, "x", x.dtype, T, h)
     py, sy = _mat(y, where, "y", x.dtype, T, h)
     po, so = _mat(out, where, "out", x.dtype, T, h)
@@ -402,7 +415,7 @@ def norm_residual(x, y, weight, eps, gate=None, residual_scale=1.0, branch_scale
     pw, wdt = _gain(weight, where, "weight", h, next_weight)
     pm, _ = _gain(next_weight, where, "next_weight", h, weight)
     kind, pg, sg = _gate(gate, where, x.dtype, T, h, gate_kind)
-    _done(lib().deamoe_norm_residual(_stream(), dt, px, sx, py, sy, T, h, 1 if normalise else 0, wdt, pw, eps, kind, pg, sg,
+    _done(lib().deamoe_norm_residual(_raw_stream(_device()), dt, px, sx, py, sy, T, h, 1 if normalise else 0, wdt, pw, eps, kind, pg, sg,
                                      residual_scale, branch_scale, po, so, pm, eps if next_eps is None else next_eps,
                                      pn, sn), where)
     return out, next_out if next_norm else None
@@ -419,9 +432,9 @@ def norm_residual_backward(x, y, weight, eps, dout, gate=None, residual_scale=1.
     T, h = x.shape
     dev = x.device
     if dx is None:
-        dx = torch.empty((T, h), dtype=x.dtype, device=dev)
+        dx = x.new_empty((T, h))
     if dy is None:
-        dy = torch.empty((T, h), dtype=x.dtype, device=dev)
+        dy = x.new_empty((T, h))
     px, sx = _mat(x, where, "x", x.dtype, T, h)
     py, sy = _mat(y, where, "y", x.dtype, T, h)
     po, so = _mat(dout, where, "dout", x.dtype, T, h)
@@ -433,7 +446,7 @@ def norm_residual_backward(x, y, weight, eps, dout, gate=None, residual_scale=1.
     kind, pg, sg = _gate(gate, where, x.dtype, T, h, gate_kind)
     dgate, sdg = None, 0
     if kind == GATE_FULL:
-        dgate, sdg = torch.empty((T, h), dtype=x.dtype, device=dev), h
+        dgate, sdg = x.new_empty((T, h)), h
     elif kind != GATE_NONE:
         dgate = torch.empty(h if kind == GATE_CHANNEL else T, dtype=torch.float32, device=dev)
     dw = torch.empty(h, dtype=torch.float32, device=dev) if weight is not None else None
@@ -441,7 +454,7 @@ def norm_residual_backward(x, y, weight, eps, dout, gate=None, residual_scale=1.
     L = lib()
     need = L.deamoe_norm_workspace(T, h)
     ws = _workspace(need, dev)
-    _done(L.deamoe_norm_residual_backward(_stream(), dt, px, sx, py, sy, T, h, 1 if normalise else 0, wdt, pw, eps, kind, pg,
+    _done(L.deamoe_norm_residual_backward(_raw_stream(_device()), dt, px, sx, py, sy, T, h, 1 if normalise else 0, wdt, pw, eps, kind, pg,
                                           sg, residual_scale, branch_scale, po, so, pm,
                                           eps if next_eps is None else next_eps, pu, su, pdx, sdx, pdy, sdy, _dptr(dgate),
                                           sdg, _dptr(dw), _dptr(dn), _dptr(ws), need), where)
@@ -464,7 +477,7 @@ def quant_product(codes, scales, x, group, zeros=None, expert_off=None, row_pair
     R = T if row_pair is None else row_pair.shape[0]
     width = n_out // 2 if swiglu else n_out
     if out is None:
-        out = torch.empty((R, width), dtype=x.dtype, device=x.device)
+        out = x.new_empty((R, width))
     sdt = _TYPES.get(scales.dtype)
     if sdt is None:
         _refuse(where, "scales must be float32 or bfloat16")
@@ -476,7 +489,7 @@ def quant_product(codes, scales, x, group, zeros=None, expert_off=None, row_pair
     L = lib()
     need = L.deamoe_quant_workspace(dt, T, n_in)
     ws = _workspace(need, x.device)
-    _done(L.deamoe_quant_product(_stream(), dt, _vec(codes, where, "codes", torch.uint8, E, n_out, n_in // 2), sdt,
+    _done(L.deamoe_quant_product(_raw_stream(_device()), dt, _vec(codes, where, "codes", torch.uint8, E, n_out, n_in // 2), sdt,
                                  _vec(scales, where, "scales", scales.dtype, E, n_out, groups), pz, E, n_out, n_in, group, px,
                                  sx, T, pe, pp, pairs_per_token, R, 1 if swiglu else 0, po, so, _dptr(ws), need), where)
     return out

@@ -15,11 +15,27 @@
 // Every operator is a few passes of HBM traffic over [T, h] rows, nothing else: bytes bound it.  Sums over the tokens
 // (dw, dwn, a per-channel dgate) are kept per thread block and added by a second kernel in block order: no atomics,
 // equal calls give equal bits.
+#include <atomic>
+
 #include "row.cuh"
 
 namespace deamoe {
 
-constexpr int NORM_CTAS = 296;  // thread blocks of the backward kernels: partial sums of the columns, one row each
+// Thread blocks of the backward kernels, each of which leaves one row of partial column sums: 8 columns a thread, and
+// as many blocks as fill the SMs' thread slots (rows of up to 8192 values, else two blocks an SM).
+constexpr int NORM_SMS = 148;
+constexpr int GRAD_COLUMNS = 8, GRAD_MAX_WIDTH = 8192;
+static int grad_threads(int h) { return ((h + GRAD_COLUMNS - 1) / GRAD_COLUMNS + 31) / 32 * 32; }
+static int grad_blocks_per_sm(int h) {
+  if (h > GRAD_MAX_WIDTH) return 2;
+  const int n = 1024 / grad_threads(h);
+  return n > 8 ? 8 : n;
+}
+static int grad_ctas(int64_t T, int h) {
+  const int most = NORM_SMS * grad_blocks_per_sm(h);
+  return T < most ? (int)T : most;
+}
+
 
 struct Rows {  // a [T, h] matrix with a row stride (elements), or a null pointer
   const void* p;
@@ -37,7 +53,7 @@ struct NormArgs {
   const void *w, *wn;      // gains, or null (ones)
   void *out, *u, *dx, *dy, *dgate;
   int64_t out_s, u_s, dx_s, dy_s, dgate_s;
-  float* part;             // [3][NORM_CTAS][h]: partial column sums of dw, dwn, dgate
+  float* part;             // [3][grad_ctas][h]: partial column sums of dw, dwn, dgate
   float* dgate_token;      // [T]
 };
 
@@ -65,6 +81,7 @@ static __device__ __forceinline__ float inv_rms(float ss, int h, float eps) { re
 // ---------------------------------------------------------------- any width, any alignment: one block a row
 
 constexpr int ANY_THREADS = 256;
+constexpr int RING_BYTES = 220 * 1024;  // of an SM's 227 KB, beside the sums' buffers
 
 template <typename T> __global__ void __launch_bounds__(ANY_THREADS) k_norm_any(NormArgs A) {
   __shared__ float buf[32];
@@ -142,12 +159,12 @@ template <typename T> __global__ void __launch_bounds__(ANY_THREADS) k_residual_
   }
 }
 
-template <typename T> __global__ void __launch_bounds__(ANY_THREADS) k_residual_grad_any(NormArgs A) {
+template <typename T> __global__ void __launch_bounds__(ANY_THREADS) k_residual_grad_any(NormArgs A, size_t part_step) {
   __shared__ float buf[4][64];  // the last sum alternates: it may be the only one of a row
   int flip = 2;
   float* part_w = A.part + (size_t)blockIdx.x * A.h;
-  float* part_n = part_w + (size_t)NORM_CTAS * A.h;
-  float* part_g = part_n + (size_t)NORM_CTAS * A.h;
+  float* part_n = part_w + part_step;
+  float* part_g = part_n + part_step;
   bool first = true;
   for (int64_t t = blockIdx.x; t < A.T; t += gridDim.x) {
     float ry = 1.f;
@@ -205,27 +222,430 @@ template <typename T> __global__ void __launch_bounds__(ANY_THREADS) k_residual_
   }
 }
 
+// ---------------------------------------------------------------- rows held in registers
+
+// VE gains at column i (null = ones)
+template <int VE> static __device__ __forceinline__ void load_gains(const void* w, int wdt, int64_t i, float (&f)[VE]) {
+  if (!w) {
+#pragma unroll
+    for (int j = 0; j < VE; ++j) f[j] = 1.f;
+  } else if constexpr (VE == 1) {
+    f[0] = load_gain(w, wdt, i);
+  } else if (wdt == DEAMOE_F32) {
+    const float4* p = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(w) + i);
+#pragma unroll
+    for (int j = 0; j < VE / 4; ++j) {
+      const float4 v = p[j];
+      f[4 * j] = v.x; f[4 * j + 1] = v.y; f[4 * j + 2] = v.z; f[4 * j + 3] = v.w;
+    }
+  } else {
+    const uint32_t* p = reinterpret_cast<const uint32_t*>(reinterpret_cast<const __nv_bfloat16*>(w) + i);
+    uint32_t u[VE / 2];
+    if constexpr (VE == 8) {
+      const uint4 v = *reinterpret_cast<const uint4*>(p);
+      u[0] = v.x; u[1] = v.y; u[2] = v.z; u[3] = v.w;
+    } else {
+      const uint2 v = *reinterpret_cast<const uint2*>(p);
+      u[0] = v.x; u[1] = v.y;
+    }
+#pragma unroll
+    for (int j = 0; j < VE / 2; ++j) {
+      f[2 * j] = __uint_as_float(u[j] << 16);
+      f[2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
+    }
+  }
+}
+
+template <typename T> static __device__ __forceinline__ const T* row_at(const Rows& m, int64_t t) {
+  return reinterpret_cast<const T*>(m.p) + t * m.stride;
+}
+template <typename T, int VE> static __device__ __forceinline__ void load_row(const Rows& m, int64_t t, int c, float (&f)[VE]) {
+  load_once<T, VE>(row_at<T>(m, t) + (int64_t)c * VE).widen(f);
+}
+template <typename T, int VE>
+static __device__ __forceinline__ void store_row(void* p, int64_t stride, int64_t t, int c, const float (&f)[VE]) {
+  Pack<T, VE> o;
+  o.narrow(f);
+  store_pack<T, VE>(reinterpret_cast<T*>(p) + t * stride + (int64_t)c * VE, o);
+}
+template <typename T, int VE> static __device__ __forceinline__ void load_gate(const NormArgs& A, int64_t t, int c, float (&g)[VE]) {
+  if (A.gate_kind == DEAMOE_GATE_FULL) {
+    load_row<T, VE>(A.gate, t, c, g);
+  } else if (A.gate_kind == DEAMOE_GATE_CHANNEL) {
+    load_pack<T, VE>(reinterpret_cast<const T*>(A.gate.p) + (int64_t)c * VE).widen(g);
+  } else {
+    const float v = A.gate_kind == DEAMOE_GATE_TOKEN ? to_f<T>(reinterpret_cast<const T*>(A.gate.p)[t]) : 1.f;
+#pragma unroll
+    for (int j = 0; j < VE; ++j) g[j] = v;
+  }
+}
+
+// Forward kernels: one block a row, NV packs of VE values a thread, the row read once.  Rows in flight hide each
+// other's two reductions.
+template <typename T, int VE, int NV, int MAXT> __global__ void __launch_bounds__(MAXT) k_norm_rows(NormArgs A, int packs) {
+  __shared__ float buf[32];
+  const int64_t t = blockIdx.x;
+  Pack<T, VE> x[NV];
+  float ss[1] = {0.f};
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    const int c = threadIdx.x + n * blockDim.x;
+    if (c < packs) x[n] = load_once<T, VE>(row_at<T>(A.x, t) + (int64_t)c * VE);
+  }
+#pragma unroll
+  for (int n = 0; n < NV; ++n)
+    if ((int)(threadIdx.x + n * blockDim.x) < packs) {
+      float f[VE];
+      x[n].widen(f);
+#pragma unroll
+      for (int j = 0; j < VE; ++j) ss[0] = fmaf(f[j], f[j], ss[0]);
+    }
+  block_sums<1>(ss, buf);
+  const float r = inv_rms(ss[0], A.h, A.eps);
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    const int c = threadIdx.x + n * blockDim.x;
+    if (c >= packs) continue;
+    float f[VE], w[VE];
+    x[n].widen(f);
+    load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
+#pragma unroll
+    for (int j = 0; j < VE; ++j) f[j] *= r * w[j];
+    store_row<T, VE>(A.u, A.u_s, t, c, f);
+  }
+}
+
+template <typename T, int VE, int NV, int MAXT> __global__ void __launch_bounds__(MAXT) k_residual_rows(NormArgs A, int packs) {
+  __shared__ float buf[2][32];
+  const int64_t t = blockIdx.x;
+  Pack<T, VE> x[NV], y[NV];
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    const int c = threadIdx.x + n * blockDim.x;
+    if (c < packs) {
+      y[n] = load_once<T, VE>(row_at<T>(A.y, t) + (int64_t)c * VE);
+      x[n] = load_once<T, VE>(row_at<T>(A.x, t) + (int64_t)c * VE);
+    }
+  }
+  float ry = 1.f;
+  if (A.post_norm) {
+    float ss[1] = {0.f};
+#pragma unroll
+    for (int n = 0; n < NV; ++n)
+      if ((int)(threadIdx.x + n * blockDim.x) < packs) {
+        float f[VE];
+        y[n].widen(f);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) ss[0] = fmaf(f[j], f[j], ss[0]);
+      }
+    block_sums<1>(ss, buf[0]);
+    ry = inv_rms(ss[0], A.h, A.eps);
+  }
+  float s[NV][VE], ss[1] = {0.f};
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    const int c = threadIdx.x + n * blockDim.x;
+    if (c >= packs) continue;
+    float f[VE], w[VE], g[VE];
+    load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
+    load_gate<T, VE>(A, t, c, g);
+    y[n].widen(f);
+    x[n].widen(s[n]);
+#pragma unroll
+    for (int j = 0; j < VE; ++j) {
+      s[n][j] = fmaf(A.a, s[n][j], A.b * g[j] * (f[j] * ry * w[j]));
+      ss[0] = fmaf(s[n][j], s[n][j], ss[0]);
+    }
+    store_row<T, VE>(A.out, A.out_s, t, c, s[n]);
+  }
+  if (!A.next_norm) return;
+  block_sums<1>(ss, buf[1]);
+  const float ro = inv_rms(ss[0], A.h, A.next_eps);
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    const int c = threadIdx.x + n * blockDim.x;
+    if (c >= packs) continue;
+    float w[VE];
+    load_gains<VE>(A.wn, A.wdt, (int64_t)c * VE, w);
+#pragma unroll
+    for (int j = 0; j < VE; ++j) s[n][j] *= ro * w[j];
+    store_row<T, VE>(A.u, A.u_s, t, c, s[n]);
+  }
+}
+
+// Backward kernels: persistent blocks, a block walks its rows with the column sums of its threads' columns in
+// registers.  A thread copies its own packs of the rows to come into shared memory (asynchronously, `stages` rows ahead)
+// and is the only one to read them back, so the loads of later rows run under a row's reductions without any barrier.
+template <int N> static __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+static __device__ __forceinline__ void copy_pack(uint4* to, const void* from) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
+}
+static __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+static __device__ __forceinline__ void copies_wait_for(int stages) {  // all but the stages - 1 youngest groups are there
+  if (stages >= 4) copies_wait<3>();
+  else if (stages == 3) copies_wait<2>();
+  else if (stages == 2) copies_wait<1>();
+  else copies_wait<0>();
+}
+
+// NIN row-wise inputs of one row: through the ring (VE > 1) or straight from memory.
+template <typename T, int VE, int NV, int NIN> struct RowFeed {
+  Pack<T, VE> v[NIN][NV];
+  int stages, packs, nin;  // nin: inputs that have room in the ring (the last may be absent)
+  uint4* ring;             // [stages][nin][NV][blockDim.x]
+
+  __device__ __forceinline__ uint4* slot(int stage, int i, int n) const {
+    return ring + ((size_t)(stage * nin + i) * NV + n) * blockDim.x + threadIdx.x;
+  }
+  __device__ __forceinline__ void request(const Rows (&m)[NIN], int64_t t, int64_t T_, int stage) const {
+    if constexpr (VE > 1) {
+      if (t < T_)
+#pragma unroll
+        for (int i = 0; i < NIN; ++i)
+#pragma unroll
+          for (int n = 0; n < NV; ++n) {
+            const int c = threadIdx.x + n * blockDim.x;
+            if (m[i].p && c < packs) copy_pack(slot(stage, i, n), row_at<T>(m[i], t) + (int64_t)c * VE);
+          }
+      copies_commit();
+    }
+  }
+  __device__ __forceinline__ void take(const Rows (&m)[NIN], int64_t t, int stage) {
+    if constexpr (VE > 1) copies_wait_for(stages);
+#pragma unroll
+    for (int i = 0; i < NIN; ++i)
+#pragma unroll
+      for (int n = 0; n < NV; ++n) {
+        const int c = threadIdx.x + n * blockDim.x;
+        if (!m[i].p || c >= packs) continue;
+        if constexpr (VE > 1) v[i][n].r = *slot(stage, i, n);
+        else v[i][n] = load_once<T, VE>(row_at<T>(m[i], t) + (int64_t)c * VE);
+      }
+  }
+};
+
+template <typename T, int VE, int NV, int MAXT>
+__global__ void __launch_bounds__(MAXT) k_norm_grad_rows(NormArgs A, int packs, int stages) {
+  extern __shared__ uint4 ring[];
+  __shared__ float buf[2][64];
+  const Rows in[3] = {A.x, A.du, A.dadd};
+  RowFeed<T, VE, NV, 3> F;
+  F.stages = stages; F.packs = packs; F.ring = ring; F.nin = A.dadd.p ? 3 : 2;
+  float acc[NV][VE] = {};
+  for (int i = 0; i < stages; ++i) F.request(in, blockIdx.x + (int64_t)i * gridDim.x, A.T, i);
+  int stage = 0, flip = 0;
+  for (int64_t t = blockIdx.x; t < A.T; t += gridDim.x) {
+    F.take(in, t, stage);
+    F.request(in, t + (int64_t)stages * gridDim.x, A.T, stage);
+    stage = stage + 1 == stages ? 0 : stage + 1;
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const int c = threadIdx.x + n * blockDim.x;
+      if (c >= packs) continue;
+      float x[VE], d[VE], w[VE];
+      F.v[0][n].widen(x);
+      F.v[1][n].widen(d);
+      load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
+#pragma unroll
+      for (int j = 0; j < VE; ++j) {
+        s[0] = fmaf(x[j], x[j], s[0]);
+        s[1] = fmaf(d[j] * w[j], x[j], s[1]);
+      }
+    }
+    block_sums<2>(s, buf[flip]);
+    flip ^= 1;
+    const float r = inv_rms(s[0], A.h, A.eps);
+    const float cc = r * r * r * (s[1] / (float)A.h);
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const int c = threadIdx.x + n * blockDim.x;
+      if (c >= packs) continue;
+      float x[VE], d[VE], w[VE], o[VE];
+      F.v[0][n].widen(x);
+      F.v[1][n].widen(d);
+      load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
+#pragma unroll
+      for (int j = 0; j < VE; ++j) {
+        acc[n][j] = fmaf(d[j] * r, x[j], acc[n][j]);
+        o[j] = r * d[j] * w[j] - x[j] * cc;
+      }
+      if (A.dadd.p) {
+        float e[VE];
+        F.v[2][n].widen(e);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) o[j] += e[j];
+      }
+      store_row<T, VE>(A.dx, A.dx_s, t, c, o);
+    }
+  }
+  float* part = A.part + (size_t)blockIdx.x * A.h;
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    const int c = threadIdx.x + n * blockDim.x;
+    if (c < packs)
+#pragma unroll
+      for (int j = 0; j < VE; ++j) part[(size_t)c * VE + j] = acc[n][j];
+  }
+}
+
+template <typename T, int VE, int NV, int MAXT>
+__global__ void __launch_bounds__(MAXT) k_residual_grad_rows(NormArgs A, int packs, int stages, size_t part_step) {
+  extern __shared__ uint4 ring[];
+  __shared__ float buf[2][64];  // taken in turn: a sum's buffer is free again after the next sum's barrier
+  const bool full = A.gate_kind == DEAMOE_GATE_FULL;
+  const Rows in[5] = {A.x, A.y, A.dout, A.du, {full ? A.gate.p : nullptr, A.gate.stride}};
+  RowFeed<T, VE, NV, 5> F;
+  F.stages = stages; F.packs = packs; F.ring = ring; F.nin = full ? 5 : 4;
+  float acc_w[NV][VE] = {}, acc_n[NV][VE] = {}, acc_g[NV][VE] = {};
+  for (int i = 0; i < stages; ++i) F.request(in, blockIdx.x + (int64_t)i * gridDim.x, A.T, i);
+  int stage = 0, flip = 0;
+  for (int64_t t = blockIdx.x; t < A.T; t += gridDim.x) {
+    F.take(in, t, stage);
+    F.request(in, t + (int64_t)stages * gridDim.x, A.T, stage);
+    stage = stage + 1 == stages ? 0 : stage + 1;
+    auto gate = [&](int n, int c, float (&g)[VE]) {
+      if (full) F.v[4][n].widen(g);
+      else load_gate<T, VE>(A, t, c, g);
+    };
+    float ry = 1.f;
+    if (A.post_norm) {
+      float ss[1] = {0.f};
+#pragma unroll
+      for (int n = 0; n < NV; ++n)
+        if ((int)(threadIdx.x + n * blockDim.x) < packs) {
+          float y[VE];
+          F.v[1][n].widen(y);
+#pragma unroll
+          for (int j = 0; j < VE; ++j) ss[0] = fmaf(y[j], y[j], ss[0]);
+        }
+      block_sums<1>(ss, buf[flip]);
+      flip ^= 1;
+      ry = inv_rms(ss[0], A.h, A.eps);
+    }
+    // the sum after the block, recomputed; then the gradient that reaches it
+    float d[NV][VE];
+    float ro = 1.f, co = 0.f;
+    if (A.next_norm) {
+      float s[2] = {0.f, 0.f};
+#pragma unroll
+      for (int n = 0; n < NV; ++n) {
+        const int c = threadIdx.x + n * blockDim.x;
+        if (c >= packs) continue;
+        float x[VE], y[VE], w[VE], g[VE], u[VE], wn[VE];
+        F.v[0][n].widen(x);
+        F.v[1][n].widen(y);
+        F.v[3][n].widen(u);
+        load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
+        load_gains<VE>(A.wn, A.wdt, (int64_t)c * VE, wn);
+        gate(n, c, g);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) {
+          d[n][j] = fmaf(A.a, x[j], A.b * g[j] * (y[j] * ry * w[j]));
+          s[0] = fmaf(d[n][j], d[n][j], s[0]);
+          s[1] = fmaf(u[j] * wn[j], d[n][j], s[1]);
+        }
+      }
+      block_sums<2>(s, buf[flip]);
+      flip ^= 1;
+      ro = inv_rms(s[0], A.h, A.next_eps);
+      co = ro * ro * ro * (s[1] / (float)A.h);
+    }
+    float s[2] = {0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const int c = threadIdx.x + n * blockDim.x;
+      if (c >= packs) continue;
+      float y[VE], w[VE], g[VE], o[VE];
+      F.v[2][n].widen(o);
+      if (A.next_norm) {
+        float u[VE], wn[VE];
+        F.v[3][n].widen(u);
+        load_gains<VE>(A.wn, A.wdt, (int64_t)c * VE, wn);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) {
+          const float sum = d[n][j];
+          acc_n[n][j] = fmaf(u[j] * ro, sum, acc_n[n][j]);
+          o[j] += ro * u[j] * wn[j] - sum * co;
+        }
+      }
+      F.v[1][n].widen(y);
+      load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
+      gate(n, c, g);
+#pragma unroll
+      for (int j = 0; j < VE; ++j) {
+        d[n][j] = o[j];
+        const float dw = A.b * o[j] * w[j];
+        s[0] = fmaf(dw * g[j], y[j], s[0]);
+        s[1] = fmaf(dw * ry, y[j], s[1]);
+        o[j] *= A.a;
+      }
+      store_row<T, VE>(A.dx, A.dx_s, t, c, o);
+    }
+    if (A.post_norm || A.dgate_token) {
+      block_sums<2>(s, buf[flip]);
+      flip ^= 1;
+    }
+    const float cy = A.post_norm ? ry * ry * ry * (s[0] / (float)A.h) : 0.f;
+    if (A.dgate_token && threadIdx.x == 0) A.dgate_token[t] = s[1];
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const int c = threadIdx.x + n * blockDim.x;
+      if (c >= packs) continue;
+      float y[VE], w[VE], g[VE], o[VE];
+      F.v[1][n].widen(y);
+      load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
+      gate(n, c, g);
+      float dg[VE];
+#pragma unroll
+      for (int j = 0; j < VE; ++j) {
+        const float bd = A.b * d[n][j], dv = bd * g[j], yr = y[j] * ry;
+        acc_w[n][j] = fmaf(dv, yr, acc_w[n][j]);
+        dg[j] = bd * yr * w[j];
+        acc_g[n][j] += dg[j];
+        o[j] = ry * dv * w[j] - y[j] * cy;
+      }
+      if (full) store_row<T, VE>(A.dgate, A.dgate_s, t, c, dg);
+      store_row<T, VE>(A.dy, A.dy_s, t, c, o);
+    }
+  }
+  float* part = A.part + (size_t)blockIdx.x * A.h;
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    const int c = threadIdx.x + n * blockDim.x;
+    if (c >= packs) continue;
+#pragma unroll
+    for (int j = 0; j < VE; ++j) {
+      const size_t i = (size_t)c * VE + j;
+      if (A.w) part[i] = acc_w[n][j];
+      if (A.wn) part[part_step + i] = acc_n[n][j];
+      if (A.gate_kind == DEAMOE_GATE_CHANNEL) part[2 * part_step + i] = acc_g[n][j];
+    }
+  }
+}
+
 // ---------------------------------------------------------------- sums over the blocks' partial rows
 
 struct ColumnSums {
   const float* part[3];
   float* out[3];
 };
-// A block adds 32 columns of one array: 8 row groups side by side, then the groups in order.
-__global__ void __launch_bounds__(256) k_column_sums(ColumnSums S, int rows, int h) {
-  __shared__ float acc[8][33];
+// A block adds 32 columns of one array: 32 row groups side by side, then the groups in order.
+__global__ void __launch_bounds__(1024) k_column_sums(ColumnSums S, int rows, int h) {
+  __shared__ float acc[32][33];
   pdl_wait();
   const float* p = S.part[blockIdx.y];
-  float* out = S.out[blockIdx.y];
   const int c = blockIdx.x * 32 + (threadIdx.x & 31), g = threadIdx.x >> 5;
   float s = 0.f;
-  if (c < h)
-    for (int r = g; r < rows; r += 8) s += p[(size_t)r * h + c];
+  if (c < h) {
+#pragma unroll 4
+    for (int r = g; r < rows; r += 32) s += p[(size_t)r * h + c];
+  }
   acc[g][threadIdx.x & 31] = s;
   __syncthreads();
   if (g == 0 && c < h) {
-    for (int i = 1; i < 8; ++i) s += acc[i][threadIdx.x & 31];
-    out[c] = s;
+    for (int i = 1; i < 32; ++i) s += acc[i][threadIdx.x & 31];
+    S.out[blockIdx.y][c] = s;
   }
 }
 
@@ -241,30 +661,114 @@ static bool bad_rows(const void* p, int64_t stride, int32_t h, size_t es) { retu
 
 static deamoe_status_t launch_sums(const ColumnSums& S, int arrays, int rows, int h, cudaStream_t s) {
   if (arrays == 0) return DEAMOE_OK;
-  if (launch_pdl(k_column_sums, dim3((h + 31) / 32, arrays), dim3(256), 0, s, S, rows, h) != cudaSuccess) {
+  if (launch_pdl(k_column_sums, dim3((h + 31) / 32, arrays), dim3(1024), 0, s, S, rows, h) != cudaSuccess) {
     cudaGetLastError();
     return DEAMOE_ERR_CUDA;
   }
   return DEAMOE_OK;
 }
 
-template <typename T> static deamoe_status_t norm_t(const NormArgs& A, cudaStream_t s) {
-  k_norm_any<T><<<(unsigned)A.T, ANY_THREADS, 0, s>>>(A);
-  return cudaGetLastError() == cudaSuccess ? DEAMOE_OK : DEAMOE_ERR_CUDA;
-}
-static int grad_ctas(int64_t T) { return (int)(T < NORM_CTAS ? T : NORM_CTAS); }
+static deamoe_status_t ran() { return cudaGetLastError() == cudaSuccess ? DEAMOE_OK : DEAMOE_ERR_CUDA; }
 
-template <typename T> static deamoe_status_t norm_grad_t(const NormArgs& A, cudaStream_t s) {
-  k_norm_grad_any<T><<<grad_ctas(A.T), ANY_THREADS, 0, s>>>(A);
-  return cudaGetLastError() == cudaSuccess ? DEAMOE_OK : DEAMOE_ERR_CUDA;
+// Lets a kernel use the SM's whole shared memory; once per kernel and device.
+template <typename K> static bool whole_smem(K* fn, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return false;
+  if (done.load(std::memory_order_acquire) >> dev & 1) return true;
+  if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES) != cudaSuccess) return false;
+  done.fetch_or(1ull << dev, std::memory_order_release);
+  return true;
+}
+
+// Whether all of a call's rows and gains can be read 16 bytes at a time.
+template <typename T> static bool wide_call(const NormArgs& A) {
+  bool ok = A.h % (16 / sizeof(T)) == 0;
+  for (const Rows& m : {A.x, A.y, A.dout, A.du, A.dadd})
+    if (m.p) ok = ok && wide_rows(m.p, m.stride, A.T, sizeof(T));
+  if (A.gate_kind == DEAMOE_GATE_FULL) ok = ok && wide_rows(A.gate.p, A.gate.stride, A.T, sizeof(T));
+  if (A.gate_kind == DEAMOE_GATE_CHANNEL) ok = ok && aligned16(A.gate.p);
+  ok = ok && aligned16(A.w) && aligned16(A.wn) && wide_rows(A.out, A.out_s, A.T, sizeof(T)) &&
+       wide_rows(A.u, A.u_s, A.T, sizeof(T)) && wide_rows(A.dx, A.dx_s, A.T, sizeof(T)) &&
+       wide_rows(A.dy, A.dy_s, A.T, sizeof(T));
+  if (A.gate_kind == DEAMOE_GATE_FULL) ok = ok && wide_rows(A.dgate, A.dgate_s, A.T, sizeof(T));
+  return ok;
+}
+
+static unsigned warps_of(int packs, int nv) { return (unsigned)(((packs + nv - 1) / nv + 31) / 32 * 32); }
+// Few rows: one pack a thread, the shortest way through a row.  Many: four, so that the rows in flight on an SM are
+// enough bytes to keep HBM busy.
+static bool few_rows(int64_t T) { return T <= 2 * NORM_SMS; }
+
+#define DEAMOE_ROW_FORMS(KERNEL, ANY)                                                                                   \
+  constexpr int VE = 16 / sizeof(T);                                                                                     \
+  const unsigned grid = (unsigned)A.T;                                                                                   \
+  if (wide_call<T>(A)) {                                                                                                 \
+    const int packs = A.h / VE;                                                                                          \
+    if (packs <= 1024 && (few_rows(A.T) || packs < 128)) {                                                               \
+      KERNEL<T, VE, 1, 1024><<<grid, warps_of(packs, 1), 0, s>>>(A, packs);                                              \
+      return ran();                                                                                                      \
+    }                                                                                                                    \
+    if (packs <= 2048) {                                                                                                 \
+      KERNEL<T, VE, 4, 512><<<grid, warps_of(packs, 4), 0, s>>>(A, packs);                                               \
+      return ran();                                                                                                      \
+    }                                                                                                                    \
+  } else if (A.h <= 2048) {                                                                                              \
+    KERNEL<T, 1, 4, 512><<<grid, warps_of(A.h, 4), 0, s>>>(A, A.h);                                                      \
+    return ran();                                                                                                        \
+  } else if (A.h <= 8192) {                                                                                              \
+    KERNEL<T, 1, 16, 512><<<grid, warps_of(A.h, 16), 0, s>>>(A, A.h);                                                    \
+    return ran();                                                                                                        \
+  }                                                                                                                      \
+  ANY<T><<<grid, ANY_THREADS, 0, s>>>(A);                                                                                \
+  return ran()
+
+template <typename T> static deamoe_status_t norm_t(const NormArgs& A, cudaStream_t s) {
+  DEAMOE_ROW_FORMS(k_norm_rows, k_norm_any);
 }
 template <typename T> static deamoe_status_t residual_t(const NormArgs& A, cudaStream_t s) {
-  k_residual_any<T><<<(unsigned)A.T, ANY_THREADS, 0, s>>>(A);
-  return cudaGetLastError() == cudaSuccess ? DEAMOE_OK : DEAMOE_ERR_CUDA;
+  DEAMOE_ROW_FORMS(k_residual_rows, k_residual_any);
 }
+#undef DEAMOE_ROW_FORMS
+
+// Rows ahead in the ring: what the blocks of an SM can share of its shared memory, four at most.
+static int grad_stages(int h, size_t stage_bytes) {
+  const size_t n = RING_BYTES / grad_blocks_per_sm(h) / stage_bytes;
+  return n > 4 ? 4 : (n < 1 ? 1 : (int)n);
+}
+
+template <typename T> static deamoe_status_t norm_grad_t(const NormArgs& A, cudaStream_t s) {
+  constexpr int VE = 16 / sizeof(T), NV = GRAD_COLUMNS / VE;
+  const int ctas = grad_ctas(A.T, A.h), threads = grad_threads(A.h);
+  if (A.h > GRAD_MAX_WIDTH) {
+    k_norm_grad_any<T><<<ctas, ANY_THREADS, 0, s>>>(A);
+  } else if (wide_call<T>(A)) {
+    static std::atomic<uint64_t> done{0};
+    if (!whole_smem(k_norm_grad_rows<T, VE, NV, 1024>, done)) return DEAMOE_ERR_CUDA;
+    const size_t stage = (size_t)(A.dadd.p ? 3 : 2) * NV * threads * 16;
+    const int stages = grad_stages(A.h, stage);
+    k_norm_grad_rows<T, VE, NV, 1024><<<ctas, threads, stage * stages, s>>>(A, A.h / VE, stages);
+  } else {
+    k_norm_grad_rows<T, 1, GRAD_COLUMNS, 1024><<<ctas, threads, 0, s>>>(A, A.h, 1);
+  }
+  return ran();
+}
+
 template <typename T> static deamoe_status_t residual_grad_t(const NormArgs& A, cudaStream_t s) {
-  k_residual_grad_any<T><<<grad_ctas(A.T), ANY_THREADS, 0, s>>>(A);
-  return cudaGetLastError() == cudaSuccess ? DEAMOE_OK : DEAMOE_ERR_CUDA;
+  constexpr int VE = 16 / sizeof(T), NV = GRAD_COLUMNS / VE;
+  const int ctas = grad_ctas(A.T, A.h), threads = grad_threads(A.h);
+  const size_t step = (size_t)ctas * A.h;
+  if (A.h > GRAD_MAX_WIDTH) {
+    k_residual_grad_any<T><<<ctas, ANY_THREADS, 0, s>>>(A, step);
+  } else if (wide_call<T>(A)) {
+    static std::atomic<uint64_t> done{0};
+    if (!whole_smem(k_residual_grad_rows<T, VE, NV, 1024>, done)) return DEAMOE_ERR_CUDA;
+    const size_t stage = (size_t)(A.gate_kind == DEAMOE_GATE_FULL ? 5 : 4) * NV * threads * 16;
+    const int stages = grad_stages(A.h, stage);
+    k_residual_grad_rows<T, VE, NV, 1024><<<ctas, threads, stage * stages, s>>>(A, A.h / VE, stages, step);
+  } else {
+    k_residual_grad_rows<T, 1, GRAD_COLUMNS, 1024><<<ctas, threads, 0, s>>>(A, A.h, 1, step);
+  }
+  return ran();
 }
 
 }  // namespace deamoe
@@ -275,7 +779,7 @@ extern "C" {
 
 uint64_t deamoe_norm_workspace(int32_t n_token, int32_t hidden) {
   if (n_token <= 0 || hidden <= 0) return 0;
-  return (uint64_t)3 * NORM_CTAS * hidden * sizeof(float);
+  return (uint64_t)3 * grad_ctas(n_token, hidden) * hidden * sizeof(float);
 }
 
 deamoe_status_t deamoe_norm(void* cuda_stream, int32_t dtype, const void* x, int64_t x_stride, int32_t n_token,
@@ -319,7 +823,7 @@ deamoe_status_t deamoe_norm_backward(void* cuda_stream, int32_t dtype, const voi
   if (st != DEAMOE_OK) return st;
   ColumnSums S = {};
   S.part[0] = A.part; S.out[0] = dweight;
-  return launch_sums(S, 1, grad_ctas(n_token), hidden, s);
+  return launch_sums(S, 1, grad_ctas(n_token, hidden), hidden, s);
 }
 
 static deamoe_status_t check_block(int32_t gate_kind, const void* gate, int64_t gate_stride, int32_t hidden, size_t es,
@@ -411,11 +915,11 @@ deamoe_status_t deamoe_norm_residual_backward(
   if (st != DEAMOE_OK) return st;
   ColumnSums S = {};
   int n = 0;
-  const size_t step = (size_t)NORM_CTAS * hidden;
+  const size_t step = (size_t)grad_ctas(n_token, hidden) * hidden;
   if (dweight) { S.part[n] = A.part; S.out[n++] = dweight; }
   if (dnext_weight) { S.part[n] = A.part + step; S.out[n++] = dnext_weight; }
   if (gate_kind == DEAMOE_GATE_CHANNEL) { S.part[n] = A.part + 2 * step; S.out[n++] = reinterpret_cast<float*>(dgate); }
-  return launch_sums(S, n, grad_ctas(n_token), hidden, s);
+  return launch_sums(S, n, grad_ctas(n_token, hidden), hidden, s);
 }
 
 }  // extern "C"
