@@ -487,7 +487,7 @@ def quant_product(codes, scales, x, group, zeros=None, expert_off=None, row_pair
     pe = _vec(expert_off, where, "expert_off", torch.int32, E + 1) if expert_off is not None else None
     pp = _vec(row_pair, where, "row_pair", torch.int32, R) if row_pair is not None else None
     L = lib()
-    need = L.deamoe_quant_workspace(dt, T, n_in)
+    need = L.deamoe_quant_workspace(dt, R, n_in)
     ws = _workspace(need, x.device)
     _done(L.deamoe_quant_product(_raw_stream(_device()), dt, _vec(codes, where, "codes", torch.uint8, E, n_out, n_in // 2), sdt,
                                  _vec(scales, where, "scales", scales.dtype, E, n_out, groups), pz, E, n_out, n_in, group, px,

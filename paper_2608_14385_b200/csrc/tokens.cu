@@ -42,36 +42,6 @@ static __device__ __forceinline__ int warp_rank(unsigned short* cnt, int e, int 
   return old + before;
 }
 
-// Exclusive prefix sums of tot[0..n) in place, tot[n] = the total.  All threads of the block; ends with a barrier.
-static __device__ void block_exclusive_scan(int* tot, int n, int* warp_sums) {
-  const int nt = blockDim.x, per = (n + nt - 1) / nt;
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, warps = nt >> 5;
-  const int lo = min(n, (int)threadIdx.x * per), hi = min(n, lo + per);
-  int s = 0;
-  for (int i = lo; i < hi; ++i) s += tot[i];
-  int x = s;
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
-  }
-  if (lane == 31) warp_sums[w] = x;
-  __syncthreads();
-  int base = 0, all = 0;
-  for (int i = 0; i < warps; ++i) {
-    if (i < w) base += warp_sums[i];
-    all += warp_sums[i];
-  }
-  int run = base + x - s;
-  for (int i = lo; i < hi; ++i) {
-    const int c = tot[i];
-    tot[i] = run;
-    run += c;
-  }
-  if (threadIdx.x == 0) tot[n] = all;
-  __syncthreads();
-}
-
 __global__ void __launch_bounds__(1024) k_sort_small(const int32_t* __restrict__ idx, int P, int n, int warps,
                                                      int32_t* __restrict__ expert_off, int32_t* __restrict__ pair_row,
                                                      int32_t* __restrict__ row_pair) {

@@ -67,7 +67,7 @@ def test_norms():
 
 
 def test_quant():
-    need = binding.lib().deamoe_quant_workspace(1, 4, 256)
+    need = binding.lib().deamoe_quant_workspace(1, 8, 256)
     good = dict(s=None, dt=1, codes=A, sdt=1, scales=B, zeros=None, E=8, N=64, K=256, group=64, x=D, xs=256, T=4, off=E, pair=W, ppt=2,
                 R=8, swiglu=0, out=0x60000, os=64, ws=0x70000, size=need)
     for change, want in ((dict(dt=7), INVALID), (dict(sdt=7), INVALID), (dict(codes=A + 8), INVALID), (dict(codes=None), INVALID),
