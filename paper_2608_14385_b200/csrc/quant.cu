@@ -7,12 +7,12 @@
 //
 // Tensor cores: mma.m16n8k16 with 16 matrix rows as M and up to 8 tokens as N (legacy path: with this few tokens the
 // instruction rate it needs is a fraction of what it has, and its A operand comes from registers, where the codes
-// have to be widened anyway).  q - z is a whole number of at most 15, exact in any 16-bit type; fp16 is used because
-// its 10 mantissa bits let two nibbles of a 16-bit half be widened in place (1024 + q and 1024 + 16 q), one shift
-// less per pair than bf16's 7 bits.  x therefore becomes fp16 as well, in a kernel of its own: each row scaled by a
-// power of two to a largest magnitude of 2^14..2^15, so that fp16's range costs nothing (values below 2^-39 of the
-// row's largest lose bits, far under fp32's own resolution of the sum); bf16 values fit exactly, fp32 values as two
-// parts (2^-23 relative).
+// have to be widened anyway).  Widening is an AND and a subtraction a pair: a nibble in the low bits of a 16-bit half IS
+// the fp16 subnormal q 2^-24, and in the next four bits q 2^-20; q - z is exact there, and tensor cores multiply
+// subnormals exactly.  x becomes fp16 in a kernel of its own: each row scaled by a power of two to a largest magnitude
+// of 2^14..2^15, the columns that meet 2^-20 by another 2^-4, so that fp16's range costs nothing (values below 2^-35
+// of the row's largest lose bits, far under fp32's own resolution of the sum); bf16 values fit exactly, fp32 values as
+// two parts (2^-23 relative).
 #include <atomic>
 #include <climits>
 #include <cuda_fp16.h>
@@ -37,9 +37,9 @@ struct QuantArgs {
   int n_expert, n_out, n_in, groups, n_token, ppt, n_rows, swiglu, scale_f32;
   int steps;        // column steps of a row
   int wk;           // warps that share a row tile's columns (the others of the block take other tiles)
-  int tile_groups;  // blocks of QW / wk row tiles a matrix
+  int tile_groups;  // blocks of QW / wk warp tiles (16 MT rows) a matrix
   __half* xh;       // [n_rows][planes][steps * QCOLS]
-  int32_t* xe;      // [n_rows] exponent the row was scaled by
+  int32_t* xe;      // [n_rows] exponent the products are scaled by
 };
 
 static __device__ __forceinline__ float quant_scale(const QuantArgs& A, size_t i) {
@@ -47,8 +47,8 @@ static __device__ __forceinline__ float quant_scale(const QuantArgs& A, size_t i
                      : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(A.scales)[i]);
 }
 
-// x in the order of the rows, as fp16 scaled by 2^-exponent, 8 columns in the order 0 4 1 5 2 6 3 7 (the order in
-// which the codes of a 32-bit word are widened).  One block a row; a row without a source is zero.
+// x in the order of the rows, as fp16 scaled by 2^-e, 8 columns in the order 0 4 1 5 2 6 3 7 (the order in which the
+// codes of a 32-bit word are widened; 1 5 3 7 by another 1/16).  One block a row; a row without a source is zero.
 template <typename T, int PLANES> __global__ void __launch_bounds__(256) k_quant_x(QuantArgs A) {
   __shared__ float buf[32];
   const int64_t r = blockIdx.x;
@@ -68,7 +68,7 @@ template <typename T, int PLANES> __global__ void __launch_bounds__(256) k_quant
   __syncthreads();
   for (int i = 0; i < 8; ++i) top = fmaxf(top, buf[i]);
   const int e = top > 0.f ? ilogbf(top) - 14 : 0;
-  if (threadIdx.x == 0) A.xe[r] = e;
+  if (threadIdx.x == 0) A.xe[r] = e + 24;
   const int width = A.steps * QCOLS;
   __half* out = A.xh + r * PLANES * width;
   for (int c = threadIdx.x; c < width / 8; c += 256) {
@@ -76,7 +76,7 @@ template <typename T, int PLANES> __global__ void __launch_bounds__(256) k_quant
 #pragma unroll
     for (int p = 0; p < 8; ++p) {
       const int col = c * 8 + (p >> 1) + (p & 1) * 4;
-      const float v = have && col < A.n_in ? scalbnf(to_f<T>(x[col]), -e) : 0.f;
+      const float v = have && col < A.n_in ? scalbnf(to_f<T>(x[col]), (p & 2) ? -e - 4 : -e) : 0.f;
       hi.h[p] = __float2half_rn(v);
       const float rest = v - __half2float(hi.h[p]);
       lo.h[p] = __float2half_rn(isfinite(v) ? rest : 0.f);
@@ -92,194 +92,271 @@ static __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint3
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-static __device__ __forceinline__ uint32_t half2_bits(__half2 h) { return *reinterpret_cast<uint32_t*>(&h); }
-static __device__ __forceinline__ __half2 bits_half2(uint32_t u) { return *reinterpret_cast<__half2*>(&u); }
-static __device__ __forceinline__ uint32_t pick(uint32_t w, uint32_t mask) { return (w & mask) | 0x64006400u; }  // one LOP3
-
-// The 8 codes of a word minus the zero point, as four half pairs: columns (0 4) (1 5) (2 6) (3 7).
-// low = 1024 + z, high = -(64 + z): 1024 + q - (1024 + z) and (1024 + 16 q) / 16 - (64 + z), both exact.
-static __device__ __forceinline__ void widen(uint32_t w, __half2 low, __half2 high, uint32_t (&p)[4]) {
-  const __half2 sixteenth = __float2half2_rn(0.0625f);
-  const uint32_t v = w >> 8;
-  p[0] = half2_bits(__hsub2(bits_half2(pick(w, 0x000f000fu)), low));
-  p[1] = half2_bits(__hfma2(bits_half2(pick(w, 0x00f000f0u)), sixteenth, high));
-  p[2] = half2_bits(__hsub2(bits_half2(pick(v, 0x000f000fu)), low));
-  p[3] = half2_bits(__hfma2(bits_half2(pick(v, 0x00f000f0u)), sixteenth, high));
+// The 8 codes of a word less the zero point as four pairs of fp16 subnormals: columns (0 4) (1 5) (2 6) (3 7), (q - z)
+// times 2^-24 and 2^-20 in turn.  z: the zero point in the low bits of both halves.
+static __device__ __forceinline__ uint32_t less(uint32_t a, uint32_t b) {
+  const __half2 d = __hsub2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&d);
+}
+static __device__ __forceinline__ void widen(uint32_t w, uint32_t z, uint32_t (&p)[4]) {
+  const uint32_t v = w >> 8, z4 = z << 4;
+  p[0] = less(w & 0x000f000fu, z);
+  p[1] = less(w & 0x00f000f0u, z4);
+  p[2] = less(v & 0x000f000fu, z);
+  p[3] = less(v & 0x00f000f0u, z4);
+}
+static __device__ __forceinline__ uint4 load_b128(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
 }
 
-// A block takes a contiguous share of the items (expert, group of row tiles, pass of 8 NT rows); its warps split an
-// item's columns (wk of them a tile).  Every warp streams its own codes, `DEPTH` steps of 16 rows x 128 columns ahead
-// and across items, into its own part of shared memory; nothing is shared between warps but the sums at an item's end.
-template <typename T, int PLANES, int NT, int NG, int DEPTH>
+// Where a warp is in the block's items: expert, group of warp tiles, pass of 16 rows (innermost: the passes of a tile
+// find its codes in the caches).
+struct QuantAt {
+  int item, e, tg, pass, passes;
+};
+static __device__ __forceinline__ void quant_enter(QuantAt& at, const int* first, int tile_groups) {
+  while (at.item >= first[at.e + 1]) ++at.e;
+  at.passes = (first[at.e + 1] - first[at.e]) / tile_groups;
+}
+static __device__ __forceinline__ void quant_next(QuantAt& at, int end, const int* first, int tile_groups) {
+  ++at.item;
+  if (++at.pass < at.passes) return;
+  at.pass = 0;
+  if (++at.tg < tile_groups) return;
+  at.tg = 0;
+  if (at.item < end) quant_enter(at, first, tile_groups);
+}
+
+constexpr int Q_TOKENS = 16;  // tokens of a pass
+
+// A block takes a contiguous share of the items; its warps split an item's columns (wk of them a tile of 16 MT rows).
+// Every warp streams its own codes, DEPTH steps of 16 MT rows x 128 columns ahead and across items, into its own part
+// of shared memory; nothing is shared between warps but the sums at an item's end.
+template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
+  static constexpr int STEP = MT * 1024, NB = 2 * MT;  // NB: blocks of 8 matrix rows in a warp tile
+  const QuantArgs& A;
+  const int* first;
+  int i1, wr, c0, c1, tiles_per, width, lane, g, j;
+  uint32_t ring_at;
+  size_t pair_rows, next_rows;  // matrix rows from block 2 m to block 2 m + 1, and to block 2 m + 2
+  // the codes' cursor
+  QuantAt ahead;
+  int p_c, p_slot, p_out;  // p_out: output column of row g of block 0
+  const uint8_t* p_code;   // this lane's 16-byte piece of it
+
+  __device__ __forceinline__ QuantWarp(const QuantArgs& a, const int* f, const QuantAt& at, int end, int w, int ln, uint32_t ring)
+      : A(a), first(f), i1(end), lane(ln), g(ln >> 2), j(ln & 3), ring_at(ring), ahead(at), p_slot(0) {
+    tiles_per = QW / A.wk;
+    wr = w / A.wk;
+    const int share = w - wr * A.wk;
+    c0 = A.steps * share / A.wk;
+    c1 = A.steps * (share + 1) / A.wk;
+    width = A.swiglu ? A.n_out / 2 : A.n_out;
+    pair_rows = A.swiglu ? width : 8;
+    next_rows = A.swiglu ? 8 : 16;
+    p_c = c0;
+  }
+  // output column of row g of the tile's block 0; block b adds out_of(b)
+  __device__ __forceinline__ int out_at(const QuantAt& at) const {
+    return ((at.tg * tiles_per + wr) * MT) * (A.swiglu ? 8 : 16) + g;
+  }
+  __device__ __forceinline__ int out_of(int b) const { return A.swiglu ? (b >> 1) * 8 : b * 8; }
+  __device__ __forceinline__ size_t rows_to(int b) const { return (b >> 1) * next_rows + (b & 1) * pair_rows; }
+
+  __device__ __forceinline__ void aim() {
+    p_out = out_at(ahead);
+    p_code = A.codes + ((size_t)ahead.e * A.n_out + p_out) * (A.n_in / 2) + (size_t)c0 * 64 + j * 16;
+  }
+  __device__ __forceinline__ void request() {
+    if (ahead.item < i1) {
+      const bool in = p_c * QCOLS + j * 32 < A.n_in;
+      const uint32_t to = ring_at + p_slot * STEP + g * 64 + ((j ^ ((g >> 1) & 3)) * 16);
+      const size_t half = A.n_in / 2;
+#pragma unroll
+      for (int b = 0; b < NB; ++b) {
+        const bool have = in && p_out + out_of(b) < width;  // else nothing is read, zeros are written
+        const uint8_t* from = have ? p_code + rows_to(b) * half : A.codes;
+        asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(to + b * 512), "l"(from), "r"(have ? 16 : 0)
+                     : "memory");
+      }
+      p_code += 64;
+      if (++p_c == c1) {
+        p_c = c0;
+        quant_next(ahead, i1, first, A.tile_groups);
+        if (ahead.item < i1) aim();
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    p_slot = p_slot + 1 == DEPTH ? 0 : p_slot + 1;
+  }
+
+  // The warp's columns of one item for NT * 8 tokens: acc[mt][t] = this warp's share of the products.
+  template <int NT>
+  __device__ __forceinline__ void item(const QuantAt& at, int row0, int rows, int& slot, float (&acc)[MT][2][4]) {
+    const int xw = A.steps * QCOLS, o0 = out_at(at);
+    size_t s_at = ((size_t)at.e * A.n_out + o0) * A.groups + (size_t)c0 * NG;
+    int grp_at = c0 * NG;
+    const int grp_end = min(c1 * NG, A.groups);
+    // scale and zero point of the group to come, for the lane's rows
+    float sc_next[NB];
+    uint32_t z_next[NB];
+    auto fetch = [&]() {
+      if (grp_at < grp_end) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+          if (o0 + out_of(b) < width) {
+            const size_t i = s_at + rows_to(b) * A.groups;
+            sc_next[b] = quant_scale(A, i);
+            if constexpr (Z) z_next[b] = A.zeros[i];
+          }
+      }
+      ++s_at;
+      ++grp_at;
+    };
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      sc_next[b] = 0.f;
+      z_next[b] = 8;
+    }
+    fetch();
+    // tokens past the last take the last one's values: their sums are not looked at
+    const __half* xp[NT];
+    uint4 next[NT][PLANES];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      xp[t] = A.xh + (size_t)(row0 + min(t * 8 + g, rows - 1)) * PLANES * xw + (size_t)c0 * QCOLS + j * 8;
+#pragma unroll
+      for (int p = 0; p < PLANES; ++p) next[t][p] = load_b128(xp[t] + (size_t)p * xw);
+    }
+#pragma unroll 1
+    for (int c = c0; c < c1; ++c) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
+      __syncwarp();
+      uint32_t code[NB][4];
+      const uint32_t from = ring_at + slot * STEP + (lane & 7) * 64 + (((lane >> 3) ^ (((lane & 7) >> 1) & 3)) * 16);
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+        asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                     : "=r"(code[b][0]), "=r"(code[b][1]), "=r"(code[b][2]), "=r"(code[b][3]) : "r"(from + b * 512) : "memory");
+      __syncwarp();
+      request();  // the slot just read
+      slot = slot + 1 == DEPTH ? 0 : slot + 1;
+      float sc[NB];
+      uint32_t z[NB];
+      float grp[MT][NT][4];
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        if (m * NG % 4 == 0) {  // a group begins
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            sc[b] = sc_next[b];
+            z[b] = Z ? (z_next[b] & 15) * 0x00010001u : 0x00080008u;
+          }
+          fetch();
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int t = 0; t < NT; ++t) grp[mt][t][0] = grp[mt][t][1] = grp[mt][t][2] = grp[mt][t][3] = 0.f;
+        }
+        uint4 now[NT][PLANES];
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+          for (int p = 0; p < PLANES; ++p) {
+            now[t][p] = next[t][p];
+            if (m < 3 || c + 1 < c1) next[t][p] = load_b128(xp[t] + (size_t)p * xw + (m + 1) * 32);
+          }
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) {
+          uint32_t lo[4], hi[4];
+          widen(code[2 * mt][m], z[2 * mt], lo);
+          widen(code[2 * mt + 1][m], z[2 * mt + 1], hi);
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p) {
+              mma_f16(grp[mt][t], lo[0], hi[0], lo[1], hi[1], now[t][p].x, now[t][p].y);
+              mma_f16(grp[mt][t], lo[2], hi[2], lo[3], hi[3], now[t][p].z, now[t][p].w);
+            }
+        }
+        if ((m + 1) * NG % 4 == 0 && (NG == 1 || c * NG + m * NG / 4 < A.groups)) {  // a group ends (the last step may have fewer)
+#pragma unroll
+          for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[mt][t][i] = fmaf(sc[2 * mt + (i >> 1)], grp[mt][t][i], acc[mt][t][i]);
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < NT; ++t) xp[t] += QCOLS;
+    }
+  }
+};
+
+template <typename T, int PLANES, int MT, int NG, bool Z, int DEPTH>
 __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int warp_sums[QW];
-  uint8_t* ring = smem + (threadIdx.x >> 5) * (DEPTH * 1024);
-  float4* sums = reinterpret_cast<float4*>(smem + QW * DEPTH * 1024);     // [2][QW][NT][32]
-  int* first = reinterpret_cast<int*>(sums + 2 * QW * NT * 32);           // [n_expert + 1] first item of each expert
-  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  const int g = lane >> 2, j = lane & 3;
-  const int R = A.n_rows;
+  float4* sums = reinterpret_cast<float4*>(smem + QW * DEPTH * MT * 1024);  // [QW][MT][2][32]
+  int* first = reinterpret_cast<int*>(sums + QW * MT * 2 * 32);            // [n_expert + 1] first item of each expert
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, R = A.n_rows;
   auto row_begin = [&](int e) { return A.expert_off ? min(max(A.expert_off[e], 0), R) : 0; };
   auto row_end = [&](int e) { return A.expert_off ? min(max(A.expert_off[e + 1], 0), R) : R; };
   for (int e = threadIdx.x; e < A.n_expert; e += QW * 32) {
     const int rows = max(row_end(e) - row_begin(e), 0);
-    first[e] = (rows + 8 * NT - 1) / (8 * NT) * A.tile_groups;
+    first[e] = (rows + Q_TOKENS - 1) / Q_TOKENS * A.tile_groups;
   }
   __syncthreads();
   block_exclusive_scan(first, A.n_expert, warp_sums);
   const int total = first[A.n_expert];
   const int i0 = (int)((int64_t)total * blockIdx.x / gridDim.x), i1 = (int)((int64_t)total * (blockIdx.x + 1) / gridDim.x);
-  const int wr = w / A.wk, wkk = w - wr * A.wk, tiles_per = QW / A.wk;
-  const int c0 = A.steps * wkk / A.wk, c1 = A.steps * (wkk + 1) / A.wk;
-  const int width = A.swiglu ? A.n_out / 2 : A.n_out;
-  const int tile_rows = A.swiglu ? 8 : 16;  // output columns of a tile
-
-  int e_start = 0;
+  if (i0 == i1) return;
+  const int tiles_per = QW / A.wk;
+  QuantAt at;
   {
     int lo = 0, hi = A.n_expert;  // the last e with first[e] <= i0
     while (hi - lo > 1) {
       const int m = (lo + hi) / 2;
       if (first[m] <= i0) lo = m; else hi = m;
     }
-    e_start = lo;
+    at.item = i0;
+    at.e = lo;
+    quant_enter(at, first, A.tile_groups);
+    at.tg = (i0 - first[at.e]) / at.passes;
+    at.pass = (i0 - first[at.e]) - at.tg * at.passes;
   }
-  auto tile_of = [&](int item, int e, int& pass) {
-    const int local = item - first[e], passes = (first[e + 1] - first[e]) / A.tile_groups;
-    const int tg = passes == 1 ? local : local / passes;
-    pass = local - tg * passes;
-    return tg * tiles_per + wr;
-  };
-  // matrix row of tile row r, or -1
-  auto matrix_row = [&](int tile, int r) {
-    if (A.swiglu) {
-      const int i = tile * 8 + (r & 7);
-      return i < width ? (r < 8 ? i : width + i) : -1;
-    }
-    const int i = tile * 16 + r;
-    return i < width ? i : -1;
-  };
-
-  // -- the codes' cursor
-  int p_item = i0, p_e = e_start, p_c = c0, p_slot = 0;
-  const uint8_t *p_lo = nullptr, *p_hi = nullptr;  // this lane's 16-byte piece of rows g and g + 8, or null
-  auto p_enter = [&]() {
-    if (p_item >= i1 || c0 == c1) return;
-    while (p_item >= first[p_e + 1]) ++p_e;
-    int pass;
-    const int tile = tile_of(p_item, p_e, pass);
-    const int lo = matrix_row(tile, g), hi = matrix_row(tile, g + 8);
-    const size_t base = (size_t)p_e * A.n_out, half = A.n_in / 2;
-    p_lo = lo >= 0 ? A.codes + (base + lo) * half + j * 16 : nullptr;
-    p_hi = hi >= 0 ? A.codes + (base + hi) * half + j * 16 : nullptr;
-  };
-  const uint32_t ring_at = (uint32_t)__cvta_generic_to_shared(ring);
-  const uint32_t put_at = ring_at + g * 64 + ((j ^ ((g >> 1) & 3)) * 16);
-  auto p_request = [&]() {
-    if (p_item < i1 && c0 < c1) {
-      const bool in = p_c * QCOLS + j * 32 < A.n_in;
-      const uint32_t to = put_at + p_slot * 1024;
-      const uint8_t* lo = in && p_lo ? p_lo + (size_t)p_c * 64 : A.codes;
-      const uint8_t* hi = in && p_hi ? p_hi + (size_t)p_c * 64 : A.codes;
-      const int nlo = in && p_lo ? 16 : 0, nhi = in && p_hi ? 16 : 0;
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to), "l"(lo), "r"(nlo) : "memory");
-      asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + 512), "l"(hi), "r"(nhi) : "memory");
-      if (++p_c == c1) {
-        p_c = c0;
-        ++p_item;
-        p_enter();
-      }
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-    p_slot = p_slot + 1 == DEPTH ? 0 : p_slot + 1;
-  };
-  p_enter();
+  const int width = A.swiglu ? A.n_out / 2 : A.n_out;
+  QuantWarp<PLANES, MT, NG, Z, DEPTH> W(A, first, at, i1, w, lane, (uint32_t)__cvta_generic_to_shared(smem + w * (DEPTH * MT * 1024)));
+  W.aim();
 #pragma unroll 1
-  for (int i = 0; i < DEPTH; ++i) p_request();
+  for (int i = 0; i < DEPTH; ++i) W.request();
   pdl_wait();  // x in fp16
 
-  // -- the items
-  const uint32_t get_at = ring_at + (lane & 7) * 64 + (((lane >> 3) ^ (((lane & 7) >> 1) & 3)) * 16);
-  const int xw = A.steps * QCOLS;
-  int slot = 0, flip = 0, e = e_start;
-  for (int item = i0; item < i1; ++item, flip ^= 1) {
-    while (item >= first[e + 1]) ++e;
-    int pass;
-    const int tile = tile_of(item, e, pass);
-    const int r_lo = max(matrix_row(tile, g), 0), r_hi = max(matrix_row(tile, g + 8), 0);
-    const size_t s_lo = ((size_t)e * A.n_out + r_lo) * A.groups, s_hi = ((size_t)e * A.n_out + r_hi) * A.groups;
-    const int row0 = row_begin(e) + pass * 8 * NT, rows = min(row_end(e) - row0, 8 * NT);
-    const __half* xp = A.xh + (size_t)(row0 + g) * PLANES * xw + j * 8;
-    float acc[NT][4] = {};
-    for (int c = c0; c < c1; ++c) {
-      // scales and zero points of the step's groups (the last step may have fewer)
-      float sl[NG], sh[NG];
-      int zl[NG], zh[NG];
+  int slot = 0;
+  for (; at.item < i1; quant_next(at, i1, first, A.tile_groups)) {
+    const int row0 = row_begin(at.e) + at.pass * Q_TOKENS, rows = min(row_end(at.e) - row0, Q_TOKENS);
+    float acc[MT][2][4] = {};
+    if (rows <= 8) W.template item<1>(at, row0, rows, slot, acc);
+    else W.template item<2>(at, row0, rows, slot, acc);
+    // join the warps' column shares, in order
+    float4* mine = sums + (size_t)w * MT * 2 * 32 + lane;
 #pragma unroll
-      for (int k = 0; k < NG; ++k) {
-        const int grp = c * NG + k;
-        const bool in = grp < A.groups;
-        sl[k] = in ? quant_scale(A, s_lo + grp) : 0.f;
-        sh[k] = in ? quant_scale(A, s_hi + grp) : 0.f;
-        zl[k] = in && A.zeros ? A.zeros[s_lo + grp] & 15 : 8;
-        zh[k] = in && A.zeros ? A.zeros[s_hi + grp] & 15 : 8;
-      }
-      asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
-      __syncwarp();
-      uint32_t lo[4], hi[4];
-      const uint32_t from = get_at + slot * 1024;
-      asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-                   : "=r"(lo[0]), "=r"(lo[1]), "=r"(lo[2]), "=r"(lo[3]) : "r"(from) : "memory");
-      asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-                   : "=r"(hi[0]), "=r"(hi[1]), "=r"(hi[2]), "=r"(hi[3]) : "r"(from + 512) : "memory");
-      __syncwarp();
-      p_request();  // the slot just read
-      slot = slot + 1 == DEPTH ? 0 : slot + 1;
-      float grp[NT][4] = {};
-      const __half* xc = xp + (size_t)c * QCOLS;
+    for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
-      for (int m = 0; m < 4; ++m) {
-        const int k = m * NG / 4;
-        uint32_t pl[4], ph[4];
-        widen(lo[m], __half2half2(__ushort_as_half(0x6400 | zl[k])), __half2half2(__ushort_as_half(0xd400 | zl[k] << 4)), pl);
-        widen(hi[m], __half2half2(__ushort_as_half(0x6400 | zh[k])), __half2half2(__ushort_as_half(0xd400 | zh[k] << 4)), ph);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-          if (NT > 1 && t * 8 >= rows) break;
-#pragma unroll
-          for (int p = 0; p < PLANES; ++p) {
-            uint4 b = make_uint4(0, 0, 0, 0);
-            if (t * 8 + g < rows)
-              b = *reinterpret_cast<const uint4*>(xc + (size_t)(t * 8 * PLANES + p) * xw + m * 32);
-            mma_f16(grp[t], pl[0], ph[0], pl[1], ph[1], b.x, b.y);
-            mma_f16(grp[t], pl[2], ph[2], pl[3], ph[3], b.z, b.w);
-          }
-        }
-        if ((m + 1) * NG % 4 == 0 && c * NG + k < A.groups) {  // a group ends
-#pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            acc[t][0] = fmaf(sl[k], grp[t][0], acc[t][0]);
-            acc[t][1] = fmaf(sl[k], grp[t][1], acc[t][1]);
-            acc[t][2] = fmaf(sh[k], grp[t][2], acc[t][2]);
-            acc[t][3] = fmaf(sh[k], grp[t][3], acc[t][3]);
-            grp[t][0] = grp[t][1] = grp[t][2] = grp[t][3] = 0.f;
-          }
-        }
-      }
-    }
-    // join the warps' column shares, in order; the other buffer is still being read by slower warps
-    float4* mine = sums + ((size_t)flip * QW + w) * NT * 32 + lane;
-#pragma unroll
-    for (int t = 0; t < NT; ++t) mine[t * 32] = make_float4(acc[t][0], acc[t][1], acc[t][2], acc[t][3]);
+      for (int t = 0; t < 2; ++t)
+        if (t * 8 < rows) mine[(mt * 2 + t) * 32] = make_float4(acc[mt][t][0], acc[mt][t][1], acc[mt][t][2], acc[mt][t][3]);
     __syncthreads();
     // a thread: one token, one tile row g and its partner g + 8
-    for (int i = threadIdx.x; i < tiles_per * NT * 64; i += QW * 32) {
-      const int h = i & 1, l = (i >> 1) & 31, t = (i >> 6) % NT, tr = (i >> 6) / NT;
+    for (int i = threadIdx.x; i < tiles_per * MT * 128; i += QW * 32) {
+      const int h = i & 1, l = (i >> 1) & 31, t = (i >> 6) & 1, mt = (i >> 7) % MT, tr = (i >> 7) / MT;
       const int token = t * 8 + (l & 3) * 2 + h;
       if (token >= rows) continue;
       float a = 0.f, b = 0.f;
       for (int k = 0; k < A.wk; ++k) {
-        const float* v = reinterpret_cast<const float*>(sums + ((size_t)flip * QW + tr * A.wk + k) * NT * 32 + t * 32 + l);
+        const float* v = reinterpret_cast<const float*>(sums + (((size_t)tr * A.wk + k) * MT * 2 + mt * 2 + t) * 32 + l);
         a += v[h];
         b += v[h + 2];
       }
@@ -288,20 +365,29 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
       a = scalbnf(a, ex);
       b = scalbnf(b, ex);
       T* out = reinterpret_cast<T*>(A.out) + r * A.os;
-      const int i_tile = (tile - wr + tr) * tile_rows + (l >> 2);
+      const int t16 = (at.tg * tiles_per + tr) * MT + mt;
       if (A.swiglu) {
-        if (i_tile < width) out[i_tile] = from_f<T>(a / (1.f + expf(-a)) * b);
+        const int o = t16 * 8 + (l >> 2);
+        if (o < width) out[o] = from_f<T>(a / (1.f + expf(-a)) * b);
       } else {
-        if (i_tile < width) out[i_tile] = from_f<T>(a);
-        if (i_tile + 8 < width) out[i_tile + 8] = from_f<T>(b);
+        const int o = t16 * 16 + (l >> 2);
+        if (o < width) out[o] = from_f<T>(a);
+        if (o + 8 < width) out[o + 8] = from_f<T>(b);
       }
     }
+    __syncthreads();
   }
 }
 
-template <typename T, int NG> static deamoe_status_t quant_t(const QuantArgs& A, cudaStream_t s) {
+template <typename T, int NG> static deamoe_status_t quant_t(QuantArgs& A, cudaStream_t s) {
   constexpr int PLANES = sizeof(T) == 4 ? 2 : 1;
-  auto run = [&](auto kernel, int nt, int depth, std::atomic<uint64_t>& done) {
+  const int tiles16 = A.swiglu ? (A.n_out / 2 + 7) / 8 : (A.n_out + 15) / 16;
+  const int active = A.n_expert < A.n_rows ? A.n_expert : A.n_rows;
+  // Two row tiles a warp share its x values and loop; one where that would leave blocks without work
+  const int mt = (int64_t)(tiles16 / 2) * active >= Q_GRID ? 2 : 1;
+  const int per = QW / A.wk * mt;
+  A.tile_groups = (tiles16 + per - 1) / per;
+  auto run = [&](auto kernel, int depth, std::atomic<uint64_t>& done) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!(done.load(std::memory_order_acquire) >> dev & 1)) {
@@ -309,14 +395,16 @@ template <typename T, int NG> static deamoe_status_t quant_t(const QuantArgs& A,
       if (e != cudaSuccess) return e;
       done.fetch_or(1ull << dev, std::memory_order_release);
     }
-    const size_t smem = (size_t)QW * depth * 1024 + 2 * QW * nt * 512 + (size_t)(A.n_expert + 1) * 4;
+    const size_t smem = (size_t)QW * depth * mt * 1024 + (size_t)QW * mt * 1024 + (size_t)(A.n_expert + 1) * 4;
     k_quant_x<T, PLANES><<<A.n_rows, 256, 0, s>>>(A);
     const cudaError_t e = cudaGetLastError();
     return e != cudaSuccess ? e : launch_pdl(kernel, dim3(Q_GRID), dim3(QW * 32), smem, s, A);
   };
-  static std::atomic<uint64_t> done[2];
-  const cudaError_t e = A.n_rows <= 8 ? run(k_quant<T, PLANES, 1, NG, 10>, 1, 10, done[0])
-                                      : run(k_quant<T, PLANES, 4, NG, 8>, 4, 8, done[1]);
+  static std::atomic<uint64_t> done[4];
+  const cudaError_t e = mt == 2 ? (A.zeros ? run(k_quant<T, PLANES, 2, NG, true, 5>, 5, done[0])
+                                           : run(k_quant<T, PLANES, 2, NG, false, 5>, 5, done[1]))
+                                : (A.zeros ? run(k_quant<T, PLANES, 1, NG, true, 9>, 9, done[2])
+                                           : run(k_quant<T, PLANES, 1, NG, false, 9>, 9, done[3]));
   if (e == cudaSuccess) return DEAMOE_OK;
   cudaGetLastError();
   return DEAMOE_ERR_CUDA;
@@ -365,9 +453,8 @@ deamoe_status_t deamoe_quant_product(void* cuda_stream, int32_t dtype, const uin
   A.wk = QW;
   while (A.wk > A.steps) A.wk /= 2;
   const int tiles = swiglu ? (width + 7) / 8 : (width + 15) / 16;
-  A.tile_groups = (tiles + QW / A.wk - 1) / (QW / A.wk);
   // items are counted in 32 bits (an expert's last pass may be short, hence one more each)
-  if ((int64_t)A.tile_groups * ((int64_t)n_rows / 8 + n_expert) > INT_MAX) return DEAMOE_ERR_BATCH;
+  if ((int64_t)tiles * ((int64_t)n_rows / Q_TOKENS + n_expert) > INT_MAX) return DEAMOE_ERR_BATCH;
   A.xh = reinterpret_cast<__half*>(workspace);
   A.xe = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(workspace) +
                                     (size_t)n_rows * A.steps * QCOLS * (dtype == DEAMOE_F32 ? 4 : 2));
