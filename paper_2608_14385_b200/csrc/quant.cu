@@ -39,13 +39,8 @@ struct QuantArgs {
   int wk;           // warps that share a row tile's columns (the others of the block take other tiles)
   int tile_groups;  // blocks of QW / wk warp tiles (16 MT rows) a matrix
   __half* xh;       // [n_rows][planes][steps * QCOLS]
-  int32_t* xe;      // [n_rows] exponent the products are scaled by
+  int32_t* xe;      // [2][n_rows] two powers of two (fp32 bits) that undo the row's scaling
 };
-
-static __device__ __forceinline__ float quant_scale(const QuantArgs& A, size_t i) {
-  return A.scale_f32 ? reinterpret_cast<const float*>(A.scales)[i]
-                     : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(A.scales)[i]);
-}
 
 // x in the order of the rows, as fp16 scaled by 2^-e, 8 columns in the order 0 4 1 5 2 6 3 7 (the order in which the
 // codes of a 32-bit word are widened; 1 5 3 7 by another 1/16).  One block a row; a row without a source is zero.
@@ -68,7 +63,11 @@ template <typename T, int PLANES> __global__ void __launch_bounds__(256) k_quant
   __syncthreads();
   for (int i = 0; i < 8; ++i) top = fmaxf(top, buf[i]);
   const int e = top > 0.f ? ilogbf(top) - 14 : 0;
-  if (threadIdx.x == 0) A.xe[r] = e + 24;
+  if (threadIdx.x == 0) {  // 2^(e + 24) as two factors, each in fp32's range
+    const int half = (e + 24) / 2;
+    A.xe[r] = (127 + half) << 23;
+    A.xe[(size_t)A.n_rows + r] = (127 + (e + 24) - half) << 23;
+  }
   const int width = A.steps * QCOLS;
   __half* out = A.xh + r * PLANES * width;
   for (int c = threadIdx.x; c < width / 8; c += 256) {
@@ -136,6 +135,9 @@ constexpr int Q_TOKENS = 16;  // tokens of a pass
 // of shared memory; nothing is shared between warps but the sums at an item's end.
 template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
   static constexpr int STEP = MT * 1024, NB = 2 * MT;  // NB: blocks of 8 matrix rows in a warp tile
+  // Matrices narrower than a warp tile are MT = 1's; else the last tile of a matrix is moved up to its last row, so that
+  // every row of every tile exists (the rows that it shares with the tile before are computed twice and written once).
+  static constexpr bool NARROW = MT == 1;
   const QuantArgs& A;
   const int* first;
   int i1, wr, c0, c1, tiles_per, width, lane, g, j;
@@ -143,8 +145,8 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
   size_t pair_rows, next_rows;  // matrix rows from block 2 m to block 2 m + 1, and to block 2 m + 2
   // the codes' cursor
   QuantAt ahead;
-  int p_c, p_slot, p_out;  // p_out: output column of row g of block 0
-  const uint8_t* p_code;   // this lane's 16-byte piece of it
+  int p_c, p_slot, p_out;        // p_out: output column of row g of block 0
+  const uint8_t* p_code[NB];     // this lane's 16-byte pieces of row g of the blocks
 
   __device__ __forceinline__ QuantWarp(const QuantArgs& a, const int* f, const QuantAt& at, int end, int w, int ln, uint32_t ring)
       : A(a), first(f), i1(end), lane(ln), g(ln >> 2), j(ln & 3), ring_at(ring), ahead(at), p_slot(0) {
@@ -160,28 +162,40 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
   }
   // output column of row g of the tile's block 0; block b adds out_of(b)
   __device__ __forceinline__ int out_at(const QuantAt& at) const {
-    return ((at.tg * tiles_per + wr) * MT) * (A.swiglu ? 8 : 16) + g;
+    const int per = MT * (A.swiglu ? 8 : 16), o = (at.tg * tiles_per + wr) * per;
+    return (NARROW ? o : max(min(o, width - per), 0)) + g;
   }
   __device__ __forceinline__ int out_of(int b) const { return A.swiglu ? (b >> 1) * 8 : b * 8; }
   __device__ __forceinline__ size_t rows_to(int b) const { return (b >> 1) * next_rows + (b & 1) * pair_rows; }
+  __device__ __forceinline__ bool exists(int o, int b) const { return !NARROW || o + out_of(b) < width; }
 
   __device__ __forceinline__ void aim() {
     p_out = out_at(ahead);
-    p_code = A.codes + ((size_t)ahead.e * A.n_out + p_out) * (A.n_in / 2) + (size_t)c0 * 64 + j * 16;
+    const size_t row = (size_t)ahead.e * A.n_out + p_out, half = A.n_in / 2;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      p_code[b] = A.codes + (row + rows_to(b)) * half + (size_t)c0 * 64 + j * 16;
+      // the scales of the item to come: into the L2
+      if (exists(p_out, b)) {
+        const size_t i = (row + rows_to(b)) * A.groups + (size_t)c0 * NG;
+        const int shift = A.scale_f32 ? 2 : 1, bytes = (min(c1 * NG, A.groups) - c0 * NG) << shift;
+        const char* s = reinterpret_cast<const char*>(A.scales) + (i << shift) + (j * 32 < bytes ? j * 32 : 0);
+        asm volatile("prefetch.global.L2 [%0];" ::"l"(s));
+        if constexpr (Z) asm volatile("prefetch.global.L2 [%0];" ::"l"(A.zeros + i));
+      }
+    }
   }
   __device__ __forceinline__ void request() {
     if (ahead.item < i1) {
-      const bool in = p_c * QCOLS + j * 32 < A.n_in;
+      const int bytes = p_c * QCOLS + j * 32 < A.n_in ? 16 : 0;  // 0: nothing is read, zeros are written
       const uint32_t to = ring_at + p_slot * STEP + g * 64 + ((j ^ ((g >> 1) & 3)) * 16);
-      const size_t half = A.n_in / 2;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        const bool have = in && p_out + out_of(b) < width;  // else nothing is read, zeros are written
-        const uint8_t* from = have ? p_code + rows_to(b) * half : A.codes;
-        asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(to + b * 512), "l"(from), "r"(have ? 16 : 0)
-                     : "memory");
+        const bool have = exists(p_out, b);
+        asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(to + b * 512), "l"(have ? p_code[b] : A.codes),
+                     "r"(have ? bytes : 0) : "memory");
+        p_code[b] += 64;
       }
-      p_code += 64;
       if (++p_c == c1) {
         p_c = c0;
         quant_next(ahead, i1, first, A.tile_groups);
@@ -196,7 +210,10 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
   template <int NT>
   __device__ __forceinline__ void item(const QuantAt& at, int row0, int rows, int& slot, float (&acc)[MT][2][4]) {
     const int xw = A.steps * QCOLS, o0 = out_at(at);
-    size_t s_at = ((size_t)at.e * A.n_out + o0) * A.groups + (size_t)c0 * NG;
+    const int shift = A.scale_f32 ? 2 : 1;
+    const size_t s_first = ((size_t)at.e * A.n_out + o0) * A.groups + (size_t)c0 * NG;
+    const char* s_at = reinterpret_cast<const char*>(A.scales) + (s_first << shift);
+    const uint8_t* z_at = A.zeros + s_first;
     int grp_at = c0 * NG;
     const int grp_end = min(c1 * NG, A.groups);
     // scale and zero point of the group to come, for the lane's rows
@@ -204,15 +221,24 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
     uint32_t z_next[NB];
     auto fetch = [&]() {
       if (grp_at < grp_end) {
+        if (A.scale_f32) {
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
-          if (o0 + out_of(b) < width) {
-            const size_t i = s_at + rows_to(b) * A.groups;
-            sc_next[b] = quant_scale(A, i);
-            if constexpr (Z) z_next[b] = A.zeros[i];
-          }
+          for (int b = 0; b < NB; ++b)
+            if (exists(o0, b)) sc_next[b] = *reinterpret_cast<const float*>(s_at + rows_to(b) * A.groups * 4);
+        } else {
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+            if (exists(o0, b))
+              sc_next[b] = __uint_as_float((uint32_t)*reinterpret_cast<const unsigned short*>(s_at + rows_to(b) * A.groups * 2) << 16);
+        }
+        if constexpr (Z) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b)
+            if (exists(o0, b)) z_next[b] = z_at[rows_to(b) * A.groups];
+        }
       }
-      ++s_at;
+      s_at += 1 << shift;
+      ++z_at;
       ++grp_at;
     };
 #pragma unroll
@@ -361,18 +387,17 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
         b += v[h + 2];
       }
       const int64_t r = row0 + token;
-      const int ex = A.xe[r];
-      a = scalbnf(a, ex);
-      b = scalbnf(b, ex);
+      const float p2 = __int_as_float(A.xe[r]), q2 = __int_as_float(A.xe[(size_t)R + r]);  // two powers of two
+      a = a * p2 * q2;
+      b = b * p2 * q2;
       T* out = reinterpret_cast<T*>(A.out) + r * A.os;
-      const int t16 = (at.tg * tiles_per + tr) * MT + mt;
+      const int per = A.swiglu ? 8 : 16, o_tile = (at.tg * tiles_per + tr) * MT * per;  // its first column, before it was moved up
+      const int o = (MT == 1 ? o_tile : max(min(o_tile, width - MT * per), 0)) + mt * per + (l >> 2);
       if (A.swiglu) {
-        const int o = t16 * 8 + (l >> 2);
-        if (o < width) out[o] = from_f<T>(a / (1.f + expf(-a)) * b);
+        if (o >= o_tile && o < width) out[o] = from_f<T>(a / (1.f + expf(-a)) * b);
       } else {
-        const int o = t16 * 16 + (l >> 2);
-        if (o < width) out[o] = from_f<T>(a);
-        if (o + 8 < width) out[o + 8] = from_f<T>(b);
+        if (o >= o_tile && o < width) out[o] = from_f<T>(a);
+        if (o + 8 >= o_tile && o + 8 < width) out[o + 8] = from_f<T>(b);
       }
     }
     __syncthreads();
@@ -384,7 +409,7 @@ template <typename T, int NG> static deamoe_status_t quant_t(QuantArgs& A, cudaS
   const int tiles16 = A.swiglu ? (A.n_out / 2 + 7) / 8 : (A.n_out + 15) / 16;
   const int active = A.n_expert < A.n_rows ? A.n_expert : A.n_rows;
   // Two row tiles a warp share its x values and loop; one where that would leave blocks without work
-  const int mt = (int64_t)(tiles16 / 2) * active >= Q_GRID ? 2 : 1;
+  const int mt = (int64_t)(tiles16 / 2) * active >= Q_GRID && A.n_out >= 32 ? 2 : 1;
   const int per = QW / A.wk * mt;
   A.tile_groups = (tiles16 + per - 1) / per;
   auto run = [&](auto kernel, int depth, std::atomic<uint64_t>& done) {
@@ -419,7 +444,7 @@ extern "C" {
 uint64_t deamoe_quant_workspace(int32_t dtype, int32_t n_rows, int32_t n_in) {
   if (n_rows <= 0 || n_in <= 0) return 0;
   const uint64_t width = ((uint64_t)n_in + QCOLS - 1) / QCOLS * QCOLS;
-  return (uint64_t)n_rows * (width * (dtype == DEAMOE_F32 ? 4 : 2) + sizeof(int32_t));
+  return (uint64_t)n_rows * (width * (dtype == DEAMOE_F32 ? 4 : 2) + 2 * sizeof(int32_t));
 }
 
 deamoe_status_t deamoe_quant_product(void* cuda_stream, int32_t dtype, const uint8_t* codes, int32_t scale_dtype,
