@@ -7,12 +7,16 @@
 //
 // Tensor cores: mma.m16n8k16 with 16 matrix rows as M and up to 8 tokens as N (legacy path: with this few tokens the
 // instruction rate it needs is a fraction of what it has, and its A operand comes from registers, where the codes
-// have to be widened anyway).  Widening is an AND and a subtraction a pair: a nibble in the low bits of a 16-bit half IS
-// the fp16 subnormal q 2^-24, and in the next four bits q 2^-20; q - z is exact there, and tensor cores multiply
-// subnormals exactly.  x becomes fp16 in a kernel of its own: each row scaled by a power of two to a largest magnitude
-// of 2^14..2^15, the columns that meet 2^-20 by another 2^-4, so that fp16's range costs nothing (values below 2^-35
-// of the row's largest lose bits, far under fp32's own resolution of the sum); bf16 values fit exactly, fp32 values as
-// two parts (2^-23 relative).
+// have to be widened anyway).  Widening is one AND a pair: a nibble in the low bits of a 16-bit half IS the fp16
+// subnormal q 2^-24, and in the next four bits q 2^-20; tensor cores multiply subnormals exactly.  x becomes fp16 in a
+// kernel of its own: each row scaled by a power of two to a largest magnitude of 2^14..2^15, the columns that meet
+// 2^-20 by another 2^-4, so that fp16's range costs nothing (values below 2^-35 of the row's largest lose bits, far
+// under fp32's own resolution of the sum); bf16 values fit exactly, fp32 values as two parts (2^-23 relative).
+// The zero points.  For bf16 tokens they leave the sum, sum (q - z) x = sum q x - z sum x, with the groups' sums of x from
+// the same kernel: the subtraction may cancel some of fp32's bits, which a bf16 result does not see, and it saves a
+// third of the loop's instructions (the loop is bound by their issue).  For fp32 tokens q - z is formed first,
+// exactly.  A bf16 row with an infinity or a NaN would lose the difference between them that way; such rows are
+// computed from the definition, value by value.
 #include <atomic>
 #include <climits>
 #include <cuda_fp16.h>
@@ -39,50 +43,81 @@ struct QuantArgs {
   int wk;           // warps that share a row tile's columns (the others of the block take other tiles)
   int tile_groups;  // blocks of QW / wk warp tiles (16 MT rows) a matrix
   __half* xh;       // [n_rows][planes][steps * QCOLS]
+  float* xg;        // bf16 tokens: [groups][n_rows + 32] sums of the groups of the scaled rows, times 2^-24
   int32_t* xe;      // [2][n_rows] two powers of two (fp32 bits) that undo the row's scaling
 };
 
 // x in the order of the rows, as fp16 scaled by 2^-e, 8 columns in the order 0 4 1 5 2 6 3 7 (the order in which the
 // codes of a 32-bit word are widened; 1 5 3 7 by another 1/16).  One block a row; a row without a source is zero.
-template <typename T, int PLANES> __global__ void __launch_bounds__(256) k_quant_x(QuantArgs A) {
-  __shared__ float buf[32];
+template <typename T, int PLANES, int GROUP> __global__ void __launch_bounds__(256) k_quant_x(QuantArgs A) {
+  __shared__ float buf[8];
   const int64_t r = blockIdx.x;
   int64_t src = r;
   if (A.row_pair) src = A.row_pair[r] >= 0 ? A.row_pair[r] / A.ppt : -1;
-  const bool have = src >= 0 && src < A.n_token;
+  bool have = src >= 0 && src < A.n_token;
   const T* x = reinterpret_cast<const T*>(A.x) + (have ? src : 0) * A.xs;
   pdl_trigger();
   float top = 0.f;
+  bool odd = false;
   for (int c = threadIdx.x; have && c < A.n_in; c += 256) {
     const float v = fabsf(to_f<T>(x[c]));
-    if (v <= 3.4028234663852886e38f) top = fmaxf(top, v);  // infinities and NaN stay what they are
+    if (v <= 3.4028234663852886e38f) top = fmaxf(top, v);
+    else odd = true;  // infinities and NaN
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = top;
-  __syncthreads();
+  odd = __syncthreads_or(odd);
   for (int i = 0; i < 8; ++i) top = fmaxf(top, buf[i]);
   const int e = top > 0.f ? ilogbf(top) - 14 : 0;
-  if (threadIdx.x == 0) {  // 2^(e + 24) as two factors, each in fp32's range
+  const bool apart = PLANES == 1 && odd;  // marked by a NaN in the place of its scale
+  if (threadIdx.x == 0) {                 // 2^(e + 24) as two factors, each in fp32's range
     const int half = (e + 24) / 2;
-    A.xe[r] = (127 + half) << 23;
+    A.xe[r] = apart ? 0x7fc00000 : (127 + half) << 23;
     A.xe[(size_t)A.n_rows + r] = (127 + (e + 24) - half) << 23;
   }
+  have = have && !apart;
   const int width = A.steps * QCOLS;
   __half* out = A.xh + r * PLANES * width;
-  for (int c = threadIdx.x; c < width / 8; c += 256) {
+  for (int c0 = threadIdx.x & ~31; c0 < width / 8; c0 += 256) {  // whole warps: the group sums shuffle
+    const int c = c0 + (threadIdx.x & 31);
     union { __half h[8]; uint4 u; } hi, lo;
+    float sum = 0.f;
 #pragma unroll
     for (int p = 0; p < 8; ++p) {
       const int col = c * 8 + (p >> 1) + (p & 1) * 4;
-      const float v = have && col < A.n_in ? scalbnf(to_f<T>(x[col]), (p & 2) ? -e - 4 : -e) : 0.f;
-      hi.h[p] = __float2half_rn(v);
-      const float rest = v - __half2float(hi.h[p]);
-      lo.h[p] = __float2half_rn(isfinite(v) ? rest : 0.f);
+      const float v = have && col < A.n_in ? scalbnf(to_f<T>(x[col]), -e) : 0.f;
+      const float u = (p & 2) ? v * 0.0625f : v;
+      sum += v;
+      hi.h[p] = __float2half_rn(u);
+      const float rest = u - __half2float(hi.h[p]);
+      lo.h[p] = __float2half_rn(isfinite(u) ? rest : 0.f);
     }
+    if constexpr (PLANES == 1) {
+#pragma unroll
+      for (int o = 1; o < GROUP / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    }
+    if (c >= width / 8) continue;
     *reinterpret_cast<uint4*>(out + c * 8) = hi.u;
     if constexpr (PLANES == 2) *reinterpret_cast<uint4*>(out + width + c * 8) = lo.u;
+    const int grp = c / (GROUP / 8);
+    if (PLANES == 1 && c % (GROUP / 8) == 0 && grp < A.groups)
+      A.xg[(size_t)grp * (A.n_rows + 32) + r] = sum * 5.9604644775390625e-8f;
   }
+}
+
+// One product from the definition, for the rows set apart.
+template <typename T>
+static __device__ __noinline__ float quant_dot(const uint8_t* codes, const void* scales, bool scale_f32, const uint8_t* zeros,
+                                               const T* x, int n_in, int group) {
+  float acc = 0.f;
+  for (int c = 0; c < n_in; ++c) {
+    const int k = c / group, q = (codes[c >> 1] >> ((c & 1) * 4)) & 15;
+    const float s = scale_f32 ? reinterpret_cast<const float*>(scales)[k]
+                              : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(scales)[k]);
+    acc = fmaf(s * (float)(q - (zeros ? zeros[k] & 15 : 8)), to_f<T>(x[c]), acc);
+  }
+  return acc;
 }
 
 static __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -91,14 +126,21 @@ static __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint3
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// The 8 codes of a word less the zero point as four pairs of fp16 subnormals: columns (0 4) (1 5) (2 6) (3 7), (q - z)
+// The 8 codes of a word (LESS: less the zero point) as four pairs of fp16 subnormals: columns (0 4) (1 5) (2 6) (3 7),
 // times 2^-24 and 2^-20 in turn.  z: the zero point in the low bits of both halves.
 static __device__ __forceinline__ uint32_t less(uint32_t a, uint32_t b) {
   const __half2 d = __hsub2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&d);
 }
-static __device__ __forceinline__ void widen(uint32_t w, uint32_t z, uint32_t (&p)[4]) {
+template <bool LESS> static __device__ __forceinline__ void widen(uint32_t w, uint32_t z, uint32_t (&p)[4]) {
   const uint32_t v = w >> 8, z4 = z << 4;
+  if constexpr (!LESS) {
+    p[0] = w & 0x000f000fu;
+    p[1] = w & 0x00f000f0u;
+    p[2] = v & 0x000f000fu;
+    p[3] = v & 0x00f000f0u;
+    return;
+  }
   p[0] = less(w & 0x000f000fu, z);
   p[1] = less(w & 0x00f000f0u, z4);
   p[2] = less(v & 0x000f000fu, z);
@@ -138,6 +180,7 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
   // Matrices narrower than a warp tile are MT = 1's; else the last tile of a matrix is moved up to its last row, so that
   // every row of every tile exists (the rows that it shares with the tile before are computed twice and written once).
   static constexpr bool NARROW = MT == 1;
+  static constexpr bool LIN = PLANES == 1;  // zero points leave the sum
   const QuantArgs& A;
   const int* first;
   int i1, wr, c0, c1, tiles_per, width, lane, g, j;
@@ -214,13 +257,24 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
     const size_t s_first = ((size_t)at.e * A.n_out + o0) * A.groups + (size_t)c0 * NG;
     const char* s_at = reinterpret_cast<const char*>(A.scales) + (s_first << shift);
     const uint8_t* z_at = A.zeros + s_first;
+    const size_t xg_step = (size_t)A.n_rows + 32;
+    const float* xg_at = A.xg + (size_t)c0 * NG * xg_step + row0 + j * 2;
     int grp_at = c0 * NG;
     const int grp_end = min(c1 * NG, A.groups);
     // scale and zero point of the group to come, for the lane's rows
     float sc_next[NB];
     uint32_t z_next[NB];
+    float x_next[NT][2];  // sums of x, for the lane's tokens of the products
     auto fetch = [&]() {
       if (grp_at < grp_end) {
+        if constexpr (LIN) {
+#pragma unroll
+          for (int t = 0; t < NT; ++t) {
+            x_next[t][0] = xg_at[t * 8];
+            x_next[t][1] = xg_at[t * 8 + 1];
+          }
+          xg_at += xg_step;
+        }
         if (A.scale_f32) {
 #pragma unroll
           for (int b = 0; b < NB; ++b)
@@ -246,6 +300,8 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
       sc_next[b] = 0.f;
       z_next[b] = 8;
     }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) x_next[t][0] = x_next[t][1] = 0.f;
     fetch();
     // tokens past the last take the last one's values: their sums are not looked at
     const __half* xp[NT];
@@ -279,12 +335,15 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
           for (int b = 0; b < NB; ++b) {
             sc[b] = sc_next[b];
             z[b] = Z ? (z_next[b] & 15) * 0x00010001u : 0x00080008u;
+            // the group's sum starts at - z sum x, or at 0
+            const float zf = !LIN ? 0.f : Z ? 8388608.f - __uint_as_float(0x4b000000u | (z_next[b] & 15)) : -8.f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+              grp[b >> 1][t][(b & 1) * 2] = LIN ? zf * x_next[t][0] : 0.f;
+              grp[b >> 1][t][(b & 1) * 2 + 1] = LIN ? zf * x_next[t][1] : 0.f;
+            }
           }
           fetch();
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) grp[mt][t][0] = grp[mt][t][1] = grp[mt][t][2] = grp[mt][t][3] = 0.f;
         }
         uint4 now[NT][PLANES];
 #pragma unroll
@@ -297,8 +356,8 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
           uint32_t lo[4], hi[4];
-          widen(code[2 * mt][m], z[2 * mt], lo);
-          widen(code[2 * mt + 1][m], z[2 * mt + 1], hi);
+          widen<!LIN>(code[2 * mt][m], z[2 * mt], lo);
+          widen<!LIN>(code[2 * mt + 1][m], z[2 * mt + 1], hi);
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -390,15 +449,25 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
       const float p2 = __int_as_float(A.xe[r]), q2 = __int_as_float(A.xe[(size_t)R + r]);  // two powers of two
       a = a * p2 * q2;
       b = b * p2 * q2;
+      const bool apart = PLANES == 1 && !(p2 == p2);
       T* out = reinterpret_cast<T*>(A.out) + r * A.os;
       const int per = A.swiglu ? 8 : 16, o_tile = (at.tg * tiles_per + tr) * MT * per;  // its first column, before it was moved up
       const int o = (MT == 1 ? o_tile : max(min(o_tile, width - MT * per), 0)) + mt * per + (l >> 2);
-      if (A.swiglu) {
-        if (o >= o_tile && o < width) out[o] = from_f<T>(a / (1.f + expf(-a)) * b);
-      } else {
-        if (o >= o_tile && o < width) out[o] = from_f<T>(a);
-        if (o + 8 >= o_tile && o + 8 < width) out[o + 8] = from_f<T>(b);
+      const bool w0 = o >= o_tile && o < width, w1 = !A.swiglu && o + 8 >= o_tile && o + 8 < width;
+      if (apart) {
+        auto dot = [&](int row) {
+          const size_t i = (size_t)at.e * A.n_out + row, k = i * A.groups;
+          const int64_t src = A.row_pair ? A.row_pair[r] / A.ppt : r;
+          return quant_dot<T>(A.codes + i * (A.n_in / 2), reinterpret_cast<const char*>(A.scales) + k * (A.scale_f32 ? 4 : 2),
+                              A.scale_f32, A.zeros ? A.zeros + k : nullptr, reinterpret_cast<const T*>(A.x) + src * A.xs, A.n_in,
+                              QCOLS / NG);
+        };
+        if (w0) a = dot(o);
+        if (A.swiglu ? w0 : w1) b = dot(A.swiglu ? width + o : o + 8);
       }
+      if (A.swiglu) a = a / (1.f + expf(-a)) * b;
+      if (w0) out[o] = from_f<T>(a);
+      if (w1) out[o + 8] = from_f<T>(b);
     }
     __syncthreads();
   }
@@ -410,6 +479,11 @@ template <typename T, int NG> static deamoe_status_t quant_t(QuantArgs& A, cudaS
   const int active = A.n_expert < A.n_rows ? A.n_expert : A.n_rows;
   // Two row tiles a warp share its x values and loop; one where that would leave blocks without work
   const int mt = (int64_t)(tiles16 / 2) * active >= Q_GRID && A.n_out >= 32 ? 2 : 1;
+  // Warps that share a tile's columns: all, or fewer (longer walks, fewer sums to join) while the blocks keep at least
+  // 16 items each, so that their counts differ by little
+  A.wk = QW;
+  while (A.wk > A.steps) A.wk /= 2;
+  while (A.wk > 1 && (int64_t)((tiles16 + mt - 1) / mt) * (A.wk / 2) / QW * active >= 16 * Q_GRID) A.wk /= 2;
   const int per = QW / A.wk * mt;
   A.tile_groups = (tiles16 + per - 1) / per;
   auto run = [&](auto kernel, int depth, std::atomic<uint64_t>& done) {
@@ -421,15 +495,15 @@ template <typename T, int NG> static deamoe_status_t quant_t(QuantArgs& A, cudaS
       done.fetch_or(1ull << dev, std::memory_order_release);
     }
     const size_t smem = (size_t)QW * depth * mt * 1024 + (size_t)QW * mt * 1024 + (size_t)(A.n_expert + 1) * 4;
-    k_quant_x<T, PLANES><<<A.n_rows, 256, 0, s>>>(A);
+    k_quant_x<T, PLANES, QCOLS / NG><<<A.n_rows, 256, 0, s>>>(A);
     const cudaError_t e = cudaGetLastError();
     return e != cudaSuccess ? e : launch_pdl(kernel, dim3(Q_GRID), dim3(QW * 32), smem, s, A);
   };
   static std::atomic<uint64_t> done[4];
-  const cudaError_t e = mt == 2 ? (A.zeros ? run(k_quant<T, PLANES, 2, NG, true, 5>, 5, done[0])
-                                           : run(k_quant<T, PLANES, 2, NG, false, 5>, 5, done[1]))
-                                : (A.zeros ? run(k_quant<T, PLANES, 1, NG, true, 9>, 9, done[2])
-                                           : run(k_quant<T, PLANES, 1, NG, false, 9>, 9, done[3]));
+  const cudaError_t e = mt == 2 ? (A.zeros ? run(k_quant<T, PLANES, 2, NG, true, 3>, 3, done[0])
+                                           : run(k_quant<T, PLANES, 2, NG, false, 3>, 3, done[1]))
+                                : (A.zeros ? run(k_quant<T, PLANES, 1, NG, true, 6>, 6, done[2])
+                                           : run(k_quant<T, PLANES, 1, NG, false, 6>, 6, done[3]));
   if (e == cudaSuccess) return DEAMOE_OK;
   cudaGetLastError();
   return DEAMOE_ERR_CUDA;
@@ -444,7 +518,9 @@ extern "C" {
 uint64_t deamoe_quant_workspace(int32_t dtype, int32_t n_rows, int32_t n_in) {
   if (n_rows <= 0 || n_in <= 0) return 0;
   const uint64_t width = ((uint64_t)n_in + QCOLS - 1) / QCOLS * QCOLS;
-  return (uint64_t)n_rows * (width * (dtype == DEAMOE_F32 ? 4 : 2) + 2 * sizeof(int32_t));
+  uint64_t bytes = (uint64_t)n_rows * (width * (dtype == DEAMOE_F32 ? 4 : 2) + 2 * sizeof(int32_t));
+  if (dtype != DEAMOE_F32) bytes += ((uint64_t)n_rows + 32) * (width / 32) * sizeof(float);  // groups of 32 at least
+  return bytes;
 }
 
 deamoe_status_t deamoe_quant_product(void* cuda_stream, int32_t dtype, const uint8_t* codes, int32_t scale_dtype,
@@ -475,14 +551,13 @@ deamoe_status_t deamoe_quant_product(void* cuda_stream, int32_t dtype, const uin
   A.groups = (n_in + group - 1) / group; A.n_token = n_token; A.ppt = pairs_per_token; A.n_rows = n_rows;
   A.swiglu = swiglu; A.scale_f32 = scale_dtype == DEAMOE_F32;
   A.steps = (n_in + QCOLS - 1) / QCOLS;
-  A.wk = QW;
-  while (A.wk > A.steps) A.wk /= 2;
   const int tiles = swiglu ? (width + 7) / 8 : (width + 15) / 16;
   // items are counted in 32 bits (an expert's last pass may be short, hence one more each)
   if ((int64_t)tiles * ((int64_t)n_rows / Q_TOKENS + n_expert) > INT_MAX) return DEAMOE_ERR_BATCH;
   A.xh = reinterpret_cast<__half*>(workspace);
   A.xe = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(workspace) +
                                     (size_t)n_rows * A.steps * QCOLS * (dtype == DEAMOE_F32 ? 4 : 2));
+  A.xg = reinterpret_cast<float*>(A.xe + (size_t)2 * n_rows);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
   if (dtype == DEAMOE_F32)
     return group == 128 ? quant_t<float, 1>(A, s) : group == 64 ? quant_t<float, 2>(A, s) : quant_t<float, 4>(A, s);

@@ -149,6 +149,23 @@ def test_values_of_every_size():
         assert not torch.isfinite(got2[0]).any() and torch.isnan(got2[5]).all()
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_an_infinity_meets_the_weights_sign(zeros, dtype):
+    """A product with one infinity is an infinity of the weight's sign, or NaN where the weight is 0."""
+    N, K, group = 200, 256, 32
+    codes, scales, z = _matrices(1, N, K, group, zeros, BF16, 11)
+    x = torch.randn((3, K), generator=torch.Generator(device=DEV).manual_seed(12), device=DEV).to(dtype)
+    clean = binding.quant_product(codes, scales, x, group, zeros=z)
+    x[1, 77] = float("-inf")
+    got = binding.quant_product(codes, scales, x, group, zeros=z)
+    w = _widened(codes[0], scales[0], None if z is None else z[0], group, K)[:, 77]
+    assert (w == 0).any() and (w > 0).any() and (w < 0).any()
+    assert torch.isnan(got[1][w == 0]).all()
+    assert (got[1][w > 0] == float("-inf")).all() and (got[1][w < 0] == float("inf")).all()
+    assert torch.equal(got[[0, 2]], clean[[0, 2]])
+
+
 def test_sources_outside_x_count_as_zero():
     N, K, group = 16, 64, 32
     codes, scales, _ = _matrices(2, N, K, group, False, BF16, 7)
