@@ -122,7 +122,7 @@ static __device__ __noinline__ float quant_dot(const uint8_t* codes, const void*
 
 static __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                                uint32_t b1) {
-  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -180,6 +180,7 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
   // Matrices narrower than a warp tile are MT = 1's; else the last tile of a matrix is moved up to its last row, so that
   // every row of every tile exists (the rows that it shares with the tile before are computed twice and written once).
   static constexpr bool NARROW = MT == 1;
+  static constexpr int LM = MT == 2 ? 1 : 2;
   static constexpr bool LIN = PLANES == 1;  // zero points leave the sum
   const QuantArgs& A;
   const int* first;
@@ -305,26 +306,24 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
     fetch();
     // tokens past the last take the last one's values: their sums are not looked at
     const __half* xp[NT];
-    uint4 next[NT][PLANES];
+    constexpr int XA = PLANES * NT == 1 ? 4 : 1;  // quarter steps of x ahead: a whole step where registers allow
+    uint4 next[XA][NT][PLANES];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       xp[t] = A.xh + (size_t)(row0 + min(t * 8 + g, rows - 1)) * PLANES * xw + (size_t)c0 * QCOLS + j * 8;
 #pragma unroll
-      for (int p = 0; p < PLANES; ++p) next[t][p] = load_b128(xp[t] + (size_t)p * xw);
+      for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+        for (int m = 0; m < XA; ++m) next[m][t][p] = load_b128(xp[t] + (size_t)p * xw + m * 32);
     }
 #pragma unroll 1
     for (int c = c0; c < c1; ++c) {
       asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
       __syncwarp();
-      uint32_t code[NB][4];
-      const uint32_t from = ring_at + slot * STEP + (lane & 7) * 64 + (((lane >> 3) ^ (((lane & 7) >> 1) & 3)) * 16);
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-        asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(code[b][0]), "=r"(code[b][1]), "=r"(code[b][2]), "=r"(code[b][3]) : "r"(from + b * 512) : "memory");
-      __syncwarp();
-      request();  // the slot just read
-      slot = slot + 1 == DEPTH ? 0 : slot + 1;
+      uint32_t code[NB * LM];  // the codes of LM quarter steps
+      // the lane's row of the eight matrices an ldmatrix takes: block lane / 8 (MT == 1: block and quarter step)
+      const uint32_t from = ring_at + slot * STEP + (MT == 2 ? (lane >> 3) : (lane >> 3) & 1) * 512 + (lane & 7) * 64 +
+                            ((((lane & 7) >> 1) ^ (MT == 2 ? 0 : lane >> 4)) & 3) * 16;
       float sc[NB];
       uint32_t z[NB];
       float grp[MT][NT][4];
@@ -345,19 +344,27 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
           }
           fetch();
         }
+        if (m % LM == 0)
+          asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                       : "=r"(code[0]), "=r"(code[1]), "=r"(code[2]), "=r"(code[3]) : "r"(from ^ (m * 16)) : "memory");
+        if (m == 4 - LM) {  // the slot has been read
+          __syncwarp();
+          request();
+          slot = slot + 1 == DEPTH ? 0 : slot + 1;
+        }
         uint4 now[NT][PLANES];
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
           for (int p = 0; p < PLANES; ++p) {
-            now[t][p] = next[t][p];
-            if (m < 3 || c + 1 < c1) next[t][p] = load_b128(xp[t] + (size_t)p * xw + (m + 1) * 32);
+            now[t][p] = next[m % XA][t][p];
+            if (m + XA < 4 || c + 1 < c1) next[m % XA][t][p] = load_b128(xp[t] + (size_t)p * xw + (m + XA) * 32);
           }
 #pragma unroll
         for (int mt = 0; mt < MT; ++mt) {
           uint32_t lo[4], hi[4];
-          widen<!LIN>(code[2 * mt][m], z[2 * mt], lo);
-          widen<!LIN>(code[2 * mt + 1][m], z[2 * mt + 1], hi);
+          widen<!LIN>(code[(m % LM) * NB + 2 * mt], z[2 * mt], lo);
+          widen<!LIN>(code[(m % LM) * NB + 2 * mt + 1], z[2 * mt + 1], hi);
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -385,8 +392,8 @@ template <typename T, int PLANES, int MT, int NG, bool Z, int DEPTH>
 __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int warp_sums[QW];
-  float4* sums = reinterpret_cast<float4*>(smem + QW * DEPTH * MT * 1024);  // [QW][MT][2][32]
-  int* first = reinterpret_cast<int*>(sums + QW * MT * 2 * 32);            // [n_expert + 1] first item of each expert
+  float4* sums = reinterpret_cast<float4*>(smem + QW * DEPTH * MT * 1024);  // [2][QW][MT][2][32]
+  int* first = reinterpret_cast<int*>(sums + 2 * QW * MT * 2 * 32);            // [n_expert + 1] first item of each expert
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, R = A.n_rows;
   auto row_begin = [&](int e) { return A.expert_off ? min(max(A.expert_off[e], 0), R) : 0; };
   auto row_end = [&](int e) { return A.expert_off ? min(max(A.expert_off[e + 1], 0), R) : R; };
@@ -420,28 +427,31 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
   for (int i = 0; i < DEPTH; ++i) W.request();
   pdl_wait();  // x in fp16
 
-  int slot = 0;
+  int slot = 0, flip = 0;
   for (; at.item < i1; quant_next(at, i1, first, A.tile_groups)) {
     const int row0 = row_begin(at.e) + at.pass * Q_TOKENS, rows = min(row_end(at.e) - row0, Q_TOKENS);
     float acc[MT][2][4] = {};
     if (rows <= 8) W.template item<1>(at, row0, rows, slot, acc);
     else W.template item<2>(at, row0, rows, slot, acc);
-    // join the warps' column shares, in order
-    float4* mine = sums + (size_t)w * MT * 2 * 32 + lane;
+    // join the column shares of the tile's warps, in order.  Two buffers: one is written while slower warps still read
+    // the other, and no warp is two items ahead of its partners
+    const int tile_warp = W.wr * A.wk;  // the tile's first warp
+    float4* mine = sums + (size_t)(flip * QW + w) * MT * 2 * 32 + lane;
 #pragma unroll
     for (int mt = 0; mt < MT; ++mt)
 #pragma unroll
       for (int t = 0; t < 2; ++t)
         if (t * 8 < rows) mine[(mt * 2 + t) * 32] = make_float4(acc[mt][t][0], acc[mt][t][1], acc[mt][t][2], acc[mt][t][3]);
-    __syncthreads();
+    if (A.wk == 1) __syncwarp();
+    else asm volatile("bar.sync %0, %1;" ::"r"(1 + W.wr), "r"(A.wk * 32) : "memory");
     // a thread: one token, one tile row g and its partner g + 8
-    for (int i = threadIdx.x; i < tiles_per * MT * 128; i += QW * 32) {
-      const int h = i & 1, l = (i >> 1) & 31, t = (i >> 6) & 1, mt = (i >> 7) % MT, tr = (i >> 7) / MT;
+    for (int i = threadIdx.x - tile_warp * 32; i < MT * 128; i += A.wk * 32) {
+      const int h = i & 1, l = (i >> 1) & 31, t = (i >> 6) & 1, mt = i >> 7;
       const int token = t * 8 + (l & 3) * 2 + h;
       if (token >= rows) continue;
       float a = 0.f, b = 0.f;
       for (int k = 0; k < A.wk; ++k) {
-        const float* v = reinterpret_cast<const float*>(sums + (((size_t)tr * A.wk + k) * MT * 2 + mt * 2 + t) * 32 + l);
+        const float* v = reinterpret_cast<const float*>(sums + ((size_t)(flip * QW + tile_warp + k) * MT * 2 + mt * 2 + t) * 32 + l);
         a += v[h];
         b += v[h + 2];
       }
@@ -451,7 +461,7 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
       b = b * p2 * q2;
       const bool apart = PLANES == 1 && !(p2 == p2);
       T* out = reinterpret_cast<T*>(A.out) + r * A.os;
-      const int per = A.swiglu ? 8 : 16, o_tile = (at.tg * tiles_per + tr) * MT * per;  // its first column, before it was moved up
+      const int per = A.swiglu ? 8 : 16, o_tile = (at.tg * tiles_per + W.wr) * MT * per;  // its first column, before it was moved up
       const int o = (MT == 1 ? o_tile : max(min(o_tile, width - MT * per), 0)) + mt * per + (l >> 2);
       const bool w0 = o >= o_tile && o < width, w1 = !A.swiglu && o + 8 >= o_tile && o + 8 < width;
       if (apart) {
@@ -469,7 +479,7 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
       if (w0) out[o] = from_f<T>(a);
       if (w1) out[o + 8] = from_f<T>(b);
     }
-    __syncthreads();
+    flip ^= 1;
   }
 }
 
@@ -494,7 +504,7 @@ template <typename T, int NG> static deamoe_status_t quant_t(QuantArgs& A, cudaS
       if (e != cudaSuccess) return e;
       done.fetch_or(1ull << dev, std::memory_order_release);
     }
-    const size_t smem = (size_t)QW * depth * mt * 1024 + (size_t)QW * mt * 1024 + (size_t)(A.n_expert + 1) * 4;
+    const size_t smem = (size_t)QW * depth * mt * 1024 + (size_t)QW * mt * 2048 + (size_t)(A.n_expert + 1) * 4;
     k_quant_x<T, PLANES, QCOLS / NG><<<A.n_rows, 256, 0, s>>>(A);
     const cudaError_t e = cudaGetLastError();
     return e != cudaSuccess ? e : launch_pdl(kernel, dim3(Q_GRID), dim3(QW * 32), smem, s, A);
