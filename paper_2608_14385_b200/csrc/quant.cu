@@ -126,6 +126,13 @@ static __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint3
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// the same with a sum that starts at 0
+static __device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+                                                     uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
 // The 8 codes of a word (LESS: less the zero point) as four pairs of fp16 subnormals: columns (0 4) (1 5) (2 6) (3 7),
 // times 2^-24 and 2^-20 in turn.  z: the zero point in the low bits of both halves.
 static __device__ __forceinline__ uint32_t less(uint32_t a, uint32_t b) {
@@ -186,14 +193,15 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
   const int* first;
   int i1, wr, c0, c1, tiles_per, width, lane, g, j;
   uint32_t ring_at;
+  uint32_t scale_to[NB];        // bytes from block 0's scales to block b's (a matrix has less than 4 GB of them)
   size_t pair_rows, next_rows;  // matrix rows from block 2 m to block 2 m + 1, and to block 2 m + 2
   // the codes' cursor
   QuantAt ahead;
-  int p_c, p_slot, p_out;        // p_out: output column of row g of block 0
+  int p_c, p_out;                // p_out: output column of row g of block 0
   const uint8_t* p_code[NB];     // this lane's 16-byte pieces of row g of the blocks
 
   __device__ __forceinline__ QuantWarp(const QuantArgs& a, const int* f, const QuantAt& at, int end, int w, int ln, uint32_t ring)
-      : A(a), first(f), i1(end), lane(ln), g(ln >> 2), j(ln & 3), ring_at(ring), ahead(at), p_slot(0) {
+      : A(a), first(f), i1(end), lane(ln), g(ln >> 2), j(ln & 3), ring_at(ring), ahead(at) {
     tiles_per = QW / A.wk;
     wr = w / A.wk;
     const int share = w - wr * A.wk;
@@ -203,6 +211,11 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
     pair_rows = A.swiglu ? width : 8;
     next_rows = A.swiglu ? 8 : 16;
     p_c = c0;
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      scale_to[b] = (uint32_t)(rows_to(b) * A.groups) << (A.scale_f32 ? 2 : 1);
+      asm volatile("" : "+r"(scale_to[b]));  // computed once, kept
+    }
   }
   // output column of row g of the tile's block 0; block b adds out_of(b)
   __device__ __forceinline__ int out_at(const QuantAt& at) const {
@@ -229,10 +242,11 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
       }
     }
   }
-  __device__ __forceinline__ void request() {
+  // the next step's codes into the slot at byte `slot` of the ring
+  __device__ __forceinline__ void request(uint32_t slot) {
     if (ahead.item < i1) {
       const int bytes = p_c * QCOLS + j * 32 < A.n_in ? 16 : 0;  // 0: nothing is read, zeros are written
-      const uint32_t to = ring_at + p_slot * STEP + g * 64 + ((j ^ ((g >> 1) & 3)) * 16);
+      const uint32_t to = ring_at + slot + g * 64 + ((j ^ ((g >> 1) & 3)) * 16);
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         const bool have = exists(p_out, b);
@@ -247,12 +261,11 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
       }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
-    p_slot = p_slot + 1 == DEPTH ? 0 : p_slot + 1;
   }
 
   // The warp's columns of one item for NT * 8 tokens: acc[mt][t] = this warp's share of the products.
   template <int NT>
-  __device__ __forceinline__ void item(const QuantAt& at, int row0, int rows, int& slot, float (&acc)[MT][2][4]) {
+  __device__ __forceinline__ void item(const QuantAt& at, int row0, int rows, uint32_t& slot, float (&acc)[MT][2][4]) {
     const int xw = A.steps * QCOLS, o0 = out_at(at);
     const int shift = A.scale_f32 ? 2 : 1;
     const size_t s_first = ((size_t)at.e * A.n_out + o0) * A.groups + (size_t)c0 * NG;
@@ -260,126 +273,123 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
     const uint8_t* z_at = A.zeros + s_first;
     const size_t xg_step = (size_t)A.n_rows + 32;
     const float* xg_at = A.xg + (size_t)c0 * NG * xg_step + row0 + j * 2;
-    int grp_at = c0 * NG;
-    const int grp_end = min(c1 * NG, A.groups);
-    // scale and zero point of the group to come, for the lane's rows
-    float sc_next[NB];
-    uint32_t z_next[NB];
-    float x_next[NT][2];  // sums of x, for the lane's tokens of the products
+    int groups_left = min(c1 * NG, A.groups) - c0 * NG;
+    // of the group at hand: scale and zero point of the lane's rows, sums of x of the lane's tokens of the products.  Loaded
+    // when the group before is done with them
+    float sc[NB], gx[NT][2];
+    uint32_t z[NB];
     auto fetch = [&]() {
-      if (grp_at < grp_end) {
+      if (groups_left-- > 0) {
         if constexpr (LIN) {
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
-            x_next[t][0] = xg_at[t * 8];
-            x_next[t][1] = xg_at[t * 8 + 1];
+            gx[t][0] = xg_at[t * 8];
+            gx[t][1] = xg_at[t * 8 + 1];
           }
           xg_at += xg_step;
         }
         if (A.scale_f32) {
 #pragma unroll
           for (int b = 0; b < NB; ++b)
-            if (exists(o0, b)) sc_next[b] = *reinterpret_cast<const float*>(s_at + rows_to(b) * A.groups * 4);
+            if (exists(o0, b)) sc[b] = *reinterpret_cast<const float*>(s_at + scale_to[b]);
         } else {
 #pragma unroll
           for (int b = 0; b < NB; ++b)
-            if (exists(o0, b))
-              sc_next[b] = __uint_as_float((uint32_t)*reinterpret_cast<const unsigned short*>(s_at + rows_to(b) * A.groups * 2) << 16);
+            if (exists(o0, b)) sc[b] = __uint_as_float((uint32_t)*reinterpret_cast<const unsigned short*>(s_at + scale_to[b]) << 16);
         }
         if constexpr (Z) {
 #pragma unroll
           for (int b = 0; b < NB; ++b)
-            if (exists(o0, b)) z_next[b] = z_at[rows_to(b) * A.groups];
+            if (exists(o0, b)) z[b] = z_at[scale_to[b] >> shift];
         }
       }
       s_at += 1 << shift;
       ++z_at;
-      ++grp_at;
     };
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      sc_next[b] = 0.f;
-      z_next[b] = 8;
+      sc[b] = 0.f;
+      z[b] = 8;
     }
 #pragma unroll
-    for (int t = 0; t < NT; ++t) x_next[t][0] = x_next[t][1] = 0.f;
+    for (int t = 0; t < NT; ++t) gx[t][0] = gx[t][1] = 0.f;
     fetch();
     // tokens past the last take the last one's values: their sums are not looked at
     const __half* xp[NT];
-    constexpr int XA = PLANES * NT == 1 ? 4 : 1;  // quarter steps of x ahead: a whole step where registers allow
-    uint4 next[XA][NT][PLANES];
+    constexpr bool WHOLE = PLANES * NT == 1;  // x a whole step ahead where registers allow, else a quarter
+    constexpr int XB = WHOLE ? 4 : 2;
+    uint4 xb[XB][NT][PLANES];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
       xp[t] = A.xh + (size_t)(row0 + min(t * 8 + g, rows - 1)) * PLANES * xw + (size_t)c0 * QCOLS + j * 8;
 #pragma unroll
       for (int p = 0; p < PLANES; ++p)
 #pragma unroll
-        for (int m = 0; m < XA; ++m) next[m][t][p] = load_b128(xp[t] + (size_t)p * xw + m * 32);
+        for (int m = 0; m < (WHOLE ? 4 : 1); ++m) xb[m][t][p] = load_b128(xp[t] + (size_t)p * xw + m * 32);
     }
+    // the lane's row of the eight matrices an ldmatrix takes: block lane / 8 (MT == 1: block and quarter step)
+    const uint32_t lane_at = ring_at + (MT == 2 ? (lane >> 3) : (lane >> 3) & 1) * 512 + (lane & 7) * 64 +
+                             ((((lane & 7) >> 1) ^ (MT == 2 ? 0 : lane >> 4)) & 3) * 16;
 #pragma unroll 1
     for (int c = c0; c < c1; ++c) {
+      const bool more = c + 1 < c1;
       asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
       __syncwarp();
       uint32_t code[NB * LM];  // the codes of LM quarter steps
-      // the lane's row of the eight matrices an ldmatrix takes: block lane / 8 (MT == 1: block and quarter step)
-      const uint32_t from = ring_at + slot * STEP + (MT == 2 ? (lane >> 3) : (lane >> 3) & 1) * 512 + (lane & 7) * 64 +
-                            ((((lane & 7) >> 1) ^ (MT == 2 ? 0 : lane >> 4)) & 3) * 16;
-      float sc[NB];
-      uint32_t z[NB];
+      const uint32_t from = lane_at + slot;
       float grp[MT][NT][4];
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
-        if (m * NG % 4 == 0) {  // a group begins
-#pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            sc[b] = sc_next[b];
-            z[b] = Z ? (z_next[b] & 15) * 0x00010001u : 0x00080008u;
-            // the group's sum starts at - z sum x, or at 0
-            const float zf = !LIN ? 0.f : Z ? 8388608.f - __uint_as_float(0x4b000000u | (z_next[b] & 15)) : -8.f;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-              grp[b >> 1][t][(b & 1) * 2] = LIN ? zf * x_next[t][0] : 0.f;
-              grp[b >> 1][t][(b & 1) * 2 + 1] = LIN ? zf * x_next[t][1] : 0.f;
-            }
-          }
-          fetch();
-        }
         if (m % LM == 0)
           asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                        : "=r"(code[0]), "=r"(code[1]), "=r"(code[2]), "=r"(code[3]) : "r"(from ^ (m * 16)) : "memory");
         if (m == 4 - LM) {  // the slot has been read
           __syncwarp();
-          request();
-          slot = slot + 1 == DEPTH ? 0 : slot + 1;
+          request(slot);
+          slot = slot + STEP == DEPTH * STEP ? 0 : slot + STEP;
         }
-        uint4 now[NT][PLANES];
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-          for (int p = 0; p < PLANES; ++p) {
-            now[t][p] = next[m % XA][t][p];
-            if (m + XA < 4 || c + 1 < c1) next[m % XA][t][p] = load_b128(xp[t] + (size_t)p * xw + (m + XA) * 32);
-          }
-#pragma unroll
-        for (int mt = 0; mt < MT; ++mt) {
-          uint32_t lo[4], hi[4];
-          widen<!LIN>(code[(m % LM) * NB + 2 * mt], z[2 * mt], lo);
-          widen<!LIN>(code[(m % LM) * NB + 2 * mt + 1], z[2 * mt + 1], hi);
-#pragma unroll
-          for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int p = 0; p < PLANES; ++p) {
-              mma_f16(grp[mt][t], lo[0], hi[0], lo[1], hi[1], now[t][p].x, now[t][p].y);
-              mma_f16(grp[mt][t], lo[2], hi[2], lo[3], hi[3], now[t][p].z, now[t][p].w);
-            }
-        }
-        if ((m + 1) * NG % 4 == 0 && (NG == 1 || c * NG + m * NG / 4 < A.groups)) {  // a group ends (the last step may have fewer)
-#pragma unroll
-          for (int mt = 0; mt < MT; ++mt)
+        if constexpr (!WHOLE) {
+          if (m < 3 || more)
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-              for (int i = 0; i < 4; ++i) acc[mt][t][i] = fmaf(sc[2 * mt + (i >> 1)], grp[mt][t][i], acc[mt][t][i]);
+              for (int p = 0; p < PLANES; ++p) xb[(m + 1) % 2][t][p] = load_b128(xp[t] + (size_t)p * xw + (m + 1) * 32);
+        }
+        uint32_t w[NB][4];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) widen<!LIN>(code[(m % LM) * NB + b], Z ? (z[b] & 15) * 0x00010001u : 0x00080008u, w[b]);
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p)
+#pragma unroll
+              for (int mt = 0; mt < MT; ++mt) {
+                const uint4 x = xb[m % XB][t][p];
+                const uint32_t(&lo)[4] = w[2 * mt], (&hi)[4] = w[2 * mt + 1];
+                if (m * NG % 4 == 0 && half == 0 && p == 0) mma_f16_first(grp[mt][t], lo[0], hi[0], lo[1], hi[1], x.x, x.y);
+                else if (half == 0) mma_f16(grp[mt][t], lo[0], hi[0], lo[1], hi[1], x.x, x.y);
+                else mma_f16(grp[mt][t], lo[2], hi[2], lo[3], hi[3], x.z, x.w);
+              }
+        if constexpr (WHOLE) {
+          if (more) xb[m][0][0] = load_b128(xp[0] + QCOLS + m * 32);
+        }
+        if ((m + 1) * NG % 4 == 0 && (NG == 1 || c * NG + m * NG / 4 < A.groups)) {  // a group ends (the last step may have fewer)
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            // - z, and the group's sum less z sum x
+            const float zf = Z ? 8388608.f - __uint_as_float(0x4b000000u | (z[b] & 15)) : -8.f;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+                const float v = grp[b >> 1][t][(b & 1) * 2 + i];
+                float& a = acc[b >> 1][t][(b & 1) * 2 + i];
+                a = fmaf(sc[b], LIN ? fmaf(zf, gx[t][i], v) : v, a);
+              }
+          }
+          fetch();
         }
       }
 #pragma unroll
@@ -424,10 +434,11 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
   QuantWarp<PLANES, MT, NG, Z, DEPTH> W(A, first, at, i1, w, lane, (uint32_t)__cvta_generic_to_shared(smem + w * (DEPTH * MT * 1024)));
   W.aim();
 #pragma unroll 1
-  for (int i = 0; i < DEPTH; ++i) W.request();
+  for (int i = 0; i < DEPTH; ++i) W.request(i * MT * 1024);
   pdl_wait();  // x in fp16
 
-  int slot = 0, flip = 0;
+  uint32_t slot = 0;
+  int flip = 0;
   for (; at.item < i1; quant_next(at, i1, first, A.tile_groups)) {
     const int row0 = row_begin(at.e) + at.pass * Q_TOKENS, rows = min(row_end(at.e) - row0, Q_TOKENS);
     float acc[MT][2][4] = {};
@@ -545,6 +556,8 @@ deamoe_status_t deamoe_quant_product(void* cuda_stream, int32_t dtype, const uin
   if (n_in % 32 != 0 || (swiglu && n_out % 2 != 0) || n_expert > DEAMOE_MAX_EXPERTS || n_in > DEAMOE_MAX_WIDTH ||
       n_out > DEAMOE_MAX_WIDTH)
     return DEAMOE_ERR_UNSUPPORTED;
+  // the kernel holds offsets within a matrix's scales in 32 bits
+  if ((uint64_t)n_out * ((n_in + group - 1) / group) * 4 > UINT32_MAX) return DEAMOE_ERR_UNSUPPORTED;
   if (n_rows < 0 || n_token < 0) return DEAMOE_ERR_BATCH;
   if (n_rows == 0) return DEAMOE_OK;
   const size_t es = type_bytes(dtype);
