@@ -26,7 +26,8 @@
 namespace deamoe {
 
 constexpr int QW = 8;        // warps of a block
-constexpr int QCOLS = 128;   // columns of a step: 64 bytes of a row
+constexpr int QCOLS = 256;   // columns of a step: 128 bytes of a row
+constexpr int QM = QCOLS / 32;  // its parts of 32 columns: two matrix instructions
 constexpr int Q_GRID = 296;  // two blocks on each of the 148 SMs
 
 struct QuantArgs {
@@ -180,10 +181,10 @@ static __device__ __forceinline__ void quant_next(QuantAt& at, int end, const in
 constexpr int Q_TOKENS = 16;  // tokens of a pass
 
 // A block takes a contiguous share of the items; its warps split an item's columns (wk of them a tile of 16 MT rows).
-// Every warp streams its own codes, DEPTH steps of 16 MT rows x 128 columns ahead and across items, into its own part
+// Every warp streams its own codes, DEPTH steps of 16 MT rows x 256 columns ahead and across items, into its own part
 // of shared memory; nothing is shared between warps but the sums at an item's end.
 template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
-  static constexpr int STEP = MT * 1024, NB = 2 * MT;  // NB: blocks of 8 matrix rows in a warp tile
+  static constexpr int STEP = MT * 2048, NB = 2 * MT;  // NB: blocks of 8 matrix rows in a warp tile
   // Matrices narrower than a warp tile are MT = 1's; else the last tile of a matrix is moved up to its last row, so that
   // every row of every tile exists (the rows that it shares with the tile before are computed twice and written once).
   static constexpr bool NARROW = MT == 1;
@@ -231,7 +232,7 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
     const size_t row = (size_t)ahead.e * A.n_out + p_out, half = A.n_in / 2;
 #pragma unroll
     for (int b = 0; b < NB; ++b) {
-      p_code[b] = A.codes + (row + rows_to(b)) * half + (size_t)c0 * 64 + j * 16;
+      p_code[b] = A.codes + (row + rows_to(b)) * half + (size_t)c0 * (QCOLS / 2) + j * 16;
       // the scales of the item to come: into the L2
       if (exists(p_out, b)) {
         const size_t i = (row + rows_to(b)) * A.groups + (size_t)c0 * NG;
@@ -245,14 +246,18 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
   // the next step's codes into the slot at byte `slot` of the ring
   __device__ __forceinline__ void request(uint32_t slot) {
     if (ahead.item < i1) {
-      const int bytes = p_c * QCOLS + j * 32 < A.n_in ? 16 : 0;  // 0: nothing is read, zeros are written
-      const uint32_t to = ring_at + slot + g * 64 + ((j ^ ((g >> 1) & 3)) * 16);
+      const int left = A.n_in - p_c * QCOLS - j * 32;  // columns from this lane's first piece on; the other is 128 further
+      const uint32_t to = ring_at + slot + g * 128 + ((j ^ g) * 16);
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         const bool have = exists(p_out, b);
-        asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(to + b * 512), "l"(have ? p_code[b] : A.codes),
-                     "r"(have ? bytes : 0) : "memory");
-        p_code[b] += 64;
+        const uint8_t* from = have ? p_code[b] : A.codes;
+        // 0 bytes: nothing is read, zeros are written
+        asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(to + b * 1024), "l"(from),
+                     "r"(have && left > 0 ? 16 : 0) : "memory");
+        asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1 + 64], 16, %2;" ::"r"((to ^ 64) + b * 1024), "l"(from),
+                     "r"(have && left > 128 ? 16 : 0) : "memory");
+        p_code[b] += QCOLS / 2;
       }
       if (++p_c == c1) {
         p_c = c0;
@@ -273,13 +278,13 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
     const uint8_t* z_at = A.zeros + s_first;
     const size_t xg_step = (size_t)A.n_rows + 32;
     const float* xg_at = A.xg + (size_t)c0 * NG * xg_step + row0 + j * 2;
-    int groups_left = min(c1 * NG, A.groups) - c0 * NG;
+    int groups_left = min(c1 * NG, A.groups) - c0 * NG;  // from the one at hand on (the last step may have fewer than NG)
     // of the group at hand: scale and zero point of the lane's rows, sums of x of the lane's tokens of the products.  Loaded
     // when the group before is done with them
     float sc[NB], gx[NT][2];
     uint32_t z[NB];
     auto fetch = [&]() {
-      if (groups_left-- > 0) {
+      if (groups_left > 0) {
         if constexpr (LIN) {
 #pragma unroll
           for (int t = 0; t < NT; ++t) {
@@ -316,8 +321,8 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
     fetch();
     // tokens past the last take the last one's values: their sums are not looked at
     const __half* xp[NT];
-    constexpr bool WHOLE = PLANES * NT == 1;  // x a whole step ahead where registers allow, else a quarter
-    constexpr int XB = WHOLE ? 4 : 2;
+    // parts of x ahead: as many as registers allow
+    constexpr int XB = PLANES * NT == 1 ? 4 : 2;
     uint4 xb[XB][NT][PLANES];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -325,31 +330,31 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
 #pragma unroll
       for (int p = 0; p < PLANES; ++p)
 #pragma unroll
-        for (int m = 0; m < (WHOLE ? 4 : 1); ++m) xb[m][t][p] = load_b128(xp[t] + (size_t)p * xw + m * 32);
+        for (int m = 0; m < (XB == 4 ? 4 : 1); ++m) xb[m][t][p] = load_b128(xp[t] + (size_t)p * xw + m * 32);
     }
-    // the lane's row of the eight matrices an ldmatrix takes: block lane / 8 (MT == 1: block and quarter step)
-    const uint32_t lane_at = ring_at + (MT == 2 ? (lane >> 3) : (lane >> 3) & 1) * 512 + (lane & 7) * 64 +
-                             ((((lane & 7) >> 1) ^ (MT == 2 ? 0 : lane >> 4)) & 3) * 16;
+    // the lane's row of the eight matrices an ldmatrix takes: block lane / 8 (MT == 1: block and part)
+    const uint32_t lane_at = ring_at + (MT == 2 ? (lane >> 3) : (lane >> 3) & 1) * 1024 + (lane & 7) * 128 +
+                             ((lane & 7) ^ (MT == 2 ? 0 : lane >> 4)) * 16;
 #pragma unroll 1
     for (int c = c0; c < c1; ++c) {
       const bool more = c + 1 < c1;
       asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
       __syncwarp();
-      uint32_t code[NB * LM];  // the codes of LM quarter steps
+      uint32_t code[NB * LM];  // the codes of LM parts
       const uint32_t from = lane_at + slot;
       float grp[MT][NT][4];
 #pragma unroll
-      for (int m = 0; m < 4; ++m) {
+      for (int m = 0; m < QM; ++m) {
         if (m % LM == 0)
           asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                        : "=r"(code[0]), "=r"(code[1]), "=r"(code[2]), "=r"(code[3]) : "r"(from ^ (m * 16)) : "memory");
-        if (m == 4 - LM) {  // the slot has been read
+        if (m == QM - LM) {  // the slot has been read
           __syncwarp();
           request(slot);
           slot = slot + STEP == DEPTH * STEP ? 0 : slot + STEP;
         }
-        if constexpr (!WHOLE) {
-          if (m < 3 || more)
+        if constexpr (XB == 2) {
+          if (m + 1 < QM || more)
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
@@ -368,14 +373,15 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
               for (int mt = 0; mt < MT; ++mt) {
                 const uint4 x = xb[m % XB][t][p];
                 const uint32_t(&lo)[4] = w[2 * mt], (&hi)[4] = w[2 * mt + 1];
-                if (m * NG % 4 == 0 && half == 0 && p == 0) mma_f16_first(grp[mt][t], lo[0], hi[0], lo[1], hi[1], x.x, x.y);
+                if (m * NG % QM == 0 && half == 0 && p == 0) mma_f16_first(grp[mt][t], lo[0], hi[0], lo[1], hi[1], x.x, x.y);
                 else if (half == 0) mma_f16(grp[mt][t], lo[0], hi[0], lo[1], hi[1], x.x, x.y);
                 else mma_f16(grp[mt][t], lo[2], hi[2], lo[3], hi[3], x.z, x.w);
               }
-        if constexpr (WHOLE) {
-          if (more) xb[m][0][0] = load_b128(xp[0] + QCOLS + m * 32);
+        if constexpr (XB == 4) {
+          if (m + 4 < QM || more) xb[m % 4][0][0] = load_b128(xp[0] + (m + 4) * 32);
         }
-        if ((m + 1) * NG % 4 == 0 && (NG == 1 || c * NG + m * NG / 4 < A.groups)) {  // a group ends (the last step may have fewer)
+        if ((m + 1) * NG % QM == 0) {  // a group ends
+          if (groups_left > 0)
 #pragma unroll
           for (int b = 0; b < NB; ++b) {
             // - z, and the group's sum less z sum x
@@ -389,6 +395,7 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
                 a = fmaf(sc[b], LIN ? fmaf(zf, gx[t][i], v) : v, a);
               }
           }
+          --groups_left;
           fetch();
         }
       }
@@ -402,8 +409,8 @@ template <typename T, int PLANES, int MT, int NG, bool Z, int DEPTH>
 __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int warp_sums[QW];
-  float4* sums = reinterpret_cast<float4*>(smem + QW * DEPTH * MT * 1024);  // [2][QW][MT][2][32]
-  int* first = reinterpret_cast<int*>(sums + 2 * QW * MT * 2 * 32);            // [n_expert + 1] first item of each expert
+  float4* sums = reinterpret_cast<float4*>(smem + QW * DEPTH * MT * 2048);  // [2][QW][MT][32]
+  int* first = reinterpret_cast<int*>(sums + 2 * QW * MT * 32);            // [n_expert + 1] first item of each expert
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, R = A.n_rows;
   auto row_begin = [&](int e) { return A.expert_off ? min(max(A.expert_off[e], 0), R) : 0; };
   auto row_end = [&](int e) { return A.expert_off ? min(max(A.expert_off[e + 1], 0), R) : R; };
@@ -431,38 +438,23 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
     at.pass = (i0 - first[at.e]) - at.tg * at.passes;
   }
   const int width = A.swiglu ? A.n_out / 2 : A.n_out;
-  QuantWarp<PLANES, MT, NG, Z, DEPTH> W(A, first, at, i1, w, lane, (uint32_t)__cvta_generic_to_shared(smem + w * (DEPTH * MT * 1024)));
+  QuantWarp<PLANES, MT, NG, Z, DEPTH> W(A, first, at, i1, w, lane, (uint32_t)__cvta_generic_to_shared(smem + w * (DEPTH * MT * 2048)));
   W.aim();
 #pragma unroll 1
-  for (int i = 0; i < DEPTH; ++i) W.request(i * MT * 1024);
+  for (int i = 0; i < DEPTH; ++i) W.request(i * MT * 2048);
   pdl_wait();  // x in fp16
 
   uint32_t slot = 0;
   int flip = 0;
-  for (; at.item < i1; quant_next(at, i1, first, A.tile_groups)) {
-    const int row0 = row_begin(at.e) + at.pass * Q_TOKENS, rows = min(row_end(at.e) - row0, Q_TOKENS);
-    float acc[MT][2][4] = {};
-    if (rows <= 8) W.template item<1>(at, row0, rows, slot, acc);
-    else W.template item<2>(at, row0, rows, slot, acc);
-    // join the column shares of the tile's warps, in order.  Two buffers: one is written while slower warps still read
-    // the other, and no warp is two items ahead of its partners
-    const int tile_warp = W.wr * A.wk;  // the tile's first warp
-    float4* mine = sums + (size_t)(flip * QW + w) * MT * 2 * 32 + lane;
-#pragma unroll
-    for (int mt = 0; mt < MT; ++mt)
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-        if (t * 8 < rows) mine[(mt * 2 + t) * 32] = make_float4(acc[mt][t][0], acc[mt][t][1], acc[mt][t][2], acc[mt][t][3]);
-    if (A.wk == 1) __syncwarp();
-    else asm volatile("bar.sync %0, %1;" ::"r"(1 + W.wr), "r"(A.wk * 32) : "memory");
-    // a thread: one token, one tile row g and its partner g + 8
-    for (int i = threadIdx.x - tile_warp * 32; i < MT * 128; i += A.wk * 32) {
-      const int h = i & 1, l = (i >> 1) & 31, t = (i >> 6) & 1, mt = i >> 7;
+  // a thread: one token, one tile row g and its partner g + 8
+  auto join = [&](int t, const QuantAt& at, int row0, int rows, int tile_warp) {
+    for (int i = threadIdx.x - tile_warp * 32; i < MT * 64; i += A.wk * 32) {
+      const int h = i & 1, l = (i >> 1) & 31, mt = i >> 6;
       const int token = t * 8 + (l & 3) * 2 + h;
       if (token >= rows) continue;
       float a = 0.f, b = 0.f;
       for (int k = 0; k < A.wk; ++k) {
-        const float* v = reinterpret_cast<const float*>(sums + ((size_t)(flip * QW + tile_warp + k) * MT * 2 + mt * 2 + t) * 32 + l);
+        const float* v = reinterpret_cast<const float*>(sums + ((size_t)(flip * QW + tile_warp + k) * MT + mt) * 32 + l);
         a += v[h];
         b += v[h + 2];
       }
@@ -490,7 +482,26 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
       if (w0) out[o] = from_f<T>(a);
       if (w1) out[o + 8] = from_f<T>(b);
     }
-    flip ^= 1;
+  };
+  for (; at.item < i1; quant_next(at, i1, first, A.tile_groups)) {
+    const int row0 = row_begin(at.e) + at.pass * Q_TOKENS, rows = min(row_end(at.e) - row0, Q_TOKENS);
+    float acc[MT][2][4] = {};
+    if (rows <= 8) W.template item<1>(at, row0, rows, slot, acc);
+    else W.template item<2>(at, row0, rows, slot, acc);
+    // join the column shares of the tile's warps, in order, 8 tokens at a time.  Two buffers: one is written while slower
+    // warps still read the other, and no warp is two turns ahead of its partners
+    const int tile_warp = W.wr * A.wk;  // the tile's first warp
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      if (t * 8 >= rows) break;
+      float4* mine = sums + (size_t)(flip * QW + w) * MT * 32 + lane;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) mine[mt * 32] = make_float4(acc[mt][t][0], acc[mt][t][1], acc[mt][t][2], acc[mt][t][3]);
+      if (A.wk == 1) __syncwarp();
+      else asm volatile("bar.sync %0, %1;" ::"r"(1 + W.wr), "r"(A.wk * 32) : "memory");
+      join(t, at, row0, rows, tile_warp);
+      flip ^= 1;
+    }
   }
 }
 
@@ -515,16 +526,16 @@ template <typename T, int NG> static deamoe_status_t quant_t(QuantArgs& A, cudaS
       if (e != cudaSuccess) return e;
       done.fetch_or(1ull << dev, std::memory_order_release);
     }
-    const size_t smem = (size_t)QW * depth * mt * 1024 + (size_t)QW * mt * 2048 + (size_t)(A.n_expert + 1) * 4;
+    const size_t smem = (size_t)QW * depth * mt * 2048 + (size_t)QW * mt * 1024 + (size_t)(A.n_expert + 1) * 4;
     k_quant_x<T, PLANES, QCOLS / NG><<<A.n_rows, 256, 0, s>>>(A);
     const cudaError_t e = cudaGetLastError();
     return e != cudaSuccess ? e : launch_pdl(kernel, dim3(Q_GRID), dim3(QW * 32), smem, s, A);
   };
   static std::atomic<uint64_t> done[4];
-  const cudaError_t e = mt == 2 ? (A.zeros ? run(k_quant<T, PLANES, 2, NG, true, 3>, 3, done[0])
-                                           : run(k_quant<T, PLANES, 2, NG, false, 3>, 3, done[1]))
-                                : (A.zeros ? run(k_quant<T, PLANES, 1, NG, true, 6>, 6, done[2])
-                                           : run(k_quant<T, PLANES, 1, NG, false, 6>, 6, done[3]));
+  const cudaError_t e = mt == 2 ? (A.zeros ? run(k_quant<T, PLANES, 2, NG, true, 2>, 2, done[0])
+                                           : run(k_quant<T, PLANES, 2, NG, false, 2>, 2, done[1]))
+                                : (A.zeros ? run(k_quant<T, PLANES, 1, NG, true, 4>, 4, done[2])
+                                           : run(k_quant<T, PLANES, 1, NG, false, 4>, 4, done[3]));
   if (e == cudaSuccess) return DEAMOE_OK;
   cudaGetLastError();
   return DEAMOE_ERR_CUDA;
@@ -583,9 +594,9 @@ deamoe_status_t deamoe_quant_product(void* cuda_stream, int32_t dtype, const uin
   A.xg = reinterpret_cast<float*>(A.xe + (size_t)2 * n_rows);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
   if (dtype == DEAMOE_F32)
-    return group == 128 ? quant_t<float, 1>(A, s) : group == 64 ? quant_t<float, 2>(A, s) : quant_t<float, 4>(A, s);
-  return group == 128 ? quant_t<__nv_bfloat16, 1>(A, s)
-                      : group == 64 ? quant_t<__nv_bfloat16, 2>(A, s) : quant_t<__nv_bfloat16, 4>(A, s);
+    return group == 128 ? quant_t<float, 2>(A, s) : group == 64 ? quant_t<float, 4>(A, s) : quant_t<float, 8>(A, s);
+  return group == 128 ? quant_t<__nv_bfloat16, 2>(A, s)
+                      : group == 64 ? quant_t<__nv_bfloat16, 4>(A, s) : quant_t<__nv_bfloat16, 8>(A, s);
 }
 
 }  // extern "C"
