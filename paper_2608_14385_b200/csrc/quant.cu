@@ -512,10 +512,10 @@ template <typename T, int NG> static deamoe_status_t quant_t(QuantArgs& A, cudaS
   // Two row tiles a warp share its x values and loop; one where that would leave blocks without work
   const int mt = (int64_t)(tiles16 / 2) * active >= Q_GRID && A.n_out >= 32 ? 2 : 1;
   // Warps that share a tile's columns: all, or fewer (longer walks, fewer sums to join) while the blocks keep at least
-  // 16 items each, so that their counts differ by little
+  // 8 items each, so that their counts differ by little
   A.wk = QW;
   while (A.wk > A.steps) A.wk /= 2;
-  while (A.wk > 1 && (int64_t)((tiles16 + mt - 1) / mt) * (A.wk / 2) / QW * active >= 16 * Q_GRID) A.wk /= 2;
+  while (A.wk > 1 && (int64_t)((tiles16 + mt - 1) / mt) * (A.wk / 2) / QW * active >= 8 * Q_GRID) A.wk /= 2;
   const int per = QW / A.wk * mt;
   A.tile_groups = (tiles16 + per - 1) / per;
   auto run = [&](auto kernel, int depth, std::atomic<uint64_t>& done) {
