@@ -25,17 +25,16 @@ namespace deamoe {
 // as many blocks as fill the SMs' thread slots (rows of up to 8192 values, else two blocks an SM).
 constexpr int NORM_SMS = 148;
 constexpr int GRAD_COLUMNS = 8, GRAD_MAX_WIDTH = 8192;
-static int grad_threads(int h) { return ((h + GRAD_COLUMNS - 1) / GRAD_COLUMNS + 31) / 32 * 32; }
+static int grad_threads(int h, int columns) { return ((h + columns - 1) / columns + 31) / 32 * 32; }
 static int grad_blocks_per_sm(int h) {
   if (h > GRAD_MAX_WIDTH) return 2;
-  const int n = 1024 / grad_threads(h);
+  const int n = 1024 / grad_threads(h, GRAD_COLUMNS);
   return n > 8 ? 8 : n;
 }
 static int grad_ctas(int64_t T, int h) {
   const int most = NORM_SMS * grad_blocks_per_sm(h);
   return T < most ? (int)T : most;
 }
-
 
 struct Rows {  // a [T, h] matrix with a row stride (elements), or a null pointer
   const void* p;
@@ -388,64 +387,66 @@ static __device__ __forceinline__ void copies_wait_for(int stages) {  // all but
   else copies_wait<0>();
 }
 
-// NIN row-wise inputs of one row: through the ring (VE > 1) or straight from memory.
+// NIN row-wise inputs of the rows to come: through the ring (VE > 1) or straight from memory when they are used.
 template <typename T, int VE, int NV, int NIN> struct RowFeed {
-  Pack<T, VE> v[NIN][NV];
-  int stages, packs, nin;  // nin: inputs that have room in the ring (the last may be absent)
+  const Rows (&in)[NIN];
+  int64_t rows;
+  int packs, stages, nin;  // nin: inputs that have room in the ring (the last may be absent)
   uint4* ring;             // [stages][nin][NV][blockDim.x]
 
   __device__ __forceinline__ uint4* slot(int stage, int i, int n) const {
     return ring + ((size_t)(stage * nin + i) * NV + n) * blockDim.x + threadIdx.x;
   }
-  __device__ __forceinline__ void request(const Rows (&m)[NIN], int64_t t, int64_t T_, int stage) const {
+  __device__ __forceinline__ void request(int64_t t, int stage) const {
     if constexpr (VE > 1) {
-      if (t < T_)
+      if (t < rows)
 #pragma unroll
         for (int i = 0; i < NIN; ++i)
 #pragma unroll
           for (int n = 0; n < NV; ++n) {
             const int c = threadIdx.x + n * blockDim.x;
-            if (m[i].p && c < packs) copy_pack(slot(stage, i, n), row_at<T>(m[i], t) + (int64_t)c * VE);
+            if (in[i].p && c < packs) copy_pack(slot(stage, i, n), row_at<T>(in[i], t) + (int64_t)c * VE);
           }
       copies_commit();
     }
   }
-  __device__ __forceinline__ void take(const Rows (&m)[NIN], int64_t t, int stage) {
+  __device__ __forceinline__ void wait() const {
     if constexpr (VE > 1) copies_wait_for(stages);
-#pragma unroll
-    for (int i = 0; i < NIN; ++i)
-#pragma unroll
-      for (int n = 0; n < NV; ++n) {
-        const int c = threadIdx.x + n * blockDim.x;
-        if (!m[i].p || c >= packs) continue;
-        if constexpr (VE > 1) v[i][n].r = *slot(stage, i, n);
-        else v[i][n] = load_once<T, VE>(row_at<T>(m[i], t) + (int64_t)c * VE);
-      }
+  }
+  __device__ __forceinline__ Pack<T, VE> get(int i, int64_t t, int stage, int n) const {
+    if constexpr (VE > 1) {
+      Pack<T, VE> v;
+      v.r = *slot(stage, i, n);
+      return v;
+    } else {
+      return load_once<T, VE>(row_at<T>(in[i], t) + (int64_t)(threadIdx.x + n * blockDim.x) * VE);
+    }
   }
 };
 
 template <typename T, int VE, int NV, int MAXT>
-__global__ void __launch_bounds__(MAXT) k_norm_grad_rows(NormArgs A, int packs, int stages) {
+__global__ void __launch_bounds__(MAXT, 1024 / MAXT) k_norm_grad_rows(NormArgs A, int packs, int stages) {
   extern __shared__ uint4 ring[];
-  __shared__ float buf[2][64];
+  __shared__ float buf[2][64];  // taken in turn: a sum's buffer is free again after the next sum's barrier
   const Rows in[3] = {A.x, A.du, A.dadd};
-  RowFeed<T, VE, NV, 3> F;
-  F.stages = stages; F.packs = packs; F.ring = ring; F.nin = A.dadd.p ? 3 : 2;
+  const RowFeed<T, VE, NV, 3> F{in, A.T, packs, stages, A.dadd.p ? 3 : 2, ring};
+  const bool add = A.dadd.p != nullptr;
   float acc[NV][VE] = {};
-  for (int i = 0; i < stages; ++i) F.request(in, blockIdx.x + (int64_t)i * gridDim.x, A.T, i);
+  for (int i = 0; i < stages; ++i) F.request(blockIdx.x + (int64_t)i * gridDim.x, i);
   int stage = 0, flip = 0;
   for (int64_t t = blockIdx.x; t < A.T; t += gridDim.x) {
-    F.take(in, t, stage);
-    F.request(in, t + (int64_t)stages * gridDim.x, A.T, stage);
-    stage = stage + 1 == stages ? 0 : stage + 1;
+    Pack<T, VE> px[NV], pd[NV];
     float s[2] = {0.f, 0.f};
+    F.wait();
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
       const int c = threadIdx.x + n * blockDim.x;
       if (c >= packs) continue;
       float x[VE], d[VE], w[VE];
-      F.v[0][n].widen(x);
-      F.v[1][n].widen(d);
+      px[n] = F.get(0, t, stage, n);
+      pd[n] = F.get(1, t, stage, n);
+      px[n].widen(x);
+      pd[n].widen(d);
       load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
@@ -462,22 +463,25 @@ __global__ void __launch_bounds__(MAXT) k_norm_grad_rows(NormArgs A, int packs, 
       const int c = threadIdx.x + n * blockDim.x;
       if (c >= packs) continue;
       float x[VE], d[VE], w[VE], o[VE];
-      F.v[0][n].widen(x);
-      F.v[1][n].widen(d);
+      px[n].widen(x);
+      pd[n].widen(d);
       load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
-        acc[n][j] = fmaf(d[j] * r, x[j], acc[n][j]);
-        o[j] = r * d[j] * w[j] - x[j] * cc;
+        const float rd = r * d[j];
+        acc[n][j] = fmaf(rd, x[j], acc[n][j]);
+        o[j] = fmaf(rd, w[j], -x[j] * cc);
       }
-      if (A.dadd.p) {
+      if (add) {
         float e[VE];
-        F.v[2][n].widen(e);
+        F.get(2, t, stage, n).widen(e);
 #pragma unroll
         for (int j = 0; j < VE; ++j) o[j] += e[j];
       }
       store_row<T, VE>(A.dx, A.dx_s, t, c, o);
     }
+    F.request(t + (int64_t)stages * gridDim.x, stage);
+    stage = stage + 1 == stages ? 0 : stage + 1;
   }
   float* part = A.part + (size_t)blockIdx.x * A.h;
 #pragma unroll
@@ -489,25 +493,43 @@ __global__ void __launch_bounds__(MAXT) k_norm_grad_rows(NormArgs A, int packs, 
   }
 }
 
-template <typename T, int VE, int NV, int MAXT>
-__global__ void __launch_bounds__(MAXT) k_residual_grad_rows(NormArgs A, int packs, int stages, size_t part_step) {
+// With p = b g w (a column's constant unless the gate is full) and gt the token's gate (or 1):
+//   s = a x + gt ry p y,   D = dout + ro du wn - co s,   dx = a D,   sum3 = sum p D y,
+//   dy = gt ry p D - y gt ry^3 sum3 / h,   dgate_token = ry sum3,   E = gt ry D y,
+//   dw = b g sum_t E,   dgate_channel = b w sum_t E   -- one accumulator a column for both.
+template <typename T, int VE, int NV, int MAXT, bool FULL>
+__global__ void __launch_bounds__(MAXT, 1) k_residual_grad_rows(NormArgs A, int packs, int stages, size_t part_step) {
   extern __shared__ uint4 ring[];
-  __shared__ float buf[2][64];  // taken in turn: a sum's buffer is free again after the next sum's barrier
-  const bool full = A.gate_kind == DEAMOE_GATE_FULL;
-  const Rows in[5] = {A.x, A.y, A.dout, A.du, {full ? A.gate.p : nullptr, A.gate.stride}};
-  RowFeed<T, VE, NV, 5> F;
-  F.stages = stages; F.packs = packs; F.ring = ring; F.nin = full ? 5 : 4;
-  float acc_w[NV][VE] = {}, acc_n[NV][VE] = {}, acc_g[NV][VE] = {};
-  for (int i = 0; i < stages; ++i) F.request(in, blockIdx.x + (int64_t)i * gridDim.x, A.T, i);
+  __shared__ float buf[2][64];
+  const Rows in[5] = {A.x, A.y, A.dout, A.du, {FULL ? A.gate.p : nullptr, A.gate.stride}};
+  const RowFeed<T, VE, NV, 5> F{in, A.T, packs, stages, FULL ? 5 : 4, ring};
+  float acc_e[NV][VE] = {}, acc_n[NV][VE] = {}, p[NV][VE], q[NV][VE];
+  auto channel_gate = [&](int c, float (&g)[VE]) {
+#pragma unroll
+    for (int j = 0; j < VE; ++j) g[j] = 1.f;
+    if (A.gate_kind == DEAMOE_GATE_CHANNEL) load_pack<T, VE>(reinterpret_cast<const T*>(A.gate.p) + (int64_t)c * VE).widen(g);
+  };
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    const int c = threadIdx.x + n * blockDim.x;
+    if (c >= packs) continue;
+    float g[VE];
+    channel_gate(c, g);
+    load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, p[n]);
+    load_gains<VE>(A.wn, A.wdt, (int64_t)c * VE, q[n]);
+#pragma unroll
+    for (int j = 0; j < VE; ++j) p[n][j] *= A.b * g[j];
+  }
+  for (int i = 0; i < stages; ++i) F.request(blockIdx.x + (int64_t)i * gridDim.x, i);
   int stage = 0, flip = 0;
   for (int64_t t = blockIdx.x; t < A.T; t += gridDim.x) {
-    F.take(in, t, stage);
-    F.request(in, t + (int64_t)stages * gridDim.x, A.T, stage);
-    stage = stage + 1 == stages ? 0 : stage + 1;
-    auto gate = [&](int n, int c, float (&g)[VE]) {
-      if (full) F.v[4][n].widen(g);
-      else load_gate<T, VE>(A, t, c, g);
-    };
+    Pack<T, VE> py[NV], pu[NV];
+    float d[NV][VE];
+    const float gt = A.gate_kind == DEAMOE_GATE_TOKEN ? to_f<T>(reinterpret_cast<const T*>(A.gate.p)[t]) : 1.f;
+    F.wait();
+#pragma unroll
+    for (int n = 0; n < NV; ++n)
+      if ((int)(threadIdx.x + n * blockDim.x) < packs) py[n] = F.get(1, t, stage, n);
     float ry = 1.f;
     if (A.post_norm) {
       float ss[1] = {0.f};
@@ -515,7 +537,7 @@ __global__ void __launch_bounds__(MAXT) k_residual_grad_rows(NormArgs A, int pac
       for (int n = 0; n < NV; ++n)
         if ((int)(threadIdx.x + n * blockDim.x) < packs) {
           float y[VE];
-          F.v[1][n].widen(y);
+          py[n].widen(y);
 #pragma unroll
           for (int j = 0; j < VE; ++j) ss[0] = fmaf(y[j], y[j], ss[0]);
         }
@@ -523,27 +545,25 @@ __global__ void __launch_bounds__(MAXT) k_residual_grad_rows(NormArgs A, int pac
       flip ^= 1;
       ry = inv_rms(ss[0], A.h, A.eps);
     }
-    // the sum after the block, recomputed; then the gradient that reaches it
-    float d[NV][VE];
+    const float gr = gt * ry;
     float ro = 1.f, co = 0.f;
-    if (A.next_norm) {
+    if (A.next_norm) {  // the sum after the block once more
       float s[2] = {0.f, 0.f};
 #pragma unroll
       for (int n = 0; n < NV; ++n) {
-        const int c = threadIdx.x + n * blockDim.x;
-        if (c >= packs) continue;
-        float x[VE], y[VE], w[VE], g[VE], u[VE], wn[VE];
-        F.v[0][n].widen(x);
-        F.v[1][n].widen(y);
-        F.v[3][n].widen(u);
-        load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
-        load_gains<VE>(A.wn, A.wdt, (int64_t)c * VE, wn);
-        gate(n, c, g);
+        if ((int)(threadIdx.x + n * blockDim.x) >= packs) continue;
+        float x[VE], y[VE], u[VE], g[VE];
+        F.get(0, t, stage, n).widen(x);
+        py[n].widen(y);
+        pu[n] = F.get(3, t, stage, n);
+        pu[n].widen(u);
+        if constexpr (FULL) F.get(4, t, stage, n).widen(g);
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
-          d[n][j] = fmaf(A.a, x[j], A.b * g[j] * (y[j] * ry * w[j]));
+          const float pj = FULL ? p[n][j] * g[j] : p[n][j];
+          d[n][j] = fmaf(gr * pj, y[j], A.a * x[j]);
           s[0] = fmaf(d[n][j], d[n][j], s[0]);
-          s[1] = fmaf(u[j] * wn[j], d[n][j], s[1]);
+          s[1] = fmaf(u[j] * q[n][j], d[n][j], s[1]);
         }
       }
       block_sums<2>(s, buf[flip]);
@@ -551,75 +571,79 @@ __global__ void __launch_bounds__(MAXT) k_residual_grad_rows(NormArgs A, int pac
       ro = inv_rms(s[0], A.h, A.next_eps);
       co = ro * ro * ro * (s[1] / (float)A.h);
     }
-    float s[2] = {0.f, 0.f};
+    float s3[1] = {0.f};
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
       const int c = threadIdx.x + n * blockDim.x;
       if (c >= packs) continue;
-      float y[VE], w[VE], g[VE], o[VE];
-      F.v[2][n].widen(o);
+      float o[VE], y[VE], g[VE];
+      F.get(2, t, stage, n).widen(o);
       if (A.next_norm) {
-        float u[VE], wn[VE];
-        F.v[3][n].widen(u);
-        load_gains<VE>(A.wn, A.wdt, (int64_t)c * VE, wn);
+        float u[VE];
+        pu[n].widen(u);
 #pragma unroll
         for (int j = 0; j < VE; ++j) {
-          const float sum = d[n][j];
-          acc_n[n][j] = fmaf(u[j] * ro, sum, acc_n[n][j]);
-          o[j] += ro * u[j] * wn[j] - sum * co;
+          const float ru = ro * u[j];
+          acc_n[n][j] = fmaf(ru, d[n][j], acc_n[n][j]);
+          o[j] = fmaf(ru, q[n][j], fmaf(-co, d[n][j], o[j]));
         }
       }
-      F.v[1][n].widen(y);
-      load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
-      gate(n, c, g);
+      py[n].widen(y);
+      if constexpr (FULL) F.get(4, t, stage, n).widen(g);
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
+        const float pj = FULL ? p[n][j] * g[j] : p[n][j];
         d[n][j] = o[j];
-        const float dw = A.b * o[j] * w[j];
-        s[0] = fmaf(dw * g[j], y[j], s[0]);
-        s[1] = fmaf(dw * ry, y[j], s[1]);
+        s3[0] = fmaf(pj * o[j], y[j], s3[0]);
         o[j] *= A.a;
       }
       store_row<T, VE>(A.dx, A.dx_s, t, c, o);
     }
     if (A.post_norm || A.dgate_token) {
-      block_sums<2>(s, buf[flip]);
+      block_sums<1>(s3, buf[flip]);
       flip ^= 1;
     }
-    const float cy = A.post_norm ? ry * ry * ry * (s[0] / (float)A.h) : 0.f;
-    if (A.dgate_token && threadIdx.x == 0) A.dgate_token[t] = s[1];
+    const float cy = A.post_norm ? gt * ry * ry * ry * (s3[0] / (float)A.h) : 0.f;
+    if (A.dgate_token && threadIdx.x == 0) A.dgate_token[t] = ry * s3[0];
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
       const int c = threadIdx.x + n * blockDim.x;
       if (c >= packs) continue;
-      float y[VE], w[VE], g[VE], o[VE];
-      F.v[1][n].widen(y);
-      load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
-      gate(n, c, g);
-      float dg[VE];
+      float y[VE], o[VE], g[VE], dg[VE];
+      py[n].widen(y);
+      if constexpr (FULL) F.get(4, t, stage, n).widen(g);
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
-        const float bd = A.b * d[n][j], dv = bd * g[j], yr = y[j] * ry;
-        acc_w[n][j] = fmaf(dv, yr, acc_w[n][j]);
-        dg[j] = bd * yr * w[j];
-        acc_g[n][j] += dg[j];
-        o[j] = ry * dv * w[j] - y[j] * cy;
+        const float gd = gr * d[n][j];
+        if constexpr (FULL) {
+          dg[j] = p[n][j] * gd * y[j];
+          acc_e[n][j] = fmaf(g[j] * gd, y[j], acc_e[n][j]);
+          o[j] = fmaf(p[n][j] * g[j], gd, -y[j] * cy);
+        } else {
+          acc_e[n][j] = fmaf(gd, y[j], acc_e[n][j]);
+          o[j] = fmaf(p[n][j], gd, -y[j] * cy);
+        }
       }
-      if (full) store_row<T, VE>(A.dgate, A.dgate_s, t, c, dg);
+      if constexpr (FULL) store_row<T, VE>(A.dgate, A.dgate_s, t, c, dg);
       store_row<T, VE>(A.dy, A.dy_s, t, c, o);
     }
+    F.request(t + (int64_t)stages * gridDim.x, stage);
+    stage = stage + 1 == stages ? 0 : stage + 1;
   }
   float* part = A.part + (size_t)blockIdx.x * A.h;
 #pragma unroll
   for (int n = 0; n < NV; ++n) {
     const int c = threadIdx.x + n * blockDim.x;
     if (c >= packs) continue;
+    float w[VE], g[VE];
+    channel_gate(c, g);
+    load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
       const size_t i = (size_t)c * VE + j;
-      if (A.w) part[i] = acc_w[n][j];
+      if (A.w) part[i] = A.b * g[j] * acc_e[n][j];
       if (A.wn) part[part_step + i] = acc_n[n][j];
-      if (A.gate_kind == DEAMOE_GATE_CHANNEL) part[2 * part_step + i] = acc_g[n][j];
+      if (A.gate_kind == DEAMOE_GATE_CHANNEL) part[2 * part_step + i] = A.b * w[j] * acc_e[n][j];
     }
   }
 }
@@ -731,44 +755,55 @@ template <typename T> static deamoe_status_t residual_t(const NormArgs& A, cudaS
 #undef DEAMOE_ROW_FORMS
 
 // Rows ahead in the ring: what the blocks of an SM can share of its shared memory, four at most.
-static int grad_stages(int h, size_t stage_bytes) {
-  const size_t n = RING_BYTES / grad_blocks_per_sm(h) / stage_bytes;
+static int grad_stages(int blocks_per_sm, size_t stage_bytes) {
+  const size_t n = RING_BYTES / blocks_per_sm / stage_bytes;
   return n > 4 ? 4 : (n < 1 ? 1 : (int)n);
+}
+template <typename K, typename... Rest>
+static deamoe_status_t run_grad(K* kernel, std::atomic<uint64_t>& done, const NormArgs& A, int ctas, int threads, int packs,
+                                size_t stage_bytes, cudaStream_t s, Rest... rest) {
+  int stages = 1;
+  if (stage_bytes) {
+    if (!whole_smem(kernel, done)) return DEAMOE_ERR_CUDA;
+    stages = grad_stages((ctas + NORM_SMS - 1) / NORM_SMS, stage_bytes);
+  }
+  kernel<<<ctas, threads, stage_bytes * stages, s>>>(A, packs, stages, rest...);
+  return ran();
 }
 
 template <typename T> static deamoe_status_t norm_grad_t(const NormArgs& A, cudaStream_t s) {
   constexpr int VE = 16 / sizeof(T), NV = GRAD_COLUMNS / VE;
-  const int ctas = grad_ctas(A.T, A.h), threads = grad_threads(A.h);
+  const int ctas = grad_ctas(A.T, A.h), threads = grad_threads(A.h, GRAD_COLUMNS);
+  static std::atomic<uint64_t> done[2];
   if (A.h > GRAD_MAX_WIDTH) {
     k_norm_grad_any<T><<<ctas, ANY_THREADS, 0, s>>>(A);
-  } else if (wide_call<T>(A)) {
-    static std::atomic<uint64_t> done{0};
-    if (!whole_smem(k_norm_grad_rows<T, VE, NV, 1024>, done)) return DEAMOE_ERR_CUDA;
-    const size_t stage = (size_t)(A.dadd.p ? 3 : 2) * NV * threads * 16;
-    const int stages = grad_stages(A.h, stage);
-    k_norm_grad_rows<T, VE, NV, 1024><<<ctas, threads, stage * stages, s>>>(A, A.h / VE, stages);
-  } else {
-    k_norm_grad_rows<T, 1, GRAD_COLUMNS, 1024><<<ctas, threads, 0, s>>>(A, A.h, 1);
+    return ran();
   }
-  return ran();
+  if (!wide_call<T>(A)) return run_grad(k_norm_grad_rows<T, 1, GRAD_COLUMNS, 1024>, done[0], A, ctas, threads, A.h, 0, s);
+  return run_grad(k_norm_grad_rows<T, VE, NV, 1024>, done[1], A, ctas, threads, A.h / VE,
+                  (size_t)(A.dadd.p ? 3 : 2) * NV * threads * 16, s);
 }
 
 template <typename T> static deamoe_status_t residual_grad_t(const NormArgs& A, cudaStream_t s) {
   constexpr int VE = 16 / sizeof(T), NV = GRAD_COLUMNS / VE;
-  const int ctas = grad_ctas(A.T, A.h), threads = grad_threads(A.h);
+  const int ctas = grad_ctas(A.T, A.h), threads = grad_threads(A.h, GRAD_COLUMNS);
   const size_t step = (size_t)ctas * A.h;
+  static std::atomic<uint64_t> done[6];
   if (A.h > GRAD_MAX_WIDTH) {
     k_residual_grad_any<T><<<ctas, ANY_THREADS, 0, s>>>(A, step);
-  } else if (wide_call<T>(A)) {
-    static std::atomic<uint64_t> done{0};
-    if (!whole_smem(k_residual_grad_rows<T, VE, NV, 1024>, done)) return DEAMOE_ERR_CUDA;
-    const size_t stage = (size_t)(A.gate_kind == DEAMOE_GATE_FULL ? 5 : 4) * NV * threads * 16;
-    const int stages = grad_stages(A.h, stage);
-    k_residual_grad_rows<T, VE, NV, 1024><<<ctas, threads, stage * stages, s>>>(A, A.h / VE, stages, step);
-  } else {
-    k_residual_grad_rows<T, 1, GRAD_COLUMNS, 1024><<<ctas, threads, 0, s>>>(A, A.h, 1, step);
+    return ran();
   }
-  return ran();
+  const bool full = A.gate_kind == DEAMOE_GATE_FULL, wide = wide_call<T>(A);
+  const size_t stage = wide ? (size_t)(full ? 5 : 4) * NV * threads * 16 : 0;
+  const int packs = wide ? A.h / VE : A.h;
+  if (!wide)
+    return full ? run_grad(k_residual_grad_rows<T, 1, GRAD_COLUMNS, 1024, true>, done[0], A, ctas, threads, packs, stage, s, step)
+                : run_grad(k_residual_grad_rows<T, 1, GRAD_COLUMNS, 1024, false>, done[1], A, ctas, threads, packs, stage, s, step);
+  if (threads <= 896)  // 72 registers a thread instead of 64
+    return full ? run_grad(k_residual_grad_rows<T, VE, NV, 896, true>, done[2], A, ctas, threads, packs, stage, s, step)
+                : run_grad(k_residual_grad_rows<T, VE, NV, 896, false>, done[3], A, ctas, threads, packs, stage, s, step);
+  return full ? run_grad(k_residual_grad_rows<T, VE, NV, 1024, true>, done[4], A, ctas, threads, packs, stage, s, step)
+              : run_grad(k_residual_grad_rows<T, VE, NV, 1024, false>, done[5], A, ctas, threads, packs, stage, s, step);
 }
 
 }  // namespace deamoe
