@@ -21,14 +21,15 @@
 
 namespace deamoe {
 
-// Thread blocks of the backward kernels, each of which leaves one row of partial column sums: 8 columns a thread, and
-// as many blocks as fill the SMs' thread slots (rows of up to 8192 values, else two blocks an SM).
+// Thread blocks of the backward kernels, each of which leaves one row of partial column sums: 16 columns a thread (a
+// row's fixed work -- addresses, the reduction -- is spread over more values than with 8, and 128 registers hold the
+// columns' constants and sums), 512 threads an SM (rows of up to 8192 values; else two blocks an SM).
 constexpr int NORM_SMS = 148;
-constexpr int GRAD_COLUMNS = 8, GRAD_MAX_WIDTH = 8192;
-static int grad_threads(int h, int columns) { return ((h + columns - 1) / columns + 31) / 32 * 32; }
+constexpr int GRAD_COLUMNS = 16, GRAD_MAX_WIDTH = 8192;
+static int grad_threads(int h) { return ((h + GRAD_COLUMNS - 1) / GRAD_COLUMNS + 31) / 32 * 32; }
 static int grad_blocks_per_sm(int h) {
   if (h > GRAD_MAX_WIDTH) return 2;
-  const int n = 1024 / grad_threads(h, GRAD_COLUMNS);
+  const int n = 512 / grad_threads(h);
   return n > 8 ? 8 : n;
 }
 static int grad_ctas(int64_t T, int h) {
@@ -376,9 +377,6 @@ template <typename T, int VE, int NV, int MAXT> __global__ void __launch_bounds_
 // registers.  A thread copies its own packs of the rows to come into shared memory (asynchronously, `stages` rows ahead)
 // and is the only one to read them back, so the loads of later rows run under a row's reductions without any barrier.
 template <int N> static __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-static __device__ __forceinline__ void copy_pack(uint4* to, const void* from) {
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(to)), "l"(from) : "memory");
-}
 static __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 static __device__ __forceinline__ void copies_wait_for(int stages) {  // all but the stages - 1 youngest groups are there
   if (stages >= 4) copies_wait<3>();
@@ -391,32 +389,45 @@ static __device__ __forceinline__ void copies_wait_for(int stages) {  // all but
 template <typename T, int VE, int NV, int NIN> struct RowFeed {
   const Rows (&in)[NIN];
   int64_t rows;
-  int packs, stages, nin;  // nin: inputs that have room in the ring (the last may be absent)
-  uint4* ring;             // [stages][nin][NV][blockDim.x]
+  int packs, stages;
+  uint32_t mine, pitch;  // shared address of this thread's first pack; bytes from one input's packs to the next's
+  uint32_t row_bytes;    // ... and from one row's to the next's
 
-  __device__ __forceinline__ uint4* slot(int stage, int i, int n) const {
-    return ring + ((size_t)(stage * nin + i) * NV + n) * blockDim.x + threadIdx.x;
+  __device__ __forceinline__ RowFeed(const Rows (&m)[NIN], int64_t T_, int packs_, int stages_, int nin, uint4* ring)
+      : in(m), rows(T_), packs(packs_), stages(stages_) {
+    mine = (uint32_t)__cvta_generic_to_shared(ring) + threadIdx.x * 16;
+    pitch = NV * blockDim.x * 16;
+    row_bytes = nin * pitch;
   }
-  __device__ __forceinline__ void request(int64_t t, int stage) const {
+  __device__ __forceinline__ uint32_t next(uint32_t at) const { return at + row_bytes == stages * row_bytes ? 0 : at + row_bytes; }
+  // `at`: byte offset of the row's slot in the ring
+  __device__ __forceinline__ void request(int64_t t, uint32_t at) const {
     if constexpr (VE > 1) {
       if (t < rows)
 #pragma unroll
-        for (int i = 0; i < NIN; ++i)
+        for (int i = 0; i < NIN; ++i) {
+          if (!in[i].p) continue;
+          const char* row = reinterpret_cast<const char*>(row_at<T>(in[i], t));
 #pragma unroll
           for (int n = 0; n < NV; ++n) {
-            const int c = threadIdx.x + n * blockDim.x;
-            if (in[i].p && c < packs) copy_pack(slot(stage, i, n), row_at<T>(in[i], t) + (int64_t)c * VE);
+            const uint32_t c = threadIdx.x + n * blockDim.x;
+            if ((int)c < packs)
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(mine + at + i * pitch + n * blockDim.x * 16), "l"(row + c * 16u)
+                           : "memory");
           }
+        }
       copies_commit();
     }
   }
-  __device__ __forceinline__ void wait() const {
-    if constexpr (VE > 1) copies_wait_for(stages);
+  // until the oldest `n` rows of the ring are there
+  __device__ __forceinline__ void wait_for(int n) const {
+    if constexpr (VE > 1) copies_wait_for(stages - n + 1);
   }
-  __device__ __forceinline__ Pack<T, VE> get(int i, int64_t t, int stage, int n) const {
+  __device__ __forceinline__ Pack<T, VE> get(int i, int64_t t, uint32_t at, int n) const {
     if constexpr (VE > 1) {
       Pack<T, VE> v;
-      v.r = *slot(stage, i, n);
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];"
+                   : "=r"(v.r.x), "=r"(v.r.y), "=r"(v.r.z), "=r"(v.r.w) : "r"(mine + at + i * pitch + n * blockDim.x * 16) : "memory");
       return v;
     } else {
       return load_once<T, VE>(row_at<T>(in[i], t) + (int64_t)(threadIdx.x + n * blockDim.x) * VE);
@@ -425,36 +436,41 @@ template <typename T, int VE, int NV, int NIN> struct RowFeed {
 };
 
 template <typename T, int VE, int NV, int MAXT>
-__global__ void __launch_bounds__(MAXT, 1024 / MAXT) k_norm_grad_rows(NormArgs A, int packs, int stages) {
+__global__ void __launch_bounds__(MAXT, 1) k_norm_grad_rows(NormArgs A, int packs, int stages) {
   extern __shared__ uint4 ring[];
   __shared__ float buf[2][64];  // taken in turn: a sum's buffer is free again after the next sum's barrier
   const Rows in[3] = {A.x, A.du, A.dadd};
-  const RowFeed<T, VE, NV, 3> F{in, A.T, packs, stages, A.dadd.p ? 3 : 2, ring};
+  const RowFeed<T, VE, NV, 3> F(in, A.T, packs, stages, A.dadd.p ? 3 : 2, ring);
   const bool add = A.dadd.p != nullptr;
-  float acc[NV][VE] = {};
-  for (int i = 0; i < stages; ++i) F.request(blockIdx.x + (int64_t)i * gridDim.x, i);
-  int stage = 0, flip = 0;
+  float acc[NV][VE] = {}, w[NV][VE];
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    const int c = threadIdx.x + n * blockDim.x;
+    if (c < packs) load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w[n]);
+  }
+  for (int i = 0; i < stages; ++i) F.request(blockIdx.x + (int64_t)i * gridDim.x, i * F.row_bytes);
+  uint32_t stage = 0;
+  int flip = 0;
   for (int64_t t = blockIdx.x; t < A.T; t += gridDim.x) {
     Pack<T, VE> px[NV], pd[NV];
     float s[2] = {0.f, 0.f};
-    F.wait();
+    F.wait_for(1);
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
       const int c = threadIdx.x + n * blockDim.x;
       if (c >= packs) continue;
-      float x[VE], d[VE], w[VE];
+      float x[VE], d[VE];
       px[n] = F.get(0, t, stage, n);
       pd[n] = F.get(1, t, stage, n);
       px[n].widen(x);
       pd[n].widen(d);
-      load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
         s[0] = fmaf(x[j], x[j], s[0]);
-        s[1] = fmaf(d[j] * w[j], x[j], s[1]);
+        s[1] = fmaf(d[j] * w[n][j], x[j], s[1]);
       }
     }
-    block_sums<2>(s, buf[flip]);
+    block_sums_many<2, 2>(s, buf[flip]);
     flip ^= 1;
     const float r = inv_rms(s[0], A.h, A.eps);
     const float cc = r * r * r * (s[1] / (float)A.h);
@@ -462,15 +478,14 @@ __global__ void __launch_bounds__(MAXT, 1024 / MAXT) k_norm_grad_rows(NormArgs A
     for (int n = 0; n < NV; ++n) {
       const int c = threadIdx.x + n * blockDim.x;
       if (c >= packs) continue;
-      float x[VE], d[VE], w[VE], o[VE];
+      float x[VE], d[VE], o[VE];
       px[n].widen(x);
       pd[n].widen(d);
-      load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
         const float rd = r * d[j];
         acc[n][j] = fmaf(rd, x[j], acc[n][j]);
-        o[j] = fmaf(rd, w[j], -x[j] * cc);
+        o[j] = fmaf(rd, w[n][j], -x[j] * cc);
       }
       if (add) {
         float e[VE];
@@ -481,7 +496,7 @@ __global__ void __launch_bounds__(MAXT, 1024 / MAXT) k_norm_grad_rows(NormArgs A
       store_row<T, VE>(A.dx, A.dx_s, t, c, o);
     }
     F.request(t + (int64_t)stages * gridDim.x, stage);
-    stage = stage + 1 == stages ? 0 : stage + 1;
+    stage = F.next(stage);
   }
   float* part = A.part + (size_t)blockIdx.x * A.h;
 #pragma unroll
@@ -493,16 +508,19 @@ __global__ void __launch_bounds__(MAXT, 1024 / MAXT) k_norm_grad_rows(NormArgs A
   }
 }
 
-// With p = b g w (a column's constant unless the gate is full) and gt the token's gate (or 1):
-//   s = a x + gt ry p y,   D = dout + ro du wn - co s,   dx = a D,   sum3 = sum p D y,
-//   dy = gt ry p D - y gt ry^3 sum3 / h,   dgate_token = ry sum3,   E = gt ry D y,
+// With p = b g w (a column's constant unless the gate is full), gt the token's gate (or 1) and gr = gt ry:
+//   s = a x + gr p y,   D = dout + ro du wn - co s,   dx = a D,   sum3 = sum p D y,
+//   dy = gr p D - y gr ry^2 sum3 / h,   dgate_token = ry sum3,   E = gr D y,
 //   dw = b g sum_t E,   dgate_channel = b w sum_t E   -- one accumulator a column for both.
+// sum3 = sum p y dout + ro sum p y du wn - co sum p y s, so all of a row's sums are taken before ro and co are known,
+// and the sum of the next row's y^2 with them: one reduction and one barrier a row (three before: 5 us a row of 7168
+// values, most of it their latency).
 template <typename T, int VE, int NV, int MAXT, bool FULL>
 __global__ void __launch_bounds__(MAXT, 1) k_residual_grad_rows(NormArgs A, int packs, int stages, size_t part_step) {
   extern __shared__ uint4 ring[];
-  __shared__ float buf[2][64];
+  __shared__ float buf[2][256];
   const Rows in[5] = {A.x, A.y, A.dout, A.du, {FULL ? A.gate.p : nullptr, A.gate.stride}};
-  const RowFeed<T, VE, NV, 5> F{in, A.T, packs, stages, FULL ? 5 : 4, ring};
+  const RowFeed<T, VE, NV, 5> F(in, A.T, packs, stages, FULL ? 5 : 4, ring);
   float acc_e[NV][VE] = {}, acc_n[NV][VE] = {}, p[NV][VE], q[NV][VE];
   auto channel_gate = [&](int c, float (&g)[VE]) {
 #pragma unroll
@@ -520,101 +538,92 @@ __global__ void __launch_bounds__(MAXT, 1) k_residual_grad_rows(NormArgs A, int 
 #pragma unroll
     for (int j = 0; j < VE; ++j) p[n][j] *= A.b * g[j];
   }
-  for (int i = 0; i < stages; ++i) F.request(blockIdx.x + (int64_t)i * gridDim.x, i);
-  int stage = 0, flip = 0;
-  for (int64_t t = blockIdx.x; t < A.T; t += gridDim.x) {
-    Pack<T, VE> py[NV], pu[NV];
-    float d[NV][VE];
-    const float gt = A.gate_kind == DEAMOE_GATE_TOKEN ? to_f<T>(reinterpret_cast<const T*>(A.gate.p)[t]) : 1.f;
-    F.wait();
-#pragma unroll
-    for (int n = 0; n < NV; ++n)
-      if ((int)(threadIdx.x + n * blockDim.x) < packs) py[n] = F.get(1, t, stage, n);
-    float ry = 1.f;
-    if (A.post_norm) {
-      float ss[1] = {0.f};
+  auto squares = [&](int64_t t, uint32_t stage) {  // of y
+    float ss = 0.f;
+    if (A.post_norm && t < A.T)
 #pragma unroll
       for (int n = 0; n < NV; ++n)
         if ((int)(threadIdx.x + n * blockDim.x) < packs) {
           float y[VE];
-          py[n].widen(y);
+          if (stages > 1) F.get(1, t, stage, n).widen(y);
+          else load_pack<T, VE>(row_at<T>(A.y, t) + (int64_t)(threadIdx.x + n * blockDim.x) * VE).widen(y);  // no room for two rows
 #pragma unroll
-          for (int j = 0; j < VE; ++j) ss[0] = fmaf(y[j], y[j], ss[0]);
+          for (int j = 0; j < VE; ++j) ss = fmaf(y[j], y[j], ss);
         }
-      block_sums<1>(ss, buf[flip]);
-      flip ^= 1;
-      ry = inv_rms(ss[0], A.h, A.eps);
-    }
+    return ss;
+  };
+  const float inv_h = 1.f / (float)A.h;
+  for (int i = 0; i < stages; ++i) F.request(blockIdx.x + (int64_t)i * gridDim.x, i * F.row_bytes);
+  uint32_t stage = 0;
+  int flip = 0;
+  float s[6];
+  F.wait_for(1);
+  s[0] = squares(blockIdx.x, 0);
+  block_sums_many<1, 2>(reinterpret_cast<float(&)[1]>(s), buf[flip]);
+  flip ^= 1;
+  for (int64_t t = blockIdx.x; t < A.T; t += gridDim.x) {
+    const float gt = A.gate_kind == DEAMOE_GATE_TOKEN ? to_f<T>(reinterpret_cast<const T*>(A.gate.p)[t]) : 1.f;
+    const float ry = A.post_norm ? inv_rms(s[0], A.h, A.eps) : 1.f;
     const float gr = gt * ry;
-    float ro = 1.f, co = 0.f;
-    if (A.next_norm) {  // the sum after the block once more
-      float s[2] = {0.f, 0.f};
-#pragma unroll
-      for (int n = 0; n < NV; ++n) {
-        if ((int)(threadIdx.x + n * blockDim.x) >= packs) continue;
-        float x[VE], y[VE], u[VE], g[VE];
-        F.get(0, t, stage, n).widen(x);
-        py[n].widen(y);
-        pu[n] = F.get(3, t, stage, n);
-        pu[n].widen(u);
-        if constexpr (FULL) F.get(4, t, stage, n).widen(g);
-#pragma unroll
-        for (int j = 0; j < VE; ++j) {
-          const float pj = FULL ? p[n][j] * g[j] : p[n][j];
-          d[n][j] = fmaf(gr * pj, y[j], A.a * x[j]);
-          s[0] = fmaf(d[n][j], d[n][j], s[0]);
-          s[1] = fmaf(u[j] * q[n][j], d[n][j], s[1]);
-        }
-      }
-      block_sums<2>(s, buf[flip]);
-      flip ^= 1;
-      ro = inv_rms(s[0], A.h, A.next_eps);
-      co = ro * ro * ro * (s[1] / (float)A.h);
-    }
-    float s3[1] = {0.f};
+    const uint32_t later = F.next(stage);
+    F.wait_for(2);  // this row and the next
+    s[0] = squares(t + gridDim.x, later);
+    s[1] = s[2] = s[3] = s[4] = s[5] = 0.f;
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
-      const int c = threadIdx.x + n * blockDim.x;
-      if (c >= packs) continue;
-      float o[VE], y[VE], g[VE];
+      if ((int)(threadIdx.x + n * blockDim.x) >= packs) continue;
+      float x[VE], y[VE], u[VE], o[VE], g[VE];
+      F.get(0, t, stage, n).widen(x);
+      F.get(1, t, stage, n).widen(y);
       F.get(2, t, stage, n).widen(o);
-      if (A.next_norm) {
-        float u[VE];
-        pu[n].widen(u);
-#pragma unroll
-        for (int j = 0; j < VE; ++j) {
-          const float ru = ro * u[j];
-          acc_n[n][j] = fmaf(ru, d[n][j], acc_n[n][j]);
-          o[j] = fmaf(ru, q[n][j], fmaf(-co, d[n][j], o[j]));
-        }
-      }
-      py[n].widen(y);
+      if (A.next_norm) F.get(3, t, stage, n).widen(u);
       if constexpr (FULL) F.get(4, t, stage, n).widen(g);
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
-        const float pj = FULL ? p[n][j] * g[j] : p[n][j];
-        d[n][j] = o[j];
-        s3[0] = fmaf(pj * o[j], y[j], s3[0]);
-        o[j] *= A.a;
+        const float py = (FULL ? p[n][j] * g[j] : p[n][j]) * y[j];
+        s[3] = fmaf(py, o[j], s[3]);
+        if (A.next_norm) {
+          const float sum = fmaf(gr, py, A.a * x[j]), uq = u[j] * q[n][j];
+          s[1] = fmaf(sum, sum, s[1]);
+          s[2] = fmaf(uq, sum, s[2]);
+          s[4] = fmaf(py, uq, s[4]);
+          s[5] = fmaf(py, sum, s[5]);
+        }
       }
-      store_row<T, VE>(A.dx, A.dx_s, t, c, o);
     }
-    if (A.post_norm || A.dgate_token) {
-      block_sums<1>(s3, buf[flip]);
-      flip ^= 1;
-    }
-    const float cy = A.post_norm ? gt * ry * ry * ry * (s3[0] / (float)A.h) : 0.f;
-    if (A.dgate_token && threadIdx.x == 0) A.dgate_token[t] = ry * s3[0];
+    block_sums_many<6, 8>(s, buf[flip]);
+    flip ^= 1;
+    const float ro = A.next_norm ? inv_rms(s[1], A.h, A.next_eps) : 0.f;
+    const float co = ro * ro * ro * (s[2] * inv_h);
+    const float s3 = s[3] + ro * s[4] - co * s[5];
+    const float cy = A.post_norm ? gr * ry * ry * (s3 * inv_h) : 0.f;
+    if (A.dgate_token && threadIdx.x == 0) A.dgate_token[t] = ry * s3;
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
       const int c = threadIdx.x + n * blockDim.x;
       if (c >= packs) continue;
-      float y[VE], o[VE], g[VE], dg[VE];
-      py[n].widen(y);
+      float o[VE], y[VE], g[VE], dg[VE];
+      F.get(2, t, stage, n).widen(o);
+      F.get(1, t, stage, n).widen(y);
       if constexpr (FULL) F.get(4, t, stage, n).widen(g);
+      if (A.next_norm) {
+        float x[VE], u[VE];
+        F.get(0, t, stage, n).widen(x);
+        F.get(3, t, stage, n).widen(u);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) {
+          const float sum = fmaf(gr, (FULL ? p[n][j] * g[j] : p[n][j]) * y[j], A.a * x[j]), ru = ro * u[j];
+          acc_n[n][j] = fmaf(ru, sum, acc_n[n][j]);
+          o[j] = fmaf(ru, q[n][j], fmaf(-co, sum, o[j]));
+        }
+      }
+      float dx[VE];
+#pragma unroll
+      for (int j = 0; j < VE; ++j) dx[j] = A.a * o[j];
+      store_row<T, VE>(A.dx, A.dx_s, t, c, dx);
 #pragma unroll
       for (int j = 0; j < VE; ++j) {
-        const float gd = gr * d[n][j];
+        const float gd = gr * o[j];
         if constexpr (FULL) {
           dg[j] = p[n][j] * gd * y[j];
           acc_e[n][j] = fmaf(g[j] * gd, y[j], acc_e[n][j]);
@@ -628,7 +637,7 @@ __global__ void __launch_bounds__(MAXT, 1) k_residual_grad_rows(NormArgs A, int 
       store_row<T, VE>(A.dy, A.dy_s, t, c, o);
     }
     F.request(t + (int64_t)stages * gridDim.x, stage);
-    stage = stage + 1 == stages ? 0 : stage + 1;
+    stage = later;
   }
   float* part = A.part + (size_t)blockIdx.x * A.h;
 #pragma unroll
@@ -773,22 +782,22 @@ static deamoe_status_t run_grad(K* kernel, std::atomic<uint64_t>& done, const No
 
 template <typename T> static deamoe_status_t norm_grad_t(const NormArgs& A, cudaStream_t s) {
   constexpr int VE = 16 / sizeof(T), NV = GRAD_COLUMNS / VE;
-  const int ctas = grad_ctas(A.T, A.h), threads = grad_threads(A.h, GRAD_COLUMNS);
+  const int ctas = grad_ctas(A.T, A.h), threads = grad_threads(A.h);
   static std::atomic<uint64_t> done[2];
   if (A.h > GRAD_MAX_WIDTH) {
     k_norm_grad_any<T><<<ctas, ANY_THREADS, 0, s>>>(A);
     return ran();
   }
-  if (!wide_call<T>(A)) return run_grad(k_norm_grad_rows<T, 1, GRAD_COLUMNS, 1024>, done[0], A, ctas, threads, A.h, 0, s);
-  return run_grad(k_norm_grad_rows<T, VE, NV, 1024>, done[1], A, ctas, threads, A.h / VE,
+  if (!wide_call<T>(A)) return run_grad(k_norm_grad_rows<T, 1, GRAD_COLUMNS, 512>, done[0], A, ctas, threads, A.h, 0, s);
+  return run_grad(k_norm_grad_rows<T, VE, NV, 512>, done[1], A, ctas, threads, A.h / VE,
                   (size_t)(A.dadd.p ? 3 : 2) * NV * threads * 16, s);
 }
 
 template <typename T> static deamoe_status_t residual_grad_t(const NormArgs& A, cudaStream_t s) {
   constexpr int VE = 16 / sizeof(T), NV = GRAD_COLUMNS / VE;
-  const int ctas = grad_ctas(A.T, A.h), threads = grad_threads(A.h, GRAD_COLUMNS);
+  const int ctas = grad_ctas(A.T, A.h), threads = grad_threads(A.h);
   const size_t step = (size_t)ctas * A.h;
-  static std::atomic<uint64_t> done[6];
+  static std::atomic<uint64_t> done[4];
   if (A.h > GRAD_MAX_WIDTH) {
     k_residual_grad_any<T><<<ctas, ANY_THREADS, 0, s>>>(A, step);
     return ran();
@@ -797,13 +806,10 @@ template <typename T> static deamoe_status_t residual_grad_t(const NormArgs& A, 
   const size_t stage = wide ? (size_t)(full ? 5 : 4) * NV * threads * 16 : 0;
   const int packs = wide ? A.h / VE : A.h;
   if (!wide)
-    return full ? run_grad(k_residual_grad_rows<T, 1, GRAD_COLUMNS, 1024, true>, done[0], A, ctas, threads, packs, stage, s, step)
-                : run_grad(k_residual_grad_rows<T, 1, GRAD_COLUMNS, 1024, false>, done[1], A, ctas, threads, packs, stage, s, step);
-  if (threads <= 896)  // 72 registers a thread instead of 64
-    return full ? run_grad(k_residual_grad_rows<T, VE, NV, 896, true>, done[2], A, ctas, threads, packs, stage, s, step)
-                : run_grad(k_residual_grad_rows<T, VE, NV, 896, false>, done[3], A, ctas, threads, packs, stage, s, step);
-  return full ? run_grad(k_residual_grad_rows<T, VE, NV, 1024, true>, done[4], A, ctas, threads, packs, stage, s, step)
-              : run_grad(k_residual_grad_rows<T, VE, NV, 1024, false>, done[5], A, ctas, threads, packs, stage, s, step);
+    return full ? run_grad(k_residual_grad_rows<T, 1, GRAD_COLUMNS, 512, true>, done[0], A, ctas, threads, packs, stage, s, step)
+                : run_grad(k_residual_grad_rows<T, 1, GRAD_COLUMNS, 512, false>, done[1], A, ctas, threads, packs, stage, s, step);
+  return full ? run_grad(k_residual_grad_rows<T, VE, NV, 512, true>, done[2], A, ctas, threads, packs, stage, s, step)
+              : run_grad(k_residual_grad_rows<T, VE, NV, 512, false>, done[3], A, ctas, threads, packs, stage, s, step);
 }
 
 }  // namespace deamoe

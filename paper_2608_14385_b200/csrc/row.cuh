@@ -94,6 +94,43 @@ template <int N> static __device__ __forceinline__ void block_sums(float (&v)[N]
     for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
 }
 
+// Sums of N <= P values (P a power of two up to 8) over a block, to every thread, with one barrier: a warp halves the
+// number of values it carries while it halves the lanes (P / 2 + P / 4 + ... shuffles instead of 5 P), and a group of
+// 32 / P lanes adds one value's partials of the warps.  Fixed order.  `buf`: 32 * P floats, as for block_sums.
+template <int N, int P> static __device__ __forceinline__ void block_sums_many(float (&out)[N], float* buf) {
+  static_assert(N <= P && P <= 8 && (P & (P - 1)) == 0, "");
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  float v[P];
+#pragma unroll
+  for (int i = 0; i < P; ++i) v[i] = i < N ? out[i] : 0.f;
+  int o = 16;
+#pragma unroll
+  for (int half = P / 2; half >= 1; half /= 2, o /= 2)
+#pragma unroll
+    for (int i = 0; i < half; ++i) {
+      const bool up = (lane & o) != 0;
+      const float send = up ? v[i] : v[i + half], keep = up ? v[i + half] : v[i];
+      v[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+    }
+  constexpr int G = 32 / P;  // lanes that now hold the same value
+  float s = v[0];
+#pragma unroll
+  for (int d = G / 2; d >= 1; d /= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
+  if (warps > 1) {
+    const int which = lane / G, sub = lane % G;
+    if (sub == 0) buf[w * P + which] = s;
+    __syncthreads();
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32 / G; ++i)
+      if (i * G + sub < warps) s += buf[(i * G + sub) * P + which];
+#pragma unroll
+    for (int d = G / 2; d >= 1; d /= 2) s += __shfl_xor_sync(0xffffffffu, s, d);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) out[i] = __shfl_sync(0xffffffffu, s, i * G);
+}
+
 // Exclusive prefix sums of tot[0..n) in place, tot[n] = the total.  All threads of the block; ends with a barrier.
 static __device__ void block_exclusive_scan(int* tot, int n, int* warp_sums) {
   const int nt = blockDim.x, per = (n + nt - 1) / nt;
