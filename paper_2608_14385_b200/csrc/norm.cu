@@ -26,7 +26,8 @@ namespace deamoe {
 // columns' constants and sums), 512 threads an SM (rows of up to 8192 values; else two blocks an SM).
 constexpr int NORM_SMS = 148;
 constexpr int GRAD_COLUMNS = 16, GRAD_MAX_WIDTH = 8192;
-static int grad_threads(int h) { return ((h + GRAD_COLUMNS - 1) / GRAD_COLUMNS + 31) / 32 * 32; }
+constexpr int GRAD_ODD_COLUMNS = 8;  // of rows that are read value by value
+static int grad_threads(int h, int columns = GRAD_COLUMNS) { return ((h + columns - 1) / columns + 31) / 32 * 32; }
 static int grad_blocks_per_sm(int h) {
   if (h > GRAD_MAX_WIDTH) return 2;
   const int n = 512 / grad_threads(h);
@@ -81,7 +82,7 @@ static __device__ __forceinline__ float inv_rms(float ss, int h, float eps) { re
 // ---------------------------------------------------------------- any width, any alignment: one block a row
 
 constexpr int ANY_THREADS = 256;
-constexpr int RING_BYTES = 220 * 1024;  // of an SM's 227 KB, beside the sums' buffers
+constexpr int RING_BYTES = 225 * 1024;  // of an SM's 227 KB, beside the sums' buffers (two fp32 rows of 4 x 7168 values)
 
 template <typename T> __global__ void __launch_bounds__(ANY_THREADS) k_norm_any(NormArgs A) {
   __shared__ float buf[32];
@@ -373,6 +374,56 @@ template <typename T, int VE, int NV, int MAXT> __global__ void __launch_bounds_
   }
 }
 
+// Two fp32 values in one register pair: the backward kernels are bound by instruction issue, and sm_100a has multiply
+// and multiply-add on such pairs, each value rounded as by itself.
+struct F2 { unsigned long long v; };
+static __device__ __forceinline__ F2 pair(float a, float b) {
+  F2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(a), "f"(b));
+  return r;
+}
+static __device__ __forceinline__ float low(F2 a) { return __uint_as_float((uint32_t)a.v); }
+static __device__ __forceinline__ float high(F2 a) { return __uint_as_float((uint32_t)(a.v >> 32)); }
+static __device__ __forceinline__ F2 fma_(F2 a, F2 b, F2 c) {
+  F2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+  return r;
+}
+static __device__ __forceinline__ F2 mul_(F2 a, F2 b) {
+  F2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+  return r;
+}
+static __device__ __forceinline__ float fma_(float a, float b, float c) { return fmaf(a, b, c); }
+static __device__ __forceinline__ float mul_(float a, float b) { return a * b; }
+static __device__ __forceinline__ float total(F2 a) { return low(a) + high(a); }
+static __device__ __forceinline__ float total(float a) { return a; }
+template <typename P> static __device__ __forceinline__ P splat(float a);
+template <> __device__ __forceinline__ float splat<float>(float a) { return a; }
+template <> __device__ __forceinline__ F2 splat<F2>(float a) { return pair(a, a); }
+// VE values as VE / 2 pairs (or the one value)
+template <int VE> struct Lanes {
+  using P = F2;
+  static constexpr int N = VE / 2;
+  static __device__ __forceinline__ void from(const float (&f)[VE], P (&p)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) p[i] = pair(f[2 * i], f[2 * i + 1]);
+  }
+  static __device__ __forceinline__ void to(const P (&p)[N], float (&f)[VE]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      f[2 * i] = low(p[i]);
+      f[2 * i + 1] = high(p[i]);
+    }
+  }
+};
+template <> struct Lanes<1> {
+  using P = float;
+  static constexpr int N = 1;
+  static __device__ __forceinline__ void from(const float (&f)[1], P (&p)[1]) { p[0] = f[0]; }
+  static __device__ __forceinline__ void to(const P (&p)[1], float (&f)[1]) { f[0] = p[0]; }
+};
+
 // Backward kernels: persistent blocks, a block walks its rows with the column sums of its threads' columns in
 // registers.  A thread copies its own packs of the rows to come into shared memory (asynchronously, `stages` rows ahead)
 // and is the only one to read them back, so the loads of later rows run under a row's reductions without any barrier.
@@ -433,7 +484,18 @@ template <typename T, int VE, int NV, int NIN> struct RowFeed {
       return load_once<T, VE>(row_at<T>(in[i], t) + (int64_t)(threadIdx.x + n * blockDim.x) * VE);
     }
   }
+  __device__ __forceinline__ void get(int i, int64_t t, uint32_t at, int n, typename Lanes<VE>::P (&p)[Lanes<VE>::N]) const {
+    float f[VE];
+    get(i, t, at, n).widen(f);
+    Lanes<VE>::from(f, p);
+  }
 };
+template <typename T, int VE>
+static __device__ __forceinline__ void store_lanes(void* p, int64_t stride, int64_t t, int c, const typename Lanes<VE>::P (&v)[Lanes<VE>::N]) {
+  float f[VE];
+  Lanes<VE>::to(v, f);
+  store_row<T, VE>(p, stride, t, c, f);
+}
 
 template <typename T, int VE, int NV, int MAXT>
 __global__ void __launch_bounds__(MAXT, 1) k_norm_grad_rows(NormArgs A, int packs, int stages) {
@@ -442,58 +504,72 @@ __global__ void __launch_bounds__(MAXT, 1) k_norm_grad_rows(NormArgs A, int pack
   const Rows in[3] = {A.x, A.du, A.dadd};
   const RowFeed<T, VE, NV, 3> F(in, A.T, packs, stages, A.dadd.p ? 3 : 2, ring);
   const bool add = A.dadd.p != nullptr;
-  float acc[NV][VE] = {}, w[NV][VE];
+  using L = Lanes<VE>;
+  using P = typename L::P;
+  constexpr int N = L::N;
+  P acc[NV][N], w[NV][N];
 #pragma unroll
   for (int n = 0; n < NV; ++n) {
     const int c = threadIdx.x + n * blockDim.x;
-    if (c < packs) load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w[n]);
+    float f[VE] = {};
+    if (c < packs) load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, f);
+    L::from(f, w[n]);
+#pragma unroll
+    for (int j = 0; j < N; ++j) acc[n][j] = splat<P>(0.f);
   }
+  const float inv_h = 1.f / (float)A.h;
   for (int i = 0; i < stages; ++i) F.request(blockIdx.x + (int64_t)i * gridDim.x, i * F.row_bytes);
   uint32_t stage = 0;
   int flip = 0;
   for (int64_t t = blockIdx.x; t < A.T; t += gridDim.x) {
     Pack<T, VE> px[NV], pd[NV];
-    float s[2] = {0.f, 0.f};
+    P s0 = splat<P>(0.f), s1 = s0;
     F.wait_for(1);
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
-      const int c = threadIdx.x + n * blockDim.x;
-      if (c >= packs) continue;
-      float x[VE], d[VE];
+      if ((int)(threadIdx.x + n * blockDim.x) >= packs) continue;
+      float f[VE];
+      P x[N], d[N];
       px[n] = F.get(0, t, stage, n);
       pd[n] = F.get(1, t, stage, n);
-      px[n].widen(x);
-      pd[n].widen(d);
+      px[n].widen(f);
+      L::from(f, x);
+      pd[n].widen(f);
+      L::from(f, d);
 #pragma unroll
-      for (int j = 0; j < VE; ++j) {
-        s[0] = fmaf(x[j], x[j], s[0]);
-        s[1] = fmaf(d[j] * w[n][j], x[j], s[1]);
+      for (int j = 0; j < N; ++j) {
+        s0 = fma_(x[j], x[j], s0);
+        s1 = fma_(mul_(d[j], w[n][j]), x[j], s1);
       }
     }
+    float s[2] = {total(s0), total(s1)};
     block_sums_many<2, 2>(s, buf[flip]);
     flip ^= 1;
     const float r = inv_rms(s[0], A.h, A.eps);
-    const float cc = r * r * r * (s[1] / (float)A.h);
+    const P r2 = splat<P>(r), c2 = splat<P>(-(r * r * r * (s[1] * inv_h)));
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
       const int c = threadIdx.x + n * blockDim.x;
       if (c >= packs) continue;
-      float x[VE], d[VE], o[VE];
-      px[n].widen(x);
-      pd[n].widen(d);
+      float f[VE];
+      P x[N], d[N];
+      px[n].widen(f);
+      L::from(f, x);
+      pd[n].widen(f);
+      L::from(f, d);
 #pragma unroll
-      for (int j = 0; j < VE; ++j) {
-        const float rd = r * d[j];
-        acc[n][j] = fmaf(rd, x[j], acc[n][j]);
-        o[j] = fmaf(rd, w[n][j], -x[j] * cc);
+      for (int j = 0; j < N; ++j) {
+        d[j] = mul_(r2, d[j]);
+        acc[n][j] = fma_(d[j], x[j], acc[n][j]);
+        d[j] = fma_(d[j], w[n][j], mul_(x[j], c2));
       }
       if (add) {
-        float e[VE];
-        F.get(2, t, stage, n).widen(e);
+        P e[N];
+        F.get(2, t, stage, n, e);
 #pragma unroll
-        for (int j = 0; j < VE; ++j) o[j] += e[j];
+        for (int j = 0; j < N; ++j) d[j] = fma_(splat<P>(1.f), e[j], d[j]);
       }
-      store_row<T, VE>(A.dx, A.dx_s, t, c, o);
+      store_lanes<T, VE>(A.dx, A.dx_s, t, c, d);
     }
     F.request(t + (int64_t)stages * gridDim.x, stage);
     stage = F.next(stage);
@@ -502,9 +578,11 @@ __global__ void __launch_bounds__(MAXT, 1) k_norm_grad_rows(NormArgs A, int pack
 #pragma unroll
   for (int n = 0; n < NV; ++n) {
     const int c = threadIdx.x + n * blockDim.x;
-    if (c < packs)
+    if (c >= packs) continue;
+    float f[VE];
+    L::to(acc[n], f);
 #pragma unroll
-      for (int j = 0; j < VE; ++j) part[(size_t)c * VE + j] = acc[n][j];
+    for (int j = 0; j < VE; ++j) part[(size_t)c * VE + j] = f[j];
   }
 }
 
@@ -521,7 +599,10 @@ __global__ void __launch_bounds__(MAXT, 1) k_residual_grad_rows(NormArgs A, int 
   __shared__ float buf[2][256];
   const Rows in[5] = {A.x, A.y, A.dout, A.du, {FULL ? A.gate.p : nullptr, A.gate.stride}};
   const RowFeed<T, VE, NV, 5> F(in, A.T, packs, stages, FULL ? 5 : 4, ring);
-  float acc_e[NV][VE] = {}, acc_n[NV][VE] = {}, p[NV][VE], q[NV][VE];
+  using L = Lanes<VE>;
+  using P = typename L::P;
+  constexpr int N = L::N;
+  P acc_e[NV][N], acc_n[NV][N], p[NV][N], q[NV][N];
   auto channel_gate = [&](int c, float (&g)[VE]) {
 #pragma unroll
     for (int j = 0; j < VE; ++j) g[j] = 1.f;
@@ -530,29 +611,41 @@ __global__ void __launch_bounds__(MAXT, 1) k_residual_grad_rows(NormArgs A, int 
 #pragma unroll
   for (int n = 0; n < NV; ++n) {
     const int c = threadIdx.x + n * blockDim.x;
-    if (c >= packs) continue;
-    float g[VE];
-    channel_gate(c, g);
-    load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, p[n]);
-    load_gains<VE>(A.wn, A.wdt, (int64_t)c * VE, q[n]);
+    float w[VE] = {}, wn[VE] = {}, g[VE];
+    if (c < packs) {
+      channel_gate(c, g);
+      load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
+      load_gains<VE>(A.wn, A.wdt, (int64_t)c * VE, wn);
 #pragma unroll
-    for (int j = 0; j < VE; ++j) p[n][j] *= A.b * g[j];
+      for (int j = 0; j < VE; ++j) w[j] *= A.b * g[j];
+    }
+    L::from(w, p[n]);
+    L::from(wn, q[n]);
+#pragma unroll
+    for (int j = 0; j < N; ++j) acc_e[n][j] = acc_n[n][j] = splat<P>(0.f);
   }
   auto squares = [&](int64_t t, uint32_t stage) {  // of y
-    float ss = 0.f;
+    P ss = splat<P>(0.f);
     if (A.post_norm && t < A.T)
 #pragma unroll
-      for (int n = 0; n < NV; ++n)
-        if ((int)(threadIdx.x + n * blockDim.x) < packs) {
-          float y[VE];
-          if (stages > 1) F.get(1, t, stage, n).widen(y);
-          else load_pack<T, VE>(row_at<T>(A.y, t) + (int64_t)(threadIdx.x + n * blockDim.x) * VE).widen(y);  // no room for two rows
-#pragma unroll
-          for (int j = 0; j < VE; ++j) ss = fmaf(y[j], y[j], ss);
+      for (int n = 0; n < NV; ++n) {
+        const int c = threadIdx.x + n * blockDim.x;
+        if (c >= packs) continue;
+        P y[N];
+        if (stages > 1) {
+          F.get(1, t, stage, n, y);
+        } else {  // no room for two rows
+          float f[VE];
+          load_pack<T, VE>(row_at<T>(A.y, t) + (int64_t)c * VE).widen(f);
+          L::from(f, y);
         }
-    return ss;
+#pragma unroll
+        for (int j = 0; j < N; ++j) ss = fma_(y[j], y[j], ss);
+      }
+    return total(ss);
   };
   const float inv_h = 1.f / (float)A.h;
+  const P a2 = splat<P>(A.a);
   for (int i = 0; i < stages; ++i) F.request(blockIdx.x + (int64_t)i * gridDim.x, i * F.row_bytes);
   uint32_t stage = 0;
   int flip = 0;
@@ -565,76 +658,82 @@ __global__ void __launch_bounds__(MAXT, 1) k_residual_grad_rows(NormArgs A, int 
     const float gt = A.gate_kind == DEAMOE_GATE_TOKEN ? to_f<T>(reinterpret_cast<const T*>(A.gate.p)[t]) : 1.f;
     const float ry = A.post_norm ? inv_rms(s[0], A.h, A.eps) : 1.f;
     const float gr = gt * ry;
+    const P gr2 = splat<P>(gr);
     const uint32_t later = F.next(stage);
     F.wait_for(2);  // this row and the next
-    s[0] = squares(t + gridDim.x, later);
-    s[1] = s[2] = s[3] = s[4] = s[5] = 0.f;
+    P s1 = splat<P>(0.f), s2 = s1, s3 = s1, s4 = s1, s5 = s1;
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
       if ((int)(threadIdx.x + n * blockDim.x) >= packs) continue;
-      float x[VE], y[VE], u[VE], o[VE], g[VE];
-      F.get(0, t, stage, n).widen(x);
-      F.get(1, t, stage, n).widen(y);
-      F.get(2, t, stage, n).widen(o);
-      if (A.next_norm) F.get(3, t, stage, n).widen(u);
-      if constexpr (FULL) F.get(4, t, stage, n).widen(g);
+      P x[N], y[N], u[N], o[N], g[N];
+      F.get(1, t, stage, n, y);
+      F.get(2, t, stage, n, o);
+      if constexpr (FULL) F.get(4, t, stage, n, g);
 #pragma unroll
-      for (int j = 0; j < VE; ++j) {
-        const float py = (FULL ? p[n][j] * g[j] : p[n][j]) * y[j];
-        s[3] = fmaf(py, o[j], s[3]);
-        if (A.next_norm) {
-          const float sum = fmaf(gr, py, A.a * x[j]), uq = u[j] * q[n][j];
-          s[1] = fmaf(sum, sum, s[1]);
-          s[2] = fmaf(uq, sum, s[2]);
-          s[4] = fmaf(py, uq, s[4]);
-          s[5] = fmaf(py, sum, s[5]);
+      for (int j = 0; j < N; ++j) {
+        y[j] = mul_(FULL ? mul_(p[n][j], g[j]) : p[n][j], y[j]);  // p y
+        s3 = fma_(y[j], o[j], s3);
+      }
+      if (A.next_norm) {
+        F.get(0, t, stage, n, x);
+        F.get(3, t, stage, n, u);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          const P sum = fma_(gr2, y[j], mul_(a2, x[j])), uq = mul_(u[j], q[n][j]);
+          s1 = fma_(sum, sum, s1);
+          s2 = fma_(uq, sum, s2);
+          s4 = fma_(y[j], uq, s4);
+          s5 = fma_(y[j], sum, s5);
         }
       }
     }
+    s[0] = squares(t + gridDim.x, later);
+    s[1] = total(s1); s[2] = total(s2); s[3] = total(s3); s[4] = total(s4); s[5] = total(s5);
     block_sums_many<6, 8>(s, buf[flip]);
     flip ^= 1;
     const float ro = A.next_norm ? inv_rms(s[1], A.h, A.next_eps) : 0.f;
     const float co = ro * ro * ro * (s[2] * inv_h);
-    const float s3 = s[3] + ro * s[4] - co * s[5];
-    const float cy = A.post_norm ? gr * ry * ry * (s3 * inv_h) : 0.f;
-    if (A.dgate_token && threadIdx.x == 0) A.dgate_token[t] = ry * s3;
+    const float sum3 = s[3] + ro * s[4] - co * s[5];
+    const float cy = A.post_norm ? gr * ry * ry * (sum3 * inv_h) : 0.f;
+    if (A.dgate_token && threadIdx.x == 0) A.dgate_token[t] = ry * sum3;
+    const P ro2 = splat<P>(ro), co2 = splat<P>(-co), cy2 = splat<P>(-cy);
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
       const int c = threadIdx.x + n * blockDim.x;
       if (c >= packs) continue;
-      float o[VE], y[VE], g[VE], dg[VE];
-      F.get(2, t, stage, n).widen(o);
-      F.get(1, t, stage, n).widen(y);
-      if constexpr (FULL) F.get(4, t, stage, n).widen(g);
+      P o[N], y[N], g[N], dx[N];
+      F.get(2, t, stage, n, o);
+      F.get(1, t, stage, n, y);
+      if constexpr (FULL) F.get(4, t, stage, n, g);
       if (A.next_norm) {
-        float x[VE], u[VE];
-        F.get(0, t, stage, n).widen(x);
-        F.get(3, t, stage, n).widen(u);
+        P x[N], u[N];
+        F.get(0, t, stage, n, x);
+        F.get(3, t, stage, n, u);
 #pragma unroll
-        for (int j = 0; j < VE; ++j) {
-          const float sum = fmaf(gr, (FULL ? p[n][j] * g[j] : p[n][j]) * y[j], A.a * x[j]), ru = ro * u[j];
-          acc_n[n][j] = fmaf(ru, sum, acc_n[n][j]);
-          o[j] = fmaf(ru, q[n][j], fmaf(-co, sum, o[j]));
+        for (int j = 0; j < N; ++j) {
+          const P sum = fma_(gr2, mul_(FULL ? mul_(p[n][j], g[j]) : p[n][j], y[j]), mul_(a2, x[j])), ru = mul_(ro2, u[j]);
+          acc_n[n][j] = fma_(ru, sum, acc_n[n][j]);
+          o[j] = fma_(ru, q[n][j], fma_(co2, sum, o[j]));
         }
       }
-      float dx[VE];
 #pragma unroll
-      for (int j = 0; j < VE; ++j) dx[j] = A.a * o[j];
-      store_row<T, VE>(A.dx, A.dx_s, t, c, dx);
+      for (int j = 0; j < N; ++j) dx[j] = mul_(a2, o[j]);
+      store_lanes<T, VE>(A.dx, A.dx_s, t, c, dx);
 #pragma unroll
-      for (int j = 0; j < VE; ++j) {
-        const float gd = gr * o[j];
+      for (int j = 0; j < N; ++j) {
+        const P gd = mul_(gr2, o[j]), yc = mul_(y[j], cy2);
         if constexpr (FULL) {
-          dg[j] = p[n][j] * gd * y[j];
-          acc_e[n][j] = fmaf(g[j] * gd, y[j], acc_e[n][j]);
-          o[j] = fmaf(p[n][j] * g[j], gd, -y[j] * cy);
+          dx[j] = mul_(mul_(p[n][j], gd), y[j]);  // dgate
+          const P gg = mul_(g[j], gd);
+          acc_e[n][j] = fma_(gg, y[j], acc_e[n][j]);
+          o[j] = fma_(p[n][j], gg, yc);
         } else {
-          acc_e[n][j] = fmaf(gd, y[j], acc_e[n][j]);
-          o[j] = fmaf(p[n][j], gd, -y[j] * cy);
+          acc_e[n][j] = fma_(gd, y[j], acc_e[n][j]);
+          o[j] = fma_(p[n][j], gd, yc);
         }
       }
-      if constexpr (FULL) store_row<T, VE>(A.dgate, A.dgate_s, t, c, dg);
-      store_row<T, VE>(A.dy, A.dy_s, t, c, o);
+      if constexpr (FULL) store_lanes<T, VE>(A.dgate, A.dgate_s, t, c, dx);
+      store_lanes<T, VE>(A.dy, A.dy_s, t, c, o);
     }
     F.request(t + (int64_t)stages * gridDim.x, stage);
     stage = later;
@@ -644,15 +743,17 @@ __global__ void __launch_bounds__(MAXT, 1) k_residual_grad_rows(NormArgs A, int 
   for (int n = 0; n < NV; ++n) {
     const int c = threadIdx.x + n * blockDim.x;
     if (c >= packs) continue;
-    float w[VE], g[VE];
+    float w[VE], g[VE], ae[VE], an[VE];
     channel_gate(c, g);
     load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
+    L::to(acc_e[n], ae);
+    L::to(acc_n[n], an);
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
       const size_t i = (size_t)c * VE + j;
-      if (A.w) part[i] = A.b * g[j] * acc_e[n][j];
-      if (A.wn) part[part_step + i] = acc_n[n][j];
-      if (A.gate_kind == DEAMOE_GATE_CHANNEL) part[2 * part_step + i] = A.b * w[j] * acc_e[n][j];
+      if (A.w) part[i] = A.b * g[j] * ae[j];
+      if (A.wn) part[part_step + i] = an[j];
+      if (A.gate_kind == DEAMOE_GATE_CHANNEL) part[2 * part_step + i] = A.b * w[j] * ae[j];
     }
   }
 }
@@ -788,14 +889,14 @@ template <typename T> static deamoe_status_t norm_grad_t(const NormArgs& A, cuda
     k_norm_grad_any<T><<<ctas, ANY_THREADS, 0, s>>>(A);
     return ran();
   }
-  if (!wide_call<T>(A)) return run_grad(k_norm_grad_rows<T, 1, GRAD_COLUMNS, 512>, done[0], A, ctas, threads, A.h, 0, s);
+  if (!wide_call<T>(A)) return run_grad(k_norm_grad_rows<T, 1, GRAD_ODD_COLUMNS, 1024>, done[0], A, ctas, grad_threads(A.h, GRAD_ODD_COLUMNS), A.h, 0, s);
   return run_grad(k_norm_grad_rows<T, VE, NV, 512>, done[1], A, ctas, threads, A.h / VE,
                   (size_t)(A.dadd.p ? 3 : 2) * NV * threads * 16, s);
 }
 
 template <typename T> static deamoe_status_t residual_grad_t(const NormArgs& A, cudaStream_t s) {
   constexpr int VE = 16 / sizeof(T), NV = GRAD_COLUMNS / VE;
-  const int ctas = grad_ctas(A.T, A.h), threads = grad_threads(A.h);
+  const int ctas = grad_ctas(A.T, A.h), threads = grad_threads(A.h), odd = grad_threads(A.h, GRAD_ODD_COLUMNS);
   const size_t step = (size_t)ctas * A.h;
   static std::atomic<uint64_t> done[4];
   if (A.h > GRAD_MAX_WIDTH) {
@@ -806,8 +907,8 @@ template <typename T> static deamoe_status_t residual_grad_t(const NormArgs& A, 
   const size_t stage = wide ? (size_t)(full ? 5 : 4) * NV * threads * 16 : 0;
   const int packs = wide ? A.h / VE : A.h;
   if (!wide)
-    return full ? run_grad(k_residual_grad_rows<T, 1, GRAD_COLUMNS, 512, true>, done[0], A, ctas, threads, packs, stage, s, step)
-                : run_grad(k_residual_grad_rows<T, 1, GRAD_COLUMNS, 512, false>, done[1], A, ctas, threads, packs, stage, s, step);
+    return full ? run_grad(k_residual_grad_rows<T, 1, GRAD_ODD_COLUMNS, 1024, true>, done[0], A, ctas, odd, packs, stage, s, step)
+                : run_grad(k_residual_grad_rows<T, 1, GRAD_ODD_COLUMNS, 1024, false>, done[1], A, ctas, odd, packs, stage, s, step);
   return full ? run_grad(k_residual_grad_rows<T, VE, NV, 512, true>, done[2], A, ctas, threads, packs, stage, s, step)
               : run_grad(k_residual_grad_rows<T, VE, NV, 512, false>, done[3], A, ctas, threads, packs, stage, s, step);
 }
