@@ -201,11 +201,11 @@ if hasattr(torch._C, "_cuda_getCurrentRawStream"):
     _raw_stream = torch._C._cuda_getCurrentRawStream
 
 
-def _mat(t, where, name, dtype, rows, cols):
-    """Address and row stride of a [rows, cols] matrix of the current device."""
+def _mat(t, where, name, dtype, rows, cols, dev):
+    """Address and row stride of a [rows, cols] matrix of device `dev`, the current one."""
     if t.dtype is not dtype or t.shape != (rows, cols):
         _refuse(where, f"{name} must be {dtype} [{rows}, {cols}], got {t.dtype} {list(t.shape)}")
-    if t.get_device() != _device():
+    if t.get_device() != dev:
         _refuse(where, f"{name} is not on the current CUDA device")
     stride, step = t.stride()
     if step != 1 and cols > 1:
@@ -213,11 +213,11 @@ def _mat(t, where, name, dtype, rows, cols):
     return t.data_ptr(), stride if rows > 1 else cols
 
 
-def _vec(t, where, name, dtype, *shape):
-    """Address of a contiguous array of the current device."""
+def _vec(t, where, name, dtype, shape, dev):
+    """Address of a contiguous array of device `dev`, the current one."""
     if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
         _refuse(where, f"{name} must be contiguous {dtype} {list(shape)}, got {t.dtype} {list(t.shape)}")
-    if t.get_device() != _device():
+    if t.get_device() != dev:
         _refuse(where, f"{name} is not on the current CUDA device")
     return t.data_ptr()
 
@@ -244,20 +244,19 @@ def sort_pairs(topk_idx, n_expert):
     """(token, slot) pairs in expert order (deamoe_sort_pairs).  topk_idx: int32 [T, k], as Layer.route gives it; entries
     outside [0, n_expert) drop their pair.  Returns expert_off [n_expert + 1], pair_row [T, k] (-1 = dropped) and
     row_pair [T * k] (-1 behind the last row), all int32."""
-    where = "deamoe_sort_pairs"
+    where, dev = "deamoe_sort_pairs", _device()
     if topk_idx.dim() != 2:
         _refuse(where, "topk_idx must be [T, k]")
     T, k = topk_idx.shape
-    src = _vec(topk_idx, where, "topk_idx", torch.int32, T, k)
-    dev = topk_idx.device
+    src = _vec(topk_idx, where, "topk_idx", torch.int32, (T, k), dev)
     n = int(n_expert)
     off = topk_idx.new_empty(max(n, 0) + 1)
     pair_row = topk_idx.new_empty((T, k))
     row_pair = topk_idx.new_empty(T * k)
     L = lib()
     need = L.deamoe_sort_workspace(T, k, n)
-    ws = _workspace(need, dev)
-    _done(L.deamoe_sort_pairs(_raw_stream(_device()), src, T, k, n, off.data_ptr(), pair_row.data_ptr(), row_pair.data_ptr(),
+    ws = _workspace(need, topk_idx.device)
+    _done(L.deamoe_sort_pairs(_raw_stream(dev), src, T, k, n, off.data_ptr(), pair_row.data_ptr(), row_pair.data_ptr(),
                               _dptr(ws), need), where)
     return off, pair_row, row_pair
 
@@ -265,47 +264,47 @@ def sort_pairs(topk_idx, n_expert):
 def dispatch(x, pair_row, rows=None):
     """rows[pair_row[t, q]] = x[t] (deamoe_dispatch).  rows: [n_rows, h] to fill; made with T * k rows if omitted (rows
     that no pair points to are then uninitialised)."""
-    where = "deamoe_dispatch"
+    where, dev = "deamoe_dispatch", _device()
     dt = _type(x, where, "x")
     T, h = x.shape
     k = pair_row.shape[-1]
     if rows is None:
         rows = x.new_empty((T * k, h))
     n = rows.shape[0]
-    px, sx = _mat(x, where, "x", x.dtype, T, h)
-    pr, sr = _mat(rows, where, "rows", x.dtype, n, h)
-    _done(lib().deamoe_dispatch(_raw_stream(_device()), dt, px, sx, _vec(pair_row, where, "pair_row", torch.int32, T, k), T, k, h, pr, sr,
+    px, sx = _mat(x, where, "x", x.dtype, T, h, dev)
+    pr, sr = _mat(rows, where, "rows", x.dtype, n, h, dev)
+    _done(lib().deamoe_dispatch(_raw_stream(dev), dt, px, sx, _vec(pair_row, where, "pair_row", torch.int32, (T, k), dev), T, k, h, pr, sr,
                                 n), where)
     return rows
 
 
 def dispatch_backward(drows, pair_row, dx=None):
     """dx[t] = sum_q drows[pair_row[t, q]] (deamoe_dispatch_backward)."""
-    where = "deamoe_dispatch_backward"
+    where, dev = "deamoe_dispatch_backward", _device()
     dt = _type(drows, where, "drows")
     n, h = drows.shape
     T, k = pair_row.shape
     if dx is None:
         dx = drows.new_empty((T, h))
-    pd, sd = _mat(drows, where, "drows", drows.dtype, n, h)
-    px, sx = _mat(dx, where, "dx", drows.dtype, T, h)
-    _done(lib().deamoe_dispatch_backward(_raw_stream(_device()), dt, pd, sd, n, _vec(pair_row, where, "pair_row", torch.int32, T, k), T, k,
+    pd, sd = _mat(drows, where, "drows", drows.dtype, n, h, dev)
+    px, sx = _mat(dx, where, "dx", drows.dtype, T, h, dev)
+    _done(lib().deamoe_dispatch_backward(_raw_stream(dev), dt, pd, sd, n, _vec(pair_row, where, "pair_row", torch.int32, (T, k), dev), T, k,
                                          h, px, sx), where)
     return dx
 
 
 def combine(rows, pair_row, topk_w, out=None):
     """out[t] = sum_q topk_w[t, q] rows[pair_row[t, q]] (deamoe_combine)."""
-    where = "deamoe_combine"
+    where, dev = "deamoe_combine", _device()
     dt = _type(rows, where, "rows")
     n, h = rows.shape
     T, k = pair_row.shape
     if out is None:
         out = rows.new_empty((T, h))
-    pr, sr = _mat(rows, where, "rows", rows.dtype, n, h)
-    po, so = _mat(out, where, "out", rows.dtype, T, h)
-    _done(lib().deamoe_combine(_raw_stream(_device()), dt, pr, sr, n, _vec(pair_row, where, "pair_row", torch.int32, T, k),
-                               _vec(topk_w, where, "topk_w", torch.float32, T, k), T, k, h, po, so), where)
+    pr, sr = _mat(rows, where, "rows", rows.dtype, n, h, dev)
+    po, so = _mat(out, where, "out", rows.dtype, T, h, dev)
+    _done(lib().deamoe_combine(_raw_stream(dev), dt, pr, sr, n, _vec(pair_row, where, "pair_row", torch.int32, (T, k), dev),
+                               _vec(topk_w, where, "topk_w", torch.float32, (T, k), dev), T, k, h, po, so), where)
     return out
 
 
@@ -313,7 +312,7 @@ def combine_backward(dout, rows, pair_row, topk_w, drows=None, dw=None):
     """drows[pair_row[t, q]] = topk_w[t, q] dout[t] and dw[t, q] = <dout[t], rows[pair_row[t, q]]>
     (deamoe_combine_backward).  Returns (drows, dw); rows of drows that no pair points to are left as they were
     (uninitialised if drows was made here)."""
-    where = "deamoe_combine_backward"
+    where, dev = "deamoe_combine_backward", _device()
     dt = _type(dout, where, "dout")
     T, h = dout.shape
     k = pair_row.shape[-1]
@@ -322,64 +321,63 @@ def combine_backward(dout, rows, pair_row, topk_w, drows=None, dw=None):
         drows = dout.new_empty((n, h))
     if dw is None:
         dw = torch.empty((T, k), dtype=torch.float32, device=dout.device)
-    pd, sd = _mat(dout, where, "dout", dout.dtype, T, h)
-    pr, sr = _mat(rows, where, "rows", dout.dtype, n, h)
-    pg, sg = _mat(drows, where, "drows", dout.dtype, n, h)
-    _done(lib().deamoe_combine_backward(_raw_stream(_device()), dt, pd, sd, pr, sr, n, _vec(pair_row, where, "pair_row", torch.int32, T, k),
-                                        _vec(topk_w, where, "topk_w", torch.float32, T, k), T, k, h, pg, sg,
-                                        _vec(dw, where, "dw", torch.float32, T, k)), where)
+    pd, sd = _mat(dout, where, "dout", dout.dtype, T, h, dev)
+    pr, sr = _mat(rows, where, "rows", dout.dtype, n, h, dev)
+    pg, sg = _mat(drows, where, "drows", dout.dtype, n, h, dev)
+    _done(lib().deamoe_combine_backward(_raw_stream(dev), dt, pd, sd, pr, sr, n, _vec(pair_row, where, "pair_row", torch.int32, (T, k), dev),
+                                        _vec(topk_w, where, "topk_w", torch.float32, (T, k), dev), T, k, h, pg, sg,
+                                        _vec(dw, where, "dw", torch.float32, (T, k), dev)), where)
     return drows, dw
 
 
-def _gain(w, where, name, h, other=None):
+def _gain(w, where, name, h, dev, other=None):
     """Address and type code of a gain (None = ones).  Two gains of one call have one type."""
     if w is None:
         return None, (F32 if other is None else _TYPES.get(other.dtype, -1))
     code = _TYPES.get(w.dtype)
     if code is None or (other is not None and other.dtype != w.dtype):
         _refuse(where, f"{name} must be float32 or bfloat16, and of one type with the call's other gain")
-    return _vec(w, where, name, w.dtype, h), code
+    return _vec(w, where, name, w.dtype, (h,), dev), code
 
 
 def norm(x, weight, eps, out=None):
     """out = x / sqrt(mean(x^2) + eps) * weight, row by row (deamoe_norm).  weight [h] (float32 or bfloat16) or None; out may
     be x."""
-    where = "deamoe_norm"
+    where, dev = "deamoe_norm", _device()
     dt = _type(x, where, "x")
     T, h = x.shape
     if out is None:
-        out = x.new_empty((T, h))
-    px, sx = _mat(x, where, "x", x.dtype, T, h)
-    po, so = _mat(out, where, "out", x.dtype, T, h)
-    pw, wdt = _gain(weight, where, "weight", h)
-    _done(lib().deamoe_norm(_raw_stream(_device()), dt, px, sx, T, h, wdt, pw, eps, po, so), where)
+        out = torch.empty_like(x)
+    px, sx = _mat(x, where, "x", x.dtype, T, h, dev)
+    po, so = _mat(out, where, "out", x.dtype, T, h, dev)
+    pw, wdt = _gain(weight, where, "weight", h, dev)
+    _done(lib().deamoe_norm(_raw_stream(dev), dt, px, sx, T, h, wdt, pw, eps, po, so), where)
     return out
 
 
 def norm_backward(x, weight, eps, du, dadd=None, dx=None):
     """Gradients of `norm`: dx (plus dadd, the gradient that reaches x past the norm; dx may be dadd) and dweight
     (float32 [h]) (deamoe_norm_backward)."""
-    where = "deamoe_norm_backward"
+    where, dev = "deamoe_norm_backward", _device()
     dt = _type(x, where, "x")
     T, h = x.shape
-    dev = x.device
     if dx is None:
-        dx = x.new_empty((T, h))
-    dw = torch.empty(h, dtype=torch.float32, device=dev)
-    px, sx = _mat(x, where, "x", x.dtype, T, h)
-    pu, su = _mat(du, where, "du", x.dtype, T, h)
-    pa, sa = _mat(dadd, where, "dadd", x.dtype, T, h) if dadd is not None else (None, 0)
-    pd, sd = _mat(dx, where, "dx", x.dtype, T, h)
-    pw, wdt = _gain(weight, where, "weight", h)
+        dx = torch.empty_like(x)
+    dw = torch.empty(h, dtype=torch.float32, device=x.device)
+    px, sx = _mat(x, where, "x", x.dtype, T, h, dev)
+    pu, su = _mat(du, where, "du", x.dtype, T, h, dev)
+    pa, sa = _mat(dadd, where, "dadd", x.dtype, T, h, dev) if dadd is not None else (None, 0)
+    pd, sd = _mat(dx, where, "dx", x.dtype, T, h, dev)
+    pw, wdt = _gain(weight, where, "weight", h, dev)
     L = lib()
     need = L.deamoe_norm_workspace(T, h)
-    ws = _workspace(need, dev)
-    _done(L.deamoe_norm_backward(_raw_stream(_device()), dt, px, sx, T, h, wdt, pw, eps, pu, su, pa, sa, pd, sd, dw.data_ptr(), _dptr(ws),
+    ws = _workspace(need, x.device)
+    _done(L.deamoe_norm_backward(_raw_stream(dev), dt, px, sx, T, h, wdt, pw, eps, pu, su, pa, sa, pd, sd, dw.data_ptr(), _dptr(ws),
                                  need), where)
     return dx, dw
 
 
-def _gate(gate, where, dtype, T, h, kind):
+def _gate(gate, where, dtype, T, h, kind, dev):
     """Kind, address and row stride of a gate.  [h] is one per channel, [T, 1] or [T] one per token, [T, h] full; a gate of
     one dimension with T == h needs `gate_kind`."""
     if gate is None:
@@ -390,10 +388,10 @@ def _gate(gate, where, dtype, T, h, kind):
             _refuse(where, "gate [h] with as many tokens as channels: say gate_kind")
         kind = {(h,): GATE_CHANNEL, (T,): GATE_TOKEN, (T, h): GATE_FULL}.get(shape)
     if kind == GATE_FULL:
-        return (kind,) + _mat(gate, where, "gate", dtype, T, h)
+        return (kind,) + _mat(gate, where, "gate", dtype, T, h, dev)
     if kind not in (GATE_CHANNEL, GATE_TOKEN):
         _refuse(where, f"gate must be [{h}] (channels), [{T}] (tokens) or [{T}, {h}], got {list(shape)}")
-    return kind, _vec(gate, where, "gate", dtype, h if kind == GATE_CHANNEL else T), 0
+    return kind, _vec(gate, where, "gate", dtype, (h if kind == GATE_CHANNEL else T,), dev), 0
 
 
 def norm_residual(x, y, weight, eps, gate=None, residual_scale=1.0, branch_scale=1.0, normalise=True, next_norm=True,
@@ -401,21 +399,21 @@ def norm_residual(x, y, weight, eps, gate=None, residual_scale=1.0, branch_scale
     """s = residual_scale x + branch_scale gate (y / rms(y) weight); returns s and s / rms(s) next_weight (None with
     next_norm=False) in one pass (deamoe_norm_residual).  gate: None, [h], [T] or [T, h]; normalise=False takes y as it
     is.  out may be x."""
-    where = "deamoe_norm_residual"
+    where, dev = "deamoe_norm_residual", _device()
     dt = _type(x, where, "x")
     T, h = x.shape
     if out is None:
-        out = x.new_empty((T, h))
+        out = torch.empty_like(x)
     if next_out is None and next_norm:
-        next_out = x.new_empty((T, h))
-    px, sx = _mat(x, where, "x", x.dtype, T, h)
-    py, sy = _mat(y, where, "y", x.dtype, T, h)
-    po, so = _mat(out, where, "out", x.dtype, T, h)
-    pn, sn = _mat(next_out, where, "next_out", x.dtype, T, h) if next_norm else (None, 0)
-    pw, wdt = _gain(weight, where, "weight", h, next_weight)
-    pm, _ = _gain(next_weight, where, "next_weight", h, weight)
-    kind, pg, sg = _gate(gate, where, x.dtype, T, h, gate_kind)
-    _done(lib().deamoe_norm_residual(_raw_stream(_device()), dt, px, sx, py, sy, T, h, 1 if normalise else 0, wdt, pw, eps, kind, pg, sg,
+        next_out = torch.empty_like(x)
+    px, sx = _mat(x, where, "x", x.dtype, T, h, dev)
+    py, sy = _mat(y, where, "y", x.dtype, T, h, dev)
+    po, so = _mat(out, where, "out", x.dtype, T, h, dev)
+    pn, sn = _mat(next_out, where, "next_out", x.dtype, T, h, dev) if next_norm else (None, 0)
+    pw, wdt = _gain(weight, where, "weight", h, dev, next_weight)
+    pm, _ = _gain(next_weight, where, "next_weight", h, dev, weight)
+    kind, pg, sg = _gate(gate, where, x.dtype, T, h, gate_kind, dev)
+    _done(lib().deamoe_norm_residual(_raw_stream(dev), dt, px, sx, py, sy, T, h, 1 if normalise else 0, wdt, pw, eps, kind, pg, sg,
                                      residual_scale, branch_scale, po, so, pm, eps if next_eps is None else next_eps,
                                      pn, sn), where)
     return out, next_out if next_norm else None
@@ -427,34 +425,38 @@ def norm_residual_backward(x, y, weight, eps, dout, gate=None, residual_scale=1.
     dweight, dnext_weight; the last three are None where the call has no such input.  dweight, dnext_weight and the
     gradient of a per-channel or per-token gate are float32, that of a full gate has the gate's type
     (deamoe_norm_residual_backward)."""
-    where = "deamoe_norm_residual_backward"
+    where, dev = "deamoe_norm_residual_backward", _device()
     dt = _type(x, where, "x")
     T, h = x.shape
-    dev = x.device
     if dx is None:
-        dx = x.new_empty((T, h))
+        dx = torch.empty_like(x)
     if dy is None:
-        dy = x.new_empty((T, h))
-    px, sx = _mat(x, where, "x", x.dtype, T, h)
-    py, sy = _mat(y, where, "y", x.dtype, T, h)
-    po, so = _mat(dout, where, "dout", x.dtype, T, h)
-    pu, su = _mat(du, where, "du", x.dtype, T, h) if du is not None else (None, 0)
-    pdx, sdx = _mat(dx, where, "dx", x.dtype, T, h)
-    pdy, sdy = _mat(dy, where, "dy", x.dtype, T, h)
-    pw, wdt = _gain(weight, where, "weight", h, next_weight)
-    pm, _ = _gain(next_weight, where, "next_weight", h, weight)
-    kind, pg, sg = _gate(gate, where, x.dtype, T, h, gate_kind)
+        dy = torch.empty_like(x)
+    px, sx = _mat(x, where, "x", x.dtype, T, h, dev)
+    py, sy = _mat(y, where, "y", x.dtype, T, h, dev)
+    po, so = _mat(dout, where, "dout", x.dtype, T, h, dev)
+    pu, su = _mat(du, where, "du", x.dtype, T, h, dev) if du is not None else (None, 0)
+    pdx, sdx = _mat(dx, where, "dx", x.dtype, T, h, dev)
+    pdy, sdy = _mat(dy, where, "dy", x.dtype, T, h, dev)
+    pw, wdt = _gain(weight, where, "weight", h, dev, next_weight)
+    pm, _ = _gain(next_weight, where, "next_weight", h, dev, weight)
+    kind, pg, sg = _gate(gate, where, x.dtype, T, h, gate_kind, dev)
     dgate, sdg = None, 0
-    if kind == GATE_FULL:
+    channel = kind == GATE_CHANNEL
+    n = (weight is not None) + (next_weight is not None) + channel
+    sums = list(torch.empty((n, h), dtype=torch.float32, device=x.device).unbind(0)) if n else []
+    dw = sums.pop() if weight is not None else None
+    dn = sums.pop() if next_weight is not None else None
+    if channel:
+        dgate = sums.pop()
+    elif kind == GATE_TOKEN:
+        dgate = torch.empty(T, dtype=torch.float32, device=x.device)
+    elif kind == GATE_FULL:
         dgate, sdg = x.new_empty((T, h)), h
-    elif kind != GATE_NONE:
-        dgate = torch.empty(h if kind == GATE_CHANNEL else T, dtype=torch.float32, device=dev)
-    dw = torch.empty(h, dtype=torch.float32, device=dev) if weight is not None else None
-    dn = torch.empty(h, dtype=torch.float32, device=dev) if next_weight is not None else None
     L = lib()
     need = L.deamoe_norm_workspace(T, h)
-    ws = _workspace(need, dev)
-    _done(L.deamoe_norm_residual_backward(_raw_stream(_device()), dt, px, sx, py, sy, T, h, 1 if normalise else 0, wdt, pw, eps, kind, pg,
+    ws = _workspace(need, x.device)
+    _done(L.deamoe_norm_residual_backward(_raw_stream(dev), dt, px, sx, py, sy, T, h, 1 if normalise else 0, wdt, pw, eps, kind, pg,
                                           sg, residual_scale, branch_scale, po, so, pm,
                                           eps if next_eps is None else next_eps, pu, su, pdx, sdx, pdy, sdy, _dptr(dgate),
                                           sdg, _dptr(dw), _dptr(dn), _dptr(ws), need), where)
@@ -467,7 +469,7 @@ def quant_product(codes, scales, x, group, zeros=None, expert_off=None, row_pair
     scales (float32 or bfloat16) and zeros (uint8, None = 8) [E, n_out, ceil(n_in / group)], x [T, n_in].
     expert_off / row_pair: as sort_pairs gives them; row r is a product with x[row_pair[r] // pairs_per_token].  Without
     row_pair, row r takes x[r].  Rows behind the last expert's are left as they were (uninitialised if out was made here)."""
-    where = "deamoe_quant_product"
+    where, dev = "deamoe_quant_product", _device()
     dt = _type(x, where, "x")
     T, n_in = x.shape
     if codes.dim() != 3 or n_in != 2 * codes.shape[2]:
@@ -481,16 +483,16 @@ def quant_product(codes, scales, x, group, zeros=None, expert_off=None, row_pair
     sdt = _TYPES.get(scales.dtype)
     if sdt is None:
         _refuse(where, "scales must be float32 or bfloat16")
-    px, sx = _mat(x, where, "x", x.dtype, T, n_in)
-    po, so = _mat(out, where, "out", x.dtype, R, width)
-    pz = _vec(zeros, where, "zeros", torch.uint8, E, n_out, groups) if zeros is not None else None
-    pe = _vec(expert_off, where, "expert_off", torch.int32, E + 1) if expert_off is not None else None
-    pp = _vec(row_pair, where, "row_pair", torch.int32, R) if row_pair is not None else None
+    px, sx = _mat(x, where, "x", x.dtype, T, n_in, dev)
+    po, so = _mat(out, where, "out", x.dtype, R, width, dev)
+    pz = _vec(zeros, where, "zeros", torch.uint8, (E, n_out, groups), dev) if zeros is not None else None
+    pe = _vec(expert_off, where, "expert_off", torch.int32, (E + 1,), dev) if expert_off is not None else None
+    pp = _vec(row_pair, where, "row_pair", torch.int32, (R,), dev) if row_pair is not None else None
     L = lib()
     need = L.deamoe_quant_workspace(dt, R, n_in)
     ws = _workspace(need, x.device)
-    _done(L.deamoe_quant_product(_raw_stream(_device()), dt, _vec(codes, where, "codes", torch.uint8, E, n_out, n_in // 2), sdt,
-                                 _vec(scales, where, "scales", scales.dtype, E, n_out, groups), pz, E, n_out, n_in, group, px,
+    _done(L.deamoe_quant_product(_raw_stream(dev), dt, _vec(codes, where, "codes", torch.uint8, (E, n_out, n_in // 2), dev), sdt,
+                                 _vec(scales, where, "scales", scales.dtype, (E, n_out, groups), dev), pz, E, n_out, n_in, group, px,
                                  sx, T, pe, pp, pairs_per_token, R, 1 if swiglu else 0, po, so, _dptr(ws), need), where)
     return out
 
