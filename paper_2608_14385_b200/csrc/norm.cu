@@ -764,22 +764,34 @@ struct ColumnSums {
   const float* part[3];
   float* out[3];
 };
-// A block adds 32 columns of one array: 32 row groups side by side, then the groups in order.
-__global__ void __launch_bounds__(1024) k_column_sums(ColumnSums S, int rows, int h) {
-  __shared__ float acc[32][33];
+// A block adds 32 CE columns of one array: 8 row groups side by side, then the groups in order.  CE: columns a thread, 4
+// where rows start on 16-byte boundaries.
+template <int CE> __global__ void __launch_bounds__(256) k_column_sums(ColumnSums S, int rows, int h) {
+  __shared__ float acc[8][32 * CE];
   pdl_wait();
   const float* p = S.part[blockIdx.y];
-  const int c = blockIdx.x * 32 + (threadIdx.x & 31), g = threadIdx.x >> 5;
-  float s = 0.f;
+  const int lane = threadIdx.x & 31, g = threadIdx.x >> 5, c = (blockIdx.x * 32 + lane) * CE;
+  float s[CE] = {};
   if (c < h) {
-#pragma unroll 4
-    for (int r = g; r < rows; r += 32) s += p[(size_t)r * h + c];
+#pragma unroll 8
+    for (int r = g; r < rows; r += 8) {
+      float v[CE];
+      if constexpr (CE == 4) load_pack<float, 4>(p + (size_t)r * h + c).widen(v);
+      else v[0] = p[(size_t)r * h + c];
+#pragma unroll
+      for (int j = 0; j < CE; ++j) s[j] += v[j];
+    }
   }
-  acc[g][threadIdx.x & 31] = s;
+#pragma unroll
+  for (int j = 0; j < CE; ++j) acc[g][j * 32 + lane] = s[j];
   __syncthreads();
-  if (g == 0 && c < h) {
-    for (int i = 1; i < 32; ++i) s += acc[i][threadIdx.x & 31];
-    S.out[blockIdx.y][c] = s;
+  for (int i = threadIdx.x; i < 32 * CE; i += 256) {
+    const int col = (blockIdx.x * 32 + (i & 31)) * CE + (i >> 5);
+    if (col >= h) continue;
+    float t = 0.f;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) t += acc[k][i];
+    S.out[blockIdx.y][col] = t;
   }
 }
 
@@ -795,7 +807,9 @@ static bool bad_rows(const void* p, int64_t stride, int32_t h, size_t es) { retu
 
 static deamoe_status_t launch_sums(const ColumnSums& S, int arrays, int rows, int h, cudaStream_t s) {
   if (arrays == 0) return DEAMOE_OK;
-  if (launch_pdl(k_column_sums, dim3((h + 31) / 32, arrays), dim3(1024), 0, s, S, rows, h) != cudaSuccess) {
+  const cudaError_t e = h % 4 == 0 ? launch_pdl(k_column_sums<4>, dim3((h + 127) / 128, arrays), dim3(256), 0, s, S, rows, h)
+                                   : launch_pdl(k_column_sums<1>, dim3((h + 31) / 32, arrays), dim3(256), 0, s, S, rows, h);
+  if (e != cudaSuccess) {
     cudaGetLastError();
     return DEAMOE_ERR_CUDA;
   }

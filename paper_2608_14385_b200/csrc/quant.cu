@@ -50,46 +50,71 @@ struct QuantArgs {
 
 // x in the order of the rows, as fp16 scaled by 2^-e, 8 columns in the order 0 4 1 5 2 6 3 7 (the order in which the
 // codes of a 32-bit word are widened; 1 5 3 7 by another 1/16).  One block a row; a row without a source is zero.
-template <typename T, int PLANES, int GROUP> __global__ void __launch_bounds__(256) k_quant_x(QuantArgs A) {
-  __shared__ float buf[8];
+template <typename T> static __device__ __forceinline__ void eight_of(const T* x, int col, int n_in, bool wide, float (&v)[8]) {
+  constexpr int VE = 16 / sizeof(T);
+  if (wide && col + 8 <= n_in) {
+#pragma unroll
+    for (int i = 0; i < 8 / VE; ++i) {
+      float f[VE];
+      load_pack<T, VE>(x + col + i * VE).widen(f);
+#pragma unroll
+      for (int k = 0; k < VE; ++k) v[i * VE + k] = f[k];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = col + i < n_in ? to_f<T>(x[col + i]) : 0.f;
+  }
+}
+template <typename T, int PLANES, int GROUP> __global__ void __launch_bounds__(1024) k_quant_x(QuantArgs A, bool wide) {
+  __shared__ float buf[32];
   const int64_t r = blockIdx.x;
   int64_t src = r;
   if (A.row_pair) src = A.row_pair[r] >= 0 ? A.row_pair[r] / A.ppt : -1;
-  bool have = src >= 0 && src < A.n_token;
+  const bool have = src >= 0 && src < A.n_token;
   const T* x = reinterpret_cast<const T*>(A.x) + (have ? src : 0) * A.xs;
   pdl_trigger();
+  const int width = A.steps * QCOLS;
+  float v[8] = {};  // the thread's first eight columns (all of them up to 8192 columns); later ones are read twice
   float top = 0.f;
   bool odd = false;
-  for (int c = threadIdx.x; have && c < A.n_in; c += 256) {
-    const float v = fabsf(to_f<T>(x[c]));
-    if (v <= 3.4028234663852886e38f) top = fmaxf(top, v);
-    else odd = true;  // infinities and NaN
+  for (int c = threadIdx.x; have && c < width / 8; c += blockDim.x) {
+    float u[8];
+    eight_of<T>(x, c * 8, A.n_in, wide, u);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float m = fabsf(u[i]);
+      if (m <= 3.4028234663852886e38f) top = fmaxf(top, m);
+      else odd = true;  // infinities and NaN
+      if (c == (int)threadIdx.x) v[i] = u[i];
+    }
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = top;
   odd = __syncthreads_or(odd);
-  for (int i = 0; i < 8; ++i) top = fmaxf(top, buf[i]);
+  top = (threadIdx.x & 31) < (blockDim.x >> 5) ? buf[threadIdx.x & 31] : 0.f;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   const int e = top > 0.f ? ilogbf(top) - 14 : 0;
-  const bool apart = PLANES == 1 && odd;  // marked by a NaN in the place of its scale
-  if (threadIdx.x == 0) {                 // 2^(e + 24) as two factors, each in fp32's range
+  auto power = [](int k) { return __int_as_float((127 + k) << 23); };
+  const float f0 = power(-e / 2), f1 = power(-e - -e / 2);  // 2^-e as two factors, each in fp32's range
+  const bool apart = PLANES == 1 && odd;                    // marked by a NaN in the place of its scale
+  if (threadIdx.x == 0) {
     const int half = (e + 24) / 2;
-    A.xe[r] = apart ? 0x7fc00000 : (127 + half) << 23;
-    A.xe[(size_t)A.n_rows + r] = (127 + (e + 24) - half) << 23;
+    A.xe[r] = apart ? 0x7fc00000 : __float_as_int(power(half));
+    A.xe[(size_t)A.n_rows + r] = __float_as_int(power((e + 24) - half));
   }
-  have = have && !apart;
-  const int width = A.steps * QCOLS;
   __half* out = A.xh + r * PLANES * width;
-  for (int c0 = threadIdx.x & ~31; c0 < width / 8; c0 += 256) {  // whole warps: the group sums shuffle
-    const int c = c0 + (threadIdx.x & 31);
+  for (int c = threadIdx.x; c < width / 8; c += blockDim.x) {  // whole warps, a multiple of 32 packs: the group sums shuffle
+    if (c != (int)threadIdx.x && have) eight_of<T>(x, c * 8, A.n_in, wide, v);
     union { __half h[8]; uint4 u; } hi, lo;
     float sum = 0.f;
 #pragma unroll
     for (int p = 0; p < 8; ++p) {
-      const int col = c * 8 + (p >> 1) + (p & 1) * 4;
-      const float v = have && col < A.n_in ? scalbnf(to_f<T>(x[col]), -e) : 0.f;
-      const float u = (p & 2) ? v * 0.0625f : v;
-      sum += v;
+      const int i = (p >> 1) + (p & 1) * 4;
+      const float s = apart ? 0.f : v[i] * f0 * f1;
+      const float u = (p & 2) ? s * 0.0625f : s;
+      sum += s;
       hi.h[p] = __float2half_rn(u);
       const float rest = u - __half2float(hi.h[p]);
       lo.h[p] = __float2half_rn(isfinite(u) ? rest : 0.f);
@@ -98,7 +123,6 @@ template <typename T, int PLANES, int GROUP> __global__ void __launch_bounds__(2
 #pragma unroll
       for (int o = 1; o < GROUP / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     }
-    if (c >= width / 8) continue;
     *reinterpret_cast<uint4*>(out + c * 8) = hi.u;
     if constexpr (PLANES == 2) *reinterpret_cast<uint4*>(out + width + c * 8) = lo.u;
     const int grp = c / (GROUP / 8);
@@ -527,7 +551,9 @@ template <typename T, int NG> static deamoe_status_t quant_t(QuantArgs& A, cudaS
       done.fetch_or(1ull << dev, std::memory_order_release);
     }
     const size_t smem = (size_t)QW * depth * mt * 2048 + (size_t)QW * mt * 1024 + (size_t)(A.n_expert + 1) * 4;
-    k_quant_x<T, PLANES, QCOLS / NG><<<A.n_rows, 256, 0, s>>>(A);
+    const int threads = A.steps * (QCOLS / 8) < 1024 ? A.steps * (QCOLS / 8) : 1024;
+    const bool wide = aligned16(A.x) && (A.xs * (int64_t)sizeof(T)) % 16 == 0;
+    k_quant_x<T, PLANES, QCOLS / NG><<<A.n_rows, threads, 0, s>>>(A, wide);
     const cudaError_t e = cudaGetLastError();
     return e != cudaSuccess ? e : launch_pdl(kernel, dim3(Q_GRID), dim3(QW * 32), smem, s, A);
   };

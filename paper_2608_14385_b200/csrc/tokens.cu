@@ -19,7 +19,7 @@ namespace deamoe {
 constexpr int SORT_SMALL_PAIRS = 4096;     // up to here one block sorts everything
 constexpr int SORT_COUNTERS = 16384;       // 16-bit counters of one block (warps x experts)
 constexpr int SORT_SMALL_ITERS = SORT_SMALL_PAIRS / 32 / (SORT_COUNTERS / DEAMOE_MAX_EXPERTS);
-constexpr int SORT_SEG = 2048;             // pairs of one block in the three-kernel form
+constexpr int SORT_SEG = 1024;             // pairs of one block in the three-kernel form
 constexpr int SORT_SEG_WARPS = 8;          // (8 warps x 2048 experts fit the counters)
 constexpr int SORT_SEG_ITERS = SORT_SEG / 32 / SORT_SEG_WARPS;
 
@@ -167,19 +167,30 @@ __global__ void __launch_bounds__(SORT_SEG_WARPS * 32) k_sort_place(const int32_
                                                                    int32_t* __restrict__ row_pair) {
   __shared__ int tot[DEAMOE_MAX_EXPERTS + 1];
   __shared__ int warp_sums[32];
+  constexpr int THREADS = SORT_SEG_WARPS * 32, PER = SORT_SEG / THREADS;
+  const int64_t begin = (int64_t)blockIdx.x * SORT_SEG + threadIdx.x;
+  int e[PER], base[PER], rk[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) e[i] = begin + i * THREADS < P ? sort_key(idx, (int)(begin + i * THREADS), P, n) : n;
   pdl_wait();
-  for (int e = threadIdx.x; e < n; e += blockDim.x) tot[e] = total[e];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    base[i] = e[i] < n ? hist[(size_t)blockIdx.x * n + e[i]] : 0;
+    rk[i] = e[i] < n ? rank[begin + i * THREADS] : 0;
+  }
+  for (int k = threadIdx.x; k < n; k += THREADS) tot[k] = total[k];
   __syncthreads();
   block_exclusive_scan(tot, n, warp_sums);
   if (blockIdx.x == 0)
-    for (int e = threadIdx.x; e <= n; e += blockDim.x) expert_off[e] = tot[e];
+    for (int k = threadIdx.x; k <= n; k += THREADS) expert_off[k] = tot[k];
   const int filled = tot[n];
-  const int64_t begin = (int64_t)blockIdx.x * SORT_SEG, end = min((int64_t)P, begin + SORT_SEG);
-  for (int64_t p = begin + threadIdx.x; p < end; p += blockDim.x) {
-    const int e = sort_key(idx, (int)p, P, n);
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int64_t p = begin + i * THREADS;
+    if (p >= P) break;
     int row = -1;
-    if (e < n) {
-      row = tot[e] + hist[(size_t)blockIdx.x * n + e] + rank[p];
+    if (e[i] < n) {
+      row = tot[e[i]] + base[i] + rk[i];
       row_pair[row] = (int)p;
     }
     pair_row[p] = row;
