@@ -7,16 +7,12 @@
 //
 // Tensor cores: mma.m16n8k16 with 16 matrix rows as M and up to 8 tokens as N (legacy path: with this few tokens the
 // instruction rate it needs is a fraction of what it has, and its A operand comes from registers, where the codes
-// have to be widened anyway).  Widening is one AND a pair: a nibble in the low bits of a 16-bit half IS the fp16
-// subnormal q 2^-24, and in the next four bits q 2^-20; tensor cores multiply subnormals exactly.  x becomes fp16 in a
-// kernel of its own: each row scaled by a power of two to a largest magnitude of 2^14..2^15, the columns that meet
-// 2^-20 by another 2^-4, so that fp16's range costs nothing (values below 2^-35 of the row's largest lose bits, far
-// under fp32's own resolution of the sum); bf16 values fit exactly, fp32 values as two parts (2^-23 relative).
-// The zero points.  For bf16 tokens they leave the sum, sum (q - z) x = sum q x - z sum x, with the groups' sums of x from
-// the same kernel: the subtraction may cancel some of fp32's bits, which a bf16 result does not see, and it saves a
-// third of the loop's instructions (the loop is bound by their issue).  For fp32 tokens q - z is formed first,
-// exactly.  A bf16 row with an infinity or a NaN would lose the difference between them that way; such rows are
-// computed from the definition, value by value.
+// have to be widened anyway).  Widening is an AND and a subtraction a pair: a nibble in the low bits of a 16-bit half IS
+// the fp16 subnormal q 2^-24, and in the next four bits q 2^-20; q - z is exact there, and tensor cores multiply
+// subnormals exactly.  x becomes fp16 in a kernel of its own: each row scaled by a power of two to a largest magnitude
+// of 2^14..2^15, the columns that meet 2^-20 by another 2^-4, so that fp16's range costs nothing (values below 2^-35
+// of the row's largest lose bits, far under fp32's own resolution of the sum); bf16 values fit exactly, fp32 values as
+// two parts (2^-23 relative).
 #include <atomic>
 #include <climits>
 #include <cuda_fp16.h>
@@ -40,11 +36,11 @@ struct QuantArgs {
   void* out;
   int64_t os;
   int n_expert, n_out, n_in, groups, n_token, ppt, n_rows, swiglu, scale_f32;
+  int vec_scales, vec_zeros;  // a step's scales / zero points of a row can be read as one vector
   int steps;        // column steps of a row
   int wk;           // warps that share a row tile's columns (the others of the block take other tiles)
   int tile_groups;  // blocks of QW / wk warp tiles (16 MT rows) a matrix
   __half* xh;       // [n_rows][planes][steps * QCOLS]
-  float* xg;        // bf16 tokens: [groups][n_rows + 32] sums of the groups of the scaled rows, times 2^-24
   int32_t* xe;      // [2][n_rows] two powers of two (fp32 bits) that undo the row's scaling
 };
 
@@ -65,7 +61,7 @@ template <typename T> static __device__ __forceinline__ void eight_of(const T* x
     for (int i = 0; i < 8; ++i) v[i] = col + i < n_in ? to_f<T>(x[col + i]) : 0.f;
   }
 }
-template <typename T, int PLANES, int GROUP> __global__ void __launch_bounds__(1024) k_quant_x(QuantArgs A, bool wide) {
+template <typename T, int PLANES> __global__ void __launch_bounds__(1024) k_quant_x(QuantArgs A, bool wide) {
   __shared__ float buf[32];
   const int64_t r = blockIdx.x;
   int64_t src = r;
@@ -76,73 +72,46 @@ template <typename T, int PLANES, int GROUP> __global__ void __launch_bounds__(1
   const int width = A.steps * QCOLS;
   float v[8] = {};  // the thread's first eight columns (all of them up to 8192 columns); later ones are read twice
   float top = 0.f;
-  bool odd = false;
   for (int c = threadIdx.x; have && c < width / 8; c += blockDim.x) {
     float u[8];
     eight_of<T>(x, c * 8, A.n_in, wide, u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float m = fabsf(u[i]);
-      if (m <= 3.4028234663852886e38f) top = fmaxf(top, m);
-      else odd = true;  // infinities and NaN
+      if (m <= 3.4028234663852886e38f) top = fmaxf(top, m);  // infinities and NaN stay what they are
       if (c == (int)threadIdx.x) v[i] = u[i];
     }
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = top;
-  odd = __syncthreads_or(odd);
+  __syncthreads();
   top = (threadIdx.x & 31) < (blockDim.x >> 5) ? buf[threadIdx.x & 31] : 0.f;
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
   const int e = top > 0.f ? ilogbf(top) - 14 : 0;
   auto power = [](int k) { return __int_as_float((127 + k) << 23); };
   const float f0 = power(-e / 2), f1 = power(-e - -e / 2);  // 2^-e as two factors, each in fp32's range
-  const bool apart = PLANES == 1 && odd;                    // marked by a NaN in the place of its scale
   if (threadIdx.x == 0) {
     const int half = (e + 24) / 2;
-    A.xe[r] = apart ? 0x7fc00000 : __float_as_int(power(half));
+    A.xe[r] = __float_as_int(power(half));
     A.xe[(size_t)A.n_rows + r] = __float_as_int(power((e + 24) - half));
   }
   __half* out = A.xh + r * PLANES * width;
-  for (int c = threadIdx.x; c < width / 8; c += blockDim.x) {  // whole warps, a multiple of 32 packs: the group sums shuffle
+  for (int c = threadIdx.x; c < width / 8; c += blockDim.x) {
     if (c != (int)threadIdx.x && have) eight_of<T>(x, c * 8, A.n_in, wide, v);
     union { __half h[8]; uint4 u; } hi, lo;
-    float sum = 0.f;
 #pragma unroll
     for (int p = 0; p < 8; ++p) {
       const int i = (p >> 1) + (p & 1) * 4;
-      const float s = apart ? 0.f : v[i] * f0 * f1;
-      const float u = (p & 2) ? s * 0.0625f : s;
-      sum += s;
+      const float s = v[i] * f0 * f1, u = (p & 2) ? s * 0.0625f : s;
       hi.h[p] = __float2half_rn(u);
       const float rest = u - __half2float(hi.h[p]);
       lo.h[p] = __float2half_rn(isfinite(u) ? rest : 0.f);
     }
-    if constexpr (PLANES == 1) {
-#pragma unroll
-      for (int o = 1; o < GROUP / 8; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    }
     *reinterpret_cast<uint4*>(out + c * 8) = hi.u;
     if constexpr (PLANES == 2) *reinterpret_cast<uint4*>(out + width + c * 8) = lo.u;
-    const int grp = c / (GROUP / 8);
-    if (PLANES == 1 && c % (GROUP / 8) == 0 && grp < A.groups)
-      A.xg[(size_t)grp * (A.n_rows + 32) + r] = sum * 5.9604644775390625e-8f;
   }
-}
-
-// One product from the definition, for the rows set apart.
-template <typename T>
-static __device__ __noinline__ float quant_dot(const uint8_t* codes, const void* scales, bool scale_f32, const uint8_t* zeros,
-                                               const T* x, int n_in, int group) {
-  float acc = 0.f;
-  for (int c = 0; c < n_in; ++c) {
-    const int k = c / group, q = (codes[c >> 1] >> ((c & 1) * 4)) & 15;
-    const float s = scale_f32 ? reinterpret_cast<const float*>(scales)[k]
-                              : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(scales)[k]);
-    acc = fmaf(s * (float)(q - (zeros ? zeros[k] & 15 : 8)), to_f<T>(x[c]), acc);
-  }
-  return acc;
 }
 
 static __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
@@ -158,21 +127,13 @@ static __device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0,
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-// The 8 codes of a word (LESS: less the zero point) as four pairs of fp16 subnormals: columns (0 4) (1 5) (2 6) (3 7),
-// times 2^-24 and 2^-20 in turn.  z: the zero point in the low bits of both halves.
+// The 8 codes of a word less the zero point as four pairs of fp16 subnormals: columns (0 4) (1 5) (2 6) (3 7), times 2^-24 and 2^-20 in turn.  z: the zero point in the low bits of both halves.
 static __device__ __forceinline__ uint32_t less(uint32_t a, uint32_t b) {
   const __half2 d = __hsub2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&d);
 }
-template <bool LESS> static __device__ __forceinline__ void widen(uint32_t w, uint32_t z, uint32_t (&p)[4]) {
+static __device__ __forceinline__ void widen(uint32_t w, uint32_t z, uint32_t (&p)[4]) {
   const uint32_t v = w >> 8, z4 = z << 4;
-  if constexpr (!LESS) {
-    p[0] = w & 0x000f000fu;
-    p[1] = w & 0x00f000f0u;
-    p[2] = v & 0x000f000fu;
-    p[3] = v & 0x00f000f0u;
-    return;
-  }
   p[0] = less(w & 0x000f000fu, z);
   p[1] = less(w & 0x00f000f0u, z4);
   p[2] = less(v & 0x000f000fu, z);
@@ -208,22 +169,28 @@ constexpr int Q_TOKENS = 16;  // tokens of a pass
 // Every warp streams its own codes, DEPTH steps of 16 MT rows x 256 columns ahead and across items, into its own part
 // of shared memory; nothing is shared between warps but the sums at an item's end.
 template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
-  static constexpr int STEP = MT * 2048, NB = 2 * MT;  // NB: blocks of 8 matrix rows in a warp tile
+  static constexpr int NB = 2 * MT;  // blocks of 8 matrix rows in a warp tile
+  // a slot of the ring: codes, then every row's scales of the step (fp32), then its zero points (bytes)
+  static constexpr int SCALES = MT * 2048, ZEROS = SCALES + 16 * MT * NG * 4, STEP = (ZEROS + (Z ? 16 * MT * NG : 0) + 127) / 128 * 128;
   // Matrices narrower than a warp tile are MT = 1's; else the last tile of a matrix is moved up to its last row, so that
   // every row of every tile exists (the rows that it shares with the tile before are computed twice and written once).
   static constexpr bool NARROW = MT == 1;
   static constexpr int LM = MT == 2 ? 1 : 2;
-  static constexpr bool LIN = PLANES == 1;  // zero points leave the sum
   const QuantArgs& A;
   const int* first;
   int i1, wr, c0, c1, tiles_per, width, lane, g, j;
   uint32_t ring_at;
-  uint32_t scale_to[NB];        // bytes from block 0's scales to block b's (a matrix has less than 4 GB of them)
   size_t pair_rows, next_rows;  // matrix rows from block 2 m to block 2 m + 1, and to block 2 m + 2
   // the codes' cursor
   QuantAt ahead;
   int p_c, p_out;                // p_out: output column of row g of block 0
   const uint8_t* p_code[NB];     // this lane's 16-byte pieces of row g of the blocks
+  // A lane also brings the scales and zero points of one tile row (lane; MT == 1: the first 16 lanes).  They go through
+  // registers: a step's are loaded when its codes are requested and written to its slot at the request after, when
+  // they have arrived
+  bool held, s_exists;
+  uint32_t held_at, s_raw[NG], z_raw[NG];
+  size_t s_at;                   // index of the row's scales of the next step
 
   __device__ __forceinline__ QuantWarp(const QuantArgs& a, const int* f, const QuantAt& at, int end, int w, int ln, uint32_t ring)
       : A(a), first(f), i1(end), lane(ln), g(ln >> 2), j(ln & 3), ring_at(ring), ahead(at) {
@@ -236,11 +203,7 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
     pair_rows = A.swiglu ? width : 8;
     next_rows = A.swiglu ? 8 : 16;
     p_c = c0;
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      scale_to[b] = (uint32_t)(rows_to(b) * A.groups) << (A.scale_f32 ? 2 : 1);
-      asm volatile("" : "+r"(scale_to[b]));  // computed once, kept
-    }
+    held = false;
   }
   // output column of row g of the tile's block 0; block b adds out_of(b)
   __device__ __forceinline__ int out_at(const QuantAt& at) const {
@@ -255,17 +218,78 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
     p_out = out_at(ahead);
     const size_t row = (size_t)ahead.e * A.n_out + p_out, half = A.n_in / 2;
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      p_code[b] = A.codes + (row + rows_to(b)) * half + (size_t)c0 * (QCOLS / 2) + j * 16;
-      // the scales of the item to come: into the L2
-      if (exists(p_out, b)) {
-        const size_t i = (row + rows_to(b)) * A.groups + (size_t)c0 * NG;
-        const int shift = A.scale_f32 ? 2 : 1, bytes = (min(c1 * NG, A.groups) - c0 * NG) << shift;
-        const char* s = reinterpret_cast<const char*>(A.scales) + (i << shift) + (j * 32 < bytes ? j * 32 : 0);
-        asm volatile("prefetch.global.L2 [%0];" ::"l"(s));
-        if constexpr (Z) asm volatile("prefetch.global.L2 [%0];" ::"l"(A.zeros + i));
+    for (int b = 0; b < NB; ++b) p_code[b] = A.codes + (row + rows_to(b)) * half + (size_t)c0 * (QCOLS / 2) + j * 16;
+    const int sb = lane >> 3, sr = lane & 7;
+    s_exists = sb < NB && exists(p_out - g + sr, sb);
+    s_at = (row - g + sr + rows_to(sb)) * A.groups + (size_t)c0 * NG;
+  }
+  static __device__ __forceinline__ void put_words(uint32_t to, const uint32_t (&v)[NG]) {
+#pragma unroll
+    for (int k = 0; k < NG; k += 2) asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(to + k * 4), "r"(v[k]), "r"(v[k + 1]) : "memory");
+  }
+  // what the lane holds, to its slot
+  __device__ __forceinline__ void flush() {
+    if (!held) return;
+    uint32_t v[NG];
+#pragma unroll
+    for (int k = 0; k < NG; ++k)
+      v[k] = A.scale_f32 ? s_raw[k] : !A.vec_scales ? s_raw[k] << 16 : (k & 1) ? s_raw[k / 2] & 0xffff0000u : s_raw[k / 2] << 16;
+    put_words(held_at + SCALES + lane * NG * 4, v);
+    if constexpr (Z) {
+#pragma unroll
+      for (int k = 0; k < NG; k += 2) {
+        const uint32_t two = !A.vec_zeros ? s_zero(k) | s_zero(k + 1) << 8 : z_raw[k / 4] >> (k & 2) * 8;
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"(held_at + ZEROS + lane * NG + k), "h"((unsigned short)two) : "memory");
       }
     }
+    held = false;
+  }
+  __device__ __forceinline__ uint32_t s_zero(int k) const { return z_raw[k] & 255; }
+  // the next step's scales and zero points, to be held
+  __device__ __forceinline__ void hold(uint32_t slot) {
+    held = lane < 16 * MT;
+    held_at = ring_at + slot;
+    const bool have = held && s_exists;
+    const int groups = have ? min(NG, A.groups - p_c * NG) : 0;  // absent ones count as 0: their codes and x are 0 too
+#pragma unroll
+    for (int k = 0; k < NG; ++k) s_raw[k] = z_raw[k] = 0;
+    const char* s = reinterpret_cast<const char*>(A.scales) + s_at * (A.scale_f32 ? 4 : 2);
+    if (A.vec_scales) {
+      if (have) {
+        constexpr int HALF = NG / 2;  // words of NG bf16 values
+        if (A.scale_f32) {
+#pragma unroll
+          for (int k = 0; k < NG; k += 2) *reinterpret_cast<uint2*>(s_raw + k) = reinterpret_cast<const uint2*>(s)[k / 2];
+        } else if constexpr (HALF == 1) {
+          s_raw[0] = *reinterpret_cast<const uint32_t*>(s);
+        } else {
+#pragma unroll
+          for (int k = 0; k < HALF; k += 2) *reinterpret_cast<uint2*>(s_raw + k) = reinterpret_cast<const uint2*>(s)[k / 2];
+        }
+      }
+    } else {
+#pragma unroll
+      for (int k = 0; k < NG; ++k)
+        if (k < groups) s_raw[k] = A.scale_f32 ? reinterpret_cast<const uint32_t*>(s)[k] : reinterpret_cast<const unsigned short*>(s)[k];
+    }
+    if constexpr (Z) {
+      const uint8_t* z = A.zeros + s_at;
+      if (A.vec_zeros) {
+        if (have) {
+          if constexpr (NG == 2) {
+            z_raw[0] = *reinterpret_cast<const unsigned short*>(z);
+          } else {
+#pragma unroll
+            for (int k = 0; k < NG; k += 4) z_raw[k / 4] = reinterpret_cast<const uint32_t*>(z)[k / 4];
+          }
+        }
+      } else {
+#pragma unroll
+        for (int k = 0; k < NG; ++k)
+          if (k < groups) z_raw[k] = z[k];
+      }
+    }
+    s_at += NG;
   }
   // the next step's codes into the slot at byte `slot` of the ring
   __device__ __forceinline__ void request(uint32_t slot) {
@@ -283,11 +307,15 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
                      "r"(have && left > 128 ? 16 : 0) : "memory");
         p_code[b] += QCOLS / 2;
       }
+      flush();
+      hold(slot);
       if (++p_c == c1) {
         p_c = c0;
         quant_next(ahead, i1, first, A.tile_groups);
         if (ahead.item < i1) aim();
       }
+    } else {
+      flush();
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
   }
@@ -295,54 +323,7 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
   // The warp's columns of one item for NT * 8 tokens: acc[mt][t] = this warp's share of the products.
   template <int NT>
   __device__ __forceinline__ void item(const QuantAt& at, int row0, int rows, uint32_t& slot, float (&acc)[MT][2][4]) {
-    const int xw = A.steps * QCOLS, o0 = out_at(at);
-    const int shift = A.scale_f32 ? 2 : 1;
-    const size_t s_first = ((size_t)at.e * A.n_out + o0) * A.groups + (size_t)c0 * NG;
-    const char* s_at = reinterpret_cast<const char*>(A.scales) + (s_first << shift);
-    const uint8_t* z_at = A.zeros + s_first;
-    const size_t xg_step = (size_t)A.n_rows + 32;
-    const float* xg_at = A.xg + (size_t)c0 * NG * xg_step + row0 + j * 2;
-    int groups_left = min(c1 * NG, A.groups) - c0 * NG;  // from the one at hand on (the last step may have fewer than NG)
-    // of the group at hand: scale and zero point of the lane's rows, sums of x of the lane's tokens of the products.  Loaded
-    // when the group before is done with them
-    float sc[NB], gx[NT][2];
-    uint32_t z[NB];
-    auto fetch = [&]() {
-      if (groups_left > 0) {
-        if constexpr (LIN) {
-#pragma unroll
-          for (int t = 0; t < NT; ++t) {
-            gx[t][0] = xg_at[t * 8];
-            gx[t][1] = xg_at[t * 8 + 1];
-          }
-          xg_at += xg_step;
-        }
-        if (A.scale_f32) {
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-            if (exists(o0, b)) sc[b] = *reinterpret_cast<const float*>(s_at + scale_to[b]);
-        } else {
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-            if (exists(o0, b)) sc[b] = __uint_as_float((uint32_t)*reinterpret_cast<const unsigned short*>(s_at + scale_to[b]) << 16);
-        }
-        if constexpr (Z) {
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-            if (exists(o0, b)) z[b] = z_at[scale_to[b] >> shift];
-        }
-      }
-      s_at += 1 << shift;
-      ++z_at;
-    };
-#pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      sc[b] = 0.f;
-      z[b] = 8;
-    }
-#pragma unroll
-    for (int t = 0; t < NT; ++t) gx[t][0] = gx[t][1] = 0.f;
-    fetch();
+    const int xw = A.steps * QCOLS;
     // tokens past the last take the last one's values: their sums are not looked at
     const __half* xp[NT];
     // parts of x ahead: as many as registers allow
@@ -365,10 +346,23 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
       asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
       __syncwarp();
       uint32_t code[NB * LM];  // the codes of LM parts
-      const uint32_t from = lane_at + slot;
-      float grp[MT][NT][4];
+      const uint32_t from = lane_at + slot, scales = ring_at + slot + SCALES + g * NG * 4, zeros = ring_at + slot + ZEROS + g * NG;
+      float grp[MT][NT][4], sc[NB];
+      uint32_t z[NB];
 #pragma unroll
       for (int m = 0; m < QM; ++m) {
+        if (m * NG % QM == 0) {  // a group begins: scale and zero point of the lane's rows
+          const int k = m * NG / QM;
+#pragma unroll
+          for (int b = 0; b < NB; ++b) {
+            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(sc[b]) : "r"(scales + (b * 8 * NG + k) * 4) : "memory");
+            z[b] = 0x00080008u;
+            if constexpr (Z) {
+              asm volatile("ld.shared.u8 %0, [%1];" : "=r"(z[b]) : "r"(zeros + b * 8 * NG + k) : "memory");
+              z[b] = (z[b] & 15) * 0x00010001u;
+            }
+          }
+        }
         if (m % LM == 0)
           asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                        : "=r"(code[0]), "=r"(code[1]), "=r"(code[2]), "=r"(code[3]) : "r"(from ^ (m * 16)) : "memory");
@@ -386,7 +380,7 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
         }
         uint32_t w[NB][4];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) widen<!LIN>(code[(m % LM) * NB + b], Z ? (z[b] & 15) * 0x00010001u : 0x00080008u, w[b]);
+        for (int b = 0; b < NB; ++b) widen(code[(m % LM) * NB + b], z[b], w[b]);
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -405,22 +399,15 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
           if (m + 4 < QM || more) xb[m % 4][0][0] = load_b128(xp[0] + (m + 4) * 32);
         }
         if ((m + 1) * NG % QM == 0) {  // a group ends
-          if (groups_left > 0)
 #pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            // - z, and the group's sum less z sum x
-            const float zf = Z ? 8388608.f - __uint_as_float(0x4b000000u | (z[b] & 15)) : -8.f;
+          for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
               for (int i = 0; i < 2; ++i) {
-                const float v = grp[b >> 1][t][(b & 1) * 2 + i];
                 float& a = acc[b >> 1][t][(b & 1) * 2 + i];
-                a = fmaf(sc[b], LIN ? fmaf(zf, gx[t][i], v) : v, a);
+                a = fmaf(sc[b], grp[b >> 1][t][(b & 1) * 2 + i], a);
               }
-          }
-          --groups_left;
-          fetch();
         }
       }
 #pragma unroll
@@ -433,7 +420,8 @@ template <typename T, int PLANES, int MT, int NG, bool Z, int DEPTH>
 __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int warp_sums[QW];
-  float4* sums = reinterpret_cast<float4*>(smem + QW * DEPTH * MT * 2048);  // [2][QW][MT][32]
+  using Warp = QuantWarp<PLANES, MT, NG, Z, DEPTH>;
+  float4* sums = reinterpret_cast<float4*>(smem + QW * DEPTH * Warp::STEP);  // [2][QW][MT][32]
   int* first = reinterpret_cast<int*>(sums + 2 * QW * MT * 32);            // [n_expert + 1] first item of each expert
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, R = A.n_rows;
   auto row_begin = [&](int e) { return A.expert_off ? min(max(A.expert_off[e], 0), R) : 0; };
@@ -462,10 +450,10 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
     at.pass = (i0 - first[at.e]) - at.tg * at.passes;
   }
   const int width = A.swiglu ? A.n_out / 2 : A.n_out;
-  QuantWarp<PLANES, MT, NG, Z, DEPTH> W(A, first, at, i1, w, lane, (uint32_t)__cvta_generic_to_shared(smem + w * (DEPTH * MT * 2048)));
+  Warp W(A, first, at, i1, w, lane, (uint32_t)__cvta_generic_to_shared(smem + w * (DEPTH * Warp::STEP)));
   W.aim();
 #pragma unroll 1
-  for (int i = 0; i < DEPTH; ++i) W.request(i * MT * 2048);
+  for (int i = 0; i < DEPTH; ++i) W.request(i * Warp::STEP);
   pdl_wait();  // x in fp16
 
   uint32_t slot = 0;
@@ -486,22 +474,10 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
       const float p2 = __int_as_float(A.xe[r]), q2 = __int_as_float(A.xe[(size_t)R + r]);  // two powers of two
       a = a * p2 * q2;
       b = b * p2 * q2;
-      const bool apart = PLANES == 1 && !(p2 == p2);
       T* out = reinterpret_cast<T*>(A.out) + r * A.os;
       const int per = A.swiglu ? 8 : 16, o_tile = (at.tg * tiles_per + W.wr) * MT * per;  // its first column, before it was moved up
       const int o = (MT == 1 ? o_tile : max(min(o_tile, width - MT * per), 0)) + mt * per + (l >> 2);
       const bool w0 = o >= o_tile && o < width, w1 = !A.swiglu && o + 8 >= o_tile && o + 8 < width;
-      if (apart) {
-        auto dot = [&](int row) {
-          const size_t i = (size_t)at.e * A.n_out + row, k = i * A.groups;
-          const int64_t src = A.row_pair ? A.row_pair[r] / A.ppt : r;
-          return quant_dot<T>(A.codes + i * (A.n_in / 2), reinterpret_cast<const char*>(A.scales) + k * (A.scale_f32 ? 4 : 2),
-                              A.scale_f32, A.zeros ? A.zeros + k : nullptr, reinterpret_cast<const T*>(A.x) + src * A.xs, A.n_in,
-                              QCOLS / NG);
-        };
-        if (w0) a = dot(o);
-        if (A.swiglu ? w0 : w1) b = dot(A.swiglu ? width + o : o + 8);
-      }
       if (A.swiglu) a = a / (1.f + expf(-a)) * b;
       if (w0) out[o] = from_f<T>(a);
       if (w1) out[o + 8] = from_f<T>(b);
@@ -531,6 +507,8 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
 
 template <typename T, int NG> static deamoe_status_t quant_t(QuantArgs& A, cudaStream_t s) {
   constexpr int PLANES = sizeof(T) == 4 ? 2 : 1;
+  A.vec_scales = A.groups % NG == 0 && aligned_to(A.scales, NG * 2 < 8 && !A.scale_f32 ? NG * 2 : 8);
+  A.vec_zeros = A.zeros && A.groups % NG == 0 && aligned_to(A.zeros, NG < 4 ? NG : 4);
   const int tiles16 = A.swiglu ? (A.n_out / 2 + 7) / 8 : (A.n_out + 15) / 16;
   const int active = A.n_expert < A.n_rows ? A.n_expert : A.n_rows;
   // Two row tiles a warp share its x values and loop; one where that would leave blocks without work
@@ -542,7 +520,7 @@ template <typename T, int NG> static deamoe_status_t quant_t(QuantArgs& A, cudaS
   while (A.wk > 1 && (int64_t)((tiles16 + mt - 1) / mt) * (A.wk / 2) / QW * active >= 8 * Q_GRID) A.wk /= 2;
   const int per = QW / A.wk * mt;
   A.tile_groups = (tiles16 + per - 1) / per;
-  auto run = [&](auto kernel, int depth, std::atomic<uint64_t>& done) {
+  auto run = [&](auto kernel, int depth, int step, std::atomic<uint64_t>& done) {
     int dev = 0;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
     if (!(done.load(std::memory_order_acquire) >> dev & 1)) {
@@ -550,18 +528,18 @@ template <typename T, int NG> static deamoe_status_t quant_t(QuantArgs& A, cudaS
       if (e != cudaSuccess) return e;
       done.fetch_or(1ull << dev, std::memory_order_release);
     }
-    const size_t smem = (size_t)QW * depth * mt * 2048 + (size_t)QW * mt * 1024 + (size_t)(A.n_expert + 1) * 4;
+    const size_t smem = (size_t)QW * depth * step + (size_t)QW * mt * 1024 + (size_t)(A.n_expert + 1) * 4;
     const int threads = A.steps * (QCOLS / 8) < 1024 ? A.steps * (QCOLS / 8) : 1024;
     const bool wide = aligned16(A.x) && (A.xs * (int64_t)sizeof(T)) % 16 == 0;
-    k_quant_x<T, PLANES, QCOLS / NG><<<A.n_rows, threads, 0, s>>>(A, wide);
+    k_quant_x<T, PLANES><<<A.n_rows, threads, 0, s>>>(A, wide);
     const cudaError_t e = cudaGetLastError();
     return e != cudaSuccess ? e : launch_pdl(kernel, dim3(Q_GRID), dim3(QW * 32), smem, s, A);
   };
   static std::atomic<uint64_t> done[4];
-  const cudaError_t e = mt == 2 ? (A.zeros ? run(k_quant<T, PLANES, 2, NG, true, 2>, 2, done[0])
-                                           : run(k_quant<T, PLANES, 2, NG, false, 2>, 2, done[1]))
-                                : (A.zeros ? run(k_quant<T, PLANES, 1, NG, true, 4>, 4, done[2])
-                                           : run(k_quant<T, PLANES, 1, NG, false, 4>, 4, done[3]));
+  const cudaError_t e = mt == 2 ? (A.zeros ? run(k_quant<T, PLANES, 2, NG, true, 2>, 2, QuantWarp<PLANES, 2, NG, true, 2>::STEP, done[0])
+                                           : run(k_quant<T, PLANES, 2, NG, false, 2>, 2, QuantWarp<PLANES, 2, NG, false, 2>::STEP, done[1]))
+                                : (A.zeros ? run(k_quant<T, PLANES, 1, NG, true, 4>, 4, QuantWarp<PLANES, 1, NG, true, 4>::STEP, done[2])
+                                           : run(k_quant<T, PLANES, 1, NG, false, 4>, 4, QuantWarp<PLANES, 1, NG, false, 4>::STEP, done[3]));
   if (e == cudaSuccess) return DEAMOE_OK;
   cudaGetLastError();
   return DEAMOE_ERR_CUDA;
@@ -576,9 +554,7 @@ extern "C" {
 uint64_t deamoe_quant_workspace(int32_t dtype, int32_t n_rows, int32_t n_in) {
   if (n_rows <= 0 || n_in <= 0) return 0;
   const uint64_t width = ((uint64_t)n_in + QCOLS - 1) / QCOLS * QCOLS;
-  uint64_t bytes = (uint64_t)n_rows * (width * (dtype == DEAMOE_F32 ? 4 : 2) + 2 * sizeof(int32_t));
-  if (dtype != DEAMOE_F32) bytes += ((uint64_t)n_rows + 32) * (width / 32) * sizeof(float);  // groups of 32 at least
-  return bytes;
+  return (uint64_t)n_rows * (width * (dtype == DEAMOE_F32 ? 4 : 2) + 2 * sizeof(int32_t));
 }
 
 deamoe_status_t deamoe_quant_product(void* cuda_stream, int32_t dtype, const uint8_t* codes, int32_t scale_dtype,
@@ -593,8 +569,6 @@ deamoe_status_t deamoe_quant_product(void* cuda_stream, int32_t dtype, const uin
   if (n_in % 32 != 0 || (swiglu && n_out % 2 != 0) || n_expert > DEAMOE_MAX_EXPERTS || n_in > DEAMOE_MAX_WIDTH ||
       n_out > DEAMOE_MAX_WIDTH)
     return DEAMOE_ERR_UNSUPPORTED;
-  // the kernel holds offsets within a matrix's scales in 32 bits
-  if ((uint64_t)n_out * ((n_in + group - 1) / group) * 4 > UINT32_MAX) return DEAMOE_ERR_UNSUPPORTED;
   if (n_rows < 0 || n_token < 0) return DEAMOE_ERR_BATCH;
   if (n_rows == 0) return DEAMOE_OK;
   const size_t es = type_bytes(dtype);
@@ -617,7 +591,6 @@ deamoe_status_t deamoe_quant_product(void* cuda_stream, int32_t dtype, const uin
   A.xh = reinterpret_cast<__half*>(workspace);
   A.xe = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(workspace) +
                                     (size_t)n_rows * A.steps * QCOLS * (dtype == DEAMOE_F32 ? 4 : 2));
-  A.xg = reinterpret_cast<float*>(A.xe + (size_t)2 * n_rows);
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
   if (dtype == DEAMOE_F32)
     return group == 128 ? quant_t<float, 2>(A, s) : group == 64 ? quant_t<float, 4>(A, s) : quant_t<float, 8>(A, s);
