@@ -168,7 +168,7 @@ constexpr int Q_TOKENS = 16;  // tokens of a pass
 // A block takes a contiguous share of the items; its warps split an item's columns (wk of them a tile of 16 MT rows).
 // Every warp streams its own codes, DEPTH steps of 16 MT rows x 256 columns ahead and across items, into its own part
 // of shared memory; nothing is shared between warps but the sums at an item's end.
-template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
+template <int PLANES, int MT, int NG, bool Z, bool SF, int DEPTH> struct QuantWarp {
   static constexpr int NB = 2 * MT;  // blocks of 8 matrix rows in a warp tile
   // a slot of the ring: codes, then every row's scales of the step (fp32), then its zero points (bytes)
   static constexpr int SCALES = MT * 2048, ZEROS = SCALES + 16 * MT * NG * 4, STEP = (ZEROS + (Z ? 16 * MT * NG : 0) + 127) / 128 * 128;
@@ -189,7 +189,8 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
   // registers: a step's are loaded when its codes are requested and written to its slot at the request after, when
   // they have arrived
   bool held, s_exists;
-  uint32_t held_at, s_raw[NG], z_raw[NG];
+  static constexpr int SW = SF ? NG : NG / 2, ZW = (NG + 3) / 4;  // words of a step's scales (SF: fp32, else bf16) and zero points
+  uint32_t held_at, s_raw[SW], z_raw[ZW];
   size_t s_at;                   // index of the row's scales of the next step
 
   __device__ __forceinline__ QuantWarp(const QuantArgs& a, const int* f, const QuantAt& at, int end, int w, int ln, uint32_t ring)
@@ -223,28 +224,19 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
     s_exists = sb < NB && exists(p_out - g + sr, sb);
     s_at = (row - g + sr + rows_to(sb)) * A.groups + (size_t)c0 * NG;
   }
-  static __device__ __forceinline__ void put_words(uint32_t to, const uint32_t (&v)[NG]) {
-#pragma unroll
-    for (int k = 0; k < NG; k += 2) asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(to + k * 4), "r"(v[k]), "r"(v[k + 1]) : "memory");
-  }
   // what the lane holds, to its slot
   __device__ __forceinline__ void flush() {
     if (!held) return;
-    uint32_t v[NG];
 #pragma unroll
-    for (int k = 0; k < NG; ++k)
-      v[k] = A.scale_f32 ? s_raw[k] : !A.vec_scales ? s_raw[k] << 16 : (k & 1) ? s_raw[k / 2] & 0xffff0000u : s_raw[k / 2] << 16;
-    put_words(held_at + SCALES + lane * NG * 4, v);
-    if constexpr (Z) {
-#pragma unroll
-      for (int k = 0; k < NG; k += 2) {
-        const uint32_t two = !A.vec_zeros ? s_zero(k) | s_zero(k + 1) << 8 : z_raw[k / 4] >> (k & 2) * 8;
-        asm volatile("st.shared.u16 [%0], %1;" ::"r"(held_at + ZEROS + lane * NG + k), "h"((unsigned short)two) : "memory");
-      }
+    for (int k = 0; k < NG; k += 2) {
+      const uint32_t a = SF ? s_raw[k] : s_raw[k / 2] << 16, b = SF ? s_raw[(k + 1) % SW] : s_raw[k / 2] & 0xffff0000u;
+      asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(held_at + SCALES + (lane * NG + k) * 4), "r"(a), "r"(b) : "memory");
+      if constexpr (Z)
+        asm volatile("st.shared.u16 [%0], %1;" ::"r"(held_at + ZEROS + lane * NG + k), "h"((unsigned short)(z_raw[k / 4] >> (k & 2) * 8))
+                     : "memory");
     }
     held = false;
   }
-  __device__ __forceinline__ uint32_t s_zero(int k) const { return z_raw[k] & 255; }
   // the next step's scales and zero points, to be held
   __device__ __forceinline__ void hold(uint32_t slot) {
     held = lane < 16 * MT;
@@ -252,25 +244,30 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
     const bool have = held && s_exists;
     const int groups = have ? min(NG, A.groups - p_c * NG) : 0;  // absent ones count as 0: their codes and x are 0 too
 #pragma unroll
-    for (int k = 0; k < NG; ++k) s_raw[k] = z_raw[k] = 0;
-    const char* s = reinterpret_cast<const char*>(A.scales) + s_at * (A.scale_f32 ? 4 : 2);
+    for (int k = 0; k < SW; ++k) s_raw[k] = 0;
+#pragma unroll
+    for (int k = 0; k < ZW; ++k) z_raw[k] = 0;
+    const char* s = reinterpret_cast<const char*>(A.scales) + s_at * (SF ? 4 : 2);
     if (A.vec_scales) {
       if (have) {
-        constexpr int HALF = NG / 2;  // words of NG bf16 values
-        if (A.scale_f32) {
-#pragma unroll
-          for (int k = 0; k < NG; k += 2) *reinterpret_cast<uint2*>(s_raw + k) = reinterpret_cast<const uint2*>(s)[k / 2];
-        } else if constexpr (HALF == 1) {
+        if constexpr (SW == 1) {
           s_raw[0] = *reinterpret_cast<const uint32_t*>(s);
         } else {
 #pragma unroll
-          for (int k = 0; k < HALF; k += 2) *reinterpret_cast<uint2*>(s_raw + k) = reinterpret_cast<const uint2*>(s)[k / 2];
+          for (int k = 0; k < SW; k += 2) {
+            const uint2 v = reinterpret_cast<const uint2*>(s)[k / 2];
+            s_raw[k] = v.x;
+            s_raw[k + 1] = v.y;
+          }
         }
       }
     } else {
 #pragma unroll
       for (int k = 0; k < NG; ++k)
-        if (k < groups) s_raw[k] = A.scale_f32 ? reinterpret_cast<const uint32_t*>(s)[k] : reinterpret_cast<const unsigned short*>(s)[k];
+        if (k < groups) {
+          if constexpr (SF) s_raw[k] = reinterpret_cast<const uint32_t*>(s)[k];
+          else s_raw[k / 2] |= (uint32_t)reinterpret_cast<const unsigned short*>(s)[k] << (k & 1) * 16;
+        }
     }
     if constexpr (Z) {
       const uint8_t* z = A.zeros + s_at;
@@ -280,13 +277,13 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
             z_raw[0] = *reinterpret_cast<const unsigned short*>(z);
           } else {
 #pragma unroll
-            for (int k = 0; k < NG; k += 4) z_raw[k / 4] = reinterpret_cast<const uint32_t*>(z)[k / 4];
+            for (int k = 0; k < ZW; ++k) z_raw[k] = reinterpret_cast<const uint32_t*>(z)[k];
           }
         }
       } else {
 #pragma unroll
         for (int k = 0; k < NG; ++k)
-          if (k < groups) z_raw[k] = z[k];
+          if (k < groups) z_raw[k / 4] |= (uint32_t)z[k] << (k & 3) * 8;
       }
     }
     s_at += NG;
@@ -326,8 +323,9 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
     const int xw = A.steps * QCOLS;
     // tokens past the last take the last one's values: their sums are not looked at
     const __half* xp[NT];
-    // parts of x ahead: as many as registers allow
-    constexpr int XB = PLANES * NT == 1 ? 4 : 2;
+    // parts of x ahead: it comes from the L2, whose latency a whole step (8 parts) hides (16 tokens' top-8 of 256
+    // experts, 4096 x 7168 each: 310 us, 361 with 4 parts); where registers do not allow that, two
+    constexpr int XB = PLANES * NT == 1 ? 8 : 2;
     uint4 xb[XB][NT][PLANES];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
@@ -335,7 +333,7 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
 #pragma unroll
       for (int p = 0; p < PLANES; ++p)
 #pragma unroll
-        for (int m = 0; m < (XB == 4 ? 4 : 1); ++m) xb[m][t][p] = load_b128(xp[t] + (size_t)p * xw + m * 32);
+        for (int m = 0; m < XB; ++m) xb[m][t][p] = load_b128(xp[t] + (size_t)p * xw + m * 32);
     }
     // the lane's row of the eight matrices an ldmatrix takes: block lane / 8 (MT == 1: block and part)
     const uint32_t lane_at = ring_at + (MT == 2 ? (lane >> 3) : (lane >> 3) & 1) * 1024 + (lane & 7) * 128 +
@@ -371,13 +369,6 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
           request(slot);
           slot = slot + STEP == DEPTH * STEP ? 0 : slot + STEP;
         }
-        if constexpr (XB == 2) {
-          if (m + 1 < QM || more)
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-              for (int p = 0; p < PLANES; ++p) xb[(m + 1) % 2][t][p] = load_b128(xp[t] + (size_t)p * xw + (m + 1) * 32);
-        }
         uint32_t w[NB][4];
 #pragma unroll
         for (int b = 0; b < NB; ++b) widen(code[(m % LM) * NB + b], z[b], w[b]);
@@ -395,9 +386,11 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
                 else if (half == 0) mma_f16(grp[mt][t], lo[0], hi[0], lo[1], hi[1], x.x, x.y);
                 else mma_f16(grp[mt][t], lo[2], hi[2], lo[3], hi[3], x.z, x.w);
               }
-        if constexpr (XB == 4) {
-          if (m + 4 < QM || more) xb[m % 4][0][0] = load_b128(xp[0] + (m + 4) * 32);
-        }
+        if (m + XB < QM || more)
+#pragma unroll
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int p = 0; p < PLANES; ++p) xb[m % XB][t][p] = load_b128(xp[t] + (size_t)p * xw + (m + XB) * 32);
         if ((m + 1) * NG % QM == 0) {  // a group ends
 #pragma unroll
           for (int b = 0; b < NB; ++b)
@@ -416,11 +409,11 @@ template <int PLANES, int MT, int NG, bool Z, int DEPTH> struct QuantWarp {
   }
 };
 
-template <typename T, int PLANES, int MT, int NG, bool Z, int DEPTH>
+template <typename T, int PLANES, int MT, int NG, bool Z, bool SF, int DEPTH>
 __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int warp_sums[QW];
-  using Warp = QuantWarp<PLANES, MT, NG, Z, DEPTH>;
+  using Warp = QuantWarp<PLANES, MT, NG, Z, SF, DEPTH>;
   float4* sums = reinterpret_cast<float4*>(smem + QW * DEPTH * Warp::STEP);  // [2][QW][MT][32]
   int* first = reinterpret_cast<int*>(sums + 2 * QW * MT * 32);            // [n_expert + 1] first item of each expert
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, R = A.n_rows;
@@ -505,9 +498,9 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
   }
 }
 
-template <typename T, int NG> static deamoe_status_t quant_t(QuantArgs& A, cudaStream_t s) {
+template <typename T, int NG, bool SF> static deamoe_status_t quant_t(QuantArgs& A, cudaStream_t s) {
   constexpr int PLANES = sizeof(T) == 4 ? 2 : 1;
-  A.vec_scales = A.groups % NG == 0 && aligned_to(A.scales, NG * 2 < 8 && !A.scale_f32 ? NG * 2 : 8);
+  A.vec_scales = A.groups % NG == 0 && aligned_to(A.scales, NG == 2 && !SF ? 4 : 8);
   A.vec_zeros = A.zeros && A.groups % NG == 0 && aligned_to(A.zeros, NG < 4 ? NG : 4);
   const int tiles16 = A.swiglu ? (A.n_out / 2 + 7) / 8 : (A.n_out + 15) / 16;
   const int active = A.n_expert < A.n_rows ? A.n_expert : A.n_rows;
@@ -536,13 +529,22 @@ template <typename T, int NG> static deamoe_status_t quant_t(QuantArgs& A, cudaS
     return e != cudaSuccess ? e : launch_pdl(kernel, dim3(Q_GRID), dim3(QW * 32), smem, s, A);
   };
   static std::atomic<uint64_t> done[4];
-  const cudaError_t e = mt == 2 ? (A.zeros ? run(k_quant<T, PLANES, 2, NG, true, 2>, 2, QuantWarp<PLANES, 2, NG, true, 2>::STEP, done[0])
-                                           : run(k_quant<T, PLANES, 2, NG, false, 2>, 2, QuantWarp<PLANES, 2, NG, false, 2>::STEP, done[1]))
-                                : (A.zeros ? run(k_quant<T, PLANES, 1, NG, true, 4>, 4, QuantWarp<PLANES, 1, NG, true, 4>::STEP, done[2])
-                                           : run(k_quant<T, PLANES, 1, NG, false, 4>, 4, QuantWarp<PLANES, 1, NG, false, 4>::STEP, done[3]));
+  cudaError_t e;
+  if (mt == 2)
+    e = A.zeros ? run(k_quant<T, PLANES, 2, NG, true, SF, 2>, 2, QuantWarp<PLANES, 2, NG, true, SF, 2>::STEP, done[0])
+                : run(k_quant<T, PLANES, 2, NG, false, SF, 2>, 2, QuantWarp<PLANES, 2, NG, false, SF, 2>::STEP, done[1]);
+  else
+    e = A.zeros ? run(k_quant<T, PLANES, 1, NG, true, SF, 4>, 4, QuantWarp<PLANES, 1, NG, true, SF, 4>::STEP, done[2])
+                : run(k_quant<T, PLANES, 1, NG, false, SF, 4>, 4, QuantWarp<PLANES, 1, NG, false, SF, 4>::STEP, done[3]);
   if (e == cudaSuccess) return DEAMOE_OK;
   cudaGetLastError();
   return DEAMOE_ERR_CUDA;
+}
+
+template <typename T> static deamoe_status_t quant_group(QuantArgs& A, int group, cudaStream_t s) {
+  if (A.scale_f32)
+    return group == 128 ? quant_t<T, 2, true>(A, s) : group == 64 ? quant_t<T, 4, true>(A, s) : quant_t<T, 8, true>(A, s);
+  return group == 128 ? quant_t<T, 2, false>(A, s) : group == 64 ? quant_t<T, 4, false>(A, s) : quant_t<T, 8, false>(A, s);
 }
 
 }  // namespace deamoe
@@ -592,10 +594,8 @@ deamoe_status_t deamoe_quant_product(void* cuda_stream, int32_t dtype, const uin
   A.xe = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(workspace) +
                                     (size_t)n_rows * A.steps * QCOLS * (dtype == DEAMOE_F32 ? 4 : 2));
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
-  if (dtype == DEAMOE_F32)
-    return group == 128 ? quant_t<float, 2>(A, s) : group == 64 ? quant_t<float, 4>(A, s) : quant_t<float, 8>(A, s);
-  return group == 128 ? quant_t<__nv_bfloat16, 2>(A, s)
-                      : group == 64 ? quant_t<__nv_bfloat16, 4>(A, s) : quant_t<__nv_bfloat16, 8>(A, s);
+  if (dtype == DEAMOE_F32) return quant_group<float>(A, group, s);
+  return quant_group<__nv_bfloat16>(A, group, s);
 }
 
 }  // extern "C"
