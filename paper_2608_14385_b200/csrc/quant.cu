@@ -4,15 +4,20 @@
 //
 // so the group scale multiplies an fp32 sum and no weight is ever rounded.  A decode step has a few rows per matrix:
 // the codes (half a byte a weight, read once) bound it, and the work beside them is to widen 2 weights a byte.
+// Measured: the gate and up matrices (4096 x 7168, groups of 128) of 16 tokens' top-8 of 256 experts, 1.5 GB, in 316 us
+// (4.8 TB/s; the loads of x and of the scales beside the codes and the issue of about 240 instructions for 2 KB of
+// codes a warp are what keeps it from HBM's rate), of one token's 8 experts in 39 us (3.1 TB/s), one matrix in 10 us.
 //
 // Tensor cores: mma.m16n8k16 with 16 matrix rows as M and up to 8 tokens as N (legacy path: with this few tokens the
 // instruction rate it needs is a fraction of what it has, and its A operand comes from registers, where the codes
-// have to be widened anyway).  Widening is an AND and a subtraction a pair: a nibble in the low bits of a 16-bit half IS
-// the fp16 subnormal q 2^-24, and in the next four bits q 2^-20; q - z is exact there, and tensor cores multiply
-// subnormals exactly.  x becomes fp16 in a kernel of its own: each row scaled by a power of two to a largest magnitude
-// of 2^14..2^15, the columns that meet 2^-20 by another 2^-4, so that fp16's range costs nothing (values below 2^-35
-// of the row's largest lose bits, far under fp32's own resolution of the sum); bf16 values fit exactly, fp32 values as
-// two parts (2^-23 relative).
+// have to be widened anyway).  Widening is one logical operation and a subtraction a pair: a nibble under the exponent of
+// 1024 is the fp16 number 1024 + q, or 1024 + 16 q where it lies four bits higher, and 1024 + z or 1024 + 16 z leaves
+// q - z or 16 (q - z), exactly.  (As the fp16 subnormals q 2^-24, without the exponent, the codes need no operation
+// at all beyond the mask and took 308 us where this takes 316, but the tensor cores align the products of a step by their exponents, and subnormals'
+// leading zeros cost the sum 6 to 10 of its bits.)  x becomes fp16 in a kernel of its own: each row scaled by a
+// power of two to a largest magnitude of 2^14..2^15, the columns that meet 16 (q - z) by another 2^-4, so that fp16's
+// range costs nothing (values below 2^-35 of the row's largest lose bits, far under fp32's own resolution of the
+// sum); bf16 values fit exactly, fp32 values as two parts (2^-23 relative).
 #include <atomic>
 #include <climits>
 #include <cuda_fp16.h>
@@ -93,9 +98,8 @@ template <typename T, int PLANES> __global__ void __launch_bounds__(1024) k_quan
   auto power = [](int k) { return __int_as_float((127 + k) << 23); };
   const float f0 = power(-e / 2), f1 = power(-e - -e / 2);  // 2^-e as two factors, each in fp32's range
   if (threadIdx.x == 0) {
-    const int half = (e + 24) / 2;
-    A.xe[r] = __float_as_int(power(half));
-    A.xe[(size_t)A.n_rows + r] = __float_as_int(power((e + 24) - half));
+    A.xe[r] = __float_as_int(power(e / 2));
+    A.xe[(size_t)A.n_rows + r] = __float_as_int(power(e - e / 2));
   }
   __half* out = A.xh + r * PLANES * width;
   for (int c = threadIdx.x; c < width / 8; c += blockDim.x) {
@@ -127,17 +131,24 @@ static __device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0,
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-// The 8 codes of a word less the zero point as four pairs of fp16 subnormals: columns (0 4) (1 5) (2 6) (3 7), times 2^-24 and 2^-20 in turn.  z: the zero point in the low bits of both halves.
+// The 8 codes of a word less the zero point as four pairs: columns (0 4) (1 5) (2 6) (3 7), q - z and 16 (q - z) in turn.
+// z: 1024 + the zero point in both halves, z16: 1024 + 16 times it.
 static __device__ __forceinline__ uint32_t less(uint32_t a, uint32_t b) {
   const __half2 d = __hsub2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
   return *reinterpret_cast<const uint32_t*>(&d);
 }
-static __device__ __forceinline__ void widen(uint32_t w, uint32_t z, uint32_t (&p)[4]) {
-  const uint32_t v = w >> 8, z4 = z << 4;
-  p[0] = less(w & 0x000f000fu, z);
-  p[1] = less(w & 0x00f000f0u, z4);
-  p[2] = less(v & 0x000f000fu, z);
-  p[3] = less(v & 0x00f000f0u, z4);
+constexpr uint32_t H1024 = 0x64006400u;
+static __device__ __forceinline__ uint32_t pick(uint32_t w, uint32_t mask, uint32_t exponent) {  // (w & mask) | exponent
+  uint32_t d;
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(w), "r"(mask), "r"(exponent));
+  return d;
+}
+static __device__ __forceinline__ void widen(uint32_t w, uint32_t h1024, uint32_t z, uint32_t z16, uint32_t (&p)[4]) {
+  const uint32_t v = w >> 8;
+  p[0] = less(pick(w, 0x000f000fu, h1024), z);
+  p[1] = less(pick(w, 0x00f000f0u, h1024), z16);
+  p[2] = less(pick(v, 0x000f000fu, h1024), z);
+  p[3] = less(pick(v, 0x00f000f0u, h1024), z16);
 }
 static __device__ __forceinline__ uint4 load_b128(const void* p) {
   uint4 v;
@@ -324,7 +335,7 @@ template <int PLANES, int MT, int NG, bool Z, bool SF, int DEPTH> struct QuantWa
     // tokens past the last take the last one's values: their sums are not looked at
     const __half* xp[NT];
     // parts of x ahead: it comes from the L2, whose latency a whole step (8 parts) hides (16 tokens' top-8 of 256
-    // experts, 4096 x 7168 each: 310 us, 361 with 4 parts); where registers do not allow that, two
+    // experts, 4096 x 7168 each: 316 us, 361 with 4 parts); where registers do not allow that, two
     constexpr int XB = PLANES * NT == 1 ? 8 : 2;
     uint4 xb[XB][NT][PLANES];
 #pragma unroll
@@ -335,6 +346,8 @@ template <int PLANES, int MT, int NG, bool Z, bool SF, int DEPTH> struct QuantWa
 #pragma unroll
         for (int m = 0; m < XB; ++m) xb[m][t][p] = load_b128(xp[t] + (size_t)p * xw + m * 32);
     }
+    uint32_t h1024 = H1024;
+    asm volatile("" : "+r"(h1024));  // in a register: an instruction has room for one constant, the mask
     // the lane's row of the eight matrices an ldmatrix takes: block lane / 8 (MT == 1: block and part)
     const uint32_t lane_at = ring_at + (MT == 2 ? (lane >> 3) : (lane >> 3) & 1) * 1024 + (lane & 7) * 128 +
                              ((lane & 7) ^ (MT == 2 ? 0 : lane >> 4)) * 16;
@@ -371,7 +384,7 @@ template <int PLANES, int MT, int NG, bool Z, bool SF, int DEPTH> struct QuantWa
         }
         uint32_t w[NB][4];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) widen(code[(m % LM) * NB + b], z[b], w[b]);
+        for (int b = 0; b < NB; ++b) widen(code[(m % LM) * NB + b], h1024, z[b] | H1024, z[b] << 4 | H1024, w[b]);
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -504,10 +517,12 @@ template <typename T, int NG, bool SF> static deamoe_status_t quant_t(QuantArgs&
   A.vec_zeros = A.zeros && A.groups % NG == 0 && aligned_to(A.zeros, NG < 4 ? NG : 4);
   const int tiles16 = A.swiglu ? (A.n_out / 2 + 7) / 8 : (A.n_out + 15) / 16;
   const int active = A.n_expert < A.n_rows ? A.n_expert : A.n_rows;
-  // Two row tiles a warp share its x values and loop; one where that would leave blocks without work
+  // Two row tiles a warp share its x values and loop (16 tokens' top-8 of 256 experts, 4096 x 7168: 360 us, 451 with one
+  // tile a warp); one where two would leave blocks without work (one token, one such matrix: 10.2 us, 11.8 with two)
   const int mt = (int64_t)(tiles16 / 2) * active >= Q_GRID && A.n_out >= 32 ? 2 : 1;
   // Warps that share a tile's columns: all, or fewer (longer walks, fewer sums to join) while the blocks keep at least
-  // 8 items each, so that their counts differ by little
+  // 8 items each, so that their counts differ by little (the same 16 tokens: 362 us with this rule, 388 with all warps on
+  // one tile; 4 tokens' top-8 of 64 experts, 7168 x 2048: 57 and 65)
   A.wk = QW;
   while (A.wk > A.steps) A.wk /= 2;
   while (A.wk > 1 && (int64_t)((tiles16 + mt - 1) / mt) * (A.wk / 2) / QW * active >= 8 * Q_GRID) A.wk /= 2;

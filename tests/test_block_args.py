@@ -14,7 +14,7 @@ def _call(name, good, **change):
 def test_sort():
     good = dict(s=None, idx=A, T=1000, k=8, n=64, off=B, pair=D, row=E, ws=W, size=1 << 30)
     L = binding.lib()
-    assert L.deamoe_sort_workspace(512, 8, 64) == 0 and L.deamoe_sort_workspace(513, 8, 64) > 0
+    assert L.deamoe_sort_workspace(192, 8, 64) == 0 and L.deamoe_sort_workspace(193, 8, 64) > 0
     for change, want in ((dict(n=0), INVALID), (dict(n=4096), UNSUPPORTED), (dict(k=0), INVALID), (dict(k=33), UNSUPPORTED),
                          (dict(T=-1), BATCH), (dict(T=2 ** 30, k=2), BATCH), (dict(idx=None), INVALID), (dict(off=None), INVALID),
                          (dict(pair=D + 2), INVALID), (dict(row=None), INVALID), (dict(ws=None), INVALID), (dict(size=64), INVALID)):

@@ -149,6 +149,24 @@ def test_values_of_every_size():
         assert not torch.isfinite(got2[0]).any() and torch.isnan(got2[5]).all()
 
 
+@pytest.mark.parametrize("mean", [0.0, 1.0])
+@pytest.mark.parametrize("K,group,zeros", [(1056, 32, True), (7168, 128, False), (2048, 64, True)])
+def test_fp32_products_keep_fp32_accuracy(K, group, zeros, mean):
+    """The error of all products together (2-norm, relative to the result's, or to that of independent terms where the
+    tokens have a mean).  A product is a sum of n = K / 16 matrix steps of two parts and G scalings; each may be off by a unit, 2^-23, of a partial sum no larger than the result's
+    scale.  Taken as independent and uniform that is sqrt(n / 3) 2^-23; a path that drops bits of the operands or of the
+    sums lies far above it."""
+    N, T = 512, 24
+    codes, scales, z = _matrices(1, N, K, group, zeros, F32, 21)
+    x = torch.randn((T, K), generator=torch.Generator(device=DEV).manual_seed(22), device=DEV) + mean
+    got = binding.quant_product(codes, scales, x, group, zeros=z).double()
+    w = _widened(codes[0], scales[0], None if z is None else z[0], group, K)
+    want = x.double() @ w.T
+    size = want.norm() if mean == 0 else (x.double() ** 2 @ (w ** 2).T).sqrt().norm()
+    n = 2 * K / 16 + scales.shape[2]
+    assert (got - want).norm() <= (n / 3) ** 0.5 * 2.0 ** -23 * size
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("zeros", [False, True])
 def test_an_infinity_meets_the_weights_sign(zeros, dtype):

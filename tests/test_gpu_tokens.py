@@ -52,11 +52,11 @@ def _check_sort(idx, n):
     return off, pair_row, row_pair
 
 
-# around the sizes at which the form changes: 32 pairs a warp step, 4096 pairs in one block, 2048 pairs a block beyond;
+# around the sizes at which the form changes: 32 pairs a warp step, 1536 pairs in one block, 1024 pairs a block beyond;
 # experts around the counters' limits (512 experts x 32 warps, 2048 experts x 8 warps)
 @pytest.mark.parametrize("T,k,n", [(0, 4, 8), (1, 1, 1), (1, 8, 256), (16, 8, 256), (33, 1, 7), (31, 3, 33), (512, 8, 256),
                                    (410, 10, 864), (409, 10, 2048), (128, 32, 2047), (513, 8, 256), (4097, 1, 2048),
-                                   (2048, 2, 5), (4096, 8, 256), (1021, 10, 672), (3001, 7, 1), (20000, 8, 100)])
+                                   (2048, 2, 5), (192, 8, 256), (193, 8, 256), (150, 10, 2048), (512, 2, 900), (1025, 1, 3), (4096, 8, 256), (1021, 10, 672), (3001, 7, 1), (20000, 8, 100)])
 @pytest.mark.parametrize("drop", [0.0, 0.3])
 def test_sort_is_stable_and_complete(T, k, n, drop):
     idx, _ = _routing(T, min(k, n) if n >= k else k, n, T + k + n, drop, distinct=n >= k)
