@@ -229,6 +229,12 @@ def _type(t, where, name):
     return code
 
 
+def _pairs(pair_row, where):
+    if pair_row.dim() != 2:
+        _refuse(where, f"pair_row must be [T, k], got {list(pair_row.shape)}")
+    return pair_row.shape
+
+
 def _workspace(nbytes, device):
     """Scratch of one call: from torch's allocator on the current stream (a captured graph's own pool while capturing),
     so no two calls share it unless the stream orders them."""
@@ -267,7 +273,7 @@ def dispatch(x, pair_row, rows=None):
     where, dev = "deamoe_dispatch", _device()
     dt = _type(x, where, "x")
     T, h = x.shape
-    k = pair_row.shape[-1]
+    k = _pairs(pair_row, where)[1]
     if rows is None:
         rows = x.new_empty((T * k, h))
     n = rows.shape[0]
@@ -283,7 +289,7 @@ def dispatch_backward(drows, pair_row, dx=None):
     where, dev = "deamoe_dispatch_backward", _device()
     dt = _type(drows, where, "drows")
     n, h = drows.shape
-    T, k = pair_row.shape
+    T, k = _pairs(pair_row, where)
     if dx is None:
         dx = drows.new_empty((T, h))
     pd, sd = _mat(drows, where, "drows", drows.dtype, n, h, dev)
@@ -298,7 +304,7 @@ def combine(rows, pair_row, topk_w, out=None):
     where, dev = "deamoe_combine", _device()
     dt = _type(rows, where, "rows")
     n, h = rows.shape
-    T, k = pair_row.shape
+    T, k = _pairs(pair_row, where)
     if out is None:
         out = rows.new_empty((T, h))
     pr, sr = _mat(rows, where, "rows", rows.dtype, n, h, dev)
@@ -315,7 +321,9 @@ def combine_backward(dout, rows, pair_row, topk_w, drows=None, dw=None):
     where, dev = "deamoe_combine_backward", _device()
     dt = _type(dout, where, "dout")
     T, h = dout.shape
-    k = pair_row.shape[-1]
+    k = _pairs(pair_row, where)[1]
+    if rows.dim() != 2:
+        _refuse(where, f"rows must be a matrix, got {list(rows.shape)}")
     n = rows.shape[0]
     if drows is None:
         drows = dout.new_empty((n, h))

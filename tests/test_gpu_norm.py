@@ -239,3 +239,18 @@ def test_wrapper_refuses_what_does_not_fit():
     for call in bad:
         with pytest.raises(binding.DeaMoEError):
             call()
+
+
+def test_rows_beyond_32_bit_offsets():
+    """Over 2^31 values: the last rows of the norm and of its gradient."""
+    T, h = 300032, 7168
+    assert T * h > 2 ** 31
+    x = torch.empty((T, h), dtype=BF16, device=DEV)
+    x[:-40] = 1
+    x[-40:] = _gauss((40, h), BF16, 1)
+    w = _gauss((h,), BF16, 2, 0.3, 1.0)
+    X, W = Bounded(x[-40:]), Bounded(w)
+    r = _inv(X, 1e-6)
+    (X * r * W).within(binding.norm(x, w, 1e-6)[-40:], "norm")
+    dx, _ = binding.norm_backward(x, w, 1e-6, x)
+    _unit_grad(X, r, X * W).within(dx[-40:], "dx")

@@ -71,7 +71,7 @@ def _routed(T, k, E, seed, skew=False):
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("group,zeros,sdtype", [(32, True, BF16), (64, False, F32), (128, True, F32), (128, False, BF16)])
 @pytest.mark.parametrize("T,N,K", [(1, 1, 32), (1, 16, 128), (1, 4096, 7168), (2, 17, 96), (3, 100, 1056), (7, 33, 160),
-                                   (8, 48, 224), (9, 1003, 2048), (20, 66, 608), (33, 130, 1408), (70, 24, 384)])
+                                   (8, 48, 224), (9, 1003, 2048), (20, 66, 608), (33, 130, 1408), (70, 24, 384), (2, 40, 9248)])
 def test_one_matrix(T, N, K, group, zeros, sdtype, dtype):
     codes, scales, z = _matrices(1, N, K, group, zeros, sdtype, T + N)
     x = torch.randn((T, K), generator=torch.Generator(device=DEV).manual_seed(K), device=DEV).to(dtype)
@@ -258,3 +258,19 @@ def test_wrapper_refuses_what_does_not_fit():
     for call in bad:
         with pytest.raises(binding.DeaMoEError):
             call()
+
+
+def test_matrices_beyond_32_bit_offsets():
+    """5 GB of codes: the products of the last experts against their definition."""
+    E, N, K, group, T = 288, 4096, 8704, 128, 3
+    codes = torch.empty((E, N, K // 2), dtype=torch.uint8, device=DEV)
+    for e in range(E):
+        codes[e].random_(0, 256, generator=torch.Generator(device=DEV).manual_seed(e))
+    assert codes.numel() > 2 ** 32
+    scales = torch.rand((E, N, K // group), generator=torch.Generator(device=DEV).manual_seed(1), device=DEV).mul_(0.01).to(BF16)
+    x = torch.randn((T, K), generator=torch.Generator(device=DEV).manual_seed(2), device=DEV).to(BF16)
+    off = torch.zeros(E + 1, dtype=torch.int32, device=DEV)
+    off[E - 1] = 1
+    off[E] = T
+    got = binding.quant_product(codes, scales, x, group, expert_off=off)
+    _check(got, *_want(codes, scales, None, group, x, [E - 2, E - 1, E - 1], [0, 1, 2], False))

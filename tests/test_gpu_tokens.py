@@ -234,7 +234,26 @@ def test_wrapper_refuses_what_does_not_fit():
            lambda: binding.dispatch(x.t(), pair_row), lambda: binding.dispatch(x, pair_row, rows=x.float()),
            lambda: binding.combine(x, pair_row, w.double()), lambda: binding.combine(x, pair_row, w[:, :1]),
            lambda: binding.combine_backward(x, x.float(), pair_row, w),
-           lambda: binding.dispatch(x[:, :1].expand(4, 64), pair_row)]
+           lambda: binding.dispatch(x[:, :1].expand(4, 64), pair_row), lambda: binding.combine(x, pair_row.reshape(-1), w),
+           lambda: binding.dispatch(x, pair_row.reshape(-1)), lambda: binding.combine_backward(x, x[0], pair_row, w)]
     for call in bad:
         with pytest.raises(binding.DeaMoEError):
             call()
+
+
+def test_rows_beyond_32_bit_offsets():
+    """Over 2^31 values of rows: the last tokens' rows out, back, and in the gradients."""
+    T, k, n, h = 40000, 8, 64, 7168
+    idx, w = _routing(T, k, n, 1)
+    _, pair_row, row_pair = binding.sort_pairs(idx, n)
+    assert T * k * h > 2 ** 31
+    x = torch.randn((T, h), generator=_gen(2), device=DEV).to(torch.bfloat16)
+    rows = binding.dispatch(x, pair_row)
+    tail = slice(T * k - 100, T * k)
+    assert torch.equal(rows[tail], x[row_pair[tail].long() // k])
+    last = pair_row[-50:].long()
+    ones = torch.ones_like(w)
+    Bounded(x[-50:, None].double().expand(50, k, h)).sum(1).within(binding.combine(rows, pair_row, ones)[-50:], "out")
+    drows, dw = binding.combine_backward(x, rows, pair_row, w)
+    (Bounded(x[row_pair[tail].long() // k]) * Bounded(w.reshape(-1)[row_pair[tail].long()][:, None])).within(drows[tail], "drows")
+    (Bounded(x[-50:, None].double().expand(50, k, h)) * Bounded(rows[last].double())).sum(2).within(dw[-50:], "dw")
