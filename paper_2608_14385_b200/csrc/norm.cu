@@ -15,9 +15,8 @@
 // Every operator is one pass of HBM traffic over [T, h] rows: bytes bound the forward calls (8192 x 7168 bf16: norm 39 us,
 // norm_residual with a channel gate and the next norm 83 us, 5.9 and 5.7 TB/s) and, with the instruction issue of a
 // row's work, the backward calls (norm_backward 68 us, 84 with dadd; norm_residual_backward 175 us: 5.2, 5.6 and 4.0
-// TB/s).  Sums over the tokens
-// (dw, dwn, a per-channel dgate) are kept per thread block and added by a second kernel in block order: no atomics,
-// equal calls give equal bits.
+// TB/s).  Sums over the tokens (dw, dwn, a per-channel dgate) are kept per thread block and added by a second kernel
+// in block order: no atomics, equal calls give equal bits.
 #include <atomic>
 
 #include "row.cuh"

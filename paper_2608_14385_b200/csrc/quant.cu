@@ -10,14 +10,14 @@
 //
 // Tensor cores: mma.m16n8k16 with 16 matrix rows as M and up to 8 tokens as N (legacy path: with this few tokens the
 // instruction rate it needs is a fraction of what it has, and its A operand comes from registers, where the codes
-// have to be widened anyway).  Widening is one logical operation and a subtraction a pair: a nibble under the exponent of
-// 1024 is the fp16 number 1024 + q, or 1024 + 16 q where it lies four bits higher, and 1024 + z or 1024 + 16 z leaves
-// q - z or 16 (q - z), exactly.  (As the fp16 subnormals q 2^-24, without the exponent, the codes need no operation
-// at all beyond the mask and took 308 us where this takes 316, but the tensor cores align the products of a step by their exponents, and subnormals'
-// leading zeros cost the sum 6 to 10 of its bits.)  x becomes fp16 in a kernel of its own: each row scaled by a
-// power of two to a largest magnitude of 2^14..2^15, the columns that meet 16 (q - z) by another 2^-4, so that fp16's
-// range costs nothing (values below 2^-35 of the row's largest lose bits, far under fp32's own resolution of the
-// sum); bf16 values fit exactly, fp32 values as two parts (2^-23 relative).
+// have to be widened anyway).  Widening is one logical operation and a subtraction a pair: a nibble under the exponent
+// of 1024 is the fp16 number 1024 + q, or 1024 + 16 q where it lies four bits higher, and 1024 + z or 1024 + 16 z
+// leaves q - z or 16 (q - z), exactly.  (As the fp16 subnormals q 2^-24, without the exponent, the masked codes took 308
+// us where this takes 316, but the tensor cores align the products of a step by their exponents, and subnormals'
+// leading zeros cost the sum 6 to 10 of its bits.)  x becomes fp16 in a kernel of its own: each row scaled by a power of
+// two to a largest magnitude of 2^14..2^15, the columns that meet 16 (q - z) by another 2^-4, so that fp16's range
+// costs nothing (values below 2^-35 of the row's largest lose bits, far under fp32's own resolution of the sum); bf16
+// values fit exactly, fp32 values as two parts (2^-23 relative).
 #include <atomic>
 #include <climits>
 #include <cuda_fp16.h>
@@ -49,8 +49,7 @@ struct QuantArgs {
   int32_t* xe;      // [2][n_rows] two powers of two (fp32 bits) that undo the row's scaling
 };
 
-// x in the order of the rows, as fp16 scaled by 2^-e, 8 columns in the order 0 4 1 5 2 6 3 7 (the order in which the
-// codes of a 32-bit word are widened; 1 5 3 7 by another 1/16).  One block a row; a row without a source is zero.
+// eight values of a row from column col on, 0 past its end
 template <typename T> static __device__ __forceinline__ void eight_of(const T* x, int col, int n_in, bool wide, float (&v)[8]) {
   constexpr int VE = 16 / sizeof(T);
   if (wide && col + 8 <= n_in) {
@@ -66,6 +65,8 @@ template <typename T> static __device__ __forceinline__ void eight_of(const T* x
     for (int i = 0; i < 8; ++i) v[i] = col + i < n_in ? to_f<T>(x[col + i]) : 0.f;
   }
 }
+// x in the order of the rows, as fp16 scaled by 2^-e, 8 columns in the order 0 4 1 5 2 6 3 7 (the order in which the
+// codes of a 32-bit word are widened; 1 5 3 7 by another 1/16).  One block a row; a row without a source is zero.
 template <typename T, int PLANES> __global__ void __launch_bounds__(1024) k_quant_x(QuantArgs A, bool wide) {
   __shared__ float buf[32];
   const int64_t r = blockIdx.x;
