@@ -235,10 +235,14 @@ def _pairs(pair_row, where):
     return pair_row.shape
 
 
-def _workspace(nbytes, device):
+def _workspace(nbytes, like):
     """Scratch of one call: from torch's allocator on the current stream (a captured graph's own pool while capturing),
     so no two calls share it unless the stream orders them."""
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    return like.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+
+
+def _ptr(t):
+    return t.data_ptr() if t is not None else None
 
 
 def _done(status, where):
@@ -261,9 +265,9 @@ def sort_pairs(topk_idx, n_expert):
     row_pair = topk_idx.new_empty(T * k)
     L = lib()
     need = L.deamoe_sort_workspace(T, k, n)
-    ws = _workspace(need, topk_idx.device)
+    ws = _workspace(need, topk_idx)
     _done(L.deamoe_sort_pairs(_raw_stream(dev), src, T, k, n, off.data_ptr(), pair_row.data_ptr(), row_pair.data_ptr(),
-                              _dptr(ws), need), where)
+                              _ptr(ws), need), where)
     return off, pair_row, row_pair
 
 
@@ -328,7 +332,7 @@ def combine_backward(dout, rows, pair_row, topk_w, drows=None, dw=None):
     if drows is None:
         drows = dout.new_empty((n, h))
     if dw is None:
-        dw = torch.empty((T, k), dtype=torch.float32, device=dout.device)
+        dw = dout.new_empty((T, k), dtype=torch.float32)
     pd, sd = _mat(dout, where, "dout", dout.dtype, T, h, dev)
     pr, sr = _mat(rows, where, "rows", dout.dtype, n, h, dev)
     pg, sg = _mat(drows, where, "drows", dout.dtype, n, h, dev)
@@ -371,7 +375,7 @@ def norm_backward(x, weight, eps, du, dadd=None, dx=None):
     T, h = x.shape
     if dx is None:
         dx = torch.empty_like(x)
-    dw = torch.empty(h, dtype=torch.float32, device=x.device)
+    dw = x.new_empty(h, dtype=torch.float32)
     px, sx = _mat(x, where, "x", x.dtype, T, h, dev)
     pu, su = _mat(du, where, "du", x.dtype, T, h, dev)
     pa, sa = _mat(dadd, where, "dadd", x.dtype, T, h, dev) if dadd is not None else (None, 0)
@@ -379,8 +383,8 @@ def norm_backward(x, weight, eps, du, dadd=None, dx=None):
     pw, wdt = _gain(weight, where, "weight", h, dev)
     L = lib()
     need = L.deamoe_norm_workspace(T, h)
-    ws = _workspace(need, x.device)
-    _done(L.deamoe_norm_backward(_raw_stream(dev), dt, px, sx, T, h, wdt, pw, eps, pu, su, pa, sa, pd, sd, dw.data_ptr(), _dptr(ws),
+    ws = _workspace(need, x)
+    _done(L.deamoe_norm_backward(_raw_stream(dev), dt, px, sx, T, h, wdt, pw, eps, pu, su, pa, sa, pd, sd, dw.data_ptr(), _ptr(ws),
                                  need), where)
     return dx, dw
 
@@ -452,22 +456,22 @@ def norm_residual_backward(x, y, weight, eps, dout, gate=None, residual_scale=1.
     dgate, sdg = None, 0
     channel = kind == GATE_CHANNEL
     n = (weight is not None) + (next_weight is not None) + channel
-    sums = list(torch.empty((n, h), dtype=torch.float32, device=x.device).unbind(0)) if n else []
+    sums = list(x.new_empty((n, h), dtype=torch.float32).unbind(0)) if n else []
     dw = sums.pop() if weight is not None else None
     dn = sums.pop() if next_weight is not None else None
     if channel:
         dgate = sums.pop()
     elif kind == GATE_TOKEN:
-        dgate = torch.empty(T, dtype=torch.float32, device=x.device)
+        dgate = x.new_empty(T, dtype=torch.float32)
     elif kind == GATE_FULL:
         dgate, sdg = x.new_empty((T, h)), h
     L = lib()
     need = L.deamoe_norm_workspace(T, h)
-    ws = _workspace(need, x.device)
+    ws = _workspace(need, x)
     _done(L.deamoe_norm_residual_backward(_raw_stream(dev), dt, px, sx, py, sy, T, h, 1 if normalise else 0, wdt, pw, eps, kind, pg,
                                           sg, residual_scale, branch_scale, po, so, pm,
-                                          eps if next_eps is None else next_eps, pu, su, pdx, sdx, pdy, sdy, _dptr(dgate),
-                                          sdg, _dptr(dw), _dptr(dn), _dptr(ws), need), where)
+                                          eps if next_eps is None else next_eps, pu, su, pdx, sdx, pdy, sdy, _ptr(dgate),
+                                          sdg, _ptr(dw), _ptr(dn), _ptr(ws), need), where)
     return dx, dy, dgate, dw, dn
 
 
@@ -498,10 +502,10 @@ def quant_product(codes, scales, x, group, zeros=None, expert_off=None, row_pair
     pp = _vec(row_pair, where, "row_pair", torch.int32, (R,), dev) if row_pair is not None else None
     L = lib()
     need = L.deamoe_quant_workspace(dt, R, n_in)
-    ws = _workspace(need, x.device)
+    ws = _workspace(need, x)
     _done(L.deamoe_quant_product(_raw_stream(dev), dt, _vec(codes, where, "codes", torch.uint8, (E, n_out, n_in // 2), dev), sdt,
                                  _vec(scales, where, "scales", scales.dtype, (E, n_out, groups), dev), pz, E, n_out, n_in, group, px,
-                                 sx, T, pe, pp, pairs_per_token, R, 1 if swiglu else 0, po, so, _dptr(ws), need), where)
+                                 sx, T, pe, pp, pairs_per_token, R, 1 if swiglu else 0, po, so, _ptr(ws), need), where)
     return out
 
 

@@ -67,7 +67,7 @@ def _routed(T, k, E, seed, skew=False):
     return off, row_pair, experts, [p // k for p in row_pair.tolist()]
 
 
-# one and several rows, around 8-row passes; widths around 16-row tiles; columns around 128-column steps and short groups
+# one and several rows, around 8-row passes; widths around 16-row tiles; columns around 256-column steps and short groups
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("group,zeros,sdtype", [(32, True, BF16), (64, False, F32), (128, True, F32), (128, False, BF16)])
 @pytest.mark.parametrize("T,N,K", [(1, 1, 32), (1, 16, 128), (1, 4096, 7168), (2, 17, 96), (3, 100, 1056), (7, 33, 160),
