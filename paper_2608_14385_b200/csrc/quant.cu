@@ -441,7 +441,10 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
   block_exclusive_scan(first, A.n_expert, warp_sums);
   const int total = first[A.n_expert];
   const int i0 = (int)((int64_t)total * blockIdx.x / gridDim.x), i1 = (int)((int64_t)total * (blockIdx.x + 1) / gridDim.x);
-  if (i0 == i1) return;
+  if (i0 == i1) {  // no share; the grid must not end before the kernel that it was launched beside, even if nobody has one
+    pdl_wait();
+    return;
+  }
   const int tiles_per = QW / A.wk;
   QuantAt at;
   {

@@ -274,3 +274,33 @@ def test_matrices_beyond_32_bit_offsets():
     off[E] = T
     got = binding.quant_product(codes, scales, x, group, expert_off=off)
     _check(got, *_want(codes, scales, None, group, x, [E - 2, E - 1, E - 1], [0, 1, 2], False))
+
+
+@pytest.mark.parametrize("captured", [False, True])
+def test_product_without_rows_is_over_when_its_call_is(captured):
+    """No expert has a row: the workspace is the caller's again, and stays what the next kernel of the stream makes it."""
+    E, N, K, group, T = 4, 64, 16384, 32, 4096
+    codes, scales, _ = _matrices(E, N, K, group, False, F32, 31)
+    x = torch.randn((T, K), generator=torch.Generator(device=DEV).manual_seed(32), device=DEV)
+    off = torch.zeros(E + 1, dtype=torch.int32, device=DEV)
+    out = torch.full((T, N), 7.0, device=DEV)
+    L, p = binding.lib(), binding._dptr
+    need = L.deamoe_quant_workspace(binding.F32, T, K)
+    workspace = torch.empty(need, dtype=torch.uint8, device=DEV)
+
+    def step():
+        assert L.deamoe_quant_product(binding._stream(), binding.F32, p(codes), binding.F32, p(scales), None, E, N, K, group, p(x), K,
+                                      T, p(off), None, 1, T, 0, p(out), N, p(workspace), need) == binding.OK
+        workspace.fill_(0xa5)
+
+    step()
+    torch.cuda.synchronize()
+    if captured:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+    for _ in range(20):
+        workspace.zero_()
+        graph.replay() if captured else step()
+        torch.cuda.synchronize()
+        assert (workspace == 0xa5).all() and (out == 7).all()
