@@ -430,8 +430,8 @@ deamoe_status_t deamoe_norm_residual_backward(
  *
  * group: 32, 64 or 128; n_in a multiple of 32 (the last group may be short); n_out even with swiglu; codes 16-byte
  * aligned; n_in <= DEAMOE_MAX_WIDTH (else UNSUPPORTED / INVALID_ARG).  Any number of rows is computed; the
- * matrices of experts without rows are not read.  Sums are fp32; the weights and bf16 x are never rounded, fp32 x is
- * carried to 23 bits.
+ * matrices of experts without rows are not read.  Sums are fp32; the weights are never rounded, and x is carried
+ * exactly down to 2^-133 (2^-101 in a row that holds 2^96 or more).
  */
 uint64_t deamoe_quant_workspace(int32_t dtype, int32_t n_rows, int32_t n_in);
 deamoe_status_t deamoe_quant_product(void *cuda_stream, int32_t dtype, const uint8_t *codes, int32_t scale_dtype,

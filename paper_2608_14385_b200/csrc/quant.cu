@@ -4,23 +4,20 @@
 //
 // so the group scale multiplies an fp32 sum and no weight is ever rounded.  A decode step has a few rows per matrix:
 // the codes (half a byte a weight, read once) bound it, and the work beside them is to widen 2 weights a byte.
-// Measured: the gate and up matrices (4096 x 7168, groups of 128) of 16 tokens' top-8 of 256 experts, 1.5 GB, in 316 us
-// (4.8 TB/s; the loads of x and of the scales beside the codes and the issue of about 240 instructions for 2 KB of
-// codes a warp are what keeps it from HBM's rate), of one token's 8 experts in 39 us (3.1 TB/s), one matrix in 10 us.
+// Measured: the gate and up matrices (4096 x 7168, groups of 128) of 16 tokens' top-8 of 256 experts, 1.4 GB, in 308 us
+// (4.6 TB/s; fp32 tokens 591), of one token's 8 experts in 39 us (3.1 TB/s; 62), one matrix in 11 us (14).
 //
 // Tensor cores: mma.m16n8k16 with 16 matrix rows as M and up to 8 tokens as N (legacy path: with this few tokens the
 // instruction rate it needs is a fraction of what it has, and its A operand comes from registers, where the codes
-// have to be widened anyway).  Widening is one logical operation and a subtraction a pair: a nibble under the exponent
-// of 1024 is the fp16 number 1024 + q, or 1024 + 16 q where it lies four bits higher, and 1024 + z or 1024 + 16 z
-// leaves q - z or 16 (q - z), exactly.  (As the fp16 subnormals q 2^-24, without the exponent, the masked codes took 308
-// us where this takes 316, but the tensor cores align the products of a step by their exponents, and subnormals'
-// leading zeros cost the sum 6 to 10 of its bits.)  x becomes fp16 in a kernel of its own: each row scaled by a power of
-// two to a largest magnitude of 2^14..2^15, the columns that meet 16 (q - z) by another 2^-4, so that fp16's range
-// costs nothing (values below 2^-35 of the row's largest lose bits, far under fp32's own resolution of the sum); bf16
-// values fit exactly, fp32 values as two parts (2^-23 relative).
+// have to be widened anyway).  Widening is a shift, a logical operation and a subtraction a pair: a nibble under the
+// exponent of 128 is the bf16 number 128 + q, and 128 + z leaves q - z, exactly (the magic-number conversion of Kim et
+// al., 2022, arXiv 2211.10017, there for fp16).  bf16 because x has to stay what it is: bf16 tokens are operands as they
+// are, fp32 tokens as three bf16 parts of 8 bits each, which add up to the value.  (As fp16 operands, with a power of two
+// a row to bring x into fp16's range and fp32 in two parts, the codes' odd nibbles need no shift and fp32 two thirds of the
+// products: 295 us, fp32 468.  But what is 2^-28 of its row's largest value loses bits there, fp32 values from 2^-11 on,
+// and that shows where the large value meets a weight of 0.)
 #include <atomic>
 #include <climits>
-#include <cuda_fp16.h>
 
 #include "row.cuh"
 
@@ -45,8 +42,8 @@ struct QuantArgs {
   int steps;        // column steps of a row
   int wk;           // warps that share a row tile's columns (the others of the block take other tiles)
   int tile_groups;  // blocks of QW / wk warp tiles (16 MT rows) a matrix
-  __half* xh;       // [n_rows][planes][steps * QCOLS]
-  int32_t* xe;      // [2][n_rows] two powers of two (fp32 bits) that undo the row's scaling
+  uint16_t* xb;     // [n_rows][planes][steps * QCOLS] bf16
+  float* xf;        // [n_rows] factor of the row's products
 };
 
 // eight values of a row from column col on, 0 past its end
@@ -65,10 +62,17 @@ template <typename T> static __device__ __forceinline__ void eight_of(const T* x
     for (int i = 0; i < 8; ++i) v[i] = col + i < n_in ? to_f<T>(x[col + i]) : 0.f;
   }
 }
-// x in the order of the rows, as fp16 scaled by 2^-e, 8 columns in the order 0 4 1 5 2 6 3 7 (the order in which the
-// codes of a 32-bit word are widened; 1 5 3 7 by another 1/16).  One block a row; a row without a source is zero.
+// the bf16 number of v's sign, exponent and top 8 bits (a NaN stays one)
+static __device__ __forceinline__ float top_bits(float v) {
+  return __uint_as_float(v == v ? __float_as_uint(v) & 0xffff0000u : 0x7fc00000u);
+}
+// x in the order of the rows, as bf16 parts that add up to the value (fp32: three, each the top 8 bits of what is left, so
+// that no part can round to infinity), 8 columns in the order 0 4 1 5 2 6 3 7 (the order in which the codes of a 32-bit
+// word are widened).  One block a row; a row without a source is zero.
+// A group's sum of (q - z) x comes before its scale: rows with a value of 2^96 or more are carried times 2^-32, so that the
+// sum (below 2^24 times the value) overflows no earlier than the scaled products do.  fp32 rows below 2^-64 are carried
+// times 2^24, because a part below 2^-133 is no bf16 number: beside larger ones, that is where a value's bits end.
 template <typename T, int PLANES> __global__ void __launch_bounds__(1024) k_quant_x(QuantArgs A, bool wide) {
-  __shared__ float buf[32];
   const int64_t r = blockIdx.x;
   int64_t src = r;
   if (A.row_pair) src = A.row_pair[r] >= 0 ? A.row_pair[r] / A.ppt : -1;
@@ -77,79 +81,78 @@ template <typename T, int PLANES> __global__ void __launch_bounds__(1024) k_quan
   pdl_trigger();
   const int width = A.steps * QCOLS;
   float v[8] = {};  // the thread's first eight columns (all of them up to 8192 columns); later ones are read twice
-  float top = 0.f;
+  bool huge = false, tiny = true;
   for (int c = threadIdx.x; have && c < width / 8; c += blockDim.x) {
     float u[8];
     eight_of<T>(x, c * 8, A.n_in, wide, u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float m = fabsf(u[i]);
-      if (m <= 3.4028234663852886e38f) top = fmaxf(top, m);  // infinities and NaN stay what they are
+      huge |= m >= 0x1p96f && m <= 0x1.fffffep127f;  // infinities and NaN stay what they are
+      tiny &= !(m >= 0x1p-64f && m <= 0x1.fffffep127f);
       if (c == (int)threadIdx.x) v[i] = u[i];
     }
   }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = top;
-  __syncthreads();
-  top = (threadIdx.x & 31) < (blockDim.x >> 5) ? buf[threadIdx.x & 31] : 0.f;
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  const int e = top > 0.f ? ilogbf(top) - 14 : 0;
-  auto power = [](int k) { return __int_as_float((127 + k) << 23); };
-  const float f0 = power(-e / 2), f1 = power(-e - -e / 2);  // 2^-e as two factors, each in fp32's range
-  if (threadIdx.x == 0) {
-    A.xe[r] = __float_as_int(power(e / 2));
-    A.xe[(size_t)A.n_rows + r] = __float_as_int(power(e - e / 2));
-  }
-  __half* out = A.xh + r * PLANES * width;
+  huge = __syncthreads_or(huge);
+  if constexpr (PLANES > 1) tiny = __syncthreads_and(tiny);
+  const float f = huge ? 0x1p-32f : PLANES > 1 && tiny ? 0x1p24f : 1.f;
+  if (threadIdx.x == 0) A.xf[r] = 1.f / f;
+  uint16_t* out = A.xb + r * PLANES * width;
   for (int c = threadIdx.x; c < width / 8; c += blockDim.x) {
     if (c != (int)threadIdx.x && have) eight_of<T>(x, c * 8, A.n_in, wide, v);
-    union { __half h[8]; uint4 u; } hi, lo;
+    uint32_t part[PLANES][4];
 #pragma unroll
-    for (int p = 0; p < 8; ++p) {
-      const int i = (p >> 1) + (p & 1) * 4;
-      const float s = v[i] * f0 * f1, u = (p & 2) ? s * 0.0625f : s;
-      hi.h[p] = __float2half_rn(u);
-      const float rest = u - __half2float(hi.h[p]);
-      lo.h[p] = __float2half_rn(isfinite(u) ? rest : 0.f);
+    for (int p = 0; p < 4; ++p) {  // columns p and p + 4
+      float a = v[p] * f, b = v[p + 4] * f;
+#pragma unroll
+      for (int k = 0; k < PLANES; ++k) {
+        const float ta = top_bits(a), tb = top_bits(b);
+        part[k][p] = __float_as_uint(ta) >> 16 | (__float_as_uint(tb) & 0xffff0000u);
+        a = isfinite(ta) ? a - ta : 0.f;
+        b = isfinite(tb) ? b - tb : 0.f;
+      }
     }
-    *reinterpret_cast<uint4*>(out + c * 8) = hi.u;
-    if constexpr (PLANES == 2) *reinterpret_cast<uint4*>(out + width + c * 8) = lo.u;
+#pragma unroll
+    for (int k = 0; k < PLANES; ++k)
+      *reinterpret_cast<uint4*>(out + k * width + c * 8) = make_uint4(part[k][0], part[k][1], part[k][2], part[k][3]);
   }
 }
 
-static __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+static __device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                                uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 // the same with a sum that starts at 0
-static __device__ __forceinline__ void mma_f16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
+static __device__ __forceinline__ void mma_bf16_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0,
                                                      uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
       : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
-// The 8 codes of a word less the zero point as four pairs: columns (0 4) (1 5) (2 6) (3 7), q - z and 16 (q - z) in turn.
-// z: 1024 + the zero point in both halves, z16: 1024 + 16 times it.
+// Half of a part (16 of its 32 columns); `first`: the sum starts at 0.
+static __device__ __forceinline__ void part(float (&d)[4], const uint32_t (&lo)[4], const uint32_t (&hi)[4], const uint4& x, int half,
+                                            bool first) {
+  if (first) mma_bf16_first(d, lo[0], hi[0], lo[1], hi[1], x.x, x.y);
+  else if (half == 0) mma_bf16(d, lo[0], hi[0], lo[1], hi[1], x.x, x.y);
+  else mma_bf16(d, lo[2], hi[2], lo[3], hi[3], x.z, x.w);
+}
+// The 8 codes of a word less the zero point as four pairs: columns (0 4) (1 5) (2 6) (3 7).  z: 128 + the zero point in both
+// halves.
 static __device__ __forceinline__ uint32_t less(uint32_t a, uint32_t b) {
-  const __half2 d = __hsub2(*reinterpret_cast<__half2*>(&a), *reinterpret_cast<__half2*>(&b));
+  const __nv_bfloat162 d = __hsub2(*reinterpret_cast<__nv_bfloat162*>(&a), *reinterpret_cast<__nv_bfloat162*>(&b));
   return *reinterpret_cast<const uint32_t*>(&d);
 }
-constexpr uint32_t H1024 = 0x64006400u;
-static __device__ __forceinline__ uint32_t pick(uint32_t w, uint32_t mask, uint32_t exponent) {  // (w & mask) | exponent
+constexpr uint32_t B128 = 0x43004300u;
+static __device__ __forceinline__ uint32_t pick(uint32_t w, uint32_t exponent) {  // (w & 0x000f000f) | exponent
   uint32_t d;
-  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(w), "r"(mask), "r"(exponent));
+  asm("lop3.b32 %0, %1, %2, %3, 0xEA;" : "=r"(d) : "r"(w), "r"(0x000f000fu), "r"(exponent));
   return d;
 }
-static __device__ __forceinline__ void widen(uint32_t w, uint32_t h1024, uint32_t z, uint32_t z16, uint32_t (&p)[4]) {
-  const uint32_t v = w >> 8;
-  p[0] = less(pick(w, 0x000f000fu, h1024), z);
-  p[1] = less(pick(w, 0x00f000f0u, h1024), z16);
-  p[2] = less(pick(v, 0x000f000fu, h1024), z);
-  p[3] = less(pick(v, 0x00f000f0u, h1024), z16);
+static __device__ __forceinline__ void widen(uint32_t w, uint32_t b128, uint32_t z, uint32_t (&p)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p[i] = less(pick(w >> 4 * i, b128), z);
 }
 static __device__ __forceinline__ uint4 load_b128(const void* p) {
   uint4 v;
@@ -175,12 +178,15 @@ static __device__ __forceinline__ void quant_next(QuantAt& at, int end, const in
   if (at.item < end) quant_enter(at, first, tile_groups);
 }
 
-constexpr int Q_TOKENS = 16;  // tokens of a pass
+// Tokens of a pass.  fp32: what 16 need beside three parts does not fit the registers (16 tokens' top-8 of 64 experts, 4096
+// x 7168: 362 us, 409 with 16 a pass; groups of 32 with zero points 578 and 667).
+template <int PLANES> constexpr int TOKENS_OF_PASS = PLANES == 1 ? 16 : 8;
 
 // A block takes a contiguous share of the items; its warps split an item's columns (wk of them a tile of 16 MT rows).
 // Every warp streams its own codes, DEPTH steps of 16 MT rows x 256 columns ahead and across items, into its own part
 // of shared memory; nothing is shared between warps but the sums at an item's end.
 template <int PLANES, int MT, int NG, bool Z, bool SF, int DEPTH> struct QuantWarp {
+  static constexpr int NTOK = TOKENS_OF_PASS<PLANES> / 8;  // of 8 tokens, in a pass
   static constexpr int NB = 2 * MT;  // blocks of 8 matrix rows in a warp tile
   // a slot of the ring: codes, then every row's scales of the step (fp32), then its zero points (bytes)
   static constexpr int SCALES = MT * 2048, ZEROS = SCALES + 16 * MT * NG * 4, STEP = (ZEROS + (Z ? 16 * MT * NG : 0) + 127) / 128 * 128;
@@ -331,24 +337,24 @@ template <int PLANES, int MT, int NG, bool Z, bool SF, int DEPTH> struct QuantWa
 
   // The warp's columns of one item for NT * 8 tokens: acc[mt][t] = this warp's share of the products.
   template <int NT>
-  __device__ __forceinline__ void item(const QuantAt& at, int row0, int rows, uint32_t& slot, float (&acc)[MT][2][4]) {
+  __device__ __forceinline__ void item(const QuantAt& at, int row0, int rows, uint32_t& slot, float (&acc)[MT][NTOK][4]) {
     const int xw = A.steps * QCOLS;
     // tokens past the last take the last one's values: their sums are not looked at
-    const __half* xp[NT];
+    const uint16_t* xp[NT];
     // parts of x ahead: it comes from the L2, whose latency a whole step (8 parts) hides (16 tokens' top-8 of 256
-    // experts, 4096 x 7168 each: 316 us, 361 with 4 parts); where registers do not allow that, two
+    // experts, 4096 x 7168 each: 308 us, 336 with 4 parts); where registers do not allow that, two
     constexpr int XB = PLANES * NT == 1 ? 8 : 2;
     uint4 xb[XB][NT][PLANES];
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
-      xp[t] = A.xh + (size_t)(row0 + min(t * 8 + g, rows - 1)) * PLANES * xw + (size_t)c0 * QCOLS + j * 8;
+      xp[t] = A.xb + (size_t)(row0 + min(t * 8 + g, rows - 1)) * PLANES * xw + (size_t)c0 * QCOLS + j * 8;
 #pragma unroll
       for (int p = 0; p < PLANES; ++p)
 #pragma unroll
         for (int m = 0; m < XB; ++m) xb[m][t][p] = load_b128(xp[t] + (size_t)p * xw + m * 32);
     }
-    uint32_t h1024 = H1024;
-    asm volatile("" : "+r"(h1024));  // in a register: an instruction has room for one constant, the mask
+    uint32_t b128 = B128;
+    asm volatile("" : "+r"(b128));  // in a register: an instruction has room for one constant, the mask
     // the lane's row of the eight matrices an ldmatrix takes: block lane / 8 (MT == 1: block and part)
     const uint32_t lane_at = ring_at + (MT == 2 ? (lane >> 3) : (lane >> 3) & 1) * 1024 + (lane & 7) * 128 +
                              ((lane & 7) ^ (MT == 2 ? 0 : lane >> 4)) * 16;
@@ -385,21 +391,36 @@ template <int PLANES, int MT, int NG, bool Z, bool SF, int DEPTH> struct QuantWa
         }
         uint32_t w[NB][4];
 #pragma unroll
-        for (int b = 0; b < NB; ++b) widen(code[(m % LM) * NB + b], h1024, z[b] | H1024, z[b] << 4 | H1024, w[b]);
+        for (int b = 0; b < NB; ++b) widen(code[(m % LM) * NB + b], b128, z[b] | B128, w[b]);
+        // fp32: the lower parts by themselves, added to the group's sum once.  A matrix step cuts its sum at the largest
+        // term's last bit, so each step on the group's sum costs up to a unit of it, each of these 2^-8 of that.
+        float low[MT][NT][4];
+        if constexpr (PLANES > 1) {
+#pragma unroll
+          for (int p = PLANES - 1; p > 0; --p)
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+              for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int mt = 0; mt < MT; ++mt)
+                  part(low[mt][t], w[2 * mt], w[2 * mt + 1], xb[m % XB][t][p], half, p == PLANES - 1 && half == 0);
+        }
 #pragma unroll
         for (int half = 0; half < 2; ++half)
 #pragma unroll
           for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int p = 0; p < PLANES; ++p)
+            for (int mt = 0; mt < MT; ++mt)
+              part(grp[mt][t], w[2 * mt], w[2 * mt + 1], xb[m % XB][t][0], half, m * NG % QM == 0 && half == 0);
+        if constexpr (PLANES > 1) {
 #pragma unroll
-              for (int mt = 0; mt < MT; ++mt) {
-                const uint4 x = xb[m % XB][t][p];
-                const uint32_t(&lo)[4] = w[2 * mt], (&hi)[4] = w[2 * mt + 1];
-                if (m * NG % QM == 0 && half == 0 && p == 0) mma_f16_first(grp[mt][t], lo[0], hi[0], lo[1], hi[1], x.x, x.y);
-                else if (half == 0) mma_f16(grp[mt][t], lo[0], hi[0], lo[1], hi[1], x.x, x.y);
-                else mma_f16(grp[mt][t], lo[2], hi[2], lo[3], hi[3], x.z, x.w);
-              }
+          for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) grp[mt][t][i] += low[mt][t][i];
+        }
         if (m + XB < QM || more)
 #pragma unroll
           for (int t = 0; t < NT; ++t)
@@ -428,6 +449,7 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
   extern __shared__ __align__(128) uint8_t smem[];
   __shared__ int warp_sums[QW];
   using Warp = QuantWarp<PLANES, MT, NG, Z, SF, DEPTH>;
+  constexpr int TOKENS = TOKENS_OF_PASS<PLANES>;
   float4* sums = reinterpret_cast<float4*>(smem + QW * DEPTH * Warp::STEP);  // [2][QW][MT][32]
   int* first = reinterpret_cast<int*>(sums + 2 * QW * MT * 32);            // [n_expert + 1] first item of each expert
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, R = A.n_rows;
@@ -435,7 +457,7 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
   auto row_end = [&](int e) { return A.expert_off ? min(max(A.expert_off[e + 1], 0), R) : R; };
   for (int e = threadIdx.x; e < A.n_expert; e += QW * 32) {
     const int rows = max(row_end(e) - row_begin(e), 0);
-    first[e] = (rows + Q_TOKENS - 1) / Q_TOKENS * A.tile_groups;
+    first[e] = (rows + TOKENS - 1) / TOKENS * A.tile_groups;
   }
   __syncthreads();
   block_exclusive_scan(first, A.n_expert, warp_sums);
@@ -464,7 +486,7 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
   W.aim();
 #pragma unroll 1
   for (int i = 0; i < DEPTH; ++i) W.request(i * Warp::STEP);
-  pdl_wait();  // x in fp16
+  pdl_wait();  // x in bf16
 
   uint32_t slot = 0;
   int flip = 0;
@@ -481,9 +503,8 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
         b += v[h + 2];
       }
       const int64_t r = row0 + token;
-      const float p2 = __int_as_float(A.xe[r]), q2 = __int_as_float(A.xe[(size_t)R + r]);  // two powers of two
-      a = a * p2 * q2;
-      b = b * p2 * q2;
+      a *= A.xf[r];
+      b *= A.xf[r];
       T* out = reinterpret_cast<T*>(A.out) + r * A.os;
       const int per = A.swiglu ? 8 : 16, o_tile = (at.tg * tiles_per + W.wr) * MT * per;  // its first column, before it was moved up
       const int o = (MT == 1 ? o_tile : max(min(o_tile, width - MT * per), 0)) + mt * per + (l >> 2);
@@ -494,15 +515,15 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
     }
   };
   for (; at.item < i1; quant_next(at, i1, first, A.tile_groups)) {
-    const int row0 = row_begin(at.e) + at.pass * Q_TOKENS, rows = min(row_end(at.e) - row0, Q_TOKENS);
-    float acc[MT][2][4] = {};
-    if (rows <= 8) W.template item<1>(at, row0, rows, slot, acc);
-    else W.template item<2>(at, row0, rows, slot, acc);
+    const int row0 = row_begin(at.e) + at.pass * TOKENS, rows = min(row_end(at.e) - row0, TOKENS);
+    float acc[MT][Warp::NTOK][4] = {};
+    if (TOKENS == 8 || rows <= 8) W.template item<1>(at, row0, rows, slot, acc);
+    else W.template item<Warp::NTOK>(at, row0, rows, slot, acc);
     // join the column shares of the tile's warps, in order, 8 tokens at a time.  Two buffers: one is written while slower
     // warps still read the other, and no warp is two turns ahead of its partners
     const int tile_warp = W.wr * A.wk;  // the tile's first warp
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < Warp::NTOK; ++t) {
       if (t * 8 >= rows) break;
       float4* mine = sums + (size_t)(flip * QW + w) * MT * 32 + lane;
 #pragma unroll
@@ -516,17 +537,18 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
 }
 
 template <typename T, int NG, bool SF> static deamoe_status_t quant_t(QuantArgs& A, cudaStream_t s) {
-  constexpr int PLANES = sizeof(T) == 4 ? 2 : 1;
+  constexpr int PLANES = sizeof(T) == 4 ? 3 : 1;
   A.vec_scales = A.groups % NG == 0 && aligned_to(A.scales, NG == 2 && !SF ? 4 : 8);
   A.vec_zeros = A.zeros && A.groups % NG == 0 && aligned_to(A.zeros, NG < 4 ? NG : 4);
   const int tiles16 = A.swiglu ? (A.n_out / 2 + 7) / 8 : (A.n_out + 15) / 16;
   const int active = A.n_expert < A.n_rows ? A.n_expert : A.n_rows;
-  // Two row tiles a warp share its x values and loop (16 tokens' top-8 of 256 experts, 4096 x 7168: 360 us, 451 with one
-  // tile a warp); one where two would leave blocks without work (one token, one such matrix: 10.2 us, 11.8 with two)
+  // Two row tiles a warp share its x values and loop (16 tokens' top-8 of 256 experts, 4096 x 7168: 308 us, 350 with one
+  // tile a warp; fp32 591, 766); one where two would leave blocks without work (one token, one such matrix: 11.4 us, 13.3
+  // with two; fp32 14.4, 18.5)
   const int mt = (int64_t)(tiles16 / 2) * active >= Q_GRID && A.n_out >= 32 ? 2 : 1;
   // Warps that share a tile's columns: all, or fewer (longer walks, fewer sums to join) while the blocks keep at least
-  // 8 items each, so that their counts differ by little (the same 16 tokens: 362 us with this rule, 388 with all warps on
-  // one tile; 4 tokens' top-8 of 64 experts, 7168 x 2048: 57 and 65)
+  // 8 items each, so that their counts differ by little (the same 16 tokens: 308 us with this rule, 335 with all warps on
+  // one tile; 4 tokens' top-8 of 64 experts, 7168 x 2048: 56 and 61; fp32 591 and 555, 85 and 90)
   A.wk = QW;
   while (A.wk > A.steps) A.wk /= 2;
   while (A.wk > 1 && (int64_t)((tiles16 + mt - 1) / mt) * (A.wk / 2) / QW * active >= 8 * Q_GRID) A.wk /= 2;
@@ -575,7 +597,7 @@ extern "C" {
 uint64_t deamoe_quant_workspace(int32_t dtype, int32_t n_rows, int32_t n_in) {
   if (n_rows <= 0 || n_in <= 0) return 0;
   const uint64_t width = ((uint64_t)n_in + QCOLS - 1) / QCOLS * QCOLS;
-  return (uint64_t)n_rows * (width * (dtype == DEAMOE_F32 ? 4 : 2) + 2 * sizeof(int32_t));
+  return (uint64_t)n_rows * (width * (dtype == DEAMOE_F32 ? 6 : 2) + sizeof(float));
 }
 
 deamoe_status_t deamoe_quant_product(void* cuda_stream, int32_t dtype, const uint8_t* codes, int32_t scale_dtype,
@@ -608,10 +630,11 @@ deamoe_status_t deamoe_quant_product(void* cuda_stream, int32_t dtype, const uin
   A.steps = (n_in + QCOLS - 1) / QCOLS;
   const int tiles = swiglu ? (width + 7) / 8 : (width + 15) / 16;
   // items are counted in 32 bits (an expert's last pass may be short, hence one more each)
-  if ((int64_t)tiles * ((int64_t)n_rows / Q_TOKENS + n_expert) > INT_MAX) return DEAMOE_ERR_BATCH;
-  A.xh = reinterpret_cast<__half*>(workspace);
-  A.xe = reinterpret_cast<int32_t*>(reinterpret_cast<char*>(workspace) +
-                                    (size_t)n_rows * A.steps * QCOLS * (dtype == DEAMOE_F32 ? 4 : 2));
+  const int64_t passes = (int64_t)n_rows / (dtype == DEAMOE_F32 ? TOKENS_OF_PASS<3> : TOKENS_OF_PASS<1>) + n_expert;
+  if (tiles * passes > INT_MAX) return DEAMOE_ERR_BATCH;
+  A.xb = reinterpret_cast<uint16_t*>(workspace);
+  A.xf = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) +
+                                  (size_t)n_rows * A.steps * QCOLS * (dtype == DEAMOE_F32 ? 6 : 2));
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
   if (dtype == DEAMOE_F32) return quant_group<float>(A, group, s);
   return quant_group<__nv_bfloat16>(A, group, s);

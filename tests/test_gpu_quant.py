@@ -304,3 +304,40 @@ def test_product_without_rows_is_over_when_its_call_is(captured):
         graph.replay() if captured else step()
         torch.cuda.synchronize()
         assert (workspace == 0xa5).all() and (out == 7).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("group,zeros", [(32, True), (128, False)])
+@pytest.mark.parametrize("large", [1e4, 1e6, 1e12, 1e30, 3e38])
+def test_small_values_keep_their_bits_beside_a_large_one_of_weight_zero(large, group, zeros, dtype):
+    """The bound is relative to the products, of which the large value's is 0: the others are as exact as without it."""
+    N, K, T = 96, 1408, 11
+    codes, scales, z = _matrices(1, N, K, group, zeros, F32, 41)
+    at = [5, 130, 1407]                                        # columns of either nibble, of the first and the last group
+    for c in at:
+        zero = torch.full((N,), 8, dtype=torch.uint8, device=DEV) if z is None else z[0, :, c // group]
+        old = codes[0, :, c // 2]
+        codes[0, :, c // 2] = (old & 15) | zero << 4 if c & 1 else (old & 240) | zero
+    x = torch.randn((T, K), generator=torch.Generator(device=DEV).manual_seed(42), device=DEV)
+    x[:, at[0]], x[::2, at[1]], x[1:9, at[2]] = large, -large, large
+    x = x.to(dtype)
+    assert torch.isfinite(x).all()
+    got = binding.quant_product(codes, scales, x, group, zeros=z)
+    _check(got, *_want(codes, scales, z, group, x, [0] * T, list(range(T)), False))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_values_at_the_ends_of_the_range(dtype):
+    """Rows whose products with the codes alone would overflow, and rows of subnormal values: results that the type can hold
+    are held.  A result's subnormal operands count in full: the bound has no absolute part."""
+    N, K, group, T = 48, 32, 32, 6
+    codes, _, z = _matrices(1, N, K, group, True, F32, 43)
+    x = torch.randn((T, K), generator=torch.Generator(device=DEV).manual_seed(44), device=DEV).clamp(-3, 3)
+    for size, scale in ((1e38, 2.0 ** -12), (2.0 ** 96, 1.0), (2.0 ** -120, 2.0 ** 40), (2.0 ** -126, 2.0 ** 60)):
+        t = (x * size).to(dtype)
+        scales = torch.full((1, N, 1), scale, device=DEV)
+        want, err = _want(codes, scales, z, group, t, [0] * T, list(range(T)), False)
+        got = binding.quant_product(codes, scales, t, group, zeros=z)
+        assert torch.isfinite(got).all()
+        half = torch.finfo(dtype).eps / 2
+        assert ((got.double() - want).abs() <= err + half * (want.abs() + err)).all(), size
