@@ -424,6 +424,7 @@ deamoe_status_t deamoe_norm_residual_backward(
  *              whose range holds it and reads x row row_pair[r] / pairs_per_token.  expert_off may be NULL for
  *              one matrix (n_expert 1: every row is its); row_pair may be NULL: src(r) = r (rows already in expert
  *              order, as a second product's input is).  A row whose source lies outside x gets the product with 0.
+ *              Offsets outside [0, n_rows] count as its ends; if they decrease anywhere, nothing is written.
  *   swiglu     1: rows [0, n_out / 2) of a matrix are the gate, the others the up projection, and
  *              out[r, i] = SiLU(W x)[i] * (W x)[n_out / 2 + i]  (Eq. (1); out has n_out / 2 columns)
  *   out        [n_rows, n_out or n_out / 2] in dtype; rows behind expert_off[n_expert] are left as they were

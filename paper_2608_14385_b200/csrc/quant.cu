@@ -455,13 +455,15 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, R = A.n_rows;
   auto row_begin = [&](int e) { return A.expert_off ? min(max(A.expert_off[e], 0), R) : 0; };
   auto row_end = [&](int e) { return A.expert_off ? min(max(A.expert_off[e + 1], 0), R) : R; };
+  bool falling = false;  // ranges that overlap: their items may be more than 32 bits can count
   for (int e = threadIdx.x; e < A.n_expert; e += QW * 32) {
-    const int rows = max(row_end(e) - row_begin(e), 0);
+    const int rows = row_end(e) - row_begin(e);
+    falling |= rows < 0;
     first[e] = (rows + TOKENS - 1) / TOKENS * A.tile_groups;
   }
-  __syncthreads();
+  falling = __syncthreads_or(falling);
   block_exclusive_scan(first, A.n_expert, warp_sums);
-  const int total = first[A.n_expert];
+  const int total = falling ? 0 : first[A.n_expert];
   const int i0 = (int)((int64_t)total * blockIdx.x / gridDim.x), i1 = (int)((int64_t)total * (blockIdx.x + 1) / gridDim.x);
   if (i0 == i1) {  // no share; the grid must not end before the kernel that it was launched beside, even if nobody has one
     pdl_wait();

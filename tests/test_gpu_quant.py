@@ -341,3 +341,14 @@ def test_values_at_the_ends_of_the_range(dtype):
         assert torch.isfinite(got).all()
         half = torch.finfo(dtype).eps / 2
         assert ((got.double() - want).abs() <= err + half * (want.abs() + err)).all(), size
+
+
+@pytest.mark.parametrize("off", [[0, 64, 0, 64, 64], [0, 10, 9, 20, 64], [64, 0, 0, 0, 0], [0, 0, 0, 70, 69 - 64]])
+def test_offsets_that_decrease_write_nothing(off):
+    """Ranges that overlap could hold more rows in all than n_rows, which is what the kernel's counting is sized by."""
+    N, K, group, R = 48, 64, 32, 64
+    codes, scales, _ = _matrices(4, N, K, group, False, BF16, 51)
+    x = torch.randn((R, K), device=DEV).to(BF16)
+    out = torch.full((R, N), 5.0, dtype=BF16, device=DEV)
+    binding.quant_product(codes, scales, x, group, expert_off=torch.tensor(off, dtype=torch.int32, device=DEV), out=out)
+    assert (out == 5).all()
