@@ -80,6 +80,8 @@ template <typename T> static __device__ __forceinline__ float gate_at(const Norm
   return 1.f;
 }
 static __device__ __forceinline__ float inv_rms(float ss, int h, float eps) { return rsqrtf(ss / (float)h + eps); }
+// r^3 m for a mean m of values of size 1 / r: r^3 alone leaves fp32's range for rows beyond 1e13 or below 1e-13
+static __device__ __forceinline__ float cube_times(float r, float m) { return r * (r * (r * m)); }
 
 // ---------------------------------------------------------------- any width, any alignment: one block a row
 
@@ -115,7 +117,7 @@ template <typename T> __global__ void __launch_bounds__(ANY_THREADS) k_norm_grad
     block_sums<2>(s, buf[flip]);
     flip ^= 1;
     const float r = inv_rms(s[0], A.h, A.eps);
-    const float c = r * r * r * (s[1] / (float)A.h);
+    const float c = cube_times(r, s[1] / (float)A.h);
     for (int i = threadIdx.x; i < A.h; i += ANY_THREADS) {
       const float v = at<T>(A.x, t, i), d = at<T>(A.du, t, i);
       float dx = r * d * load_gain(A.w, A.wdt, i) - v * c;
@@ -192,7 +194,7 @@ template <typename T> __global__ void __launch_bounds__(ANY_THREADS) k_residual_
       }
       block_sums<2>(s, buf[1]);
       ro = inv_rms(s[0], A.h, A.next_eps);
-      co = ro * ro * ro * (s[1] / (float)A.h);
+      co = cube_times(ro, s[1] / (float)A.h);
     }
     auto total = [&](int i) {  // gradient of the sum
       float d = at<T>(A.dout, t, i);
@@ -207,7 +209,7 @@ template <typename T> __global__ void __launch_bounds__(ANY_THREADS) k_residual_
     }
     block_sums<2>(s, buf[flip]);
     flip ^= 1;
-    const float cy = A.post_norm ? ry * ry * ry * (s[0] / (float)A.h) : 0.f;
+    const float cy = A.post_norm ? cube_times(ry, s[0] / (float)A.h) : 0.f;
     if (A.gate_kind == DEAMOE_GATE_TOKEN && threadIdx.x == 0) A.dgate_token[t] = s[1];
     for (int i = threadIdx.x; i < A.h; i += ANY_THREADS) {
       const float d = total(i), y = at<T>(A.y, t, i), w = load_gain(A.w, A.wdt, i);
@@ -548,7 +550,7 @@ __global__ void __launch_bounds__(MAXT, 1) k_norm_grad_rows(NormArgs A, int pack
     block_sums_many<2, 2>(s, buf[flip]);
     flip ^= 1;
     const float r = inv_rms(s[0], A.h, A.eps);
-    const P r2 = splat<P>(r), c2 = splat<P>(-(r * r * r * (s[1] * inv_h)));
+    const P r2 = splat<P>(r), c2 = splat<P>(-cube_times(r, s[1] * inv_h));
 #pragma unroll
     for (int n = 0; n < NV; ++n) {
       const int c = threadIdx.x + n * blockDim.x;
@@ -694,9 +696,9 @@ __global__ void __launch_bounds__(MAXT, 1) k_residual_grad_rows(NormArgs A, int 
     block_sums_many<6, 8>(s, buf[flip]);
     flip ^= 1;
     const float ro = A.next_norm ? inv_rms(s[1], A.h, A.next_eps) : 0.f;
-    const float co = ro * ro * ro * (s[2] * inv_h);
+    const float co = cube_times(ro, s[2] * inv_h);
     const float sum3 = s[3] + ro * s[4] - co * s[5];
-    const float cy = A.post_norm ? gr * ry * ry * (sum3 * inv_h) : 0.f;
+    const float cy = A.post_norm ? gt * cube_times(ry, sum3 * inv_h) : 0.f;
     if (A.dgate_token && threadIdx.x == 0) A.dgate_token[t] = ry * sum3;
     const P ro2 = splat<P>(ro), co2 = splat<P>(-co), cy2 = splat<P>(-cy);
 #pragma unroll

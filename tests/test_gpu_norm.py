@@ -254,3 +254,30 @@ def test_rows_beyond_32_bit_offsets():
     (X * r * W).within(binding.norm(x, w, 1e-6)[-40:], "norm")
     dx, _ = binding.norm_backward(x, w, 1e-6, x)
     _unit_grad(X, r, X * W).within(dx[-40:], "dx")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,h", [(5, 1024), (3, 1027), (2, 16392)])
+@pytest.mark.parametrize("x_size,y_size,eps", [(1e15, 1.0, 1e-6), (1.0, 1e15, 1e-6), (1e15, 1e15, 1e-6), (1.0, 1e-14, 0.0), (1e-14, 1.0, 0.0)])
+def test_gradients_of_very_large_and_very_small_rows(x_size, y_size, eps, T, h, dtype):
+    """Rows whose inverse rms cubed no fp32 number holds, but whose gradients one does."""
+    x, y = _gauss((T, h), dtype, 1, x_size), _gauss((T, h), dtype, 2, y_size)
+    w, wn, gate = _gauss((h,), dtype, 3, 0.3, 1.0), _gauss((h,), dtype, 4, 0.3, 1.0), _gauss((T,), dtype, 5, 0.3, 1.0)
+    dout, du = _gauss((T, h), dtype, 6), _gauss((T, h), dtype, 7)
+    X, W, D = Bounded(x), Bounded(w), Bounded(du)
+    r = _inv(X, eps)
+    (X * r * W).within(binding.norm(x, w, eps), "norm")
+    dx, dw = binding.norm_backward(x, w, eps, du)
+    _unit_grad(X, r, D * W).within(dx, "dx")
+    (D * X * r).sum(0).within(dw, "dw")
+    kind = binding.GATE_TOKEN
+    X, Y, W, ry, branch, G, s, ro = _block(x, y, w, wn, gate, kind, 0.75, 1.5, eps, eps, True)
+    dx, dy, dgate, dw, dn = binding.norm_residual_backward(x, y, w, eps, dout, gate=gate, residual_scale=0.75, branch_scale=1.5,
+                                                           next_weight=wn, du=du, gate_kind=kind)
+    total = Bounded(dout) + _unit_grad(s, ro, Bounded(du) * Bounded(wn))
+    (Bounded(0.75) * total).within(dx, "dx of the block")
+    dv = Bounded(1.5) * G * total
+    _unit_grad(Y, ry, dv * W).within(dy, "dy")
+    (dv * Y * ry).sum(0).within(dw, "dweight")
+    (Bounded(du) * s * ro).sum(0).within(dn, "dnext_weight")
+    (Bounded(1.5) * total * branch).sum(1).within(dgate, "dgate")
