@@ -391,25 +391,26 @@ def norm_backward(x, weight, eps, du, dadd=None, dx=None):
 
 def _gate(gate, where, dtype, T, h, kind, dev):
     """Kind, address and row stride of a gate.  [h] is one per channel, [T, 1] or [T] one per token, [T, h] full; a gate of
-    one dimension with T == h needs `gate_kind`."""
+    one dimension with T == h needs `gate_kind` (and [T, 1] with h == 1 is full without it)."""
     if gate is None:
         return GATE_NONE, None, 0
     shape = tuple(gate.shape)
     if kind is None:
         if len(shape) == 1 and T == h and shape == (h,):
             _refuse(where, "gate [h] with as many tokens as channels: say gate_kind")
-        kind = {(h,): GATE_CHANNEL, (T,): GATE_TOKEN, (T, h): GATE_FULL}.get(shape)
+        kind = {(h,): GATE_CHANNEL, (T,): GATE_TOKEN, (T, 1): GATE_TOKEN, (T, h): GATE_FULL}.get(shape)
     if kind == GATE_FULL:
         return (kind,) + _mat(gate, where, "gate", dtype, T, h, dev)
     if kind not in (GATE_CHANNEL, GATE_TOKEN):
-        _refuse(where, f"gate must be [{h}] (channels), [{T}] (tokens) or [{T}, {h}], got {list(shape)}")
-    return kind, _vec(gate, where, "gate", dtype, (h if kind == GATE_CHANNEL else T,), dev), 0
+        _refuse(where, f"gate must be [{h}] (channels), [{T}] or [{T}, 1] (tokens) or [{T}, {h}], got {list(shape)}")
+    want = (h,) if kind == GATE_CHANNEL else shape if shape == (T, 1) else (T,)
+    return kind, _vec(gate, where, "gate", dtype, want, dev), 0
 
 
 def norm_residual(x, y, weight, eps, gate=None, residual_scale=1.0, branch_scale=1.0, normalise=True, next_norm=True,
                   next_weight=None, next_eps=None, gate_kind=None, out=None, next_out=None):
     """s = residual_scale x + branch_scale gate (y / rms(y) weight); returns s and s / rms(s) next_weight (None with
-    next_norm=False) in one pass (deamoe_norm_residual).  gate: None, [h], [T] or [T, h]; normalise=False takes y as it
+    next_norm=False) in one pass (deamoe_norm_residual).  gate: None, [h], [T], [T, 1] or [T, h]; normalise=False takes y as it
     is.  out may be x."""
     where, dev = "deamoe_norm_residual", _device()
     dt = _type(x, where, "x")
@@ -435,8 +436,8 @@ def norm_residual_backward(x, y, weight, eps, dout, gate=None, residual_scale=1.
                            next_weight=None, next_eps=None, du=None, gate_kind=None, dx=None, dy=None):
     """Gradients of `norm_residual` from those of its outputs (dout, and du of the next norm or None): dx, dy, dgate,
     dweight, dnext_weight; the last three are None where the call has no such input.  dweight, dnext_weight and the
-    gradient of a per-channel or per-token gate are float32, that of a full gate has the gate's type
-    (deamoe_norm_residual_backward)."""
+    gradient of a per-channel or per-token gate are float32, that of a full gate has the gate's type; dgate has the gate's
+    shape (deamoe_norm_residual_backward)."""
     where, dev = "deamoe_norm_residual_backward", _device()
     dt = _type(x, where, "x")
     T, h = x.shape
@@ -462,7 +463,7 @@ def norm_residual_backward(x, y, weight, eps, dout, gate=None, residual_scale=1.
     if channel:
         dgate = sums.pop()
     elif kind == GATE_TOKEN:
-        dgate = x.new_empty(T, dtype=torch.float32)
+        dgate = x.new_empty(gate.shape, dtype=torch.float32)
     elif kind == GATE_FULL:
         dgate, sdg = x.new_empty((T, h)), h
     L = lib()

@@ -281,3 +281,23 @@ def test_gradients_of_very_large_and_very_small_rows(x_size, y_size, eps, T, h, 
     (dv * Y * ry).sum(0).within(dw, "dweight")
     (Bounded(du) * s * ro).sum(0).within(dn, "dnext_weight")
     (Bounded(1.5) * total * branch).sum(1).within(dgate, "dgate")
+
+
+@pytest.mark.parametrize("T,h", [(6, 64), (64, 64), (1, 8), (5, 1)])
+def test_a_column_of_token_gates(T, h):
+    """[T, 1], as a projection with one output makes it, is the gate [T]; its gradient comes in its shape."""
+    x, y, w, dout = _gauss((T, h), BF16, 1), _gauss((T, h), BF16, 2), _gauss((h,), BF16, 3, 0.3, 1.0), _gauss((T, h), BF16, 4)
+    gate = _gauss((T, 1), BF16, 5)
+    flat, column = dict(gate=gate[:, 0].contiguous(), gate_kind=binding.GATE_TOKEN), dict(gate=gate, gate_kind=binding.GATE_TOKEN)
+    for kw in (column, dict(gate=gate)) if h > 1 else (column,):
+        for a, b in zip(binding.norm_residual(x, y, w, 1e-6, next_weight=w, **kw), binding.norm_residual(x, y, w, 1e-6, next_weight=w, **flat)):
+            assert torch.equal(a, b)
+        got = binding.norm_residual_backward(x, y, w, 1e-6, dout, next_weight=w, du=y, **kw)
+        want = binding.norm_residual_backward(x, y, w, 1e-6, dout, next_weight=w, du=y, **flat)
+        assert got[2].shape == (T, 1) and got[2].dtype == F32 and want[2].shape == (T,)
+        for i, (a, b) in enumerate(zip(got, want)):
+            assert torch.equal(a[:, 0] if i == 2 else a, b)
+    wide = _gauss((T, 2), BF16, 6)[:, :1]                       # not contiguous
+    if T > 1:
+        with pytest.raises(binding.DeaMoEError):
+            binding.norm_residual(x, y, w, 1e-6, gate=wide, gate_kind=binding.GATE_TOKEN)
