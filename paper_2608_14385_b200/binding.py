@@ -181,6 +181,7 @@ def route_static(router, tokens, n_dept, experts_per_dept, top_k, norm_topk=1, r
 # lives on), make outputs and workspaces that were not handed in, and call.  Matrices may have any row stride.
 
 _TYPES = {torch.float32: F32, torch.bfloat16: BF16}
+_INT_MAX = 2 ** 31 - 1  # sizes beyond it would reach the library without their upper bits
 
 
 def _refuse(where, why):
@@ -207,6 +208,8 @@ def _mat(t, where, name, dtype, rows, cols, dev):
         _refuse(where, f"{name} must be {dtype} [{rows}, {cols}], got {t.dtype} {list(t.shape)}")
     if t.get_device() != dev:
         _refuse(where, f"{name} is not on the current CUDA device")
+    if rows > _INT_MAX or cols > _INT_MAX:
+        _refuse(where, f"{name} [{rows}, {cols}] has a side of 2^31 or more")
     stride, step = t.stride()
     if step != 1 and cols > 1:
         _refuse(where, f"{name} must have consecutive values in a row")
@@ -232,6 +235,8 @@ def _type(t, where, name):
 def _pairs(pair_row, where):
     if pair_row.dim() != 2:
         _refuse(where, f"pair_row must be [T, k], got {list(pair_row.shape)}")
+    if pair_row.shape[1] > _INT_MAX:
+        _refuse(where, "top_k of 2^31 or more")
     return pair_row.shape
 
 
@@ -260,7 +265,9 @@ def sort_pairs(topk_idx, n_expert):
     T, k = topk_idx.shape
     src = _vec(topk_idx, where, "topk_idx", torch.int32, (T, k), dev)
     n = int(n_expert)
-    off = topk_idx.new_empty(max(n, 0) + 1)
+    if not 0 < n <= _INT_MAX or T > _INT_MAX or k > _INT_MAX:
+        _refuse(where, f"{T} tokens, top_k {k}, {n} experts")
+    off = topk_idx.new_empty(n + 1)
     pair_row = topk_idx.new_empty((T, k))
     row_pair = topk_idx.new_empty(T * k)
     L = lib()
@@ -488,7 +495,9 @@ def quant_product(codes, scales, x, group, zeros=None, expert_off=None, row_pair
     if codes.dim() != 3 or n_in != 2 * codes.shape[2]:
         _refuse(where, f"codes must be [E, n_out, {n_in} / 2], got {list(codes.shape)}")
     E, n_out, _ = codes.shape
-    groups = -(-n_in // group) if group > 0 else 0
+    if group not in (32, 64, 128) or not 0 < pairs_per_token <= _INT_MAX or E > _INT_MAX or n_out > _INT_MAX:
+        _refuse(where, f"group {group} (32, 64 or 128), pairs_per_token {pairs_per_token}, {E} matrices of {n_out} rows")
+    groups = -(-n_in // group)
     R = T if row_pair is None else row_pair.shape[0]
     width = n_out // 2 if swiglu else n_out
     if out is None:

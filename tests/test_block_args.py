@@ -1,4 +1,7 @@
 """Argument errors of the operators around a layer, found on the host before any CUDA call (no GPU needed)."""
+import pytest
+import torch
+
 from paper_2608_14385_b200 import binding
 
 INVALID, UNSUPPORTED, BATCH = binding.ERR_INVALID_ARG, binding.ERR_UNSUPPORTED, binding.ERR_BATCH
@@ -80,3 +83,39 @@ def test_quant():
     if need:
         assert _call("deamoe_quant_product", good, ws=None) == INVALID
         assert _call("deamoe_quant_product", good, size=need - 1) == INVALID
+
+
+class _NoCalls:
+    """Stands in for the library: sizes of workspaces and the names of errors, no operator."""
+
+    def __init__(self, real):
+        self.deamoe_status_string = real.deamoe_status_string
+        self.deamoe_sort_workspace = self.deamoe_quant_workspace = self.deamoe_norm_workspace = lambda *a: 0
+
+    def __getattr__(self, name):
+        raise AssertionError(f"{name} was called")
+
+
+def test_sizes_that_32_bits_cannot_hold_do_not_reach_the_library(monkeypatch):
+    """ctypes passes the low 32 bits of what is larger: a group of 2^32 + 32 would be one of 32 with one scale a row, -2^32 + 8
+    experts would be 8 with room for none."""
+    stub = _NoCalls(binding.lib())
+    monkeypatch.setattr(binding, "lib", lambda: stub)
+    monkeypatch.setattr(binding, "_device", lambda: -1)          # CPU tensors pass for those of the current device
+    monkeypatch.setattr(binding, "_raw_stream", lambda dev: 0)
+    big = 2 ** 32
+    idx = torch.zeros((4, 2), dtype=torch.int32)
+    codes, scales = torch.zeros((1, 16, 32), dtype=torch.uint8), torch.zeros((1, 16, 1))
+    x = torch.zeros((4, 64))
+    tall, long = torch.zeros((1, 1)).expand(big + 4, 1), torch.zeros((1, 1)).expand(1, big + 4)
+    pairs = torch.zeros((1, 1), dtype=torch.int32)
+    bad = [lambda: binding.sort_pairs(idx, big + 8), lambda: binding.sort_pairs(idx, 8 - big),
+           lambda: binding.quant_product(codes, scales, x, big + 32), lambda: binding.quant_product(codes, scales, x, 32 - big),
+           lambda: binding.quant_product(codes, torch.zeros((1, 16, 2)), x, 32, pairs_per_token=big + 1),
+           lambda: binding.quant_product(codes.expand(big + 1, 16, 32), scales, x, 64),
+           lambda: binding.norm(tall, None, 1e-6, out=tall), lambda: binding.norm(long, None, 1e-6, out=long),
+           lambda: binding.dispatch(x[:1], pairs.expand(1, big + 1), rows=x)]
+    for call in bad:
+        with pytest.raises(binding.DeaMoEError) as e:
+            call()
+        assert e.value.status == INVALID
