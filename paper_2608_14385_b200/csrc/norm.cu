@@ -86,7 +86,9 @@ static __device__ __forceinline__ float cube_times(float r, float m) { return r 
 // ---------------------------------------------------------------- any width, any alignment: one block a row
 
 constexpr int ANY_THREADS = 256;
-constexpr int RING_BYTES = 225 * 1024;  // of an SM's 227 KB, beside the sums' buffers (two fp32 rows of 4 x 7168 values)
+// An SM's 228 KB of shared memory go to its blocks: each has its ring, 2 KB for the sums' buffers and 1 KB that the device keeps.
+constexpr int SM_SMEM = 228 * 1024, BLOCK_SMEM = 3 * 1024;
+constexpr int RING_BYTES = SM_SMEM - BLOCK_SMEM;  // of one block alone (two fp32 rows of 4 x 7168 values)
 
 template <typename T> __global__ void __launch_bounds__(ANY_THREADS) k_norm_any(NormArgs A) {
   __shared__ float buf[32];
@@ -883,11 +885,24 @@ template <typename T> static deamoe_status_t residual_t(const NormArgs& A, cudaS
 }
 #undef DEAMOE_ROW_FORMS
 
-// Rows ahead in the ring: what the blocks of an SM can share of its shared memory, four at most.
-static int grad_stages(int blocks_per_sm, size_t stage_bytes) {
-  const size_t n = RING_BYTES / blocks_per_sm / stage_bytes;
+// Rows ahead in the ring: what the blocks of an SM can share of its shared memory, four at most.  All of an SM's blocks have
+// to be resident: one that waits for another's end makes the grid twice as long (4096 x 3584 bf16, where two blocks miss
+// it by 2 KB if their own needs are not counted: 83 us, 64 with one stage less).
+static constexpr int grad_stages(int blocks_per_sm, size_t stage_bytes) {
+  const size_t n = (SM_SMEM / blocks_per_sm - BLOCK_SMEM) / stage_bytes;
   return n > 4 ? 4 : (n < 1 ? 1 : (int)n);
 }
+static constexpr bool grad_blocks_fit() {
+  for (int threads = 32; threads <= 512; threads += 32)
+    for (int blocks = 1; blocks <= 8 && blocks * threads <= 512; ++blocks)
+      for (int inputs = 2; inputs <= 5; ++inputs)
+        for (int value_bytes = 2; value_bytes <= 4; value_bytes += 2) {
+          const size_t stage = (size_t)inputs * GRAD_COLUMNS * value_bytes * threads;
+          if (blocks * (stage * grad_stages(blocks, stage) + BLOCK_SMEM) > SM_SMEM) return false;
+        }
+  return true;
+}
+static_assert(grad_blocks_fit(), "an SM's blocks of the gradient kernels do not fit its shared memory");
 template <typename K, typename... Rest>
 static deamoe_status_t run_grad(K* kernel, std::atomic<uint64_t>& done, const NormArgs& A, int ctas, int threads, int packs,
                                 size_t stage_bytes, cudaStream_t s, Rest... rest) {
