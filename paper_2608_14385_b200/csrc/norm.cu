@@ -81,7 +81,7 @@ template <typename T> static __device__ __forceinline__ float gate_at(const Norm
 }
 static __device__ __forceinline__ float inv_rms(float ss, int h, float eps) { return rsqrtf(ss / (float)h + eps); }
 // r^3 m for a mean m of values of size 1 / r: r^3 alone leaves fp32's range for rows beyond 1e13 or below 1e-13
-static __device__ __forceinline__ float cube_times(float r, float m) { return r * (r * (r * m)); }
+static __device__ __forceinline__ float cube_times(float r, float m) { return (r * r) * (r * m); }
 
 // ---------------------------------------------------------------- any width, any alignment: one block a row
 
@@ -700,7 +700,7 @@ __global__ void __launch_bounds__(MAXT, 1) k_residual_grad_rows(NormArgs A, int 
     const float ro = A.next_norm ? inv_rms(s[1], A.h, A.next_eps) : 0.f;
     const float co = cube_times(ro, s[2] * inv_h);
     const float sum3 = s[3] + ro * s[4] - co * s[5];
-    const float cy = A.post_norm ? gt * cube_times(ry, sum3 * inv_h) : 0.f;
+    const float cy = A.post_norm ? (gr * ry) * (ry * (sum3 * inv_h)) : 0.f;
     if (A.dgate_token && threadIdx.x == 0) A.dgate_token[t] = ry * sum3;
     const P ro2 = splat<P>(ro), co2 = splat<P>(-co), cy2 = splat<P>(-cy);
 #pragma unroll
