@@ -301,3 +301,70 @@ def test_a_column_of_token_gates(T, h):
     if T > 1:
         with pytest.raises(binding.DeaMoEError):
             binding.norm_residual(x, y, w, 1e-6, gate=wide, gate_kind=binding.GATE_TOKEN)
+
+
+# Blocks of the gradient kernels that walk several rows each: the ring of rows ahead holds 4 (7168 bf16), 3 (7168 bf16 with a
+# full gate, 4096 and 1024 bf16), 2 (7168 fp32) or 1 (7168 fp32 with a full gate, 4096 and 1024 fp32); 1027 is read value by
+# value; 9001 goes through the form for any width.
+MANY = [(500, 7168), (950, 4096), (3700, 1024), (2300, 1027), (900, 9001), (4000, 24)]
+
+
+def _rows_a_block(T, h):
+    return T * 12 * h / binding.lib().deamoe_norm_workspace(T, h)    # the workspace holds three rows of sums a block
+
+
+@pytest.mark.parametrize("dtype,wdtype", [(BF16, F32), (F32, F32)])
+@pytest.mark.parametrize("T,h", MANY)
+def test_norm_gradient_with_many_rows_a_block(T, h, dtype, wdtype):
+    assert _rows_a_block(T, h) >= 3
+    eps = 1e-6
+    x, du, dadd = (_gauss((T, h), dtype, i, 1.0 + i) for i in range(3))
+    w = _gauss((h,), wdtype, 9, 0.3, 1.0)
+    X, W, D = Bounded(x), Bounded(w), Bounded(du)
+    r = _inv(X, eps)
+    want, sums = _unit_grad(X, r, D * W), (D * X * r).sum(0)
+    for add in (None, dadd):
+        dx, dw = binding.norm_backward(x, w, eps, du, dadd=add)
+        (want if add is None else want + Bounded(add)).within(dx, "dx")
+        sums.within(dw, "dw")
+        again = binding.norm_backward(x, w, eps, du, dadd=add)
+        assert torch.equal(again[0], dx) and torch.equal(again[1], dw)
+
+
+@pytest.mark.parametrize("normalise,next_norm", [(True, True), (False, True), (True, False)])
+@pytest.mark.parametrize("gate_kind", ["none", "channel", "token", "full"])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,h", MANY)
+def test_residual_gradient_with_many_rows_a_block(T, h, dtype, gate_kind, normalise, next_norm):
+    assert _rows_a_block(T, h) >= 3
+    a, b, eps, next_eps = 0.75, 1.5, 2.0 ** -20, 2.0 ** -17
+    kind = KINDS[gate_kind]
+    shape = {"none": None, "channel": (h,), "token": (T,), "full": (T, h)}[gate_kind]
+    x, y, dout = (_gauss((T, h), dtype, i, 0.5 + i) for i in range(3))
+    du = _gauss((T, h), dtype, 3) if next_norm else None
+    w = _gauss((h,), F32, 4, 0.3, 1.0) if normalise else None
+    wn = _gauss((h,), F32, 5, 0.3, 1.0) if next_norm else None
+    gate = None if shape is None else _gauss(shape, dtype, 6, 0.5, 0.3)
+    X, Y, W, ry, branch, G, s, ro = _block(x, y, w, wn, gate, kind, a, b, eps, next_eps, normalise)
+
+    def call():
+        return binding.norm_residual_backward(x, y, w, eps, dout, gate=gate, residual_scale=a, branch_scale=b, normalise=normalise,
+                                              next_weight=wn, next_eps=next_eps, du=du, gate_kind=kind)
+
+    dx, dy, dgate, dw, dn = got = call()
+    D = Bounded(dout)
+    if next_norm:
+        D = D + _unit_grad(s, ro, Bounded(du) * Bounded(wn))
+        (Bounded(du) * s * ro).sum(0).within(dn, "dnext_weight")
+    (Bounded(a) * D).within(dx, "dx")
+    dv = Bounded(b) * G * D
+    if normalise:
+        _unit_grad(Y, ry, dv * W).within(dy, "dy")
+        (dv * Y * ry).sum(0).within(dw, "dweight")
+    else:
+        dv.within(dy, "dy")
+    if kind is not None:
+        dg = Bounded(b) * D * branch
+        (dg if kind == binding.GATE_FULL else dg.sum(0 if kind == binding.GATE_CHANNEL else 1)).within(dgate, "dgate")
+    for p, q in zip(got, call()):
+        assert p is None and q is None or torch.equal(p, q)
