@@ -352,3 +352,43 @@ def test_offsets_that_decrease_write_nothing(off):
     out = torch.full((R, N), 5.0, dtype=BF16, device=DEV)
     binding.quant_product(codes, scales, x, group, expert_off=torch.tensor(off, dtype=torch.int32, device=DEV), out=out)
     assert (out == 5).all()
+
+
+# Rows of an expert: none, one, around passes of 8 and 16 tokens, several passes
+COUNTS = [5, 12, 40, 0, 1, 8, 9, 16, 17, 3, 2, 0, 24, 33, 7, 15]
+
+
+def _in_expert_order(counts, k, seed):
+    off = torch.tensor([0] + torch.tensor(counts).cumsum(0).tolist(), dtype=torch.int32, device=DEV)
+    R = sum(counts)
+    pairs = torch.randperm(R, generator=torch.Generator(device=DEV).manual_seed(seed), device=DEV)
+    return off, pairs.to(torch.int32), [e for e, c in enumerate(counts) for _ in range(c)], [p // k for p in pairs.tolist()]
+
+
+# Two row tiles a warp (296 and more of them to share): 628 SwiGLU columns and 1256 rows are no multiple of the 32-row tile,
+# which then overlaps the one before; 2080 columns end inside a step, 1120 inside a group of 64 or 128
+@pytest.mark.parametrize("swiglu", [True, False])
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("zeros,sdtype", [(False, BF16), (True, BF16), (True, F32)])
+@pytest.mark.parametrize("N,K", [(1256, 2080), (1300, 1120)])
+def test_two_tiles_a_warp(N, K, zeros, sdtype, group, dtype, swiglu):
+    k = 8
+    off, pairs, experts, sources = _in_expert_order(COUNTS, k, N)
+    codes, scales, z = _matrices(len(COUNTS), N, K, group, zeros, sdtype, K)
+    x = torch.randn((-(-sum(COUNTS) // k), K), generator=torch.Generator(device=DEV).manual_seed(K), device=DEV).to(dtype)
+    got = binding.quant_product(codes, scales, x, group, zeros=z, expert_off=off, row_pair=pairs, pairs_per_token=k, swiglu=swiglu)
+    _check(got, *_want(codes, scales, z, group, x, experts, sources, swiglu))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("zeros", [False, True])
+@pytest.mark.parametrize("E,N,K", [(40, 4096, 2048), (80, 4096, 768), (160, 4096, 512)])
+def test_fewer_warps_a_tile(E, N, K, zeros, dtype):
+    """So many items that 4, 2 or 1 of a block's warps share a tile's columns: the main form of a decode step over experts."""
+    counts = [1 + (7 * e) % 19 if e % 8 == 0 else 1 + e % 3 for e in range(E)]
+    off, _, experts, _ = _in_expert_order(counts, 1, 1)
+    codes, scales, z = _matrices(E, N, K, 128, zeros, BF16, E)
+    x = torch.randn((sum(counts), K), generator=torch.Generator(device=DEV).manual_seed(K), device=DEV).to(dtype)
+    got = binding.quant_product(codes, scales, x, 128, zeros=z, expert_off=off, swiglu=True)
+    _check(got, *_want(codes, scales, z, 128, x, experts, list(range(len(experts))), True))
