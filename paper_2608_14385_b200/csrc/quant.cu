@@ -461,9 +461,12 @@ __global__ void __launch_bounds__(QW * 32, 2) k_quant(QuantArgs A) {
     falling |= rows < 0;
     first[e] = (rows + TOKENS - 1) / TOKENS * A.tile_groups;
   }
-  falling = __syncthreads_or(falling);
+  if (__syncthreads_or(falling)) {
+    pdl_wait();
+    return;
+  }
   block_exclusive_scan(first, A.n_expert, warp_sums);
-  const int total = falling ? 0 : first[A.n_expert];
+  const int total = first[A.n_expert];
   const int i0 = (int)((int64_t)total * blockIdx.x / gridDim.x), i1 = (int)((int64_t)total * (blockIdx.x + 1) / gridDim.x);
   if (i0 == i1) {  // no share; the grid must not end before the kernel that it was launched beside, even if nobody has one
     pdl_wait();
