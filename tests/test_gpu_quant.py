@@ -392,3 +392,24 @@ def test_fewer_warps_a_tile(E, N, K, zeros, dtype):
     x = torch.randn((sum(counts), K), generator=torch.Generator(device=DEV).manual_seed(K), device=DEV).to(dtype)
     got = binding.quant_product(codes, scales, x, 128, zeros=z, expert_off=off, swiglu=True)
     _check(got, *_want(codes, scales, z, 128, x, experts, list(range(len(experts))), True))
+
+
+@pytest.mark.parametrize("large", [0.0, 1e6, 1e20])
+@pytest.mark.parametrize("K,group,zeros", [(1056, 32, True), (7168, 128, False), (2048, 64, True)])
+def test_fp32_products_round_only_their_sums(K, group, zeros, large):
+    """The error of all products together, 2-norm.  Of zero-mean terms a partial sum's square is the share of its terms in the
+    result's, half of that on average.  On a group's sum (share group / K) there are two matrix steps in 32 columns, which
+    cut: a unit of 2^-23, a third of its square.  On the whole sum there are G scalings, which round: a twelfth.  So the
+    squares add up to (K / 16) (group / K) / 6 + G / 24 squared units.  A large value that meets weights of 0 adds nothing."""
+    N, T = 512, 24
+    codes, scales, z = _matrices(1, N, K, group, zeros, F32, 61)
+    x = torch.randn((T, K), generator=torch.Generator(device=DEV).manual_seed(62), device=DEV)
+    if large:
+        for c in (3, 700):
+            zero = torch.full((N,), 8, dtype=torch.uint8, device=DEV) if z is None else z[0, :, c // group]
+            old = codes[0, :, c // 2]
+            codes[0, :, c // 2] = (old & 15) | zero << 4 if c & 1 else (old & 240) | zero
+            x[:, c] = large
+    got = binding.quant_product(codes, scales, x, group, zeros=z).double()
+    want = x.double() @ _widened(codes[0], scales[0], None if z is None else z[0], group, K).T
+    assert (got - want).norm() <= (group / 96 + scales.shape[2] / 24) ** 0.5 * 2.0 ** -23 * want.norm()
