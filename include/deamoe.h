@@ -316,7 +316,8 @@ deamoe_status_t deamoe_route_static(void *cuda_stream, const float *router, cons
  * to their value for the others (rows that start on 16-byte boundaries are read 16 bytes at a time, any
  * others value by value).  Matrices are row-major with a row stride in VALUES (>= the row's length), so a
  * column range of a wider matrix is a valid operand.  Outputs must not overlap inputs except where it is
- * said.  Sums, statistics and products are fp32; every output is rounded once.  Equal calls give equal
+ * said.  Sums, statistics and products are fp32 (the norms' sums of squares too: a row whose rms is above
+ * about 1e17 overflows them); every output is rounded once.  Equal calls give equal
  * bits: no kernel here adds in an order that depends on timing.  n_token == 0 is valid everywhere.
  * Sizes: hidden <= DEAMOE_MAX_WIDTH, top_k <= DEAMOE_MAX_TOPK, n_expert <= DEAMOE_MAX_EXPERTS (else
  * UNSUPPORTED); n_token * top_k < 2^31 (else BATCH).

@@ -39,7 +39,6 @@ SYMBOLS = ("deamoe_layer_create", "deamoe_vanilla_create", "deamoe_layer_destroy
            "deamoe_norm_residual", "deamoe_norm_residual_backward", "deamoe_quant_workspace", "deamoe_quant_product")
 
 GATE_NONE, GATE_CHANNEL, GATE_TOKEN, GATE_FULL = 0, 1, 2, 3
-MAX_WIDTH = 1 << 20
 
 
 class Config(C.Structure):

@@ -12,11 +12,11 @@
 // row statistics are recomputed too, they cost nothing next to the loads.  All sums are fp32; each output is rounded
 // once.
 //
-// Every operator is one pass of HBM traffic over [T, h] rows: bytes bound the forward calls (8192 x 7168 bf16: norm 39 us,
-// norm_residual with a channel gate and the next norm 83 us, 5.9 and 5.7 TB/s) and, with the instruction issue of a
-// row's work, the backward calls (norm_backward 68 us, 84 with dadd; norm_residual_backward 175 us: 5.2, 5.6 and 4.0
-// TB/s).  Sums over the tokens (dw, dwn, a per-channel dgate) are kept per thread block and added by a second kernel
-// in block order: no atomics, equal calls give equal bits.
+// Every operator is one pass of HBM traffic over [T, h] rows: bytes bound the forward calls (8192 x 7168 bf16: norm 38 us,
+// norm_residual with a channel gate and the next norm 81 us, 6.2 and 5.8 TB/s) and norm_backward (67 us, 80 with dadd:
+// 5.3 and 5.8 TB/s); norm_residual_backward (170 us, 4.1 TB/s) is held by a row's latency, see there.  Sums over the
+// tokens (dw, dwn, a per-channel dgate) are kept per thread block and added by a second kernel in block order: no
+// atomics, equal calls give equal bits.
 #include <atomic>
 
 #include "row.cuh"
@@ -25,7 +25,8 @@ namespace deamoe {
 
 // Thread blocks of the backward kernels, each of which leaves one row of partial column sums: 16 columns a thread (a
 // row's fixed work -- addresses, the reduction -- is spread over more values than with 8, and 128 registers hold the
-// columns' constants and sums), 512 threads an SM (rows of up to 8192 values; else two blocks an SM).
+// columns' constants and sums), 512 threads an SM or the 8 blocks that they come in for rows below 1024 values (rows of up
+// to 8192 values; else two blocks an SM).
 constexpr int NORM_SMS = 148;
 constexpr int GRAD_COLUMNS = 16, GRAD_MAX_WIDTH = 8192;
 constexpr int GRAD_ODD_COLUMNS = 8;  // of rows that are read value by value
@@ -597,8 +598,9 @@ __global__ void __launch_bounds__(MAXT, 1) k_norm_grad_rows(NormArgs A, int pack
 //   dy = gr p D - y gr ry^2 sum3 / h,   dgate_token = ry sum3,   E = gr D y,
 //   dw = b g sum_t E,   dgate_channel = b w sum_t E   -- one accumulator a column for both.
 // sum3 = sum p y dout + ro sum p y du wn - co sum p y s, so all of a row's sums are taken before ro and co are known,
-// and the sum of the next row's y^2 with them: one reduction and one barrier a row (three before: 5 us a row of 7168
-// values, most of it their latency).
+// and the sum of the next row's y^2 with them: one reduction and one barrier a row, not three in turn.  That one is still
+// what a row waits for (4096 x 7168 bf16: 100 us, of which some 45 are issue): the column constants p and q and the sums
+// take the registers that a second block would need to work meanwhile.
 template <typename T, int VE, int NV, int MAXT, bool FULL>
 __global__ void __launch_bounds__(MAXT, 1) k_residual_grad_rows(NormArgs A, int packs, int stages, size_t part_step) {
   extern __shared__ uint4 ring[];

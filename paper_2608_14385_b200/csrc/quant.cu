@@ -4,8 +4,11 @@
 //
 // so the group scale multiplies an fp32 sum and no weight is ever rounded.  A decode step has a few rows per matrix:
 // the codes (half a byte a weight, read once) bound it, and the work beside them is to widen 2 weights a byte.
-// Measured: the gate and up matrices (4096 x 7168, groups of 128) of 16 tokens' top-8 of 256 experts, 1.4 GB, in 308 us
-// (4.6 TB/s; fp32 tokens 591), of one token's 8 experts in 39 us (3.1 TB/s; 62), one matrix in 11 us (14).
+// Measured: the gate and up matrices (4096 x 7168, groups of 128) of 16 tokens' top-8 of 256 experts, 93 of them active
+// (1.4 GB), in 308 us (4.6 TB/s; fp32 tokens 591), of one token's 8 experts in 39 us (3.1 TB/s; 62), one matrix in 11 us
+// (14).  Back to back for seconds the first takes a tenth longer: the power limit then holds the clock near 1.75 GHz.  No
+// unit is full (issue 56 %, DRAM 52 %, tensor pipe 26 %): four warps a scheduler, which 128 registers a thread allow, do
+// not hide the latency of their loads of x and of their own widening.
 //
 // Tensor cores: mma.m16n8k16 with 16 matrix rows as M and up to 8 tokens as N (legacy path: with this few tokens the
 // instruction rate it needs is a fraction of what it has, and its A operand comes from registers, where the codes
