@@ -60,7 +60,11 @@ typedef enum {
   DEAMOE_ERR_INTERNAL = 7     /* a device-side consistency check failed; the access was skipped (get_stats) */
 } deamoe_status_t;
 
-typedef enum { DEAMOE_F32 = 0, DEAMOE_BF16 = 1 } deamoe_dtype_t;
+typedef enum {
+  DEAMOE_F32 = 0,
+  DEAMOE_BF16 = 1,
+  DEAMOE_E4M3 = 2 /* 8-bit rows with an fp32 scale each; only where it is said */
+} deamoe_dtype_t;
 
 /* sigma of Section 3.1: the non-linearity between department and expert projections */
 typedef enum {
@@ -442,6 +446,87 @@ deamoe_status_t deamoe_quant_product(void *cuda_stream, int32_t dtype, const uin
                                      const int32_t *expert_off, const int32_t *row_pair, int32_t pairs_per_token,
                                      int32_t n_rows, int32_t swiglu, void *out, int64_t out_stride, void *workspace,
                                      uint64_t workspace_bytes);
+
+/*
+ * Norms with an output in 8 bits, as deamoe_product takes it:  code = e4m3(u / scale),  scale = max |u| / 448 of the row.
+ *
+ *   deamoe_norm_quant            u = x / rms(x) * weight   (normalise = 0: u = x * weight, which quantises any rows)
+ *   deamoe_norm_residual_quant   deamoe_norm_residual with its second output, next, in this form
+ *
+ * codes: [n_token, hidden] bytes with a row stride; scale: [n_token] fp32.  u is not rounded in between.  A row whose
+ * max |s * weight| (s: what is normed) is below 2^-110, a row of zeros among them, has a scale as if it were 2^-110.  A value
+ * that is not finite gives its row a scale that is not.
+ */
+deamoe_status_t deamoe_norm_quant(void *cuda_stream, int32_t dtype, const void *x, int64_t x_stride, int32_t n_token,
+                                  int32_t hidden, int32_t normalise, int32_t weight_dtype, const void *weight, float eps,
+                                  void *codes, int64_t codes_stride, float *scale);
+deamoe_status_t deamoe_norm_residual_quant(void *cuda_stream, int32_t dtype, const void *x, int64_t x_stride, const void *y,
+                                           int64_t y_stride, int32_t n_token, int32_t hidden, int32_t normalise,
+                                           int32_t weight_dtype, const void *weight, float eps, int32_t gate_kind,
+                                           const void *gate, int64_t gate_stride, float residual_scale, float branch_scale,
+                                           void *out, int64_t out_stride, const void *next_weight, float next_eps, void *codes,
+                                           int64_t codes_stride, float *scale);
+
+/*
+ * Gated feed-forward blocks (the experts of Eq. (1)) over rows in expert order, for prompts, training and decode; bf16.
+ *
+ *   h = SiLU(x Wg^T) * (x Wu^T),   out = h Wd^T          row r with the matrices of the expert whose range holds it
+ *
+ *   x, out, dout, dx  [n_rows, hidden] bf16, 16-byte aligned, row strides in values and multiples of 8
+ *   w_gate_up   [n_expert, 2 ffn, hidden] bf16: rows [0, ffn) of a matrix are the gate, the others the up projection
+ *   w_down      [n_expert, hidden, ffn] bf16
+ *   expert_off  [n_expert + 1] as deamoe_sort_pairs gives it; NULL for one expert (every row is its).  Offsets outside
+ *               [0, n_rows] count as its ends; if they decrease anywhere, no row is written and the gradients are undefined.
+ *
+ * Rows behind expert_off[n_expert] are left as they were (out, dx).  h is rounded to bf16 once.
+ * deamoe_ffn_backward takes the forward call's inputs and dout:  dx, dw_gate_up and dw_down (shapes and type of the
+ * matrices; an expert without rows gets zeros).  Gate and up are recomputed in fp32, the gradients of gate and up are rounded to
+ * bf16 once.  hidden and ffn: multiples of 8 (else UNSUPPORTED).
+ */
+uint64_t deamoe_ffn_workspace(int32_t n_rows, int32_t ffn, int32_t backward);
+deamoe_status_t deamoe_ffn(void *cuda_stream, const void *x, int64_t x_stride, const void *w_gate_up, const void *w_down,
+                           const int32_t *expert_off, int32_t n_expert, int32_t n_rows, int32_t hidden, int32_t ffn,
+                           void *out, int64_t out_stride, void *workspace, uint64_t workspace_bytes);
+deamoe_status_t deamoe_ffn_backward(void *cuda_stream, const void *x, int64_t x_stride, const void *w_gate_up,
+                                    const void *w_down, const void *dout, int64_t dout_stride, const int32_t *expert_off,
+                                    int32_t n_expert, int32_t n_rows, int32_t hidden, int32_t ffn, void *dx,
+                                    int64_t dx_stride, void *dw_gate_up, void *dw_down, void *workspace,
+                                    uint64_t workspace_bytes);
+
+/*
+ * Matrix products with bias, activation and residual in their epilogue:
+ *
+ *   out = act(z) + residual,   z = x W^T + bias        (dtype DEAMOE_E4M3: z = x_scale weight_scale (x W^T) + bias)
+ *
+ *   dtype      of x and weight: DEAMOE_BF16, or DEAMOE_E4M3 with x_scale [n_token] and weight_scale [n_out] fp32 (NULL for bf16)
+ *   x          [n_token, n_in], 16-byte aligned, row stride a multiple of 16 bytes
+ *   weight     [n_out, n_in], dense, 16-byte aligned
+ *   bias       [n_out] in bias_dtype (DEAMOE_F32 or DEAMOE_BF16), or NULL
+ *   act        DEAMOE_SIGMA_NONE, _SILU or _GELU
+ *   residual   [n_token, n_out] bf16 with a row stride, or NULL; out may be residual itself (same stride)
+ *   out        [n_token, n_out] bf16
+ * n_in: a multiple of 8 (e4m3: of 16; else UNSUPPORTED); n_out: any.  Rounded once.
+ *
+ * deamoe_product_backward (bf16; n_out a multiple of 8) takes the forward call's inputs and dout:
+ *   dz = dout act'(z),   dx = dz W,   dweight = dz^T x (bf16),   dbias = sum over tokens of dz (fp32, or NULL)
+ * The residual's gradient is dout.  z is recomputed in fp32; dz is rounded to bf16 once for dx and dweight, not for dbias.
+ */
+uint64_t deamoe_product_workspace(int32_t n_token, int32_t n_out, int32_t act); /* of the backward call */
+deamoe_status_t deamoe_product(void *cuda_stream, int32_t dtype, const void *x, int64_t x_stride, const float *x_scale,
+                               int32_t n_token, const void *weight, const float *weight_scale, int32_t n_out, int32_t n_in,
+                               int32_t bias_dtype, const void *bias, int32_t act, const void *residual,
+                               int64_t residual_stride, void *out, int64_t out_stride);
+deamoe_status_t deamoe_product_backward(void *cuda_stream, int32_t dtype, const void *x, int64_t x_stride, int32_t n_token,
+                                        const void *weight, int32_t n_out, int32_t n_in, int32_t bias_dtype, const void *bias,
+                                        int32_t act, const void *dout, int64_t dout_stride, void *dx, int64_t dx_stride,
+                                        void *dweight, float *dbias, void *workspace, uint64_t workspace_bytes);
+
+/*
+ * The tensor-core kernels of deamoe_ffn and deamoe_product wait in bounded loops like the rest of the library.  HOST status
+ * receives DEAMOE_OK, or DEAMOE_ERR_TIMEOUT if a wait has expired on this device since the last such call (what those calls
+ * wrote is then invalid).  Synchronises the stream.
+ */
+deamoe_status_t deamoe_operator_status(void *cuda_stream, int32_t *status);
 
 /*
  * Measurement aid.  (The paper has no counterpart.)  Enqueues one kernel that reads `bytes` bytes

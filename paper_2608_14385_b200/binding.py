@@ -17,7 +17,7 @@ OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALLOC, ERR_CUDA, ERR_BATCH, ERR_TIMEOU
 DENSE_MIN_BATCH = 32   # calls of this many tokens and more take the dense schedule under SCHED_AUTO (csrc/dense.cuh) ...
 DENSE_SMALL_ROUTER = 64  # ... twice as many on layers of fewer experts than this
 
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
 SIGMA_NONE, SIGMA_SILU, SIGMA_GELU, SIGMA_RMSNORM = 0, 1, 2, 3
 SCHED_AUTO, SCHED_PLAIN, SCHED_STAGED, SCHED_FUSED, SCHED_DENSE = 0, 1, 2, 3, 4
 
@@ -36,7 +36,9 @@ SYMBOLS = ("deamoe_layer_create", "deamoe_vanilla_create", "deamoe_layer_destroy
            "deamoe_last_launches", "deamoe_device_bytes", "deamoe_status_string",
            "deamoe_sort_workspace", "deamoe_sort_pairs", "deamoe_dispatch", "deamoe_dispatch_backward", "deamoe_combine",
            "deamoe_combine_backward", "deamoe_norm_workspace", "deamoe_norm", "deamoe_norm_backward",
-           "deamoe_norm_residual", "deamoe_norm_residual_backward", "deamoe_quant_workspace", "deamoe_quant_product")
+           "deamoe_norm_residual", "deamoe_norm_residual_backward", "deamoe_quant_workspace", "deamoe_quant_product",
+           "deamoe_norm_quant", "deamoe_norm_residual_quant", "deamoe_ffn_workspace", "deamoe_ffn", "deamoe_ffn_backward",
+           "deamoe_product_workspace", "deamoe_product", "deamoe_product_backward", "deamoe_operator_status")
 
 GATE_NONE, GATE_CHANNEL, GATE_TOKEN, GATE_FULL = 0, 1, 2, 3
 
@@ -112,7 +114,16 @@ def lib():
                 ("deamoe_norm_residual_backward", i, (p, i, p, l, p, l, i, i, i, i, p, f, i, p, l, f, f, p, l, p, f, p, l,
                                                       p, l, p, l, p, l, p, p, p, u)),
                 ("deamoe_quant_workspace", u, (i, i, i)),
-                ("deamoe_quant_product", i, (p, i, p, i, p, p, i, i, i, i, p, l, i, p, p, i, i, i, p, l, p, u))):
+                ("deamoe_quant_product", i, (p, i, p, i, p, p, i, i, i, i, p, l, i, p, p, i, i, i, p, l, p, u)),
+                ("deamoe_norm_quant", i, (p, i, p, l, i, i, i, i, p, f, p, l, p)),
+                ("deamoe_norm_residual_quant", i, (p, i, p, l, p, l, i, i, i, i, p, f, i, p, l, f, f, p, l, p, f, p, l, p)),
+                ("deamoe_ffn_workspace", u, (i, i, i)),
+                ("deamoe_ffn", i, (p, p, l, p, p, p, i, i, i, i, p, l, p, u)),
+                ("deamoe_ffn_backward", i, (p, p, l, p, p, p, l, p, i, i, i, i, p, l, p, p, p, u)),
+                ("deamoe_product_workspace", u, (i, i, i)),
+                ("deamoe_product", i, (p, i, p, l, p, i, p, p, i, i, i, p, i, p, l, p, l)),
+                ("deamoe_product_backward", i, (p, i, p, l, i, p, i, i, i, p, i, p, l, p, l, p, p, p, u)),
+                ("deamoe_operator_status", i, (p, C.POINTER(C.c_int32)))):
             getattr(L, name).restype = res
             getattr(L, name).argtypes = args
         _lib = L
@@ -516,6 +527,172 @@ def quant_product(codes, scales, x, group, zeros=None, expert_off=None, row_pair
                                  _vec(scales, where, "scales", scales.dtype, (E, n_out, groups), dev), pz, E, n_out, n_in, group, px,
                                  sx, T, pe, pp, pairs_per_token, R, 1 if swiglu else 0, po, so, _ptr(ws), need), where)
     return out
+
+
+def norm_quant(x, weight, eps, normalise=True, codes=None, scale=None):
+    """The norm of x in 8 bits (deamoe_norm_quant): codes (torch.float8_e4m3fn [T, h]) and a scale a row (float32 [T]) with
+    x / rms(x) weight = codes * scale.  normalise=False leaves the norm away: any rows in 8 bits."""
+    where, dev = "deamoe_norm_quant", _device()
+    dt = _type(x, where, "x")
+    T, h = x.shape
+    if codes is None:
+        codes = x.new_empty((T, h), dtype=torch.float8_e4m3fn)
+    if scale is None:
+        scale = x.new_empty(T, dtype=torch.float32)
+    px, sx = _mat(x, where, "x", x.dtype, T, h, dev)
+    pc, sc = _mat(codes, where, "codes", torch.float8_e4m3fn, T, h, dev)
+    pw, wdt = _gain(weight, where, "weight", h, dev)
+    _done(lib().deamoe_norm_quant(_raw_stream(dev), dt, px, sx, T, h, 1 if normalise else 0, wdt, pw, eps, pc, sc,
+                                  _vec(scale, where, "scale", torch.float32, (T,), dev)), where)
+    return codes, scale
+
+
+def norm_residual_quant(x, y, weight, eps, gate=None, residual_scale=1.0, branch_scale=1.0, normalise=True, next_weight=None,
+                        next_eps=None, gate_kind=None, out=None, codes=None, scale=None):
+    """`norm_residual` with the next norm in 8 bits (deamoe_norm_residual_quant): returns s, and codes and scale of
+    s / rms(s) next_weight as `norm_quant` gives them."""
+    where, dev = "deamoe_norm_residual_quant", _device()
+    dt = _type(x, where, "x")
+    T, h = x.shape
+    if out is None:
+        out = torch.empty_like(x)
+    if codes is None:
+        codes = x.new_empty((T, h), dtype=torch.float8_e4m3fn)
+    if scale is None:
+        scale = x.new_empty(T, dtype=torch.float32)
+    px, sx = _mat(x, where, "x", x.dtype, T, h, dev)
+    py, sy = _mat(y, where, "y", x.dtype, T, h, dev)
+    po, so = _mat(out, where, "out", x.dtype, T, h, dev)
+    pc, sc = _mat(codes, where, "codes", torch.float8_e4m3fn, T, h, dev)
+    pw, wdt = _gain(weight, where, "weight", h, dev, next_weight)
+    pm, _ = _gain(next_weight, where, "next_weight", h, dev, weight)
+    kind, pg, sg = _gate(gate, where, x.dtype, T, h, gate_kind, dev)
+    _done(lib().deamoe_norm_residual_quant(_raw_stream(dev), dt, px, sx, py, sy, T, h, 1 if normalise else 0, wdt, pw, eps, kind,
+                                           pg, sg, residual_scale, branch_scale, po, so, pm,
+                                           eps if next_eps is None else next_eps, pc, sc,
+                                           _vec(scale, where, "scale", torch.float32, (T,), dev)), where)
+    return out, codes, scale
+
+
+def _ffn_operands(x, w_gate_up, w_down, expert_off, where, dev):
+    """Sizes and addresses that the feed-forward calls share."""
+    if x.dim() != 2 or w_gate_up.dim() != 3 or w_down.dim() != 3:
+        _refuse(where, "x must be [R, h], w_gate_up [E, 2 f, h], w_down [E, h, f]")
+    R, h = x.shape
+    E, _, f = w_down.shape
+    if E > _INT_MAX or f > _INT_MAX:
+        _refuse(where, f"{E} experts, ffn {f}")
+    px, sx = _mat(x, where, "x", torch.bfloat16, R, h, dev)
+    return (R, h, E, f, px, sx, _vec(w_gate_up, where, "w_gate_up", torch.bfloat16, (E, 2 * f, h), dev),
+            _vec(w_down, where, "w_down", torch.bfloat16, (E, h, f), dev),
+            _vec(expert_off, where, "expert_off", torch.int32, (E + 1,), dev) if expert_off is not None else None)
+
+
+def ffn(x, w_gate_up, w_down, expert_off=None, out=None):
+    """Rows in expert order through their experts' gated blocks, (SiLU(x Wg^T) * (x Wu^T)) Wd^T (deamoe_ffn): x bf16 [R, h] as
+    `dispatch` gives it, w_gate_up [E, 2 f, h], w_down [E, h, f], expert_off as `sort_pairs` gives it (None: one expert).
+    Rows behind the last expert's are left as they were (uninitialised if out was made here)."""
+    where, dev = "deamoe_ffn", _device()
+    R, h, E, f, px, sx, pu, pd, pe = _ffn_operands(x, w_gate_up, w_down, expert_off, where, dev)
+    if out is None:
+        out = x.new_empty((R, h))
+    po, so = _mat(out, where, "out", torch.bfloat16, R, h, dev)
+    L = lib()
+    need = L.deamoe_ffn_workspace(R, f, 0)
+    ws = _workspace(need, x)
+    _done(L.deamoe_ffn(_raw_stream(dev), px, sx, pu, pd, pe, E, R, h, f, po, so, _ptr(ws), need), where)
+    return out
+
+
+def ffn_backward(x, w_gate_up, w_down, dout, expert_off=None, dx=None, dw_gate_up=None, dw_down=None):
+    """Gradients of `ffn` from its inputs and dout: dx (rows behind the last expert's as in `ffn`), dw_gate_up, dw_down
+    (deamoe_ffn_backward)."""
+    where, dev = "deamoe_ffn_backward", _device()
+    R, h, E, f, px, sx, pu, pd, pe = _ffn_operands(x, w_gate_up, w_down, expert_off, where, dev)
+    if dx is None:
+        dx = x.new_empty((R, h))
+    if dw_gate_up is None:
+        dw_gate_up = torch.empty_like(w_gate_up)
+    if dw_down is None:
+        dw_down = torch.empty_like(w_down)
+    po, so = _mat(dout, where, "dout", torch.bfloat16, R, h, dev)
+    pg, sg = _mat(dx, where, "dx", torch.bfloat16, R, h, dev)
+    L = lib()
+    need = L.deamoe_ffn_workspace(R, f, 1)
+    ws = _workspace(need, x)
+    _done(L.deamoe_ffn_backward(_raw_stream(dev), px, sx, pu, pd, po, so, pe, E, R, h, f, pg, sg,
+                                _vec(dw_gate_up, where, "dw_gate_up", torch.bfloat16, (E, 2 * f, h), dev),
+                                _vec(dw_down, where, "dw_down", torch.bfloat16, (E, h, f), dev), _ptr(ws), need), where)
+    return dx, dw_gate_up, dw_down
+
+
+def _product_operands(x, weight, bias, act, where, dev):
+    """Sizes, types and addresses that the product calls share."""
+    if x.dim() != 2 or weight.dim() != 2:
+        _refuse(where, "x must be [T, n_in], weight [n_out, n_in]")
+    T, K = x.shape
+    N = weight.shape[0]
+    if N > _INT_MAX or act not in (SIGMA_NONE, SIGMA_SILU, SIGMA_GELU):
+        _refuse(where, f"{N} outputs, activation {act}")
+    px, sx = _mat(x, where, "x", x.dtype, T, K, dev)
+    bdt = F32
+    if bias is not None:
+        bdt = _TYPES.get(bias.dtype)
+        if bdt is None:
+            _refuse(where, "bias must be float32 or bfloat16")
+    return (T, K, N, px, sx, _vec(weight, where, "weight", x.dtype, (N, K), dev), bdt,
+            _vec(bias, where, "bias", bias.dtype, (N,), dev) if bias is not None else None)
+
+
+def product(x, weight, bias=None, act=SIGMA_NONE, residual=None, x_scale=None, weight_scale=None, out=None):
+    """act(x weight^T + bias) + residual in bf16 (deamoe_product): x [T, n_in] and weight [n_out, n_in] bfloat16, or both
+    torch.float8_e4m3fn with x_scale [T] and weight_scale [n_out] float32 (as `norm_quant` gives rows and scales); bias [n_out]
+    float32 or bfloat16; act SIGMA_NONE, SIGMA_SILU or SIGMA_GELU; residual [T, n_out] bfloat16 (out may be it)."""
+    where, dev = "deamoe_product", _device()
+    dt = {torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}.get(x.dtype)
+    if dt is None:
+        _refuse(where, f"x must be bfloat16 or float8_e4m3fn, got {x.dtype}")
+    T, K, N, px, sx, pw, bdt, pb = _product_operands(x, weight, bias, act, where, dev)
+    if (x_scale is None) != (dt == BF16) or (weight_scale is None) != (dt == BF16):
+        _refuse(where, "x_scale and weight_scale belong to float8_e4m3fn operands, and only to them")
+    if out is None:
+        out = x.new_empty((T, N), dtype=torch.bfloat16)
+    po, so = _mat(out, where, "out", torch.bfloat16, T, N, dev)
+    pr, sr = _mat(residual, where, "residual", torch.bfloat16, T, N, dev) if residual is not None else (None, 0)
+    psx = _vec(x_scale, where, "x_scale", torch.float32, (T,), dev) if x_scale is not None else None
+    psw = _vec(weight_scale, where, "weight_scale", torch.float32, (N,), dev) if weight_scale is not None else None
+    _done(lib().deamoe_product(_raw_stream(dev), dt, px, sx, psx, T, pw, psw, N, K, bdt, pb, act, pr, sr, po, so), where)
+    return out
+
+
+def product_backward(x, weight, dout, bias=None, act=SIGMA_NONE, dx=None, dweight=None):
+    """Gradients of `product` (bfloat16) from its inputs and dout: dx, dweight, and dbias (float32, None without a bias); the
+    residual's is dout itself (deamoe_product_backward)."""
+    where, dev = "deamoe_product_backward", _device()
+    if x.dtype is not torch.bfloat16:
+        _refuse(where, f"x must be bfloat16, got {x.dtype}")
+    T, K, N, px, sx, pw, bdt, pb = _product_operands(x, weight, bias, act, where, dev)
+    if dx is None:
+        dx = x.new_empty((T, K))
+    if dweight is None:
+        dweight = torch.empty_like(weight)
+    dbias = x.new_empty(N, dtype=torch.float32) if bias is not None else None
+    po, so = _mat(dout, where, "dout", torch.bfloat16, T, N, dev)
+    pd, sd = _mat(dx, where, "dx", torch.bfloat16, T, K, dev)
+    L = lib()
+    need = L.deamoe_product_workspace(T, N, act)
+    ws = _workspace(need, x)
+    _done(L.deamoe_product_backward(_raw_stream(dev), BF16, px, sx, T, pw, N, K, bdt, pb, act, po, so, pd, sd,
+                                    _vec(dweight, where, "dweight", torch.bfloat16, (N, K), dev), _ptr(dbias), _ptr(ws), need), where)
+    return dx, dweight, dbias
+
+
+def operator_status():
+    """OK, or ERR_TIMEOUT if a bounded wait of the tensor-core kernels of `ffn` and `product` has expired on the current device
+    since the last call (deamoe_operator_status; synchronises the current stream)."""
+    status = C.c_int32()
+    _done(lib().deamoe_operator_status(_stream(), C.byref(status)), "deamoe_operator_status")
+    return status.value
 
 
 class Layer:

@@ -1,0 +1,128 @@
+// Gated feed-forward blocks of experts over rows in expert order (or of one expert), and their gradients.
+//
+//   g = x Wg^T, u = x Wu^T, h = silu(g) u, y = h Wd^T
+//   dh = dy Wd,  dg = dh u s (1 + g (1 - s)),  du = dh silu(g),  s = sigmoid(g)
+//   dx = dg Wg + du Wu,  d[Wg; Wu] = [dg du]^T x,  dWd = dy^T h
+//
+// Two launches forward: gate and up as one product whose epilogue forms h, then the down product.  h is rounded to bf16 between
+// them (the tensor cores' operand; half a step of bf16 beside that of the output).  Five launches backward: dh (kept in fp32),
+// gate and up once more from the forward's inputs with an epilogue that turns them and dh into dg, du and h (each rounded
+// once, as operands), dx, and the two weight gradients.  The backward call takes the forward's inputs and keeps nothing of the
+// forward pass: gate and up would cost 4 bytes a value to keep exactly, and recomputing them lets no rounding but the
+// operands' into a gradient.
+#include "matmul.cuh"
+
+namespace deamoe {
+
+static uint64_t ceil256(uint64_t v) { return (v + 255) / 256 * 256; }
+
+struct FfnShape {
+  int E, R, h, f;
+  const int32_t* off;
+};
+
+static MatmulCall ffn_call(const FfnShape& S, int M, int K) {
+  MatmulCall c = {};
+  c.args.M = M; c.args.K = K; c.args.N = S.R; c.args.groups = S.E; c.args.off = S.off; c.args.tile_n = MM_N; c.args.chunk = 64;
+  c.args.f = S.f; c.args.wide = 1;
+  return c;
+}
+
+static deamoe_status_t check_ffn(const void* x, int64_t xs, const void* wgu, const void* wd, const int32_t* off, int E, int R, int h, int f) {
+  if (E <= 0 || h <= 0 || f <= 0 || (!off && E != 1)) return DEAMOE_ERR_INVALID_ARG;
+  if (E > DEAMOE_MAX_EXPERTS || h > DEAMOE_MAX_WIDTH || f > DEAMOE_MAX_WIDTH || h % 8 || f % 8) return DEAMOE_ERR_UNSUPPORTED;
+  if (R < 0) return DEAMOE_ERR_BATCH;
+  // tiles are counted in 32 bits: a group has at most one tile more than its share of the rows
+  const int64_t most = (int64_t)R / MM_N + E, wide = (int64_t)(2 * (int64_t)f > h ? 2 * (int64_t)f : h) / 128 + 1;
+  if (most * wide > INT32_MAX) return DEAMOE_ERR_BATCH;
+  if (!wgu || !wd || !aligned16(wgu) || !aligned16(wd) || !aligned_to(off, 4)) return DEAMOE_ERR_INVALID_ARG;
+  if (R > 0 && (!x || !aligned16(x) || xs < h || xs % 8)) return DEAMOE_ERR_INVALID_ARG;
+  return DEAMOE_OK;
+}
+static bool bad_rows8(const void* p, int64_t stride, int h) { return !p || !aligned16(p) || stride < h || stride % 8; }
+
+}  // namespace deamoe
+
+using namespace deamoe;
+
+extern "C" {
+
+uint64_t deamoe_ffn_workspace(int32_t n_rows, int32_t ffn, int32_t backward) {
+  if (n_rows <= 0 || ffn <= 0) return 0;
+  const uint64_t v = (uint64_t)n_rows * ffn;
+  return backward ? ceil256(4 * v) + ceil256(4 * v) + ceil256(2 * v) : ceil256(2 * v);
+}
+
+deamoe_status_t deamoe_ffn(void* cuda_stream, const void* x, int64_t x_stride, const void* w_gate_up, const void* w_down,
+                           const int32_t* expert_off, int32_t n_expert, int32_t n_rows, int32_t hidden, int32_t ffn, void* out,
+                           int64_t out_stride, void* workspace, uint64_t workspace_bytes) {
+  deamoe_status_t st = check_ffn(x, x_stride, w_gate_up, w_down, expert_off, n_expert, n_rows, hidden, ffn);
+  if (st != DEAMOE_OK || n_rows == 0) return st;
+  if (bad_rows8(out, out_stride, hidden) || out == x) return DEAMOE_ERR_INVALID_ARG;
+  if (!workspace || !aligned16(workspace) || workspace_bytes < deamoe_ffn_workspace(n_rows, ffn, 0)) return DEAMOE_ERR_INVALID_ARG;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const FfnShape S = {n_expert, n_rows, hidden, ffn, expert_off};
+  MatmulCall up = ffn_call(S, ffn, hidden), down = ffn_call(S, hidden, ffn);
+  up.args.out = workspace; up.args.os = ffn;
+  down.args.out = out; down.args.os = out_stride;
+  if (!map_gate_up(&up.maps.a, w_gate_up, hidden, ffn, n_expert) || !map_b(&up.maps, x, 2, hidden, n_rows, x_stride) ||
+      !map_rows(&down.maps.a, w_down, 2, ffn, hidden, ffn, n_expert, (int64_t)hidden * ffn, 128) ||
+      !map_b(&down.maps, workspace, 2, ffn, n_rows, ffn))
+    return DEAMOE_ERR_CUDA;
+  if (matmul_launch(MF_SWIGLU, up, s, false) == cudaSuccess && matmul_launch(MF_STORE, down, s, true) == cudaSuccess) return DEAMOE_OK;
+  cudaGetLastError();
+  return DEAMOE_ERR_CUDA;
+}
+
+deamoe_status_t deamoe_ffn_backward(void* cuda_stream, const void* x, int64_t x_stride, const void* w_gate_up, const void* w_down,
+                                    const void* dout, int64_t dout_stride, const int32_t* expert_off, int32_t n_expert,
+                                    int32_t n_rows, int32_t hidden, int32_t ffn, void* dx, int64_t dx_stride, void* dw_gate_up,
+                                    void* dw_down, void* workspace, uint64_t workspace_bytes) {
+  deamoe_status_t st = check_ffn(x, x_stride, w_gate_up, w_down, expert_off, n_expert, n_rows, hidden, ffn);
+  if (st != DEAMOE_OK) return st;
+  if (!dw_gate_up || !dw_down || !aligned16(dw_gate_up) || !aligned16(dw_down) || dw_gate_up == w_gate_up || dw_down == w_down ||
+      dw_gate_up == dw_down)
+    return DEAMOE_ERR_INVALID_ARG;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const size_t wd_bytes = (size_t)n_expert * hidden * ffn * 2;
+  if (n_rows == 0)  // sums over no rows
+    return cudaMemsetAsync(dw_gate_up, 0, 2 * wd_bytes, s) == cudaSuccess && cudaMemsetAsync(dw_down, 0, wd_bytes, s) == cudaSuccess
+               ? DEAMOE_OK : DEAMOE_ERR_CUDA;
+  if (bad_rows8(dout, dout_stride, hidden) || bad_rows8(dx, dx_stride, hidden) || dx == x || dx == dout) return DEAMOE_ERR_INVALID_ARG;
+  if (!workspace || !aligned16(workspace) || workspace_bytes < deamoe_ffn_workspace(n_rows, ffn, 1)) return DEAMOE_ERR_INVALID_ARG;
+  const FfnShape S = {n_expert, n_rows, hidden, ffn, expert_off};
+  const uint64_t v = (uint64_t)n_rows * ffn;
+  char* ws = reinterpret_cast<char*>(workspace);
+  float* dh = reinterpret_cast<float*>(ws);
+  void* dgu = ws + ceil256(4 * v);
+  void* hh = ws + 2 * ceil256(4 * v);
+  const int64_t wd_one = (int64_t)hidden * ffn;
+
+  MatmulCall a = ffn_call(S, ffn, hidden);  // dh = dy Wd
+  a.args.out = dh; a.args.os = ffn;
+  MatmulCall b = ffn_call(S, ffn, hidden);  // gate, up -> dg, du, h
+  b.args.out = dgu; b.args.os = 2 * (int64_t)ffn; b.args.dh = dh; b.args.h_out = hh;
+  MatmulCall c = ffn_call(S, hidden, 2 * ffn);  // dx = [dg du] [Wg; Wu]
+  c.args.out = dx; c.args.os = dx_stride;
+  MatmulCall d = ffn_call(S, hidden, n_rows);  // d[Wg; Wu] = [dg du]^T x
+  d.args.N = 2 * ffn; d.args.out = dw_gate_up; d.args.os = hidden; d.args.out_group = 2 * wd_one;
+  MatmulCall e = ffn_call(S, ffn, n_rows);  // dWd = dy^T h
+  e.args.N = hidden; e.args.out = dw_down; e.args.os = ffn; e.args.out_group = wd_one;
+  if (!map_rows(&a.maps.a, w_down, 2, ffn, hidden, ffn, n_expert, wd_one, 64) || !map_b(&a.maps, dout, 2, hidden, n_rows, dout_stride) ||
+      !map_gate_up(&b.maps.a, w_gate_up, hidden, ffn, n_expert) || !map_b(&b.maps, x, 2, hidden, n_rows, x_stride) ||
+      !map_rows(&c.maps.a, w_gate_up, 2, hidden, 2 * (int64_t)ffn, hidden, n_expert, 2 * wd_one, 64) ||
+      !map_b(&c.maps, dgu, 2, 2 * (int64_t)ffn, n_rows, 2 * (int64_t)ffn) ||
+      !map_rows(&d.maps.a, x, 2, hidden, n_rows, x_stride, 1, x_stride, 64) ||
+      !map_rows(&d.maps.b[0], dgu, 2, 2 * (int64_t)ffn, n_rows, 2 * (int64_t)ffn, 1, 2 * (int64_t)ffn, 64) ||
+      !map_rows(&e.maps.a, hh, 2, ffn, n_rows, ffn, 1, ffn, 64) ||
+      !map_rows(&e.maps.b[0], dout, 2, hidden, n_rows, dout_stride, 1, dout_stride, 64))
+    return DEAMOE_ERR_CUDA;
+  if (matmul_launch(MF_F32_TRANSPOSED, a, s, false) == cudaSuccess && matmul_launch(MF_SWIGLU_GRAD, b, s, true) == cudaSuccess &&
+      matmul_launch(MF_STORE_TRANSPOSED, c, s, true) == cudaSuccess && matmul_launch(MF_WEIGHT_GRAD, d, s, true) == cudaSuccess &&
+      matmul_launch(MF_WEIGHT_GRAD, e, s, true) == cudaSuccess)
+    return DEAMOE_OK;
+  cudaGetLastError();
+  return DEAMOE_ERR_CUDA;
+}
+
+}  // extern "C"

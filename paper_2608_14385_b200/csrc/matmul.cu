@@ -1,0 +1,634 @@
+// The tensor-core kernel behind the operators around a layer; what it computes and why it is laid out so: matmul.cuh.
+#include "matmul.cuh"
+
+#include <atomic>
+
+namespace deamoe {
+
+namespace {
+
+constexpr int MM_STAGES = 6;
+constexpr int MM_OPERAND = 16 * 1024;          // one CTA's part of a chunk of A or of B: 128 rows of 128 bytes
+constexpr int MM_STAGE = 2 * MM_OPERAND;
+constexpr int MM_WARP_COPY = 4, MM_WARP_MMA = 5, MM_WARP_CLEAR = 6;
+constexpr int MM_THREADS = 7 * 32;
+constexpr int MM_EPI = 128;                    // threads of the epilogue
+constexpr int MM_COLS = 16;                    // accumulator columns of an epilogue step
+constexpr int MM_PITCH = 128 + 4;              // floats of a row of the transposing buffer
+constexpr int MM_STAGING = 2 * MM_COLS * MM_PITCH * 4;
+constexpr int MM_CONTROL = 512;
+constexpr int MM_TABLE = (DEAMOE_MAX_EXPERTS + 1) * 8 + 8;  // groups' first tile and first row
+constexpr size_t MM_SMEM = (size_t)MM_STAGES * MM_STAGE + MM_STAGING + MM_CONTROL + MM_TABLE;
+static_assert(MM_SMEM <= 227 * 1024, "shared memory budget");
+// One CTA fills more than half of an SM's shared memory, so none of another grid's can be beside it and the
+// allocation of all 512 columns of tensor memory never waits.
+static_assert(2 * MM_SMEM > 228 * 1024, "tensor-memory allocation must never block");
+constexpr unsigned long long MM_WAIT_NS = 2000000000ull;  // after which a wait gives up (the longest contraction takes some 10 ms)
+constexpr int MM_PAIRS = 74;                   // 148 SMs
+
+__device__ int32_t mm_status;                  // DEAMOE_ERR_TIMEOUT once a wait has expired
+
+// ---------------------------------------------------------------- PTX
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ uint32_t cluster_rank() {
+  uint32_t r;
+  asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+  return r;
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t in_first(uint32_t addr) {  // the same shared address in the pair's first CTA
+  uint32_t r;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+  return r;
+}
+__device__ __forceinline__ void bar_init(uint32_t bar, uint32_t count) {
+  asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count));
+}
+__device__ __forceinline__ void bar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void bar_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
+  uint32_t done;
+  asm volatile(
+      "{\n.reg .pred p;\nmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\nselp.u32 %0, 1, 0, p;\n}"
+      : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+  return done != 0;
+}
+__device__ __forceinline__ unsigned long long now_ns() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+  return t;
+}
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  if (bar_try(bar, parity)) return true;
+  const unsigned long long start = now_ns();
+  for (unsigned it = 1;; ++it) {
+    if (bar_try(bar, parity)) return true;
+    if ((it & 63u) == 0 && *abort_flag) return false;
+    if ((it & 255u) == 0 && now_ns() - start > MM_WAIT_NS) break;
+  }
+  *abort_flag = 1;
+  return false;
+}
+// `bar` may lie in the pair's other CTA
+__device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap* m, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void load_5d(uint32_t dst, const CUtensorMap* m, int x, int y, int z, int u, int v, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(u), "r"(v), "r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// Shared-memory operand with 128-byte swizzle.  k inner: 8 rows of 128 bytes are a block of 1024 bytes, `sbo` apart.
+// Rows inner: a block is 64 values of 8 k's; `sbo` between blocks along k, `lbo` between blocks along the rows.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, uint32_t lbo, uint32_t sbo) {
+  return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)(lbo >> 4) << 16 | (uint64_t)(sbo >> 4) << 32 | 1ull << 46 | 2ull << 61;
+}
+template <bool FP8> __device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t add) {
+  if constexpr (FP8)
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+  else
+    asm volatile("{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\ntcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+// arrives at the barrier of that offset in both CTAs once the MMAs issued so far are done
+__device__ __forceinline__ void commit_pair(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+               ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+      : "r"(addr));
+}
+__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+
+// ---------------------------------------------------------------- the order of the tiles
+struct Tile {
+  int group;
+  int m0, n0;    // first row of A in the group; first row of B: in all rows (grouped rows) or in the group
+  int n, valid;  // width (a multiple of 32), and its columns that exist
+  int row0, rows;  // the group's rows (ragged contraction)
+  int n_index;   // index of the tile along N in its group
+};
+// Tiles of group e: columns are dealt evenly, so that a group a little above a multiple of the widest tile has no sliver.
+__device__ __forceinline__ int tiles_along(int n, int widest) { return (n + widest - 1) / widest; }
+constexpr int MM_BAND = 8;  // tiles along N that are walked side by side: 74 pairs then share some 8 + 9 operand tiles in the L2
+
+template <bool RAGGED> __device__ __forceinline__ Tile find_tile(const MatmulArgs& A, const int* first_tile, const int* first_row, int t,
+                                                                 int m_step) {
+  int lo = 0, hi = A.groups;  // the group whose range of tiles holds t
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first_tile[mid] <= t) lo = mid;
+    else hi = mid;
+  }
+  Tile o;
+  o.group = lo;
+  o.row0 = first_row[lo];
+  o.rows = first_row[lo + 1] - o.row0;
+  const int cols = RAGGED ? A.N : o.rows;
+  const int nt = tiles_along(cols, A.tile_n), mt = (A.M + m_step - 1) / m_step;
+  const int r = t - first_tile[lo];
+  const int band = r / (MM_BAND * mt), rest = r - band * MM_BAND * mt;
+  const int width = min(MM_BAND, nt - band * MM_BAND);
+  const int mi = rest / width, ni = band * MM_BAND + rest - mi * width;
+  const int per = (cols + nt - 1) / nt;
+  o.n = (per + 31) & ~31;
+  o.m0 = mi * m_step;
+  o.n_index = ni;
+  o.valid = min(o.n, cols - ni * o.n);
+  o.n0 = ni * o.n + (RAGGED ? 0 : o.row0);
+  return o;
+}
+
+// ---------------------------------------------------------------- epilogue arithmetic
+__device__ __forceinline__ float sigmoid(float v) { return 1.f / (1.f + __expf(-v)); }
+__device__ __forceinline__ float act_grad(int kind, float z) {
+  if (kind == DEAMOE_SIGMA_SILU) {
+    const float p = sigmoid(z);
+    return p * (1.f + z * (1.f - p));
+  }
+  if (kind == DEAMOE_SIGMA_GELU)
+    return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * __expf(-0.5f * z * z) * 0.39894228040143268f;
+  return 1.f;
+}
+// n <= 8 bf16 values at p; wide: all eight, 16 bytes at once
+__device__ __forceinline__ void put8(__nv_bfloat16* p, const float (&v)[8], int n, bool wide) {
+  if (wide && n == 8) {
+    Pack<__nv_bfloat16, 8> o;
+    o.narrow(v);
+    store_pack(p, o);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (j < n) p[j] = __float2bfloat16_rn(v[j]);
+  }
+}
+__device__ __forceinline__ void get8(const __nv_bfloat16* p, float (&v)[8], int n, bool wide) {
+  if (wide && n == 8) {
+    load_once<__nv_bfloat16, 8>(p).widen(v);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = j < n ? __bfloat162float(p[j]) : 0.f;
+  }
+}
+__device__ __forceinline__ void floats8(const float* p, float (&v)[8]) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+}
+__device__ __forceinline__ float gain(const void* p, int f32, int i) {
+  return f32 ? reinterpret_cast<const float*>(p)[i] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[i]);
+}
+
+// ---------------------------------------------------------------- the kernel
+// AT / BT: A / B lies with its rows as the inner axis (k outer); RAGGED: the contraction runs over a group's rows.
+template <int EPI, bool AT, bool BT, bool FP8, bool RAGGED>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
+    k_matmul(const __grid_constant__ MatmulArgs A, const __grid_constant__ MatmulMaps maps) {
+  constexpr bool DUAL = EPI == ME_SWIGLU || EPI == ME_SWIGLU_GRAD;  // A's rows alternate gate and up
+  constexpr int M_STEP = DUAL ? MM_M / 2 : MM_M;                    // in rows of A as the caller counts them (DUAL: features)
+  extern __shared__ __align__(1024) unsigned char smem[];
+  float* staging = reinterpret_cast<float*>(smem + (size_t)MM_STAGES * MM_STAGE);
+  uint64_t* control = reinterpret_cast<uint64_t*>(smem + (size_t)MM_STAGES * MM_STAGE + MM_STAGING);
+  const uint32_t ring = smem_u32(smem), bars = smem_u32(control);
+  auto full = [&](int s) { return bars + 8 * s; };
+  auto empty = [&](int s) { return bars + 8 * (MM_STAGES + s); };
+  auto tail = [&](int s) { return bars + 8 * (2 * MM_STAGES + s); };
+  auto acc_full = [&](int b) { return bars + 8 * (3 * MM_STAGES + b); };
+  auto acc_empty = [&](int b) { return bars + 8 * (3 * MM_STAGES + 2 + b); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(control + 3 * MM_STAGES + 4);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  int* warp_sums = reinterpret_cast<int*>(tmem_slot + 2);
+  static_assert((3 * MM_STAGES + 4) * 8 + 8 + 8 * 4 <= MM_CONTROL, "control region");
+  int* first_row = reinterpret_cast<int*>(smem + (size_t)MM_STAGES * MM_STAGE + MM_STAGING + MM_CONTROL);
+  int* first_tile = first_row + A.groups + 1;
+
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = cluster_rank();
+  if (tid == 0) {
+    for (int s = 0; s < MM_STAGES; ++s) {
+      bar_init(full(s), RAGGED ? 2 : 1);
+      bar_init(empty(s), 1);
+      bar_init(tail(s), 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      bar_init(acc_full(b), 1);
+      bar_init(acc_empty(b), 8);
+    }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == MM_WARP_MMA) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  pdl_wait();
+  pdl_trigger();
+  // groups' rows (offsets outside the range count as its ends) and their tiles; offsets that decrease: no tile at all
+  const int mt = (A.M + M_STEP - 1) / M_STEP;
+  bool falls = false;
+  const int limit = RAGGED ? A.K : A.N;
+  for (int e = tid; e <= A.groups; e += MM_THREADS) {
+    if (A.off) {
+      const int o = A.off[e];
+      if (e > 0) falls |= o < A.off[e - 1];
+      first_row[e] = min(max(o, 0), limit);
+    } else {
+      first_row[e] = e == 0 ? 0 : limit;
+    }
+  }
+  falls = __syncthreads_or(falls);
+  for (int e = tid; e < A.groups; e += MM_THREADS)
+    first_tile[e] = falls ? 0 : mt * tiles_along(RAGGED ? A.N : first_row[e + 1] - first_row[e], A.tile_n);
+  __syncthreads();
+  block_exclusive_scan(first_tile, A.groups, warp_sums);
+  tc_before();
+  cluster_sync();
+  tc_after();
+  const uint32_t tmem = *tmem_slot;
+  const int tiles = first_tile[A.groups];
+  const int pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
+  auto chunks_of = [&](const Tile& t) { return ((RAGGED ? t.rows : A.K) + A.chunk - 1) / A.chunk; };
+
+  if (warp == MM_WARP_COPY) {
+    // ============================================================ copies
+    if (lane == 0) {
+      uint32_t g = 0;
+      bool ok = true;
+      for (int it = pair; ok && it < tiles; it += pairs) {
+        const Tile t = find_tile<RAGGED>(A, first_tile, first_row, it, M_STEP);
+        const int half = t.n / 2, chunks = chunks_of(t);
+        const uint32_t bytes = MM_OPERAND + (BT ? MM_OPERAND : half * 128);
+        for (int c = 0; c < chunks; ++c, ++g) {
+          const int s = g % MM_STAGES;
+          if (!bar_wait(empty(s), ((g / MM_STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+          const uint32_t a = ring + s * MM_STAGE, b = a + MM_OPERAND;
+          uint32_t bar = in_first(full(s));
+          const int k0 = c * A.chunk;
+          if (RAGGED && k0 + A.chunk > t.rows) {  // rows of the next group come along: this CTA's clearing warp sees them first
+            bar = tail(s);
+            bar_expect(bar, bytes);
+          } else if (rank == 0) {
+            bar_expect(full(s), 2 * bytes);
+          } else if (RAGGED) {
+            bar_arrive_cluster(bar);
+          }
+          const int ka = RAGGED ? t.row0 + k0 : k0;
+          if constexpr (DUAL) {
+            load_5d(a, &maps.a, k0, 0, 0, (t.m0 + (int)rank * 64) / 8, t.group, bar);
+          } else if constexpr (AT) {
+            const int m = t.m0 + rank * 128;
+            load_3d(a, &maps.a, m, ka, RAGGED ? 0 : t.group, bar);
+            load_3d(a + MM_OPERAND / 2, &maps.a, m + 64, ka, RAGGED ? 0 : t.group, bar);
+          } else {
+            load_3d(a, &maps.a, k0, t.m0 + rank * 128, t.group, bar);
+          }
+          const int n = t.n0 + rank * half;
+          if constexpr (BT) {
+            load_3d(b, &maps.b[0], n, ka, 0, bar);
+            load_3d(b + MM_OPERAND / 2, &maps.b[0], n + 64, ka, 0, bar);
+          } else if (half == 128) {
+            load_3d(b, &maps.b[2], k0, n, 0, bar);
+          } else {
+            int r = 0;
+            if (half >= 64) {
+              load_3d(b, &maps.b[1], k0, n, 0, bar);
+              r = 64;
+            }
+            for (; r < half; r += 16) load_3d(b + r * 128, &maps.b[0], k0, n + r, 0, bar);
+          }
+        }
+      }
+      // the last commits must have arrived here before this CTA may end
+      for (uint32_t d = g > MM_STAGES ? g - MM_STAGES : 0; ok && d < g; ++d)
+        ok = bar_wait(empty(d % MM_STAGES), (d / MM_STAGES) & 1u, abort_flag);
+    }
+  } else if (warp == MM_WARP_MMA) {
+    // ============================================================ MMAs, by the pair's first CTA
+    if (rank == 0 && lane == 0) {
+      uint32_t g = 0, a = 0;
+      bool ok = true;
+      const uint64_t da = operand_desc(ring, AT ? MM_OPERAND / 2 : 16, 1024);
+      const uint64_t db = operand_desc(ring + MM_OPERAND, BT ? MM_OPERAND / 2 : 16, 1024);
+      // fp32 sums of bf16 (or e4m3: type 0) values, 256 rows, both CTAs
+      const uint32_t kind = 1u << 4 | (FP8 ? 0u : (1u << 7 | 1u << 10)) | (AT ? 1u << 15 : 0u) | (BT ? 1u << 16 : 0u) | (MM_M >> 4) << 24;
+      for (int it = pair; ok && it < tiles; it += pairs) {
+        const Tile t = find_tile<RAGGED>(A, first_tile, first_row, it, M_STEP);
+        const int chunks = chunks_of(t);
+        if (RAGGED && chunks == 0) continue;
+        const uint32_t buf = a & 1u, idesc = kind | (uint32_t)(t.n >> 3) << 17;
+        if (!bar_wait(acc_empty(buf), ((a >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+        tc_after();
+        const uint32_t d = tmem + buf * MM_N;
+        for (int c = 0; c < chunks; ++c, ++g) {
+          const int s = g % MM_STAGES;
+          if (!bar_wait(full(s), (g / MM_STAGES) & 1u, abort_flag)) { ok = false; break; }
+          tc_after();
+#pragma unroll
+          for (int k = 0; k < 4; ++k)  // 32 bytes of k; rows inner: 16 k's, two blocks of 1024 bytes
+            mma_pair<FP8>(d, da + ((s * MM_STAGE + k * (AT ? 2048 : 32)) >> 4), db + ((s * MM_STAGE + k * (BT ? 2048 : 32)) >> 4),
+                          idesc, (c | k) ? 1u : 0u);
+          commit_pair(empty(s));
+        }
+        if (ok) commit_pair(acc_full(buf));
+        ++a;
+      }
+    }
+  } else if (warp == MM_WARP_CLEAR) {
+    // ============================================================ rows behind a group's end
+    if constexpr (RAGGED) {
+      uint32_t g = 0, uses = 0;  // uses: bit s = parity of the next use of tail(s)
+      for (int it = pair; it < tiles; it += pairs) {
+        const Tile t = find_tile<RAGGED>(A, first_tile, first_row, it, M_STEP);
+        const int chunks = chunks_of(t), left = t.rows % A.chunk;
+        g += chunks;
+        if (left == 0) continue;
+        const int s = (g - 1) % MM_STAGES;
+        int ok = lane == 0 ? bar_wait(tail(s), (uses >> s) & 1u, abort_flag) : 0;
+        ok = __shfl_sync(0xffffffffu, ok, 0);
+        if (!ok) break;
+        uses ^= 1u << s;
+        unsigned char* st = smem + (size_t)s * MM_STAGE;
+        const int from = left * 8, per = 64 * 8;  // 16-byte pieces of a box: 64 rows of 128 bytes
+        for (int b = 0; b < 4; ++b)
+          for (int i = from + lane; i < per; i += 32) *reinterpret_cast<uint4*>(st + b * (MM_OPERAND / 2) + i * 16) = make_uint4(0, 0, 0, 0);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) bar_arrive_cluster(in_first(full(s)));
+      }
+    }
+  } else {
+    // ============================================================ epilogue
+    uint32_t a = 0;
+    int flip = 0;
+    bool ok = true;
+    const uint32_t lane_base = tmem + ((uint32_t)(warp * 32) << 16);
+    for (int it = pair; ok && it < tiles; it += pairs) {
+      const Tile t = find_tile<RAGGED>(A, first_tile, first_row, it, M_STEP);
+      const bool none = RAGGED && t.rows == 0;  // a group without rows: zeros
+      const uint32_t buf = a & 1u;
+      if (!none) {
+        int w = lane == 0 ? bar_wait(acc_full(buf), (a >> 1) & 1u, abort_flag) : 0;
+        ok = __shfl_sync(0xffffffffu, w, 0) != 0;
+        // all four warps or none: they meet at barriers below
+        int all;
+        asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %1, 0;\nbar.red.and.pred q, 1, 128, p;\nselp.b32 %0, 1, 0, q;\n}"
+                     : "=r"(all) : "r"((int)ok) : "memory");
+        ok = all != 0;
+        if (!ok) break;
+        tc_after();
+        ++a;
+      }
+      const int m_cta = t.m0 + (int)rank * (M_STEP / 2);
+      float sums[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) sums[j] = 0.f;
+      for (int c0 = 0; c0 < t.n; c0 += MM_COLS) {
+        float* st = staging + flip * (MM_COLS * MM_PITCH);
+        flip ^= 1;
+        uint32_t r[16];
+        if (none) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) r[i] = 0;
+        } else {
+          tmem_load(lane_base + buf * MM_N + c0, r);
+          tmem_load_wait();
+          if (c0 + MM_COLS >= t.n) {  // the accumulator has been read
+            tc_before();
+            __syncwarp();
+            if (lane == 0) bar_arrive_cluster(in_first(acc_empty(buf)));
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) st[i * MM_PITCH + warp * 32 + lane] = __uint_as_float(r[i]);
+        epilogue_sync();
+        if constexpr (DUAL) {
+          const int c = tid >> 3, q = tid & 7;  // column (row of B) of the step; block of 8 features
+          const int m = m_cta + q * 8;
+          if (c0 + c < t.valid && m < A.M) {    // (f is a multiple of 8)
+            const int64_t row = t.n0 + c0 + c;
+            float gate[8], up[8], v[8];
+            floats8(st + c * MM_PITCH + q * 16, gate);
+            floats8(st + c * MM_PITCH + q * 16 + 8, up);
+            __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(A.out) + row * A.os + m;
+            if constexpr (EPI == ME_SWIGLU) {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] = gate[j] * sigmoid(gate[j]) * up[j];
+              put8(out, v, 8, true);
+            } else {
+              float dh[8], dg[8], du[8];
+              floats8(A.dh + row * A.f + m, dh);
+#pragma unroll
+              for (int j = 0; j < 8; ++j) {
+                const float p = sigmoid(gate[j]), act = gate[j] * p;
+                v[j] = act * up[j];
+                du[j] = dh[j] * act;
+                dg[j] = dh[j] * up[j] * (p * (1.f + gate[j] * (1.f - p)));
+              }
+              put8(out, dg, 8, true);
+              put8(out + A.f, du, 8, true);
+              put8(reinterpret_cast<__nv_bfloat16*>(A.h_out) + row * A.f + m, v, 8, true);
+            }
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < MM_COLS * 16 / MM_EPI; ++i) {
+            const int c = (tid >> 4) + 8 * i, q = tid & 15;
+            const int m = m_cta + q * 8, n = min(8, A.M - m);
+            if (c0 + c < t.valid && n > 0) {
+              const int64_t row = t.n0 + c0 + c;
+              float v[8];
+              floats8(st + c * MM_PITCH + q * 8, v);
+              if constexpr (EPI == ME_STORE_F32) {
+                float4* out = reinterpret_cast<float4*>(reinterpret_cast<float*>(A.out) + row * A.os + m);
+                out[0] = make_float4(v[0], v[1], v[2], v[3]);
+                out[1] = make_float4(v[4], v[5], v[6], v[7]);
+              } else {
+                __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(A.out) + (int64_t)t.group * A.out_group + row * A.os + m;
+                if constexpr (EPI == ME_PRODUCT) {
+                  if (A.x_scale) {
+                    const float xs = A.x_scale[row];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] *= j < n ? xs * A.w_scale[m + j] : 0.f;
+                  }
+                }
+                if constexpr (EPI == ME_PRODUCT || EPI == ME_PRODUCT_GRAD) {
+                  if (A.bias) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] += j < n ? gain(A.bias, A.bias_f32, m + j) : 0.f;
+                  }
+                }
+                if constexpr (EPI == ME_PRODUCT) {
+                  if (A.act != DEAMOE_SIGMA_NONE) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = sigma_f(A.act, v[j]);
+                  }
+                  if (A.residual) {
+                    float add[8];
+                    get8(reinterpret_cast<const __nv_bfloat16*>(A.residual) + row * A.rs + m, add, n, A.wide_in);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] += add[j];
+                  }
+                }
+                if constexpr (EPI == ME_PRODUCT_GRAD) {
+                  float d[8];
+                  get8(reinterpret_cast<const __nv_bfloat16*>(A.dout) + row * A.rs + m, d, n, A.wide_in);
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) {
+                    v[j] = d[j] * act_grad(A.act, v[j]);
+                    sums[j] += v[j];
+                  }
+                }
+                put8(out, v, n, A.wide);
+              }
+            }
+          }
+        }
+      }
+      if constexpr (EPI == ME_PRODUCT_GRAD) {
+        if (A.part) {  // 8 threads hold sums of the same columns: added in their order
+          float* st = staging + flip * (MM_COLS * MM_PITCH);
+          flip ^= 1;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) st[(tid >> 4) * MM_PITCH + (tid & 15) * 8 + j] = sums[j];
+          epilogue_sync();
+          float s = 0.f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) s += st[i * MM_PITCH + tid];
+          if (m_cta + tid < A.M) A.part[(int64_t)t.n_index * A.M + m_cta + tid] = s;
+        }
+      }
+    }
+  }
+
+  // common end, also after a wait that has expired
+  tc_before();
+  __syncthreads();
+  if (*abort_flag) {
+    if (tid == 0) mm_status = DEAMOE_ERR_TIMEOUT;
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i) __nanosleep(1000);  // copies in flight land before the shared memory is given back
+  }
+  cluster_sync();
+  if (warp == MM_WARP_MMA) {
+    tc_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, 512;" ::"r"(tmem) : "memory");
+  }
+}
+
+// ---------------------------------------------------------------- host
+typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
+                             const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle,
+                             CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeFn encode_fn() {
+  static std::atomic<EncodeFn> found{nullptr};
+  EncodeFn f = found.load(std::memory_order_acquire);
+  if (!f) {
+    void* p = nullptr;
+    cudaDriverEntryPointQueryResult q = cudaDriverEntryPointSymbolNotFound;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
+        q != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      return nullptr;
+    }
+    f = reinterpret_cast<EncodeFn>(p);
+    found.store(f, std::memory_order_release);
+  }
+  return f;
+}
+bool encode(CUtensorMap* m, const void* p, int esize, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+  EncodeFn f = encode_fn();
+  if (!f) return false;
+  const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
+  return f(m, esize == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(p), dims, strides, box,
+           ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int EPI, bool AT, bool BT, bool FP8, bool RAGGED>
+cudaError_t launch(const MatmulCall& c, cudaStream_t s, bool chained) {
+  static std::atomic<uint64_t> done{0};
+  auto kernel = k_matmul<EPI, AT, BT, FP8, RAGGED>;
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
+  if (!(done.load(std::memory_order_acquire) >> dev & 1)) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MM_SMEM);
+    if (e != cudaSuccess) return e;
+    done.fetch_or(1ull << dev, std::memory_order_release);
+  }
+  if (chained) return launch_pdl(kernel, dim3(2 * MM_PAIRS), dim3(MM_THREADS), MM_SMEM, s, c.args, c.maps);
+  kernel<<<2 * MM_PAIRS, MM_THREADS, MM_SMEM, s>>>(c.args, c.maps);
+  return cudaGetLastError();
+}
+
+}  // namespace
+
+bool map_rows(CUtensorMap* m, const void* p, int esize, int64_t cols, int64_t rows, int64_t stride, int64_t groups, int64_t group_stride,
+              int box_rows) {
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)groups};
+  const cuuint64_t strides[2] = {(cuuint64_t)stride * esize, (cuuint64_t)group_stride * esize};
+  const cuuint32_t box[3] = {(cuuint32_t)(128 / esize), (cuuint32_t)box_rows, 1};
+  return encode(m, p, esize, 3, dims, strides, box);
+}
+bool map_gate_up(CUtensorMap* m, const void* p, int64_t cols, int64_t f, int64_t groups) {
+  const cuuint64_t dims[5] = {(cuuint64_t)cols, 8, 2, (cuuint64_t)f / 8, (cuuint64_t)groups};
+  const cuuint64_t strides[4] = {(cuuint64_t)cols * 2, (cuuint64_t)(f * cols) * 2, (cuuint64_t)cols * 16, (cuuint64_t)(f * cols) * 4};
+  const cuuint32_t box[5] = {64, 8, 2, 8, 1};
+  return encode(m, p, 2, 5, dims, strides, box);
+}
+bool map_b(MatmulMaps* m, const void* p, int esize, int64_t cols, int64_t rows, int64_t stride) {
+  return map_rows(&m->b[0], p, esize, cols, rows, stride, 1, stride, 16) && map_rows(&m->b[1], p, esize, cols, rows, stride, 1, stride, 64) &&
+         map_rows(&m->b[2], p, esize, cols, rows, stride, 1, stride, 128);
+}
+
+int matmul_tile_n(int64_t n, int64_t m_tiles) {
+  (void)n; (void)m_tiles;
+  return MM_N;
+}
+
+cudaError_t matmul_launch(MatmulForm form, const MatmulCall& c, cudaStream_t s, bool chained) {
+  switch (form) {
+    case MF_SWIGLU: return launch<ME_SWIGLU, false, false, false, false>(c, s, chained);
+    case MF_STORE: return launch<ME_STORE, false, false, false, false>(c, s, chained);
+    case MF_STORE_TRANSPOSED: return launch<ME_STORE, true, false, false, false>(c, s, chained);
+    case MF_F32_TRANSPOSED: return launch<ME_STORE_F32, true, false, false, false>(c, s, chained);
+    case MF_SWIGLU_GRAD: return launch<ME_SWIGLU_GRAD, false, false, false, false>(c, s, chained);
+    case MF_WEIGHT_GRAD: return launch<ME_STORE, true, true, false, true>(c, s, chained);
+    case MF_PRODUCT: return launch<ME_PRODUCT, false, false, false, false>(c, s, chained);
+    case MF_PRODUCT_E4M3: return launch<ME_PRODUCT, false, false, true, false>(c, s, chained);
+    case MF_PRODUCT_GRAD: return launch<ME_PRODUCT_GRAD, false, false, false, false>(c, s, chained);
+  }
+  return cudaErrorInvalidValue;
+}
+
+}  // namespace deamoe
+
+using namespace deamoe;
+
+extern "C" deamoe_status_t deamoe_operator_status(void* cuda_stream, int32_t* status) {
+  if (!status) return DEAMOE_ERR_INVALID_ARG;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+  int32_t got = 0;
+  void* word = nullptr;
+  if (cudaGetSymbolAddress(&word, mm_status) != cudaSuccess || cudaMemcpyAsync(&got, word, 4, cudaMemcpyDeviceToHost, s) != cudaSuccess ||
+      cudaMemsetAsync(word, 0, 4, s) != cudaSuccess || cudaStreamSynchronize(s) != cudaSuccess) {
+    cudaGetLastError();
+    return DEAMOE_ERR_CUDA;
+  }
+  *status = got;
+  return DEAMOE_OK;
+}

@@ -1,0 +1,88 @@
+// Products on the fifth-generation tensor cores for the operators around a layer (ffn.cu, product.cu): one persistent
+// kernel over 256 x 256 tiles by pairs of CTAs, its operand orders, row groups and epilogues as template parameters.
+//
+//   D[m, n] = sum_k A[m, k] B[n, k]      stored at out[n][m]
+//
+// A is the operand whose rows become the outputs' columns (a weight matrix, or the inputs in a weight gradient), B the one
+// whose rows become the outputs' rows (tokens; the outputs' gradients in a weight gradient).  With the tokens on the
+// N side a group of any size is a tile of its own width (32 to 256 columns in steps of 32), from a decode step's few rows
+// an expert to a prompt's thousands, and the matrix side is always full.
+//
+// What bounds it.  A bf16 MMA of 256 x 256 x 16 by a pair keeps both SMs' tensor cores busy for 128 cycles; each CTA's
+// shared memory then delivers 128 rows of A and 128 of B (8 KB) and takes in as much, 128 bytes a cycle together: a pair
+// shares B, a lone CTA with 128 x 256 would need half as much again.  Few rows a group: the matrix's bytes.
+//
+// Roles of a CTA (1 CTA per SM, clusters of 2, tiles dealt in a fixed order so that equal calls give equal bits):
+//   warps 0-3  epilogue: accumulator -> registers -> a small transposing buffer -> 16-byte rows, with the epilogue's arithmetic in fp32
+//   warp  4    one thread issues the TMA copies of a chunk (128 bytes of k, 128-byte swizzle) into a ring of 6 stages
+//   warp  5    in the pair's first CTA one thread issues the MMAs for both
+//   warp  6    ragged contractions (weight gradients: k runs over a group's rows): clears the rows behind the group's end
+//              that the last chunk's box brought in, in both operands, before the MMAs may read them
+// Two accumulators of 256 columns take turns in tensor memory, so an epilogue runs under the next tile's MMAs.
+// Every wait is bounded; one that expires ends the CTA's roles and raises the status word that
+// deamoe_operator_status reads.
+#pragma once
+#include <cuda.h>
+
+#include "row.cuh"
+
+namespace deamoe {
+
+enum MatmulEpilogue : int {
+  ME_STORE = 0,        // bf16
+  ME_STORE_F32 = 1,    // fp32
+  ME_SWIGLU = 2,       // A's rows alternate 8 gate, 8 up: silu(gate) up
+  ME_SWIGLU_GRAD = 3,  // the same accumulators and the gradient of their product -> gradients of gate and up, and the product
+  ME_PRODUCT = 4,      // scales, bias, activation, residual
+  ME_PRODUCT_GRAD = 5  // dout times the activation's derivative, and its sums over a tile's rows
+};
+
+struct MatmulArgs {
+  int M, K;              // rows of A of a group; length of the contraction in values (ragged: the group's rows instead)
+  int N;                 // rows of B of one group; grouped rows: the length of the row range
+  int groups;
+  const int32_t* off;    // [groups + 1] rows of the groups, or null (one group of all rows)
+  int tile_n;            // widest tile
+  int chunk;             // values of k in 128 bytes
+  // epilogue
+  void* out;
+  int64_t os;            // values between out's rows
+  int64_t out_group;     // values between groups of outputs (weight gradients)
+  int wide;              // out's rows take 16-byte stores
+  const float* dh;       // [N, f]                       (ME_SWIGLU_GRAD)
+  void* h_out;           // [N, f] bf16
+  int f;
+  const void *bias, *residual, *dout;
+  const float *x_scale, *w_scale;
+  int64_t rs;            // residual's or dout's row stride
+  int bias_f32, act, wide_in;
+  float* part;           // [tiles of N][M] sums of dz    (ME_PRODUCT_GRAD)
+};
+
+struct MatmulMaps {
+  CUtensorMap a;
+  CUtensorMap b[3];  // B with k as the inner axis: boxes of 16, 64 and 128 rows; else b[0] alone
+};
+
+// Launch one product.  kind: epilogue; a_rows_inner / b_rows_inner: A / B stored with its rows as the inner axis; fp8: e4m3.
+struct MatmulCall {
+  MatmulArgs args;
+  MatmulMaps maps;
+};
+enum MatmulForm : int {
+  MF_SWIGLU, MF_STORE, MF_STORE_TRANSPOSED, MF_F32_TRANSPOSED, MF_SWIGLU_GRAD, MF_WEIGHT_GRAD, MF_PRODUCT, MF_PRODUCT_E4M3, MF_PRODUCT_GRAD
+};
+cudaError_t matmul_launch(MatmulForm form, const MatmulCall& c, cudaStream_t s, bool chained);
+
+// Tensor maps.  A matrix of `rows` rows of `cols` values per group, row stride and group stride in values.
+bool map_rows(CUtensorMap* m, const void* p, int esize, int64_t cols, int64_t rows, int64_t stride, int64_t groups, int64_t group_stride,
+              int box_rows);                       // box: 128 bytes of a row x box_rows rows
+bool map_gate_up(CUtensorMap* m, const void* p, int64_t cols, int64_t f, int64_t groups);  // 128 rows: 8 gate, 8 up, ...
+bool map_b(MatmulMaps* m, const void* p, int esize, int64_t cols, int64_t rows, int64_t stride);
+
+// Tile width of `n` rows in one group for `m_tiles` tiles of A's rows: see matmul.cu
+int matmul_tile_n(int64_t n, int64_t m_tiles);
+
+constexpr int MM_M = 256, MM_N = 256;
+
+}  // namespace deamoe

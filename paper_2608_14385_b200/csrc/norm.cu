@@ -17,6 +17,8 @@
 // 5.3 and 5.8 TB/s); norm_residual_backward (170 us, 4.1 TB/s) is held by a row's latency, see there.  Sums over the
 // tokens (dw, dwn, a per-channel dgate) are kept per thread block and added by a second kernel in block order: no
 // atomics, equal calls give equal bits.
+#include <cuda_fp8.h>
+
 #include <atomic>
 
 #include "row.cuh"
@@ -57,6 +59,9 @@ struct NormArgs {
   const void *w, *wn;      // gains, or null (ones)
   void *out, *u, *dx, *dy, *dgate;
   int64_t out_s, u_s, dx_s, dy_s, dgate_s;
+  uint8_t* codes;          // [T, h] e4m3 of the quantised norms, and their rows' scales
+  int64_t codes_s;
+  float* scale;
   float* part;             // [3][grad_ctas][h]: partial column sums of dw, dwn, dgate
   float* dgate_token;      // [T]
 };
@@ -378,6 +383,154 @@ template <typename T, int VE, int NV, int MAXT> __global__ void __launch_bounds_
 #pragma unroll
     for (int j = 0; j < VE; ++j) s[n][j] *= ro * w[j];
     store_row<T, VE>(A.u, A.u_s, t, c, s[n]);
+  }
+}
+
+// ---------------------------------------------------------------- norms with an output in 8 bits
+//
+//   u = s / rms(s) * w,   scale = max |u| / 448,   code = e4m3(u / scale)            (s: x, or the sum after the block)
+//
+// With m = max |s w| the code is e4m3(s w * 448 / m) and the scale m / rms(s) / 448: the sum of squares and the maximum
+// come from one reduction, and the codes do not wait for the root.  Rows whose m is below 2^-110 (a row of zeros among
+// them) take 2^-110 for it.  The row stays in registers; HBM bounds it: 5 bytes a value without a sum, 7 with one (bf16).
+constexpr float E4M3_MAX = 448.f, QUANT_LEAST = 0x1p-110f;
+
+// the sum of v[0] and the maximum of v[1] over a block, to every thread; buf: 64 floats, as for block_sums
+static __device__ __forceinline__ void block_sum_max(float (&v)[2], float* buf) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    v[1] = fmaxf(v[1], __shfl_xor_sync(0xffffffffu, v[1], o));
+  }
+  const int warps = blockDim.x >> 5;
+  if (warps == 1) return;
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+  if (lane == 0) {
+    buf[w] = v[0];
+    buf[32 + w] = v[1];
+  }
+  __syncthreads();
+  v[0] = lane < warps ? buf[lane] : 0.f;
+  v[1] = lane < warps ? buf[32 + lane] : 0.f;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) {
+    v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    v[1] = fmaxf(v[1], __shfl_xor_sync(0xffffffffu, v[1], o));
+  }
+}
+// scale of a row into memory; returns what its values are multiplied by
+static __device__ __forceinline__ float row_scale(const NormArgs& A, int64_t t, float ss, float m) {
+  m = fmaxf(m, QUANT_LEAST);
+  const float r = A.next_norm ? inv_rms(ss, A.h, A.next_eps) : 1.f;
+  if (threadIdx.x == 0) A.scale[t] = r * m / E4M3_MAX;
+  return E4M3_MAX / m;
+}
+template <int VE> static __device__ __forceinline__ void store_codes(uint8_t* p, const float (&f)[VE]) {
+  if constexpr (VE == 1) {
+    *p = __nv_cvt_float_to_fp8(f[0], __NV_SATFINITE, __NV_E4M3);
+  } else {
+    uint32_t u[VE / 4];
+#pragma unroll
+    for (int i = 0; i < VE / 4; ++i)
+      u[i] = (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f[4 * i], f[4 * i + 1]), __NV_SATFINITE, __NV_E4M3) |
+             (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f[4 * i + 2], f[4 * i + 3]), __NV_SATFINITE, __NV_E4M3) << 16;
+    if constexpr (VE == 8) *reinterpret_cast<uint2*>(p) = make_uint2(u[0], u[1]);
+    else *reinterpret_cast<uint32_t*>(p) = u[0];
+  }
+}
+
+// y.p null: s = x, nothing but the codes is written
+template <typename T> __global__ void __launch_bounds__(ANY_THREADS) k_codes_any(NormArgs A) {
+  __shared__ float buf[2][64];
+  const int64_t t = blockIdx.x;
+  float ry = 1.f;
+  if (A.post_norm) {
+    float ss[1] = {0.f};
+    for (int i = threadIdx.x; i < A.h; i += ANY_THREADS) {
+      const float v = at<T>(A.y, t, i);
+      ss[0] = fmaf(v, v, ss[0]);
+    }
+    block_sums<1>(ss, buf[0]);
+    ry = inv_rms(ss[0], A.h, A.eps);
+  }
+  auto sum = [&](int i) {
+    const float x = at<T>(A.x, t, i);
+    return A.y.p ? fmaf(A.a, x, A.b * gate_at<T>(A, t, i) * (at<T>(A.y, t, i) * ry * load_gain(A.w, A.wdt, i))) : x;
+  };
+  float v[2] = {0.f, 0.f};
+  for (int i = threadIdx.x; i < A.h; i += ANY_THREADS) {
+    const float s = sum(i);
+    v[0] = fmaf(s, s, v[0]);
+    v[1] = fmaxf(v[1], fabsf(s * load_gain(A.wn, A.wdt, i)));
+  }
+  block_sum_max(v, buf[1]);
+  const float f = row_scale(A, t, v[0], v[1]);
+  for (int i = threadIdx.x; i < A.h; i += ANY_THREADS) {
+    const float s = sum(i);
+    if (A.y.p) put<T>(A.out, A.out_s, t, i, s);
+    const float c[1] = {s * load_gain(A.wn, A.wdt, i) * f};
+    store_codes<1>(A.codes + t * A.codes_s + i, c);
+  }
+}
+
+template <typename T, int VE, int NV, int MAXT> __global__ void __launch_bounds__(MAXT) k_codes_rows(NormArgs A, int packs) {
+  __shared__ float buf[2][64];
+  const int64_t t = blockIdx.x;
+  Pack<T, VE> x[NV], y[NV];
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    const int c = threadIdx.x + n * blockDim.x;
+    if (c < packs) {
+      if (A.y.p) y[n] = load_once<T, VE>(row_at<T>(A.y, t) + (int64_t)c * VE);
+      x[n] = load_once<T, VE>(row_at<T>(A.x, t) + (int64_t)c * VE);
+    }
+  }
+  float ry = 1.f;
+  if (A.post_norm) {
+    float ss[1] = {0.f};
+#pragma unroll
+    for (int n = 0; n < NV; ++n)
+      if ((int)(threadIdx.x + n * blockDim.x) < packs) {
+        float f[VE];
+        y[n].widen(f);
+#pragma unroll
+        for (int j = 0; j < VE; ++j) ss[0] = fmaf(f[j], f[j], ss[0]);
+      }
+    block_sums<1>(ss, buf[0]);
+    ry = inv_rms(ss[0], A.h, A.eps);
+  }
+  float s[NV][VE], v[2] = {0.f, 0.f};
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    const int c = threadIdx.x + n * blockDim.x;
+    if (c >= packs) continue;
+    float f[VE], w[VE], g[VE];
+    x[n].widen(s[n]);
+    if (A.y.p) {
+      load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, w);
+      load_gate<T, VE>(A, t, c, g);
+      y[n].widen(f);
+#pragma unroll
+      for (int j = 0; j < VE; ++j) s[n][j] = fmaf(A.a, s[n][j], A.b * g[j] * (f[j] * ry * w[j]));
+      store_row<T, VE>(A.out, A.out_s, t, c, s[n]);
+    }
+    load_gains<VE>(A.wn, A.wdt, (int64_t)c * VE, w);
+#pragma unroll
+    for (int j = 0; j < VE; ++j) {
+      v[0] = fmaf(s[n][j], s[n][j], v[0]);
+      s[n][j] *= w[j];
+      v[1] = fmaxf(v[1], fabsf(s[n][j]));
+    }
+  }
+  block_sum_max(v, buf[1]);
+  const float scale = row_scale(A, t, v[0], v[1]);
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    const int c = threadIdx.x + n * blockDim.x;
+    if (c >= packs) continue;
+#pragma unroll
+    for (int j = 0; j < VE; ++j) s[n][j] *= scale;
+    store_codes<VE>(A.codes + t * A.codes_s + (int64_t)c * VE, s[n]);
   }
 }
 
@@ -847,6 +1000,8 @@ template <typename T> static bool wide_call(const NormArgs& A) {
        wide_rows(A.u, A.u_s, A.T, sizeof(T)) && wide_rows(A.dx, A.dx_s, A.T, sizeof(T)) &&
        wide_rows(A.dy, A.dy_s, A.T, sizeof(T));
   if (A.gate_kind == DEAMOE_GATE_FULL) ok = ok && wide_rows(A.dgate, A.dgate_s, A.T, sizeof(T));
+  // the codes of 16 bytes of values: 8 bytes, or 4
+  if (A.codes) ok = ok && aligned_to(A.codes, 16 / sizeof(T)) && (A.T == 1 || A.codes_s % (16 / sizeof(T)) == 0);
   return ok;
 }
 
@@ -884,6 +1039,9 @@ template <typename T> static deamoe_status_t norm_t(const NormArgs& A, cudaStrea
 }
 template <typename T> static deamoe_status_t residual_t(const NormArgs& A, cudaStream_t s) {
   DEAMOE_ROW_FORMS(k_residual_rows, k_residual_any);
+}
+template <typename T> static deamoe_status_t codes_t(const NormArgs& A, cudaStream_t s) {
+  DEAMOE_ROW_FORMS(k_codes_rows, k_codes_any);
 }
 #undef DEAMOE_ROW_FORMS
 
@@ -1039,6 +1197,48 @@ deamoe_status_t deamoe_norm_residual(void* cuda_stream, int32_t dtype, const voi
   A.out = out; A.out_s = out_stride; A.u = next; A.u_s = next_stride;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
   return dtype == DEAMOE_F32 ? residual_t<float>(A, s) : residual_t<__nv_bfloat16>(A, s);
+}
+
+deamoe_status_t deamoe_norm_quant(void* cuda_stream, int32_t dtype, const void* x, int64_t x_stride, int32_t n_token, int32_t hidden,
+                                  int32_t normalise, int32_t weight_dtype, const void* weight, float eps, void* codes,
+                                  int64_t codes_stride, float* scale) {
+  deamoe_status_t st = check_norm(dtype, weight_dtype, n_token, hidden, eps);
+  if (st == DEAMOE_OK && normalise != 0 && normalise != 1) st = DEAMOE_ERR_INVALID_ARG;
+  if (st != DEAMOE_OK || n_token == 0) return st;
+  if (bad_rows(x, x_stride, hidden, type_bytes(dtype)) || bad_rows(codes, codes_stride, hidden, 1) || !scale || !aligned_to(scale, 4) ||
+      !aligned_to(weight, type_bytes(weight_dtype)) || codes == x)
+    return DEAMOE_ERR_INVALID_ARG;
+  NormArgs A = {};
+  A.T = n_token; A.h = hidden; A.wdt = weight_dtype; A.next_eps = eps; A.next_norm = normalise; A.wn = weight;
+  A.x = {x, x_stride}; A.codes = reinterpret_cast<uint8_t*>(codes); A.codes_s = codes_stride; A.scale = scale;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+  return dtype == DEAMOE_F32 ? codes_t<float>(A, s) : codes_t<__nv_bfloat16>(A, s);
+}
+
+deamoe_status_t deamoe_norm_residual_quant(void* cuda_stream, int32_t dtype, const void* x, int64_t x_stride, const void* y,
+                                           int64_t y_stride, int32_t n_token, int32_t hidden, int32_t normalise,
+                                           int32_t weight_dtype, const void* weight, float eps, int32_t gate_kind,
+                                           const void* gate, int64_t gate_stride, float residual_scale, float branch_scale,
+                                           void* out, int64_t out_stride, const void* next_weight, float next_eps, void* codes,
+                                           int64_t codes_stride, float* scale) {
+  deamoe_status_t st = check_norm(dtype, weight_dtype, n_token, hidden, eps);
+  if (st == DEAMOE_OK && !(next_eps >= 0.f)) st = DEAMOE_ERR_INVALID_ARG;
+  if (st != DEAMOE_OK || n_token == 0) return st;
+  const size_t es = type_bytes(dtype), ws = type_bytes(weight_dtype);
+  if (bad_rows(x, x_stride, hidden, es) || bad_rows(y, y_stride, hidden, es) || bad_rows(out, out_stride, hidden, es) ||
+      bad_rows(codes, codes_stride, hidden, 1) || !scale || !aligned_to(scale, 4) || !aligned_to(weight, ws) ||
+      !aligned_to(next_weight, ws))
+    return DEAMOE_ERR_INVALID_ARG;
+  if ((out == x && out_stride != x_stride) || out == y || codes == x || codes == y || codes == out) return DEAMOE_ERR_INVALID_ARG;
+  st = check_block(gate_kind, gate, gate_stride, hidden, es, normalise, weight, residual_scale, branch_scale);
+  if (st != DEAMOE_OK) return st;
+  NormArgs A = {};
+  A.T = n_token; A.h = hidden; A.wdt = weight_dtype; A.eps = eps; A.next_eps = next_eps;
+  A.a = residual_scale; A.b = branch_scale; A.gate_kind = gate_kind; A.post_norm = normalise; A.next_norm = 1;
+  A.x = {x, x_stride}; A.y = {y, y_stride}; A.gate = {gate, gate_stride}; A.w = weight; A.wn = next_weight;
+  A.out = out; A.out_s = out_stride; A.codes = reinterpret_cast<uint8_t*>(codes); A.codes_s = codes_stride; A.scale = scale;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+  return dtype == DEAMOE_F32 ? codes_t<float>(A, s) : codes_t<__nv_bfloat16>(A, s);
 }
 
 deamoe_status_t deamoe_norm_residual_backward(
