@@ -7,15 +7,16 @@ namespace deamoe {
 
 namespace {
 
-constexpr int MM_STAGES = 6;
+constexpr int MM_STAGES = 5;
 constexpr int MM_OPERAND = 16 * 1024;          // one CTA's part of a chunk of A or of B: 128 rows of 128 bytes
 constexpr int MM_STAGE = 2 * MM_OPERAND;
-constexpr int MM_WARP_COPY = 4, MM_WARP_MMA = 5, MM_WARP_CLEAR = 6;
-constexpr int MM_THREADS = 7 * 32;
-constexpr int MM_EPI = 128;                    // threads of the epilogue
-constexpr int MM_COLS = 16;                    // accumulator columns of an epilogue step
+constexpr int MM_TEAMS = 2;                    // epilogue teams of 4 warps (a warp reads the 32 lanes of tensor memory of its number mod 4)
+constexpr int MM_WARP_COPY = 4 * MM_TEAMS, MM_WARP_MMA = MM_WARP_COPY + 1, MM_WARP_CLEAR = MM_WARP_COPY + 2;
+constexpr int MM_THREADS = (MM_WARP_CLEAR + 1) * 32;
+constexpr int MM_COLS = 16;                    // accumulator columns of one of the two transposing buffers
+constexpr int MM_STEP = 2 * MM_COLS;           // ... of an epilogue step; the teams take steps in turn
 constexpr int MM_PITCH = 128 + 4;              // floats of a row of the transposing buffer
-constexpr int MM_STAGING = 2 * MM_COLS * MM_PITCH * 4;
+constexpr int MM_STAGING = MM_TEAMS * 2 * MM_COLS * MM_PITCH * 4;
 constexpr int MM_CONTROL = 512;
 constexpr int MM_TABLE = (DEAMOE_MAX_EXPERTS + 1) * 8 + 8;  // groups' first tile and first row
 constexpr size_t MM_SMEM = (size_t)MM_STAGES * MM_STAGE + MM_STAGING + MM_CONTROL + MM_TABLE;
@@ -106,15 +107,18 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
                ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
-__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[16]) {
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[32]) {
   asm volatile(
-      "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+      "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+      "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
       : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+        "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+        "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(addr));
 }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void epilogue_sync() { asm volatile("bar.sync 1, 128;" ::: "memory"); }
+__device__ __forceinline__ void team_sync(int team) { asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory"); }
 
 // ---------------------------------------------------------------- the order of the tiles
 struct Tile {
@@ -156,7 +160,7 @@ template <bool RAGGED> __device__ __forceinline__ Tile find_tile(const MatmulArg
 }
 
 // ---------------------------------------------------------------- epilogue arithmetic
-__device__ __forceinline__ float sigmoid(float v) { return 1.f / (1.f + __expf(-v)); }
+__device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
 __device__ __forceinline__ float act_grad(int kind, float z) {
   if (kind == DEAMOE_SIGMA_SILU) {
     const float p = sigmoid(z);
@@ -178,13 +182,9 @@ __device__ __forceinline__ void put8(__nv_bfloat16* p, const float (&v)[8], int 
       if (j < n) p[j] = __float2bfloat16_rn(v[j]);
   }
 }
-__device__ __forceinline__ void get8(const __nv_bfloat16* p, float (&v)[8], int n, bool wide) {
-  if (wide && n == 8) {
-    load_once<__nv_bfloat16, 8>(p).widen(v);
-  } else {
+__device__ __forceinline__ void get8(const __nv_bfloat16* p, float (&v)[8], int n) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = j < n ? __bfloat162float(p[j]) : 0.f;
-  }
+  for (int j = 0; j < 8; ++j) v[j] = j < n ? __bfloat162float(p[j]) : 0.f;
 }
 __device__ __forceinline__ void floats8(const float* p, float (&v)[8]) {
   const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
@@ -193,6 +193,11 @@ __device__ __forceinline__ void floats8(const float* p, float (&v)[8]) {
 __device__ __forceinline__ float gain(const void* p, int f32, int i) {
   return f32 ? reinterpret_cast<const float*>(p)[i] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[i]);
 }
+// What an epilogue step of a thread takes from memory, asked for a step ahead.
+struct Ahead {
+  uint4 v[4];
+  float scale[4];
+};
 
 // ---------------------------------------------------------------- the kernel
 // AT / BT: A / B lies with its rows as the inner axis (k outer); RAGGED: the contraction runs over a group's rows.
@@ -208,12 +213,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   auto full = [&](int s) { return bars + 8 * s; };
   auto empty = [&](int s) { return bars + 8 * (MM_STAGES + s); };
   auto tail = [&](int s) { return bars + 8 * (2 * MM_STAGES + s); };
-  auto acc_full = [&](int b) { return bars + 8 * (3 * MM_STAGES + b); };
-  auto acc_empty = [&](int b) { return bars + 8 * (3 * MM_STAGES + 2 + b); };
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(control + 3 * MM_STAGES + 4);
+  auto cleared = [&](int s) { return bars + 8 * (3 * MM_STAGES + s); };
+  auto acc_full = [&](int b) { return bars + 8 * (4 * MM_STAGES + b); };
+  auto acc_empty = [&](int b) { return bars + 8 * (4 * MM_STAGES + 2 + b); };
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(control + 4 * MM_STAGES + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* warp_sums = reinterpret_cast<int*>(tmem_slot + 2);
-  static_assert((3 * MM_STAGES + 4) * 8 + 8 + 8 * 4 <= MM_CONTROL, "control region");
+  static_assert((4 * MM_STAGES + 4) * 8 + 8 + 16 * 4 <= MM_CONTROL, "control region");
   int* first_row = reinterpret_cast<int*>(smem + (size_t)MM_STAGES * MM_STAGE + MM_STAGING + MM_CONTROL);
   int* first_tile = first_row + A.groups + 1;
 
@@ -221,13 +227,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   const uint32_t rank = cluster_rank();
   if (tid == 0) {
     for (int s = 0; s < MM_STAGES; ++s) {
-      bar_init(full(s), RAGGED ? 2 : 1);
+      bar_init(full(s), 1);
       bar_init(empty(s), 1);
       bar_init(tail(s), 1);
+      bar_init(cleared(s), 1);
     }
     for (int b = 0; b < 2; ++b) {
       bar_init(acc_full(b), 1);
-      bar_init(acc_empty(b), 8);
+      bar_init(acc_empty(b), 2 * 4 * MM_TEAMS);
     }
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -284,8 +291,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
             bar_expect(bar, bytes);
           } else if (rank == 0) {
             bar_expect(full(s), 2 * bytes);
-          } else if (RAGGED) {
-            bar_arrive_cluster(bar);
           }
           const int ka = RAGGED ? t.row0 + k0 : k0;
           if constexpr (DUAL) {
@@ -351,165 +356,204 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   } else if (warp == MM_WARP_CLEAR) {
     // ============================================================ rows behind a group's end
     if constexpr (RAGGED) {
-      uint32_t g = 0, uses = 0;  // uses: bit s = parity of the next use of tail(s)
+      uint32_t g = 0, parity = 0;  // bit s: of the next use of tail(s) and cleared(s)
       for (int it = pair; it < tiles; it += pairs) {
         const Tile t = find_tile<RAGGED>(A, first_tile, first_row, it, M_STEP);
         const int chunks = chunks_of(t), left = t.rows % A.chunk;
         g += chunks;
         if (left == 0) continue;
         const int s = (g - 1) % MM_STAGES;
-        int ok = lane == 0 ? bar_wait(tail(s), (uses >> s) & 1u, abort_flag) : 0;
+        int ok = lane == 0 ? bar_wait(tail(s), (parity >> s) & 1u, abort_flag) : 0;
         ok = __shfl_sync(0xffffffffu, ok, 0);
         if (!ok) break;
-        uses ^= 1u << s;
         unsigned char* st = smem + (size_t)s * MM_STAGE;
         const int from = left * 8, per = 64 * 8;  // 16-byte pieces of a box: 64 rows of 128 bytes
         for (int b = 0; b < 4; ++b)
           for (int i = from + lane; i < per; i += 32) *reinterpret_cast<uint4*>(st + b * (MM_OPERAND / 2) + i * 16) = make_uint4(0, 0, 0, 0);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        if (lane == 0) bar_arrive_cluster(in_first(full(s)));
+        // the second CTA tells the first, whose stage is full when both are cleared (a remote arrival of every chunk's copies
+        // instead, with its release, made this kernel half as fast)
+        if (lane == 0) {
+          if (rank != 0) bar_arrive_cluster(in_first(cleared(s)));
+          else if (bar_wait(cleared(s), (parity >> s) & 1u, abort_flag)) bar_arrive_cluster(full(s));
+        }
+        parity ^= 1u << s;
       }
     }
   } else {
     // ============================================================ epilogue
+    // One warp a scheduler runs such code at some seven cycles an instruction, so two teams share a tile's columns,
+    // and rows are walked by pointer.
     uint32_t a = 0;
-    int flip = 0;
     bool ok = true;
-    const uint32_t lane_base = tmem + ((uint32_t)(warp * 32) << 16);
+    const int team = warp >> 2, me = tid & 127;
+    float* const st = staging + team * (2 * MM_COLS * MM_PITCH);
+    const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+    // A thread's part of a buffer: DUAL: one row, 8 features; else rows c and c + 8, 8 columns of the output.
+    constexpr int ITEMS = DUAL ? 1 : 2, ITEM_ROWS = MM_COLS / ITEMS;
+    constexpr int OUT_BYTES = EPI == ME_STORE_F32 ? 4 : 2;
+    const int q = DUAL ? me & 7 : me & 15, c = DUAL ? me >> 3 : me >> 4;
+    const int64_t out_step = A.os * (ITEM_ROWS * OUT_BYTES);
+    const float* const mine = st + c * MM_PITCH + q * (DUAL ? 16 : 8);
     for (int it = pair; ok && it < tiles; it += pairs) {
       const Tile t = find_tile<RAGGED>(A, first_tile, first_row, it, M_STEP);
       const bool none = RAGGED && t.rows == 0;  // a group without rows: zeros
       const uint32_t buf = a & 1u;
+      const int m = t.m0 + (int)rank * (M_STEP / 2) + q * 8, n = min(8, A.M - m);
+      const int valid = n > 0 ? t.valid : 0;
+      const int64_t row0 = t.n0 + team * MM_STEP + c;
+      char* out = reinterpret_cast<char*>(A.out) + ((RAGGED ? (int64_t)t.group * A.out_group : 0) + row0 * A.os + m) * OUT_BYTES;
+      // rows of dh, residual or dout of this thread's items, and x's scales
+      const void* const from = EPI == ME_SWIGLU_GRAD ? (const void*)A.dh : EPI == ME_PRODUCT ? A.residual : EPI == ME_PRODUCT_GRAD ? A.dout : nullptr;
+      const int64_t in_stride = EPI == ME_SWIGLU_GRAD ? (int64_t)A.f * 4 : A.rs * 2;
+      const char* in = reinterpret_cast<const char*>(from) + row0 * in_stride + (int64_t)m * (EPI == ME_SWIGLU_GRAD ? 4 : 2);
+      const float* xs = FP8 ? A.x_scale + row0 : nullptr;
+      const bool wide_in = EPI == ME_SWIGLU_GRAD || (from && A.wide_in && n == 8);
+      auto ask = [&](int at, Ahead& w) {  // `at`: column of the thread's first item
+        if constexpr (EPI == ME_SWIGLU_GRAD || EPI == ME_PRODUCT || EPI == ME_PRODUCT_GRAD) {
+          const char* p = in;
+#pragma unroll
+          for (int i = 0; i < 2 * ITEMS; ++i, p += in_stride * ITEM_ROWS)
+            if (at + i * ITEM_ROWS < valid) {
+              if constexpr (EPI == ME_SWIGLU_GRAD) {
+                w.v[2 * i] = reinterpret_cast<const uint4*>(p)[0];
+                w.v[2 * i + 1] = reinterpret_cast<const uint4*>(p)[1];
+              } else if (wide_in) {
+                w.v[i] = load_once<__nv_bfloat16, 8>(reinterpret_cast<const __nv_bfloat16*>(p)).r;
+              }
+              if constexpr (FP8) w.scale[i] = xs[i * ITEM_ROWS];
+            }
+          in += in_stride * (MM_TEAMS * MM_STEP);
+          if constexpr (FP8) xs += MM_TEAMS * MM_STEP;
+        }
+      };
+      float bias[8], scale[8], sums[8];  // of this thread's columns of the output
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        sums[j] = bias[j] = 0.f;
+        if constexpr (EPI == ME_PRODUCT || EPI == ME_PRODUCT_GRAD)
+          if (A.bias && j < n) bias[j] = gain(A.bias, A.bias_f32, m + j);
+        if constexpr (EPI == ME_PRODUCT && FP8) scale[j] = j < n ? A.w_scale[m + j] : 0.f;
+      }
+      Ahead now, next;
+      ask(team * MM_STEP + c, now);
       if (!none) {
-        int w = lane == 0 ? bar_wait(acc_full(buf), (a >> 1) & 1u, abort_flag) : 0;
+        const int w = lane == 0 ? bar_wait(acc_full(buf), (a >> 1) & 1u, abort_flag) : 0;
         ok = __shfl_sync(0xffffffffu, w, 0) != 0;
-        // all four warps or none: they meet at barriers below
+        // all four warps of a team or none: they meet at barriers below
         int all;
-        asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %1, 0;\nbar.red.and.pred q, 1, 128, p;\nselp.b32 %0, 1, 0, q;\n}"
-                     : "=r"(all) : "r"((int)ok) : "memory");
+        asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %1, 0;\nbar.red.and.pred q, %2, 128, p;\nselp.b32 %0, 1, 0, q;\n}"
+                     : "=r"(all) : "r"((int)ok), "r"(1 + team) : "memory");
         ok = all != 0;
         if (!ok) break;
         tc_after();
         ++a;
       }
-      const int m_cta = t.m0 + (int)rank * (M_STEP / 2);
-      float sums[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) sums[j] = 0.f;
-      for (int c0 = 0; c0 < t.n; c0 += MM_COLS) {
-        float* st = staging + flip * (MM_COLS * MM_PITCH);
-        flip ^= 1;
-        uint32_t r[16];
+      auto release = [&] {  // the accumulator has been read
+        tc_before();
+        __syncwarp();
+        if (lane == 0) bar_arrive_cluster(in_first(acc_empty(buf)));
+      };
+      if (!none && team * MM_STEP >= t.n) release();
+      for (int c0 = team * MM_STEP; c0 < t.n; c0 += MM_TEAMS * MM_STEP) {
+        uint32_t r[MM_STEP];
         if (none) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i) r[i] = 0;
+          for (int i = 0; i < MM_STEP; ++i) r[i] = 0;
         } else {
           tmem_load(lane_base + buf * MM_N + c0, r);
+          ask(c0 + MM_TEAMS * MM_STEP + c, next);  // (past the tile's end: nothing)
           tmem_load_wait();
-          if (c0 + MM_COLS >= t.n) {  // the accumulator has been read
-            tc_before();
-            __syncwarp();
-            if (lane == 0) bar_arrive_cluster(in_first(acc_empty(buf)));
-          }
+          if (c0 + MM_TEAMS * MM_STEP >= t.n) release();
         }
 #pragma unroll
-        for (int i = 0; i < 16; ++i) st[i * MM_PITCH + warp * 32 + lane] = __uint_as_float(r[i]);
-        epilogue_sync();
-        if constexpr (DUAL) {
-          const int c = tid >> 3, q = tid & 7;  // column (row of B) of the step; block of 8 features
-          const int m = m_cta + q * 8;
-          if (c0 + c < t.valid && m < A.M) {    // (f is a multiple of 8)
-            const int64_t row = t.n0 + c0 + c;
-            float gate[8], up[8], v[8];
-            floats8(st + c * MM_PITCH + q * 16, gate);
-            floats8(st + c * MM_PITCH + q * 16 + 8, up);
-            __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(A.out) + row * A.os + m;
-            if constexpr (EPI == ME_SWIGLU) {
+        for (int h = 0; h < 2; ++h) {
+          constexpr int BUF = MM_COLS * MM_PITCH;
 #pragma unroll
-              for (int j = 0; j < 8; ++j) v[j] = gate[j] * sigmoid(gate[j]) * up[j];
-              put8(out, v, 8, true);
-            } else {
-              float dh[8], dg[8], du[8];
-              floats8(A.dh + row * A.f + m, dh);
+          for (int i = 0; i < MM_COLS; ++i) st[h * BUF + i * MM_PITCH + (warp & 3) * 32 + lane] = __uint_as_float(r[h * MM_COLS + i]);
+          team_sync(team);
 #pragma unroll
-              for (int j = 0; j < 8; ++j) {
-                const float p = sigmoid(gate[j]), act = gate[j] * p;
-                v[j] = act * up[j];
-                du[j] = dh[j] * act;
-                dg[j] = dh[j] * up[j] * (p * (1.f + gate[j] * (1.f - p)));
-              }
-              put8(out, dg, 8, true);
-              put8(out + A.f, du, 8, true);
-              put8(reinterpret_cast<__nv_bfloat16*>(A.h_out) + row * A.f + m, v, 8, true);
-            }
-          }
-        } else {
+          for (int i = 0; i < ITEMS; ++i, out += out_step) {
+            if (c0 + h * MM_COLS + i * ITEM_ROWS + c >= valid) continue;
+            const float* from_st = mine + h * BUF + i * (ITEM_ROWS * MM_PITCH);
+            __nv_bfloat16* const to = reinterpret_cast<__nv_bfloat16*>(out);
+            const int k = ITEMS * h + i;
+            float v[8];
+            floats8(from_st, v);
+            if constexpr (DUAL) {  // (f is a multiple of 8)
+              float up[8];
+              floats8(from_st + 8, up);
+              if constexpr (EPI == ME_SWIGLU) {
 #pragma unroll
-          for (int i = 0; i < MM_COLS * 16 / MM_EPI; ++i) {
-            const int c = (tid >> 4) + 8 * i, q = tid & 15;
-            const int m = m_cta + q * 8, n = min(8, A.M - m);
-            if (c0 + c < t.valid && n > 0) {
-              const int64_t row = t.n0 + c0 + c;
-              float v[8];
-              floats8(st + c * MM_PITCH + q * 8, v);
-              if constexpr (EPI == ME_STORE_F32) {
-                float4* out = reinterpret_cast<float4*>(reinterpret_cast<float*>(A.out) + row * A.os + m);
-                out[0] = make_float4(v[0], v[1], v[2], v[3]);
-                out[1] = make_float4(v[4], v[5], v[6], v[7]);
+                for (int j = 0; j < 8; ++j) v[j] *= sigmoid(v[j]) * up[j];
+                put8(to, v, 8, true);
               } else {
-                __nv_bfloat16* out = reinterpret_cast<__nv_bfloat16*>(A.out) + (int64_t)t.group * A.out_group + row * A.os + m;
-                if constexpr (EPI == ME_PRODUCT) {
-                  if (A.x_scale) {
-                    const float xs = A.x_scale[row];
+                const uint32_t d[8] = {now.v[2 * k].x, now.v[2 * k].y, now.v[2 * k].z, now.v[2 * k].w,
+                                       now.v[2 * k + 1].x, now.v[2 * k + 1].y, now.v[2 * k + 1].z, now.v[2 * k + 1].w};
+                float dg[8], du[8];
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] *= j < n ? xs * A.w_scale[m + j] : 0.f;
-                  }
+                for (int j = 0; j < 8; ++j) {
+                  const float p = sigmoid(v[j]), act = v[j] * p, dh = __uint_as_float(d[j]);
+                  du[j] = dh * act;
+                  dg[j] = dh * up[j] * (p * (1.f + v[j] * (1.f - p)));
+                  v[j] = act * up[j];
                 }
-                if constexpr (EPI == ME_PRODUCT || EPI == ME_PRODUCT_GRAD) {
-                  if (A.bias) {
+                put8(to, dg, 8, true);
+                put8(to + A.f, du, 8, true);
+                put8(reinterpret_cast<__nv_bfloat16*>(A.h_out) + (row0 + c0 - team * MM_STEP + h * MM_COLS) * A.f + m, v, 8, true);
+              }
+            } else if constexpr (EPI == ME_STORE_F32) {
+              float4* o = reinterpret_cast<float4*>(out);
+              o[0] = make_float4(v[0], v[1], v[2], v[3]);
+              o[1] = make_float4(v[4], v[5], v[6], v[7]);
+            } else {
+              if constexpr (EPI == ME_PRODUCT || EPI == ME_PRODUCT_GRAD) {
+                float add[8];
+                if (wide_in) {
+                  Pack<__nv_bfloat16, 8> w;
+                  w.r = now.v[k];
+                  w.widen(add);
+                } else if (from) {
+                  get8(reinterpret_cast<const __nv_bfloat16*>(from) + (row0 + c0 - team * MM_STEP + h * MM_COLS + i * ITEM_ROWS) * A.rs + m, add, n);
+                }
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] += j < n ? gain(A.bias, A.bias_f32, m + j) : 0.f;
-                  }
-                }
+                for (int j = 0; j < 8; ++j) v[j] = FP8 ? fmaf(v[j], now.scale[k] * scale[j], bias[j]) : v[j] + bias[j];
                 if constexpr (EPI == ME_PRODUCT) {
                   if (A.act != DEAMOE_SIGMA_NONE) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = sigma_f(A.act, v[j]);
+                    for (int j = 0; j < 8; ++j) v[j] = A.act == DEAMOE_SIGMA_SILU ? v[j] * sigmoid(v[j]) : sigma_f(DEAMOE_SIGMA_GELU, v[j]);
                   }
-                  if (A.residual) {
-                    float add[8];
-                    get8(reinterpret_cast<const __nv_bfloat16*>(A.residual) + row * A.rs + m, add, n, A.wide_in);
+                  if (from) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j) v[j] += add[j];
                   }
-                }
-                if constexpr (EPI == ME_PRODUCT_GRAD) {
-                  float d[8];
-                  get8(reinterpret_cast<const __nv_bfloat16*>(A.dout) + row * A.rs + m, d, n, A.wide_in);
+                } else {
 #pragma unroll
                   for (int j = 0; j < 8; ++j) {
-                    v[j] = d[j] * act_grad(A.act, v[j]);
+                    v[j] = add[j] * act_grad(A.act, v[j]);
                     sums[j] += v[j];
                   }
                 }
-                put8(out, v, n, A.wide);
               }
+              put8(to, v, n, A.wide);
             }
           }
         }
+        out += 2 * ITEMS * (MM_TEAMS - 1) * out_step;
+        now = next;
       }
       if constexpr (EPI == ME_PRODUCT_GRAD) {
-        if (A.part) {  // 8 threads hold sums of the same columns: added in their order
-          float* st = staging + flip * (MM_COLS * MM_PITCH);
-          flip ^= 1;
+        if (A.part) {  // 8 threads of a team hold sums of the same columns: added in their order (the first buffer is free again here)
 #pragma unroll
-          for (int j = 0; j < 8; ++j) st[(tid >> 4) * MM_PITCH + (tid & 15) * 8 + j] = sums[j];
-          epilogue_sync();
-          float s = 0.f;
+          for (int j = 0; j < 8; ++j) st[c * MM_PITCH + q * 8 + j] = sums[j];
+          team_sync(team);
+          float v = 0.f;
 #pragma unroll
-          for (int i = 0; i < 8; ++i) s += st[i * MM_PITCH + tid];
-          if (m_cta + tid < A.M) A.part[(int64_t)t.n_index * A.M + m_cta + tid] = s;
+          for (int i = 0; i < 8; ++i) v += st[i * MM_PITCH + me];
+          const int col = t.m0 + (int)rank * (M_STEP / 2) + me;
+          if (col < A.M) A.part[(int64_t)(MM_TEAMS * t.n_index + team) * A.M + col] = v;
+          team_sync(team);
         }
       }
     }

@@ -13,10 +13,10 @@
 // shares B, a lone CTA with 128 x 256 would need half as much again.  Few rows a group: the matrix's bytes.
 //
 // Roles of a CTA (1 CTA per SM, clusters of 2, tiles dealt in a fixed order so that equal calls give equal bits):
-//   warps 0-3  epilogue: accumulator -> registers -> a small transposing buffer -> 16-byte rows, with the epilogue's arithmetic in fp32
-//   warp  4    one thread issues the TMA copies of a chunk (128 bytes of k, 128-byte swizzle) into a ring of 6 stages
-//   warp  5    in the pair's first CTA one thread issues the MMAs for both
-//   warp  6    ragged contractions (weight gradients: k runs over a group's rows): clears the rows behind the group's end
+//   warps 0-7  epilogue, two teams that share a tile's columns: accumulator -> registers -> a small transposing buffer -> 16-byte rows, with the epilogue's arithmetic in fp32
+//   warp  8    one thread issues the TMA copies of a chunk (128 bytes of k, 128-byte swizzle) into a ring of 5 stages
+//   warp  9    in the pair's first CTA one thread issues the MMAs for both
+//   warp  10   ragged contractions (weight gradients: k runs over a group's rows): clears the rows behind the group's end
 //              that the last chunk's box brought in, in both operands, before the MMAs may read them
 // Two accumulators of 256 columns take turns in tensor memory, so an epilogue runs under the next tile's MMAs.
 // Every wait is bounded; one that expires ends the CTA's roles and raises the status word that
@@ -56,7 +56,7 @@ struct MatmulArgs {
   const float *x_scale, *w_scale;
   int64_t rs;            // residual's or dout's row stride
   int bias_f32, act, wide_in;
-  float* part;           // [tiles of N][M] sums of dz    (ME_PRODUCT_GRAD)
+  float* part;           // [2 tiles of N][M] sums of dz    (ME_PRODUCT_GRAD)
 };
 
 struct MatmulMaps {
@@ -84,5 +84,7 @@ bool map_b(MatmulMaps* m, const void* p, int esize, int64_t cols, int64_t rows, 
 int matmul_tile_n(int64_t n, int64_t m_tiles);
 
 constexpr int MM_M = 256, MM_N = 256;
+constexpr int MM_N_LEAST = 128;  // matmul_tile_n gives no less
+constexpr int MM_PARTS = 2;      // rows of sums that a tile leaves in `part`
 
 }  // namespace deamoe

@@ -107,8 +107,8 @@ deamoe_status_t deamoe_product(void* cuda_stream, int32_t dtype, const void* x, 
 }
 
 static uint64_t bias_parts(int T, int n_out, int act) {
-  // with an activation one row of sums a tile of tokens (32 rows at least), else one a block of rows
-  return (uint64_t)(act == DEAMOE_SIGMA_NONE ? (T + BIAS_ROWS - 1) / BIAS_ROWS : (T + 31) / 32) * n_out * 4;
+  // with an activation two rows of sums a tile of tokens, else one a block of rows
+  return (uint64_t)(act == DEAMOE_SIGMA_NONE ? (T + BIAS_ROWS - 1) / BIAS_ROWS : MM_PARTS * ((T + MM_N_LEAST - 1) / MM_N_LEAST)) * n_out * 4;
 }
 
 uint64_t deamoe_product_workspace(int32_t n_token, int32_t n_out, int32_t act) {
@@ -153,7 +153,7 @@ deamoe_status_t deamoe_product_backward(void* cuda_stream, int32_t dtype, const 
   bool ok = true;
   int parts = 0;
   if (!plain) {
-    parts = (n_token + a.args.tile_n - 1) / a.args.tile_n;
+    parts = MM_PARTS * ((n_token + a.args.tile_n - 1) / a.args.tile_n);
     ok = matmul_launch(MF_PRODUCT_GRAD, a, s, false) == cudaSuccess;
   } else if (dbias) {
     parts = (n_token + BIAS_ROWS - 1) / BIAS_ROWS;
