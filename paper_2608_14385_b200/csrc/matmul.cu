@@ -87,6 +87,11 @@ __device__ __forceinline__ void load_5d(uint32_t dst, const CUtensorMap* m, int 
       "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(u), "r"(v), "r"(bar) : "memory");
 }
+__device__ __forceinline__ bool elected() {
+  uint32_t p;
+  asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(p));
+  return p != 0;
+}
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 // Shared-memory operand with 128-byte swizzle.  k inner: 8 rows of 128 bytes are a block of 1024 bytes, `sbo` apart.
@@ -324,7 +329,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     }
   } else if (warp == MM_WARP_MMA) {
     // ============================================================ MMAs, by the pair's first CTA
-    if (rank == 0 && lane == 0) {
+    // The issue of a chunk has to fit the 512 cycles of its MMAs.  The whole warp walks the loop, so that descriptors are
+    // warp-uniform values, and one elected thread issues; the next stage is asked for before this one's MMAs are issued.
+    if (rank == 0) {
       uint32_t g = 0, a = 0;
       bool ok = true;
       const uint64_t da = operand_desc(ring, AT ? MM_OPERAND / 2 : 16, 1024);
@@ -339,17 +346,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
         if (!bar_wait(acc_empty(buf), ((a >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
         tc_after();
         const uint32_t d = tmem + buf * MM_N;
-        for (int c = 0; c < chunks; ++c, ++g) {
+        bool ready = bar_try(full(g % MM_STAGES), (g / MM_STAGES) & 1u);
+        for (int c = 0; c < chunks; ++c) {
           const int s = g % MM_STAGES;
-          if (!bar_wait(full(s), (g / MM_STAGES) & 1u, abort_flag)) { ok = false; break; }
+          if (!ready && !bar_wait(full(s), (g / MM_STAGES) & 1u, abort_flag)) { ok = false; break; }
+          ++g;
+          if (c + 1 < chunks) ready = bar_try(full(g % MM_STAGES), (g / MM_STAGES) & 1u);
           tc_after();
+          if (elected()) {
 #pragma unroll
-          for (int k = 0; k < 4; ++k)  // 32 bytes of k; rows inner: 16 k's, two blocks of 1024 bytes
-            mma_pair<FP8>(d, da + ((s * MM_STAGE + k * (AT ? 2048 : 32)) >> 4), db + ((s * MM_STAGE + k * (BT ? 2048 : 32)) >> 4),
-                          idesc, (c | k) ? 1u : 0u);
-          commit_pair(empty(s));
+            for (int k = 0; k < 4; ++k)  // 32 bytes of k; rows inner: 16 k's, two blocks of 1024 bytes
+              mma_pair<FP8>(d, da + ((s * MM_STAGE + k * (AT ? 2048 : 32)) >> 4), db + ((s * MM_STAGE + k * (BT ? 2048 : 32)) >> 4),
+                            idesc, (c | k) ? 1u : 0u);
+            commit_pair(empty(s));
+          }
+          __syncwarp();
         }
-        if (ok) commit_pair(acc_full(buf));
+        if (ok && elected()) commit_pair(acc_full(buf));
+        __syncwarp();
         ++a;
       }
     }
