@@ -11,13 +11,14 @@ constexpr int MM_STAGES = 5;
 constexpr int MM_OPERAND = 16 * 1024;          // one CTA's part of a chunk of A or of B: 128 rows of 128 bytes
 constexpr int MM_STAGE = 2 * MM_OPERAND;
 constexpr int MM_TEAMS = 2;                    // epilogue teams of 4 warps (a warp reads the 32 lanes of tensor memory of its number mod 4)
-constexpr int MM_WARP_COPY = 4 * MM_TEAMS, MM_WARP_MMA = MM_WARP_COPY + 1, MM_WARP_CLEAR = MM_WARP_COPY + 2;
+constexpr int MM_WARP_A = 4 * MM_TEAMS, MM_WARP_B = MM_WARP_A + 1, MM_WARP_MMA = MM_WARP_A + 2, MM_WARP_CLEAR = MM_WARP_A + 3;
 constexpr int MM_THREADS = (MM_WARP_CLEAR + 1) * 32;
 constexpr int MM_COLS = 16;                    // accumulator columns of one of the two transposing buffers
 constexpr int MM_STEP = 2 * MM_COLS;           // ... of an epilogue step; the teams take steps in turn
 constexpr int MM_PITCH = 128 + 4;              // floats of a row of the transposing buffer
 constexpr int MM_STAGING = MM_TEAMS * 2 * MM_COLS * MM_PITCH * 4;
 constexpr int MM_CONTROL = 512;
+constexpr uint32_t STAGE_FIRST = 1u << 16, STAGE_LAST = 1u << 17, STAGE_END = 1u << 18;  // a tile's first / last chunk; no more tiles
 constexpr int MM_TABLE = (DEAMOE_MAX_EXPERTS + 1) * 8 + 8;  // groups' first tile and first row
 constexpr size_t MM_SMEM = (size_t)MM_STAGES * MM_STAGE + MM_STAGING + MM_CONTROL + MM_TABLE;
 static_assert(MM_SMEM <= 227 * 1024, "shared memory budget");
@@ -129,7 +130,7 @@ __device__ __forceinline__ void team_sync(int team) { asm volatile("bar.sync %0,
 struct Tile {
   int group;
   int m0, n0;    // first row of A in the group; first row of B: in all rows (grouped rows) or in the group
-  int n, valid;  // width (a multiple of 32), and its columns that exist
+  int n, valid;  // width (a multiple of 16), and its columns that exist
   int row0, rows;  // the group's rows (ragged contraction)
   int n_index;   // index of the tile along N in its group
 };
@@ -156,13 +157,16 @@ template <bool RAGGED> __device__ __forceinline__ Tile find_tile(const MatmulArg
   const int width = min(MM_BAND, nt - band * MM_BAND);
   const int mi = rest / width, ni = band * MM_BAND + rest - mi * width;
   const int per = (cols + nt - 1) / nt;
-  o.n = (per + 31) & ~31;
+  o.n = (per + 15) & ~15;
   o.m0 = mi * m_step;
   o.n_index = ni;
   o.valid = min(o.n, cols - ni * o.n);
   o.n0 = ni * o.n + (RAGGED ? 0 : o.row0);
   return o;
 }
+
+// the lowest box (16, 32, 64 or 128 rows of B) that holds a CTA's half of a tile: one copy a chunk, whatever it brings along
+__device__ __forceinline__ int box_of(int half) { return half <= 16 ? 0 : half <= 32 ? 1 : half <= 64 ? 2 : 3; }
 
 // ---------------------------------------------------------------- epilogue arithmetic
 __device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
@@ -221,10 +225,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   auto cleared = [&](int s) { return bars + 8 * (3 * MM_STAGES + s); };
   auto acc_full = [&](int b) { return bars + 8 * (4 * MM_STAGES + b); };
   auto acc_empty = [&](int b) { return bars + 8 * (4 * MM_STAGES + 2 + b); };
+  const uint32_t first_full = in_first(full(0));
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(control + 4 * MM_STAGES + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* warp_sums = reinterpret_cast<int*>(tmem_slot + 2);
-  static_assert((4 * MM_STAGES + 4) * 8 + 8 + 16 * 4 <= MM_CONTROL, "control region");
+  uint32_t* info = tmem_slot + 2 + 16;  // [MM_STAGES] width of a stage's tile, STAGE_* flags
+  static_assert((4 * MM_STAGES + 4) * 8 + 8 + 16 * 4 + MM_STAGES * 4 <= MM_CONTROL, "control region");
   int* first_row = reinterpret_cast<int*>(smem + (size_t)MM_STAGES * MM_STAGE + MM_STAGING + MM_CONTROL);
   int* first_tile = first_row + A.groups + 1;
 
@@ -276,53 +282,56 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   const int pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
   auto chunks_of = [&](const Tile& t) { return ((RAGGED ? t.rows : A.K) + A.chunk - 1) / A.chunk; };
 
-  if (warp == MM_WARP_COPY) {
+  if (warp == MM_WARP_A || warp == MM_WARP_B) {
     // ============================================================ copies
-    if (lane == 0) {
-      uint32_t g = 0;
-      bool ok = true;
-      for (int it = pair; ok && it < tiles; it += pairs) {
-        const Tile t = find_tile<RAGGED>(A, first_tile, first_row, it, M_STEP);
-        const int half = t.n / 2, chunks = chunks_of(t);
-        const uint32_t bytes = MM_OPERAND + (BT ? MM_OPERAND : half * 128);
-        for (int c = 0; c < chunks; ++c, ++g) {
-          const int s = g % MM_STAGES;
-          if (!bar_wait(empty(s), ((g / MM_STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-          const uint32_t a = ring + s * MM_STAGE, b = a + MM_OPERAND;
-          uint32_t bar = in_first(full(s));
-          const int k0 = c * A.chunk;
-          if (RAGGED && k0 + A.chunk > t.rows) {  // rows of the next group come along: this CTA's clearing warp sees them first
-            bar = tail(s);
-            bar_expect(bar, bytes);
-          } else if (rank == 0) {
-            bar_expect(full(s), 2 * bytes);
+    // A chunk's issue has to fit the 512 cycles of its MMAs here too, and a copy costs its thread some 100: one warp an
+    // operand, one box a chunk where the layout allows it, uniform values as in the MMA role.
+    const bool is_a = warp == MM_WARP_A;
+    uint32_t g = 0;
+    bool ok = true, free = true;  // (the first round of the ring is free)
+    const bool rows_inner = is_a ? AT : BT;
+    for (int it = pair; ok && it < tiles; it += pairs) {
+      const Tile t = find_tile<RAGGED>(A, first_tile, first_row, it, M_STEP);
+      const int half = t.n / 2, chunks = chunks_of(t);
+      const int box = BT ? 3 : box_of(half);
+      const uint32_t bytes = MM_OPERAND + (BT ? MM_OPERAND : 128 * (16 << box));
+      const int at = is_a ? t.m0 + (int)rank * (M_STEP / 2) : t.n0 + (int)rank * half;  // first row of this CTA's part
+      const int z = is_a && !RAGGED ? t.group : 0;
+      const CUtensorMap* map = is_a ? &maps.a : &maps.b[BT ? 0 : box];
+      for (int c = 0; c < chunks; ++c, ++g) {
+        const int s = g % MM_STAGES;
+        if (!free && !bar_wait(empty(s), ((g / MM_STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+        const int k0 = c * A.chunk, k = RAGGED ? t.row0 + k0 : k0;
+        // rows of the next group come along: this CTA's clearing warp sees them first
+        const bool last_rows = RAGGED && k0 + A.chunk > t.rows;
+        const uint32_t bar = last_rows ? tail(s) : first_full + 8 * s, dst = ring + s * MM_STAGE + (is_a ? 0 : MM_OPERAND);
+        if (elected()) {
+          if (is_a && (last_rows || rank == 0)) {
+            info[s] = t.n | (c == 0 ? STAGE_FIRST : 0) | (c + 1 == chunks ? STAGE_LAST : 0);
+            bar_expect(last_rows ? tail(s) : full(s), last_rows ? bytes : 2 * bytes);
           }
-          const int ka = RAGGED ? t.row0 + k0 : k0;
-          if constexpr (DUAL) {
-            load_5d(a, &maps.a, k0, 0, 0, (t.m0 + (int)rank * 64) / 8, t.group, bar);
-          } else if constexpr (AT) {
-            const int m = t.m0 + rank * 128;
-            load_3d(a, &maps.a, m, ka, RAGGED ? 0 : t.group, bar);
-            load_3d(a + MM_OPERAND / 2, &maps.a, m + 64, ka, RAGGED ? 0 : t.group, bar);
+          if (DUAL && is_a) {
+            load_5d(dst, map, k0, 0, 0, at / 8, z, bar);
+          } else if (rows_inner) {
+            load_3d(dst, map, at, k, z, bar);
+            load_3d(dst + MM_OPERAND / 2, map, at + 64, k, z, bar);
           } else {
-            load_3d(a, &maps.a, k0, t.m0 + rank * 128, t.group, bar);
-          }
-          const int n = t.n0 + rank * half;
-          if constexpr (BT) {
-            load_3d(b, &maps.b[0], n, ka, 0, bar);
-            load_3d(b + MM_OPERAND / 2, &maps.b[0], n + 64, ka, 0, bar);
-          } else if (half == 128) {
-            load_3d(b, &maps.b[2], k0, n, 0, bar);
-          } else {
-            int r = 0;
-            if (half >= 64) {
-              load_3d(b, &maps.b[1], k0, n, 0, bar);
-              r = 64;
-            }
-            for (; r < half; r += 16) load_3d(b + r * 128, &maps.b[0], k0, n + r, 0, bar);
+            load_3d(dst, map, k, at, z, bar);
           }
         }
+        __syncwarp();
+        const uint32_t next = g + 1;
+        free = next < MM_STAGES || bar_try(empty(next % MM_STAGES), ((next / MM_STAGES) & 1u) ^ 1u);
       }
+    }
+    if (ok && is_a) {  // the end of the list, to the MMA role
+      const int s = g % MM_STAGES;
+      ok = free || bar_wait(empty(s), ((g / MM_STAGES) & 1u) ^ 1u, abort_flag);
+      if (ok && rank == 0 && elected()) {
+        info[s] = STAGE_END;
+        bar_expect(full(s), 0);
+      }
+      __syncwarp();
       // the last commits must have arrived here before this CTA may end
       for (uint32_t d = g > MM_STAGES ? g - MM_STAGES : 0; ok && d < g; ++d)
         ok = bar_wait(empty(d % MM_STAGES), (d / MM_STAGES) & 1u, abort_flag);
@@ -330,41 +339,39 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   } else if (warp == MM_WARP_MMA) {
     // ============================================================ MMAs, by the pair's first CTA
     // The issue of a chunk has to fit the 512 cycles of its MMAs.  The whole warp walks the loop, so that descriptors are
-    // warp-uniform values, and one elected thread issues; the next stage is asked for before this one's MMAs are issued.
+    // warp-uniform values, and one elected thread issues; the next stage is asked for before this one's MMAs are issued; what a
+    // stage holds the copy role has written beside it.
     if (rank == 0) {
       uint32_t g = 0, a = 0;
-      bool ok = true;
       const uint64_t da = operand_desc(ring, AT ? MM_OPERAND / 2 : 16, 1024);
       const uint64_t db = operand_desc(ring + MM_OPERAND, BT ? MM_OPERAND / 2 : 16, 1024);
       // fp32 sums of bf16 (or e4m3: type 0) values, 256 rows, both CTAs
       const uint32_t kind = 1u << 4 | (FP8 ? 0u : (1u << 7 | 1u << 10)) | (AT ? 1u << 15 : 0u) | (BT ? 1u << 16 : 0u) | (MM_M >> 4) << 24;
-      for (int it = pair; ok && it < tiles; it += pairs) {
-        const Tile t = find_tile<RAGGED>(A, first_tile, first_row, it, M_STEP);
-        const int chunks = chunks_of(t);
-        if (RAGGED && chunks == 0) continue;
-        const uint32_t buf = a & 1u, idesc = kind | (uint32_t)(t.n >> 3) << 17;
-        if (!bar_wait(acc_empty(buf), ((a >> 1) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-        tc_after();
-        const uint32_t d = tmem + buf * MM_N;
-        bool ready = bar_try(full(g % MM_STAGES), (g / MM_STAGES) & 1u);
-        for (int c = 0; c < chunks; ++c) {
-          const int s = g % MM_STAGES;
-          if (!ready && !bar_wait(full(s), (g / MM_STAGES) & 1u, abort_flag)) { ok = false; break; }
-          ++g;
-          if (c + 1 < chunks) ready = bar_try(full(g % MM_STAGES), (g / MM_STAGES) & 1u);
-          tc_after();
-          if (elected()) {
-#pragma unroll
-            for (int k = 0; k < 4; ++k)  // 32 bytes of k; rows inner: 16 k's, two blocks of 1024 bytes
-              mma_pair<FP8>(d, da + ((s * MM_STAGE + k * (AT ? 2048 : 32)) >> 4), db + ((s * MM_STAGE + k * (BT ? 2048 : 32)) >> 4),
-                            idesc, (c | k) ? 1u : 0u);
-            commit_pair(empty(s));
-          }
-          __syncwarp();
+      uint32_t d = tmem, idesc = 0;
+      bool ready = bar_try(full(0), 0);
+      for (;; ++g) {
+        const int s = g % MM_STAGES;
+        if (!ready && !bar_wait(full(s), (g / MM_STAGES) & 1u, abort_flag)) break;
+        const uint32_t what = *(volatile uint32_t*)(info + s);
+        if (what & STAGE_END) break;
+        const bool first = what & STAGE_FIRST;
+        if (first) {
+          idesc = kind | (what & 0x1ffu) >> 3 << 17;
+          d = tmem + (a & 1u) * MM_N;
+          if (!bar_wait(acc_empty(a & 1u), ((a >> 1) & 1u) ^ 1u, abort_flag)) break;
         }
-        if (ok && elected()) commit_pair(acc_full(buf));
+        ready = bar_try(full((g + 1) % MM_STAGES), ((g + 1) / MM_STAGES) & 1u);
+        tc_after();
+        if (elected()) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)  // 32 bytes of k; rows inner: 16 k's, two blocks of 1024 bytes
+            mma_pair<FP8>(d, da + ((s * MM_STAGE + k * (AT ? 2048 : 32)) >> 4), db + ((s * MM_STAGE + k * (BT ? 2048 : 32)) >> 4),
+                          idesc, (first && k == 0) ? 0u : 1u);
+          commit_pair(empty(s));
+          if (what & STAGE_LAST) commit_pair(acc_full(a & 1u));
+        }
         __syncwarp();
-        ++a;
+        if (what & STAGE_LAST) ++a;
       }
     }
   } else if (warp == MM_WARP_CLEAR) {
@@ -649,8 +656,9 @@ bool map_gate_up(CUtensorMap* m, const void* p, int64_t cols, int64_t f, int64_t
   return encode(m, p, 2, 5, dims, strides, box);
 }
 bool map_b(MatmulMaps* m, const void* p, int esize, int64_t cols, int64_t rows, int64_t stride) {
-  return map_rows(&m->b[0], p, esize, cols, rows, stride, 1, stride, 16) && map_rows(&m->b[1], p, esize, cols, rows, stride, 1, stride, 64) &&
-         map_rows(&m->b[2], p, esize, cols, rows, stride, 1, stride, 128);
+  for (int i = 0; i < 4; ++i)
+    if (!map_rows(&m->b[i], p, esize, cols, rows, stride, 1, stride, 16 << i)) return false;
+  return true;
 }
 
 int matmul_tile_n(int64_t n, int64_t m_tiles) {

@@ -5,7 +5,7 @@
 //
 // A is the operand whose rows become the outputs' columns (a weight matrix, or the inputs in a weight gradient), B the one
 // whose rows become the outputs' rows (tokens; the outputs' gradients in a weight gradient).  With the tokens on the
-// N side a group of any size is a tile of its own width (32 to 256 columns in steps of 32), from a decode step's few rows
+// N side a group of any size is a tile of its own width (16 to 256 columns in steps of 16), from a decode step's few rows
 // an expert to a prompt's thousands, and the matrix side is always full.
 //
 // What bounds it.  A bf16 MMA of 256 x 256 x 16 by a pair keeps both SMs' tensor cores busy for 128 cycles; each CTA's
@@ -14,9 +14,9 @@
 //
 // Roles of a CTA (1 CTA per SM, clusters of 2, tiles dealt in a fixed order so that equal calls give equal bits):
 //   warps 0-7  epilogue, two teams that share a tile's columns: accumulator -> registers -> a small transposing buffer -> 16-byte rows, with the epilogue's arithmetic in fp32
-//   warp  8    one thread issues the TMA copies of a chunk (128 bytes of k, 128-byte swizzle) into a ring of 5 stages
-//   warp  9    in the pair's first CTA one thread issues the MMAs for both
-//   warp  10   ragged contractions (weight gradients: k runs over a group's rows): clears the rows behind the group's end
+//   warps 8, 9 one thread each issues the TMA copies of A's / B's part of a chunk (128 bytes of k, 128-byte swizzle) into a ring of 5 stages
+//   warp  10   in the pair's first CTA one thread issues the MMAs for both
+//   warp  11   ragged contractions (weight gradients: k runs over a group's rows): clears the rows behind the group's end
 //              that the last chunk's box brought in, in both operands, before the MMAs may read them
 // Two accumulators of 256 columns take turns in tensor memory, so an epilogue runs under the next tile's MMAs.
 // Every wait is bounded; one that expires ends the CTA's roles and raises the status word that
@@ -61,7 +61,7 @@ struct MatmulArgs {
 
 struct MatmulMaps {
   CUtensorMap a;
-  CUtensorMap b[3];  // B with k as the inner axis: boxes of 16, 64 and 128 rows; else b[0] alone
+  CUtensorMap b[4];  // B with k as the inner axis: boxes of 16, 32, 64 and 128 rows; else b[0] alone
 };
 
 // Launch one product.  kind: epilogue; a_rows_inner / b_rows_inner: A / B stored with its rows as the inner axis; fp8: e4m3.
