@@ -11,6 +11,7 @@
 // forward pass: gate and up would cost 4 bytes a value to keep exactly, and recomputing them lets no rounding but the
 // operands' into a gradient.
 #include "matmul.cuh"
+#include "thin.cuh"
 
 namespace deamoe {
 
@@ -61,6 +62,16 @@ deamoe_status_t deamoe_ffn(void* cuda_stream, const void* x, int64_t x_stride, c
   if (bad_rows8(out, out_stride, hidden) || out == x) return DEAMOE_ERR_INVALID_ARG;
   if (!workspace || !aligned16(workspace) || workspace_bytes < deamoe_ffn_workspace(n_rows, ffn, 0)) return DEAMOE_ERR_INVALID_ARG;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+  if (n_rows <= THIN_ROWS) {
+    ThinArgs a = {};
+    a.x = x; a.xs = x_stride; a.w = w_gate_up; a.M = ffn; a.K = hidden; a.n_rows = n_rows; a.groups = n_expert; a.off = expert_off;
+    a.out = reinterpret_cast<__nv_bfloat16*>(workspace); a.os = ffn;
+    ThinArgs b = a;
+    b.x = workspace; b.xs = ffn; b.w = w_down; b.M = hidden; b.K = ffn; b.out = reinterpret_cast<__nv_bfloat16*>(out); b.os = out_stride;
+    if (thin_launch(false, true, a, s, false) == cudaSuccess && thin_launch(false, false, b, s, true) == cudaSuccess) return DEAMOE_OK;
+    cudaGetLastError();
+    return DEAMOE_ERR_CUDA;
+  }
   const FfnShape S = {n_expert, n_rows, hidden, ffn, expert_off};
   MatmulCall up = ffn_call(S, ffn, hidden), down = ffn_call(S, hidden, ffn);
   up.args.out = workspace; up.args.os = ffn;

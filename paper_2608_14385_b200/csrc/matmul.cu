@@ -661,9 +661,22 @@ bool map_b(MatmulMaps* m, const void* p, int esize, int64_t cols, int64_t rows, 
   return true;
 }
 
+// The pairs take the tiles in rounds, and a round costs a tile's width and some 100 columns more (2048 x 4096 x 4096: rounds of
+// 144, 240 and 256 columns 21, 28 and 30 us), so a narrower tile pays where it saves a part of the last round: 3000 x
+// 2000 x 4096 in 18 tiles of 176 48 us, in 12 of 256 57; 1024 x 7168 x 7168 in 5 of 208 98 us, in 4 of 256 107.
 int matmul_tile_n(int64_t n, int64_t m_tiles) {
-  (void)n; (void)m_tiles;
-  return MM_N;
+  int best = MM_N;
+  int64_t least = INT64_MAX;
+  for (int64_t nt = (n + MM_N - 1) / MM_N, k = 0; k < 8; ++nt, ++k) {
+    const int64_t width = ((n + nt - 1) / nt + 15) / 16 * 16;
+    if (k > 0 && width < MM_N_LEAST) break;
+    const int64_t cost = (nt * m_tiles + MM_PAIRS - 1) / MM_PAIRS * (width + 100);
+    if (cost < least) {
+      least = cost;
+      best = (int)width;
+    }
+  }
+  return best;
 }
 
 cudaError_t matmul_launch(MatmulForm form, const MatmulCall& c, cudaStream_t s, bool chained) {

@@ -84,7 +84,7 @@ bool map_b(MatmulMaps* m, const void* p, int esize, int64_t cols, int64_t rows, 
 int matmul_tile_n(int64_t n, int64_t m_tiles);
 
 constexpr int MM_M = 256, MM_N = 256;
-constexpr int MM_N_LEAST = 128;  // matmul_tile_n gives no less
+constexpr int MM_N_LEAST = 64;   // matmul_tile_n gives no less for more rows
 constexpr int MM_PARTS = 2;      // rows of sums that a tile leaves in `part`
 
 }  // namespace deamoe

@@ -9,6 +9,7 @@
 // operand of the two products behind it, db is summed from the unrounded dz.  Without an activation dz is dout itself and no
 // product but dx and dW runs.
 #include "matmul.cuh"
+#include "thin.cuh"
 
 namespace deamoe {
 
@@ -94,6 +95,15 @@ deamoe_status_t deamoe_product(void* cuda_stream, int32_t dtype, const void* x, 
       !aligned_to(out, 2) || out_stride < n_out || out == x || out == weight || !aligned_to(residual, 2) ||
       (residual && residual_stride < n_out) || (residual == out && residual && residual_stride != out_stride))
     return DEAMOE_ERR_INVALID_ARG;
+  if (n_token <= THIN_ROWS) {
+    ThinArgs a = {};
+    a.x = x; a.xs = x_stride; a.w = weight; a.M = n_out; a.K = n_in; a.n_rows = n_token; a.groups = 1;
+    a.out = reinterpret_cast<__nv_bfloat16*>(out); a.os = out_stride; a.x_scale = x_scale; a.w_scale = weight_scale;
+    a.bias = bias; a.bias_f32 = bias_dtype == DEAMOE_F32; a.act = act; a.residual = residual; a.rs = residual_stride;
+    if (thin_launch(e4m3, false, a, reinterpret_cast<cudaStream_t>(cuda_stream), false) == cudaSuccess) return DEAMOE_OK;
+    cudaGetLastError();
+    return DEAMOE_ERR_CUDA;
+  }
   MatmulCall c = product_call(n_out, n_in, n_token, e4m3 ? 128 : 64);
   c.args.out = out; c.args.os = out_stride; c.args.wide = wide_rows(out, out_stride, n_token, 2);
   c.args.bias = bias; c.args.bias_f32 = bias_dtype == DEAMOE_F32; c.args.act = act;
