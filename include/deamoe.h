@@ -483,7 +483,7 @@ deamoe_status_t deamoe_norm_residual_quant(void *cuda_stream, int32_t dtype, con
  * matrices; an expert without rows gets zeros).  Gate and up are recomputed in fp32, the gradients of gate and up are rounded to
  * bf16 once.  hidden and ffn: multiples of 8 (else UNSUPPORTED).
  */
-uint64_t deamoe_ffn_workspace(int32_t n_rows, int32_t ffn, int32_t backward);
+uint64_t deamoe_ffn_workspace(int32_t n_expert, int32_t n_rows, int32_t hidden, int32_t ffn, int32_t backward);
 deamoe_status_t deamoe_ffn(void *cuda_stream, const void *x, int64_t x_stride, const void *w_gate_up, const void *w_down,
                            const int32_t *expert_off, int32_t n_expert, int32_t n_rows, int32_t hidden, int32_t ffn,
                            void *out, int64_t out_stride, void *workspace, uint64_t workspace_bytes);
@@ -511,11 +511,12 @@ deamoe_status_t deamoe_ffn_backward(void *cuda_stream, const void *x, int64_t x_
  *   dz = dout act'(z),   dx = dz W,   dweight = dz^T x (bf16),   dbias = sum over tokens of dz (fp32, or NULL)
  * The residual's gradient is dout.  z is recomputed in fp32; dz is rounded to bf16 once for dx and dweight, not for dbias.
  */
-uint64_t deamoe_product_workspace(int32_t n_token, int32_t n_out, int32_t act); /* of the backward call */
+uint64_t deamoe_product_workspace(int32_t dtype, int32_t n_token, int32_t n_out, int32_t n_in, int32_t act, int32_t backward);
 deamoe_status_t deamoe_product(void *cuda_stream, int32_t dtype, const void *x, int64_t x_stride, const float *x_scale,
                                int32_t n_token, const void *weight, const float *weight_scale, int32_t n_out, int32_t n_in,
                                int32_t bias_dtype, const void *bias, int32_t act, const void *residual,
-                               int64_t residual_stride, void *out, int64_t out_stride);
+                               int64_t residual_stride, void *out, int64_t out_stride, void *workspace,
+                               uint64_t workspace_bytes);
 deamoe_status_t deamoe_product_backward(void *cuda_stream, int32_t dtype, const void *x, int64_t x_stride, int32_t n_token,
                                         const void *weight, int32_t n_out, int32_t n_in, int32_t bias_dtype, const void *bias,
                                         int32_t act, const void *dout, int64_t dout_stride, void *dx, int64_t dx_stride,

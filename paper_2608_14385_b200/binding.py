@@ -117,11 +117,11 @@ def lib():
                 ("deamoe_quant_product", i, (p, i, p, i, p, p, i, i, i, i, p, l, i, p, p, i, i, i, p, l, p, u)),
                 ("deamoe_norm_quant", i, (p, i, p, l, i, i, i, i, p, f, p, l, p)),
                 ("deamoe_norm_residual_quant", i, (p, i, p, l, p, l, i, i, i, i, p, f, i, p, l, f, f, p, l, p, f, p, l, p)),
-                ("deamoe_ffn_workspace", u, (i, i, i)),
+                ("deamoe_ffn_workspace", u, (i, i, i, i, i)),
                 ("deamoe_ffn", i, (p, p, l, p, p, p, i, i, i, i, p, l, p, u)),
                 ("deamoe_ffn_backward", i, (p, p, l, p, p, p, l, p, i, i, i, i, p, l, p, p, p, u)),
-                ("deamoe_product_workspace", u, (i, i, i)),
-                ("deamoe_product", i, (p, i, p, l, p, i, p, p, i, i, i, p, i, p, l, p, l)),
+                ("deamoe_product_workspace", u, (i, i, i, i, i, i)),
+                ("deamoe_product", i, (p, i, p, l, p, i, p, p, i, i, i, p, i, p, l, p, l, p, u)),
                 ("deamoe_product_backward", i, (p, i, p, l, i, p, i, i, i, p, i, p, l, p, l, p, p, p, u)),
                 ("deamoe_operator_status", i, (p, C.POINTER(C.c_int32)))):
             getattr(L, name).restype = res
@@ -598,7 +598,7 @@ def ffn(x, w_gate_up, w_down, expert_off=None, out=None):
         out = x.new_empty((R, h))
     po, so = _mat(out, where, "out", torch.bfloat16, R, h, dev)
     L = lib()
-    need = L.deamoe_ffn_workspace(R, f, 0)
+    need = L.deamoe_ffn_workspace(E, R, h, f, 0)
     ws = _workspace(need, x)
     _done(L.deamoe_ffn(_raw_stream(dev), px, sx, pu, pd, pe, E, R, h, f, po, so, _ptr(ws), need), where)
     return out
@@ -618,7 +618,7 @@ def ffn_backward(x, w_gate_up, w_down, dout, expert_off=None, dx=None, dw_gate_u
     po, so = _mat(dout, where, "dout", torch.bfloat16, R, h, dev)
     pg, sg = _mat(dx, where, "dx", torch.bfloat16, R, h, dev)
     L = lib()
-    need = L.deamoe_ffn_workspace(R, f, 1)
+    need = L.deamoe_ffn_workspace(E, R, h, f, 1)
     ws = _workspace(need, x)
     _done(L.deamoe_ffn_backward(_raw_stream(dev), px, sx, pu, pd, po, so, pe, E, R, h, f, pg, sg,
                                 _vec(dw_gate_up, where, "dw_gate_up", torch.bfloat16, (E, 2 * f, h), dev),
@@ -661,7 +661,10 @@ def product(x, weight, bias=None, act=SIGMA_NONE, residual=None, x_scale=None, w
     pr, sr = _mat(residual, where, "residual", torch.bfloat16, T, N, dev) if residual is not None else (None, 0)
     psx = _vec(x_scale, where, "x_scale", torch.float32, (T,), dev) if x_scale is not None else None
     psw = _vec(weight_scale, where, "weight_scale", torch.float32, (N,), dev) if weight_scale is not None else None
-    _done(lib().deamoe_product(_raw_stream(dev), dt, px, sx, psx, T, pw, psw, N, K, bdt, pb, act, pr, sr, po, so), where)
+    L = lib()
+    need = L.deamoe_product_workspace(dt, T, N, K, act, 0)
+    ws = x.new_empty(need, dtype=torch.uint8) if need else None
+    _done(L.deamoe_product(_raw_stream(dev), dt, px, sx, psx, T, pw, psw, N, K, bdt, pb, act, pr, sr, po, so, _ptr(ws), need), where)
     return out
 
 
@@ -680,7 +683,7 @@ def product_backward(x, weight, dout, bias=None, act=SIGMA_NONE, dx=None, dweigh
     po, so = _mat(dout, where, "dout", torch.bfloat16, T, N, dev)
     pd, sd = _mat(dx, where, "dx", torch.bfloat16, T, K, dev)
     L = lib()
-    need = L.deamoe_product_workspace(T, N, act)
+    need = L.deamoe_product_workspace(BF16, T, N, K, act, 1)
     ws = _workspace(need, x)
     _done(L.deamoe_product_backward(_raw_stream(dev), BF16, px, sx, T, pw, N, K, bdt, pb, act, po, so, pd, sd,
                                     _vec(dweight, where, "dweight", torch.bfloat16, (N, K), dev), _ptr(dbias), _ptr(ws), need), where)

@@ -24,9 +24,20 @@ struct FfnShape {
 
 static MatmulCall ffn_call(const FfnShape& S, int M, int K) {
   MatmulCall c = {};
-  c.args.M = M; c.args.K = K; c.args.N = S.R; c.args.groups = S.E; c.args.off = S.off; c.args.tile_n = MM_N; c.args.chunk = 64;
+  c.args.M = M; c.args.K = K; c.args.N = S.R; c.args.groups = S.E; c.args.off = S.off; c.args.tile_n = MM_N; c.args.chunk = 64; c.args.splits = 1;
   c.args.f = S.f; c.args.wide = 1;
   return c;
+}
+
+// A forward product's parts of k: M rows of a matrix (gate and up: of both), K columns.
+static int ffn_splits(int E, int R, int64_t M, int64_t K) {
+  const int64_t tiles = (M + MM_M - 1) / MM_M * (R / MM_N + (E < R ? E : R));  // no more than that, whatever the offsets
+  return matmul_splits(tiles, (K + 63) / 64, R);
+}
+static uint64_t ffn_parts_bytes(int E, int R, int h, int f) {
+  const int a = ffn_splits(E, R, 2 * (int64_t)f, h), b = ffn_splits(E, R, h, f);
+  const uint64_t up = a > 1 ? (uint64_t)a * R * 2 * f * 4 : 0, down = b > 1 ? (uint64_t)b * R * h * 4 : 0;
+  return up > down ? up : down;
 }
 
 static deamoe_status_t check_ffn(const void* x, int64_t xs, const void* wgu, const void* wd, const int32_t* off, int E, int R, int h, int f) {
@@ -48,10 +59,11 @@ using namespace deamoe;
 
 extern "C" {
 
-uint64_t deamoe_ffn_workspace(int32_t n_rows, int32_t ffn, int32_t backward) {
-  if (n_rows <= 0 || ffn <= 0) return 0;
+uint64_t deamoe_ffn_workspace(int32_t n_expert, int32_t n_rows, int32_t hidden, int32_t ffn, int32_t backward) {
+  if (n_expert <= 0 || n_rows <= 0 || hidden <= 0 || ffn <= 0) return 0;
   const uint64_t v = (uint64_t)n_rows * ffn;
-  return backward ? ceil256(4 * v) + ceil256(4 * v) + ceil256(2 * v) : ceil256(2 * v);
+  if (backward) return ceil256(4 * v) + ceil256(4 * v) + ceil256(2 * v);
+  return ceil256(2 * v) + (n_rows <= THIN_ROWS ? 0 : ffn_parts_bytes(n_expert, n_rows, hidden, ffn));
 }
 
 deamoe_status_t deamoe_ffn(void* cuda_stream, const void* x, int64_t x_stride, const void* w_gate_up, const void* w_down,
@@ -60,7 +72,7 @@ deamoe_status_t deamoe_ffn(void* cuda_stream, const void* x, int64_t x_stride, c
   deamoe_status_t st = check_ffn(x, x_stride, w_gate_up, w_down, expert_off, n_expert, n_rows, hidden, ffn);
   if (st != DEAMOE_OK || n_rows == 0) return st;
   if (bad_rows8(out, out_stride, hidden) || out == x) return DEAMOE_ERR_INVALID_ARG;
-  if (!workspace || !aligned16(workspace) || workspace_bytes < deamoe_ffn_workspace(n_rows, ffn, 0)) return DEAMOE_ERR_INVALID_ARG;
+  if (!workspace || !aligned16(workspace) || workspace_bytes < deamoe_ffn_workspace(n_expert, n_rows, hidden, ffn, 0)) return DEAMOE_ERR_INVALID_ARG;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
   if (n_rows <= THIN_ROWS) {
     ThinArgs a = {};
@@ -76,11 +88,36 @@ deamoe_status_t deamoe_ffn(void* cuda_stream, const void* x, int64_t x_stride, c
   MatmulCall up = ffn_call(S, ffn, hidden), down = ffn_call(S, hidden, ffn);
   up.args.out = workspace; up.args.os = ffn;
   down.args.out = out; down.args.os = out_stride;
+  // few tiles: dealt along k, the parts' sums joined by a kernel of their own
+  const int up_splits = ffn_splits(n_expert, n_rows, 2 * (int64_t)ffn, hidden), down_splits = ffn_splits(n_expert, n_rows, hidden, ffn);
+  float* part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + ceil256(2 * (uint64_t)n_rows * ffn));
+  auto joined = [&](MatmulCall& c, int splits, bool dual) {
+    JoinArgs j = {};
+    j.part = part; j.splits = splits; j.n_rows = n_rows; j.M = c.args.M; j.groups = n_expert; j.dual = dual; j.off = expert_off;
+    j.out = reinterpret_cast<__nv_bfloat16*>(c.args.out); j.os = c.args.os; j.wide = 1;
+    c.args.splits = splits; c.args.out = part; c.args.os = (int64_t)c.args.M * (dual ? 2 : 1); c.args.out_group = c.args.os * n_rows;
+    return j;
+  };
   if (!map_gate_up(&up.maps.a, w_gate_up, hidden, ffn, n_expert) || !map_b(&up.maps, x, 2, hidden, n_rows, x_stride) ||
       !map_rows(&down.maps.a, w_down, 2, ffn, hidden, ffn, n_expert, (int64_t)hidden * ffn, 128) ||
       !map_b(&down.maps, workspace, 2, ffn, n_rows, ffn))
     return DEAMOE_ERR_CUDA;
-  if (matmul_launch(MF_SWIGLU, up, s, false) == cudaSuccess && matmul_launch(MF_STORE, down, s, true) == cudaSuccess) return DEAMOE_OK;
+  cudaError_t e;
+  if (up_splits > 1) {
+    const JoinArgs j = joined(up, up_splits, true);
+    e = matmul_launch(MF_PART_SWIGLU, up, s, false);
+    if (e == cudaSuccess) e = join_launch(j, s);
+  } else {
+    e = matmul_launch(MF_SWIGLU, up, s, false);
+  }
+  if (e == cudaSuccess && down_splits > 1) {
+    const JoinArgs j = joined(down, down_splits, false);
+    e = matmul_launch(MF_PART, down, s, true);
+    if (e == cudaSuccess) e = join_launch(j, s);
+  } else if (e == cudaSuccess) {
+    e = matmul_launch(MF_STORE, down, s, true);
+  }
+  if (e == cudaSuccess) return DEAMOE_OK;
   cudaGetLastError();
   return DEAMOE_ERR_CUDA;
 }
@@ -100,7 +137,7 @@ deamoe_status_t deamoe_ffn_backward(void* cuda_stream, const void* x, int64_t x_
     return cudaMemsetAsync(dw_gate_up, 0, 2 * wd_bytes, s) == cudaSuccess && cudaMemsetAsync(dw_down, 0, wd_bytes, s) == cudaSuccess
                ? DEAMOE_OK : DEAMOE_ERR_CUDA;
   if (bad_rows8(dout, dout_stride, hidden) || bad_rows8(dx, dx_stride, hidden) || dx == x || dx == dout) return DEAMOE_ERR_INVALID_ARG;
-  if (!workspace || !aligned16(workspace) || workspace_bytes < deamoe_ffn_workspace(n_rows, ffn, 1)) return DEAMOE_ERR_INVALID_ARG;
+  if (!workspace || !aligned16(workspace) || workspace_bytes < deamoe_ffn_workspace(n_expert, n_rows, hidden, ffn, 1)) return DEAMOE_ERR_INVALID_ARG;
   const FfnShape S = {n_expert, n_rows, hidden, ffn, expert_off};
   const uint64_t v = (uint64_t)n_rows * ffn;
   char* ws = reinterpret_cast<char*>(workspace);

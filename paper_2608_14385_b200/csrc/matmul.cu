@@ -191,6 +191,10 @@ __device__ __forceinline__ void put8(__nv_bfloat16* p, const float (&v)[8], int 
       if (j < n) p[j] = __float2bfloat16_rn(v[j]);
   }
 }
+__device__ __forceinline__ void put8(float* p, const float (&v)[8]) {
+  reinterpret_cast<float4*>(p)[0] = make_float4(v[0], v[1], v[2], v[3]);
+  reinterpret_cast<float4*>(p)[1] = make_float4(v[4], v[5], v[6], v[7]);
+}
 __device__ __forceinline__ void get8(const __nv_bfloat16* p, float (&v)[8], int n) {
 #pragma unroll
   for (int j = 0; j < 8; ++j) v[j] = j < n ? __bfloat162float(p[j]) : 0.f;
@@ -213,7 +217,8 @@ struct Ahead {
 template <int EPI, bool AT, bool BT, bool FP8, bool RAGGED>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     k_matmul(const __grid_constant__ MatmulArgs A, const __grid_constant__ MatmulMaps maps) {
-  constexpr bool DUAL = EPI == ME_SWIGLU || EPI == ME_SWIGLU_GRAD;  // A's rows alternate gate and up
+  constexpr bool DUAL = EPI == ME_SWIGLU || EPI == ME_SWIGLU_GRAD || EPI == ME_PART_DUAL;  // A's rows alternate gate and up
+  constexpr bool SPLIT = EPI == ME_PART || EPI == ME_PART_DUAL;
   constexpr int M_STEP = DUAL ? MM_M / 2 : MM_M;                    // in rows of A as the caller counts them (DUAL: features)
   extern __shared__ __align__(1024) unsigned char smem[];
   float* staging = reinterpret_cast<float*>(smem + (size_t)MM_STAGES * MM_STAGE);
@@ -278,9 +283,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   cluster_sync();
   tc_after();
   const uint32_t tmem = *tmem_slot;
-  const int tiles = first_tile[A.groups];
+  const int tiles = first_tile[A.groups] * (SPLIT ? A.splits : 1);  // (SPLIT: parts of tiles)
   const int pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
   auto chunks_of = [&](const Tile& t) { return ((RAGGED ? t.rows : A.K) + A.chunk - 1) / A.chunk; };
+  auto tile_at = [&](int it) { return find_tile<RAGGED>(A, first_tile, first_row, SPLIT ? it / A.splits : it, M_STEP); };
 
   if (warp == MM_WARP_A || warp == MM_WARP_B) {
     // ============================================================ copies
@@ -291,14 +297,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     bool ok = true, free = true;  // (the first round of the ring is free)
     const bool rows_inner = is_a ? AT : BT;
     for (int it = pair; ok && it < tiles; it += pairs) {
-      const Tile t = find_tile<RAGGED>(A, first_tile, first_row, it, M_STEP);
-      const int half = t.n / 2, chunks = chunks_of(t);
+      const Tile t = tile_at(it);
+      const int half = t.n / 2, all = chunks_of(t);
+      // the part's chunks: dealt evenly, none without one (splits <= chunks)
+      const int part = SPLIT ? it % A.splits : 0;
+      const int c_begin = SPLIT ? (int)((int64_t)all * part / A.splits) : 0, chunks = SPLIT ? (int)((int64_t)all * (part + 1) / A.splits) : all;
       const int box = BT ? 3 : box_of(half);
       const uint32_t bytes = MM_OPERAND + (BT ? MM_OPERAND : 128 * (16 << box));
       const int at = is_a ? t.m0 + (int)rank * (M_STEP / 2) : t.n0 + (int)rank * half;  // first row of this CTA's part
       const int z = is_a && !RAGGED ? t.group : 0;
       const CUtensorMap* map = is_a ? &maps.a : &maps.b[BT ? 0 : box];
-      for (int c = 0; c < chunks; ++c, ++g) {
+      for (int c = c_begin; c < chunks; ++c, ++g) {
         const int s = g % MM_STAGES;
         if (!free && !bar_wait(empty(s), ((g / MM_STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
         const int k0 = c * A.chunk, k = RAGGED ? t.row0 + k0 : k0;
@@ -307,7 +316,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
         const uint32_t bar = last_rows ? tail(s) : first_full + 8 * s, dst = ring + s * MM_STAGE + (is_a ? 0 : MM_OPERAND);
         if (elected()) {
           if (is_a && (last_rows || rank == 0)) {
-            info[s] = t.n | (c == 0 ? STAGE_FIRST : 0) | (c + 1 == chunks ? STAGE_LAST : 0);
+            info[s] = t.n | (c == c_begin ? STAGE_FIRST : 0) | (c + 1 == chunks ? STAGE_LAST : 0);
             bar_expect(last_rows ? tail(s) : full(s), last_rows ? bytes : 2 * bytes);
           }
           if (DUAL && is_a) {
@@ -379,7 +388,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     if constexpr (RAGGED) {
       uint32_t g = 0, parity = 0;  // bit s: of the next use of tail(s) and cleared(s)
       for (int it = pair; it < tiles; it += pairs) {
-        const Tile t = find_tile<RAGGED>(A, first_tile, first_row, it, M_STEP);
+        const Tile t = tile_at(it);
         const int chunks = chunks_of(t), left = t.rows % A.chunk;
         g += chunks;
         if (left == 0) continue;
@@ -413,18 +422,19 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
     // A thread's part of a buffer: DUAL: one row, 8 features; else rows c and c + 8, 8 columns of the output.
     constexpr int ITEMS = DUAL ? 1 : 2, ITEM_ROWS = MM_COLS / ITEMS;
-    constexpr int OUT_BYTES = EPI == ME_STORE_F32 ? 4 : 2;
+    constexpr int OUT_BYTES = EPI == ME_STORE_F32 || SPLIT ? 4 : 2;
     const int q = DUAL ? me & 7 : me & 15, c = DUAL ? me >> 3 : me >> 4;
     const int64_t out_step = A.os * (ITEM_ROWS * OUT_BYTES);
     const float* const mine = st + c * MM_PITCH + q * (DUAL ? 16 : 8);
     for (int it = pair; ok && it < tiles; it += pairs) {
-      const Tile t = find_tile<RAGGED>(A, first_tile, first_row, it, M_STEP);
+      const Tile t = tile_at(it);
       const bool none = RAGGED && t.rows == 0;  // a group without rows: zeros
       const uint32_t buf = a & 1u;
       const int m = t.m0 + (int)rank * (M_STEP / 2) + q * 8, n = min(8, A.M - m);
       const int valid = n > 0 ? t.valid : 0;
       const int64_t row0 = t.n0 + team * MM_STEP + c;
-      char* out = reinterpret_cast<char*>(A.out) + ((RAGGED ? (int64_t)t.group * A.out_group : 0) + row0 * A.os + m) * OUT_BYTES;
+      char* out = reinterpret_cast<char*>(A.out) + ((RAGGED ? (int64_t)t.group * A.out_group : SPLIT ? (int64_t)(it % A.splits) * A.out_group : 0) +
+                                                           row0 * A.os + (EPI == ME_PART_DUAL ? 2 : 1) * m) * OUT_BYTES;
       // rows of dh, residual or dout of this thread's items, and x's scales
       const void* const from = EPI == ME_SWIGLU_GRAD ? (const void*)A.dh : EPI == ME_PRODUCT ? A.residual : EPI == ME_PRODUCT_GRAD ? A.dout : nullptr;
       const int64_t in_stride = EPI == ME_SWIGLU_GRAD ? (int64_t)A.f * 4 : A.rs * 2;
@@ -505,7 +515,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
             if constexpr (DUAL) {  // (f is a multiple of 8)
               float up[8];
               floats8(from_st + 8, up);
-              if constexpr (EPI == ME_SWIGLU) {
+              if constexpr (EPI == ME_PART_DUAL) {
+                put8(reinterpret_cast<float*>(out), v);
+                put8(reinterpret_cast<float*>(out) + 8, up);
+              } else if constexpr (EPI == ME_SWIGLU) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[j] *= sigmoid(v[j]) * up[j];
                 put8(to, v, 8, true);
@@ -524,10 +537,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
                 put8(to + A.f, du, 8, true);
                 put8(reinterpret_cast<__nv_bfloat16*>(A.h_out) + (row0 + c0 - team * MM_STEP + h * MM_COLS) * A.f + m, v, 8, true);
               }
-            } else if constexpr (EPI == ME_STORE_F32) {
-              float4* o = reinterpret_cast<float4*>(out);
-              o[0] = make_float4(v[0], v[1], v[2], v[3]);
-              o[1] = make_float4(v[4], v[5], v[6], v[7]);
+            } else if constexpr (EPI == ME_STORE_F32 || EPI == ME_PART) {
+              put8(reinterpret_cast<float*>(out), v);  // (rows of fp32 outputs have room for whole groups of 8)
             } else {
               if constexpr (EPI == ME_PRODUCT || EPI == ME_PRODUCT_GRAD) {
                 float add[8];
@@ -663,17 +674,33 @@ bool map_b(MatmulMaps* m, const void* p, int esize, int64_t cols, int64_t rows, 
 
 // The pairs take the tiles in rounds, and a round costs a tile's width and some 100 columns more (2048 x 4096 x 4096: rounds of
 // 144, 240 and 256 columns 21, 28 and 30 us), so a narrower tile pays where it saves a part of the last round: 3000 x
-// 2000 x 4096 in 18 tiles of 176 48 us, in 12 of 256 57; 1024 x 7168 x 7168 in 5 of 208 98 us, in 4 of 256 107.
-int matmul_tile_n(int64_t n, int64_t m_tiles) {
+// 2000 x 4096 in 18 tiles of 176 48 us, in 12 of 256 57; 1024 x 7168 x 7168 in 5 of 208 98 us, in 4 of 256 107.  Up to 256
+// rows A's bytes bound a product that can be split along k, so it reads them once (`whole`).
+int matmul_tile_n(int64_t n, int64_t m_tiles, bool whole) {
   int best = MM_N;
   int64_t least = INT64_MAX;
-  for (int64_t nt = (n + MM_N - 1) / MM_N, k = 0; k < 8; ++nt, ++k) {
+  for (int64_t nt = (n + MM_N - 1) / MM_N, k = 0; k < (whole && n <= MM_N ? 1 : 8); ++nt, ++k) {
     const int64_t width = ((n + nt - 1) / nt + 15) / 16 * 16;
     if (k > 0 && width < MM_N_LEAST) break;
     const int64_t cost = (nt * m_tiles + MM_PAIRS - 1) / MM_PAIRS * (width + 100);
     if (cost < least) {
       least = cost;
       best = (int)width;
+    }
+  }
+  return best;
+}
+// A decode step's product has fewer tiles than the device has pairs (7168 outputs: 28): its tiles are dealt along k, as evenly over
+// the pairs as some number of parts allows, where that saves a quarter of the chunks that a pair walks.  The parts' sums
+// (4 bytes a value and part, written and read once, mostly in the L2) stay below the matrix's bytes times four.
+int matmul_splits(int64_t tiles, int64_t chunks, int64_t rows) {
+  int best = 1;
+  int64_t least = (tiles + MM_PAIRS - 1) / MM_PAIRS * (chunks + 2) * 3 / 4;
+  for (int s = 2; s <= 16 && s * 4 <= chunks && s * rows <= chunks * 16; ++s) {
+    const int64_t cost = (tiles * s + MM_PAIRS - 1) / MM_PAIRS * ((chunks + s - 1) / s + 2);
+    if (cost < least) {
+      least = cost;
+      best = s;
     }
   }
   return best;
@@ -689,6 +716,9 @@ cudaError_t matmul_launch(MatmulForm form, const MatmulCall& c, cudaStream_t s, 
     case MF_WEIGHT_GRAD: return launch<ME_STORE, true, true, false, true>(c, s, chained);
     case MF_PRODUCT: return launch<ME_PRODUCT, false, false, false, false>(c, s, chained);
     case MF_PRODUCT_E4M3: return launch<ME_PRODUCT, false, false, true, false>(c, s, chained);
+    case MF_PART: return launch<ME_PART, false, false, false, false>(c, s, chained);
+    case MF_PART_E4M3: return launch<ME_PART, false, false, true, false>(c, s, chained);
+    case MF_PART_SWIGLU: return launch<ME_PART_DUAL, false, false, false, false>(c, s, chained);
     case MF_PRODUCT_GRAD: return launch<ME_PRODUCT_GRAD, false, false, false, false>(c, s, chained);
   }
   return cudaErrorInvalidValue;

@@ -34,7 +34,9 @@ enum MatmulEpilogue : int {
   ME_SWIGLU = 2,       // A's rows alternate 8 gate, 8 up: silu(gate) up
   ME_SWIGLU_GRAD = 3,  // the same accumulators and the gradient of their product -> gradients of gate and up, and the product
   ME_PRODUCT = 4,      // scales, bias, activation, residual
-  ME_PRODUCT_GRAD = 5  // dout times the activation's derivative, and its sums over a tile's rows
+  ME_PRODUCT_GRAD = 5, // dout times the activation's derivative, and its sums over a tile's rows
+  ME_PART = 6,         // fp32 sums of a part of k, [split][row][M rounded up to 8], for join.cu
+  ME_PART_DUAL = 7     // ... of alternating gate and up, [split][row][2 M]
 };
 
 struct MatmulArgs {
@@ -44,10 +46,11 @@ struct MatmulArgs {
   const int32_t* off;    // [groups + 1] rows of the groups, or null (one group of all rows)
   int tile_n;            // widest tile
   int chunk;             // values of k in 128 bytes
+  int splits;            // parts of k that a tile is dealt in (ME_PART, ME_PART_DUAL; else 1)
   // epilogue
   void* out;
   int64_t os;            // values between out's rows
-  int64_t out_group;     // values between groups of outputs (weight gradients)
+  int64_t out_group;     // values between groups of outputs (weight gradients), or between splits
   int wide;              // out's rows take 16-byte stores
   const float* dh;       // [N, f]                       (ME_SWIGLU_GRAD)
   void* h_out;           // [N, f] bf16
@@ -70,7 +73,8 @@ struct MatmulCall {
   MatmulMaps maps;
 };
 enum MatmulForm : int {
-  MF_SWIGLU, MF_STORE, MF_STORE_TRANSPOSED, MF_F32_TRANSPOSED, MF_SWIGLU_GRAD, MF_WEIGHT_GRAD, MF_PRODUCT, MF_PRODUCT_E4M3, MF_PRODUCT_GRAD
+  MF_SWIGLU, MF_STORE, MF_STORE_TRANSPOSED, MF_F32_TRANSPOSED, MF_SWIGLU_GRAD, MF_WEIGHT_GRAD, MF_PRODUCT, MF_PRODUCT_E4M3, MF_PRODUCT_GRAD,
+  MF_PART, MF_PART_E4M3, MF_PART_SWIGLU
 };
 cudaError_t matmul_launch(MatmulForm form, const MatmulCall& c, cudaStream_t s, bool chained);
 
@@ -80,8 +84,25 @@ bool map_rows(CUtensorMap* m, const void* p, int esize, int64_t cols, int64_t ro
 bool map_gate_up(CUtensorMap* m, const void* p, int64_t cols, int64_t f, int64_t groups);  // 128 rows: 8 gate, 8 up, ...
 bool map_b(MatmulMaps* m, const void* p, int esize, int64_t cols, int64_t rows, int64_t stride);
 
-// Tile width of `n` rows in one group for `m_tiles` tiles of A's rows: see matmul.cu
-int matmul_tile_n(int64_t n, int64_t m_tiles);
+// Tile width of `n` rows in one group for `m_tiles` tiles of A's rows; whole: the product may be split along k.  See matmul.cu
+int matmul_tile_n(int64_t n, int64_t m_tiles, bool whole);
+
+// Parts of k for a product of at most `tiles` tiles, `chunks` chunks of k and `rows` rows in all (1: not split): see matmul.cu
+int matmul_splits(int64_t tiles, int64_t chunks, int64_t rows);
+
+// Adds the splits' sums in their order and applies the epilogue: [splits][n_rows][M rounded up to 8] (dual: [2 M]) -> out.  (join.cu)
+struct JoinArgs {
+  const float* part;
+  int splits, n_rows, M, groups, dual;
+  const int32_t* off;    // rows outside [off[0], off[groups]) and rows of falling offsets are left alone; or null
+  __nv_bfloat16* out;
+  int64_t os;
+  const float *x_scale, *w_scale;
+  const void *bias, *residual;
+  int64_t rs;
+  int bias_f32, act, wide;
+};
+cudaError_t join_launch(const JoinArgs& a, cudaStream_t s);
 
 constexpr int MM_M = 256, MM_N = 256;
 constexpr int MM_N_LEAST = 64;   // matmul_tile_n gives no less for more rows

@@ -60,11 +60,16 @@ __global__ void __launch_bounds__(256) k_add_parts(const float* __restrict__ par
 
 static uint64_t ceil256(uint64_t v) { return (v + 255) / 256 * 256; }
 
-static MatmulCall product_call(int M, int K, int N, int chunk) {
+static MatmulCall product_call(int M, int K, int N, int chunk, bool whole) {
   MatmulCall c = {};
   c.args.M = M; c.args.K = K; c.args.N = N; c.args.groups = 1; c.args.chunk = chunk;
-  c.args.tile_n = matmul_tile_n(N, (M + MM_M - 1) / MM_M);
+  c.args.splits = 1;
+  c.args.tile_n = matmul_tile_n(N, (M + MM_M - 1) / MM_M, whole);
   return c;
+}
+
+static int product_splits(const MatmulArgs& a) {
+  return matmul_splits((int64_t)((a.M + MM_M - 1) / MM_M) * ((a.N + a.tile_n - 1) / a.tile_n), (a.K + a.chunk - 1) / a.chunk, a.N);
 }
 
 static deamoe_status_t check_product(int dtype, int T, int n_out, int n_in, int act, int bias_dtype, const void* bias) {
@@ -86,7 +91,7 @@ extern "C" {
 deamoe_status_t deamoe_product(void* cuda_stream, int32_t dtype, const void* x, int64_t x_stride, const float* x_scale, int32_t n_token,
                                const void* weight, const float* weight_scale, int32_t n_out, int32_t n_in, int32_t bias_dtype,
                                const void* bias, int32_t act, const void* residual, int64_t residual_stride, void* out,
-                               int64_t out_stride) {
+                               int64_t out_stride, void* workspace, uint64_t workspace_bytes) {
   deamoe_status_t st = check_product(dtype, n_token, n_out, n_in, act, bias_dtype, bias);
   if (st != DEAMOE_OK || n_token == 0) return st;
   const bool e4m3 = dtype == DEAMOE_E4M3;
@@ -95,6 +100,8 @@ deamoe_status_t deamoe_product(void* cuda_stream, int32_t dtype, const void* x, 
       !aligned_to(out, 2) || out_stride < n_out || out == x || out == weight || !aligned_to(residual, 2) ||
       (residual && residual_stride < n_out) || (residual == out && residual && residual_stride != out_stride))
     return DEAMOE_ERR_INVALID_ARG;
+  const uint64_t need = deamoe_product_workspace(dtype, n_token, n_out, n_in, act, 0);
+  if (need && (!workspace || !aligned16(workspace) || workspace_bytes < need)) return DEAMOE_ERR_INVALID_ARG;
   if (n_token <= THIN_ROWS) {
     ThinArgs a = {};
     a.x = x; a.xs = x_stride; a.w = weight; a.M = n_out; a.K = n_in; a.n_rows = n_token; a.groups = 1;
@@ -104,14 +111,25 @@ deamoe_status_t deamoe_product(void* cuda_stream, int32_t dtype, const void* x, 
     cudaGetLastError();
     return DEAMOE_ERR_CUDA;
   }
-  MatmulCall c = product_call(n_out, n_in, n_token, e4m3 ? 128 : 64);
+  MatmulCall c = product_call(n_out, n_in, n_token, e4m3 ? 128 : 64, true);
   c.args.out = out; c.args.os = out_stride; c.args.wide = wide_rows(out, out_stride, n_token, 2);
   c.args.bias = bias; c.args.bias_f32 = bias_dtype == DEAMOE_F32; c.args.act = act;
   c.args.residual = residual; c.args.rs = residual_stride; c.args.wide_in = wide_rows(residual, residual_stride, n_token, 2);
   c.args.x_scale = x_scale; c.args.w_scale = weight_scale;
   const int es = e4m3 ? 1 : 2;
   if (!map_rows(&c.maps.a, weight, es, n_in, n_out, n_in, 1, n_in, 128) || !map_b(&c.maps, x, es, n_in, n_token, x_stride)) return DEAMOE_ERR_CUDA;
-  if (matmul_launch(e4m3 ? MF_PRODUCT_E4M3 : MF_PRODUCT, c, reinterpret_cast<cudaStream_t>(cuda_stream), false) == cudaSuccess) return DEAMOE_OK;
+  cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
+  const int splits = product_splits(c.args);
+  if (splits > 1) {  // few tiles: dealt along k, the parts' sums joined by a kernel of their own
+    JoinArgs j = {};
+    j.part = reinterpret_cast<float*>(workspace); j.splits = splits; j.n_rows = n_token; j.M = n_out; j.groups = 1;
+    j.out = reinterpret_cast<__nv_bfloat16*>(out); j.os = out_stride; j.x_scale = x_scale; j.w_scale = weight_scale; j.bias = bias;
+    j.residual = residual; j.rs = residual_stride; j.bias_f32 = c.args.bias_f32; j.act = act; j.wide = c.args.wide;
+    c.args.splits = splits; c.args.out = workspace; c.args.os = (n_out + 7) / 8 * 8; c.args.out_group = c.args.os * n_token;
+    if (matmul_launch(e4m3 ? MF_PART_E4M3 : MF_PART, c, s, false) == cudaSuccess && join_launch(j, s) == cudaSuccess) return DEAMOE_OK;
+  } else if (matmul_launch(e4m3 ? MF_PRODUCT_E4M3 : MF_PRODUCT, c, s, false) == cudaSuccess) {
+    return DEAMOE_OK;
+  }
   cudaGetLastError();
   return DEAMOE_ERR_CUDA;
 }
@@ -121,8 +139,13 @@ static uint64_t bias_parts(int T, int n_out, int act) {
   return (uint64_t)(act == DEAMOE_SIGMA_NONE ? (T + BIAS_ROWS - 1) / BIAS_ROWS : MM_PARTS * ((T + MM_N_LEAST - 1) / MM_N_LEAST)) * n_out * 4;
 }
 
-uint64_t deamoe_product_workspace(int32_t n_token, int32_t n_out, int32_t act) {
-  if (n_token <= 0 || n_out <= 0) return 0;
+uint64_t deamoe_product_workspace(int32_t dtype, int32_t n_token, int32_t n_out, int32_t n_in, int32_t act, int32_t backward) {
+  if (n_token <= 0 || n_out <= 0 || n_in <= 0) return 0;
+  if (!backward) {
+    if (n_token <= THIN_ROWS) return 0;
+    const int splits = product_splits(product_call(n_out, n_in, n_token, dtype == DEAMOE_E4M3 ? 128 : 64, true).args);
+    return splits > 1 ? (uint64_t)splits * n_token * ((n_out + 7) / 8 * 8) * 4 : 0;
+  }
   return ceil256(bias_parts(n_token, n_out, act)) + (act == DEAMOE_SIGMA_NONE ? 0 : (uint64_t)n_token * n_out * 2);
 }
 
@@ -143,14 +166,15 @@ deamoe_status_t deamoe_product_backward(void* cuda_stream, int32_t dtype, const 
   if (!x || !aligned16(x) || x_stride < n_in || x_stride % 8 || !dout || !aligned16(dout) || dout_stride < n_out || dout_stride % 8 ||
       !dx || !aligned16(dx) || dx_stride < n_in || dx_stride % 8 || dx == x || dx == dout || dx == weight)
     return DEAMOE_ERR_INVALID_ARG;
-  const uint64_t need = deamoe_product_workspace(n_token, n_out, act);
+  const uint64_t need = deamoe_product_workspace(dtype, n_token, n_out, n_in, act, 1);
   if (!workspace || !aligned16(workspace) || workspace_bytes < need) return DEAMOE_ERR_INVALID_ARG;
   float* part = reinterpret_cast<float*>(workspace);
   const bool plain = act == DEAMOE_SIGMA_NONE;
   void* dz = reinterpret_cast<char*>(workspace) + ceil256(bias_parts(n_token, n_out, act));
   const void* g = plain ? dout : dz;  // gradient of z as an operand
   const int64_t gs = plain ? dout_stride : n_out;
-  MatmulCall a = product_call(n_out, n_in, n_token, 64), b = product_call(n_in, n_out, n_token, 64), c = product_call(n_in, n_token, n_out, 64);
+  MatmulCall a = product_call(n_out, n_in, n_token, 64, false), b = product_call(n_in, n_out, n_token, 64, false),
+             c = product_call(n_in, n_token, n_out, 64, false);
   a.args.out = dz; a.args.os = n_out; a.args.wide = 1; a.args.bias = bias; a.args.bias_f32 = bias_dtype == DEAMOE_F32; a.args.act = act;
   a.args.dout = dout; a.args.rs = dout_stride; a.args.wide_in = 1; a.args.part = dbias ? part : nullptr;
   b.args.out = dx; b.args.os = dx_stride; b.args.wide = 1;
