@@ -1,5 +1,5 @@
 // Few rows: every matrix is read once and the bytes bound it.  A block takes 16 rows of a matrix (DUAL: 8 of gate and the same 8
-// of up) and all of a group's rows of x, 8 or 16 at a time; its eight warps split the columns and add up in a fixed order.
+// of up) and all of a group's rows of x, 8 or 16 at a time; its four or eight warps split the columns and add up in a fixed order.
 //
 // The products run on mma.sync with the matrix rows as M and the rows of x as N (the tcgen05 kernel would leave most SMs
 // without a tile: 4096 rows are 16 tiles of 256).  Its operands come from registers, and since the order of k is free as long as
@@ -13,8 +13,8 @@ namespace deamoe {
 
 namespace {
 
-constexpr int TW = 8;      // warps of a block
 constexpr int T_AHEAD = 4; // steps of loads in flight
+constexpr int T_SMS = 148;
 
 template <bool FP8> __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   if constexpr (FP8)
@@ -30,8 +30,8 @@ __device__ __forceinline__ uint4 load_stream(const char* p) {
   return v;
 }
 
-// NT: groups of 8 rows of x in a pass
-template <bool FP8, bool DUAL, int NT> __global__ void __launch_bounds__(TW * 32) k_thin(const __grid_constant__ ThinArgs A) {
+// NT: groups of 8 rows of x in a pass; TW: warps of a block
+template <bool FP8, bool DUAL, int NT, int TW> __global__ void __launch_bounds__(TW * 32) k_thin(const __grid_constant__ ThinArgs A) {
   constexpr int ES = FP8 ? 1 : 2, VE = 16 / ES, STEP = 4 * VE, COLS = 8 * NT, ROWS = DUAL ? 8 : 16;
   __shared__ float part[TW][16][COLS + 1];
   __shared__ int found, counts[TW * 32 + 1], warp_sums[32];
@@ -113,8 +113,9 @@ template <bool FP8, bool DUAL, int NT> __global__ void __launch_bounds__(TW * 32
 #pragma unroll
       for (int j = 0; j < 4; ++j) part[warp][g + 8 * (j >> 1)][n * 8 + 2 * q + (j & 1)] = acc[n][j];
     __syncthreads();
-    const int m = tid % ROWS, c = tid / ROWS;
-    if (c < COLS && r0 + c < row1 && m0 + m < A.M) {
+    for (int o = tid; o < ROWS * COLS; o += TW * 32) {
+      const int m = o % ROWS, c = o / ROWS;
+      if (r0 + c >= row1 || m0 + m >= A.M) continue;
       const int64_t row = r0 + c;
       float v = 0.f;
 #pragma unroll
@@ -140,9 +141,14 @@ template <bool FP8, bool DUAL, int NT> __global__ void __launch_bounds__(TW * 32
 template <bool FP8, bool DUAL> cudaError_t launch(const ThinArgs& a, cudaStream_t s, bool chained) {
   const int rows = DUAL ? 8 : 16;
   const dim3 grid((a.M + rows - 1) / rows, a.off ? (a.groups < a.n_rows ? a.groups : a.n_rows) : 1);
-  auto kernel = a.n_rows <= 8 ? k_thin<FP8, DUAL, 1> : k_thin<FP8, DUAL, 2>;
-  if (chained) return launch_pdl(kernel, grid, dim3(TW * 32), 0, s, a);
-  kernel<<<grid, TW * 32, 0, s>>>(a);
+  // With three blocks an SM and more, blocks of four warps are all resident at once (7168 x 7168: 448 blocks, where 444 of eight
+  // warps fit; one row 20.8 us, 21.2 - 25.4 with eight; 16 rows over 13 of 32 experts 201 us, 239); with fewer, eight keep
+  // more loads in flight (4096 x 4096: 9.0 us, 11.7 with four).
+  const bool many = (int64_t)grid.x * grid.y >= 3 * T_SMS;
+  auto kernel = a.n_rows <= 8 ? (many ? k_thin<FP8, DUAL, 1, 4> : k_thin<FP8, DUAL, 1, 8>) : (many ? k_thin<FP8, DUAL, 2, 4> : k_thin<FP8, DUAL, 2, 8>);
+  const int threads = many ? 128 : 256;
+  if (chained) return launch_pdl(kernel, grid, dim3(threads), 0, s, a);
+  kernel<<<grid, threads, 0, s>>>(a);
   return cudaGetLastError();
 }
 
