@@ -18,7 +18,13 @@ constexpr int MM_STEP = 2 * MM_COLS;           // ... of an epilogue step; the t
 constexpr int MM_PITCH = 128 + 4;              // floats of a row of the transposing buffer
 constexpr int MM_STAGING = MM_TEAMS * 2 * MM_COLS * MM_PITCH * 4;
 constexpr int MM_CONTROL = 512;
-constexpr uint32_t STAGE_FIRST = 1u << 16, STAGE_LAST = 1u << 17, STAGE_END = 1u << 18;  // a tile's first / last chunk; no more tiles
+// What a stage holds: the first / last chunk of a tile in the ring; a chunk that has to be cleared behind its group's end (and how many
+// steps of 16 rows it has); no more tiles.
+constexpr uint32_t STAGE_FIRST = 1u << 16, STAGE_LAST = 1u << 17, STAGE_END = 1u << 18, STAGE_TAIL = 1u << 19;
+constexpr int STAGE_STEPS = 20;
+// A chunk to be cleared goes into the ring so many chunks before the tile's end, but is taken last: the MMA role need not wait for
+// the clearing (weight gradients of 16384 rows over 16 experts 861 -> XXX us).
+constexpr int MM_TAIL_LEAD = 2;
 constexpr int MM_TABLE = (DEAMOE_MAX_EXPERTS + 1) * 8 + 8;  // groups' first tile and first row
 constexpr size_t MM_SMEM = (size_t)MM_STAGES * MM_STAGE + MM_STAGING + MM_CONTROL + MM_TABLE;
 static_assert(MM_SMEM <= 227 * 1024, "shared memory budget");
@@ -134,7 +140,8 @@ struct Tile {
   int row0, rows;  // the group's rows (ragged contraction)
   int n_index;   // index of the tile along N in its group
 };
-// Tiles of group e: columns are dealt evenly, so that a group a little above a multiple of the widest tile has no sliver.
+// Tiles of a group: its columns are dealt evenly in units of 16, so that one a little above a multiple of the widest tile has no
+// sliver.
 __device__ __forceinline__ int tiles_along(int n, int widest) { return (n + widest - 1) / widest; }
 constexpr int MM_BAND = 8;  // tiles along N that are walked side by side: 74 pairs then share some 8 + 9 operand tiles in the L2
 
@@ -156,12 +163,12 @@ template <bool RAGGED> __device__ __forceinline__ Tile find_tile(const MatmulArg
   const int band = r / (MM_BAND * mt), rest = r - band * MM_BAND * mt;
   const int width = min(MM_BAND, nt - band * MM_BAND);
   const int mi = rest / width, ni = band * MM_BAND + rest - mi * width;
-  const int per = (cols + nt - 1) / nt;
-  o.n = (per + 15) & ~15;
+  const int units = (cols + 15) / 16, u0 = (int)((int64_t)ni * units / nt);
+  o.n = ((int)((int64_t)(ni + 1) * units / nt) - u0) * 16;
   o.m0 = mi * m_step;
   o.n_index = ni;
-  o.valid = min(o.n, cols - ni * o.n);
-  o.n0 = ni * o.n + (RAGGED ? 0 : o.row0);
+  o.valid = min(o.n, cols - u0 * 16);
+  o.n0 = u0 * 16 + (RAGGED ? 0 : o.row0);
   return o;
 }
 
@@ -246,7 +253,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
       bar_init(full(s), 1);
       bar_init(empty(s), 1);
       bar_init(tail(s), 1);
-      bar_init(cleared(s), 1);
+      bar_init(cleared(s), 2);
     }
     for (int b = 0; b < 2; ++b) {
       bar_init(acc_full(b), 1);
@@ -307,17 +314,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
       const int at = is_a ? t.m0 + (int)rank * (M_STEP / 2) : t.n0 + (int)rank * half;  // first row of this CTA's part
       const int z = is_a && !RAGGED ? t.group : 0;
       const CUtensorMap* map = is_a ? &maps.a : &maps.b[BT ? 0 : box];
-      for (int c = c_begin; c < chunks; ++c, ++g) {
+      const int left = RAGGED ? t.rows % A.chunk : 0;
+      const int tail_at = RAGGED && left ? max(0, chunks - 1 - MM_TAIL_LEAD) : -1;
+      for (int c = c_begin; c < chunks; ++c, ++g) {  // (c: the place in the ring's order)
         const int s = g % MM_STAGES;
         if (!free && !bar_wait(empty(s), ((g / MM_STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
-        const int k0 = c * A.chunk, k = RAGGED ? t.row0 + k0 : k0;
-        // rows of the next group come along: this CTA's clearing warp sees them first
-        const bool last_rows = RAGGED && k0 + A.chunk > t.rows;
+        // rows of the next group come along with the last chunk: this CTA's clearing warp sees them first
+        const bool last_rows = RAGGED && c == tail_at;
+        const int k0 = (last_rows ? chunks - 1 : RAGGED && tail_at >= 0 && c > tail_at ? c - 1 : c) * A.chunk;
+        const int k = RAGGED ? t.row0 + k0 : k0;
         const uint32_t bar = last_rows ? tail(s) : first_full + 8 * s, dst = ring + s * MM_STAGE + (is_a ? 0 : MM_OPERAND);
         if (elected()) {
-          if (is_a && (last_rows || rank == 0)) {
-            info[s] = t.n | (c == c_begin ? STAGE_FIRST : 0) | (c + 1 == chunks ? STAGE_LAST : 0);
-            bar_expect(last_rows ? tail(s) : full(s), last_rows ? bytes : 2 * bytes);
+          if (is_a && last_rows) bar_expect(tail(s), bytes);
+          if (is_a && rank == 0) {
+            info[s] = t.n | (c == c_begin ? STAGE_FIRST : 0) | (c + 1 == chunks ? STAGE_LAST : 0) |
+                      (last_rows ? STAGE_TAIL | (left + 15) / 16 << STAGE_STEPS : 0);
+            bar_expect(full(s), last_rows ? 0 : 2 * bytes);
           }
           if (DUAL && is_a) {
             load_5d(dst, map, k0, 0, 0, at / 8, z, bar);
@@ -356,59 +368,74 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
       const uint64_t db = operand_desc(ring + MM_OPERAND, BT ? MM_OPERAND / 2 : 16, 1024);
       // fp32 sums of bf16 (or e4m3: type 0) values, 256 rows, both CTAs
       const uint32_t kind = 1u << 4 | (FP8 ? 0u : (1u << 7 | 1u << 10)) | (AT ? 1u << 15 : 0u) | (BT ? 1u << 16 : 0u) | (MM_M >> 4) << 24;
-      uint32_t d = tmem, idesc = 0;
+      uint32_t d = tmem, idesc = 0, add = 0, parity = 0;
+      int waiting = -1, waiting_steps = 0;  // stage of a chunk to be cleared
+      auto issue = [&](int s, int steps) {
+        tc_after();
+        if (elected()) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k)  // 32 bytes of k; rows inner: 16 k's, two blocks of 1024 bytes
+            if (!RAGGED || k < steps)
+              mma_pair<FP8>(d, da + ((s * MM_STAGE + k * (AT ? 2048 : 32)) >> 4), db + ((s * MM_STAGE + k * (BT ? 2048 : 32)) >> 4),
+                            idesc, k == 0 ? add : 1u);
+          commit_pair(empty(s));
+        }
+        __syncwarp();
+        add = 1;
+      };
       bool ready = bar_try(full(0), 0);
       for (;; ++g) {
         const int s = g % MM_STAGES;
         if (!ready && !bar_wait(full(s), (g / MM_STAGES) & 1u, abort_flag)) break;
         const uint32_t what = *(volatile uint32_t*)(info + s);
         if (what & STAGE_END) break;
-        const bool first = what & STAGE_FIRST;
-        if (first) {
+        if (what & STAGE_FIRST) {
           idesc = kind | (what & 0x1ffu) >> 3 << 17;
           d = tmem + (a & 1u) * MM_N;
+          add = 0;
           if (!bar_wait(acc_empty(a & 1u), ((a >> 1) & 1u) ^ 1u, abort_flag)) break;
         }
         ready = bar_try(full((g + 1) % MM_STAGES), ((g + 1) / MM_STAGES) & 1u);
-        tc_after();
-        if (elected()) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k)  // 32 bytes of k; rows inner: 16 k's, two blocks of 1024 bytes
-            mma_pair<FP8>(d, da + ((s * MM_STAGE + k * (AT ? 2048 : 32)) >> 4), db + ((s * MM_STAGE + k * (BT ? 2048 : 32)) >> 4),
-                          idesc, (first && k == 0) ? 0u : 1u);
-          commit_pair(empty(s));
-          if (what & STAGE_LAST) commit_pair(acc_full(a & 1u));
+        if (RAGGED && (what & STAGE_TAIL)) {
+          waiting = s;
+          waiting_steps = what >> STAGE_STEPS;
+        } else {
+          issue(s, 4);
         }
-        __syncwarp();
-        if (what & STAGE_LAST) ++a;
+        if (what & STAGE_LAST) {
+          if (RAGGED && waiting >= 0) {
+            if (!bar_wait(cleared(waiting), (parity >> waiting) & 1u, abort_flag)) break;
+            parity ^= 1u << waiting;
+            issue(waiting, waiting_steps);
+            waiting = -1;
+          }
+          if (elected()) commit_pair(acc_full(a & 1u));
+          __syncwarp();
+          ++a;
+        }
       }
     }
   } else if (warp == MM_WARP_CLEAR) {
     // ============================================================ rows behind a group's end
     if constexpr (RAGGED) {
-      uint32_t g = 0, parity = 0;  // bit s: of the next use of tail(s) and cleared(s)
+      uint32_t g = 0, parity = 0;  // bit s: of the next use of tail(s)
       for (int it = pair; it < tiles; it += pairs) {
         const Tile t = tile_at(it);
         const int chunks = chunks_of(t), left = t.rows % A.chunk;
+        const int s = (g + max(0, chunks - 1 - MM_TAIL_LEAD)) % MM_STAGES;
         g += chunks;
         if (left == 0) continue;
-        const int s = (g - 1) % MM_STAGES;
         int ok = lane == 0 ? bar_wait(tail(s), (parity >> s) & 1u, abort_flag) : 0;
         ok = __shfl_sync(0xffffffffu, ok, 0);
         if (!ok) break;
+        parity ^= 1u << s;
         unsigned char* st = smem + (size_t)s * MM_STAGE;
-        const int from = left * 8, per = 64 * 8;  // 16-byte pieces of a box: 64 rows of 128 bytes
+        const int to = (left + 15) / 16 * 128;  // 16-byte pieces of a box's rows of 128 bytes, up to a step of 16 rows
         for (int b = 0; b < 4; ++b)
-          for (int i = from + lane; i < per; i += 32) *reinterpret_cast<uint4*>(st + b * (MM_OPERAND / 2) + i * 16) = make_uint4(0, 0, 0, 0);
+          for (int i = left * 8 + lane; i < to; i += 32) *reinterpret_cast<uint4*>(st + b * (MM_OPERAND / 2) + i * 16) = make_uint4(0, 0, 0, 0);
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         __syncwarp();
-        // the second CTA tells the first, whose stage is full when both are cleared (a remote arrival of every chunk's copies
-        // instead, with its release, made this kernel half as fast)
-        if (lane == 0) {
-          if (rank != 0) bar_arrive_cluster(in_first(cleared(s)));
-          else if (bar_wait(cleared(s), (parity >> s) & 1u, abort_flag)) bar_arrive_cluster(full(s));
-        }
-        parity ^= 1u << s;
+        if (lane == 0) bar_arrive_cluster(in_first(cleared(s)));  // both CTAs' parts
       }
     }
   } else {
