@@ -476,7 +476,7 @@ deamoe_status_t deamoe_norm_residual_quant(void *cuda_stream, int32_t dtype, con
  *   w_gate_up   [n_expert, 2 ffn, hidden] bf16: rows [0, ffn) of a matrix are the gate, the others the up projection
  *   w_down      [n_expert, hidden, ffn] bf16
  *   expert_off  [n_expert + 1] as deamoe_sort_pairs gives it; NULL for one expert (every row is its).  Offsets outside
- *               [0, n_rows] count as its ends; if they decrease anywhere, no row is written and the gradients are undefined.
+ *               [0, n_rows] count as its ends; if they decrease anywhere, nothing is written.
  *
  * Rows behind expert_off[n_expert] are left as they were (out, dx).  h is rounded to bf16 once.
  * deamoe_ffn_backward takes the forward call's inputs and dout:  dx, dw_gate_up and dw_down (shapes and type of the

@@ -156,6 +156,7 @@ deamoe_status_t deamoe_ffn_backward(void* cuda_stream, const void* x, int64_t x_
   d.args.N = 2 * ffn; d.args.out = dw_gate_up; d.args.os = hidden; d.args.out_group = 2 * wd_one;
   MatmulCall e = ffn_call(S, ffn, n_rows);  // dWd = dy^T h
   e.args.N = hidden; e.args.out = dw_down; e.args.os = ffn; e.args.out_group = wd_one;
+  d.args.late = e.args.late = 1;  // they need b's results as c does, and c waits for those
   if (!map_rows(&a.maps.a, w_down, 2, ffn, hidden, ffn, n_expert, wd_one, 64) || !map_b(&a.maps, dout, 2, hidden, n_rows, dout_stride) ||
       !map_gate_up(&b.maps.a, w_gate_up, hidden, ffn, n_expert) || !map_b(&b.maps, x, 2, hidden, n_rows, x_stride) ||
       !map_rows(&c.maps.a, w_gate_up, 2, hidden, 2 * (int64_t)ffn, hidden, n_expert, 2 * wd_one, 64) ||

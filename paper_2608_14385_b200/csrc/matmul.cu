@@ -23,7 +23,7 @@ constexpr int MM_CONTROL = 512;
 constexpr uint32_t STAGE_FIRST = 1u << 16, STAGE_LAST = 1u << 17, STAGE_END = 1u << 18, STAGE_TAIL = 1u << 19;
 constexpr int STAGE_STEPS = 20;
 // A chunk to be cleared goes into the ring so many chunks before the tile's end, but is taken last: the MMA role need not wait for
-// the clearing (weight gradients of 16384 rows over 16 experts 861 -> XXX us).
+// the clearing (weight gradients of 16384 rows over 16 experts 861 -> 721 us).
 constexpr int MM_TAIL_LEAD = 2;
 constexpr int MM_TABLE = (DEAMOE_MAX_EXPERTS + 1) * 8 + 8;  // groups' first tile and first row
 constexpr size_t MM_SMEM = (size_t)MM_STAGES * MM_STAGE + MM_STAGING + MM_CONTROL + MM_TABLE;
@@ -266,7 +266,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
-  pdl_wait();
+  // A kernel behind another one of its call waits for it here, but for two kinds.  The gradient of gate and up needs the one
+  // before it in its epilogue alone.  A.late: it needs only what was done before that one's own wait, which all its CTAs have
+  // passed by now, and waits at its end, so that the stream's order holds for what comes after.
+  if (EPI != ME_SWIGLU_GRAD && !A.late) pdl_wait();
   pdl_trigger();
   // groups' rows (offsets outside the range count as its ends) and their tiles; offsets that decrease: no tile at all
   const int mt = (A.M + M_STEP - 1) / M_STEP;
@@ -442,6 +445,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     // ============================================================ epilogue
     // One warp a scheduler runs such code at some seven cycles an instruction, so two teams share a tile's columns,
     // and rows are walked by pointer.
+    if (EPI == ME_SWIGLU_GRAD) pdl_wait();
     uint32_t a = 0;
     bool ok = true;
     const int team = warp >> 2, me = tid & 127;
@@ -619,6 +623,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   }
 
   // common end, also after a wait that has expired
+  if (A.late) pdl_wait();
   tc_before();
   __syncthreads();
   if (*abort_flag) {

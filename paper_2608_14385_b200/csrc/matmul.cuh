@@ -47,6 +47,7 @@ struct MatmulArgs {
   int tile_n;            // widest tile
   int chunk;             // values of k in 128 bytes
   int splits;            // parts of k that a tile is dealt in (ME_PART, ME_PART_DUAL; else 1)
+  int late;              // behind another kernel of the call whose results it does not need (see matmul.cu)
   // epilogue
   void* out;
   int64_t os;            // values between out's rows

@@ -393,37 +393,36 @@ template <typename T, int VE, int NV, int MAXT> __global__ void __launch_bounds_
 // With m = max |s w| the code is e4m3(s w * 448 / m) and the scale m / rms(s) / 448: the sum of squares and the maximum
 // come from one reduction, and the codes do not wait for the root.  Rows whose m is below 2^-110 (a row of zeros among
 // them) take 2^-110 for it.  The row stays in registers; HBM bounds it: 5 bytes a value without a sum, 7 with one (bf16).
+constexpr int CODES_THREADS = 512;  // of an SM, in the persistent form: 128 registers each
 constexpr float E4M3_MAX = 448.f, QUANT_LEAST = 0x1p-110f;
 
-// the sum of v[0] and the maximum of v[1] over a block, to every thread; buf: 64 floats, as for block_sums
-static __device__ __forceinline__ void block_sum_max(float (&v)[2], float* buf) {
+// the maximum of v[0] and the sums of the others over a block, to every thread; buf: 32 N floats, as for block_sums
+template <int N> static __device__ __forceinline__ void block_max_sums(float (&v)[N], float* buf) {
+  auto join = [&](int o) {
+    v[0] = fmaxf(v[0], __shfl_xor_sync(0xffffffffu, v[0], o));
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
-    v[1] = fmaxf(v[1], __shfl_xor_sync(0xffffffffu, v[1], o));
-  }
+    for (int i = 1; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+  };
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) join(o);
   const int warps = blockDim.x >> 5;
   if (warps == 1) return;
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-  if (lane == 0) {
-    buf[w] = v[0];
-    buf[32 + w] = v[1];
-  }
-  __syncthreads();
-  v[0] = lane < warps ? buf[lane] : 0.f;
-  v[1] = lane < warps ? buf[32 + lane] : 0.f;
+  if (lane == 0)
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
-    v[1] = fmaxf(v[1], __shfl_xor_sync(0xffffffffu, v[1], o));
-  }
+    for (int i = 0; i < N; ++i) buf[i * 32 + w] = v[i];
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < N; ++i) v[i] = lane < warps ? buf[i * 32 + lane] : 0.f;
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) join(o);
 }
-// scale of a row into memory; returns what its values are multiplied by
+// scale of a row into memory; returns what its values are multiplied by (to 2 units; 2^-8 keeps the reciprocal a normal number
+// up to the largest m)
 static __device__ __forceinline__ float row_scale(const NormArgs& A, int64_t t, float ss, float m) {
   m = fmaxf(m, QUANT_LEAST);
-  const float r = A.next_norm ? inv_rms(ss, A.h, A.next_eps) : 1.f;
-  if (threadIdx.x == 0) A.scale[t] = r * m / E4M3_MAX;
-  return E4M3_MAX / m;
+  if (threadIdx.x == 0) A.scale[t] = (A.next_norm ? inv_rms(ss, A.h, A.next_eps) : 1.f) * m * (1.f / E4M3_MAX);
+  return (E4M3_MAX * 0x1p-8f) * __fdividef(1.f, m * 0x1p-8f);
 }
 template <int VE> static __device__ __forceinline__ void store_codes(uint8_t* p, const float (&f)[VE]) {
   if constexpr (VE == 1) {
@@ -460,11 +459,11 @@ template <typename T> __global__ void __launch_bounds__(ANY_THREADS) k_codes_any
   float v[2] = {0.f, 0.f};
   for (int i = threadIdx.x; i < A.h; i += ANY_THREADS) {
     const float s = sum(i);
-    v[0] = fmaf(s, s, v[0]);
-    v[1] = fmaxf(v[1], fabsf(s * load_gain(A.wn, A.wdt, i)));
+    v[0] = fmaxf(v[0], fabsf(s * load_gain(A.wn, A.wdt, i)));
+    v[1] = fmaf(s, s, v[1]);
   }
-  block_sum_max(v, buf[1]);
-  const float f = row_scale(A, t, v[0], v[1]);
+  block_max_sums<2>(v, buf[1]);
+  const float f = row_scale(A, t, v[1], v[0]);
   for (int i = threadIdx.x; i < A.h; i += ANY_THREADS) {
     const float s = sum(i);
     if (A.y.p) put<T>(A.out, A.out_s, t, i, s);
@@ -517,13 +516,13 @@ template <typename T, int VE, int NV, int MAXT> __global__ void __launch_bounds_
     load_gains<VE>(A.wn, A.wdt, (int64_t)c * VE, w);
 #pragma unroll
     for (int j = 0; j < VE; ++j) {
-      v[0] = fmaf(s[n][j], s[n][j], v[0]);
+      v[1] = fmaf(s[n][j], s[n][j], v[1]);
       s[n][j] *= w[j];
-      v[1] = fmaxf(v[1], fabsf(s[n][j]));
+      v[0] = fmaxf(v[0], fabsf(s[n][j]));
     }
   }
-  block_sum_max(v, buf[1]);
-  const float scale = row_scale(A, t, v[0], v[1]);
+  block_max_sums<2>(v, buf[1]);
+  const float scale = row_scale(A, t, v[1], v[0]);
 #pragma unroll
   for (int n = 0; n < NV; ++n) {
     const int c = threadIdx.x + n * blockDim.x;
@@ -655,6 +654,121 @@ static __device__ __forceinline__ void store_lanes(void* p, int64_t stride, int6
   float f[VE];
   Lanes<VE>::to(v, f);
   store_row<T, VE>(p, stride, t, c, f);
+}
+
+// The 8-bit norms of many rows.  Done as k_codes_rows does them they are bound by instruction issue (41 instructions a value, 85 us
+// for 8192 x 7168 bf16; so 74).  So persistent blocks, whose threads hold their columns' gains (with the branch's factor and a gate per
+// channel in them) as pairs of fp32 in registers and work on pairs; whose next rows are on their way meanwhile; and one reduction a row,
+// which brings the branch's sum of squares of the row to come with it.
+//   TWO: the sum of x and a branch; FULL: with a gate per value
+template <typename T, int VE, int NV, int MAXT, bool TWO, bool FULL>
+__global__ void __launch_bounds__(MAXT, NV == 2 ? 2 : 1) k_codes_feed(NormArgs A, int packs, int stages) {
+  extern __shared__ uint4 ring[];
+  __shared__ float buf[3][96];  // one reduction a row, its buffers in turn
+  using L = Lanes<VE>;
+  using P = typename L::P;
+  constexpr int N = L::N, NIN = FULL ? 3 : TWO ? 2 : 1;
+  const Rows in[3] = {A.x, TWO ? A.y : Rows{nullptr, 0}, FULL ? A.gate : Rows{nullptr, 0}};
+  const RowFeed<T, VE, NV, 3> F(in, A.T, packs, stages, NIN, ring);
+  P wy[NV][N], wn[NV][N];
+#pragma unroll
+  for (int n = 0; n < NV; ++n) {
+    const int c = threadIdx.x + n * blockDim.x;
+    float f[VE], g[VE];
+#pragma unroll
+    for (int j = 0; j < VE; ++j) f[j] = g[j] = 0.f;
+    if (c < packs) load_gains<VE>(A.wn, A.wdt, (int64_t)c * VE, f);
+    L::from(f, wn[n]);
+    if constexpr (TWO) {
+      if (c < packs) {
+        load_gains<VE>(A.w, A.wdt, (int64_t)c * VE, f);
+        if (A.gate_kind == DEAMOE_GATE_CHANNEL) load_gate<T, VE>(A, 0, c, g);
+      }
+#pragma unroll
+      for (int j = 0; j < VE; ++j) f[j] *= A.gate_kind == DEAMOE_GATE_CHANNEL ? A.b * g[j] : A.b;
+      L::from(f, wy[n]);
+    }
+  }
+  uint32_t at = 0, to = 0;
+  int64_t ahead = blockIdx.x;
+  for (int i = 0; i < stages; ++i, ahead += gridDim.x) {
+    F.request(ahead, to);
+    to = F.next(to);
+  }
+  auto squares = [&](int64_t t, uint32_t slot) {  // of this thread's columns of a row's branch
+    P sq = splat<P>(0.f);
+#pragma unroll
+    for (int n = 0; n < NV; ++n)
+      if ((int)(threadIdx.x + n * blockDim.x) < packs) {
+        P y[N];
+        F.get(1, t, slot, n, y);
+#pragma unroll
+        for (int j = 0; j < N; ++j) sq = fma_(y[j], y[j], sq);
+      }
+    return total(sq);
+  };
+  const bool post = TWO && A.post_norm;
+  const float per_value = 1.f / (float)A.h;
+  float ry = 1.f;  // of the row to come: its sum goes with the reduction of the row before it
+  if (post) {
+    F.wait_for(1);
+    float ss[1] = {squares(blockIdx.x, 0)};
+    block_sums<1>(ss, buf[0]);
+    ry = inv_rms(ss[0], A.h, A.eps);
+  }
+  int flip = 1;
+  for (int64_t t = blockIdx.x; t < A.T; t += gridDim.x, ahead += gridDim.x) {
+    F.wait_for(post ? 2 : 1);
+    P s[NV][N];
+    float cy = ry;
+    if (TWO && A.gate_kind == DEAMOE_GATE_TOKEN) cy *= to_f<T>(reinterpret_cast<const T*>(A.gate.p)[t]);
+    const P cy2 = splat<P>(cy), a2 = splat<P>(A.a);
+    P sq = splat<P>(0.f);
+    float m = 0.f;
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const int c = threadIdx.x + n * blockDim.x;
+      if (c >= packs) continue;
+      F.get(0, t, at, n, s[n]);
+      if constexpr (TWO) {
+        P y[N];
+        F.get(1, t, at, n, y);
+        if constexpr (FULL) {
+          P g[N];
+          F.get(2, t, at, n, g);
+#pragma unroll
+          for (int j = 0; j < N; ++j) y[j] = mul_(y[j], g[j]);
+        }
+#pragma unroll
+        for (int j = 0; j < N; ++j) s[n][j] = fma_(a2, s[n][j], mul_(cy2, mul_(y[j], wy[n][j])));
+        store_lanes<T, VE>(A.out, A.out_s, t, c, s[n]);
+      }
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        sq = fma_(s[n][j], s[n][j], sq);
+        s[n][j] = mul_(s[n][j], wn[n][j]);
+        m = fmaxf(fmaxf(m, fabsf(low(s[n][j]))), fabsf(high(s[n][j])));
+      }
+    }
+    float v[3] = {m, total(sq), 0.f};
+    if (post && t + gridDim.x < A.T) v[2] = squares(t + gridDim.x, F.next(at));
+    F.request(ahead, at);  // the row has been read: its slot takes the one `stages` further
+    at = F.next(at);
+    block_max_sums<3>(v, buf[flip]);
+    flip = 3 - flip;
+    if (post) ry = rsqrtf(fmaf(v[2], per_value, A.eps));
+    const P f2 = splat<P>(row_scale(A, t, v[1], v[0]));
+#pragma unroll
+    for (int n = 0; n < NV; ++n) {
+      const int c = threadIdx.x + n * blockDim.x;
+      if (c >= packs) continue;
+      float f[VE];
+#pragma unroll
+      for (int j = 0; j < N; ++j) s[n][j] = mul_(s[n][j], f2);
+      L::to(s[n], f);
+      store_codes<VE>(A.codes + t * A.codes_s + (int64_t)c * VE, f);
+    }
+  }
 }
 
 template <typename T, int VE, int NV, int MAXT>
@@ -1040,7 +1154,7 @@ template <typename T> static deamoe_status_t norm_t(const NormArgs& A, cudaStrea
 template <typename T> static deamoe_status_t residual_t(const NormArgs& A, cudaStream_t s) {
   DEAMOE_ROW_FORMS(k_residual_rows, k_residual_any);
 }
-template <typename T> static deamoe_status_t codes_t(const NormArgs& A, cudaStream_t s) {
+template <typename T> static deamoe_status_t codes_rows_t(const NormArgs& A, cudaStream_t s) {
   DEAMOE_ROW_FORMS(k_codes_rows, k_codes_any);
 }
 #undef DEAMOE_ROW_FORMS
@@ -1074,6 +1188,37 @@ static deamoe_status_t run_grad(K* kernel, std::atomic<uint64_t>& done, const No
   kernel<<<ctas, threads, stage_bytes * stages, s>>>(A, packs, stages, rest...);
   return ran();
 }
+
+template <typename T> static deamoe_status_t codes_t(const NormArgs& A, cudaStream_t s) {
+  constexpr int VE = 16 / sizeof(T), NV = 4;
+  const int packs = A.h / VE;
+  // (a sum of narrow rows leaves the persistent blocks too few columns beside a row's fixed work: 16384 x 1024 25.8 us, 23.4 with a block a
+  // row; without a sum 9.0, 13.0)
+  if (few_rows(A.T) || !wide_call<T>(A) || packs < 128 || packs > 2048 || (A.y.p && A.gate_kind != DEAMOE_GATE_FULL && packs <= 256))
+    return codes_rows_t<T>(A, s);
+  const int nin = A.gate_kind == DEAMOE_GATE_FULL ? 3 : A.y.p ? 2 : 1;
+  auto run = [&](auto kernel, std::atomic<uint64_t>& done, int nv, int sm_threads) {
+    const int threads = (int)warps_of(packs, nv);
+    const size_t stage = (size_t)nin * nv * threads * 16;
+    int blocks = sm_threads / threads;
+    while (blocks > 1 && grad_stages(blocks, stage) < 2) --blocks;  // a row and the one to come
+    const int stages = grad_stages(blocks, stage);
+    const int64_t most = (int64_t)NORM_SMS * blocks;
+    if (!whole_smem(kernel, done)) return DEAMOE_ERR_CUDA;
+    kernel<<<(unsigned)(A.T < most ? A.T : most), threads, stage * stages, s>>>(A, packs, stages);
+    return ran();
+  };
+  static std::atomic<uint64_t> done[5];
+  // Sums of rows of 4097 to 7168 bf16 values: twice the threads with half the columns (two blocks of them fit an SM, and one reduction more a
+  // warp is little beside a long row: 8192 x 7168 75 us, 80 with four packs a thread).
+  if (nin > 1 && packs > 512 && packs <= 896)
+    return nin == 3 ? run(k_codes_feed<T, VE, 2, 448, true, true>, done[0], 2, 896) : run(k_codes_feed<T, VE, 2, 448, true, false>, done[1], 2, 896);
+  return nin == 3 ? run(k_codes_feed<T, VE, NV, CODES_THREADS, true, true>, done[2], NV, CODES_THREADS)
+       : nin == 2 ? run(k_codes_feed<T, VE, NV, CODES_THREADS, true, false>, done[3], NV, CODES_THREADS)
+                  : run(k_codes_feed<T, VE, NV, CODES_THREADS, false, false>, done[4], NV, CODES_THREADS);
+}
+// (rows of up to 2048 packs with a gate of their own take 96 KB a stage: two fit one block's ring)
+static_assert(2 * 3 * 4 * 512 * 16 <= RING_BYTES, "two rows in a ring");
 
 template <typename T> static deamoe_status_t norm_grad_t(const NormArgs& A, cudaStream_t s) {
   constexpr int VE = 16 / sizeof(T), NV = GRAD_COLUMNS / VE;

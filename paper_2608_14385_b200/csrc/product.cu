@@ -39,12 +39,15 @@ __global__ void __launch_bounds__(256) k_bias_sums(const __nv_bfloat16* __restri
   float v = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) v += buf[i][threadIdx.x];
+  pdl_trigger();
   const int col = blockIdx.x * 256 + threadIdx.x;
   if (col < n) part[(int64_t)blockIdx.y * n + col] = v;
 }
 // Partial sums added in their order: 32 columns a block, 8 threads a column.
-__global__ void __launch_bounds__(256) k_add_parts(const float* __restrict__ part, int parts, int n, float* __restrict__ out) {
+__global__ void __launch_bounds__(256) k_add_parts(const float* part, int parts, int n, float* __restrict__ out) {
   __shared__ float buf[8][32];
+  pdl_wait();
+  pdl_trigger();
   const int q = threadIdx.x & 31, r = threadIdx.x >> 5, c = blockIdx.x * 32 + q;
   float s = 0.f;
   if (c < n)
@@ -184,6 +187,7 @@ deamoe_status_t deamoe_product_backward(void* cuda_stream, int32_t dtype, const 
       !map_rows(&c.maps.a, x, 2, n_in, n_token, x_stride, 1, x_stride, 64) ||
       !map_rows(&c.maps.b[0], g, 2, n_out, n_token, gs, 1, gs, 64))
     return DEAMOE_ERR_CUDA;
+  c.args.late = 1;  // it needs dz as b does, and b waits for it
   bool ok = true;
   int parts = 0;
   if (!plain) {
@@ -194,11 +198,9 @@ deamoe_status_t deamoe_product_backward(void* cuda_stream, int32_t dtype, const 
     k_bias_sums<<<dim3((n_out + 255) / 256, parts), 256, 0, s>>>(reinterpret_cast<const __nv_bfloat16*>(dout), dout_stride, n_token, n_out, part);
     ok = cudaGetLastError() == cudaSuccess;
   }
-  if (ok && dbias) {
-    k_add_parts<<<(n_out + 31) / 32, 256, 0, s>>>(part, parts, n_out, dbias);
-    ok = cudaGetLastError() == cudaSuccess;
-  }
-  ok = ok && matmul_launch(MF_STORE_TRANSPOSED, b, s, false) == cudaSuccess && matmul_launch(MF_WEIGHT_GRAD, c, s, false) == cudaSuccess;
+  if (ok && dbias)
+    ok = launch_pdl(k_add_parts, dim3((n_out + 31) / 32), dim3(256), 0, s, (const float*)part, parts, (int)n_out, dbias) == cudaSuccess;
+  ok = ok && matmul_launch(MF_STORE_TRANSPOSED, b, s, !plain || dbias) == cudaSuccess && matmul_launch(MF_WEIGHT_GRAD, c, s, true) == cudaSuccess;
   if (ok) return DEAMOE_OK;
   cudaGetLastError();
   return DEAMOE_ERR_CUDA;
