@@ -529,21 +529,34 @@ def quant_product(codes, scales, x, group, zeros=None, expert_off=None, row_pair
     return out
 
 
+def _result(t, like, dtype, rows, cols, where, name, dev):
+    """A [rows, cols] output with its address and row stride: the caller's, or made here (which needs no checks)."""
+    if t is None:
+        t = like.new_empty((rows, cols), dtype=dtype)
+        return t, t.data_ptr(), cols
+    return (t,) + _mat(t, where, name, dtype, rows, cols, dev)
+
+
+def _codes(x, codes, scale, where, dev):
+    """Outputs of an 8-bit norm of x, their addresses and the codes' row stride."""
+    T, h = x.shape
+    codes, pc, sc = _result(codes, x, torch.float8_e4m3fn, T, h, where, "codes", dev)
+    if scale is None:
+        scale = x.new_empty(T, dtype=torch.float32)
+        return codes, scale, pc, sc, scale.data_ptr()
+    return codes, scale, pc, sc, _vec(scale, where, "scale", torch.float32, (T,), dev)
+
+
 def norm_quant(x, weight, eps, normalise=True, codes=None, scale=None):
     """The norm of x in 8 bits (deamoe_norm_quant): codes (torch.float8_e4m3fn [T, h]) and a scale a row (float32 [T]) with
     x / rms(x) weight = codes * scale.  normalise=False leaves the norm away: any rows in 8 bits."""
     where, dev = "deamoe_norm_quant", _device()
     dt = _type(x, where, "x")
     T, h = x.shape
-    if codes is None:
-        codes = x.new_empty((T, h), dtype=torch.float8_e4m3fn)
-    if scale is None:
-        scale = x.new_empty(T, dtype=torch.float32)
     px, sx = _mat(x, where, "x", x.dtype, T, h, dev)
-    pc, sc = _mat(codes, where, "codes", torch.float8_e4m3fn, T, h, dev)
+    codes, scale, pc, sc, ps = _codes(x, codes, scale, where, dev)
     pw, wdt = _gain(weight, where, "weight", h, dev)
-    _done(lib().deamoe_norm_quant(_raw_stream(dev), dt, px, sx, T, h, 1 if normalise else 0, wdt, pw, eps, pc, sc,
-                                  _vec(scale, where, "scale", torch.float32, (T,), dev)), where)
+    _done(lib().deamoe_norm_quant(_raw_stream(dev), dt, px, sx, T, h, 1 if normalise else 0, wdt, pw, eps, pc, sc, ps), where)
     return codes, scale
 
 
@@ -554,23 +567,16 @@ def norm_residual_quant(x, y, weight, eps, gate=None, residual_scale=1.0, branch
     where, dev = "deamoe_norm_residual_quant", _device()
     dt = _type(x, where, "x")
     T, h = x.shape
-    if out is None:
-        out = torch.empty_like(x)
-    if codes is None:
-        codes = x.new_empty((T, h), dtype=torch.float8_e4m3fn)
-    if scale is None:
-        scale = x.new_empty(T, dtype=torch.float32)
     px, sx = _mat(x, where, "x", x.dtype, T, h, dev)
     py, sy = _mat(y, where, "y", x.dtype, T, h, dev)
-    po, so = _mat(out, where, "out", x.dtype, T, h, dev)
-    pc, sc = _mat(codes, where, "codes", torch.float8_e4m3fn, T, h, dev)
+    out, po, so = _result(out, x, x.dtype, T, h, where, "out", dev)
+    codes, scale, pc, sc, ps = _codes(x, codes, scale, where, dev)
     pw, wdt = _gain(weight, where, "weight", h, dev, next_weight)
     pm, _ = _gain(next_weight, where, "next_weight", h, dev, weight)
     kind, pg, sg = _gate(gate, where, x.dtype, T, h, gate_kind, dev)
     _done(lib().deamoe_norm_residual_quant(_raw_stream(dev), dt, px, sx, py, sy, T, h, 1 if normalise else 0, wdt, pw, eps, kind,
                                            pg, sg, residual_scale, branch_scale, po, so, pm,
-                                           eps if next_eps is None else next_eps, pc, sc,
-                                           _vec(scale, where, "scale", torch.float32, (T,), dev)), where)
+                                           eps if next_eps is None else next_eps, pc, sc, ps), where)
     return out, codes, scale
 
 
@@ -594,9 +600,7 @@ def ffn(x, w_gate_up, w_down, expert_off=None, out=None):
     Rows behind the last expert's are left as they were (uninitialised if out was made here)."""
     where, dev = "deamoe_ffn", _device()
     R, h, E, f, px, sx, pu, pd, pe = _ffn_operands(x, w_gate_up, w_down, expert_off, where, dev)
-    if out is None:
-        out = x.new_empty((R, h))
-    po, so = _mat(out, where, "out", torch.bfloat16, R, h, dev)
+    out, po, so = _result(out, x, torch.bfloat16, R, h, where, "out", dev)
     L = lib()
     need = L.deamoe_ffn_workspace(E, R, h, f, 0)
     ws = _workspace(need, x)
@@ -609,14 +613,12 @@ def ffn_backward(x, w_gate_up, w_down, dout, expert_off=None, dx=None, dw_gate_u
     (deamoe_ffn_backward)."""
     where, dev = "deamoe_ffn_backward", _device()
     R, h, E, f, px, sx, pu, pd, pe = _ffn_operands(x, w_gate_up, w_down, expert_off, where, dev)
-    if dx is None:
-        dx = x.new_empty((R, h))
+    po, so = _mat(dout, where, "dout", torch.bfloat16, R, h, dev)
+    dx, pg, sg = _result(dx, x, torch.bfloat16, R, h, where, "dx", dev)
     if dw_gate_up is None:
         dw_gate_up = torch.empty_like(w_gate_up)
     if dw_down is None:
         dw_down = torch.empty_like(w_down)
-    po, so = _mat(dout, where, "dout", torch.bfloat16, R, h, dev)
-    pg, sg = _mat(dx, where, "dx", torch.bfloat16, R, h, dev)
     L = lib()
     need = L.deamoe_ffn_workspace(E, R, h, f, 1)
     ws = _workspace(need, x)
@@ -655,15 +657,13 @@ def product(x, weight, bias=None, act=SIGMA_NONE, residual=None, x_scale=None, w
     T, K, N, px, sx, pw, bdt, pb = _product_operands(x, weight, bias, act, where, dev)
     if (x_scale is None) != (dt == BF16) or (weight_scale is None) != (dt == BF16):
         _refuse(where, "x_scale and weight_scale belong to float8_e4m3fn operands, and only to them")
-    if out is None:
-        out = x.new_empty((T, N), dtype=torch.bfloat16)
-    po, so = _mat(out, where, "out", torch.bfloat16, T, N, dev)
+    out, po, so = _result(out, x, torch.bfloat16, T, N, where, "out", dev)
     pr, sr = _mat(residual, where, "residual", torch.bfloat16, T, N, dev) if residual is not None else (None, 0)
     psx = _vec(x_scale, where, "x_scale", torch.float32, (T,), dev) if x_scale is not None else None
     psw = _vec(weight_scale, where, "weight_scale", torch.float32, (N,), dev) if weight_scale is not None else None
     L = lib()
     need = L.deamoe_product_workspace(dt, T, N, K, act, 0)
-    ws = x.new_empty(need, dtype=torch.uint8) if need else None
+    ws = _workspace(need, x)
     _done(L.deamoe_product(_raw_stream(dev), dt, px, sx, psx, T, pw, psw, N, K, bdt, pb, act, pr, sr, po, so, _ptr(ws), need), where)
     return out
 
@@ -675,13 +675,11 @@ def product_backward(x, weight, dout, bias=None, act=SIGMA_NONE, dx=None, dweigh
     if x.dtype is not torch.bfloat16:
         _refuse(where, f"x must be bfloat16, got {x.dtype}")
     T, K, N, px, sx, pw, bdt, pb = _product_operands(x, weight, bias, act, where, dev)
-    if dx is None:
-        dx = x.new_empty((T, K))
+    po, so = _mat(dout, where, "dout", torch.bfloat16, T, N, dev)
+    dx, pd, sd = _result(dx, x, torch.bfloat16, T, K, where, "dx", dev)
     if dweight is None:
         dweight = torch.empty_like(weight)
     dbias = x.new_empty(N, dtype=torch.float32) if bias is not None else None
-    po, so = _mat(dout, where, "dout", torch.bfloat16, T, N, dev)
-    pd, sd = _mat(dx, where, "dx", torch.bfloat16, T, K, dev)
     L = lib()
     need = L.deamoe_product_workspace(BF16, T, N, K, act, 1)
     ws = _workspace(need, x)
