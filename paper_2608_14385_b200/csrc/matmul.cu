@@ -18,13 +18,14 @@ constexpr int MM_STEP = 2 * MM_COLS;           // ... of an epilogue step; the t
 constexpr int MM_PITCH = 128 + 4;              // floats of a row of the transposing buffer
 constexpr int MM_STAGING = MM_TEAMS * 2 * MM_COLS * MM_PITCH * 4;
 constexpr int MM_CONTROL = 512;
-// What a stage holds: the first / last chunk of a tile in the ring; a chunk that has to be cleared behind its group's end (and how many
-// steps of 16 rows it has); no more tiles.
-constexpr uint32_t STAGE_FIRST = 1u << 16, STAGE_LAST = 1u << 17, STAGE_END = 1u << 18, STAGE_TAIL = 1u << 19;
-constexpr int STAGE_STEPS = 20;
+// What the copy role says of a tile beside its first stage: its width, the steps of 16 rows of a chunk that has to be cleared behind
+// its group's end (0: none), or that there are no more tiles; and its number of chunks.
+constexpr uint32_t TILE_END = 1u << 16;
+constexpr int TILE_STEPS = 20;
 // A chunk to be cleared goes into the ring so many chunks before the tile's end, but is taken last: the MMA role need not wait for
 // the clearing (weight gradients of 16384 rows over 16 experts 861 -> 721 us).
 constexpr int MM_TAIL_LEAD = 2;
+__device__ __forceinline__ uint32_t tail_place(uint32_t chunks) { return chunks > MM_TAIL_LEAD ? chunks - 1 - MM_TAIL_LEAD : 0; }
 constexpr int MM_TABLE = (DEAMOE_MAX_EXPERTS + 1) * 8 + 8;  // groups' first tile and first row
 constexpr size_t MM_SMEM = (size_t)MM_STAGES * MM_STAGE + MM_STAGING + MM_CONTROL + MM_TABLE;
 static_assert(MM_SMEM <= 227 * 1024, "shared memory budget");
@@ -241,8 +242,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(control + 4 * MM_STAGES + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
   int* warp_sums = reinterpret_cast<int*>(tmem_slot + 2);
-  uint32_t* info = tmem_slot + 2 + 16;  // [MM_STAGES] width of a stage's tile, STAGE_* flags
-  static_assert((4 * MM_STAGES + 4) * 8 + 8 + 16 * 4 + MM_STAGES * 4 <= MM_CONTROL, "control region");
+  uint32_t* info = tmem_slot + 2 + 16;  // [MM_STAGES][2]: a tile whose first chunk the stage holds
+  static_assert((4 * MM_STAGES + 4) * 8 + 8 + 16 * 4 + MM_STAGES * 8 <= MM_CONTROL, "control region");
   int* first_row = reinterpret_cast<int*>(smem + (size_t)MM_STAGES * MM_STAGE + MM_STAGING + MM_CONTROL);
   int* first_tile = first_row + A.groups + 1;
 
@@ -302,36 +303,37 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     // ============================================================ copies
     // A chunk's issue has to fit the 512 cycles of its MMAs here too, and a copy costs its thread some 100: one warp an
     // operand, one box a chunk where the layout allows it, uniform values as in the MMA role.
-    const bool is_a = warp == MM_WARP_A;
-    uint32_t g = 0;
-    bool ok = true, free = true;  // (the first round of the ring is free)
+    const bool is_a = warp == MM_WARP_A, one = elected();
+    uint32_t g = 0, s = 0, phase = 1;  // chunks so far; stage, and the phase whose end frees it (a new barrier's phase 1 has ended)
+    bool ok = true, free = true;
     const bool rows_inner = is_a ? AT : BT;
     for (int it = pair; ok && it < tiles; it += pairs) {
       const Tile t = tile_at(it);
       const int half = t.n / 2, all = chunks_of(t);
       // the part's chunks: dealt evenly, none without one (splits <= chunks)
       const int part = SPLIT ? it % A.splits : 0;
-      const int c_begin = SPLIT ? (int)((int64_t)all * part / A.splits) : 0, chunks = SPLIT ? (int)((int64_t)all * (part + 1) / A.splits) : all;
+      const int c_begin = SPLIT ? (int)((int64_t)all * part / A.splits) : 0, c_end = SPLIT ? (int)((int64_t)all * (part + 1) / A.splits) : all;
       const int box = BT ? 3 : box_of(half);
       const uint32_t bytes = MM_OPERAND + (BT ? MM_OPERAND : 128 * (16 << box));
       const int at = is_a ? t.m0 + (int)rank * (M_STEP / 2) : t.n0 + (int)rank * half;  // first row of this CTA's part
       const int z = is_a && !RAGGED ? t.group : 0;
       const CUtensorMap* map = is_a ? &maps.a : &maps.b[BT ? 0 : box];
       const int left = RAGGED ? t.rows % A.chunk : 0;
-      const int tail_at = RAGGED && left ? max(0, chunks - 1 - MM_TAIL_LEAD) : -1;
-      for (int c = c_begin; c < chunks; ++c, ++g) {  // (c: the place in the ring's order)
-        const int s = g % MM_STAGES;
-        if (!free && !bar_wait(empty(s), ((g / MM_STAGES) & 1u) ^ 1u, abort_flag)) { ok = false; break; }
+      const int tail_at = RAGGED && left ? (int)tail_place(all) : -1;
+      for (int c = c_begin; c < c_end; ++c) {  // (c: the place in the ring's order)
+        if (!free && !bar_wait(empty(s), phase, abort_flag)) { ok = false; break; }
         // rows of the next group come along with the last chunk: this CTA's clearing warp sees them first
         const bool last_rows = RAGGED && c == tail_at;
-        const int k0 = (last_rows ? chunks - 1 : RAGGED && tail_at >= 0 && c > tail_at ? c - 1 : c) * A.chunk;
+        const int k0 = (last_rows ? all - 1 : RAGGED && tail_at >= 0 && c > tail_at ? c - 1 : c) * A.chunk;
         const int k = RAGGED ? t.row0 + k0 : k0;
         const uint32_t bar = last_rows ? tail(s) : first_full + 8 * s, dst = ring + s * MM_STAGE + (is_a ? 0 : MM_OPERAND);
-        if (elected()) {
+        if (one) {
           if (is_a && last_rows) bar_expect(tail(s), bytes);
           if (is_a && rank == 0) {
-            info[s] = t.n | (c == c_begin ? STAGE_FIRST : 0) | (c + 1 == chunks ? STAGE_LAST : 0) |
-                      (last_rows ? STAGE_TAIL | (left + 15) / 16 << STAGE_STEPS : 0);
+            if (c == c_begin) {
+              info[2 * s] = t.n | (left + 15) / 16 << TILE_STEPS;
+              info[2 * s + 1] = c_end - c_begin;
+            }
             bar_expect(full(s), last_rows ? 0 : 2 * bytes);
           }
           if (DUAL && is_a) {
@@ -344,15 +346,18 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
           }
         }
         __syncwarp();
-        const uint32_t next = g + 1;
-        free = next < MM_STAGES || bar_try(empty(next % MM_STAGES), ((next / MM_STAGES) & 1u) ^ 1u);
+        ++g;
+        if (++s == MM_STAGES) {
+          s = 0;
+          phase ^= 1u;
+        }
+        free = bar_try(empty(s), phase);
       }
     }
     if (ok && is_a) {  // the end of the list, to the MMA role
-      const int s = g % MM_STAGES;
-      ok = free || bar_wait(empty(s), ((g / MM_STAGES) & 1u) ^ 1u, abort_flag);
-      if (ok && rank == 0 && elected()) {
-        info[s] = STAGE_END;
+      ok = free || bar_wait(empty(s), phase, abort_flag);
+      if (ok && rank == 0 && one) {
+        info[2 * s] = TILE_END;
         bar_expect(full(s), 0);
       }
       __syncwarp();
@@ -362,60 +367,64 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     }
   } else if (warp == MM_WARP_MMA) {
     // ============================================================ MMAs, by the pair's first CTA
-    // The issue of a chunk has to fit the 512 cycles of its MMAs.  The whole warp walks the loop, so that descriptors are
-    // warp-uniform values, and one elected thread issues; the next stage is asked for before this one's MMAs are issued; what a
-    // stage holds the copy role has written beside it.
+    // The issue of a chunk has to fit the 512 cycles of its MMAs, fewer for narrow tiles, so its loop does nothing else.  The whole
+    // warp walks it, so that descriptors are warp-uniform values, and one elected thread issues; the next stage is asked for before
+    // this one's MMAs are issued; what a tile is the copy role has written beside its first stage.
     if (rank == 0) {
-      uint32_t g = 0, a = 0;
+      const bool one = elected();
       const uint64_t da = operand_desc(ring, AT ? MM_OPERAND / 2 : 16, 1024);
       const uint64_t db = operand_desc(ring + MM_OPERAND, BT ? MM_OPERAND / 2 : 16, 1024);
       // fp32 sums of bf16 (or e4m3: type 0) values, 256 rows, both CTAs
       const uint32_t kind = 1u << 4 | (FP8 ? 0u : (1u << 7 | 1u << 10)) | (AT ? 1u << 15 : 0u) | (BT ? 1u << 16 : 0u) | (MM_M >> 4) << 24;
-      uint32_t d = tmem, idesc = 0, add = 0, parity = 0;
-      int waiting = -1, waiting_steps = 0;  // stage of a chunk to be cleared
-      auto issue = [&](int s, int steps) {
-        tc_after();
-        if (elected()) {
+      uint32_t s = 0, phase = 0, a = 0, idesc = 0, d = tmem, cleared_phase = 0;
+      auto issue = [&](uint32_t stage, int steps, uint32_t add) {
+        if (one) {
+          const uint64_t pa = da + (stage * MM_STAGE >> 4), pb = db + (stage * MM_STAGE >> 4);
 #pragma unroll
           for (int k = 0; k < 4; ++k)  // 32 bytes of k; rows inner: 16 k's, two blocks of 1024 bytes
             if (!RAGGED || k < steps)
-              mma_pair<FP8>(d, da + ((s * MM_STAGE + k * (AT ? 2048 : 32)) >> 4), db + ((s * MM_STAGE + k * (BT ? 2048 : 32)) >> 4),
-                            idesc, k == 0 ? add : 1u);
-          commit_pair(empty(s));
+              mma_pair<FP8>(d, pa + (k * (AT ? 2048 : 32) >> 4), pb + (k * (BT ? 2048 : 32) >> 4), idesc, k == 0 ? add : 1u);
+          commit_pair(empty(stage));
         }
         __syncwarp();
-        add = 1;
       };
-      bool ready = bar_try(full(0), 0);
-      for (;; ++g) {
-        const int s = g % MM_STAGES;
-        if (!ready && !bar_wait(full(s), (g / MM_STAGES) & 1u, abort_flag)) break;
-        const uint32_t what = *(volatile uint32_t*)(info + s);
-        if (what & STAGE_END) break;
-        if (what & STAGE_FIRST) {
-          idesc = kind | (what & 0x1ffu) >> 3 << 17;
-          d = tmem + (a & 1u) * MM_N;
-          add = 0;
-          if (!bar_wait(acc_empty(a & 1u), ((a >> 1) & 1u) ^ 1u, abort_flag)) break;
-        }
-        ready = bar_try(full((g + 1) % MM_STAGES), ((g + 1) / MM_STAGES) & 1u);
-        if (RAGGED && (what & STAGE_TAIL)) {
-          waiting = s;
-          waiting_steps = what >> STAGE_STEPS;
-        } else {
-          issue(s, 4);
-        }
-        if (what & STAGE_LAST) {
-          if (RAGGED && waiting >= 0) {
-            if (!bar_wait(cleared(waiting), (parity >> waiting) & 1u, abort_flag)) break;
-            parity ^= 1u << waiting;
-            issue(waiting, waiting_steps);
-            waiting = -1;
+      bool ready = bar_try(full(0), 0), ok = true;
+      while (ok) {
+        if (!ready && !bar_wait(full(s), phase, abort_flag)) break;
+        const uint32_t what = *(volatile uint32_t*)(info + 2 * s), chunks = *(volatile uint32_t*)(info + 2 * s + 1);
+        if (what & TILE_END) break;
+        // a chunk to be cleared first comes MM_TAIL_LEAD places before the tile's end, but is taken last
+        const int tail_steps = RAGGED ? what >> TILE_STEPS : 0;
+        const uint32_t tail_at = RAGGED && tail_steps ? tail_place(chunks) : ~0u;
+        uint32_t tail_stage = 0, add = 0;
+        idesc = kind | (what & 0x1ffu) >> 3 << 17;
+        d = tmem + (a & 1u) * MM_N;
+        if (!bar_wait(acc_empty(a & 1u), ((a >> 1) & 1u) ^ 1u, abort_flag)) break;
+        tc_after();
+        for (uint32_t c = 0; c < chunks; ++c) {
+          if (c > 0 && !ready && !bar_wait(full(s), phase, abort_flag)) { ok = false; break; }
+          const uint32_t stage = s;
+          if (++s == MM_STAGES) {
+            s = 0;
+            phase ^= 1u;
           }
-          if (elected()) commit_pair(acc_full(a & 1u));
-          __syncwarp();
-          ++a;
+          ready = bar_try(full(s), phase);
+          if (RAGGED && c == tail_at) {
+            tail_stage = stage;
+            continue;
+          }
+          issue(stage, 4, add);
+          add = 1;
         }
+        if (RAGGED && ok && tail_steps) {
+          if (!bar_wait(cleared(tail_stage), (cleared_phase >> tail_stage) & 1u, abort_flag)) break;
+          cleared_phase ^= 1u << tail_stage;
+          tc_after();
+          issue(tail_stage, tail_steps, add);
+        }
+        if (ok && one) commit_pair(acc_full(a & 1u));
+        __syncwarp();
+        ++a;
       }
     }
   } else if (warp == MM_WARP_CLEAR) {
@@ -425,7 +434,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
       for (int it = pair; it < tiles; it += pairs) {
         const Tile t = tile_at(it);
         const int chunks = chunks_of(t), left = t.rows % A.chunk;
-        const int s = (g + max(0, chunks - 1 - MM_TAIL_LEAD)) % MM_STAGES;
+        const int s = (g + tail_place(chunks)) % MM_STAGES;
         g += chunks;
         if (left == 0) continue;
         int ok = lane == 0 ? bar_wait(tail(s), (parity >> s) & 1u, abort_flag) : 0;
