@@ -530,9 +530,10 @@ def quant_product(codes, scales, x, group, zeros=None, expert_off=None, row_pair
 
 
 def _result(t, like, dtype, rows, cols, where, name, dev):
-    """A [rows, cols] output with its address and row stride: the caller's, or made here (which needs no checks)."""
+    """A [rows, cols] output with its address and row stride: the caller's, or made here (which needs no checks).  `like`: a
+    [rows, any] matrix that _mat has seen (empty_like is the shortest way where it has the shape)."""
     if t is None:
-        t = like.new_empty((rows, cols), dtype=dtype)
+        t = torch.empty_like(like, dtype=dtype) if like.shape[1] == cols else like.new_empty((rows, cols), dtype=dtype)
         return t, t.data_ptr(), cols
     return (t,) + _mat(t, where, name, dtype, rows, cols, dev)
 

@@ -95,6 +95,9 @@ __device__ __forceinline__ void load_5d(uint32_t dst, const CUtensorMap* m, int 
       "cp.async.bulk.tensor.5d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], [%7];"
       ::"r"(dst), "l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(u), "r"(v), "r"(bar) : "memory");
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* m) {
+  asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
+}
 __device__ __forceinline__ bool elected() {
   uint32_t p;
   asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(p));
@@ -263,6 +266,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
+  if (tid == MM_WARP_A * 32) prefetch_map(&maps.a);
+  if (warp == MM_WARP_B && lane < (BT ? 1 : 4)) prefetch_map(&maps.b[lane]);
   if (warp == MM_WARP_MMA) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -274,22 +279,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   pdl_trigger();
   // groups' rows (offsets outside the range count as its ends) and their tiles; offsets that decrease: no tile at all
   const int mt = (A.M + M_STEP - 1) / M_STEP;
-  bool falls = false;
   const int limit = RAGGED ? A.K : A.N;
-  for (int e = tid; e <= A.groups; e += MM_THREADS) {
-    if (A.off) {
+  if (A.off) {
+    bool falls = false;
+    for (int e = tid; e <= A.groups; e += MM_THREADS) {
       const int o = A.off[e];
       if (e > 0) falls |= o < A.off[e - 1];
       first_row[e] = min(max(o, 0), limit);
-    } else {
-      first_row[e] = e == 0 ? 0 : limit;
     }
+    falls = __syncthreads_or(falls);
+    for (int e = tid; e < A.groups; e += MM_THREADS)
+      first_tile[e] = falls ? 0 : mt * tiles_along(RAGGED ? A.N : first_row[e + 1] - first_row[e], A.tile_n);
+    __syncthreads();
+    block_exclusive_scan(first_tile, A.groups, warp_sums);
+  } else if (tid == 0) {
+    first_row[0] = first_tile[0] = 0;
+    first_row[1] = limit;
+    first_tile[1] = mt * tiles_along(A.N, A.tile_n);
   }
-  falls = __syncthreads_or(falls);
-  for (int e = tid; e < A.groups; e += MM_THREADS)
-    first_tile[e] = falls ? 0 : mt * tiles_along(RAGGED ? A.N : first_row[e + 1] - first_row[e], A.tile_n);
-  __syncthreads();
-  block_exclusive_scan(first_tile, A.groups, warp_sums);
   tc_before();
   cluster_sync();
   tc_after();
@@ -687,8 +694,15 @@ cudaError_t launch(const MatmulCall& c, cudaStream_t s, bool chained) {
     if (e != cudaSuccess) return e;
     done.fetch_or(1ull << dev, std::memory_order_release);
   }
-  if (chained) return launch_pdl(kernel, dim3(2 * MM_PAIRS), dim3(MM_THREADS), MM_SMEM, s, c.args, c.maps);
-  kernel<<<2 * MM_PAIRS, MM_THREADS, MM_SMEM, s>>>(c.args, c.maps);
+  // no more pairs than there can be tiles, whatever the offsets
+  const MatmulArgs& a = c.args;
+  constexpr int m_step = EPI == ME_SWIGLU || EPI == ME_SWIGLU_GRAD || EPI == ME_PART_DUAL ? MM_M / 2 : MM_M;
+  const int64_t mt = (a.M + m_step - 1) / m_step;
+  const int64_t nt = RAGGED ? (int64_t)a.groups * ((a.N + a.tile_n - 1) / a.tile_n) : a.N / a.tile_n + (a.groups < a.N ? a.groups : a.N);
+  const int64_t most = mt * nt * a.splits;
+  const dim3 grid(2 * (unsigned)(most < MM_PAIRS ? most : MM_PAIRS));
+  if (chained) return launch_pdl(kernel, grid, dim3(MM_THREADS), MM_SMEM, s, c.args, c.maps);
+  kernel<<<grid, MM_THREADS, MM_SMEM, s>>>(c.args, c.maps);
   return cudaGetLastError();
 }
 
