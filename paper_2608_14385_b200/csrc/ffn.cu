@@ -43,10 +43,10 @@ static uint64_t ffn_parts_bytes(int E, int R, int h, int f) {
 static deamoe_status_t check_ffn(const void* x, int64_t xs, const void* wgu, const void* wd, const int32_t* off, int E, int R, int h, int f) {
   if (E <= 0 || h <= 0 || f <= 0 || (!off && E != 1)) return DEAMOE_ERR_INVALID_ARG;
   if (E > DEAMOE_MAX_EXPERTS || h > DEAMOE_MAX_WIDTH || f > DEAMOE_MAX_WIDTH || h % 8 || f % 8) return DEAMOE_ERR_UNSUPPORTED;
-  if (R < 0) return DEAMOE_ERR_BATCH;
-  // tiles are counted in 32 bits: a group has at most one tile more than its share of the rows
-  const int64_t most = (int64_t)R / MM_N + E, wide = (int64_t)(2 * (int64_t)f > h ? 2 * (int64_t)f : h) / 128 + 1;
-  if (most * wide > INT32_MAX) return DEAMOE_ERR_BATCH;
+  if (R < 0 || R > MM_MAX_ROWS) return DEAMOE_ERR_BATCH;
+  // tiles are counted in 32 bits: a group has at most one tile more than its share of the rows; a matrix's gradient tiles of 256 x 256
+  const int64_t most = (int64_t)R / MM_N + E, a = h / MM_M + 1, b = 2 * (int64_t)f / MM_N + 1;
+  if (most * 2 * (a > b ? a : b) > INT32_MAX || E * a * b > INT32_MAX) return DEAMOE_ERR_BATCH;
   if (!wgu || !wd || !aligned16(wgu) || !aligned16(wd) || !aligned_to(off, 4)) return DEAMOE_ERR_INVALID_ARG;
   if (R > 0 && (!x || !aligned16(x) || xs < h || xs % 8)) return DEAMOE_ERR_INVALID_ARG;
   return DEAMOE_OK;

@@ -106,6 +106,7 @@ struct JoinArgs {
 cudaError_t join_launch(const JoinArgs& a, cudaStream_t s);
 
 constexpr int MM_M = 256, MM_N = 256;
+constexpr int MM_MAX_ROWS = INT32_MAX - 256;  // so that a tile's end is a number of 32 bits
 constexpr int MM_N_LEAST = 64;   // matmul_tile_n gives no less for more rows
 constexpr int MM_PARTS = 2;      // rows of sums that a tile leaves in `part`
 

@@ -19,8 +19,8 @@ constexpr int BIAS_ROWS = 64;  // rows of dout that one block adds up
 __global__ void __launch_bounds__(256) k_bias_sums(const __nv_bfloat16* __restrict__ d, int64_t stride, int T, int n, float* __restrict__ part) {
   __shared__ float buf[8][256];
   const int q = threadIdx.x & 31, r = threadIdx.x >> 5;
-  const int c = blockIdx.x * 256 + q * 8;
-  const int64_t t0 = (int64_t)blockIdx.y * BIAS_ROWS;
+  const int c = blockIdx.y * 256 + q * 8;
+  const int64_t t0 = (int64_t)blockIdx.x * BIAS_ROWS;
   float s[8] = {};
   if (c < n)
 #pragma unroll
@@ -40,8 +40,8 @@ __global__ void __launch_bounds__(256) k_bias_sums(const __nv_bfloat16* __restri
 #pragma unroll
   for (int i = 0; i < 8; ++i) v += buf[i][threadIdx.x];
   pdl_trigger();
-  const int col = blockIdx.x * 256 + threadIdx.x;
-  if (col < n) part[(int64_t)blockIdx.y * n + col] = v;
+  const int col = blockIdx.y * 256 + threadIdx.x;
+  if (col < n) part[(int64_t)blockIdx.x * n + col] = v;
 }
 // Partial sums added in their order: 32 columns a block, 8 threads a column.
 __global__ void __launch_bounds__(256) k_add_parts(const float* part, int parts, int n, float* __restrict__ out) {
@@ -81,7 +81,7 @@ static deamoe_status_t check_product(int dtype, int T, int n_out, int n_in, int 
     return DEAMOE_ERR_INVALID_ARG;
   if (n_in % (dtype == DEAMOE_E4M3 ? 16 : 8) || n_in > DEAMOE_MAX_WIDTH || n_out > DEAMOE_MAX_WIDTH) return DEAMOE_ERR_UNSUPPORTED;
   const int64_t tiles = ((int64_t)T / 32 + 1) * ((n_out > n_in ? n_out : n_in) / MM_M + 1);  // counted in 32 bits
-  if (T < 0 || tiles > INT32_MAX) return DEAMOE_ERR_BATCH;
+  if (T < 0 || T > MM_MAX_ROWS || tiles > INT32_MAX) return DEAMOE_ERR_BATCH;
   return DEAMOE_OK;
 }
 
@@ -195,7 +195,7 @@ deamoe_status_t deamoe_product_backward(void* cuda_stream, int32_t dtype, const 
     ok = matmul_launch(MF_PRODUCT_GRAD, a, s, false) == cudaSuccess;
   } else if (dbias) {
     parts = (n_token + BIAS_ROWS - 1) / BIAS_ROWS;
-    k_bias_sums<<<dim3((n_out + 255) / 256, parts), 256, 0, s>>>(reinterpret_cast<const __nv_bfloat16*>(dout), dout_stride, n_token, n_out, part);
+    k_bias_sums<<<dim3(parts, (n_out + 255) / 256), 256, 0, s>>>(reinterpret_cast<const __nv_bfloat16*>(dout), dout_stride, n_token, n_out, part);
     ok = cudaGetLastError() == cudaSuccess;
   }
   if (ok && dbias)

@@ -236,3 +236,14 @@ def test_wrapper_refuses_what_does_not_fit():
     for call in bad:
         with pytest.raises(binding.DeaMoEError):
             call()
+
+
+def test_bias_gradient_of_millions_of_tokens():
+    """More rows than a grid's smaller sides hold blocks of them."""
+    T, K, N = 65536 * 64 + 77, 8, 8
+    x, w, d = _gauss((T, K), 1), _gauss((N, K), 2), _gauss((T, N), 3)
+    dx, dw, db = binding.product_backward(x, w, d, bias=torch.zeros(N, device=DEV))
+    for rows in (slice(0, 50), slice(T - 50, T)):
+        pb.check(dx[rows], *pb.dot(d[rows].double(), None, w.double().T, None))
+    pb.check(db, d.double().sum(0), (T + 8) * 2.0 ** -24 * d.double().abs().sum(0))
+    pb.check(dw, *pb.dot(d.double().T, None, x.double().T, None))
