@@ -24,14 +24,15 @@ struct FfnShape {
 
 static MatmulCall ffn_call(const FfnShape& S, int M, int K) {
   MatmulCall c = {};
-  c.args.M = M; c.args.K = K; c.args.N = S.R; c.args.groups = S.E; c.args.off = S.off; c.args.tile_n = MM_N; c.args.chunk = 64; c.args.splits = 1;
+  c.args.M = M; c.args.K = K; c.args.N = S.R; c.args.groups = S.E; c.args.off = S.off; c.args.tile_n = matmul_group_tile_n(S.R, S.E < S.R ? S.E : S.R); c.args.chunk = 64; c.args.splits = 1;
   c.args.f = S.f; c.args.wide = 1;
   return c;
 }
 
 // A forward product's parts of k: M rows of a matrix (gate and up: of both), K columns.
 static int ffn_splits(int E, int R, int64_t M, int64_t K) {
-  const int64_t tiles = (M + MM_M - 1) / MM_M * (R / MM_N + (E < R ? E : R));  // no more than that, whatever the offsets
+  const int groups = E < R ? E : R;
+  const int64_t tiles = (M + MM_M - 1) / MM_M * (R / matmul_group_tile_n(R, groups) + groups);  // no more than that, whatever the offsets
   return matmul_splits(tiles, (K + 63) / 64, R);
 }
 static uint64_t ffn_parts_bytes(int E, int R, int h, int f) {
@@ -45,7 +46,7 @@ static deamoe_status_t check_ffn(const void* x, int64_t xs, const void* wgu, con
   if (E > DEAMOE_MAX_EXPERTS || h > DEAMOE_MAX_WIDTH || f > DEAMOE_MAX_WIDTH || h % 8 || f % 8) return DEAMOE_ERR_UNSUPPORTED;
   if (R < 0 || R > MM_MAX_ROWS) return DEAMOE_ERR_BATCH;
   // tiles are counted in 32 bits: a group has at most one tile more than its share of the rows; a matrix's gradient tiles of 256 x 256
-  const int64_t most = (int64_t)R / MM_N + E, a = h / MM_M + 1, b = 2 * (int64_t)f / MM_N + 1;
+  const int64_t most = (int64_t)R / 32 + E, a = h / MM_M + 1, b = 2 * (int64_t)f / MM_N + 1;
   if (most * 2 * (a > b ? a : b) > INT32_MAX || E * a * b > INT32_MAX) return DEAMOE_ERR_BATCH;
   if (!wgu || !wd || !aligned16(wgu) || !aligned16(wd) || !aligned_to(off, 4)) return DEAMOE_ERR_INVALID_ARG;
   if (R > 0 && (!x || !aligned16(x) || xs < h || xs % 8)) return DEAMOE_ERR_INVALID_ARG;
@@ -98,9 +99,9 @@ deamoe_status_t deamoe_ffn(void* cuda_stream, const void* x, int64_t x_stride, c
     c.args.splits = splits; c.args.out = part; c.args.os = (int64_t)c.args.M * (dual ? 2 : 1); c.args.out_group = c.args.os * n_rows;
     return j;
   };
-  if (!map_gate_up(&up.maps.a, w_gate_up, hidden, ffn, n_expert) || !map_b(&up.maps, x, 2, hidden, n_rows, x_stride) ||
+  if (!map_gate_up(&up.maps.a, w_gate_up, hidden, ffn, n_expert) || !map_b(&up, x, 2, hidden, n_rows, x_stride) ||
       !map_rows(&down.maps.a, w_down, 2, ffn, hidden, ffn, n_expert, (int64_t)hidden * ffn, 128) ||
-      !map_b(&down.maps, workspace, 2, ffn, n_rows, ffn))
+      !map_b(&down, workspace, 2, ffn, n_rows, ffn))
     return DEAMOE_ERR_CUDA;
   cudaError_t e;
   if (up_splits > 1) {
@@ -153,18 +154,18 @@ deamoe_status_t deamoe_ffn_backward(void* cuda_stream, const void* x, int64_t x_
   MatmulCall c = ffn_call(S, hidden, 2 * ffn);  // dx = [dg du] [Wg; Wu]
   c.args.out = dx; c.args.os = dx_stride;
   MatmulCall d = ffn_call(S, hidden, n_rows);  // d[Wg; Wu] = [dg du]^T x
-  d.args.N = 2 * ffn; d.args.out = dw_gate_up; d.args.os = hidden; d.args.out_group = 2 * wd_one;
+  d.args.tile_n = MM_N; d.args.N = 2 * ffn; d.args.out = dw_gate_up; d.args.os = hidden; d.args.out_group = 2 * wd_one;
   MatmulCall e = ffn_call(S, ffn, n_rows);  // dWd = dy^T h
-  e.args.N = hidden; e.args.out = dw_down; e.args.os = ffn; e.args.out_group = wd_one;
+  e.args.tile_n = MM_N; e.args.N = hidden; e.args.out = dw_down; e.args.os = ffn; e.args.out_group = wd_one;
   d.args.late = e.args.late = 1;  // they need b's results as c does, and c waits for those
-  if (!map_rows(&a.maps.a, w_down, 2, ffn, hidden, ffn, n_expert, wd_one, 64) || !map_b(&a.maps, dout, 2, hidden, n_rows, dout_stride) ||
-      !map_gate_up(&b.maps.a, w_gate_up, hidden, ffn, n_expert) || !map_b(&b.maps, x, 2, hidden, n_rows, x_stride) ||
+  if (!map_rows(&a.maps.a, w_down, 2, ffn, hidden, ffn, n_expert, wd_one, 64) || !map_b(&a, dout, 2, hidden, n_rows, dout_stride) ||
+      !map_gate_up(&b.maps.a, w_gate_up, hidden, ffn, n_expert) || !map_b(&b, x, 2, hidden, n_rows, x_stride) ||
       !map_rows(&c.maps.a, w_gate_up, 2, hidden, 2 * (int64_t)ffn, hidden, n_expert, 2 * wd_one, 64) ||
-      !map_b(&c.maps, dgu, 2, 2 * (int64_t)ffn, n_rows, 2 * (int64_t)ffn) ||
+      !map_b(&c, dgu, 2, 2 * (int64_t)ffn, n_rows, 2 * (int64_t)ffn) ||
       !map_rows(&d.maps.a, x, 2, hidden, n_rows, x_stride, 1, x_stride, 64) ||
-      !map_rows(&d.maps.b[0], dgu, 2, 2 * (int64_t)ffn, n_rows, 2 * (int64_t)ffn, 1, 2 * (int64_t)ffn, 64) ||
+      !map_b_rows_inner(&d, dgu, 2 * (int64_t)ffn, n_rows, 2 * (int64_t)ffn) ||
       !map_rows(&e.maps.a, hh, 2, ffn, n_rows, ffn, 1, ffn, 64) ||
-      !map_rows(&e.maps.b[0], dout, 2, hidden, n_rows, dout_stride, 1, dout_stride, 64))
+      !map_b_rows_inner(&e, dout, hidden, n_rows, dout_stride))
     return DEAMOE_ERR_CUDA;
   if (matmul_launch(MF_F32_TRANSPOSED, a, s, false) == cudaSuccess && matmul_launch(MF_SWIGLU_GRAD, b, s, true) == cudaSuccess &&
       matmul_launch(MF_STORE_TRANSPOSED, c, s, true) == cudaSuccess && matmul_launch(MF_WEIGHT_GRAD, d, s, true) == cudaSuccess &&

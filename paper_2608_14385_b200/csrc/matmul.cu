@@ -7,9 +7,9 @@ namespace deamoe {
 
 namespace {
 
-constexpr int MM_STAGES = 5;
+constexpr int MM_RING = 168 * 1024;            // stages of 32 KB (five) to 18 KB (nine), as B's box needs
+constexpr int MM_STAGES = 9;                   // at most
 constexpr int MM_OPERAND = 16 * 1024;          // one CTA's part of a chunk of A or of B: 128 rows of 128 bytes
-constexpr int MM_STAGE = 2 * MM_OPERAND;
 constexpr int MM_TEAMS = 2;                    // epilogue teams of 4 warps (a warp reads the 32 lanes of tensor memory of its number mod 4)
 constexpr int MM_WARP_A = 4 * MM_TEAMS, MM_WARP_B = MM_WARP_A + 1, MM_WARP_MMA = MM_WARP_A + 2, MM_WARP_CLEAR = MM_WARP_A + 3;
 constexpr int MM_THREADS = (MM_WARP_CLEAR + 1) * 32;
@@ -27,7 +27,8 @@ constexpr int TILE_STEPS = 20;
 constexpr int MM_TAIL_LEAD = 2;
 __device__ __forceinline__ uint32_t tail_place(uint32_t chunks) { return chunks > MM_TAIL_LEAD ? chunks - 1 - MM_TAIL_LEAD : 0; }
 constexpr int MM_TABLE = (DEAMOE_MAX_EXPERTS + 1) * 8 + 8;  // groups' first tile and first row
-constexpr size_t MM_SMEM = (size_t)MM_STAGES * MM_STAGE + MM_STAGING + MM_CONTROL + MM_TABLE;
+constexpr size_t MM_SMEM = (size_t)MM_RING + MM_STAGING + MM_CONTROL + MM_TABLE;
+static_assert(MM_RING / (MM_OPERAND + 16 * 128) <= MM_STAGES, "barriers of a stage");
 static_assert(MM_SMEM <= 227 * 1024, "shared memory budget");
 // One CTA fills more than half of an SM's shared memory, so none of another grid's can be beside it and the
 // allocation of all 512 columns of tensor memory never waits.
@@ -167,17 +168,15 @@ template <bool RAGGED> __device__ __forceinline__ Tile find_tile(const MatmulArg
   const int band = r / (MM_BAND * mt), rest = r - band * MM_BAND * mt;
   const int width = min(MM_BAND, nt - band * MM_BAND);
   const int mi = rest / width, ni = band * MM_BAND + rest - mi * width;
-  const int units = (cols + 15) / 16, u0 = (int)((int64_t)ni * units / nt);
-  o.n = ((int)((int64_t)(ni + 1) * units / nt) - u0) * 16;
+  const int units = (cols + 15) / 16, base = units / nt, more = units - base * nt;  // the first `more` tiles have one more
+  const int u0 = ni * base + min(ni, more);
+  o.n = (base + (ni < more)) * 16;
   o.m0 = mi * m_step;
   o.n_index = ni;
   o.valid = min(o.n, cols - u0 * 16);
   o.n0 = u0 * 16 + (RAGGED ? 0 : o.row0);
   return o;
 }
-
-// the lowest box (16, 32, 64 or 128 rows of B) that holds a CTA's half of a tile: one copy a chunk, whatever it brings along
-__device__ __forceinline__ int box_of(int half) { return half <= 16 ? 0 : half <= 32 ? 1 : half <= 64 ? 2 : 3; }
 
 // ---------------------------------------------------------------- epilogue arithmetic
 __device__ __forceinline__ float sigmoid(float v) { return __fdividef(1.f, 1.f + __expf(-v)); }
@@ -232,8 +231,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   constexpr bool SPLIT = EPI == ME_PART || EPI == ME_PART_DUAL;
   constexpr int M_STEP = DUAL ? MM_M / 2 : MM_M;                    // in rows of A as the caller counts them (DUAL: features)
   extern __shared__ __align__(1024) unsigned char smem[];
-  float* staging = reinterpret_cast<float*>(smem + (size_t)MM_STAGES * MM_STAGE);
-  uint64_t* control = reinterpret_cast<uint64_t*>(smem + (size_t)MM_STAGES * MM_STAGE + MM_STAGING);
+  float* staging = reinterpret_cast<float*>(smem + MM_RING);
+  uint64_t* control = reinterpret_cast<uint64_t*>(smem + MM_RING + MM_STAGING);
   const uint32_t ring = smem_u32(smem), bars = smem_u32(control);
   auto full = [&](int s) { return bars + 8 * s; };
   auto empty = [&](int s) { return bars + 8 * (MM_STAGES + s); };
@@ -247,11 +246,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   int* warp_sums = reinterpret_cast<int*>(tmem_slot + 2);
   uint32_t* info = tmem_slot + 2 + 16;  // [MM_STAGES][2]: a tile whose first chunk the stage holds
   static_assert((4 * MM_STAGES + 4) * 8 + 8 + 16 * 4 + MM_STAGES * 8 <= MM_CONTROL, "control region");
-  int* first_row = reinterpret_cast<int*>(smem + (size_t)MM_STAGES * MM_STAGE + MM_STAGING + MM_CONTROL);
+  int* first_row = reinterpret_cast<int*>(smem + MM_RING + MM_STAGING + MM_CONTROL);
   int* first_tile = first_row + A.groups + 1;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-  const uint32_t rank = cluster_rank();
+  const uint32_t rank = cluster_rank(), stages = A.stages, stage_bytes = MM_OPERAND + A.b_bytes;
   if (tid == 0) {
     for (int s = 0; s < MM_STAGES; ++s) {
       bar_init(full(s), 1);
@@ -267,7 +266,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (tid == MM_WARP_A * 32) prefetch_map(&maps.a);
-  if (warp == MM_WARP_B && lane < (BT ? 1 : 4)) prefetch_map(&maps.b[lane]);
+  if (tid == MM_WARP_B * 32) prefetch_map(&maps.b);
   if (warp == MM_WARP_MMA) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -319,12 +318,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
       const int half = t.n / 2, all = chunks_of(t);
       // the part's chunks: dealt evenly, none without one (splits <= chunks)
       const int part = SPLIT ? it % A.splits : 0;
-      const int c_begin = SPLIT ? (int)((int64_t)all * part / A.splits) : 0, c_end = SPLIT ? (int)((int64_t)all * (part + 1) / A.splits) : all;
-      const int box = BT ? 3 : box_of(half);
-      const uint32_t bytes = MM_OPERAND + (BT ? MM_OPERAND : 128 * (16 << box));
+      const int base = SPLIT ? all / A.splits : all, more = SPLIT ? all - base * A.splits : 0;
+      const int c_begin = part * base + min(part, more), c_end = c_begin + base + (part < more);
       const int at = is_a ? t.m0 + (int)rank * (M_STEP / 2) : t.n0 + (int)rank * half;  // first row of this CTA's part
       const int z = is_a && !RAGGED ? t.group : 0;
-      const CUtensorMap* map = is_a ? &maps.a : &maps.b[BT ? 0 : box];
+      const CUtensorMap* map = is_a ? &maps.a : &maps.b;
       const int left = RAGGED ? t.rows % A.chunk : 0;
       const int tail_at = RAGGED && left ? (int)tail_place(all) : -1;
       for (int c = c_begin; c < c_end; ++c) {  // (c: the place in the ring's order)
@@ -333,15 +331,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
         const bool last_rows = RAGGED && c == tail_at;
         const int k0 = (last_rows ? all - 1 : RAGGED && tail_at >= 0 && c > tail_at ? c - 1 : c) * A.chunk;
         const int k = RAGGED ? t.row0 + k0 : k0;
-        const uint32_t bar = last_rows ? tail(s) : first_full + 8 * s, dst = ring + s * MM_STAGE + (is_a ? 0 : MM_OPERAND);
+        const uint32_t bar = last_rows ? tail(s) : first_full + 8 * s, dst = ring + s * stage_bytes + (is_a ? 0 : MM_OPERAND);
         if (one) {
-          if (is_a && last_rows) bar_expect(tail(s), bytes);
+          if (is_a && last_rows) bar_expect(tail(s), stage_bytes);
           if (is_a && rank == 0) {
             if (c == c_begin) {
               info[2 * s] = t.n | (left + 15) / 16 << TILE_STEPS;
               info[2 * s + 1] = c_end - c_begin;
             }
-            bar_expect(full(s), last_rows ? 0 : 2 * bytes);
+            bar_expect(full(s), last_rows ? 0 : 2 * stage_bytes);
           }
           if (DUAL && is_a) {
             load_5d(dst, map, k0, 0, 0, at / 8, z, bar);
@@ -354,7 +352,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
         }
         __syncwarp();
         ++g;
-        if (++s == MM_STAGES) {
+        if (++s == stages) {
           s = 0;
           phase ^= 1u;
         }
@@ -369,8 +367,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
       }
       __syncwarp();
       // the last commits must have arrived here before this CTA may end
-      for (uint32_t d = g > MM_STAGES ? g - MM_STAGES : 0; ok && d < g; ++d)
-        ok = bar_wait(empty(d % MM_STAGES), (d / MM_STAGES) & 1u, abort_flag);
+      for (uint32_t d = g > stages ? g - stages : 0; ok && d < g; ++d) ok = bar_wait(empty(d % stages), (d / stages) & 1u, abort_flag);
     }
   } else if (warp == MM_WARP_MMA) {
     // ============================================================ MMAs, by the pair's first CTA
@@ -386,7 +383,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
       uint32_t s = 0, phase = 0, a = 0, idesc = 0, d = tmem, cleared_phase = 0;
       auto issue = [&](uint32_t stage, int steps, uint32_t add) {
         if (one) {
-          const uint64_t pa = da + (stage * MM_STAGE >> 4), pb = db + (stage * MM_STAGE >> 4);
+          const uint64_t pa = da + (stage * stage_bytes >> 4), pb = db + (stage * stage_bytes >> 4);
 #pragma unroll
           for (int k = 0; k < 4; ++k)  // 32 bytes of k; rows inner: 16 k's, two blocks of 1024 bytes
             if (!RAGGED || k < steps)
@@ -411,7 +408,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
         for (uint32_t c = 0; c < chunks; ++c) {
           if (c > 0 && !ready && !bar_wait(full(s), phase, abort_flag)) { ok = false; break; }
           const uint32_t stage = s;
-          if (++s == MM_STAGES) {
+          if (++s == stages) {
             s = 0;
             phase ^= 1u;
           }
@@ -441,14 +438,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
       for (int it = pair; it < tiles; it += pairs) {
         const Tile t = tile_at(it);
         const int chunks = chunks_of(t), left = t.rows % A.chunk;
-        const int s = (g + tail_place(chunks)) % MM_STAGES;
+        const int s = (g + tail_place(chunks)) % stages;
         g += chunks;
         if (left == 0) continue;
         int ok = lane == 0 ? bar_wait(tail(s), (parity >> s) & 1u, abort_flag) : 0;
         ok = __shfl_sync(0xffffffffu, ok, 0);
         if (!ok) break;
         parity ^= 1u << s;
-        unsigned char* st = smem + (size_t)s * MM_STAGE;
+        unsigned char* st = smem + (size_t)s * stage_bytes;
         const int to = (left + 15) / 16 * 128;  // 16-byte pieces of a box's rows of 128 bytes, up to a step of 16 rows
         for (int b = 0; b < 4; ++b)
           for (int i = left * 8 + lane; i < to; i += 32) *reinterpret_cast<uint4*>(st + b * (MM_OPERAND / 2) + i * 16) = make_uint4(0, 0, 0, 0);
@@ -721,10 +718,26 @@ bool map_gate_up(CUtensorMap* m, const void* p, int64_t cols, int64_t f, int64_t
   const cuuint32_t box[5] = {64, 8, 2, 8, 1};
   return encode(m, p, 2, 5, dims, strides, box);
 }
-bool map_b(MatmulMaps* m, const void* p, int esize, int64_t cols, int64_t rows, int64_t stride) {
-  for (int i = 0; i < 4; ++i)
-    if (!map_rows(&m->b[i], p, esize, cols, rows, stride, 1, stride, 16 << i)) return false;
-  return true;
+bool map_b(MatmulCall* c, const void* p, int esize, int64_t cols, int64_t rows, int64_t stride) {
+  // the lowest box (16, 32, 64 or 128 rows) that holds a CTA's half of the widest tile: one copy a chunk, and what the box does not
+  // need of a stage goes to more stages
+  const int half = (c->args.tile_n + 15) / 16 * 8;
+  int box = 16;
+  while (box < half) box *= 2;
+  c->args.b_bytes = box * 128;
+  c->args.stages = MM_RING / (MM_OPERAND + c->args.b_bytes);
+  return map_rows(&c->maps.b, p, esize, cols, rows, stride, 1, stride, box);
+}
+bool map_b_rows_inner(MatmulCall* c, const void* p, int64_t cols, int64_t rows, int64_t stride) {
+  c->args.b_bytes = MM_OPERAND;
+  c->args.stages = MM_RING / (2 * MM_OPERAND);
+  return map_rows(&c->maps.b, p, 2, cols, rows, stride, 1, stride, 64);
+}
+int matmul_group_tile_n(int64_t rows, int64_t groups) {
+  const int64_t each = (rows + groups - 1) / groups;
+  int n = 32;
+  while (n < MM_N && (n < 4 * each || n < rows / 32)) n *= 2;
+  return n;
 }
 
 // The pairs take the tiles in rounds, and a round costs a tile's width and some 100 columns more (2048 x 4096 x 4096: rounds of

@@ -14,7 +14,7 @@
 //
 // Roles of a CTA (1 CTA per SM, clusters of 2, tiles dealt in a fixed order so that equal calls give equal bits):
 //   warps 0-7  epilogue, two teams that share a tile's columns: accumulator -> registers -> a small transposing buffer -> 16-byte rows, with the epilogue's arithmetic in fp32
-//   warps 8, 9 one thread each issues the TMA copies of A's / B's part of a chunk (128 bytes of k, 128-byte swizzle) into a ring of 5 stages
+//   warps 8, 9 one thread each issues the TMA copies of A's / B's part of a chunk (128 bytes of k, 128-byte swizzle) into a ring of 5 to 9 stages
 //   warp  10   in the pair's first CTA one thread issues the MMAs for both
 //   warp  11   ragged contractions (weight gradients: k runs over a group's rows): clears the rows behind the group's end
 //              that the last chunk's box brought in, in both operands, before the MMAs may read them
@@ -47,6 +47,7 @@ struct MatmulArgs {
   int tile_n;            // widest tile
   int chunk;             // values of k in 128 bytes
   int splits;            // parts of k that a tile is dealt in (ME_PART, ME_PART_DUAL; else 1)
+  int stages, b_bytes;   // of the ring; bytes of a chunk of B's box in a stage (map_b, map_b_rows_inner)
   int late;              // behind another kernel of the call whose results it does not need (see matmul.cu)
   // epilogue
   void* out;
@@ -64,8 +65,7 @@ struct MatmulArgs {
 };
 
 struct MatmulMaps {
-  CUtensorMap a;
-  CUtensorMap b[4];  // B with k as the inner axis: boxes of 16, 32, 64 and 128 rows; else b[0] alone
+  CUtensorMap a, b;
 };
 
 // Launch one product.  kind: epilogue; a_rows_inner / b_rows_inner: A / B stored with its rows as the inner axis; fp8: e4m3.
@@ -83,11 +83,16 @@ cudaError_t matmul_launch(MatmulForm form, const MatmulCall& c, cudaStream_t s, 
 bool map_rows(CUtensorMap* m, const void* p, int esize, int64_t cols, int64_t rows, int64_t stride, int64_t groups, int64_t group_stride,
               int box_rows);                       // box: 128 bytes of a row x box_rows rows
 bool map_gate_up(CUtensorMap* m, const void* p, int64_t cols, int64_t f, int64_t groups);  // 128 rows: 8 gate, 8 up, ...
-bool map_b(MatmulMaps* m, const void* p, int esize, int64_t cols, int64_t rows, int64_t stride);
+// ... of B, with its share of a stage: rows of k as the inner axis (after args.tile_n), or B's rows as the inner axis
+bool map_b(MatmulCall* c, const void* p, int esize, int64_t cols, int64_t rows, int64_t stride);
+bool map_b_rows_inner(MatmulCall* c, const void* p, int64_t cols, int64_t rows, int64_t stride);
 
 // Tile width of `n` rows in one group for `m_tiles` tiles of A's rows; whole: the product may be split along k.  See matmul.cu
 int matmul_tile_n(int64_t n, int64_t m_tiles, bool whole);
 
+// Widest tile for `rows` rows in `groups` groups of unknown sizes: four times the average, so that most groups are one tile and a
+// stage of the ring holds no more of B than they need, and a 32nd of all rows at least, should they come to one group
+int matmul_group_tile_n(int64_t rows, int64_t groups);
 // Parts of k for a product of at most `tiles` tiles, `chunks` chunks of k and `rows` rows in all (1: not split): see matmul.cu
 int matmul_splits(int64_t tiles, int64_t chunks, int64_t rows);
 

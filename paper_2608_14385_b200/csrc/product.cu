@@ -120,7 +120,7 @@ deamoe_status_t deamoe_product(void* cuda_stream, int32_t dtype, const void* x, 
   c.args.residual = residual; c.args.rs = residual_stride; c.args.wide_in = wide_rows(residual, residual_stride, n_token, 2);
   c.args.x_scale = x_scale; c.args.w_scale = weight_scale;
   const int es = e4m3 ? 1 : 2;
-  if (!map_rows(&c.maps.a, weight, es, n_in, n_out, n_in, 1, n_in, 128) || !map_b(&c.maps, x, es, n_in, n_token, x_stride)) return DEAMOE_ERR_CUDA;
+  if (!map_rows(&c.maps.a, weight, es, n_in, n_out, n_in, 1, n_in, 128) || !map_b(&c, x, es, n_in, n_token, x_stride)) return DEAMOE_ERR_CUDA;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
   const int splits = product_splits(c.args);
   if (splits > 1) {  // few tiles: dealt along k, the parts' sums joined by a kernel of their own
@@ -182,10 +182,10 @@ deamoe_status_t deamoe_product_backward(void* cuda_stream, int32_t dtype, const 
   a.args.dout = dout; a.args.rs = dout_stride; a.args.wide_in = 1; a.args.part = dbias ? part : nullptr;
   b.args.out = dx; b.args.os = dx_stride; b.args.wide = 1;
   c.args.out = dweight; c.args.os = n_in; c.args.wide = 1;
-  if ((!plain && (!map_rows(&a.maps.a, weight, 2, n_in, n_out, n_in, 1, n_in, 128) || !map_b(&a.maps, x, 2, n_in, n_token, x_stride))) ||
-      !map_rows(&b.maps.a, weight, 2, n_in, n_out, n_in, 1, n_in, 64) || !map_b(&b.maps, g, 2, n_out, n_token, gs) ||
+  if ((!plain && (!map_rows(&a.maps.a, weight, 2, n_in, n_out, n_in, 1, n_in, 128) || !map_b(&a, x, 2, n_in, n_token, x_stride))) ||
+      !map_rows(&b.maps.a, weight, 2, n_in, n_out, n_in, 1, n_in, 64) || !map_b(&b, g, 2, n_out, n_token, gs) ||
       !map_rows(&c.maps.a, x, 2, n_in, n_token, x_stride, 1, x_stride, 64) ||
-      !map_rows(&c.maps.b[0], g, 2, n_out, n_token, gs, 1, gs, 64))
+      !map_b_rows_inner(&c, g, n_out, n_token, gs))
     return DEAMOE_ERR_CUDA;
   c.args.late = 1;  // it needs dz as b does, and b waits for it
   bool ok = true;
