@@ -29,6 +29,9 @@ static MatmulCall ffn_call(const FfnShape& S, int M, int K) {
   return c;
 }
 
+// Few rows, of few experts: from some nine experts on there are tiles enough for the tensor-core kernel, whose copies keep more bytes in
+// flight (one row each, 7168 x 2048: 8 experts 120 us thin and 126, 12 experts 205 and 180, 16 experts 240 and 219).
+static bool ffn_thin(int E, int R) { return R <= THIN_ROWS && (E <= 8 || R <= 8); }
 // A forward product's parts of k: M rows of a matrix (gate and up: of both), K columns.
 static int ffn_splits(int E, int R, int64_t M, int64_t K) {
   const int groups = E < R ? E : R;
@@ -64,7 +67,7 @@ uint64_t deamoe_ffn_workspace(int32_t n_expert, int32_t n_rows, int32_t hidden, 
   if (n_expert <= 0 || n_rows <= 0 || hidden <= 0 || ffn <= 0) return 0;
   const uint64_t v = (uint64_t)n_rows * ffn;
   if (backward) return ceil256(4 * v) + ceil256(4 * v) + ceil256(2 * v);
-  return ceil256(2 * v) + (n_rows <= THIN_ROWS ? 0 : ffn_parts_bytes(n_expert, n_rows, hidden, ffn));
+  return ceil256(2 * v) + (ffn_thin(n_expert, n_rows) ? 0 : ffn_parts_bytes(n_expert, n_rows, hidden, ffn));
 }
 
 deamoe_status_t deamoe_ffn(void* cuda_stream, const void* x, int64_t x_stride, const void* w_gate_up, const void* w_down,
@@ -75,7 +78,7 @@ deamoe_status_t deamoe_ffn(void* cuda_stream, const void* x, int64_t x_stride, c
   if (bad_rows8(out, out_stride, hidden) || out == x) return DEAMOE_ERR_INVALID_ARG;
   if (!workspace || !aligned16(workspace) || workspace_bytes < deamoe_ffn_workspace(n_expert, n_rows, hidden, ffn, 0)) return DEAMOE_ERR_INVALID_ARG;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
-  if (n_rows <= THIN_ROWS) {
+  if (ffn_thin(n_expert, n_rows)) {
     ThinArgs a = {};
     a.x = x; a.xs = x_stride; a.w = w_gate_up; a.M = ffn; a.K = hidden; a.n_rows = n_rows; a.groups = n_expert; a.off = expert_off;
     a.out = reinterpret_cast<__nv_bfloat16*>(workspace); a.os = ffn;

@@ -13,10 +13,9 @@ constexpr int MM_OPERAND = 16 * 1024;          // one CTA's part of a chunk of A
 constexpr int MM_TEAMS = 2;                    // epilogue teams of 4 warps (a warp reads the 32 lanes of tensor memory of its number mod 4)
 constexpr int MM_WARP_A = 4 * MM_TEAMS, MM_WARP_B = MM_WARP_A + 1, MM_WARP_MMA = MM_WARP_A + 2, MM_WARP_CLEAR = MM_WARP_A + 3;
 constexpr int MM_THREADS = (MM_WARP_CLEAR + 1) * 32;
-constexpr int MM_COLS = 16;                    // accumulator columns of one of the two transposing buffers
-constexpr int MM_STEP = 2 * MM_COLS;           // ... of an epilogue step; the teams take steps in turn
-constexpr int MM_PITCH = 128 + 4;              // floats of a row of the transposing buffer
-constexpr int MM_STAGING = MM_TEAMS * 2 * MM_COLS * MM_PITCH * 4;
+constexpr int MM_STEP = 32;                    // accumulator columns of an epilogue step
+constexpr int MM_PITCH = 32 + 4;               // floats of a row of a warp's transposing buffer
+constexpr int MM_STAGING = MM_TEAMS * 4 * MM_STEP * MM_PITCH * 4;
 constexpr int MM_CONTROL = 512;
 // What the copy role says of a tile beside its first stage: its width, the steps of 16 rows of a chunk that has to be cleared behind
 // its group's end (0: none), or that there are no more tiles; and its number of chunks.
@@ -135,7 +134,6 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[32]) {
       : "r"(addr));
 }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ void team_sync(int team) { asm volatile("bar.sync %0, 128;" ::"r"(1 + team) : "memory"); }
 
 // ---------------------------------------------------------------- the order of the tiles
 struct Tile {
@@ -456,25 +454,25 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     }
   } else {
     // ============================================================ epilogue
-    // One warp a scheduler runs such code at some seven cycles an instruction, so two teams share a tile's columns,
-    // and rows are walked by pointer.
+    // A warp by itself: its 32 lanes of the accumulator are 32 columns of the output (DUAL: 16 features), which it turns through its own
+    // buffer, 32 rows at a time.  The warps of a team share a step's rows; the teams take steps in turn.
     if (EPI == ME_SWIGLU_GRAD) pdl_wait();
     uint32_t a = 0;
     bool ok = true;
-    const int team = warp >> 2, me = tid & 127;
-    float* const st = staging + team * (2 * MM_COLS * MM_PITCH);
+    const int team = warp >> 2;
+    float* const st = staging + warp * (MM_STEP * MM_PITCH);
     const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
-    // A thread's part of a buffer: DUAL: one row, 8 features; else rows c and c + 8, 8 columns of the output.
-    constexpr int ITEMS = DUAL ? 1 : 2, ITEM_ROWS = MM_COLS / ITEMS;
+    // A thread's part of a step: rows c, c + ITEM_ROWS, ... and 8 columns (DUAL: 8 features).
+    constexpr int ITEMS = DUAL ? 2 : 4, ITEM_ROWS = MM_STEP / ITEMS;
     constexpr int OUT_BYTES = EPI == ME_STORE_F32 || SPLIT ? 4 : 2;
-    const int q = DUAL ? me & 7 : me & 15, c = DUAL ? me >> 3 : me >> 4;
+    const int q = DUAL ? lane & 1 : lane & 3, c = DUAL ? lane >> 1 : lane >> 2;
     const int64_t out_step = A.os * (ITEM_ROWS * OUT_BYTES);
     const float* const mine = st + c * MM_PITCH + q * (DUAL ? 16 : 8);
     for (int it = pair; ok && it < tiles; it += pairs) {
       const Tile t = tile_at(it);
       const bool none = RAGGED && t.rows == 0;  // a group without rows: zeros
       const uint32_t buf = a & 1u;
-      const int m = t.m0 + (int)rank * (M_STEP / 2) + q * 8, n = min(8, A.M - m);
+      const int m = t.m0 + (int)rank * (M_STEP / 2) + (warp & 3) * (M_STEP / 8) + q * 8, n = min(8, A.M - m);
       const int valid = n > 0 ? t.valid : 0;
       const int64_t row0 = t.n0 + team * MM_STEP + c;
       char* out = reinterpret_cast<char*>(A.out) + ((RAGGED ? (int64_t)t.group * A.out_group : SPLIT ? (int64_t)(it % A.splits) * A.out_group : 0) +
@@ -489,7 +487,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
         if constexpr (EPI == ME_SWIGLU_GRAD || EPI == ME_PRODUCT || EPI == ME_PRODUCT_GRAD) {
           const char* p = in;
 #pragma unroll
-          for (int i = 0; i < 2 * ITEMS; ++i, p += in_stride * ITEM_ROWS)
+          for (int i = 0; i < ITEMS; ++i, p += in_stride * ITEM_ROWS)
             if (at + i * ITEM_ROWS < valid) {
               if constexpr (EPI == ME_SWIGLU_GRAD) {
                 w.v[2 * i] = reinterpret_cast<const uint4*>(p)[0];
@@ -497,7 +495,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
               } else if (wide_in) {
                 w.v[i] = load_once<__nv_bfloat16, 8>(reinterpret_cast<const __nv_bfloat16*>(p)).r;
               }
-              if constexpr (FP8) w.scale[i] = xs[i * ITEM_ROWS];
+              if constexpr (FP8 && !SPLIT) w.scale[i] = xs[i * ITEM_ROWS];
             }
           in += in_stride * (MM_TEAMS * MM_STEP);
           if constexpr (FP8) xs += MM_TEAMS * MM_STEP;
@@ -516,16 +514,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
       if (!none) {
         const int w = lane == 0 ? bar_wait(acc_full(buf), (a >> 1) & 1u, abort_flag) : 0;
         ok = __shfl_sync(0xffffffffu, w, 0) != 0;
-        // all four warps of a team or none: they meet at barriers below
-        int all;
-        asm volatile("{\n.reg .pred p, q;\nsetp.ne.b32 p, %1, 0;\nbar.red.and.pred q, %2, 128, p;\nselp.b32 %0, 1, 0, q;\n}"
-                     : "=r"(all) : "r"((int)ok), "r"(1 + team) : "memory");
-        ok = all != 0;
         if (!ok) break;
         tc_after();
         ++a;
       }
-      auto release = [&] {  // the accumulator has been read
+      auto release = [&] {  // this warp has read its part of the accumulator
         tc_before();
         __syncwarp();
         if (lane == 0) bar_arrive_cluster(in_first(acc_empty(buf)));
@@ -543,93 +536,88 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
           if (c0 + MM_TEAMS * MM_STEP >= t.n) release();
         }
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          constexpr int BUF = MM_COLS * MM_PITCH;
+        for (int i = 0; i < MM_STEP; ++i) st[i * MM_PITCH + lane] = __uint_as_float(r[i]);
+        __syncwarp();
 #pragma unroll
-          for (int i = 0; i < MM_COLS; ++i) st[h * BUF + i * MM_PITCH + (warp & 3) * 32 + lane] = __uint_as_float(r[h * MM_COLS + i]);
-          team_sync(team);
+        for (int i = 0; i < ITEMS; ++i, out += out_step) {
+          if (c0 + i * ITEM_ROWS + c >= valid) continue;
+          const float* from_st = mine + i * (ITEM_ROWS * MM_PITCH);
+          __nv_bfloat16* const to = reinterpret_cast<__nv_bfloat16*>(out);
+          float v[8];
+          floats8(from_st, v);
+          if constexpr (DUAL) {  // (f is a multiple of 8)
+            float up[8];
+            floats8(from_st + 8, up);
+            if constexpr (EPI == ME_PART_DUAL) {
+              put8(reinterpret_cast<float*>(out), v);
+              put8(reinterpret_cast<float*>(out) + 8, up);
+            } else if constexpr (EPI == ME_SWIGLU) {
 #pragma unroll
-          for (int i = 0; i < ITEMS; ++i, out += out_step) {
-            if (c0 + h * MM_COLS + i * ITEM_ROWS + c >= valid) continue;
-            const float* from_st = mine + h * BUF + i * (ITEM_ROWS * MM_PITCH);
-            __nv_bfloat16* const to = reinterpret_cast<__nv_bfloat16*>(out);
-            const int k = ITEMS * h + i;
-            float v[8];
-            floats8(from_st, v);
-            if constexpr (DUAL) {  // (f is a multiple of 8)
-              float up[8];
-              floats8(from_st + 8, up);
-              if constexpr (EPI == ME_PART_DUAL) {
-                put8(reinterpret_cast<float*>(out), v);
-                put8(reinterpret_cast<float*>(out) + 8, up);
-              } else if constexpr (EPI == ME_SWIGLU) {
+              for (int j = 0; j < 8; ++j) v[j] *= sigmoid(v[j]) * up[j];
+              put8(to, v, 8, true);
+            } else {
+              const uint32_t d[8] = {now.v[2 * i].x, now.v[2 * i].y, now.v[2 * i].z, now.v[2 * i].w,
+                                     now.v[2 * i + 1].x, now.v[2 * i + 1].y, now.v[2 * i + 1].z, now.v[2 * i + 1].w};
+              float dg[8], du[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] *= sigmoid(v[j]) * up[j];
-                put8(to, v, 8, true);
+              for (int j = 0; j < 8; ++j) {
+                const float p = sigmoid(v[j]), act = v[j] * p, dh = __uint_as_float(d[j]);
+                du[j] = dh * act;
+                dg[j] = dh * up[j] * (p * (1.f + v[j] * (1.f - p)));
+                v[j] = act * up[j];
+              }
+              put8(to, dg, 8, true);
+              put8(to + A.f, du, 8, true);
+              put8(reinterpret_cast<__nv_bfloat16*>(A.h_out) + (row0 + c0 - team * MM_STEP + i * ITEM_ROWS) * A.f + m, v, 8, true);
+            }
+          } else if constexpr (EPI == ME_STORE_F32 || EPI == ME_PART) {
+            put8(reinterpret_cast<float*>(out), v);  // (rows of fp32 outputs have room for whole groups of 8)
+          } else {
+            if constexpr (EPI == ME_PRODUCT || EPI == ME_PRODUCT_GRAD) {
+              float add[8];
+              if (wide_in) {
+                Pack<__nv_bfloat16, 8> w;
+                w.r = now.v[i];
+                w.widen(add);
+              } else if (from) {
+                get8(reinterpret_cast<const __nv_bfloat16*>(from) + (row0 + c0 - team * MM_STEP + i * ITEM_ROWS) * A.rs + m, add, n);
+              }
+#pragma unroll
+              for (int j = 0; j < 8; ++j) v[j] = FP8 ? fmaf(v[j], now.scale[i] * scale[j], bias[j]) : v[j] + bias[j];
+              if constexpr (EPI == ME_PRODUCT) {
+                if (A.act != DEAMOE_SIGMA_NONE) {
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) v[j] = A.act == DEAMOE_SIGMA_SILU ? v[j] * sigmoid(v[j]) : sigma_f(DEAMOE_SIGMA_GELU, v[j]);
+                }
+                if (from) {
+#pragma unroll
+                  for (int j = 0; j < 8; ++j) v[j] += add[j];
+                }
               } else {
-                const uint32_t d[8] = {now.v[2 * k].x, now.v[2 * k].y, now.v[2 * k].z, now.v[2 * k].w,
-                                       now.v[2 * k + 1].x, now.v[2 * k + 1].y, now.v[2 * k + 1].z, now.v[2 * k + 1].w};
-                float dg[8], du[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                  const float p = sigmoid(v[j]), act = v[j] * p, dh = __uint_as_float(d[j]);
-                  du[j] = dh * act;
-                  dg[j] = dh * up[j] * (p * (1.f + v[j] * (1.f - p)));
-                  v[j] = act * up[j];
-                }
-                put8(to, dg, 8, true);
-                put8(to + A.f, du, 8, true);
-                put8(reinterpret_cast<__nv_bfloat16*>(A.h_out) + (row0 + c0 - team * MM_STEP + h * MM_COLS) * A.f + m, v, 8, true);
-              }
-            } else if constexpr (EPI == ME_STORE_F32 || EPI == ME_PART) {
-              put8(reinterpret_cast<float*>(out), v);  // (rows of fp32 outputs have room for whole groups of 8)
-            } else {
-              if constexpr (EPI == ME_PRODUCT || EPI == ME_PRODUCT_GRAD) {
-                float add[8];
-                if (wide_in) {
-                  Pack<__nv_bfloat16, 8> w;
-                  w.r = now.v[k];
-                  w.widen(add);
-                } else if (from) {
-                  get8(reinterpret_cast<const __nv_bfloat16*>(from) + (row0 + c0 - team * MM_STEP + h * MM_COLS + i * ITEM_ROWS) * A.rs + m, add, n);
-                }
-#pragma unroll
-                for (int j = 0; j < 8; ++j) v[j] = FP8 ? fmaf(v[j], now.scale[k] * scale[j], bias[j]) : v[j] + bias[j];
-                if constexpr (EPI == ME_PRODUCT) {
-                  if (A.act != DEAMOE_SIGMA_NONE) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = A.act == DEAMOE_SIGMA_SILU ? v[j] * sigmoid(v[j]) : sigma_f(DEAMOE_SIGMA_GELU, v[j]);
-                  }
-                  if (from) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] += add[j];
-                  }
-                } else {
-#pragma unroll
-                  for (int j = 0; j < 8; ++j) {
-                    v[j] = add[j] * act_grad(A.act, v[j]);
-                    sums[j] += v[j];
-                  }
+                  v[j] = add[j] * act_grad(A.act, v[j]);
+                  sums[j] += v[j];
                 }
               }
-              put8(to, v, n, A.wide);
             }
+            put8(to, v, n, A.wide);
           }
         }
-        out += 2 * ITEMS * (MM_TEAMS - 1) * out_step;
+        out += ITEMS * (MM_TEAMS - 1) * out_step;
         now = next;
+        __syncwarp();
       }
       if constexpr (EPI == ME_PRODUCT_GRAD) {
-        if (A.part) {  // 8 threads of a team hold sums of the same columns: added in their order (the first buffer is free again here)
+        if (A.part) {  // 8 lanes hold sums of the same columns: added in a fixed order
 #pragma unroll
-          for (int j = 0; j < 8; ++j) st[c * MM_PITCH + q * 8 + j] = sums[j];
-          team_sync(team);
-          float v = 0.f;
+          for (int o = 4; o < 32; o *= 2)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) v += st[i * MM_PITCH + me];
-          const int col = t.m0 + (int)rank * (M_STEP / 2) + me;
-          if (col < A.M) A.part[(int64_t)(MM_TEAMS * t.n_index + team) * A.M + col] = v;
-          team_sync(team);
+            for (int j = 0; j < 8; ++j) sums[j] += __shfl_xor_sync(0xffffffffu, sums[j], o);
+          if (c == 0)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              if (j < n) A.part[(int64_t)(MM_TEAMS * t.n_index + team) * A.M + m + j] = sums[j];
         }
       }
     }

@@ -13,7 +13,8 @@
 // shares B, a lone CTA with 128 x 256 would need half as much again.  Few rows a group: the matrix's bytes.
 //
 // Roles of a CTA (1 CTA per SM, clusters of 2, tiles dealt in a fixed order so that equal calls give equal bits):
-//   warps 0-7  epilogue, two teams that share a tile's columns: accumulator -> registers -> a small transposing buffer -> 16-byte rows, with the epilogue's arithmetic in fp32
+//   warps 0-7  epilogue, two teams that share a tile's columns: accumulator -> registers -> a warp's transposing buffer -> 16-byte
+//              pieces of rows, with the epilogue's arithmetic in fp32
 //   warps 8, 9 one thread each issues the TMA copies of A's / B's part of a chunk (128 bytes of k, 128-byte swizzle) into a ring of 5 to 9 stages
 //   warp  10   in the pair's first CTA one thread issues the MMAs for both
 //   warp  11   ragged contractions (weight gradients: k runs over a group's rows): clears the rows behind the group's end
