@@ -73,8 +73,8 @@ __device__ __forceinline__ unsigned long long now_ns() {
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
   return t;
 }
-__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  if (bar_try(bar, parity)) return true;
+// (Not inlined: each role has its waits, and a small product's time is to a good part that of fetching code.)
+__device__ __noinline__ bool bar_wait_longer(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
   const unsigned long long start = now_ns();
   for (unsigned it = 1;; ++it) {
     if (bar_try(bar, parity)) return true;
@@ -83,6 +83,9 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile
   }
   *abort_flag = 1;
   return false;
+}
+__device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
+  return bar_try(bar, parity) || bar_wait_longer(bar, parity, abort_flag);
 }
 // `bar` may lie in the pair's other CTA
 __device__ __forceinline__ void load_3d(uint32_t dst, const CUtensorMap* m, int x, int y, int z, uint32_t bar) {
@@ -148,7 +151,7 @@ struct Tile {
 __device__ __forceinline__ int tiles_along(int n, int widest) { return (n + widest - 1) / widest; }
 constexpr int MM_BAND = 8;  // tiles along N that are walked side by side: 74 pairs then share some 8 + 9 operand tiles in the L2
 
-template <bool RAGGED> __device__ __forceinline__ Tile find_tile(const MatmulArgs& A, const int* first_tile, const int* first_row, int t,
+template <bool RAGGED> __device__ __noinline__ Tile find_tile(const MatmulArgs& A, const int* first_tile, const int* first_row, int t,
                                                                  int m_step) {
   int lo = 0, hi = A.groups;  // the group whose range of tiles holds t
   while (hi - lo > 1) {
@@ -241,16 +244,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   const uint32_t first_full = in_first(full(0));
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(control + 4 * MM_STAGES + 4);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  int* warp_sums = reinterpret_cast<int*>(tmem_slot + 2);
-  uint32_t* info = tmem_slot + 2 + 16;  // [MM_STAGES][2]: a tile whose first chunk the stage holds
-  static_assert((4 * MM_STAGES + 4) * 8 + 8 + 16 * 4 + MM_STAGES * 8 <= MM_CONTROL, "control region");
+  uint32_t* info = tmem_slot + 2;  // [MM_STAGES][2]: a tile whose first chunk the stage holds
+  static_assert((4 * MM_STAGES + 4) * 8 + 8 + MM_STAGES * 8 <= MM_CONTROL, "control region");
   int* first_row = reinterpret_cast<int*>(smem + MM_RING + MM_STAGING + MM_CONTROL);
   int* first_tile = first_row + A.groups + 1;
 
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = cluster_rank(), stages = A.stages, stage_bytes = MM_OPERAND + A.b_bytes;
   if (tid == 0) {
-    for (int s = 0; s < MM_STAGES; ++s) {
+#pragma unroll 1
+    for (int s = 0; s < (int)stages; ++s) {
       bar_init(full(s), 1);
       bar_init(empty(s), 1);
       bar_init(tail(s), 1);
@@ -279,16 +282,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   const int limit = RAGGED ? A.K : A.N;
   if (A.off) {
     bool falls = false;
+#pragma unroll 1
     for (int e = tid; e <= A.groups; e += MM_THREADS) {
       const int o = A.off[e];
       if (e > 0) falls |= o < A.off[e - 1];
       first_row[e] = min(max(o, 0), limit);
     }
     falls = __syncthreads_or(falls);
-    for (int e = tid; e < A.groups; e += MM_THREADS)
-      first_tile[e] = falls ? 0 : mt * tiles_along(RAGGED ? A.N : first_row[e + 1] - first_row[e], A.tile_n);
-    __syncthreads();
-    block_exclusive_scan(first_tile, A.groups, warp_sums);
+    if (warp == 0) {
+      int before = 0;
+#pragma unroll 1
+      for (int e0 = 0; e0 < A.groups; e0 += 32) {
+        const int e = e0 + lane;
+        const int n = e < A.groups && !falls ? mt * tiles_along(RAGGED ? A.N : first_row[e + 1] - first_row[e], A.tile_n) : 0;
+        int sum = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const int y = __shfl_up_sync(0xffffffffu, sum, o);
+          if (lane >= o) sum += y;
+        }
+        if (e < A.groups) first_tile[e] = before + sum - n;
+        before += __shfl_sync(0xffffffffu, sum, 31);
+      }
+      if (lane == 0) first_tile[A.groups] = before;
+    }
   } else if (tid == 0) {
     first_row[0] = first_tile[0] = 0;
     first_row[1] = limit;
@@ -365,6 +382,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
       }
       __syncwarp();
       // the last commits must have arrived here before this CTA may end
+#pragma unroll 1
       for (uint32_t d = g > stages ? g - stages : 0; ok && d < g; ++d) ok = bar_wait(empty(d % stages), (d / stages) & 1u, abort_flag);
     }
   } else if (warp == MM_WARP_MMA) {
@@ -601,7 +619,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
                 }
               }
             }
-            put8(to, v, n, A.wide);
+            put8(to, v, EPI == ME_STORE ? 8 : n, EPI == ME_STORE || A.wide);  // (ME_STORE: whole groups of 8)
           }
         }
         out += ITEMS * (MM_TEAMS - 1) * out_step;
