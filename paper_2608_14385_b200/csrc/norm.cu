@@ -417,6 +417,31 @@ template <int N> static __device__ __forceinline__ void block_max_sums(float (&v
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) join(o);
 }
+// The same for a maximum m >= 0 and two sums over at most 16 warps, in a third of the instructions: non-negative floats order as
+// integers, for which a warp has a reduction of its own, and half a warp each adds one of the sums.  Fixed order; buf: 96 floats.
+static __device__ __forceinline__ void block_max_two_sums(float& m, float& a, float& b, float* buf) {
+  const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  const bool up = lane >= 16;
+  const float send = up ? a : b;
+  m = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(m)));
+  float v = (up ? b : a) + __shfl_xor_sync(0xffffffffu, send, 16);
+#pragma unroll
+  for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (warps > 1) {
+    if ((lane & 15) == 0) {
+      buf[(up ? 64 : 32) + w] = v;
+      if (lane == 0) buf[w] = m;
+    }
+    __syncthreads();
+    const int i = lane & 15;
+    m = __uint_as_float(__reduce_max_sync(0xffffffffu, i < warps ? __float_as_uint(buf[i]) : 0u));
+    v = i < warps ? buf[(up ? 64 : 32) + i] : 0.f;
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  }
+  a = __shfl_sync(0xffffffffu, v, 0);
+  b = __shfl_sync(0xffffffffu, v, 16);
+}
 // scale of a row into memory; returns what its values are multiplied by (to 2 units; 2^-8 keeps the reciprocal a normal number
 // up to the largest m)
 static __device__ __forceinline__ float row_scale(const NormArgs& A, int64_t t, float ss, float m) {
@@ -657,7 +682,7 @@ static __device__ __forceinline__ void store_lanes(void* p, int64_t stride, int6
 }
 
 // The 8-bit norms of many rows.  Done as k_codes_rows does them they are bound by instruction issue (41 instructions a value, 85 us
-// for 8192 x 7168 bf16; so 74).  So persistent blocks, whose threads hold their columns' gains (with the branch's factor and a gate per
+// for 8192 x 7168 bf16; so 72).  So persistent blocks, whose threads hold their columns' gains (with the branch's factor and a gate per
 // channel in them) as pairs of fp32 in registers and work on pairs; whose next rows are on their way meanwhile; and one reduction a row,
 // which brings the branch's sum of squares of the row to come with it.
 //   TWO: the sum of x and a branch; FULL: with a gate per value
@@ -754,7 +779,7 @@ __global__ void __launch_bounds__(MAXT, NV == 2 ? 2 : 1) k_codes_feed(NormArgs A
     if (post && t + gridDim.x < A.T) v[2] = squares(t + gridDim.x, F.next(at));
     F.request(ahead, at);  // the row has been read: its slot takes the one `stages` further
     at = F.next(at);
-    block_max_sums<3>(v, buf[flip]);
+    block_max_two_sums(v[0], v[1], v[2], buf[flip]);
     flip = 3 - flip;
     if (post) ry = rsqrtf(fmaf(v[2], per_value, A.eps));
     const P f2 = splat<P>(row_scale(A, t, v[1], v[0]));
@@ -1210,7 +1235,7 @@ template <typename T> static deamoe_status_t codes_t(const NormArgs& A, cudaStre
   };
   static std::atomic<uint64_t> done[5];
   // Sums of rows of 4097 to 7168 bf16 values: twice the threads with half the columns (two blocks of them fit an SM, and one reduction more a
-  // warp is little beside a long row: 8192 x 7168 75 us, 80 with four packs a thread).
+  // warp is little beside a long row: 8192 x 7168 bf16 75 us, 80 with four packs a thread, before the reduction got shorter).
   if (nin > 1 && packs > 512 && packs <= 896)
     return nin == 3 ? run(k_codes_feed<T, VE, 2, 448, true, true>, done[0], 2, 896) : run(k_codes_feed<T, VE, 2, 448, true, false>, done[1], 2, 896);
   return nin == 3 ? run(k_codes_feed<T, VE, NV, CODES_THREADS, true, true>, done[2], NV, CODES_THREADS)
