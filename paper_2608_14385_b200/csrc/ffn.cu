@@ -109,17 +109,17 @@ deamoe_status_t deamoe_ffn(void* cuda_stream, const void* x, int64_t x_stride, c
   cudaError_t e;
   if (up_splits > 1) {
     const JoinArgs j = joined(up, up_splits, true);
-    e = matmul_launch(MF_PART_SWIGLU, up, s, false);
+    e = matmul_launch(MF_PART_SWIGLU, up, s);
     if (e == cudaSuccess) e = join_launch(j, s);
   } else {
-    e = matmul_launch(MF_SWIGLU, up, s, false);
+    e = matmul_launch(MF_SWIGLU, up, s);
   }
   if (e == cudaSuccess && down_splits > 1) {
     const JoinArgs j = joined(down, down_splits, false);
-    e = matmul_launch(MF_PART, down, s, true);
+    e = matmul_launch(MF_PART, down, s);
     if (e == cudaSuccess) e = join_launch(j, s);
   } else if (e == cudaSuccess) {
-    e = matmul_launch(MF_STORE, down, s, true);
+    e = matmul_launch(MF_STORE, down, s);
   }
   if (e == cudaSuccess) return DEAMOE_OK;
   cudaGetLastError();
@@ -170,9 +170,9 @@ deamoe_status_t deamoe_ffn_backward(void* cuda_stream, const void* x, int64_t x_
       !map_rows(&e.maps.a, hh, 2, ffn, n_rows, ffn, 1, ffn, 64) ||
       !map_b_rows_inner(&e, dout, hidden, n_rows, dout_stride))
     return DEAMOE_ERR_CUDA;
-  if (matmul_launch(MF_F32_TRANSPOSED, a, s, false) == cudaSuccess && matmul_launch(MF_SWIGLU_GRAD, b, s, true) == cudaSuccess &&
-      matmul_launch(MF_STORE_TRANSPOSED, c, s, true) == cudaSuccess && matmul_launch(MF_WEIGHT_GRAD, d, s, true) == cudaSuccess &&
-      matmul_launch(MF_WEIGHT_GRAD, e, s, true) == cudaSuccess)
+  if (matmul_launch(MF_F32_TRANSPOSED, a, s) == cudaSuccess && matmul_launch(MF_SWIGLU_GRAD, b, s) == cudaSuccess &&
+      matmul_launch(MF_STORE_TRANSPOSED, c, s) == cudaSuccess && matmul_launch(MF_WEIGHT_GRAD, d, s) == cudaSuccess &&
+      matmul_launch(MF_WEIGHT_GRAD, e, s) == cudaSuccess)
     return DEAMOE_OK;
   cudaGetLastError();
   return DEAMOE_ERR_CUDA;

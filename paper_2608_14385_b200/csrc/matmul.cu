@@ -272,9 +272,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
-  // A kernel behind another one of its call waits for it here, but for two kinds.  The gradient of gate and up needs the one
-  // before it in its epilogue alone.  A.late: it needs only what was done before that one's own wait, which all its CTAs have
-  // passed by now, and waits at its end, so that the stream's order holds for what comes after.
+  // Launched early behind whatever is before it in the stream, a kernel waits for that here, but for two kinds, which follow another
+  // one of their call.  The gradient of gate and up needs that one in its epilogue alone.  A.late: it needs only what was
+  // done before that one's own wait, which all its CTAs have passed by now, and waits at its end, so that the stream's order
+  // holds for what comes after.
   if (EPI != ME_SWIGLU_GRAD && !A.late) pdl_wait();
   pdl_trigger();
   // groups' rows (offsets outside the range count as its ends) and their tiles; offsets that decrease: no tile at all
@@ -687,7 +688,7 @@ bool encode(CUtensorMap* m, const void* p, int esize, int rank, const cuuint64_t
 }
 
 template <int EPI, bool AT, bool BT, bool FP8, bool RAGGED>
-cudaError_t launch(const MatmulCall& c, cudaStream_t s, bool chained) {
+cudaError_t launch(const MatmulCall& c, cudaStream_t s) {
   static std::atomic<uint64_t> done{0};
   auto kernel = k_matmul<EPI, AT, BT, FP8, RAGGED>;
   int dev = 0;
@@ -704,9 +705,7 @@ cudaError_t launch(const MatmulCall& c, cudaStream_t s, bool chained) {
   const int64_t nt = RAGGED ? (int64_t)a.groups * ((a.N + a.tile_n - 1) / a.tile_n) : a.N / a.tile_n + (a.groups < a.N ? a.groups : a.N);
   const int64_t most = mt * nt * a.splits;
   const dim3 grid(2 * (unsigned)(most < MM_PAIRS ? most : MM_PAIRS));
-  if (chained) return launch_pdl(kernel, grid, dim3(MM_THREADS), MM_SMEM, s, c.args, c.maps);
-  kernel<<<grid, MM_THREADS, MM_SMEM, s>>>(c.args, c.maps);
-  return cudaGetLastError();
+  return launch_pdl(kernel, grid, dim3(MM_THREADS), MM_SMEM, s, c.args, c.maps);
 }
 
 }  // namespace
@@ -780,20 +779,20 @@ int matmul_splits(int64_t tiles, int64_t chunks, int64_t rows) {
   return best;
 }
 
-cudaError_t matmul_launch(MatmulForm form, const MatmulCall& c, cudaStream_t s, bool chained) {
+cudaError_t matmul_launch(MatmulForm form, const MatmulCall& c, cudaStream_t s) {
   switch (form) {
-    case MF_SWIGLU: return launch<ME_SWIGLU, false, false, false, false>(c, s, chained);
-    case MF_STORE: return launch<ME_STORE, false, false, false, false>(c, s, chained);
-    case MF_STORE_TRANSPOSED: return launch<ME_STORE, true, false, false, false>(c, s, chained);
-    case MF_F32_TRANSPOSED: return launch<ME_STORE_F32, true, false, false, false>(c, s, chained);
-    case MF_SWIGLU_GRAD: return launch<ME_SWIGLU_GRAD, false, false, false, false>(c, s, chained);
-    case MF_WEIGHT_GRAD: return launch<ME_STORE, true, true, false, true>(c, s, chained);
-    case MF_PRODUCT: return launch<ME_PRODUCT, false, false, false, false>(c, s, chained);
-    case MF_PRODUCT_E4M3: return launch<ME_PRODUCT, false, false, true, false>(c, s, chained);
-    case MF_PART: return launch<ME_PART, false, false, false, false>(c, s, chained);
-    case MF_PART_E4M3: return launch<ME_PART, false, false, true, false>(c, s, chained);
-    case MF_PART_SWIGLU: return launch<ME_PART_DUAL, false, false, false, false>(c, s, chained);
-    case MF_PRODUCT_GRAD: return launch<ME_PRODUCT_GRAD, false, false, false, false>(c, s, chained);
+    case MF_SWIGLU: return launch<ME_SWIGLU, false, false, false, false>(c, s);
+    case MF_STORE: return launch<ME_STORE, false, false, false, false>(c, s);
+    case MF_STORE_TRANSPOSED: return launch<ME_STORE, true, false, false, false>(c, s);
+    case MF_F32_TRANSPOSED: return launch<ME_STORE_F32, true, false, false, false>(c, s);
+    case MF_SWIGLU_GRAD: return launch<ME_SWIGLU_GRAD, false, false, false, false>(c, s);
+    case MF_WEIGHT_GRAD: return launch<ME_STORE, true, true, false, true>(c, s);
+    case MF_PRODUCT: return launch<ME_PRODUCT, false, false, false, false>(c, s);
+    case MF_PRODUCT_E4M3: return launch<ME_PRODUCT, false, false, true, false>(c, s);
+    case MF_PART: return launch<ME_PART, false, false, false, false>(c, s);
+    case MF_PART_E4M3: return launch<ME_PART, false, false, true, false>(c, s);
+    case MF_PART_SWIGLU: return launch<ME_PART_DUAL, false, false, false, false>(c, s);
+    case MF_PRODUCT_GRAD: return launch<ME_PRODUCT_GRAD, false, false, false, false>(c, s);
   }
   return cudaErrorInvalidValue;
 }

@@ -69,7 +69,6 @@ struct MatmulMaps {
   CUtensorMap a, b;
 };
 
-// Launch one product.  kind: epilogue; a_rows_inner / b_rows_inner: A / B stored with its rows as the inner axis; fp8: e4m3.
 struct MatmulCall {
   MatmulArgs args;
   MatmulMaps maps;
@@ -78,7 +77,7 @@ enum MatmulForm : int {
   MF_SWIGLU, MF_STORE, MF_STORE_TRANSPOSED, MF_F32_TRANSPOSED, MF_SWIGLU_GRAD, MF_WEIGHT_GRAD, MF_PRODUCT, MF_PRODUCT_E4M3, MF_PRODUCT_GRAD,
   MF_PART, MF_PART_E4M3, MF_PART_SWIGLU
 };
-cudaError_t matmul_launch(MatmulForm form, const MatmulCall& c, cudaStream_t s, bool chained);
+cudaError_t matmul_launch(MatmulForm form, const MatmulCall& c, cudaStream_t s);
 
 // Tensor maps.  A matrix of `rows` rows of `cols` values per group, row stride and group stride in values.
 bool map_rows(CUtensorMap* m, const void* p, int esize, int64_t cols, int64_t rows, int64_t stride, int64_t groups, int64_t group_stride,

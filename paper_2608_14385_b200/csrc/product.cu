@@ -129,8 +129,8 @@ deamoe_status_t deamoe_product(void* cuda_stream, int32_t dtype, const void* x, 
     j.out = reinterpret_cast<__nv_bfloat16*>(out); j.os = out_stride; j.x_scale = x_scale; j.w_scale = weight_scale; j.bias = bias;
     j.residual = residual; j.rs = residual_stride; j.bias_f32 = c.args.bias_f32; j.act = act; j.wide = c.args.wide;
     c.args.splits = splits; c.args.out = workspace; c.args.os = (n_out + 7) / 8 * 8; c.args.out_group = c.args.os * n_token;
-    if (matmul_launch(e4m3 ? MF_PART_E4M3 : MF_PART, c, s, false) == cudaSuccess && join_launch(j, s) == cudaSuccess) return DEAMOE_OK;
-  } else if (matmul_launch(e4m3 ? MF_PRODUCT_E4M3 : MF_PRODUCT, c, s, false) == cudaSuccess) {
+    if (matmul_launch(e4m3 ? MF_PART_E4M3 : MF_PART, c, s) == cudaSuccess && join_launch(j, s) == cudaSuccess) return DEAMOE_OK;
+  } else if (matmul_launch(e4m3 ? MF_PRODUCT_E4M3 : MF_PRODUCT, c, s) == cudaSuccess) {
     return DEAMOE_OK;
   }
   cudaGetLastError();
@@ -192,7 +192,7 @@ deamoe_status_t deamoe_product_backward(void* cuda_stream, int32_t dtype, const 
   int parts = 0;
   if (!plain) {
     parts = MM_PARTS * ((n_token + a.args.tile_n - 1) / a.args.tile_n);
-    ok = matmul_launch(MF_PRODUCT_GRAD, a, s, false) == cudaSuccess;
+    ok = matmul_launch(MF_PRODUCT_GRAD, a, s) == cudaSuccess;
   } else if (dbias) {
     parts = (n_token + BIAS_ROWS - 1) / BIAS_ROWS;
     k_bias_sums<<<dim3(parts, (n_out + 255) / 256), 256, 0, s>>>(reinterpret_cast<const __nv_bfloat16*>(dout), dout_stride, n_token, n_out, part);
@@ -200,7 +200,7 @@ deamoe_status_t deamoe_product_backward(void* cuda_stream, int32_t dtype, const 
   }
   if (ok && dbias)
     ok = launch_pdl(k_add_parts, dim3((n_out + 31) / 32), dim3(256), 0, s, (const float*)part, parts, (int)n_out, dbias) == cudaSuccess;
-  ok = ok && matmul_launch(MF_STORE_TRANSPOSED, b, s, !plain || dbias) == cudaSuccess && matmul_launch(MF_WEIGHT_GRAD, c, s, true) == cudaSuccess;
+  ok = ok && matmul_launch(MF_STORE_TRANSPOSED, b, s) == cudaSuccess && matmul_launch(MF_WEIGHT_GRAD, c, s) == cudaSuccess;
   if (ok) return DEAMOE_OK;
   cudaGetLastError();
   return DEAMOE_ERR_CUDA;

@@ -121,3 +121,33 @@ def test_training_step_captured_while_an_eager_graph_of_the_same_leaves_lives():
     assert all(torch.equal(a, b) for a, b in zip(got, want))
     alive.sum().backward()
     assert torch.isfinite(leaf.grad).all()
+
+
+def test_what_the_kernel_before_wrote_is_seen_and_what_comes_after_sees_all():
+    """The calls' kernels are launched before the kernel in front of them has ended: inputs and weights that it writes must be
+    read after it, and the kernel behind must find every output."""
+    T = 300
+    sets = [{"x": _gauss((T, H), i), "w": _gauss((H, H), 10 + i, H ** -0.5), "wgu": _gauss((E, 2 * F, H), 20 + i, H ** -0.5),
+             "wd": _gauss((E, H, F), 30 + i, F ** -0.5), "dy": _gauss((T, H), 40 + i)} for i in range(2)]
+    off = torch.tensor([0, 9, 9, 60, 61, 100, 130, 131, 140, 200, 260, 290, 300], dtype=torch.int32, device=DEV)
+    big = torch.empty(1 << 24, device=DEV)
+
+    def calls(s):
+        return [binding.product(s["x"][:5], s["w"]), binding.product(s["x"], s["w"], act=binding.SIGMA_GELU), binding.product(s["x"][:40], s["w"]),
+                binding.ffn(s["x"][:7], s["wgu"][:1], s["wd"][:1]), binding.ffn(s["x"], s["wgu"], s["wd"], expert_off=off),
+                *binding.ffn_backward(s["x"], s["wgu"], s["wd"], s["dy"], expert_off=off),
+                *binding.product_backward(s["x"], s["w"], s["dy"], act=binding.SIGMA_SILU)[:2]]
+
+    want = [[t.clone() for t in calls(s)] for s in sets]
+    now = {n: torch.empty_like(t) for n, t in sets[0].items()}
+    wrong = []
+    for i in range(40):
+        s = sets[i % 2]
+        big.fill_(float(i))                                       # keeps the device busy until the copies' turn comes
+        for n, t in now.items():
+            t.copy_(s[n])
+        wrong.append([(a != b).sum() for a, b in zip(calls(now), want[i % 2])])
+        now["w"].zero_()                                          # one call right behind the kernels that write its weights
+        now["w"].copy_(s["w"])
+        wrong.append([(binding.product(now["x"][:5], now["w"]) != want[i % 2][0]).sum()])
+    assert all(int(n) == 0 for w in wrong for n in w)
