@@ -18,6 +18,7 @@ constexpr int BIAS_ROWS = 64;  // rows of dout that one block adds up
 // Column sums of bf16 rows: a block adds BIAS_ROWS rows of 256 columns (8 a thread, 8 threads along the rows), part[block row][column].
 __global__ void __launch_bounds__(256) k_bias_sums(const __nv_bfloat16* __restrict__ d, int64_t stride, int T, int n, float* __restrict__ part) {
   __shared__ float buf[8][256];
+  pdl_trigger();
   const int q = threadIdx.x & 31, r = threadIdx.x >> 5;
   const int c = blockIdx.y * 256 + q * 8;
   const int64_t t0 = (int64_t)blockIdx.x * BIAS_ROWS;
@@ -39,19 +40,18 @@ __global__ void __launch_bounds__(256) k_bias_sums(const __nv_bfloat16* __restri
   float v = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) v += buf[i][threadIdx.x];
-  pdl_trigger();
   const int col = blockIdx.y * 256 + threadIdx.x;
   if (col < n) part[(int64_t)blockIdx.x * n + col] = v;
 }
-// Partial sums added in their order: 32 columns a block, 8 threads a column.
-__global__ void __launch_bounds__(256) k_add_parts(const float* part, int parts, int n, float* __restrict__ out) {
+// Partial sums added in their order: 32 columns a block, 8 threads a column.  late: as in matmul.cu.
+__global__ void __launch_bounds__(256) k_add_parts(const float* part, int parts, int n, float* __restrict__ out, int late) {
   __shared__ float buf[8][32];
-  pdl_wait();
-  pdl_trigger();
   const int q = threadIdx.x & 31, r = threadIdx.x >> 5, c = blockIdx.x * 32 + q;
+  if (!late) pdl_wait();
+  pdl_trigger();
   float s = 0.f;
   if (c < n)
-    for (int i = r; i < parts; i += 8) s += part[(int64_t)i * n + c];
+    for (int i = r; i < parts; i += 8) s += __ldcg(part + (int64_t)i * n + c);
   buf[r][q] = s;
   __syncthreads();
   if (r == 0 && c < n) {
@@ -59,6 +59,7 @@ __global__ void __launch_bounds__(256) k_add_parts(const float* part, int parts,
     for (int i = 1; i < 8; ++i) s += buf[i][q];
     out[c] = s;
   }
+  if (late) pdl_wait();
 }
 
 static uint64_t ceil256(uint64_t v) { return (v + 255) / 256 * 256; }
@@ -187,20 +188,26 @@ deamoe_status_t deamoe_product_backward(void* cuda_stream, int32_t dtype, const 
       !map_rows(&c.maps.a, x, 2, n_in, n_token, x_stride, 1, x_stride, 64) ||
       !map_b_rows_inner(&c, g, n_out, n_token, gs))
     return DEAMOE_ERR_CUDA;
-  c.args.late = 1;  // it needs dz as b does, and b waits for it
+  // What depends on nothing but what is already there runs beside the rest.  With an activation: dz, dx, the sums of the bias
+  // gradient's parts and dW, of which the last two need dz as dx does, which waits for it.  Without one: the parts of the bias
+  // gradient, dx and dW beside them, and their sums at the end.
+  c.args.late = 1;
+  b.args.late = plain && dbias;
+  const int parts = plain ? (n_token + BIAS_ROWS - 1) / BIAS_ROWS : MM_PARTS * ((n_token + a.args.tile_n - 1) / a.args.tile_n);
+  auto add_parts = [&](int late) {
+    return launch_pdl(k_add_parts, dim3((n_out + 31) / 32), dim3(256), 0, s, (const float*)part, parts, (int)n_out, dbias, late) == cudaSuccess;
+  };
   bool ok = true;
-  int parts = 0;
   if (!plain) {
-    parts = MM_PARTS * ((n_token + a.args.tile_n - 1) / a.args.tile_n);
     ok = matmul_launch(MF_PRODUCT_GRAD, a, s) == cudaSuccess;
   } else if (dbias) {
-    parts = (n_token + BIAS_ROWS - 1) / BIAS_ROWS;
     k_bias_sums<<<dim3(parts, (n_out + 255) / 256), 256, 0, s>>>(reinterpret_cast<const __nv_bfloat16*>(dout), dout_stride, n_token, n_out, part);
     ok = cudaGetLastError() == cudaSuccess;
   }
-  if (ok && dbias)
-    ok = launch_pdl(k_add_parts, dim3((n_out + 31) / 32), dim3(256), 0, s, (const float*)part, parts, (int)n_out, dbias) == cudaSuccess;
-  ok = ok && matmul_launch(MF_STORE_TRANSPOSED, b, s) == cudaSuccess && matmul_launch(MF_WEIGHT_GRAD, c, s) == cudaSuccess;
+  ok = ok && matmul_launch(MF_STORE_TRANSPOSED, b, s) == cudaSuccess;
+  if (ok && dbias && !plain) ok = add_parts(1);
+  ok = ok && matmul_launch(MF_WEIGHT_GRAD, c, s) == cudaSuccess;
+  if (ok && dbias && plain) ok = add_parts(0);
   if (ok) return DEAMOE_OK;
   cudaGetLastError();
   return DEAMOE_ERR_CUDA;
