@@ -156,19 +156,19 @@ deamoe_status_t deamoe_ffn_backward(void* cuda_stream, const void* x, int64_t x_
   b.args.out = dgu; b.args.os = 2 * (int64_t)ffn; b.args.dh = dh; b.args.h_out = hh;
   MatmulCall c = ffn_call(S, hidden, 2 * ffn);  // dx = [dg du] [Wg; Wu]
   c.args.out = dx; c.args.os = dx_stride;
-  MatmulCall d = ffn_call(S, hidden, n_rows);  // d[Wg; Wu] = [dg du]^T x
-  d.args.tile_n = MM_N; d.args.N = 2 * ffn; d.args.out = dw_gate_up; d.args.os = hidden; d.args.out_group = 2 * wd_one;
-  MatmulCall e = ffn_call(S, ffn, n_rows);  // dWd = dy^T h
-  e.args.tile_n = MM_N; e.args.N = hidden; e.args.out = dw_down; e.args.os = ffn; e.args.out_group = wd_one;
+  MatmulCall d = ffn_call(S, 2 * ffn, n_rows);  // d[Wg; Wu] = [dg du]^T x
+  d.args.tile_n = MM_N; d.args.N = hidden;
+  MatmulCall e = ffn_call(S, hidden, n_rows);  // dWd = dy^T h
+  e.args.tile_n = MM_N; e.args.N = ffn;
   d.args.late = e.args.late = 1;  // they need b's results as c does, and c waits for those
   if (!map_rows(&a.maps.a, w_down, 2, ffn, hidden, ffn, n_expert, wd_one, 64) || !map_b(&a, dout, 2, hidden, n_rows, dout_stride) ||
       !map_gate_up(&b.maps.a, w_gate_up, hidden, ffn, n_expert) || !map_b(&b, x, 2, hidden, n_rows, x_stride) ||
       !map_rows(&c.maps.a, w_gate_up, 2, hidden, 2 * (int64_t)ffn, hidden, n_expert, 2 * wd_one, 64) ||
       !map_b(&c, dgu, 2, 2 * (int64_t)ffn, n_rows, 2 * (int64_t)ffn) ||
-      !map_rows(&d.maps.a, x, 2, hidden, n_rows, x_stride, 1, x_stride, 64) ||
-      !map_b_rows_inner(&d, dgu, 2 * (int64_t)ffn, n_rows, 2 * (int64_t)ffn) ||
-      !map_rows(&e.maps.a, hh, 2, ffn, n_rows, ffn, 1, ffn, 64) ||
-      !map_b_rows_inner(&e, dout, hidden, n_rows, dout_stride))
+      !map_rows(&d.maps.a, dgu, 2, 2 * (int64_t)ffn, n_rows, 2 * (int64_t)ffn, 1, 2 * (int64_t)ffn, 64) ||
+      !map_b_rows_inner(&d, x, hidden, n_rows, x_stride) || !map_out(&d, dw_gate_up, hidden, 2 * (int64_t)ffn, hidden, n_expert, 2 * wd_one) ||
+      !map_rows(&e.maps.a, dout, 2, hidden, n_rows, dout_stride, 1, dout_stride, 64) || !map_b_rows_inner(&e, hh, ffn, n_rows, ffn) ||
+      !map_out(&e, dw_down, ffn, hidden, ffn, n_expert, wd_one))
     return DEAMOE_ERR_CUDA;
   if (matmul_launch(MF_F32_TRANSPOSED, a, s) == cudaSuccess && matmul_launch(MF_SWIGLU_GRAD, b, s) == cudaSuccess &&
       matmul_launch(MF_STORE_TRANSPOSED, c, s) == cudaSuccess && matmul_launch(MF_WEIGHT_GRAD, d, s) == cudaSuccess &&

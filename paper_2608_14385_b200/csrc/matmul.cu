@@ -106,6 +106,11 @@ __device__ __forceinline__ bool elected() {
   asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(p));
   return p != 0;
 }
+// 32 x 32 bf16 values of a warp's buffer (64-byte swizzle) to columns x .., rows y .. of group z
+__device__ __forceinline__ void store_3d(const CUtensorMap* m, uint32_t src, int x, int y, int z) {
+  asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];"
+               ::"l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(src) : "memory");
+}
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 // Shared-memory operand with 128-byte swizzle.  k inner: 8 rows of 128 bytes are a block of 1024 bytes, `sbo` apart.
@@ -146,8 +151,8 @@ struct Tile {
   int row0, rows;  // the group's rows (ragged contraction)
   int n_index;   // index of the tile along N in its group
 };
-// Tiles of a group: its columns are dealt evenly in units of 16, so that one a little above a multiple of the widest tile has no
-// sliver.
+// Tiles of a group: its columns are dealt evenly in units of 16 (weight gradients: 32, an epilogue's step), so that one a little above
+// a multiple of the widest tile has no sliver.
 __device__ __forceinline__ int tiles_along(int n, int widest) { return (n + widest - 1) / widest; }
 constexpr int MM_BAND = 8;  // tiles along N that are walked side by side: 74 pairs then share some 8 + 9 operand tiles in the L2
 
@@ -169,13 +174,14 @@ template <bool RAGGED> __device__ __noinline__ Tile find_tile(const MatmulArgs& 
   const int band = r / (MM_BAND * mt), rest = r - band * MM_BAND * mt;
   const int width = min(MM_BAND, nt - band * MM_BAND);
   const int mi = rest / width, ni = band * MM_BAND + rest - mi * width;
-  const int units = (cols + 15) / 16, base = units / nt, more = units - base * nt;  // the first `more` tiles have one more
+  constexpr int UNIT = RAGGED ? 32 : 16;
+  const int units = (cols + UNIT - 1) / UNIT, base = units / nt, more = units - base * nt;  // the first `more` tiles have one more
   const int u0 = ni * base + min(ni, more);
-  o.n = (base + (ni < more)) * 16;
+  o.n = (base + (ni < more)) * UNIT;
   o.m0 = mi * m_step;
   o.n_index = ni;
-  o.valid = min(o.n, cols - u0 * 16);
-  o.n0 = u0 * 16 + (RAGGED ? 0 : o.row0);
+  o.valid = min(o.n, cols - u0 * UNIT);
+  o.n0 = u0 * UNIT + (RAGGED ? 0 : o.row0);
   return o;
 }
 
@@ -268,6 +274,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   }
   if (tid == MM_WARP_A * 32) prefetch_map(&maps.a);
   if (tid == MM_WARP_B * 32) prefetch_map(&maps.b);
+  if (EPI == ME_STORE_ROWS && tid == 0) prefetch_map(&maps.out);
   if (warp == MM_WARP_MMA) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(smem_u32(tmem_slot)) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -475,6 +482,66 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     // ============================================================ epilogue
     // A warp by itself: its 32 lanes of the accumulator are 32 columns of the output (DUAL: 16 features), which it turns through its own
     // buffer, 32 rows at a time.  The warps of a team share a step's rows; the teams take steps in turn.
+    if constexpr (EPI == ME_STORE_ROWS) {
+      // The accumulator's lanes are rows of the output and its columns the row's: nothing to turn.  A warp packs its 32 x 32 block
+      // into one of two swizzled buffers and TMA takes it from there, cut at the matrix's edges.
+      uint32_t a = 0;
+      const uint32_t bufs = smem_u32(staging) + warp * (MM_STEP * MM_PITCH * 4);
+      const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+      const int team = warp >> 2;
+      uint32_t used = 0;
+      for (int it = pair; it < tiles; it += pairs) {
+        const Tile t = tile_at(it);
+        const bool none = t.rows == 0;  // a group without rows: zeros
+        const uint32_t buf = a & 1u;
+        if (!none) {
+          const int w = lane == 0 ? bar_wait(acc_full(buf), (a >> 1) & 1u, abort_flag) : 0;
+          if (__shfl_sync(0xffffffffu, w, 0) == 0) break;
+          tc_after();
+          ++a;
+        }
+        auto release = [&] {  // this warp has read its part of the accumulator
+          tc_before();
+          __syncwarp();
+          if (lane == 0) bar_arrive_cluster(in_first(acc_empty(buf)));
+        };
+        if (!none && team * MM_STEP >= t.n) release();
+        const int row = t.m0 + (int)rank * (MM_M / 2) + (warp & 3) * 32;
+        for (int c0 = team * MM_STEP; c0 < t.n; c0 += MM_TEAMS * MM_STEP) {
+          uint32_t r[MM_STEP];
+          if (none) {
+#pragma unroll
+            for (int i = 0; i < MM_STEP; ++i) r[i] = 0;
+          } else {
+            tmem_load(lane_base + buf * MM_N + c0, r);
+            tmem_load_wait();
+            if (c0 + MM_TEAMS * MM_STEP >= t.n) release();
+          }
+          const uint32_t at = bufs + (used & 1u) * 2048;
+          ++used;
+          asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");  // (lane 0's: the buffer's last store has read it)
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {  // 16 bytes of the row of 64; the swizzle: piece ^ (row / 2) mod 4
+            uint32_t p[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(r[8 * i + 2 * j]), __uint_as_float(r[8 * i + 2 * j + 1]));
+              p[j] = *reinterpret_cast<const uint32_t*>(&v);
+            }
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};"
+                         ::"r"(at + lane * 64 + ((i ^ (lane >> 1 & 3)) << 4)), "r"(p[0]), "r"(p[1]), "r"(p[2]), "r"(p[3]) : "memory");
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          __syncwarp();
+          if (lane == 0) {
+            if (row < A.M) store_3d(&maps.out, at, t.n0 + c0, row, t.group);
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");  // (an empty one counts the step all the same)
+          }
+        }
+      }
+      asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    } else {
     if (EPI == ME_SWIGLU_GRAD) pdl_wait();
     uint32_t a = 0;
     bool ok = true;
@@ -494,7 +561,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
       const int m = t.m0 + (int)rank * (M_STEP / 2) + (warp & 3) * (M_STEP / 8) + q * 8, n = min(8, A.M - m);
       const int valid = n > 0 ? t.valid : 0;
       const int64_t row0 = t.n0 + team * MM_STEP + c;
-      char* out = reinterpret_cast<char*>(A.out) + ((RAGGED ? (int64_t)t.group * A.out_group : SPLIT ? (int64_t)(it % A.splits) * A.out_group : 0) +
+      char* out = reinterpret_cast<char*>(A.out) + ((SPLIT ? (int64_t)(it % A.splits) * A.out_group : 0) +
                                                            row0 * A.os + (EPI == ME_PART_DUAL ? 2 : 1) * m) * OUT_BYTES;
       // rows of dh, residual or dout of this thread's items, and x's scales
       const void* const from = EPI == ME_SWIGLU_GRAD ? (const void*)A.dh : EPI == ME_PRODUCT ? A.residual : EPI == ME_PRODUCT_GRAD ? A.dout : nullptr;
@@ -640,6 +707,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
         }
       }
     }
+    }
   }
 
   // common end, also after a wait that has expired
@@ -678,12 +746,13 @@ EncodeFn encode_fn() {
   }
   return f;
 }
-bool encode(CUtensorMap* m, const void* p, int esize, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
+bool encode(CUtensorMap* m, const void* p, int esize, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
+            CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
   EncodeFn f = encode_fn();
   if (!f) return false;
   const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
   return f(m, esize == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(p), dims, strides, box,
-           ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+           ones, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -722,6 +791,12 @@ bool map_gate_up(CUtensorMap* m, const void* p, int64_t cols, int64_t f, int64_t
   const cuuint64_t strides[4] = {(cuuint64_t)cols * 2, (cuuint64_t)(f * cols) * 2, (cuuint64_t)cols * 16, (cuuint64_t)(f * cols) * 4};
   const cuuint32_t box[5] = {64, 8, 2, 8, 1};
   return encode(m, p, 2, 5, dims, strides, box);
+}
+bool map_out(MatmulCall* c, const void* p, int64_t cols, int64_t rows, int64_t stride, int64_t groups, int64_t group_stride) {
+  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)groups};
+  const cuuint64_t strides[2] = {(cuuint64_t)stride * 2, (cuuint64_t)group_stride * 2};
+  const cuuint32_t box[3] = {32, 32, 1};
+  return encode(&c->maps.out, p, 2, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_64B);
 }
 bool map_b(MatmulCall* c, const void* p, int esize, int64_t cols, int64_t rows, int64_t stride) {
   // the lowest box (16, 32, 64 or 128 rows) that holds a CTA's half of the widest tile: one copy a chunk, and what the box does not
@@ -786,7 +861,7 @@ cudaError_t matmul_launch(MatmulForm form, const MatmulCall& c, cudaStream_t s) 
     case MF_STORE_TRANSPOSED: return launch<ME_STORE, true, false, false, false>(c, s);
     case MF_F32_TRANSPOSED: return launch<ME_STORE_F32, true, false, false, false>(c, s);
     case MF_SWIGLU_GRAD: return launch<ME_SWIGLU_GRAD, false, false, false, false>(c, s);
-    case MF_WEIGHT_GRAD: return launch<ME_STORE, true, true, false, true>(c, s);
+    case MF_WEIGHT_GRAD: return launch<ME_STORE_ROWS, true, true, false, true>(c, s);
     case MF_PRODUCT: return launch<ME_PRODUCT, false, false, false, false>(c, s);
     case MF_PRODUCT_E4M3: return launch<ME_PRODUCT, false, false, true, false>(c, s);
     case MF_PART: return launch<ME_PART, false, false, false, false>(c, s);

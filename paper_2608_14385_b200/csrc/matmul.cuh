@@ -1,11 +1,10 @@
 // Products on the fifth-generation tensor cores for the operators around a layer (ffn.cu, product.cu): one persistent
 // kernel over 256 x 256 tiles by pairs of CTAs, its operand orders, row groups and epilogues as template parameters.
 //
-//   D[m, n] = sum_k A[m, k] B[n, k]      stored at out[n][m]
+//   D[m, n] = sum_k A[m, k] B[n, k]      stored at out[n][m], weight gradients at out[m][n]
 //
-// A is the operand whose rows become the outputs' columns (a weight matrix, or the inputs in a weight gradient), B the one
-// whose rows become the outputs' rows (tokens; the outputs' gradients in a weight gradient).  With the tokens on the
-// N side a group of any size is a tile of its own width (16 to 256 columns in steps of 16), from a decode step's few rows
+// A is the operand whose rows become the outputs' columns (a weight matrix), B the one whose rows become the outputs' rows (tokens).
+// With the tokens on the N side a group of any size is a tile of its own width (16 to 256 columns in steps of 16), from a decode step's few rows
 // an expert to a prompt's thousands, and the matrix side is always full.
 //
 // What bounds it.  A bf16 MMA of 256 x 256 x 16 by a pair keeps both SMs' tensor cores busy for 128 cycles; each CTA's
@@ -37,7 +36,8 @@ enum MatmulEpilogue : int {
   ME_PRODUCT = 4,      // scales, bias, activation, residual
   ME_PRODUCT_GRAD = 5, // dout times the activation's derivative, and its sums over a tile's rows
   ME_PART = 6,         // fp32 sums of a part of k, [split][row][M rounded up to 8], for join.cu
-  ME_PART_DUAL = 7     // ... of alternating gate and up, [split][row][2 M]
+  ME_PART_DUAL = 7,    // ... of alternating gate and up, [split][row][2 M]
+  ME_STORE_ROWS = 8    // bf16, stored at out[m][n] (weight gradients)
 };
 
 struct MatmulArgs {
@@ -53,7 +53,7 @@ struct MatmulArgs {
   // epilogue
   void* out;
   int64_t os;            // values between out's rows
-  int64_t out_group;     // values between groups of outputs (weight gradients), or between splits
+  int64_t out_group;     // values between splits
   int wide;              // out's rows take 16-byte stores
   const float* dh;       // [N, f]                       (ME_SWIGLU_GRAD)
   void* h_out;           // [N, f] bf16
@@ -66,7 +66,7 @@ struct MatmulArgs {
 };
 
 struct MatmulMaps {
-  CUtensorMap a, b;
+  CUtensorMap a, b, out;  // (out: ME_STORE_ROWS)
 };
 
 struct MatmulCall {
@@ -89,6 +89,9 @@ bool map_b_rows_inner(MatmulCall* c, const void* p, int64_t cols, int64_t rows, 
 
 // Tile width of `n` rows in one group for `m_tiles` tiles of A's rows; whole: the product may be split along k.  See matmul.cu
 int matmul_tile_n(int64_t n, int64_t m_tiles, bool whole);
+
+// ... of the output of a weight gradient: 32 x 32 values
+bool map_out(MatmulCall* c, const void* p, int64_t cols, int64_t rows, int64_t stride, int64_t groups, int64_t group_stride);
 
 // Widest tile for `rows` rows in `groups` groups of unknown sizes: four times the average, so that most groups are one tile and a
 // stage of the ring holds no more of B than they need, and a 32nd of all rows at least, should they come to one group

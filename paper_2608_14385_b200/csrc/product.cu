@@ -178,15 +178,14 @@ deamoe_status_t deamoe_product_backward(void* cuda_stream, int32_t dtype, const 
   const void* g = plain ? dout : dz;  // gradient of z as an operand
   const int64_t gs = plain ? dout_stride : n_out;
   MatmulCall a = product_call(n_out, n_in, n_token, 64, false), b = product_call(n_in, n_out, n_token, 64, false),
-             c = product_call(n_in, n_token, n_out, 64, false);
+             c = product_call(n_out, n_token, n_in, 64, false);
   a.args.out = dz; a.args.os = n_out; a.args.wide = 1; a.args.bias = bias; a.args.bias_f32 = bias_dtype == DEAMOE_F32; a.args.act = act;
   a.args.dout = dout; a.args.rs = dout_stride; a.args.wide_in = 1; a.args.part = dbias ? part : nullptr;
   b.args.out = dx; b.args.os = dx_stride; b.args.wide = 1;
-  c.args.out = dweight; c.args.os = n_in; c.args.wide = 1;
   if ((!plain && (!map_rows(&a.maps.a, weight, 2, n_in, n_out, n_in, 1, n_in, 128) || !map_b(&a, x, 2, n_in, n_token, x_stride))) ||
       !map_rows(&b.maps.a, weight, 2, n_in, n_out, n_in, 1, n_in, 64) || !map_b(&b, g, 2, n_out, n_token, gs) ||
-      !map_rows(&c.maps.a, x, 2, n_in, n_token, x_stride, 1, x_stride, 64) ||
-      !map_b_rows_inner(&c, g, n_out, n_token, gs))
+      !map_rows(&c.maps.a, g, 2, n_out, n_token, gs, 1, gs, 64) || !map_b_rows_inner(&c, x, n_in, n_token, x_stride) ||
+      !map_out(&c, dweight, n_in, n_out, n_in, 1, (int64_t)n_out * n_in))
     return DEAMOE_ERR_CUDA;
   // What depends on nothing but what is already there runs beside the rest.  With an activation: dz, dx, the sums of the bias
   // gradient's parts and dW, of which the last two need dz as dx does, which waits for it.  Without one: the parts of the bias
