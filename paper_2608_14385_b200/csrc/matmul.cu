@@ -595,8 +595,35 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
           if (A.bias && j < n) bias[j] = gain(A.bias, A.bias_f32, m + j);
         if constexpr (EPI == ME_PRODUCT && FP8) scale[j] = j < n ? A.w_scale[m + j] : 0.f;
       }
+      float lane_bias = 0.f, lane_scale = 0.f;
+      const bool odd_rows = EPI == ME_PRODUCT && (!A.wide || (from && !A.wide_in));
+      if (odd_rows) {
+        const int col = t.m0 + (int)rank * (M_STEP / 2) + (warp & 3) * 32 + lane;
+        if (A.bias && col < A.M) lane_bias = gain(A.bias, A.bias_f32, col);
+        if (FP8 && col < A.M) lane_scale = A.w_scale[col];
+      }
+      // The same where a lane keeps its column: 16 rows of it, from row c0 of the tile on, a register each (packing them would wait for
+      // them).  `now` holds a step's first half, `next` its second.
+      auto ask_odd = [&](int c0, Ahead& w) {
+        const int col = t.m0 + (int)rank * (M_STEP / 2) + (warp & 3) * 32 + lane;
+        if (!from || col >= A.M) return;
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(from) + (int64_t)(t.n0 + c0) * A.rs + col;
+        uint32_t v[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i, p += A.rs)
+          if (c0 + i < t.valid) v[i] = *p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w.v[i] = make_uint4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+      };
+      auto row_scales = [&](int c0) { return FP8 && c0 + lane < t.valid ? A.x_scale[t.n0 + c0 + lane] : 0.f; };
+      float scale_now = 0.f, scale_next = 0.f;
       Ahead now, next;
-      ask(team * MM_STEP + c, now);
+      if (EPI == ME_PRODUCT && odd_rows) {
+        ask_odd(team * MM_STEP, now);
+        scale_now = row_scales(team * MM_STEP);
+      } else {
+        ask(team * MM_STEP + c, now);
+      }
       if (!none) {
         const int w = lane == 0 ? bar_wait(acc_full(buf), (a >> 1) & 1u, abort_flag) : 0;
         ok = __shfl_sync(0xffffffffu, w, 0) != 0;
@@ -617,13 +644,52 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
           for (int i = 0; i < MM_STEP; ++i) r[i] = 0;
         } else {
           tmem_load(lane_base + buf * MM_N + c0, r);
-          ask(c0 + MM_TEAMS * MM_STEP + c, next);  // (past the tile's end: nothing)
+          if (EPI == ME_PRODUCT && odd_rows) {
+            ask_odd(c0 + 16, next);
+            scale_next = row_scales(c0 + MM_TEAMS * MM_STEP);  // (past the tile's end: nothing)
+          } else {
+            ask(c0 + MM_TEAMS * MM_STEP + c, next);
+          }
           tmem_load_wait();
           if (c0 + MM_TEAMS * MM_STEP >= t.n) release();
         }
 #pragma unroll
         for (int i = 0; i < MM_STEP; ++i) st[i * MM_PITCH + lane] = __uint_as_float(r[i]);
         __syncwarp();
+        if constexpr (EPI == ME_PRODUCT) {
+          if (odd_rows) {
+            // Rows off 16-byte boundaries (an odd number of outputs): a lane keeps its column, and a row's 32 values go as 64 bytes of
+            // 32 lanes (eight values a lane, one by one, are 32 pieces a store: 7288 x 880 x 6971 278 us, 92 so; with GeLU and residual 329, 233).
+            const int col = t.m0 + (int)rank * (M_STEP / 2) + (warp & 3) * 32 + lane, rows = col < A.M ? min(MM_STEP, t.valid - c0) : 0;
+            if (FP8 || A.bias || A.act != DEAMOE_SIGMA_NONE) {
+#pragma unroll 4
+              for (int i = 0; i < MM_STEP; ++i) {
+                float v = st[i * MM_PITCH + lane];
+                v = FP8 ? fmaf(v, __shfl_sync(0xffffffffu, scale_now, i) * lane_scale, lane_bias) : v + lane_bias;
+                if (A.act != DEAMOE_SIGMA_NONE) v = A.act == DEAMOE_SIGMA_SILU ? v * sigmoid(v) : sigma_f(DEAMOE_SIGMA_GELU, v);
+                st[i * MM_PITCH + lane] = v;
+              }
+            }
+            __nv_bfloat16* to = reinterpret_cast<__nv_bfloat16*>(A.out) + (int64_t)(t.n0 + c0) * A.os + col;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              const Ahead& w = h ? next : now;
+              const uint32_t add[16] = {w.v[0].x, w.v[0].y, w.v[0].z, w.v[0].w, w.v[1].x, w.v[1].y, w.v[1].z, w.v[1].w,
+                                        w.v[2].x, w.v[2].y, w.v[2].z, w.v[2].w, w.v[3].x, w.v[3].y, w.v[3].z, w.v[3].w};
+#pragma unroll
+              for (int i = 0; i < 16; ++i, to += A.os)
+                if (16 * h + i < rows) {
+                  float v = st[(16 * h + i) * MM_PITCH + lane];
+                  if (from) v += __uint_as_float(add[i] << 16);
+                  *to = __float2bfloat16_rn(v);
+                }
+              if (h == 0) ask_odd(c0 + MM_TEAMS * MM_STEP, now);
+            }
+            scale_now = scale_next;
+            __syncwarp();
+            continue;
+          }
+        }
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i, out += out_step) {
           if (c0 + i * ITEM_ROWS + c >= valid) continue;
