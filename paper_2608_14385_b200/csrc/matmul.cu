@@ -14,6 +14,7 @@ constexpr int MM_TEAMS = 2;                    // epilogue teams of 4 warps (a w
 constexpr int MM_WARP_A = 4 * MM_TEAMS, MM_WARP_B = MM_WARP_A + 1, MM_WARP_MMA = MM_WARP_A + 2, MM_WARP_CLEAR = MM_WARP_A + 3;
 constexpr int MM_THREADS = (MM_WARP_CLEAR + 1) * 32;
 constexpr int MM_STEP = 32;                    // accumulator columns of an epilogue step
+constexpr int MM_ROW_STEP = 64;                // ... of weight gradients, whose rows are lanes: 128 bytes of a row
 constexpr int MM_PITCH = 32 + 4;               // floats of a row of a warp's transposing buffer
 constexpr int MM_STAGING = MM_TEAMS * 4 * MM_STEP * MM_PITCH * 4;
 constexpr int MM_CONTROL = 512;
@@ -106,7 +107,7 @@ __device__ __forceinline__ bool elected() {
   asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(p));
   return p != 0;
 }
-// 32 x 32 bf16 values of a warp's buffer (64-byte swizzle) to columns x .., rows y .. of group z
+// 32 rows of 64 bf16 values of a warp's buffer (128-byte swizzle) to columns x .., rows y .. of group z
 __device__ __forceinline__ void store_3d(const CUtensorMap* m, uint32_t src, int x, int y, int z) {
   asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];"
                ::"l"(reinterpret_cast<uint64_t>(m)), "r"(x), "r"(y), "r"(z), "r"(src) : "memory");
@@ -151,7 +152,7 @@ struct Tile {
   int row0, rows;  // the group's rows (ragged contraction)
   int n_index;   // index of the tile along N in its group
 };
-// Tiles of a group: its columns are dealt evenly in units of 16 (weight gradients: 32, an epilogue's step), so that one a little above
+// Tiles of a group: its columns are dealt evenly in units of 16 (weight gradients: 64, an epilogue's step), so that one a little above
 // a multiple of the widest tile has no sliver.
 __device__ __forceinline__ int tiles_along(int n, int widest) { return (n + widest - 1) / widest; }
 constexpr int MM_BAND = 8;  // tiles along N that are walked side by side: 74 pairs then share some 8 + 9 operand tiles in the L2
@@ -174,7 +175,7 @@ template <bool RAGGED> __device__ __noinline__ Tile find_tile(const MatmulArgs& 
   const int band = r / (MM_BAND * mt), rest = r - band * MM_BAND * mt;
   const int width = min(MM_BAND, nt - band * MM_BAND);
   const int mi = rest / width, ni = band * MM_BAND + rest - mi * width;
-  constexpr int UNIT = RAGGED ? 32 : 16;
+  constexpr int UNIT = RAGGED ? MM_ROW_STEP : 16;
   const int units = (cols + UNIT - 1) / UNIT, base = units / nt, more = units - base * nt;  // the first `more` tiles have one more
   const int u0 = ni * base + min(ni, more);
   o.n = (base + (ni < more)) * UNIT;
@@ -483,13 +484,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     // A warp by itself: its 32 lanes of the accumulator are 32 columns of the output (DUAL: 16 features), which it turns through its own
     // buffer, 32 rows at a time.  The warps of a team share a step's rows; the teams take steps in turn.
     if constexpr (EPI == ME_STORE_ROWS) {
-      // The accumulator's lanes are rows of the output and its columns the row's: nothing to turn.  A warp packs its 32 x 32 block
-      // into one of two swizzled buffers and TMA takes it from there, cut at the matrix's edges.
+      // The accumulator's lanes are rows of the output and its columns the row's: nothing to turn.  A warp packs 64 columns of its 32
+      // rows into its swizzled buffer and TMA takes them from there, whole lines of 128 bytes, cut at the matrix's edges.
       uint32_t a = 0;
-      const uint32_t bufs = smem_u32(staging) + warp * (MM_STEP * MM_PITCH * 4);
+      const uint32_t at = smem_u32(staging) + warp * 4096;
+      static_assert(MM_TEAMS * 4 * 4096 <= MM_STAGING, "buffers of 32 rows of 128 bytes");
       const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
       const int team = warp >> 2;
-      uint32_t used = 0;
       for (int it = pair; it < tiles; it += pairs) {
         const Tile t = tile_at(it);
         const bool none = t.rows == 0;  // a group without rows: zeros
@@ -505,38 +506,38 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
           __syncwarp();
           if (lane == 0) bar_arrive_cluster(in_first(acc_empty(buf)));
         };
-        if (!none && team * MM_STEP >= t.n) release();
+        if (!none && team * MM_ROW_STEP >= t.n) release();
         const int row = t.m0 + (int)rank * (MM_M / 2) + (warp & 3) * 32;
-        for (int c0 = team * MM_STEP; c0 < t.n; c0 += MM_TEAMS * MM_STEP) {
-          uint32_t r[MM_STEP];
+        for (int c0 = team * MM_ROW_STEP; c0 < t.n; c0 += MM_TEAMS * MM_ROW_STEP) {
+          uint32_t r[2][MM_STEP];
           if (none) {
 #pragma unroll
-            for (int i = 0; i < MM_STEP; ++i) r[i] = 0;
+            for (int i = 0; i < MM_STEP; ++i) r[0][i] = r[1][i] = 0;
           } else {
-            tmem_load(lane_base + buf * MM_N + c0, r);
+            tmem_load(lane_base + buf * MM_N + c0, r[0]);
+            tmem_load(lane_base + buf * MM_N + c0 + MM_STEP, r[1]);
             tmem_load_wait();
-            if (c0 + MM_TEAMS * MM_STEP >= t.n) release();
+            if (c0 + MM_TEAMS * MM_ROW_STEP >= t.n) release();
           }
-          const uint32_t at = bufs + (used & 1u) * 2048;
-          ++used;
-          asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");  // (lane 0's: the buffer's last store has read it)
+          asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");  // (lane 0's: its last store has read the buffer)
           __syncwarp();
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {  // 16 bytes of the row of 64; the swizzle: piece ^ (row / 2) mod 4
+          for (int i = 0; i < 8; ++i) {  // 16 bytes of the row's 128; the swizzle: piece ^ row mod 8
             uint32_t p[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-              const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(r[8 * i + 2 * j]), __uint_as_float(r[8 * i + 2 * j + 1]));
+              const int k = 8 * (i & 3) + 2 * j;
+              const __nv_bfloat162 v = __floats2bfloat162_rn(__uint_as_float(r[i >> 2][k]), __uint_as_float(r[i >> 2][k + 1]));
               p[j] = *reinterpret_cast<const uint32_t*>(&v);
             }
             asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};"
-                         ::"r"(at + lane * 64 + ((i ^ (lane >> 1 & 3)) << 4)), "r"(p[0]), "r"(p[1]), "r"(p[2]), "r"(p[3]) : "memory");
+                         ::"r"(at + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(p[0]), "r"(p[1]), "r"(p[2]), "r"(p[3]) : "memory");
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           __syncwarp();
           if (lane == 0) {
             if (row < A.M) store_3d(&maps.out, at, t.n0 + c0, row, t.group);
-            asm volatile("cp.async.bulk.commit_group;" ::: "memory");  // (an empty one counts the step all the same)
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
           }
         }
       }
@@ -812,13 +813,12 @@ EncodeFn encode_fn() {
   }
   return f;
 }
-bool encode(CUtensorMap* m, const void* p, int esize, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box,
-            CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B) {
+bool encode(CUtensorMap* m, const void* p, int esize, int rank, const cuuint64_t* dims, const cuuint64_t* strides, const cuuint32_t* box) {
   EncodeFn f = encode_fn();
   if (!f) return false;
   const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
   return f(m, esize == 1 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, rank, const_cast<void*>(p), dims, strides, box,
-           ones, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+           ones, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -861,8 +861,8 @@ bool map_gate_up(CUtensorMap* m, const void* p, int64_t cols, int64_t f, int64_t
 bool map_out(MatmulCall* c, const void* p, int64_t cols, int64_t rows, int64_t stride, int64_t groups, int64_t group_stride) {
   const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)groups};
   const cuuint64_t strides[2] = {(cuuint64_t)stride * 2, (cuuint64_t)group_stride * 2};
-  const cuuint32_t box[3] = {32, 32, 1};
-  return encode(&c->maps.out, p, 2, 3, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_64B);
+  const cuuint32_t box[3] = {64, 32, 1};
+  return encode(&c->maps.out, p, 2, 3, dims, strides, box);
 }
 bool map_b(MatmulCall* c, const void* p, int esize, int64_t cols, int64_t rows, int64_t stride) {
   // the lowest box (16, 32, 64 or 128 rows) that holds a CTA's half of the widest tile: one copy a chunk, and what the box does not

@@ -90,7 +90,7 @@ bool map_b_rows_inner(MatmulCall* c, const void* p, int64_t cols, int64_t rows, 
 // Tile width of `n` rows in one group for `m_tiles` tiles of A's rows; whole: the product may be split along k.  See matmul.cu
 int matmul_tile_n(int64_t n, int64_t m_tiles, bool whole);
 
-// ... of the output of a weight gradient: 32 x 32 values
+// ... of the output of a weight gradient: 32 rows of 64 values
 bool map_out(MatmulCall* c, const void* p, int64_t cols, int64_t rows, int64_t stride, int64_t groups, int64_t group_stride);
 
 // Widest tile for `rows` rows in `groups` groups of unknown sizes: four times the average, so that most groups are one tile and a
