@@ -36,7 +36,7 @@ static bool ffn_thin(int E, int R) { return R <= THIN_ROWS && (E <= 8 || R <= 8)
 static int ffn_splits(int E, int R, int64_t M, int64_t K) {
   const int groups = E < R ? E : R;
   const int64_t tiles = (M + MM_M - 1) / MM_M * (R / matmul_group_tile_n(R, groups) + groups);  // no more than that, whatever the offsets
-  return matmul_splits(tiles, (K + 63) / 64, R);
+  return matmul_splits(tiles, (K + 63) / 64, R, M);
 }
 static uint64_t ffn_parts_bytes(int E, int R, int h, int f) {
   const int a = ffn_splits(E, R, 2 * (int64_t)f, h), b = ffn_splits(E, R, h, f);

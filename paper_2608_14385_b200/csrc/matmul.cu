@@ -904,14 +904,15 @@ int matmul_tile_n(int64_t n, int64_t m_tiles, bool whole) {
   }
   return best;
 }
-// A decode step's product has fewer tiles than the device has pairs (7168 outputs: 28): its tiles are dealt along k, as evenly over
-// the pairs as some number of parts allows, where that saves a quarter of the chunks that a pair walks.  The parts' sums
-// (4 bytes a value and part, written and read once, mostly in the L2) stay below the matrix's bytes times four.
-int matmul_splits(int64_t tiles, int64_t chunks, int64_t rows) {
+// A decode step's product has fewer tiles than the device has pairs (7168 outputs: 28), and so has one of few outputs: its tiles are
+// dealt along k, as evenly over the pairs as some number of parts allows.  In us: a chunk takes a pair some 0.3, a part's sums (4
+// bytes a value) are written and read at some 4 TB/s, mostly in the L2, and joining them takes 3 more.
+int matmul_splits(int64_t tiles, int64_t chunks, int64_t rows, int64_t outputs) {
   int best = 1;
-  int64_t least = (tiles + MM_PAIRS - 1) / MM_PAIRS * (chunks + 2) * 3 / 4;
-  for (int s = 2; s <= 16 && s * 4 <= chunks && s * rows <= chunks * 16; ++s) {
-    const int64_t cost = (tiles * s + MM_PAIRS - 1) / MM_PAIRS * ((chunks + s - 1) / s + 2);
+  double least = 0.9 * 0.3 * (double)((tiles + MM_PAIRS - 1) / MM_PAIRS) * (double)(chunks + 2);
+  for (int s = 2; s <= 16 && s * 4 <= chunks; ++s) {
+    const double cost = 0.3 * (double)((tiles * s + MM_PAIRS - 1) / MM_PAIRS) * (double)((chunks + s - 1) / s + 2) + 3 +
+                        (double)s * (double)rows * (double)outputs * 8 / 4e6;
     if (cost < least) {
       least = cost;
       best = s;

@@ -96,8 +96,8 @@ bool map_out(MatmulCall* c, const void* p, int64_t cols, int64_t rows, int64_t s
 // Widest tile for `rows` rows in `groups` groups of unknown sizes: four times the average, so that most groups are one tile and a
 // stage of the ring holds no more of B than they need, and a 32nd of all rows at least, should they come to one group
 int matmul_group_tile_n(int64_t rows, int64_t groups);
-// Parts of k for a product of at most `tiles` tiles, `chunks` chunks of k and `rows` rows in all (1: not split): see matmul.cu
-int matmul_splits(int64_t tiles, int64_t chunks, int64_t rows);
+// Parts of k for a product of at most `tiles` tiles, `chunks` chunks of k and rows x outputs sums (1: not split): see matmul.cu
+int matmul_splits(int64_t tiles, int64_t chunks, int64_t rows, int64_t outputs);
 
 // Adds the splits' sums in their order and applies the epilogue: [splits][n_rows][M rounded up to 8] (dual: [2 M]) -> out.  (join.cu)
 struct JoinArgs {

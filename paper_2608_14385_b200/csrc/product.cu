@@ -73,7 +73,7 @@ static MatmulCall product_call(int M, int K, int N, int chunk, bool whole) {
 }
 
 static int product_splits(const MatmulArgs& a) {
-  return matmul_splits((int64_t)((a.M + MM_M - 1) / MM_M) * ((a.N + a.tile_n - 1) / a.tile_n), (a.K + a.chunk - 1) / a.chunk, a.N);
+  return matmul_splits((int64_t)((a.M + MM_M - 1) / MM_M) * ((a.N + a.tile_n - 1) / a.tile_n), (a.K + a.chunk - 1) / a.chunk, a.N, a.M);
 }
 
 static deamoe_status_t check_product(int dtype, int T, int n_out, int n_in, int act, int bias_dtype, const void* bias) {
