@@ -23,7 +23,7 @@ constexpr int MM_CONTROL = 512;
 constexpr uint32_t TILE_END = 1u << 16;
 constexpr int TILE_STEPS = 20;
 // A chunk to be cleared goes into the ring so many chunks before the tile's end, but is taken last: the MMA role need not wait for
-// the clearing (weight gradients of 16384 rows over 16 experts 861 -> 721 us).
+// the clearing.
 constexpr int MM_TAIL_LEAD = 2;
 __device__ __forceinline__ uint32_t tail_place(uint32_t chunks) { return chunks > MM_TAIL_LEAD ? chunks - 1 - MM_TAIL_LEAD : 0; }
 constexpr int MM_TABLE = (DEAMOE_MAX_EXPERTS + 1) * 8 + 8;  // groups' first tile and first row
@@ -906,7 +906,7 @@ int matmul_tile_n(int64_t n, int64_t m_tiles, bool whole) {
 }
 // A decode step's product has fewer tiles than the device has pairs (7168 outputs: 28), and so has one of few outputs: its tiles are
 // dealt along k, as evenly over the pairs as some number of parts allows.  In us: a chunk takes a pair some 0.3, a part's sums (4
-// bytes a value) are written and read at some 4 TB/s, mostly in the L2, and joining them takes 3 more.
+// bytes a value) are written and read at what is taken as 4 TB/s, mostly in the L2, and joining them takes 3 more.
 int matmul_splits(int64_t tiles, int64_t chunks, int64_t rows, int64_t outputs) {
   int best = 1;
   double least = 0.9 * 0.3 * (double)((tiles + MM_PAIRS - 1) / MM_PAIRS) * (double)(chunks + 2);
