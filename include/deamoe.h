@@ -455,7 +455,7 @@ deamoe_status_t deamoe_quant_product(void *cuda_stream, int32_t dtype, const uin
  *
  * codes: [n_token, hidden] bytes with a row stride; scale: [n_token] fp32.  u is not rounded in between.  A row whose
  * max |s * weight| (s: what is normed) is below 2^-110, a row of zeros among them, has a scale as if it were 2^-110.  A value
- * that is not finite gives its row a scale that is not.
+ * or a gain that is not finite (a NaN that a gain of 0 makes of an infinity too) gives its row a scale that is not.
  */
 deamoe_status_t deamoe_norm_quant(void *cuda_stream, int32_t dtype, const void *x, int64_t x_stride, int32_t n_token,
                                   int32_t hidden, int32_t normalise, int32_t weight_dtype, const void *weight, float eps,

@@ -392,14 +392,22 @@ template <typename T, int VE, int NV, int MAXT> __global__ void __launch_bounds_
 //
 // With m = max |s w| the code is e4m3(s w * 448 / m) and the scale m / rms(s) / 448: the sum of squares and the maximum
 // come from one reduction, and the codes do not wait for the root.  Rows whose m is below 2^-110 (a row of zeros among
-// them) take 2^-110 for it.  The row stays in registers; HBM bounds it: 5 bytes a value without a sum, 7 with one (bf16).
+// them) take 2^-110 for it.  A NaN stays the maximum, so that the row's scale (and all its codes) are NaN even where the sum of squares
+// is not used or does not see it (a gain of NaN).  The row stays in registers; HBM bounds it: 5 bytes a value without a sum, 7 with
+// one (bf16).
 constexpr int CODES_THREADS = 512;  // of an SM, in the persistent form: 128 registers each
 constexpr float E4M3_MAX = 448.f, QUANT_LEAST = 0x1p-110f;
 
+// the larger one, or NaN if either is (with its sign bit clear)
+static __device__ __forceinline__ float max_or_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
 // the maximum of v[0] and the sums of the others over a block, to every thread; buf: 32 N floats, as for block_sums
 template <int N> static __device__ __forceinline__ void block_max_sums(float (&v)[N], float* buf) {
   auto join = [&](int o) {
-    v[0] = fmaxf(v[0], __shfl_xor_sync(0xffffffffu, v[0], o));
+    v[0] = max_or_nan(v[0], __shfl_xor_sync(0xffffffffu, v[0], o));
 #pragma unroll
     for (int i = 1; i < N; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
   };
@@ -418,7 +426,8 @@ template <int N> static __device__ __forceinline__ void block_max_sums(float (&v
   for (int o = 16; o > 0; o >>= 1) join(o);
 }
 // The same for a maximum m >= 0 and two sums over at most 16 warps, in a third of the instructions: non-negative floats order as
-// integers, for which a warp has a reduction of its own, and half a warp each adds one of the sums.  Fixed order; buf: 96 floats.
+// integers (NaN of a clear sign bit above infinity), for which a warp has a reduction of its own, and half a warp each adds one of the
+// sums.  Fixed order; buf: 96 floats.
 static __device__ __forceinline__ void block_max_two_sums(float& m, float& a, float& b, float* buf) {
   const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, warps = blockDim.x >> 5;
   const bool up = lane >= 16;
@@ -445,7 +454,7 @@ static __device__ __forceinline__ void block_max_two_sums(float& m, float& a, fl
 // scale of a row into memory; returns what its values are multiplied by (to 2 units; 2^-8 keeps the reciprocal a normal number
 // up to the largest m)
 static __device__ __forceinline__ float row_scale(const NormArgs& A, int64_t t, float ss, float m) {
-  m = fmaxf(m, QUANT_LEAST);
+  m = max_or_nan(m, QUANT_LEAST);
   if (threadIdx.x == 0) A.scale[t] = (A.next_norm ? inv_rms(ss, A.h, A.next_eps) : 1.f) * m * (1.f / E4M3_MAX);
   return (E4M3_MAX * 0x1p-8f) * __fdividef(1.f, m * 0x1p-8f);
 }
@@ -484,7 +493,7 @@ template <typename T> __global__ void __launch_bounds__(ANY_THREADS) k_codes_any
   float v[2] = {0.f, 0.f};
   for (int i = threadIdx.x; i < A.h; i += ANY_THREADS) {
     const float s = sum(i);
-    v[0] = fmaxf(v[0], fabsf(s * load_gain(A.wn, A.wdt, i)));
+    v[0] = max_or_nan(v[0], fabsf(s * load_gain(A.wn, A.wdt, i)));
     v[1] = fmaf(s, s, v[1]);
   }
   block_max_sums<2>(v, buf[1]);
@@ -543,7 +552,7 @@ template <typename T, int VE, int NV, int MAXT> __global__ void __launch_bounds_
     for (int j = 0; j < VE; ++j) {
       v[1] = fmaf(s[n][j], s[n][j], v[1]);
       s[n][j] *= w[j];
-      v[0] = fmaxf(v[0], fabsf(s[n][j]));
+      v[0] = max_or_nan(v[0], fabsf(s[n][j]));
     }
   }
   block_max_sums<2>(v, buf[1]);
@@ -772,7 +781,7 @@ __global__ void __launch_bounds__(MAXT, NV == 2 ? 2 : 1) k_codes_feed(NormArgs A
       for (int j = 0; j < N; ++j) {
         sq = fma_(s[n][j], s[n][j], sq);
         s[n][j] = mul_(s[n][j], wn[n][j]);
-        m = fmaxf(fmaxf(m, fabsf(low(s[n][j]))), fabsf(high(s[n][j])));
+        m = max_or_nan(max_or_nan(m, fabsf(low(s[n][j]))), fabsf(high(s[n][j])));
       }
     }
     float v[3] = {m, total(sq), 0.f};

@@ -183,3 +183,60 @@ def test_wrapper_refuses_what_does_not_fit():
     for call in bad:
         with pytest.raises(binding.DeaMoEError):
             call()
+
+
+# a block a row, value by value, and persistent blocks: without a sum, with one (four and two packs a thread), rows too wide for them
+NOT_FINITE = [(1, 64), (5, 1024), (7, 1031), (400, 1031), (330, 2048), (310, 4096), (310, 7168), (300, 8192), (300, 16392)]
+
+
+def _same(got, want, rows):
+    return all(torch.equal(a[rows].view(torch.uint8), b[rows].view(torch.uint8)) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("normalise", [True, False])
+@pytest.mark.parametrize("T,h", NOT_FINITE)
+def test_a_value_that_is_not_finite_shows_in_its_rows_scale(T, h, normalise, dtype):
+    nan, inf = float("nan"), float("inf")
+    x, w = _gauss((T, h), 1, dtype), _gauss((h,), 2, F32, 0.2, 1.0)
+    w[h // 3] = 0.0
+    clean = binding.norm_quant(x, w, 1e-6, normalise=normalise)
+    assert torch.isfinite(clean[1]).all()
+    for column, value in ((h - 1, nan), (0, inf), (h // 2, -inf), (h // 3, inf), (h // 3, nan)):  # under the gain of 0: 0 times it
+        bad = x.clone()
+        bad[T // 2, column] = value
+        got = binding.norm_quant(bad, w, 1e-6, normalise=normalise)
+        rest = [t for t in range(T) if t != T // 2]
+        assert not torch.isfinite(got[1][T // 2]) and _same(got, clean, rest), (column, value)
+    x[T // 2] = nan
+    assert torch.isnan(binding.norm_quant(x, None, 1e-6, normalise=normalise)[1][T // 2])
+    w[h // 2] = nan
+    assert not torch.isfinite(binding.norm_quant(clean[0].to(dtype), w, 1e-6, normalise=normalise)[1]).any()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("kind", [binding.GATE_NONE, binding.GATE_TOKEN, binding.GATE_FULL])
+@pytest.mark.parametrize("normalise", [True, False])
+@pytest.mark.parametrize("T,h", NOT_FINITE)
+def test_a_value_that_is_not_finite_shows_in_the_scale_after_the_residual(T, h, normalise, kind, dtype):
+    nan, inf = float("nan"), float("inf")
+    x, y = _gauss((T, h), 1, dtype), _gauss((T, h), 2, dtype)
+    wn = _gauss((h,), 3, dtype, 0.2, 1.0)
+    wn[h // 3] = 0.0
+    gate = [None, None, _gauss((T,), 4, dtype), _gauss((T, h), 4, dtype)][kind]
+
+    def call(x, y, gate, wn):
+        return binding.norm_residual_quant(x, y, None, 1e-6, gate=gate, gate_kind=kind if kind else None, normalise=normalise, next_weight=wn)[1:]
+
+    clean, rest = call(x, y, gate, wn), [t for t in range(T) if t != T // 2]
+    assert torch.isfinite(clean[1]).all()
+    for which, column, value in ((0, h - 1, nan), (0, h // 3, inf), (1, 0, nan), (1, h // 2, inf), (2, 0, nan)):
+        args = [x.clone(), y.clone(), gate if gate is None else gate.clone()]
+        if args[which] is None:
+            continue
+        at = (T // 2,) if args[which].dim() == 1 else (T // 2, column)
+        args[which][at] = value
+        got = call(*args, wn)
+        assert not torch.isfinite(got[1][T // 2]) and _same(got, clean, rest), (which, column, value)
+    wn[0] = nan
+    assert not torch.isfinite(call(x, y, gate, wn)[1]).any()
