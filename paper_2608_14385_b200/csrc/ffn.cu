@@ -43,6 +43,16 @@ static uint64_t ffn_parts_bytes(int E, int R, int h, int f) {
   const uint64_t up = a > 1 ? (uint64_t)a * R * 2 * f * 4 : 0, down = b > 1 ? (uint64_t)b * R * h * 4 : 0;
   return up > down ? up : down;
 }
+// Sums of contractions of more than one stretch: the forward products run one after the other.
+static uint64_t ffn_sums(int E, int R, int h, int f) {
+  const uint64_t up = matmul_sums(h, 64, ffn_splits(E, R, 2 * (int64_t)f, h)), down = matmul_sums(f, 64, ffn_splits(E, R, h, f));
+  return up > down ? up : down;
+}
+// Backward, sums for each of the three that can overlap (dx and both weight gradients).
+static uint64_t ffn_backward_sums(int R, int h, int f) {
+  const int64_t k = h > 2 * (int64_t)f ? h : 2 * (int64_t)f;
+  return matmul_sums(k > R ? k : R, 64, 1);
+}
 
 static deamoe_status_t check_ffn(const void* x, int64_t xs, const void* wgu, const void* wd, const int32_t* off, int E, int R, int h, int f) {
   if (E <= 0 || h <= 0 || f <= 0 || (!off && E != 1)) return DEAMOE_ERR_INVALID_ARG;
@@ -66,8 +76,9 @@ extern "C" {
 uint64_t deamoe_ffn_workspace(int32_t n_expert, int32_t n_rows, int32_t hidden, int32_t ffn, int32_t backward) {
   if (n_expert <= 0 || n_rows <= 0 || hidden <= 0 || ffn <= 0) return 0;
   const uint64_t v = (uint64_t)n_rows * ffn;
-  if (backward) return ceil256(4 * v) + ceil256(4 * v) + ceil256(2 * v);
-  return ceil256(2 * v) + (ffn_thin(n_expert, n_rows) ? 0 : ffn_parts_bytes(n_expert, n_rows, hidden, ffn));
+  if (backward) return ceil256(4 * v) + ceil256(4 * v) + ceil256(2 * v) + 3 * ffn_backward_sums(n_rows, hidden, ffn);
+  if (ffn_thin(n_expert, n_rows)) return ceil256(2 * v);
+  return ceil256(2 * v) + ceil256(ffn_parts_bytes(n_expert, n_rows, hidden, ffn)) + ffn_sums(n_expert, n_rows, hidden, ffn);
 }
 
 deamoe_status_t deamoe_ffn(void* cuda_stream, const void* x, int64_t x_stride, const void* w_gate_up, const void* w_down,
@@ -95,6 +106,8 @@ deamoe_status_t deamoe_ffn(void* cuda_stream, const void* x, int64_t x_stride, c
   // few tiles: dealt along k, the parts' sums joined by a kernel of their own
   const int up_splits = ffn_splits(n_expert, n_rows, 2 * (int64_t)ffn, hidden), down_splits = ffn_splits(n_expert, n_rows, hidden, ffn);
   float* part = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + ceil256(2 * (uint64_t)n_rows * ffn));
+  if (ffn_sums(n_expert, n_rows, hidden, ffn))
+    up.args.sums = down.args.sums = reinterpret_cast<float*>(reinterpret_cast<char*>(part) + ceil256(ffn_parts_bytes(n_expert, n_rows, hidden, ffn)));
   auto joined = [&](MatmulCall& c, int splits, bool dual) {
     JoinArgs j = {};
     j.part = part; j.splits = splits; j.n_rows = n_rows; j.M = c.args.M; j.groups = n_expert; j.dual = dual; j.off = expert_off;
@@ -161,6 +174,13 @@ deamoe_status_t deamoe_ffn_backward(void* cuda_stream, const void* x, int64_t x_
   MatmulCall e = ffn_call(S, hidden, n_rows);  // dWd = dy^T h
   e.args.tile_n = MM_N; e.args.N = ffn;
   d.args.late = e.args.late = 1;  // they need b's results as c does, and c waits for those
+  // what can run at the same time has sums of its own: b beside a, d beside c, e beside both
+  if (const uint64_t each = ffn_backward_sums(n_rows, hidden, ffn)) {
+    char* sums = ws + 2 * ceil256(4 * v) + ceil256(2 * v);
+    a.args.sums = c.args.sums = reinterpret_cast<float*>(sums);
+    b.args.sums = d.args.sums = reinterpret_cast<float*>(sums + each);
+    e.args.sums = reinterpret_cast<float*>(sums + 2 * each);
+  }
   if (!map_rows(&a.maps.a, w_down, 2, ffn, hidden, ffn, n_expert, wd_one, 64) || !map_b(&a, dout, 2, hidden, n_rows, dout_stride) ||
       !map_gate_up(&b.maps.a, w_gate_up, hidden, ffn, n_expert) || !map_b(&b, x, 2, hidden, n_rows, x_stride) ||
       !map_rows(&c.maps.a, w_gate_up, 2, hidden, 2 * (int64_t)ffn, hidden, n_expert, 2 * wd_one, 64) ||

@@ -26,6 +26,12 @@ constexpr int TILE_STEPS = 20;
 // the clearing.
 constexpr int MM_TAIL_LEAD = 2;
 __device__ __forceinline__ uint32_t tail_place(uint32_t chunks) { return chunks > MM_TAIL_LEAD ? chunks - 1 - MM_TAIL_LEAD : 0; }
+// ... of a whole contraction: in its last stretch
+template <bool LONG> __device__ __forceinline__ int tail_of(int chunks) {
+  const int before = LONG && chunks > 0 ? (chunks - 1) / MM_STRETCH * MM_STRETCH : 0;
+  return before + (int)tail_place(chunks - before);
+}
+static_assert((MM_STRETCH & (MM_STRETCH - 1)) == 0, "a chunk's place in its stretch");
 constexpr int MM_TABLE = (DEAMOE_MAX_EXPERTS + 1) * 8 + 8;  // groups' first tile and first row
 constexpr size_t MM_SMEM = (size_t)MM_RING + MM_STAGING + MM_CONTROL + MM_TABLE;
 static_assert(MM_RING / (MM_OPERAND + 16 * 128) <= MM_STAGES, "barriers of a stage");
@@ -142,6 +148,16 @@ __device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&r)[32]) {
         "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
       : "r"(addr));
 }
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+      "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+      ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+        "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]),
+        "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]),
+        "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ __forceinline__ void tmem_store_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // ---------------------------------------------------------------- the order of the tiles
@@ -224,6 +240,56 @@ __device__ __forceinline__ void floats8(const float* p, float (&v)[8]) {
 __device__ __forceinline__ float gain(const void* p, int f32, int i) {
   return f32 ? reinterpret_cast<const float*>(p)[i] : __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(p)[i]);
 }
+// An epilogue warp's part of a contraction in more than one stretch.  Every stretch but the last is added to the CTA's sums, [column / 4]
+// [lane of 128][4], where a thread meets nothing but its own values; the last accumulator takes the total, and the epilogue goes on
+// from there as from any other (from the accumulator itself where there is one stretch alone).  a: turns of the accumulators so far; returns that of the last one, or ~0 if a wait has expired.
+// STEP: columns of an epilogue step.
+template <int STEP> __device__ __forceinline__ uint32_t join_stretches(uint32_t a, int chunks, uint32_t lane_base, int n, float* all_sums,
+                                                                       uint32_t acc_full, uint32_t acc_empty, volatile int* abort_flag) {
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, row = (warp & 3) * 32 + lane;
+  const int stretches = (chunks + MM_STRETCH - 1) / MM_STRETCH;
+  if (stretches <= 1) return a;
+  float* const sums = all_sums + (int64_t)blockIdx.x * (128 * MM_N);
+  for (int i = 0;; ++i, ++a) {
+    const uint32_t buf = a & 1u;
+    const int w = lane == 0 ? bar_wait(acc_full + 8 * buf, (a >> 1) & 1u, abort_flag) : 0;
+    if (__shfl_sync(0xffffffffu, w, 0) == 0) return ~0u;
+    tc_after();
+    const bool last = i + 1 == stretches;
+    for (int c0 = (warp >> 2) * STEP; c0 < n; c0 += MM_TEAMS * STEP)
+#pragma unroll 1
+      for (int c = c0; c < c0 + STEP; c += 32) {
+        uint32_t r[32];
+        tmem_load(lane_base + buf * MM_N + c, r);
+        tmem_load_wait();
+        float4* const at = reinterpret_cast<float4*>(sums) + (c / 4) * 128 + row;
+        if (i > 0)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const float4 v = __ldcg(at + j * 128);
+            r[4 * j] = __float_as_uint(v.x + __uint_as_float(r[4 * j]));
+            r[4 * j + 1] = __float_as_uint(v.y + __uint_as_float(r[4 * j + 1]));
+            r[4 * j + 2] = __float_as_uint(v.z + __uint_as_float(r[4 * j + 2]));
+            r[4 * j + 3] = __float_as_uint(v.w + __uint_as_float(r[4 * j + 3]));
+          }
+        if (last) {
+          tmem_store(lane_base + buf * MM_N + c, r);
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            __stcg(at + j * 128, make_float4(__uint_as_float(r[4 * j]), __uint_as_float(r[4 * j + 1]), __uint_as_float(r[4 * j + 2]),
+                                             __uint_as_float(r[4 * j + 3])));
+        }
+      }
+    if (last) {
+      tmem_store_wait();
+      return a;
+    }
+    tc_before();
+    __syncwarp();
+    if (lane == 0) bar_arrive_cluster(in_first(acc_empty + 8 * buf));
+  }
+}
 // What an epilogue step of a thread takes from memory, asked for a step ahead.
 struct Ahead {
   uint4 v[4];
@@ -231,8 +297,10 @@ struct Ahead {
 };
 
 // ---------------------------------------------------------------- the kernel
-// AT / BT: A / B lies with its rows as the inner axis (k outer); RAGGED: the contraction runs over a group's rows.
-template <int EPI, bool AT, bool BT, bool FP8, bool RAGGED>
+// AT / BT: A / B lies with its rows as the inner axis (k outer); RAGGED: the contraction runs over a group's rows; LONG: it may come in
+// more than one stretch (by itself, as a small product's time is to a good part that of fetching code: with both in one kernel the gradients of 10 experts
+// of 1032 x 344 took 56.3 us, 55.3 without).
+template <int EPI, bool AT, bool BT, bool FP8, bool RAGGED, bool LONG>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     k_matmul(const __grid_constant__ MatmulArgs A, const __grid_constant__ MatmulMaps maps) {
   constexpr bool DUAL = EPI == ME_SWIGLU || EPI == ME_SWIGLU_GRAD || EPI == ME_PART_DUAL;  // A's rows alternate gate and up
@@ -327,6 +395,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   const int tiles = first_tile[A.groups] * (SPLIT ? A.splits : 1);  // (SPLIT: parts of tiles)
   const int pairs = gridDim.x >> 1, pair = blockIdx.x >> 1;
   auto chunks_of = [&](const Tile& t) { return ((RAGGED ? t.rows : A.K) + A.chunk - 1) / A.chunk; };
+  // parts of a tile are dealt evenly, none without a chunk (splits <= chunks)
+  auto chunks_in = [&](int it, const Tile& t) {
+    const int all = chunks_of(t), base = SPLIT ? all / A.splits : all;
+    return SPLIT ? base + (it % A.splits < all - base * A.splits) : all;
+  };
   auto tile_at = [&](int it) { return find_tile<RAGGED>(A, first_tile, first_row, SPLIT ? it / A.splits : it, M_STEP); };
 
   if (warp == MM_WARP_A || warp == MM_WARP_B) {
@@ -340,7 +413,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     for (int it = pair; ok && it < tiles; it += pairs) {
       const Tile t = tile_at(it);
       const int half = t.n / 2, all = chunks_of(t);
-      // the part's chunks: dealt evenly, none without one (splits <= chunks)
       const int part = SPLIT ? it % A.splits : 0;
       const int base = SPLIT ? all / A.splits : all, more = SPLIT ? all - base * A.splits : 0;
       const int c_begin = part * base + min(part, more), c_end = c_begin + base + (part < more);
@@ -348,7 +420,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
       const int z = is_a && !RAGGED ? t.group : 0;
       const CUtensorMap* map = is_a ? &maps.a : &maps.b;
       const int left = RAGGED ? t.rows % A.chunk : 0;
-      const int tail_at = RAGGED && left ? (int)tail_place(all) : -1;
+      const int tail_at = RAGGED && left ? tail_of<LONG>(all) : -1;
       for (int c = c_begin; c < c_end; ++c) {  // (c: the place in the ring's order)
         if (!free && !bar_wait(empty(s), phase, abort_flag)) { ok = false; break; }
         // rows of the next group come along with the last chunk: this CTA's clearing warp sees them first
@@ -359,9 +431,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
         if (one) {
           if (is_a && last_rows) bar_expect(tail(s), stage_bytes);
           if (is_a && rank == 0) {
-            if (c == c_begin) {
-              info[2 * s] = t.n | (left + 15) / 16 << TILE_STEPS;
-              info[2 * s + 1] = c_end - c_begin;
+            if (LONG ? ((c - c_begin) & (MM_STRETCH - 1)) == 0 : c == c_begin) {  // a stretch is to the MMA role a tile of its own
+              const int n = LONG ? min(MM_STRETCH, c_end - c) : c_end - c;
+              info[2 * s] = t.n | (RAGGED && c + n == c_end ? (left + 15) / 16 << TILE_STEPS : 0);
+              info[2 * s + 1] = n;
             }
             bar_expect(full(s), last_rows ? 0 : 2 * stage_bytes);
           }
@@ -463,7 +536,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
       for (int it = pair; it < tiles; it += pairs) {
         const Tile t = tile_at(it);
         const int chunks = chunks_of(t), left = t.rows % A.chunk;
-        const int s = (g + tail_place(chunks)) % stages;
+        const int s = (g + tail_of<LONG>(chunks)) % stages;
         g += chunks;
         if (left == 0) continue;
         int ok = lane == 0 ? bar_wait(tail(s), (parity >> s) & 1u, abort_flag) : 0;
@@ -494,6 +567,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
       for (int it = pair; it < tiles; it += pairs) {
         const Tile t = tile_at(it);
         const bool none = t.rows == 0;  // a group without rows: zeros
+        if constexpr (LONG) {
+          a = join_stretches<MM_ROW_STEP>(a, chunks_in(it, t), lane_base, t.n, A.sums, acc_full(0), acc_empty(0), abort_flag);
+          if (a == ~0u) break;
+        }
         const uint32_t buf = a & 1u;
         if (!none) {
           const int w = lane == 0 ? bar_wait(acc_full(buf), (a >> 1) & 1u, abort_flag) : 0;
@@ -558,6 +635,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     for (int it = pair; ok && it < tiles; it += pairs) {
       const Tile t = tile_at(it);
       const bool none = RAGGED && t.rows == 0;  // a group without rows: zeros
+      if constexpr (LONG) {
+        a = join_stretches<MM_STEP>(a, chunks_in(it, t), lane_base, t.n, A.sums, acc_full(0), acc_empty(0), abort_flag);
+        if (a == ~0u) break;
+      }
       const uint32_t buf = a & 1u;
       const int m = t.m0 + (int)rank * (M_STEP / 2) + (warp & 3) * (M_STEP / 8) + q * 8, n = min(8, A.M - m);
       const int valid = n > 0 ? t.valid : 0;
@@ -822,10 +903,10 @@ bool encode(CUtensorMap* m, const void* p, int esize, int rank, const cuuint64_t
            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int EPI, bool AT, bool BT, bool FP8, bool RAGGED>
-cudaError_t launch(const MatmulCall& c, cudaStream_t s) {
+template <int EPI, bool AT, bool BT, bool FP8, bool RAGGED, bool LONG>
+cudaError_t launch_form(const MatmulCall& c, cudaStream_t s) {
   static std::atomic<uint64_t> done{0};
-  auto kernel = k_matmul<EPI, AT, BT, FP8, RAGGED>;
+  auto kernel = k_matmul<EPI, AT, BT, FP8, RAGGED, LONG>;
   int dev = 0;
   if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return cudaErrorInvalidDevice;
   if (!(done.load(std::memory_order_acquire) >> dev & 1)) {
@@ -841,6 +922,12 @@ cudaError_t launch(const MatmulCall& c, cudaStream_t s) {
   const int64_t most = mt * nt * a.splits;
   const dim3 grid(2 * (unsigned)(most < MM_PAIRS ? most : MM_PAIRS));
   return launch_pdl(kernel, grid, dim3(MM_THREADS), MM_SMEM, s, c.args, c.maps);
+}
+template <int EPI, bool AT, bool BT, bool FP8, bool RAGGED>
+cudaError_t launch(const MatmulCall& c, cudaStream_t s) {
+  const MatmulArgs& a = c.args;
+  if (!matmul_sums(a.K, a.chunk, a.splits)) return launch_form<EPI, AT, BT, FP8, RAGGED, false>(c, s);
+  return a.sums ? launch_form<EPI, AT, BT, FP8, RAGGED, true>(c, s) : cudaErrorInvalidValue;
 }
 
 }  // namespace

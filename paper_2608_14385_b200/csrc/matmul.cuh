@@ -19,6 +19,10 @@
 //   warp  11   ragged contractions (weight gradients: k runs over a group's rows): clears the rows behind the group's end
 //              that the last chunk's box brought in, in both operands, before the MMAs may read them
 // Two accumulators of 256 columns take turns in tensor memory, so an epilogue runs under the next tile's MMAs.
+//
+// The tensor cores cut their fp32 sums at every step: terms of one sign lose 6e-9 of their sum a term (bf16, measured: 1.8e-4 over 32768
+// terms, 6.6e-3 over 2^20, a third of the sum over 2^26; e4m3 a tenth of that).  So a contraction runs in stretches of MM_STRETCH
+// chunks: each is a turn of an accumulator, and the epilogue adds them up in fp32 proper, in their order.
 // Every wait is bounded; one that expires ends the CTA's roles and raises the status word that
 // deamoe_operator_status reads.
 #pragma once
@@ -63,6 +67,7 @@ struct MatmulArgs {
   int64_t rs;            // residual's or dout's row stride
   int bias_f32, act, wide_in;
   float* part;           // [2 tiles of N][M] sums of dz    (ME_PRODUCT_GRAD)
+  float* sums;           // MM_SUMS_BYTES of matmul_sums(), or null where a contraction is one stretch; no two launches that overlap share them
 };
 
 struct MatmulMaps {
@@ -117,5 +122,14 @@ constexpr int MM_M = 256, MM_N = 256;
 constexpr int MM_MAX_ROWS = INT32_MAX - 256;  // so that a tile's end is a number of 32 bits
 constexpr int MM_N_LEAST = 64;   // matmul_tile_n gives no less for more rows
 constexpr int MM_PARTS = 2;      // rows of sums that a tile leaves in `part`
+
+// Chunks of a stretch: 32768 values (e4m3: 65536), whose loss is a tenth of half a step of bf16 at most.
+constexpr int MM_STRETCH = 512;
+constexpr uint64_t MM_SUMS_BYTES = 148ull * 128 * MM_N * 4;  // a CTA's half of a tile
+// Bytes of `sums` for a contraction over k values in chunks of `chunk`, dealt in `splits` parts.
+inline uint64_t matmul_sums(int64_t k, int chunk, int splits) {
+  const int64_t chunks = (k + chunk - 1) / chunk;
+  return (chunks + splits - 1) / splits > MM_STRETCH ? MM_SUMS_BYTES : 0;
+}
 
 }  // namespace deamoe

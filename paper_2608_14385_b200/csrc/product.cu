@@ -76,6 +76,18 @@ static int product_splits(const MatmulArgs& a) {
   return matmul_splits((int64_t)((a.M + MM_M - 1) / MM_M) * ((a.N + a.tile_n - 1) / a.tile_n), (a.K + a.chunk - 1) / a.chunk, a.N, a.M);
 }
 
+// Forward: bytes of the parts' sums, and of those of contractions of more than one stretch
+static uint64_t parts_bytes(const MatmulArgs& a) {
+  const int splits = product_splits(a);
+  return splits > 1 ? (uint64_t)splits * a.N * ((a.M + 7) / 8 * 8) * 4 : 0;
+}
+static uint64_t product_sums(const MatmulArgs& a) { return matmul_sums(a.K, a.chunk, product_splits(a)); }
+// Backward, for each of the two that can overlap (dx and dW)
+static uint64_t backward_sums(int T, int n_out, int n_in) {
+  const int k = n_out > n_in ? n_out : n_in;
+  return matmul_sums(k > T ? k : T, 64, 1);
+}
+
 static deamoe_status_t check_product(int dtype, int T, int n_out, int n_in, int act, int bias_dtype, const void* bias) {
   if ((dtype != DEAMOE_BF16 && dtype != DEAMOE_E4M3) || n_out <= 0 || n_in <= 0 || act < DEAMOE_SIGMA_NONE || act > DEAMOE_SIGMA_GELU ||
       !known_type(bias_dtype) || !aligned_to(bias, type_bytes(bias_dtype)))
@@ -124,6 +136,7 @@ deamoe_status_t deamoe_product(void* cuda_stream, int32_t dtype, const void* x, 
   if (!map_rows(&c.maps.a, weight, es, n_in, n_out, n_in, 1, n_in, 128) || !map_b(&c, x, es, n_in, n_token, x_stride)) return DEAMOE_ERR_CUDA;
   cudaStream_t s = reinterpret_cast<cudaStream_t>(cuda_stream);
   const int splits = product_splits(c.args);
+  if (product_sums(c.args)) c.args.sums = reinterpret_cast<float*>(reinterpret_cast<char*>(workspace) + ceil256(parts_bytes(c.args)));
   if (splits > 1) {  // few tiles: dealt along k, the parts' sums joined by a kernel of their own
     JoinArgs j = {};
     j.part = reinterpret_cast<float*>(workspace); j.splits = splits; j.n_rows = n_token; j.M = n_out; j.groups = 1;
@@ -143,14 +156,16 @@ static uint64_t bias_parts(int T, int n_out, int act) {
   return (uint64_t)(act == DEAMOE_SIGMA_NONE ? (T + BIAS_ROWS - 1) / BIAS_ROWS : MM_PARTS * ((T + MM_N_LEAST - 1) / MM_N_LEAST)) * n_out * 4;
 }
 
+static uint64_t dz_bytes(int T, int n_out, int act) { return act == DEAMOE_SIGMA_NONE ? 0 : ceil256((uint64_t)T * n_out * 2); }
+
 uint64_t deamoe_product_workspace(int32_t dtype, int32_t n_token, int32_t n_out, int32_t n_in, int32_t act, int32_t backward) {
   if (n_token <= 0 || n_out <= 0 || n_in <= 0) return 0;
   if (!backward) {
     if (n_token <= THIN_ROWS) return 0;
-    const int splits = product_splits(product_call(n_out, n_in, n_token, dtype == DEAMOE_E4M3 ? 128 : 64, true).args);
-    return splits > 1 ? (uint64_t)splits * n_token * ((n_out + 7) / 8 * 8) * 4 : 0;
+    const MatmulArgs a = product_call(n_out, n_in, n_token, dtype == DEAMOE_E4M3 ? 128 : 64, true).args;
+    return ceil256(parts_bytes(a)) + product_sums(a);
   }
-  return ceil256(bias_parts(n_token, n_out, act)) + (act == DEAMOE_SIGMA_NONE ? 0 : (uint64_t)n_token * n_out * 2);
+  return ceil256(bias_parts(n_token, n_out, act)) + dz_bytes(n_token, n_out, act) + 2 * backward_sums(n_token, n_out, n_in);
 }
 
 deamoe_status_t deamoe_product_backward(void* cuda_stream, int32_t dtype, const void* x, int64_t x_stride, int32_t n_token,
@@ -192,6 +207,11 @@ deamoe_status_t deamoe_product_backward(void* cuda_stream, int32_t dtype, const 
   // gradient, dx and dW beside them, and their sums at the end.
   c.args.late = 1;
   b.args.late = plain && dbias;
+  if (const uint64_t each = backward_sums(n_token, n_out, n_in)) {  // (b waits for a, c may run beside b)
+    char* sums = reinterpret_cast<char*>(dz) + dz_bytes(n_token, n_out, act);
+    a.args.sums = b.args.sums = reinterpret_cast<float*>(sums);
+    c.args.sums = reinterpret_cast<float*>(sums + each);
+  }
   const int parts = plain ? (n_token + BIAS_ROWS - 1) / BIAS_ROWS : MM_PARTS * ((n_token + a.args.tile_n - 1) / a.args.tile_n);
   auto add_parts = [&](int late) {
     return launch_pdl(k_add_parts, dim3((n_out + 31) / 32), dim3(256), 0, s, (const float*)part, parts, (int)n_out, dbias, late) == cudaSuccess;

@@ -117,3 +117,19 @@ def test_sizes_that_32_bits_cannot_hold_do_not_reach_the_library(monkeypatch):
         with pytest.raises(binding.DeaMoEError) as e:
             call()
         assert e.value.status == INVALID
+
+
+def test_workspaces_of_sums_over_more_than_a_stretch():
+    """Contractions of more than 32768 values (8-bit: 65536) keep sums of their stretches: a CTA's half tile each, for what can overlap."""
+    L, half = binding.lib(), 148 * 128 * 256 * 4
+    assert L.deamoe_product_workspace(1, 32768, 8, 8, 0, 1) == 512 * 8 * 4
+    assert L.deamoe_product_workspace(1, 32769, 8, 8, 0, 1) == -(-513 * 8 * 4 // 256) * 256 + 2 * half
+    assert L.deamoe_product_workspace(1, 4096, 4096, 32768, 0, 0) == 0 and L.deamoe_product_workspace(1, 4096, 4096, 32776, 0, 0) == half
+    assert L.deamoe_product_workspace(2, 4096, 4096, 65536, 0, 0) == 0 and L.deamoe_product_workspace(2, 4096, 4096, 65552, 0, 0) == half
+    for R, h, f in ((32769, 8, 8), (20, 32776, 8), (20, 8, 16392)):
+        v = [-(-R * f * n // 256) * 256 for n in (4, 4, 2)]
+        assert L.deamoe_ffn_workspace(1, R, h, f, 1) == sum(v) + 3 * half
+    assert L.deamoe_ffn_workspace(1, 32768, 8, 8, 1) == 32768 * 8 * 10
+    need = L.deamoe_product_workspace(1, 40000, 8, 8, 0, 1)
+    good = dict(s=None, dt=1, x=A, xs=8, T=40000, w=B, N=8, K=8, bdt=0, bias=D, act=0, dout=E, ds=8, dx=F, dxs=8, dw=G, db=H, ws=W, size=need)
+    _refused("deamoe_product_backward", good, [(dict(size=need - 1), INVALID), (dict(ws=None), INVALID)])
