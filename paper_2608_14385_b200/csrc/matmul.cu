@@ -39,7 +39,9 @@ static_assert(MM_SMEM <= 227 * 1024, "shared memory budget");
 // One CTA fills more than half of an SM's shared memory, so none of another grid's can be beside it and the
 // allocation of all 512 columns of tensor memory never waits.
 static_assert(2 * MM_SMEM > 228 * 1024, "tensor-memory allocation must never block");
-constexpr unsigned long long MM_WAIT_NS = 2000000000ull;  // after which a wait gives up (the longest contraction takes some 10 ms)
+// After so long without a new stretch among its CTA's copies a wait gives up.  (A stretch takes 0.2 ms at 0.3 us a chunk, but some waits last a
+// whole contraction, which over 2^31 rows takes ten seconds, or several tiles.)
+constexpr unsigned long long MM_WAIT_NS = 2000000000ull;
 constexpr int MM_PAIRS = 74;                   // 148 SMs
 
 __device__ int32_t mm_status;                  // DEAMOE_ERR_TIMEOUT once a wait has expired
@@ -80,13 +82,19 @@ __device__ __forceinline__ unsigned long long now_ns() {
   asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
   return t;
 }
-// (Not inlined: each role has its waits, and a small product's time is to a good part that of fetching code.)
+// abort_flag[1]: copies at the last stretch's start.  (Not inlined: each role has its waits, and a small product's time is to a good part that of fetching code.)
 __device__ __noinline__ bool bar_wait_longer(uint32_t bar, uint32_t parity, volatile int* abort_flag) {
-  const unsigned long long start = now_ns();
+  unsigned long long start = now_ns();
+  int copies = abort_flag[1];
   for (unsigned it = 1;; ++it) {
     if (bar_try(bar, parity)) return true;
     if ((it & 63u) == 0 && *abort_flag) return false;
-    if ((it & 255u) == 0 && now_ns() - start > MM_WAIT_NS) break;
+    if ((it & 255u) == 0) {
+      const int now = abort_flag[1];
+      if (now != copies) start = now_ns();
+      else if (now_ns() - start > MM_WAIT_NS) break;
+      copies = now;
+    }
   }
   *abort_flag = 1;
   return false;
@@ -318,9 +326,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
   auto acc_empty = [&](int b) { return bars + 8 * (4 * MM_STAGES + 2 + b); };
   const uint32_t first_full = in_first(full(0));
   uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(control + 4 * MM_STAGES + 4);
-  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  uint32_t* info = tmem_slot + 2;  // [MM_STAGES][2]: a tile whose first chunk the stage holds
-  static_assert((4 * MM_STAGES + 4) * 8 + 8 + MM_STAGES * 8 <= MM_CONTROL, "control region");
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);  // and how far the copies are, see bar_wait
+  uint32_t* info = tmem_slot + 3;  // [MM_STAGES][2]: a tile whose first chunk the stage holds
+  static_assert((4 * MM_STAGES + 4) * 8 + 12 + MM_STAGES * 8 <= MM_CONTROL, "control region");
   int* first_row = reinterpret_cast<int*>(smem + MM_RING + MM_STAGING + MM_CONTROL);
   int* first_tile = first_row + A.groups + 1;
 
@@ -338,7 +346,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
       bar_init(acc_full(b), 1);
       bar_init(acc_empty(b), 2 * 4 * MM_TEAMS);
     }
-    *abort_flag = 0;
+    abort_flag[0] = abort_flag[1] = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (tid == MM_WARP_A * 32) prefetch_map(&maps.a);
@@ -430,12 +438,14 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
         const uint32_t bar = last_rows ? tail(s) : first_full + 8 * s, dst = ring + s * stage_bytes + (is_a ? 0 : MM_OPERAND);
         if (one) {
           if (is_a && last_rows) bar_expect(tail(s), stage_bytes);
+          const bool opens = is_a && (LONG ? ((c - c_begin) & (MM_STRETCH - 1)) == 0 : c == c_begin);
+          if (opens) {  // a stretch, to the MMA role a tile of its own
+            abort_flag[1] = (int)g;
+            const int n = LONG ? min(MM_STRETCH, c_end - c) : c_end - c;
+            info[2 * s] = t.n | (RAGGED && c + n == c_end ? (left + 15) / 16 << TILE_STEPS : 0);
+            info[2 * s + 1] = n;
+          }
           if (is_a && rank == 0) {
-            if (LONG ? ((c - c_begin) & (MM_STRETCH - 1)) == 0 : c == c_begin) {  // a stretch is to the MMA role a tile of its own
-              const int n = LONG ? min(MM_STRETCH, c_end - c) : c_end - c;
-              info[2 * s] = t.n | (RAGGED && c + n == c_end ? (left + 15) / 16 << TILE_STEPS : 0);
-              info[2 * s + 1] = n;
-            }
             bar_expect(full(s), last_rows ? 0 : 2 * stage_bytes);
           }
           if (DUAL && is_a) {

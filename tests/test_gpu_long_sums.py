@@ -181,3 +181,18 @@ def test_equal_calls_give_equal_bits_and_graphs_share_no_sums():
                 g.replay()
     torch.cuda.synchronize()
     assert all(torch.equal(a, b) for o, ws in zip(outs, want) for a, b in zip(o, ws))
+
+
+def test_contraction_that_takes_longer_than_a_wait():
+    """800 million rows in one tile: 12.6 million chunks at 0.3 us, longer than the 2 s after which a wait gives up where nothing moves.  Zeros but for
+    a row for each output, at the ends, at edges of stretches and in the last, ragged chunk."""
+    T, K, N = 3 * (1 << 28) + 77, 8, 8
+    x, d, w = torch.ones((T, K), dtype=BF16, device=DEV), torch.zeros((T, N), dtype=BF16, device=DEV), torch.zeros((N, K), dtype=BF16, device=DEV)
+    at = [0, 32767, 32768, 1 << 28, (1 << 29) - 1, 1 << 29, T - 14, T - 1]
+    for i, t in enumerate(at):
+        d[t, i] = float(1 << i)
+        x[t] = 1.0 + i / 8
+    dx, dw, _ = binding.product_backward(x, w, d)
+    assert binding.operator_status() == binding.OK
+    del dx
+    assert torch.equal(dw.double(), _over_rows(d[at], x[at]))
