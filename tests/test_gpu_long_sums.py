@@ -196,3 +196,25 @@ def test_contraction_that_takes_longer_than_a_wait():
     assert binding.operator_status() == binding.OK
     del dx
     assert torch.equal(dw.double(), _over_rows(d[at], x[at]))
+
+
+EDGES = ([0, 7, 8, 15, 16, 62, 63, 64], [65, 127, 128, 255, 256, 511, 512, 32767], [32768, 65535, 65536, 65599, 131071, 131072, 262143, 262144],
+         [-1, -13, -14, -77, -78, -141, -142, 1 << 21])
+
+
+@pytest.mark.parametrize("at", EDGES)
+def test_every_row_of_millions_counts_once(at):
+    """Sums that are exact: a row for each output at the edges of blocks, chunks and stretches, zeros elsewhere; and ones everywhere, whose
+    sum in fp32 is the number of rows."""
+    T, K, N = 65536 * 64 + 77, 8, 8
+    x, d, w = torch.ones((T, K), dtype=BF16, device=DEV), torch.zeros((T, N), dtype=BF16, device=DEV), torch.zeros((N, K), dtype=BF16, device=DEV)
+    for i, t in enumerate(at):
+        d[t, i], x[t] = float(1 << i), 1.0 + i / 8
+    dx, dw, db = binding.product_backward(x, w, d, bias=torch.zeros(N, device=DEV))
+    assert torch.equal(dw.double(), _over_rows(d[at], x[at])) and torch.equal(db.double(), d[at].double().sum(0)) and (dx == 0).all()
+    db = binding.product_backward(x, w, torch.ones_like(d), bias=torch.zeros(N, device=DEV))[2]
+    assert (db == float(T)).all()
+    # the derivative of SiLU at 0 is a half: the same sums behind an activation
+    dw, db = binding.product_backward(x, w, d, bias=torch.zeros(N, device=DEV), act=binding.SIGMA_SILU)[1:]
+    assert torch.equal(2 * dw.double(), _over_rows(d[at], x[at])) and torch.equal(2 * db.double(), d[at].double().sum(0))
+    assert binding.operator_status() == binding.OK
