@@ -247,3 +247,21 @@ def test_bias_gradient_of_millions_of_tokens():
         pb.check(dx[rows], *pb.dot(d[rows].double(), None, w.double().T, None))
     pb.check(db, d.double().sum(0), (T + 8) * 2.0 ** -24 * d.double().abs().sum(0))
     pb.check(dw, *pb.dot(d.double().T, None, x.double().T, None))
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("T,K,N", [(300, 144, 72), (2100, 264, 1040), (40, 2048, 136)])
+def test_residual_and_out_on_different_boundaries(T, K, N, kind):
+    """An aligned out with a residual off 16-byte boundaries, and the other way round; also rows of whole pieces with a stride that is not."""
+    K = K // 16 * 16
+    c = _case(T, K, N, kind, 21, BF16, True)
+    plain = _call(c, GELU)
+    for at, pad in ((0, 16), (3, 16), (8, 16), (0, 3)):
+        room = torch.zeros((T, N + pad), dtype=BF16, device=DEV)
+        room[:, at:at + N] = c["residual"]
+        s = dict(c, residual=room[:, at:at + N])
+        assert torch.equal(_call(s, GELU), plain)
+        out = torch.full((T, N + pad), 3.0, dtype=BF16, device=DEV)
+        assert torch.equal(_call(c, GELU, out=out[:, at:at + N]), plain)
+        assert (out[:, :at] == 3).all() and (out[:, at + N:] == 3).all()
+    pb.check(plain, *_want(c, GELU))
