@@ -313,6 +313,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     k_matmul(const __grid_constant__ MatmulArgs A, const __grid_constant__ MatmulMaps maps) {
   constexpr bool DUAL = EPI == ME_SWIGLU || EPI == ME_SWIGLU_GRAD || EPI == ME_PART_DUAL;  // A's rows alternate gate and up
   constexpr bool SPLIT = EPI == ME_PART || EPI == ME_PART_DUAL;
+  static_assert(RAGGED == (EPI == ME_STORE_ROWS), "groups without rows are zeros in that epilogue alone");
+  static_assert(MM_PARTS == MM_TEAMS, "a team leaves a row of `part`");
   constexpr int M_STEP = DUAL ? MM_M / 2 : MM_M;                    // in rows of A as the caller counts them (DUAL: features)
   extern __shared__ __align__(1024) unsigned char smem[];
   float* staging = reinterpret_cast<float*>(smem + MM_RING);
@@ -644,7 +646,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
     const float* const mine = st + c * MM_PITCH + q * (DUAL ? 16 : 8);
     for (int it = pair; ok && it < tiles; it += pairs) {
       const Tile t = tile_at(it);
-      const bool none = RAGGED && t.rows == 0;  // a group without rows: zeros
       if constexpr (LONG) {
         a = join_stretches<MM_STEP>(a, chunks_in(it, t), lane_base, t.n, A.sums, acc_full(0), acc_empty(0), abort_flag);
         if (a == ~0u) break;
@@ -673,7 +674,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
               } else if (wide_in) {
                 w.v[i] = load_once<__nv_bfloat16, 8>(reinterpret_cast<const __nv_bfloat16*>(p)).r;
               }
-              if constexpr (FP8 && !SPLIT) w.scale[i] = xs[i * ITEM_ROWS];
+              if constexpr (FP8) w.scale[i] = xs[i * ITEM_ROWS];
             }
           in += in_stride * (MM_TEAMS * MM_STEP);
           if constexpr (FP8) xs += MM_TEAMS * MM_STEP;
@@ -716,35 +717,28 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(MM_THREADS, 1)
       } else {
         ask(team * MM_STEP + c, now);
       }
-      if (!none) {
-        const int w = lane == 0 ? bar_wait(acc_full(buf), (a >> 1) & 1u, abort_flag) : 0;
-        ok = __shfl_sync(0xffffffffu, w, 0) != 0;
-        if (!ok) break;
-        tc_after();
-        ++a;
-      }
+      const int w = lane == 0 ? bar_wait(acc_full(buf), (a >> 1) & 1u, abort_flag) : 0;
+      ok = __shfl_sync(0xffffffffu, w, 0) != 0;
+      if (!ok) break;
+      tc_after();
+      ++a;
       auto release = [&] {  // this warp has read its part of the accumulator
         tc_before();
         __syncwarp();
         if (lane == 0) bar_arrive_cluster(in_first(acc_empty(buf)));
       };
-      if (!none && team * MM_STEP >= t.n) release();
+      if (team * MM_STEP >= t.n) release();
       for (int c0 = team * MM_STEP; c0 < t.n; c0 += MM_TEAMS * MM_STEP) {
         uint32_t r[MM_STEP];
-        if (none) {
-#pragma unroll
-          for (int i = 0; i < MM_STEP; ++i) r[i] = 0;
+        tmem_load(lane_base + buf * MM_N + c0, r);
+        if (EPI == ME_PRODUCT && odd_rows) {
+          ask_odd(c0 + 16, next);
+          scale_next = row_scales(c0 + MM_TEAMS * MM_STEP);  // (past the tile's end: nothing)
         } else {
-          tmem_load(lane_base + buf * MM_N + c0, r);
-          if (EPI == ME_PRODUCT && odd_rows) {
-            ask_odd(c0 + 16, next);
-            scale_next = row_scales(c0 + MM_TEAMS * MM_STEP);  // (past the tile's end: nothing)
-          } else {
-            ask(c0 + MM_TEAMS * MM_STEP + c, next);
-          }
-          tmem_load_wait();
-          if (c0 + MM_TEAMS * MM_STEP >= t.n) release();
+          ask(c0 + MM_TEAMS * MM_STEP + c, next);
         }
+        tmem_load_wait();
+        if (c0 + MM_TEAMS * MM_STEP >= t.n) release();
 #pragma unroll
         for (int i = 0; i < MM_STEP; ++i) st[i * MM_PITCH + lane] = __uint_as_float(r[i]);
         __syncwarp();
