@@ -15,6 +15,9 @@ namespace {
 
 constexpr int T_AHEAD = 4; // steps of loads in flight
 constexpr int T_SMS = 148;
+// The instruction's sums are cut at every step, as the tensor-core kernel's are (matmul.cuh): a warp adds its sums up in fp32 proper after so many turns
+// of its loop, 32768 columns (e4m3: 65536).
+constexpr int T_STRETCH = 256;
 
 template <bool FP8> __device__ __forceinline__ void mma16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   if constexpr (FP8)
@@ -32,7 +35,8 @@ __device__ __forceinline__ uint4 load_stream(const char* p) {
 
 // NT: groups of 8 rows of x in a pass; TW: warps of a block.  (One block an SM is all that the bounds ask for: without that the
 // compiler keeps to 64 - 93 registers, and fewer loads are in flight: 16 rows of 7168 x 7168 in 30 us, 22 with 112.)
-template <bool FP8, bool DUAL, int NT, int TW> __global__ void __launch_bounds__(TW * 32, 1) k_thin(const __grid_constant__ ThinArgs A, int behind) {
+// LONG: a warp has more than a stretch (by itself, for the registers: rows of up to 131072 columns never have).
+template <bool FP8, bool DUAL, int NT, int TW, bool LONG> __global__ void __launch_bounds__(TW * 32, 1) k_thin(const __grid_constant__ ThinArgs A, int behind) {
   constexpr int ES = FP8 ? 1 : 2, VE = 16 / ES, STEP = 4 * VE, COLS = 8 * NT, ROWS = DUAL ? 8 : 16;
   __shared__ float part[TW][16][COLS + 1];
   __shared__ int found, counts[TW * 32 + 1], warp_sums[32];
@@ -85,8 +89,17 @@ template <bool FP8, bool DUAL, int NT, int TW> __global__ void __launch_bounds__
 #pragma unroll
     for (int n = 0; n < NT; ++n)
       x[n] = reinterpret_cast<const char*>(A.x) + (int64_t)min(r0 + n * 8 + g, row1 - 1) * A.xs * ES + q * 16;
-    float acc[NT][4] = {};
+    float acc[NT][4] = {}, before[LONG ? NT : 1][4] = {};
     for (int s0 = warp; s0 < steps; s0 += TW * T_AHEAD) {
+      if constexpr (LONG)
+        if ((s0 - warp) % (TW * T_AHEAD * T_STRETCH) == 0)
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              before[n][j] += acc[n][j];
+              acc[n][j] = 0.f;
+            }
       uint4 a[T_AHEAD], b[T_AHEAD], v[T_AHEAD][NT];
 #pragma unroll
       for (int u = 0; u < T_AHEAD; ++u) {
@@ -115,7 +128,7 @@ template <bool FP8, bool DUAL, int NT, int TW> __global__ void __launch_bounds__
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) part[warp][g + 8 * (j >> 1)][n * 8 + 2 * q + (j & 1)] = acc[n][j];
+      for (int j = 0; j < 4; ++j) part[warp][g + 8 * (j >> 1)][n * 8 + 2 * q + (j & 1)] = acc[n][j] + (LONG ? before[LONG ? n : 0][j] : 0.f);
     __syncthreads();
     for (int o = tid; o < ROWS * COLS; o += TW * 32) {
       const int m = o % ROWS, c = o / ROWS;
@@ -149,8 +162,14 @@ template <bool FP8, bool DUAL> cudaError_t launch(const ThinArgs& a, cudaStream_
   // warps fit; one row 20.8 us, 21.2 - 25.4 with eight; 16 rows over 13 of 32 experts 201 us, 239); with fewer, eight keep
   // more loads in flight (4096 x 4096: 9.0 us, 11.7 with four).
   const bool many = (int64_t)grid.x * grid.y >= 3 * T_SMS;
-  auto kernel = a.n_rows <= 8 ? (many ? k_thin<FP8, DUAL, 1, 4> : k_thin<FP8, DUAL, 1, 8>) : (many ? k_thin<FP8, DUAL, 2, 4> : k_thin<FP8, DUAL, 2, 8>);
   const int threads = many ? 128 : 256;
+  constexpr int TURN = (FP8 ? 64 : 32) * T_AHEAD;  // columns of a warp's turn
+  const bool wide = (a.K - 1) / (TURN * T_STRETCH) >= threads / 32;
+  auto kernel = a.n_rows <= 8 ? (many ? k_thin<FP8, DUAL, 1, 4, false> : k_thin<FP8, DUAL, 1, 8, false>)
+                              : (many ? k_thin<FP8, DUAL, 2, 4, false> : k_thin<FP8, DUAL, 2, 8, false>);
+  if (wide)
+    kernel = a.n_rows <= 8 ? (many ? k_thin<FP8, DUAL, 1, 4, true> : k_thin<FP8, DUAL, 1, 8, true>)
+                           : (many ? k_thin<FP8, DUAL, 2, 4, true> : k_thin<FP8, DUAL, 2, 8, true>);
   return launch_pdl(kernel, grid, dim3(threads), 0, s, a, (int)chained);
 }
 

@@ -218,3 +218,24 @@ def test_every_row_of_millions_counts_once(at):
     dw, db = binding.product_backward(x, w, d, bias=torch.zeros(N, device=DEV), act=binding.SIGMA_SILU)[1:]
     assert torch.equal(2 * dw.double(), _over_rows(d[at], x[at])) and torch.equal(2 * db.double(), d[at].double().sum(0))
     assert binding.operator_status() == binding.OK
+
+
+@pytest.mark.parametrize("kind", ["bf16", "e4m3"])
+@pytest.mark.parametrize("T,K,N", [(16, 1 << 20, 256), (5, 1 << 20, 1000), (16, 400016, 4096), (8, 140000, 8192), (3, 262144 + 16, 7200)])
+def test_few_rows_of_great_width(T, K, N, kind):
+    x, w, scales = _wide(T, K, N, kind)
+    y = binding.product(x, w, **scales)
+    v = _over_rows(x.float().T, w.float().T) * (1.0 if kind == "bf16" else 2.0 ** -12)
+    _check_sums(y, v, K)
+
+
+@pytest.mark.parametrize("R,h,f", [(9, 1 << 20, 24), (16, 72, 1 << 20), (4, 300008, 3600)])
+def test_a_block_of_few_rows_of_great_width(tight, R, h, f):
+    x, wgu, wd = _positive((R, h), 1, 0), _positive((1, 2 * f, h), 3), _positive((1, h, f), 4)
+    wgu *= 1.0 / h
+    out = binding.ffn(x, wgu, wd)
+    for lo in range(0, h, 1 << 16):                    # columns of the output some at a time, for their room in 64 bits
+        hi = min(h, lo + (1 << 16))
+        if lo == 0:
+            _, (g, eg, u, eu, hh, eh) = pb.ffn(x.double(), wgu[0].double(), wd[0, :8].double())
+        pb.check(out[:, lo:hi], *pb.dot(hh, eh, wd[0, lo:hi].double(), None))
