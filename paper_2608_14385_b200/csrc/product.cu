@@ -151,7 +151,7 @@ deamoe_status_t deamoe_product(void* cuda_stream, int32_t dtype, const void* x, 
   return DEAMOE_ERR_CUDA;
 }
 
-static uint64_t bias_parts(int T, int n_out, int act) {
+static uint64_t bias_parts(int64_t T, int n_out, int act) {
   // with an activation two rows of sums a tile of tokens, else one a block of rows
   return (uint64_t)(act == DEAMOE_SIGMA_NONE ? (T + BIAS_ROWS - 1) / BIAS_ROWS : MM_PARTS * ((T + MM_N_LEAST - 1) / MM_N_LEAST)) * n_out * 4;
 }

@@ -133,3 +133,12 @@ def test_workspaces_of_sums_over_more_than_a_stretch():
     need = L.deamoe_product_workspace(1, 40000, 8, 8, 0, 1)
     good = dict(s=None, dt=1, x=A, xs=8, T=40000, w=B, N=8, K=8, bdt=0, bias=D, act=0, dout=E, ds=8, dx=F, dxs=8, dw=G, db=H, ws=W, size=need)
     _refused("deamoe_product_backward", good, [(dict(size=need - 1), INVALID), (dict(ws=None), INVALID)])
+
+
+@pytest.mark.parametrize("T", [2 ** 31 - 300, 2 ** 31 - 257, 2 ** 31 - 62, 2 ** 31 - 1])
+def test_workspace_of_the_most_tokens(T):
+    """Also for the few sizes beyond those that the call takes, so that it is the call that refuses them."""
+    sums = 2 * 148 * 128 * 256 * 4
+    for act, parts in ((0, -(-T // 64)), (1, 2 * -(-T // 64))):
+        want = -(-parts * 8 * 4 // 256) * 256 + (0 if act == 0 else -(-T * 16 // 256) * 256) + sums
+        assert binding.lib().deamoe_product_workspace(1, T, 8, 8, act, 1) == want
