@@ -505,7 +505,12 @@ deamoe_status_t deamoe_ffn_backward(void *cuda_stream, const void *x, int64_t x_
  *   act        DEAMOE_SIGMA_NONE, _SILU or _GELU
  *   residual   [n_token, n_out] bf16 with a row stride, or NULL; out may be residual itself (same stride)
  *   out        [n_token, n_out] bf16
- * n_in: a multiple of 8 (e4m3: of 16; else UNSUPPORTED); n_out: any.  Rounded once.
+ * n_in: a multiple of 8 (e4m3: of 16; else UNSUPPORTED); n_out: any.  Rounded once.  A row's and a column's scale are multiplied by one
+ * another first: their product should be a normal number of fp32 (2^-126 and up).
+ *
+ * The sums of deamoe_product, deamoe_ffn and their gradients are the tensor cores' fp32, which are cut, not rounded: some 6e-9 of a sum of values of
+ * one sign a term.  Every 32768 values they are added up in fp32 proper, so that no more than 2e-4 of such a sum is lost,
+ * whatever its length (half a step of the bf16 results is 2e-3 to 4e-3).
  *
  * deamoe_product_backward (bf16; n_out a multiple of 8) takes the forward call's inputs and dout:
  *   dz = dout act'(z),   dx = dz W,   dweight = dz^T x (bf16),   dbias = sum over tokens of dz (fp32, or NULL)

@@ -30,7 +30,10 @@ static MatmulCall ffn_call(const FfnShape& S, int M, int K) {
 }
 
 // Few rows, of few experts: from some nine experts on there are tiles enough for the tensor-core kernel, whose copies keep more bytes in
-// flight (one row each, 7168 x 2048: 8 experts 120 us thin and 126, 12 experts 205 and 180, 16 experts 240 and 219).
+// flight.  9 to 16 rows at random over the experts, us thin and on the tensor cores: 7168 x 2048, 8 experts 100 and 102, 9 experts 131 and
+// 120, 32 experts 193 and 167; 4096 x 1536, 8 experts 47 and 50, 16 experts 80 and 74; 2048 x 768, 8 experts 21 and 22, 16 experts 27 and
+// 28.  Narrower ones stay bound by their launches, where the line is not the best one (1024 x 384: 8 experts 9.7 and 15, 9 experts
+// 11 and 16, 64 experts 15 and 16).
 static bool ffn_thin(int E, int R) { return R <= THIN_ROWS && (E <= 8 || R <= 8); }
 // A forward product's parts of k: M rows of a matrix (gate and up: of both), K columns.
 static int ffn_splits(int E, int R, int64_t M, int64_t K) {

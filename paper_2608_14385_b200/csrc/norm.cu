@@ -1243,8 +1243,9 @@ template <typename T> static deamoe_status_t codes_t(const NormArgs& A, cudaStre
     return ran();
   };
   static std::atomic<uint64_t> done[5];
-  // Sums of rows of 4097 to 7168 bf16 values: twice the threads with half the columns (two blocks of them fit an SM, and one reduction more a
-  // warp is little beside a long row: 8192 x 7168 bf16 75 us, 80 with four packs a thread, before the reduction got shorter).
+  // Sums of rows of 513 to 896 packs: twice the threads with half the columns, two blocks an SM (448 threads are what two of them can have
+  // registers for).  With this and with four packs a thread, us: bf16 14115 x 4160 79 and 86, 11468 x 5120 77 and 76, 8340 x 7040 73 and 81,
+  // 8192 x 7168 72 and 80, with a gate of its own 84 and 95; fp32 14115 x 2080 72 and 70, 11468 x 2560 65 and 68, 8192 x 3584 69 and 68.
   if (nin > 1 && packs > 512 && packs <= 896)
     return nin == 3 ? run(k_codes_feed<T, VE, 2, 448, true, true>, done[0], 2, 896) : run(k_codes_feed<T, VE, 2, 448, true, false>, done[1], 2, 896);
   return nin == 3 ? run(k_codes_feed<T, VE, NV, CODES_THREADS, true, true>, done[2], NV, CODES_THREADS)
